@@ -44,6 +44,7 @@ enum {
 };
 
 enum { IRIS_F16 = 0, IRIS_BF16 = 1 }; /* element type of A, B, C, bias (accumulation is fp32) */
+enum { IRIS_F32 = 2 };                /* a third element type of logits (see "Operators on logits") */
 
 /* The three schedules of Section 4 ("Building Complex Multi-GPU Patterns"). */
 enum {
@@ -467,6 +468,99 @@ int iris_gemm_takeover_stats(const iris_heap* heap, int32_t out[2]);
 int iris_gemm_all_scatter_noalloc(const void* A, const void* const* B_shards, const uint64_t* slot_bases,
                                   size_t bytes_per_rank, int M, int N, int K, int world, int dtype, uint64_t c_off,
                                   uint64_t flag_off, int32_t epoch, void* stream);
+
+/* ------------------------------------------------------------------------------------------ */
+/* Operators on logits                                                                         */
+/* ------------------------------------------------------------------------------------------ */
+
+/* With the B shards = a model's output embedding, cut by columns over the ranks, gemm_all_scatter leaves the
+ * logits C[M, N] of M positions in every slot (address iris_heap_base(heap, rank) + c_off, row stride N).  These
+ * calls do what comes next with them; they take any device pointer and need no heap handle and no workspace.
+ *
+ * Common arguments:
+ *   logits      row r starts at logits + r * row_stride elements, `vocab` elements each, of type `dtype` (IRIS_F16,
+ *               IRIS_BF16 or IRIS_F32).  row_stride in elements, >= vocab; 0 = vocab.  Rows may start at any element
+ *               (16-bit logits at any even address); 16-byte aligned rows are the fast case.  Nothing outside a row is
+ *               read or written.  rows < 2^31, vocab <= 2^30 (IRIS_ERR_UNSUPPORTED beyond that).
+ *   scale       > 0: the softmax is taken of scale * z (1 / temperature).
+ *   targets, teacher_ids, top_ids   int64 column indices.
+ * Statistics, probabilities and sums are fp32.  -inf logits are masked tokens (probability 0); a mask of the type's
+ * lowest finite value is an ordinary value, also where a row holds nothing else.  A row with no finite logit has log
+ * probabilities -inf, entropy 0, statistics -inf, a loss of +inf where its teacher asks for anything, and gradient 0.
+ * A row that holds +inf or NaN gives NaN; other rows do not notice.
+ * Errors: IRIS_ERR_ARG for what the comments below exclude, before anything is launched. */
+
+/* Log probabilities of given tokens, entropy, and the largest alternatives. */
+typedef struct iris_logprob_args {
+  const void* logits;
+  int64_t rows, vocab, row_stride;
+  int dtype;
+  float scale;
+  const int64_t* targets; /* [rows, n_targets]; an index outside [0, vocab) means no token: log probability 0          */
+  int n_targets;          /* 0 .. 128 tokens of each row                                                              */
+  int top_k;              /* 0 .. 128 and <= vocab                                                                    */
+  float* logprob;         /* [rows, n_targets]; needed when n_targets > 0                                             */
+  float* entropy;         /* [rows]: -sum q ln q; NULL = not wanted                                                   */
+  float* stats;           /* [rows, 2]: max z, ln sum exp(scale (z - max z)): what the backward call needs; may be NULL */
+  int64_t* top_ids;       /* [rows, top_k]: the largest logits' columns in falling order, the lower column first among
+                             equal logits, NaN before all; needed when top_k > 0                                      */
+  float* top_logprob;     /* [rows, top_k]: their log probabilities; may be NULL                                      */
+} iris_logprob_args;
+int iris_token_logprobs(const iris_logprob_args* args, void* stream);
+
+/* Gradient for the logits:  dz_j = scale [ sum_q g_q ([t_q = j] - p_j) - g_H p_j (ln p_j + H) ].
+ * dlogits has the logits' type and may be the logits themselves (same address and stride); it must not overlap them
+ * otherwise.  Targets and scale are those of the forward call; a target that comes twice counts twice. */
+typedef struct iris_logprob_grad_args {
+  const void* logits;
+  int64_t rows, vocab, row_stride;
+  int dtype;
+  float scale;
+  const int64_t* targets;
+  int n_targets;
+  const float* stats;        /* [rows, 2] of the forward call                                */
+  const float* grad_logprob; /* [rows, n_targets]; NULL = 0                                  */
+  const float* entropy;      /* [rows] of the forward call; needed with grad_entropy         */
+  const float* grad_entropy; /* [rows]; NULL = 0                                             */
+  void* dlogits;
+  int64_t grad_stride;       /* elements between rows of dlogits; 0 = vocab                  */
+} iris_logprob_grad_args;
+int iris_token_logprobs_backward(const iris_logprob_grad_args* args, void* stream);
+
+/* Distillation from a teacher's top logits.  Row r's teacher lists list_k tokens: columns teacher_ids[r, k] and values
+ * teacher[r, k]; an id outside [0, vocab) is an absent entry.  The ids of a row are distinct (where one comes twice,
+ * each entry counts as its own term of the sums below).  q = softmax(scale * z) over the whole row.
+ *   IRIS_DISTILL_RENORM  p = softmax(teacher_scale * value) over the list;   loss = sum p_k (ln p_k - ln q_k)
+ *   IRIS_DISTILL_TAIL    values are log probabilities over the whole vocabulary, p_k = exp(value), and what is left,
+ *                        p_r = max(0, 1 - sum p_k), is one more token, compared with the student's probability of all
+ *                        tokens off the list:                 loss = sum p_k (ln p_k - ln q_k) + p_r (ln p_r - ln q_r)
+ *                        (teacher_scale is not used; p_r < 1e-5 is dropped where no token off the list has mass)
+ * Terms with p = 0 are 0; p > 0 against q = 0 gives a loss of +inf and a finite gradient. */
+enum { IRIS_DISTILL_RENORM = 0, IRIS_DISTILL_TAIL = 1 };
+typedef struct iris_distill_args {
+  const void* logits;
+  int64_t rows, vocab, row_stride;
+  int dtype;
+  float scale;
+  const float* teacher;       /* [rows, list_k]                                                                       */
+  const int64_t* teacher_ids; /* [rows, list_k]                                                                       */
+  int list_k;                 /* 0 .. 128                                                                             */
+  int mode;
+  float teacher_scale;        /* > 0                                                                                  */
+  const float* weight;        /* [rows]: what multiplies row r's gradient; NULL = 1.  A row of weight 0 gets gradient 0
+                                 whatever its logits are                                                              */
+  float* loss;                /* [rows], not multiplied by weight                                                     */
+  float* stats;               /* [rows, 3]: max z, ln sum exp(scale (z - max z)), the same sum over the tokens off the
+                                 list (0 in RENORM)                                                                   */
+  void* dlogits;              /* weight * dloss/dz, type and rules as above; NULL = loss only                         */
+  int64_t grad_stride;
+} iris_distill_args;
+/* Loss and, where dlogits is given, its gradient in the same pass over the logits (weight is known beforehand, as 1 /
+ * number of tokens is).  stats may be NULL. */
+int iris_distill_topk(const iris_distill_args* args, void* stream);
+/* The gradient alone, from the forward call's stats (an input here): weight = the gradient of loss, needed; loss is not
+ * used. */
+int iris_distill_topk_backward(const iris_distill_args* args, void* stream);
 
 #ifdef __cplusplus
 }

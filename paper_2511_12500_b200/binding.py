@@ -13,6 +13,9 @@ IRIS_ERR_ARG, IRIS_ERR_RANGE, IRIS_ERR_NOMEM, IRIS_ERR_CUDA = -1, -2, -3, -4
 IRIS_ERR_UNSUPPORTED, IRIS_ERR_TIMEOUT, IRIS_ERR_STATE = -5, -6, -7
 IRIS_F16, IRIS_BF16 = 0, 1
 DTYPES = {"fp16": IRIS_F16, "bf16": IRIS_BF16}
+IRIS_F32 = 2
+LOGIT_DTYPES = {"fp16": IRIS_F16, "bf16": IRIS_BF16, "fp32": IRIS_F32}   # operators on logits
+IRIS_DISTILL_RENORM, IRIS_DISTILL_TAIL = 0, 1
 IRIS_MODE_BULK_SYNCHRONOUS, IRIS_MODE_FUSED_SEQUENTIAL, IRIS_MODE_WORKGROUP_SPECIALIZED = 0, 1, 2
 MODES = {"bulk_synchronous": 0, "fused_sequential": 1, "workgroup_specialized": 2}
 IRIS_SEM_RELAXED, IRIS_SEM_ACQUIRE, IRIS_SEM_RELEASE, IRIS_SEM_ACQ_REL = 0, 1, 2, 3
@@ -35,6 +38,7 @@ EXPORTS = [
     "iris_consume_bias", "iris_consume_bias_ranks", "iris_gemm_all_scatter_host", "iris_gemm_out_offset", "iris_gemm_takeover_stats",
     "iris_gemm_all_scatter_noalloc", "iris_heap_create_from_bases", "iris_heap_local_rank", "iris_ipc_alloc", "iris_ipc_free", "iris_ipc_export",
     "iris_ipc_open", "iris_ipc_close", "iris_atomic_add_u64", "iris_atomic_cas_u64", "iris_copy_tile", "iris_load_tile", "iris_store_tile", "iris_atomic_rmw",
+    "iris_token_logprobs", "iris_token_logprobs_backward", "iris_distill_topk", "iris_distill_topk_backward",
 ]
 
 
@@ -52,6 +56,30 @@ class GemmArgs(C.Structure):
         ("epoch", C.c_int32), ("comm_ctas", C.c_int), ("max_ctas", C.c_int), ("raster_group", C.c_int),
         ("block_n", C.c_int), ("spin_timeout_ns", C.c_uint64), ("cta_pair", C.c_int), ("static_schedule", C.c_int), ("stream_k", C.c_int), ("wg_tail", C.c_int), ("rank_first", C.c_int), ("rank_count", C.c_int), ("pace_stores", C.c_int),
         ("consumer_bias", C.c_void_p), ("consumer_out_off", C.c_uint64), ("b_layout", C.c_int), ("fuse_tail", C.c_int), ("stage_k", C.c_int),
+    ]
+
+
+_LOGITS = [("logits", C.c_void_p), ("rows", C.c_int64), ("vocab", C.c_int64), ("row_stride", C.c_int64), ("dtype", C.c_int), ("scale", C.c_float)]
+
+
+class LogprobArgs(C.Structure):
+    _fields_ = _LOGITS + [
+        ("targets", C.c_void_p), ("n_targets", C.c_int), ("top_k", C.c_int), ("logprob", C.c_void_p), ("entropy", C.c_void_p),
+        ("stats", C.c_void_p), ("top_ids", C.c_void_p), ("top_logprob", C.c_void_p),
+    ]
+
+
+class LogprobGradArgs(C.Structure):
+    _fields_ = _LOGITS + [
+        ("targets", C.c_void_p), ("n_targets", C.c_int), ("stats", C.c_void_p), ("grad_logprob", C.c_void_p), ("entropy", C.c_void_p),
+        ("grad_entropy", C.c_void_p), ("dlogits", C.c_void_p), ("grad_stride", C.c_int64),
+    ]
+
+
+class DistillArgs(C.Structure):
+    _fields_ = _LOGITS + [
+        ("teacher", C.c_void_p), ("teacher_ids", C.c_void_p), ("list_k", C.c_int), ("mode", C.c_int), ("teacher_scale", C.c_float),
+        ("weight", C.c_void_p), ("loss", C.c_void_p), ("stats", C.c_void_p), ("dlogits", C.c_void_p), ("grad_stride", C.c_int64),
     ]
 
 
@@ -120,6 +148,10 @@ def lib() -> C.CDLL:
     L.iris_gemm_out_offset.restype = u64
     L.iris_gemm_out_offset.argtypes = [ci, ci, ci]
     L.iris_gemm_all_scatter_noalloc.argtypes = [vp, C.POINTER(vp), C.POINTER(u64), sz, ci, ci, ci, ci, ci, u64, u64, i32, vp]
+    L.iris_token_logprobs.argtypes = [C.POINTER(LogprobArgs), vp]
+    L.iris_token_logprobs_backward.argtypes = [C.POINTER(LogprobGradArgs), vp]
+    for f in (L.iris_distill_topk, L.iris_distill_topk_backward):
+        f.argtypes = [C.POINTER(DistillArgs), vp]
     _lib = L
     return L
 
@@ -402,3 +434,36 @@ def iris_gemm_all_scatter_noalloc(A, B_shards, slot_bases, bytes_per_rank, M, N,
     bases = (C.c_uint64 * len(slot_bases))(*slot_bases)
     _ck(lib().iris_gemm_all_scatter_noalloc(_ptr(A), C.cast(arr, C.POINTER(C.c_void_p)), bases, bytes_per_rank, M, N, K, world, dtype,
                                             c_off, flag_off, epoch, _stream(stream)))
+
+
+# ------------------------------------------------------------------------------------- operators on logits
+# Shapes, types and rules are the header's.  Tensors other than logits and dlogits are contiguous, ids are int64, the
+# rest fp32; row_stride and grad_stride are in elements (0 = vocab).
+def iris_token_logprobs(logits, rows, vocab, dtype, targets=None, n_targets=0, logprob=None, entropy=None, stats=None, top_k=0, top_ids=None,
+                        top_logprob=None, scale=1.0, row_stride=0, stream=None):
+    a = LogprobArgs(_ptr(logits), rows, vocab, row_stride, dtype, scale, _ptr(targets), n_targets, top_k, _ptr(logprob), _ptr(entropy), _ptr(stats),
+                    _ptr(top_ids), _ptr(top_logprob))
+    _ck(lib().iris_token_logprobs(C.byref(a), _stream(stream)))
+
+
+def iris_token_logprobs_backward(logits, rows, vocab, dtype, targets, n_targets, stats, grad_logprob, dlogits, entropy=None, grad_entropy=None,
+                                 scale=1.0, row_stride=0, grad_stride=0, stream=None):
+    a = LogprobGradArgs(_ptr(logits), rows, vocab, row_stride, dtype, scale, _ptr(targets), n_targets, _ptr(stats), _ptr(grad_logprob),
+                        _ptr(entropy), _ptr(grad_entropy), _ptr(dlogits), grad_stride)
+    _ck(lib().iris_token_logprobs_backward(C.byref(a), _stream(stream)))
+
+
+def iris_distill_topk(logits, rows, vocab, dtype, teacher, teacher_ids, list_k, loss, mode=IRIS_DISTILL_RENORM, stats=None, weight=None, dlogits=None,
+                      scale=1.0, teacher_scale=1.0, row_stride=0, grad_stride=0, stream=None):
+    """Loss per row and, with `dlogits`, weight * its gradient, in one pass over the logits."""
+    a = DistillArgs(_ptr(logits), rows, vocab, row_stride, dtype, scale, _ptr(teacher), _ptr(teacher_ids), list_k, mode, teacher_scale, _ptr(weight),
+                    _ptr(loss), _ptr(stats), _ptr(dlogits), grad_stride)
+    _ck(lib().iris_distill_topk(C.byref(a), _stream(stream)))
+
+
+def iris_distill_topk_backward(logits, rows, vocab, dtype, teacher, teacher_ids, list_k, stats, grad_loss, dlogits, mode=IRIS_DISTILL_RENORM,
+                               scale=1.0, teacher_scale=1.0, row_stride=0, grad_stride=0, stream=None):
+    """grad_loss * the gradient, from the statistics that iris_distill_topk left."""
+    a = DistillArgs(_ptr(logits), rows, vocab, row_stride, dtype, scale, _ptr(teacher), _ptr(teacher_ids), list_k, mode, teacher_scale,
+                    _ptr(grad_loss), None, _ptr(stats), _ptr(dlogits), grad_stride)
+    _ck(lib().iris_distill_topk_backward(C.byref(a), _stream(stream)))

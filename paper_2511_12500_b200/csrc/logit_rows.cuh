@@ -1,0 +1,248 @@
+// What the operators on rows of logits share: element types, 16-byte pieces of a row that may start at any element,
+// the running softmax statistics and their reductions, and the argument checks.
+//
+// A row of `vocab` elements starts at any multiple of the element size.  Its memory is seen as 16-byte granules: with
+// `ph` = the row's first element's place in its granule, granule v holds columns v*VE - ph ... v*VE - ph + VE - 1.
+// Granules that lie inside the row are moved with one 16-byte access, the first and the last one, where the row covers
+// them in part, element by element: nothing outside the row is read or written.
+#pragma once
+
+#include <cfloat>
+#include <cmath>
+
+#include "iris_device.cuh"
+
+namespace iris {
+namespace rows {
+
+constexpr int kMaxList = 128;               // targets, alternatives or teacher's tokens of one row
+constexpr int64_t kMaxVocab = 1 << 30;      // columns are counted in 32 bits inside a row
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kFloor = -1024.f;           // exponents (base 2) are cut here: 2^-1024 is 0 in 32 bits, and 0 * -1024 is not NaN
+
+template <int DT> struct Elem;
+template <> struct Elem<IRIS_F16> {
+  using T = __half;
+  static constexpr int VE = 8;
+  static __device__ __forceinline__ float to(T x) { return __half2float(x); }
+  static __device__ __forceinline__ T from(float x) { return __float2half_rn(x); }
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <> struct Elem<IRIS_BF16> {
+  using T = __nv_bfloat16;
+  static constexpr int VE = 8;
+  static __device__ __forceinline__ float to(T x) { return __bfloat162float(x); }
+  static __device__ __forceinline__ T from(float x) { return __float2bfloat16_rn(x); }
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <> struct Elem<IRIS_F32> {
+  using T = float;
+  static constexpr int VE = 4;
+  static __device__ __forceinline__ float to(T x) { return x; }
+  static __device__ __forceinline__ T from(float x) { return x; }
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
+    x[0] = __uint_as_float(v.x);
+    x[1] = __uint_as_float(v.y);
+    x[2] = __uint_as_float(v.z);
+    x[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// The larger of two, NaN if either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
+// A row of the logits (or of the gradient) as granules.
+template <int DT>
+struct Row {
+  using E = Elem<DT>;
+  using T = typename E::T;
+  static constexpr int VE = E::VE;
+  T* granule0;   // 16-byte aligned; the row's element 0 is granule0[ph]
+  int ph, end;   // elements ph .. end - 1 counted from granule0 belong to the row
+  __device__ __forceinline__ Row(const void* base, int64_t row, int64_t stride, int vocab) {
+    T* p = static_cast<T*>(const_cast<void*>(base)) + row * stride;
+    ph = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+    granule0 = p - ph;
+    end = ph + vocab;
+  }
+  __device__ __forceinline__ int granules() const { return (end + VE - 1) / VE; }
+  __device__ __forceinline__ bool whole(int v) const { return v * VE >= ph && (v + 1) * VE <= end; }
+  __device__ __forceinline__ T* at(int v) const { return granule0 + (int64_t)v * VE; }
+  __device__ __forceinline__ T& column(int j) const { return granule0[ph + (int64_t)j]; }
+  // The granule's values; -inf in the places that do not belong to the row.
+  __device__ __forceinline__ void load(int v, float (&x)[VE]) const {
+    if (whole(v)) {
+      E::unpack(ld_global_v4(at(v)), x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        const int i = v * VE + e;
+        x[e] = i >= ph && i < end ? E::to(granule0[i]) : -INFINITY;
+      }
+    }
+  }
+};
+
+// Running statistics of a set of logits: m >= every one of them (and >= -FLT_MAX, so that z - m is never inf - inf for
+// a masked z), s = sum 2^y, t = sum y 2^y with y = max((z - m) k, kFloor), k = scale log2(e).
+struct Acc {
+  float m = -FLT_MAX, s = 0.f, t = 0.f;
+  __device__ __forceinline__ void rebase(float mx, float k) {   // to a larger m
+    const float d = max_nan((m - mx) * k, kFloor), f = ex2(d);
+    t = (t + s * d) * f;
+    s *= f;
+    m = mx;
+  }
+  __device__ __forceinline__ void merge(const Acc& o, float k) {
+    Acc b = o;
+    const float mx = max_nan(m, o.m);
+    rebase(mx, k);
+    b.rebase(mx, k);
+    s += b.s;
+    t += b.t;
+  }
+  template <int N>
+  __device__ __forceinline__ void add(const float (&x)[N], float k) {
+    float mx = x[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) mx = max_nan(mx, x[e]);
+    if (!(mx <= m)) rebase(max_nan(m, mx), k);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float y = max_nan((x[e] - m) * k, kFloor), f = ex2(y);
+      s += f;
+      t = fmaf(f, y, t);
+    }
+  }
+};
+
+__device__ __forceinline__ Acc warp_merge(Acc a, float k) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    Acc b;
+    b.m = __shfl_xor_sync(~0u, a.m, o);
+    b.s = __shfl_xor_sync(~0u, a.s, o);
+    b.t = __shfl_xor_sync(~0u, a.t, o);
+    a.merge(b, k);
+  }
+  return a;
+}
+// All threads of the block get the merged statistics.  `buf`: 32 entries of shared memory, free for others after the
+// next barrier.
+__device__ __forceinline__ Acc block_merge(Acc a, float k, Acc* buf) {
+  a = warp_merge(a, k);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = a;
+  __syncthreads();
+  Acc r = (threadIdx.x & 31) < blockDim.x / 32 ? buf[threadIdx.x & 31] : Acc{};
+  return warp_merge(r, k);
+}
+
+// ln sum exp(scale (z - m)): -inf where no logit is left.
+__device__ __forceinline__ float log_sum(const Acc& a) { return a.s > 0.f ? logf(a.s) : a.s == 0.f ? -INFINITY : NAN; }
+
+// A larger logit, and among equal ones the lower column, has the larger key.  NaN comes above +inf.
+__device__ __forceinline__ uint32_t order_bits(float x) {
+  if (x != x) return 0xffffffffu;
+  const uint32_t b = __float_as_uint(x + 0.f);   // -0 counts as +0
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ uint64_t order_key(float x, int column) { return (uint64_t)order_bits(x) << 32 | (0xffffffffu - (uint32_t)column); }
+__device__ __forceinline__ int key_column(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
+__device__ __forceinline__ float key_value(uint64_t key) {
+  const uint32_t b = (uint32_t)(key >> 32);
+  return b == 0xffffffffu ? NAN : __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
+}
+
+// ---- host side -----------------------------------------------------------------------------------------------------
+inline size_t elem_size(int dtype) { return dtype == IRIS_F32 ? 4 : 2; }
+
+// Checks shared by all calls; `stride` comes back as the elements between rows.
+inline int check_logits(const char* fn, const char* what, const void* p, int dtype, int64_t rows, int64_t vocab, int64_t* stride) {
+  if (dtype != IRIS_F16 && dtype != IRIS_BF16 && dtype != IRIS_F32) return fail(IRIS_ERR_ARG, "%s: unknown dtype %d", fn, dtype);
+  if (rows < 0 || vocab < 0) return fail(IRIS_ERR_ARG, "%s: rows=%lld, vocab=%lld", fn, (long long)rows, (long long)vocab);
+  if (vocab > kMaxVocab || rows > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "%s: at most 2^31 - 1 rows of 2^30 columns", fn);
+  if (*stride == 0) *stride = vocab;
+  if (*stride < vocab) return fail(IRIS_ERR_ARG, "%s: %s: row stride %lld is less than vocab %lld", fn, what, (long long)*stride, (long long)vocab);
+  if (rows > 1 && *stride > INT64_MAX / 8 / rows) return fail(IRIS_ERR_ARG, "%s: %s: row stride %lld is too large", fn, what, (long long)*stride);
+  if (rows == 0 || vocab == 0) return IRIS_OK;
+  if (!p) return fail(IRIS_ERR_ARG, "%s: %s is NULL", fn, what);
+  if (reinterpret_cast<uintptr_t>(p) % elem_size(dtype)) return fail(IRIS_ERR_ARG, "%s: %s is not aligned to its elements", fn, what);
+  return IRIS_OK;
+}
+inline int check_scale(const char* fn, const char* what, float s) {
+  if (!(s > 0.f) || std::isinf(s)) return fail(IRIS_ERR_ARG, "%s: %s has to be positive and finite", fn, what);
+  return IRIS_OK;
+}
+inline int check_aligned(const char* fn, const char* what, const void* p, size_t a, bool needed) {
+  if (needed && !p) return fail(IRIS_ERR_ARG, "%s: %s is NULL", fn, what);
+  if (reinterpret_cast<uintptr_t>(p) % a) return fail(IRIS_ERR_ARG, "%s: %s is not %zu-byte aligned", fn, what, a);
+  return IRIS_OK;
+}
+// The gradient may be the logits themselves (same address and stride) or share no element with them.
+inline int check_in_place(const char* fn, const void* logits, int64_t stride, const void* grad, int64_t gstride, int64_t rows, int64_t vocab, int dtype) {
+  if (rows == 0 || vocab == 0) return IRIS_OK;
+  const size_t es = elem_size(dtype);
+  const uint64_t a = reinterpret_cast<uint64_t>(logits), b = reinterpret_cast<uint64_t>(grad);
+  if (a == b && (stride == gstride || rows == 1)) return IRIS_OK;
+  const uint64_t row = vocab * es, ea = a + (uint64_t)(rows - 1) * stride * es + row, eb = b + (uint64_t)(rows - 1) * gstride * es + row;
+  if (ea <= b || eb <= a) return IRIS_OK;
+  if (stride == gstride && rows > 1) {   // two column ranges of one matrix
+    const uint64_t s = stride * es, d = (a < b ? b - a : a - b) % s;
+    if (d >= row && s - d >= row) return IRIS_OK;
+  }
+  return fail(IRIS_ERR_ARG, "%s: dlogits overlaps logits and is not the same matrix", fn);
+}
+#define IRIS_CHECK(expr)              \
+  do {                                \
+    if (int rc_ = (expr)) return rc_; \
+  } while (0)
+
+}  // namespace rows
+}  // namespace iris
