@@ -10,7 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "lib", "libiris_b200.so")
 SOURCES = ["heap.cu", "tile_ops.cu", "gemm_all_scatter.cu", "consumer.cu", "token_logprobs.cu", "distill.cu"]
-HEADERS = ["iris_internal.h", "iris_device.cuh", "sm100_ptx.cuh", "logit_rows.cuh", "logit_grad.cuh"]
+HEADERS = ["iris_internal.h", "iris_device.cuh", "sm100_ptx.cuh", "logit_rows.cuh", "logit_grad.cuh", "top_list.cuh"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-O3", "-lineinfo", "-Xcompiler", "-fPIC",
               "-Xptxas", "-v", "--expt-relaxed-constexpr"]
 

@@ -17,14 +17,68 @@ namespace rows {
 
 constexpr int kMaxList = 128;               // targets, alternatives or teacher's tokens of one row
 constexpr int64_t kMaxVocab = 1 << 30;      // columns are counted in 32 bits inside a row
+constexpr int kSms = 148;                    // of a B200
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFloor = -1024.f;           // exponents (base 2) are cut here: 2^-1024 is 0 in 32 bits, and 0 * -1024 is not NaN
 
-template <int DT> struct Elem;
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Two 32-bit floats at once (one instruction on sm_100a).
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2f(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2f(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2f(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+// 16 bytes that are read once: not kept in L1.
+__device__ __forceinline__ uint4 ld_once(const void* p) {
+  uint4 v;
+  asm("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+// The larger of two, NaN if either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
+template <int DT> struct Elem;   // largest(): of a granule's values, NaN if one is; kMasked: 32 bits of -inf
 template <> struct Elem<IRIS_F16> {
   using T = __half;
   static constexpr int VE = 8;
+  static constexpr uint32_t kMasked = 0xfc00fc00u;
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    uint32_t a, b, m;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&m));
+    return max_nan(f.x, f.y);
+  }
   static __device__ __forceinline__ float to(T x) { return __half2float(x); }
   static __device__ __forceinline__ T from(float x) { return __float2half_rn(x); }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
@@ -49,6 +103,14 @@ template <> struct Elem<IRIS_F16> {
 template <> struct Elem<IRIS_BF16> {
   using T = __nv_bfloat16;
   static constexpr int VE = 8;
+  static constexpr uint32_t kMasked = 0xff80ff80u;
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    uint32_t a, b, m;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  }
   static __device__ __forceinline__ float to(T x) { return __bfloat162float(x); }
   static __device__ __forceinline__ T from(float x) { return __float2bfloat16_rn(x); }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
@@ -72,6 +134,10 @@ template <> struct Elem<IRIS_BF16> {
 template <> struct Elem<IRIS_F32> {
   using T = float;
   static constexpr int VE = 4;
+  static constexpr uint32_t kMasked = 0xff800000u;
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)), max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
   static __device__ __forceinline__ float to(T x) { return x; }
   static __device__ __forceinline__ T from(float x) { return x; }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
@@ -84,18 +150,6 @@ template <> struct Elem<IRIS_F32> {
     return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
   }
 };
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// The larger of two, NaN if either is.
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
-}
 
 // A row of the logits (or of the gradient) as granules.
 template <int DT>
@@ -115,7 +169,14 @@ struct Row {
   __device__ __forceinline__ bool whole(int v) const { return v * VE >= ph && (v + 1) * VE <= end; }
   __device__ __forceinline__ T* at(int v) const { return granule0 + (int64_t)v * VE; }
   __device__ __forceinline__ T& column(int j) const { return granule0[ph + (int64_t)j]; }
-  // The granule's values; -inf in the places that do not belong to the row.
+  // The granule's bits; -inf in the places that do not belong to the row.
+  __device__ __forceinline__ uint4 raw(int v) const {
+    if (whole(v)) return ld_once(at(v));
+    float x[VE];
+    load(v, x);
+    return E::pack(x);
+  }
+  // The granule's values, likewise.
   __device__ __forceinline__ void load(int v, float (&x)[VE]) const {
     if (whole(v)) {
       E::unpack(ld_global_v4(at(v)), x);
@@ -135,8 +196,8 @@ struct Acc {
   float m = -FLT_MAX, s = 0.f, t = 0.f;
   __device__ __forceinline__ void rebase(float mx, float k) {   // to a larger m
     const float d = max_nan((m - mx) * k, kFloor), f = ex2(d);
-    t = (t + s * d) * f;
-    s *= f;
+    t = __fmul_rn(fmaf(s, d, t), f);
+    s = __fmul_rn(s, f);
     m = mx;
   }
   __device__ __forceinline__ void merge(const Acc& o, float k) {
@@ -144,8 +205,8 @@ struct Acc {
     const float mx = max_nan(m, o.m);
     rebase(mx, k);
     b.rebase(mx, k);
-    s += b.s;
-    t += b.t;
+    s = __fadd_rn(s, b.s);   // products rounded before they are added: a.merge(b) and b.merge(a) give the same bits,
+    t = __fadd_rn(t, b.t);   // and so all threads of a butterfly
   }
   template <int N>
   __device__ __forceinline__ void add(const float (&x)[N], float k) {
@@ -158,6 +219,45 @@ struct Acc {
       const float y = max_nan((x[e] - m) * k, kFloor), f = ex2(y);
       s += f;
       t = fmaf(f, y, t);
+    }
+  }
+};
+
+// Adds granules to a thread's statistics.  All of them count from one m, which the caller raises first (raise()); two
+// elements at a time: per element about 1 instruction to unpack, 1/2 each to subtract, scale and add, 1 exponential,
+// and 1 1/2 for the entropy's sum.
+template <int DT, bool ENTROPY>
+struct Sums {
+  Acc a;
+  uint64_t s2 = 0, t2 = 0;   // the two halves' sums since the last raise
+  __device__ __forceinline__ void flush() {
+    const float2 s = unpair(s2);
+    a.s += s.x + s.y;
+    s2 = 0;
+    if (ENTROPY) {
+      const float2 t = unpair(t2);
+      a.t += t.x + t.y;
+      t2 = 0;
+    }
+  }
+  __device__ __forceinline__ void raise(float mx, float k) {
+    flush();
+    if (!(mx <= a.m)) a.rebase(max_nan(a.m, mx), k);
+  }
+  __device__ __forceinline__ void add(const uint4& v, uint64_t minus_m, uint64_t k2) {
+    constexpr int VE = Elem<DT>::VE;
+    float x[VE];
+    Elem<DT>::unpack(v, x);
+#pragma unroll
+    for (int e = 0; e < VE; e += 2) {
+      float2 y = unpair(mul2f(add2f(pair(x[e], x[e + 1]), minus_m), k2));
+      if (ENTROPY) {
+        y.x = max_nan(y.x, kFloor);
+        y.y = max_nan(y.y, kFloor);
+      }
+      const uint64_t f = pair(ex2(y.x), ex2(y.y));
+      s2 = add2f(s2, f);
+      if (ENTROPY) t2 = fma2f(f, pair(y.x, y.y), t2);
     }
   }
 };

@@ -2,17 +2,23 @@
 //
 //   m = max z,  y_j = scale (z_j - m),  s = sum exp y_j;  log probability of t: y_t - ln s;
 //   entropy: ln s - (sum y_j exp y_j) / s.
+#include <type_traits>
+
 #include "logit_grad.cuh"
+#include "top_list.cuh"
 
 namespace iris {
 namespace rows {
 
 constexpr int kScoreThreads = 256;
+constexpr int kScoreGranules = 8;       // of 16 bytes a thread holds at once
+constexpr int kMaxSplit = 8;            // blocks (one cluster) that share a row
+static_assert(kScoreThreads == kTopThreads, "the list is kept by all threads of the block");
 
 struct ScoreParams {
   const void* logits;
   int64_t stride;
-  int vocab, n_targets, top_k;
+  int vocab, n_targets, top_k, split;
   float scale;
   const int64_t* targets;
   float *logprob, *entropy, *stats, *top_logprob;
@@ -23,63 +29,150 @@ __device__ __forceinline__ float log_prob(float z, float m, float ls, float scal
   return ls == -INFINITY ? -INFINITY : (z - m) * scale - ls;
 }
 
-template <int DT>
+struct NoTop {};
+
+// One cluster of `split` blocks a row; each takes an equal run of granules and the first one joins what they found.
+template <int DT, bool ENTROPY, bool TOP>
 __global__ void __launch_bounds__(kScoreThreads) score_kernel(const ScoreParams p) {
-  constexpr int VE = Row<DT>::VE;
+  using E = Elem<DT>;
+  constexpr int T = kScoreThreads, U = kScoreGranules;
   __shared__ Acc buf[32];
-  __shared__ uint64_t kbuf[32];
-  const int64_t r = blockIdx.x;
+  __shared__ Acc parts[kMaxSplit];
+  __shared__ typename std::conditional<TOP, TopShared, NoTop>::type top;
+  extern __shared__ uint64_t lists[];   // TOP and split > 1: the blocks' sorted lists, top_k keys each, 0 where one is shorter
+  const int split = p.split, part = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x;
+  const int64_t r = blockIdx.x / split;
+  if (split > 1) ptx::cluster_arrive_relaxed();
   const Row<DT> row(p.logits, r, p.stride, p.vocab);
-  const int nv = row.granules(), tid = threadIdx.x;
+  const int nv = row.granules(), each = (nv + split - 1) / split;
+  const int v0 = min(nv, part * each), v1 = min(nv, v0 + each);
   const float k = p.scale * kLog2e;
-  Acc a;
-  for (int v = tid; v < nv; v += kScoreThreads) {
-    float x[VE];
-    row.load(v, x);
-    a.add(x, k);
+  const uint64_t k2 = pair(k, k);
+  float zt = 0.f;
+  bool there = false;
+  if (part == 0 && tid < p.n_targets) {
+    const int64_t t = p.targets[r * p.n_targets + tid];
+    there = t >= 0 && t < p.vocab;
+    if (there) zt = E::to(row.column((int)t));
   }
-  a = block_merge(a, k, buf);
+  float seen = -INFINITY;
+  if constexpr (TOP) {
+    if (tid == 0) top.n = top.n_kept = 0, top.tau = 0;
+    top.code[tid] = 0;
+  }
+  Sums<DT, ENTROPY> sums;
+  for (int base = v0; base < v1; base += T * U) {
+    uint4 g[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int v = base + u * T + tid;
+      g[u] = make_uint4(E::kMasked, E::kMasked, E::kMasked, E::kMasked);
+      if (v < v1) g[u] = row.raw(v);
+    }
+    float mx = E::largest(g[0]);
+#pragma unroll
+    for (int u = 1; u < U; ++u)
+      if (base + u * T < v1) mx = max_nan(mx, E::largest(g[u]));
+    sums.raise(mx, k);
+    if constexpr (TOP) {
+      seen = max_nan(seen, mx);
+      if (base + tid < v1) top.code[tid] = order_bits(seen);
+      __syncthreads();
+      if (tid < 32) bisect_tau(top, p.top_k);
+    }
+    const uint64_t minus_m = pair(-sums.a.m, -sums.a.m);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (base + u * T < v1) sums.add(g[u], minus_m, k2);
+    if constexpr (TOP) {
+      __syncthreads();
+      const uint32_t tau = top.tau;
+      const float at_tau = tau ? key_value((uint64_t)tau << 32) : NAN;
+      if (tau != 0xffffffffu) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (base + u * T + tid < v1) collect<DT>(top, row, base + u * T + tid, g[u], at_tau);
+      }
+    }
+  }
+  sums.flush();
+  Acc a = block_merge(sums.a, k, buf);
+
+  if (split > 1) {
+    ptx::cluster_wait();   // the first block has started
+    if (tid == 0) {
+      const uint32_t to = ptx::mapa(ptx::smem_u32(&parts[part]), 0);
+      ptx::st_shared_cluster_u32(to, __float_as_uint(a.m));
+      ptx::st_shared_cluster_u32(to + 4, __float_as_uint(a.s));
+      ptx::st_shared_cluster_u32(to + 8, __float_as_uint(a.t));
+    }
+    if constexpr (TOP) {
+      const uint32_t to = ptx::mapa(ptx::smem_u32(lists + part * p.top_k), 0);
+      const int n = finish_top<DT>(top, row, v0, v1, p.top_k, [&](int place, uint64_t key) { ptx::st_shared_cluster_u64(to + place * 8, key); });
+      if (tid >= n && tid < p.top_k) ptx::st_shared_cluster_u64(to + tid * 8, 0);
+    }
+    ptx::cluster_sync();
+    if (part != 0) return;
+    a = parts[0];
+    for (int i = 1; i < split; ++i) a.merge(parts[i], k);
+  }
   const float ls = log_sum(a);
   if (tid == 0) {
     if (p.stats) {
       p.stats[2 * r] = ls == -INFINITY ? -INFINITY : a.m;
       p.stats[2 * r + 1] = ls;
     }
-    if (p.entropy) p.entropy[r] = a.s == 0.f ? 0.f : ls - a.t / a.s * kLn2;
+    if (ENTROPY) p.entropy[r] = a.s == 0.f ? 0.f : ls - a.t / a.s * kLn2;
   }
-  if (p.logprob && tid < p.n_targets) {
-    const int64_t t = p.targets[r * p.n_targets + tid];
-    p.logprob[r * p.n_targets + tid] = t >= 0 && t < p.vocab ? log_prob(Elem<DT>::to(row.column((int)t)), a.m, ls, p.scale) : 0.f;
-  }
-  uint64_t last = ~0ull;
-  for (int i = 0; i < p.top_k; ++i) {
-    uint64_t best = 0;
-    for (int v = tid; v < nv; v += kScoreThreads) {
-      float x[VE];
-      row.load(v, x);
-#pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        const int j = v * VE + e - row.ph;
-        if (j >= 0 && j < p.vocab) {
-          const uint64_t key = order_key(x[e], j);
-          if (key > best && key < last) best = key;
+  if (tid < p.n_targets) p.logprob[r * p.n_targets + tid] = there ? log_prob(zt, a.m, ls, p.scale) : 0.f;
+  if constexpr (TOP) {
+    const auto emit = [&](int place, uint64_t key) {
+      p.top_ids[r * p.top_k + place] = key_column(key);
+      if (p.top_logprob) p.top_logprob[r * p.top_k + place] = log_prob(key_value(key), a.m, ls, p.scale);
+    };
+    if (split == 1) {
+      finish_top<DT>(top, row, v0, v1, p.top_k, emit);
+    } else {   // a key's place is the number of larger ones in every list
+      for (int i = tid; i < split * p.top_k; i += T) {
+        const uint64_t key = lists[i];
+        if (key == 0) continue;
+        int place = 0;
+        for (int s = 0; s < split; ++s) {
+          int lo = 0, hi = p.top_k;
+          while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (lists[s * p.top_k + mid] > key) lo = mid + 1;
+            else hi = mid;
+          }
+          place += lo;
         }
+        if (place < p.top_k) emit(place, key);
       }
     }
-    for (int o = 16; o; o >>= 1) {
-      const uint64_t b = __shfl_xor_sync(~0u, best, o);
-      best = b > best ? b : best;
-    }
-    __syncthreads();
-    if ((tid & 31) == 0) kbuf[tid >> 5] = best;
-    __syncthreads();
-    for (int w = 0; w < kScoreThreads / 32; ++w) best = kbuf[w] > best ? kbuf[w] : best;
-    if (tid == 0) {
-      p.top_ids[r * p.top_k + i] = key_column(best);
-      if (p.top_logprob) p.top_logprob[r * p.top_k + i] = log_prob(key_value(best), a.m, ls, p.scale);
-    }
-    last = best;
   }
+}
+
+template <int DT, bool ENTROPY, bool TOP>
+static int launch_score(const ScoreParams& p, int64_t rows, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(rows * p.split));
+  cfg.blockDim = dim3(kScoreThreads);
+  cfg.dynamicSmemBytes = TOP && p.split > 1 ? (size_t)p.split * p.top_k * 8 : 0;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)p.split;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = p.split > 1 ? 1 : 0;
+  IRIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, score_kernel<DT, ENTROPY, TOP>, p));
+  return IRIS_OK;
+}
+
+template <int DT>
+static int launch_score(const ScoreParams& p, int64_t rows, cudaStream_t st) {
+  if (p.entropy) return p.top_k ? launch_score<DT, true, true>(p, rows, st) : launch_score<DT, true, false>(p, rows, st);
+  return p.top_k ? launch_score<DT, false, true>(p, rows, st) : launch_score<DT, false, false>(p, rows, st);
 }
 
 struct ScoreGradParams {
@@ -144,14 +237,17 @@ extern "C" int iris_token_logprobs(const iris_logprob_args* a, void* stream) {
   IRIS_CHECK(check_aligned(fn, "stats", a->stats, 4, false));
   IRIS_CHECK(check_aligned(fn, "top_ids", a->top_ids, 8, a->top_k > 0));
   IRIS_CHECK(check_aligned(fn, "top_logprob", a->top_logprob, 4, false));
-  ScoreParams p{a->logits, stride, (int)a->vocab, a->n_targets, a->top_k, a->scale, a->targets, want_lp ? a->logprob : nullptr, a->entropy, a->stats,
+  // A row is shared by a cluster of blocks while the rows alone leave SMs without work and every thread of each block
+  // still has a granule.
+  const int64_t granules = a->vocab * (int64_t)elem_size(a->dtype) / 16;
+  int split = 1;
+  while (split < kMaxSplit && a->rows * split < 2 * kSms && granules >= (int64_t)split * 2 * kScoreThreads) split *= 2;
+  ScoreParams p{a->logits, stride, (int)a->vocab, want_lp ? a->n_targets : 0, a->top_k, split, a->scale, a->targets, a->logprob, a->entropy, a->stats,
                 a->top_logprob, a->top_ids};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (a->dtype == IRIS_BF16) score_kernel<IRIS_BF16><<<(unsigned)a->rows, kScoreThreads, 0, st>>>(p);
-  else if (a->dtype == IRIS_F16) score_kernel<IRIS_F16><<<(unsigned)a->rows, kScoreThreads, 0, st>>>(p);
-  else score_kernel<IRIS_F32><<<(unsigned)a->rows, kScoreThreads, 0, st>>>(p);
-  IRIS_CUDA_TRY(cudaGetLastError());
-  return IRIS_OK;
+  if (a->dtype == IRIS_BF16) return launch_score<IRIS_BF16>(p, a->rows, st);
+  if (a->dtype == IRIS_F16) return launch_score<IRIS_F16>(p, a->rows, st);
+  return launch_score<IRIS_F32>(p, a->rows, st);
 }
 
 extern "C" int iris_token_logprobs_backward(const iris_logprob_grad_args* a, void* stream) {
