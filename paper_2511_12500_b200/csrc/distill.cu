@@ -5,19 +5,22 @@
 //   with remainder:    p_k = exp v_k, p_r = max(0, 1 - sum p_k),  L = the same + p_r (ln p_r - ln q_r), q_r = sum of q off the list
 //   dL/dz_j = scale (P q_j - p_j) in the first form; in the second scale ((P + p_r) q_j - p_j) on the list and
 //   scale ((P + p_r) q_j - p_r q_j / q_r) off it;  P = sum p_k.
+#include <algorithm>
+
 #include "logit_grad.cuh"
+#include "sm100_ptx.cuh"
 
 namespace iris {
 namespace rows {
 
 constexpr int kDistillThreads = 256;
-static_assert(kDistillThreads >= kMaxList, "one thread an entry of the list");
+constexpr int kMaxSplit = 8;   // blocks (one cluster) that share a row
+static_assert(kDistillThreads >= kMaxList && kGradThreads == kDistillThreads, "one thread an entry of the list");
 
 struct DistillParams {
   const void* logits;
   int64_t stride, grad_stride;
-  int vocab, list_k, hold;   // hold: granules of a row that fit shared memory at once
-  bool tail;
+  int vocab, list_k, split, hold;   // hold: granules of its part that a block keeps in shared memory
   float scale, teacher_scale;
   const float* teacher;
   const int64_t* ids;
@@ -26,169 +29,231 @@ struct DistillParams {
   void* dlogits;
 };
 
-// The teacher's list in shared memory: probabilities p[], columns in list.id (-1: absent).
+// The teacher's list in shared memory: probabilities p[], columns in list.id (-1: absent), their sum and the remainder p_r.
 struct Teacher {
   List list;
   float p[kMaxList];
+  float sum, rest;
 };
 
-// Fills t from the row's list; returns P and the remainder p_r.  Ends with a barrier.
-__device__ __forceinline__ float2 load_teacher(const DistillParams& p, int64_t r, Teacher& t) {
-  const int i = threadIdx.x, n = p.list_k;
-  if (i < n) {
-    const int64_t id = p.ids[r * n + i];
-    const bool there = id >= 0 && id < p.vocab;
-    t.list.id[i] = there ? (int)id : -1;
-    const float v = p.teacher[r * n + i];
-    t.p[i] = !there ? (p.tail ? 0.f : -INFINITY) : p.tail ? expf(v) : v * p.teacher_scale;
+// Fills t from the row's list, by the first warp; visible to the others after the next barrier.
+template <bool TAIL>
+__device__ __forceinline__ void load_teacher(const DistillParams& p, int64_t r, Teacher& t) {
+  if (threadIdx.x >= 32) return;
+  constexpr int N = kMaxList / 32;
+  const int lane = threadIdx.x, n = p.list_k;
+  float v[N];
+  float m = TAIL ? 0.f : -FLT_MAX;   // log probabilities are taken as they are
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int j = lane + 32 * i;
+    int id = -1;
+    v[i] = -INFINITY;
+    if (j < n) {
+      const int64_t id64 = p.ids[r * n + j];
+      if (id64 >= 0 && id64 < p.vocab) {
+        id = (int)id64;
+        v[i] = p.teacher[r * n + j] * (TAIL ? 1.f : p.teacher_scale);
+      }
+    }
+    t.list.id[j] = id;
+    if (!TAIL) m = fmaxf(m, v[i]);
   }
-  __syncthreads();
-  if (!p.tail) {
-    float m = -FLT_MAX;
-    for (int j = 0; j < n; ++j) m = fmaxf(m, t.p[j]);
-    const float e = i < n ? expf(t.p[i] - m) : 0.f;
-    __syncthreads();
-    if (i < n) t.p[i] = e;
-    __syncthreads();
-    float s = 0.f;
-    for (int j = 0; j < n; ++j) s += t.p[j];
-    __syncthreads();
-    if (i < n) t.p[i] = s == 0.f ? 0.f : e / s;   // a list with no token left asks for nothing
-    __syncthreads();
-    return make_float2(s == 0.f ? 0.f : s == s ? 1.f : NAN, 0.f);
-  }
+  if (!TAIL) m = warp_max(m);
   float s = 0.f;
-  for (int j = 0; j < n; ++j) s += t.p[j];
-  return make_float2(s, max_nan(0.f, 1.f - s));
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = 32 * i < n ? expf(v[i] - m) : 0.f;
+    s += v[i];
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+#pragma unroll
+  for (int i = 0; i < N; ++i) t.p[lane + 32 * i] = TAIL ? v[i] : s == 0.f ? 0.f : v[i] / s;   // a list with no token left asks for nothing
+  if (lane == 0) {
+    t.sum = TAIL ? s : s == 0.f ? 0.f : s == s ? 1.f : NAN;
+    t.rest = TAIL ? max_nan(0.f, 1.f - s) : 0.f;
+  }
 }
 
-// Coefficients of the gradient; also fills list.add.  Ends with a barrier.
-__device__ __forceinline__ Coef distill_coef(const DistillParams& p, Teacher& t, float2 mass, float m, float ls, float lr, float w) {
+template <bool TAIL>
+__device__ __forceinline__ Coef distill_coef(const DistillParams& p, const Teacher& t, float m, float ls, float lr, float w) {
   Coef c;
   c.k = p.scale * kLog2e;
   c.m = m;
   c.beta = 0.f;
   c.off_l = ls * kLog2e;
-  c.alpha_l = w * p.scale * (mass.x + mass.y);
-  if (p.tail) {
+  c.alpha_l = w * p.scale * (t.sum + t.rest);
+  if (TAIL) {
     const bool some = lr != -INFINITY;
     c.off = some ? lr * kLog2e : 0.f;
-    c.alpha = some ? w * p.scale * ((mass.x + mass.y) * expf(lr - ls) - mass.y) : 0.f;
+    c.alpha = some ? w * p.scale * ((t.sum + t.rest) * expf(lr - ls) - t.rest) : 0.f;
   } else {
     c.off = c.off_l;
     c.alpha = c.alpha_l;
   }
   c.zero = ls == -INFINITY || w == 0.f;
-  if ((int)threadIdx.x < p.list_k) t.list.add[threadIdx.x] = -w * p.scale * t.p[threadIdx.x];
-  __syncthreads();
   return c;
 }
 
-template <int DT>
+// What a block of the cluster found in its part: the tokens off the list (all, without remainder) and those on it.
+struct Found {
+  Acc dense, listed;
+};
+
+// Rows are read once: every block of the cluster copies its part to shared memory, the blocks exchange their sums, and
+// the gradient is computed from the copy.  A part that does not fit is taken in pieces and read again for the gradient.
+template <int DT, bool TAIL>
 __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillParams p) {
   using E = Elem<DT>;
-  constexpr int VE = E::VE;
+  constexpr int VE = E::VE, T = kDistillThreads, U = 4;
   extern __shared__ uint4 held[];
   __shared__ Teacher t;
-  __shared__ Acc buf[32];
-  __shared__ float red[32];
-  const int64_t r = blockIdx.x;
-  const int tid = threadIdx.x, n = p.list_k;
+  __shared__ Warps8 buf[2];
+  __shared__ Found found[kMaxSplit];
+  __shared__ float red[kMaxList / 32];
+  const int split = p.split, rank = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x, n = p.list_k;
+  const int64_t r = blockIdx.x / split;
+  if (split > 1) ptx::cluster_arrive_relaxed();
   const Row<DT> in(p.logits, r, p.stride, p.vocab);
-  const int nv = in.granules();
+  const Part<DT> part(in, rank, split);
   const float k = p.scale * kLog2e;
-  const float2 mass = load_teacher(p, r, t);
-  const int id = tid < n ? t.list.id[tid] : -1;
-  bool first = id >= 0;
-  for (int j = 0; j < tid && j < n && first; ++j) first = t.list.id[j] != id;
+  typename E::T* cells = reinterpret_cast<typename E::T*>(held);
 
-  Acc a, on_list;
-  float zk = -INFINITY;
-  for (int v0 = 0; v0 < nv; v0 += p.hold) {
-    const int v1 = min(nv, v0 + p.hold);
-    __syncthreads();   // the previous tile has been read
-    for (int v = v0 + tid; v < v1; v += kDistillThreads) {
-      if (in.whole(v)) {
-        held[v - v0] = ld_global_v4(in.at(v));
-      } else {
-        float x[VE];
-        in.load(v, x);
-        held[v - v0] = E::pack(x);
-      }
+  Sums<DT, false> sums(k);
+  Acc listed;
+  float zk = -INFINITY;   // the listed token's logit: of all tokens in the first block, of the part's own in the others
+  int id = -1;
+  bool first = false;     // not a repetition of an earlier entry
+  for (int b0 = 0; b0 < part.n_all || b0 == 0; b0 += p.hold) {
+    const int size = min(part.n_all - b0, p.hold);
+    if (b0 > 0) __syncthreads();   // the previous piece has been read
+    for (int i = tid; i < size; i += T) {
+      if (b0 + i < part.n_int) copy_async(&held[i], in.at(part.w0 + b0 + i));
+      else held[i] = part.raw(in, b0 + i);
     }
+    if (b0 == 0) load_teacher<TAIL>(p, r, t);
+    copy_async_wait();
     __syncthreads();
-    typename E::T* cells = reinterpret_cast<typename E::T*>(held);
-    const int at = in.ph + id - v0 * VE;
-    const bool here = id >= 0 && at >= 0 && at < (v1 - v0) * VE;
+    if (b0 == 0 && tid < n) {
+      id = t.list.id[tid];
+      if (rank == 0 && id >= 0) zk = E::to(in.column(id));
+      first = TAIL && id >= 0 && !repeated(t.list, n, tid, true);
+    }
+    bool here = id >= 0 && part.has(in.ph + id);
+    int at = 0;
+    if (here) {
+      at = (part.place((in.ph + id) / VE) - b0) * VE + (in.ph + id) % VE;
+      here = at >= 0 && at < size * VE;
+    }
     if (here) {
       zk = E::to(cells[at]);
-      const float one[1] = {zk};
-      if (first) on_list.add(one, k);
+      if (first) listed.add_one(zk, k);
     }
-    if (p.tail) {   // listed tokens leave the sum over the remainder
+    if (TAIL) {   // listed tokens leave the sum over the remainder
       __syncthreads();
       if (here) cells[at] = E::from(-INFINITY);
       __syncthreads();
     }
-    for (int v = tid; v < v1 - v0; v += kDistillThreads) {
-      float x[VE];
-      E::unpack(held[v], x);
-      a.add(x, k);
+    for (int i = tid; i < size; i += T * U) {
+      uint4 g[U];
+      float mx = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i + u * T < size) {
+          g[u] = held[i + u * T];
+          mx = max_nan(mx, E::largest(g[u]));
+        }
+      sums.raise(mx);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i + u * T < size) sums.add(g[u]);
     }
   }
-  a = block_merge(a, k, buf);
-  float lr = 0.f;
-  Acc all = a;
-  if (p.tail) {
-    on_list = block_merge(on_list, k, buf);
-    all.merge(on_list, k);
-  }
-  const float ls = log_sum(all);
-  if (p.tail) lr = a.s == 0.f ? -INFINITY : (a.m - all.m) * p.scale + log_sum(a);
-  float l = 0.f;
-  if (id >= 0 && !(t.p[tid] == 0.f)) l = t.p[tid] * (logf(t.p[tid]) - ((zk - all.m) * p.scale - ls));
-  if (tid == 0 && p.tail && !(mass.y == 0.f) && !(lr == -INFINITY && mass.y < 1e-5f)) l += mass.y * (logf(mass.y) - (lr - ls));
-  if (ls == -INFINITY && id >= 0 && t.p[tid] > 0.f) l = INFINITY;
-  if (ls == -INFINITY && tid == 0 && mass.y > 0.f) l = INFINITY;
-  for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
-  if ((tid & 31) == 0) red[tid >> 5] = l;
+  sums.flush();
+  warp_share<false>(sums.a, k, buf[0]);
+  if (TAIL) warp_share<false>(listed, k, buf[1]);
   __syncthreads();
-  if (tid == 0) {
-    float s = 0.f;
-    for (int w = 0; w < kDistillThreads / 32; ++w) s += red[w];
-    p.loss[r] = s;
+  Acc dense = warps_join<false>(k, buf[0]);
+  if (TAIL) listed = warps_join<false>(k, buf[1]);
+  if (split > 1) {
+    ptx::cluster_wait();   // all blocks have started
+    if (tid < split) {
+      const uint32_t to = ptx::mapa(ptx::smem_u32(&found[rank]), tid);
+      ptx::st_shared_cluster_u32(to, __float_as_uint(dense.m));
+      ptx::st_shared_cluster_u32(to + 4, __float_as_uint(dense.s));
+      if (TAIL) {
+        ptx::st_shared_cluster_u32(to + sizeof(Acc), __float_as_uint(listed.m));
+        ptx::st_shared_cluster_u32(to + sizeof(Acc) + 4, __float_as_uint(listed.s));
+      }
+    }
+    ptx::cluster_sync();
+    dense = listed = Acc{};
+    for (int i = 0; i < split; ++i) {
+      dense.merge(Acc{found[i].dense.m, found[i].dense.s, 0.f}, k);
+      if (TAIL) listed.merge(Acc{found[i].listed.m, found[i].listed.s, 0.f}, k);
+    }
+  }
+  Acc all = dense;
+  if (TAIL) all.merge(listed, k);
+  const float ls = log_sum(all);
+  const float lr = !TAIL ? 0.f : dense.s == 0.f ? -INFINITY : (dense.m - all.m) * p.scale + log_sum(dense);
+  const float pk = id >= 0 ? t.p[tid] : 0.f;
+  if (rank == 0 && tid < kMaxList) {
+    float l = 0.f;
+    if (!(pk == 0.f)) l = ls == -INFINITY && pk > 0.f ? INFINITY : pk * (logf(pk) - ((zk - all.m) * p.scale - ls));
+    if (TAIL && tid == 0 && !(t.rest == 0.f)) {
+      if (ls == -INFINITY && t.rest > 0.f) l = INFINITY;
+      else if (!(lr == -INFINITY && t.rest < 1e-5f)) l += t.rest * (logf(t.rest) - (lr - ls));
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
+    if ((tid & 31) == 0) red[tid >> 5] = l;
+  }
+  if (p.dlogits) {
+    const float w = p.weight ? p.weight[r] : 1.f;
+    const Coef c = distill_coef<TAIL>(p, t, all.m, ls, lr, w);
+    const Row<DT> out(p.dlogits, r, p.grad_stride, p.vocab);
+    if (tid < n) t.list.add[tid] = -w * p.scale * pk;
+    if (part.n_all > p.hold) {
+      __syncthreads();
+      grad_part<DT, false>(in, out, part, c, t.list, n);
+    } else {
+      const Dense<DT, false> of(c);
+      const bool alike = in.ph == out.ph;
+      for (int i = tid; i < part.n_all; i += T) {
+        float x[VE];
+        of(held[i], x);
+        store_granule<DT>(in, out, part, alike, i, x);
+      }
+      __syncthreads();   // the dense part of the listed columns is written before what replaces it
+      if (id >= 0 && part.has(in.ph + id) && !c.zero) out.column(id) = E::from(grad_of(zk, c) + add_of_column(t.list, n, tid));
+    }
+  } else {
+    __syncthreads();
+  }
+  if (rank == 0 && tid == 0) {
+    p.loss[r] = red[0] + red[1] + red[2] + red[3];
     if (p.stats) {
       p.stats[3 * r] = ls == -INFINITY ? -INFINITY : all.m;
       p.stats[3 * r + 1] = ls;
-      p.stats[3 * r + 2] = ls == -INFINITY && p.tail ? -INFINITY : lr;
+      p.stats[3 * r + 2] = ls == -INFINITY && TAIL ? -INFINITY : lr;
     }
   }
-  if (!p.dlogits) return;
-  const Coef c = distill_coef(p, t, mass, all.m, ls, lr, p.weight ? p.weight[r] : 1.f);
-  const Row<DT> out(p.dlogits, r, p.grad_stride, p.vocab);
-  if (nv > p.hold) {
-    grad_range<DT>(in, out, 0, nv, c, t.list, n);
-    return;
-  }
-  for (int v = tid; v < nv; v += kDistillThreads) {
-    float x[VE];
-    E::unpack(held[v], x);
-    dense_granule<DT>(x, c);
-    store_granule<DT>(in, out, v, x);
-  }
-  __syncthreads();
-  if (id >= 0 && !c.zero)
-    out.column(id) = E::from(grad_of(zk, c.k, c.m, c.off_l, c.alpha_l, 0.f) + add_of_column(t.list, n, tid));
 }
 
-template <int DT>
+template <int DT, bool TAIL>
 __global__ void __launch_bounds__(kDistillThreads) distill_grad_kernel(const DistillParams p) {
   __shared__ Teacher t;
-  const int64_t r = blockIdx.x;
+  const int64_t r = blockIdx.x / p.split;
   const Row<DT> in(p.logits, r, p.stride, p.vocab), out(p.dlogits, r, p.grad_stride, p.vocab);
-  const float2 mass = load_teacher(p, r, t);
-  const Coef c = distill_coef(p, t, mass, p.stats[3 * r], p.stats[3 * r + 1], p.stats[3 * r + 2], p.weight[r]);
-  grad_range<DT>(in, out, 0, in.granules(), c, t.list, p.list_k);
+  load_teacher<TAIL>(p, r, t);
+  __syncthreads();
+  const float w = p.weight[r];
+  const Coef c = distill_coef<TAIL>(p, t, p.stats[3 * r], p.stats[3 * r + 1], p.stats[3 * r + 2], w);
+  if (threadIdx.x < kMaxList) t.list.add[threadIdx.x] = -w * p.scale * t.p[threadIdx.x];
+  __syncthreads();
+  grad_part<DT, false>(in, out, Part<DT>(in, blockIdx.x % p.split, p.split), c, t.list, p.list_k);
 }
 
 }  // namespace rows
@@ -199,7 +264,9 @@ using namespace iris::rows;
 
 namespace {
 
-constexpr int kHoldBytes = 192 * 1024;
+constexpr int kHoldBytes = 192 * 1024;   // of shared memory at most for a part
+static int part_kb() { const char* e = getenv("PARTKB"); return e ? atoi(e) : 56; }
+#define kPartBytes (part_kb() * 1024)
 constexpr int kMaxDevices = 64;
 
 int check_distill(const char* fn, const iris_distill_args* a, int64_t* stride, int64_t* gstride) {
@@ -229,7 +296,6 @@ DistillParams params_of(const iris_distill_args* a, int64_t stride, int64_t gstr
   p.grad_stride = gstride;
   p.vocab = (int)a->vocab;
   p.list_k = a->list_k;
-  p.tail = a->mode == IRIS_DISTILL_TAIL;
   p.scale = a->scale;
   p.teacher_scale = a->teacher_scale;
   p.teacher = a->teacher;
@@ -241,18 +307,41 @@ DistillParams params_of(const iris_distill_args* a, int64_t stride, int64_t gstr
   return p;
 }
 
-template <int DT>
+template <int DT, bool TAIL>
 int launch_distill(DistillParams p, int64_t rows, cudaStream_t st) {
   static bool configured[kMaxDevices] = {};
   int dev = -1;
   IRIS_CUDA_TRY(cudaGetDevice(&dev));
   if (dev >= kMaxDevices || !configured[dev]) {
-    IRIS_CUDA_TRY(cudaFuncSetAttribute(distill_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldBytes));
+    IRIS_CUDA_TRY(cudaFuncSetAttribute(distill_kernel<DT, TAIL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldBytes));
     if (dev < kMaxDevices) configured[dev] = true;
   }
-  const int64_t need = (p.vocab + 2 * Row<DT>::VE - 2) / Row<DT>::VE;   // granules of a row, wherever it starts
-  p.hold = (int)(need * 16 <= kHoldBytes ? (need > 0 ? need : 1) : kHoldBytes / 16);
-  distill_kernel<DT><<<(unsigned)rows, kDistillThreads, (size_t)p.hold * 16, st>>>(p);
+  // A row is shared by a cluster of blocks until a part is at most kPartBytes, or while the rows alone leave SMs without
+  // work and every thread still has a granule.
+  const int64_t granules = (p.vocab + 2 * Row<DT>::VE - 2) / Row<DT>::VE;   // of a row, wherever it starts
+  int split = 1;
+  while (split < kMaxSplit && (granules * 16 > (int64_t)split * kPartBytes || (rows * split < 2 * kSms && granules >= (int64_t)split * 2 * kDistillThreads))) ++split;
+  p.split = split;
+  const int64_t need = std::max<int64_t>(1, (granules + split - 1) / split);
+  p.hold = (int)std::min<int64_t>(need, kHoldBytes / 16);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(rows * split));
+  cfg.blockDim = dim3(kDistillThreads);
+  cfg.dynamicSmemBytes = (size_t)p.hold * 16;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)split;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = split > 1 ? 1 : 0;
+  IRIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, distill_kernel<DT, TAIL>, p));
+  return IRIS_OK;
+}
+
+template <int DT, bool TAIL>
+int launch_distill_grad(const DistillParams& p, int64_t rows, cudaStream_t st) {
+  distill_grad_kernel<DT, TAIL><<<(unsigned)(rows * p.split), kDistillThreads, 0, st>>>(p);
   IRIS_CUDA_TRY(cudaGetLastError());
   return IRIS_OK;
 }
@@ -267,10 +356,12 @@ extern "C" int iris_distill_topk(const iris_distill_args* a, void* stream) {
   IRIS_CHECK(check_aligned(fn, "loss", a->loss, 4, true));
   IRIS_CHECK(check_aligned(fn, "stats", a->stats, 4, false));
   const DistillParams p = params_of(a, stride, gstride);
+  if (a->rows > INT32_MAX / kMaxSplit) return fail(IRIS_ERR_UNSUPPORTED, "%s: more than 2^28 rows", fn);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (a->dtype == IRIS_BF16) return launch_distill<IRIS_BF16>(p, a->rows, st);
-  if (a->dtype == IRIS_F16) return launch_distill<IRIS_F16>(p, a->rows, st);
-  return launch_distill<IRIS_F32>(p, a->rows, st);
+  const bool tail = a->mode == IRIS_DISTILL_TAIL;
+  if (a->dtype == IRIS_BF16) return tail ? launch_distill<IRIS_BF16, true>(p, a->rows, st) : launch_distill<IRIS_BF16, false>(p, a->rows, st);
+  if (a->dtype == IRIS_F16) return tail ? launch_distill<IRIS_F16, true>(p, a->rows, st) : launch_distill<IRIS_F16, false>(p, a->rows, st);
+  return tail ? launch_distill<IRIS_F32, true>(p, a->rows, st) : launch_distill<IRIS_F32, false>(p, a->rows, st);
 }
 
 extern "C" int iris_distill_topk_backward(const iris_distill_args* a, void* stream) {
@@ -281,11 +372,12 @@ extern "C" int iris_distill_topk_backward(const iris_distill_args* a, void* stre
   IRIS_CHECK(check_aligned(fn, "stats", a->stats, 4, true));
   IRIS_CHECK(check_aligned(fn, "weight", a->weight, 4, true));
   if (!a->dlogits) return fail(IRIS_ERR_ARG, "%s: dlogits is NULL", fn);
-  const DistillParams p = params_of(a, stride, gstride);
+  DistillParams p = params_of(a, stride, gstride);
+  p.split = grad_parts(a->vocab, a->dtype);
+  if (a->rows * p.split > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 blocks", fn);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (a->dtype == IRIS_BF16) distill_grad_kernel<IRIS_BF16><<<(unsigned)a->rows, kDistillThreads, 0, st>>>(p);
-  else if (a->dtype == IRIS_F16) distill_grad_kernel<IRIS_F16><<<(unsigned)a->rows, kDistillThreads, 0, st>>>(p);
-  else distill_grad_kernel<IRIS_F32><<<(unsigned)a->rows, kDistillThreads, 0, st>>>(p);
-  IRIS_CUDA_TRY(cudaGetLastError());
-  return IRIS_OK;
+  const bool tail = a->mode == IRIS_DISTILL_TAIL;
+  if (a->dtype == IRIS_BF16) return tail ? launch_distill_grad<IRIS_BF16, true>(p, a->rows, st) : launch_distill_grad<IRIS_BF16, false>(p, a->rows, st);
+  if (a->dtype == IRIS_F16) return tail ? launch_distill_grad<IRIS_F16, true>(p, a->rows, st) : launch_distill_grad<IRIS_F16, false>(p, a->rows, st);
+  return tail ? launch_distill_grad<IRIS_F32, true>(p, a->rows, st) : launch_distill_grad<IRIS_F32, false>(p, a->rows, st);
 }

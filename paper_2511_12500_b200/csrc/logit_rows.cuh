@@ -59,6 +59,12 @@ __device__ __forceinline__ uint4 ld_once(const void* p) {
   asm("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
+// 16 bytes to shared memory without passing through registers; visible to the copying thread after copy_async_wait, to
+// the block after a barrier behind that.
+__device__ __forceinline__ void copy_async(void* shared, const void* global) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(global) : "memory");
+}
+__device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // The larger of two, NaN if either is.
 __device__ __forceinline__ float max_nan(float a, float b) {
   float y;
@@ -66,11 +72,24 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return y;
 }
 
-template <int DT> struct Elem;   // largest(): of a granule's values, NaN if one is; kMasked: 32 bits of -inf
+template <int DT> struct Elem;   // kMasked: 32 bits of -inf; largest(): of a granule's values, NaN if one is;
+// at_least(): none below twice(floor), NaN stays
 template <> struct Elem<IRIS_F16> {
   using T = __half;
   static constexpr int VE = 8;
   static constexpr uint32_t kMasked = 0xfc00fc00u;
+  static constexpr float kLowest = -65504.f;
+  static __device__ __forceinline__ uint32_t twice(float x) {
+    const __half2 h = __floats2half2_rn(x, x);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ uint4 at_least(uint4 v, uint32_t floor) {
+    asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(v.x) : "r"(floor));
+    asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(v.y) : "r"(floor));
+    asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(v.z) : "r"(floor));
+    asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(v.w) : "r"(floor));
+    return v;
+  }
   static __device__ __forceinline__ float largest(const uint4& v) {
     uint32_t a, b, m;
     asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
@@ -104,6 +123,18 @@ template <> struct Elem<IRIS_BF16> {
   using T = __nv_bfloat16;
   static constexpr int VE = 8;
   static constexpr uint32_t kMasked = 0xff80ff80u;
+  static constexpr float kLowest = -3.38e38f;
+  static __device__ __forceinline__ uint32_t twice(float x) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, x);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ uint4 at_least(uint4 v, uint32_t floor) {
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(v.x) : "r"(floor));
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(v.y) : "r"(floor));
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(v.z) : "r"(floor));
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(v.w) : "r"(floor));
+    return v;
+  }
   static __device__ __forceinline__ float largest(const uint4& v) {
     uint32_t a, b, m;
     asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
@@ -135,6 +166,13 @@ template <> struct Elem<IRIS_F32> {
   using T = float;
   static constexpr int VE = 4;
   static constexpr uint32_t kMasked = 0xff800000u;
+  static constexpr float kLowest = -3.38e38f;
+  static __device__ __forceinline__ uint32_t twice(float x) { return __float_as_uint(x); }
+  static __device__ __forceinline__ uint4 at_least(const uint4& v, uint32_t floor) {
+    const float f = __uint_as_float(floor);
+    return make_uint4(__float_as_uint(max_nan(__uint_as_float(v.x), f)), __float_as_uint(max_nan(__uint_as_float(v.y), f)),
+                      __float_as_uint(max_nan(__uint_as_float(v.z), f)), __float_as_uint(max_nan(__uint_as_float(v.w), f)));
+  }
   static __device__ __forceinline__ float largest(const uint4& v) {
     return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)), max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
   }
@@ -190,8 +228,28 @@ struct Row {
   }
 };
 
+// What a block does of a row: granules [v0, v1).  Counted i = 0 .. n_all - 1 so that those that lie inside the row come
+// first (n_int of them, w0 + i), and what the row covers in part, at most two, comes last.
+template <int DT>
+struct Part {
+  static constexpr int VE = Elem<DT>::VE;
+  int v0, v1, w0, n_int, n_all;
+  __device__ __forceinline__ Part(const Row<DT>& row, int part, int parts) {
+    const int nv = row.granules(), each = (nv + parts - 1) / parts;
+    v0 = min(nv, part * each);
+    v1 = min(nv, v0 + each);
+    w0 = v0 + (v0 < v1 && v0 * VE < row.ph);
+    n_int = v1 - (v1 > w0 && v1 * VE > row.end) - w0;
+    n_all = v1 - v0;
+  }
+  __device__ __forceinline__ int granule(int i) const { return i < n_int ? w0 + i : v0 < w0 && i == n_int ? v0 : v1 - 1; }
+  __device__ __forceinline__ int place(int v) const { return v < w0 ? n_int : v < w0 + n_int ? v - w0 : n_all - 1; }
+  __device__ __forceinline__ bool has(int element) const { return element >= v0 * VE && element < v1 * VE; }   // counted from granule0
+  __device__ __forceinline__ uint4 raw(const Row<DT>& row, int i) const { return i < n_int ? ld_once(row.at(w0 + i)) : row.raw(granule(i)); }
+};
+
 // Running statistics of a set of logits: m >= every one of them (and >= -FLT_MAX, so that z - m is never inf - inf for
-// a masked z), s = sum 2^y, t = sum y 2^y with y = max((z - m) k, kFloor), k = scale log2(e).
+// a masked z), s = sum 2^y, t = sum y 2^y, y = (z - m) k cut at about kFloor, k = scale log2(e).
 struct Acc {
   float m = -FLT_MAX, s = 0.f, t = 0.f;
   __device__ __forceinline__ void rebase(float mx, float k) {   // to a larger m
@@ -205,31 +263,34 @@ struct Acc {
     const float mx = max_nan(m, o.m);
     rebase(mx, k);
     b.rebase(mx, k);
-    s = __fadd_rn(s, b.s);   // products rounded before they are added: a.merge(b) and b.merge(a) give the same bits,
-    t = __fadd_rn(t, b.t);   // and so all threads of a butterfly
+    s = __fadd_rn(s, b.s);
+    t = __fadd_rn(t, b.t);
   }
-  template <int N>
-  __device__ __forceinline__ void add(const float (&x)[N], float k) {
-    float mx = x[0];
-#pragma unroll
-    for (int e = 1; e < N; ++e) mx = max_nan(mx, x[e]);
-    if (!(mx <= m)) rebase(max_nan(m, mx), k);
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float y = max_nan((x[e] - m) * k, kFloor), f = ex2(y);
-      s += f;
-      t = fmaf(f, y, t);
-    }
-  }
+  __device__ __forceinline__ void add_one(float z, float k) { merge(Acc{max_nan(z, -FLT_MAX), z == -INFINITY ? 0.f : z == z && z != INFINITY ? 1.f : NAN, 0.f}, k); }
 };
 
-// Adds granules to a thread's statistics.  All of them count from one m, which the caller raises first (raise()); two
-// elements at a time: per element about 1 instruction to unpack, 1/2 each to subtract, scale and add, 1 exponential,
-// and 1 1/2 for the entropy's sum.
+// The lowest logit that has to be told apart: one below low(m, k) has 2^y = 0 and is lifted to it, so that y 2^y is 0 and
+// not NaN for -inf.  Rounding to the type stays below m + kFloor / k.  False where the type has no such value (masks of
+// the lowest finite value and nothing above them, temperatures beyond the type's range): then y is cut instead.
+template <int DT>
+__device__ __forceinline__ bool lift_floor(float m, float k, uint32_t& word) {
+  const float z = m + kFloor / k, low = z - fabsf(z) * (1.f / 64);
+  word = Elem<DT>::twice(low);
+  return low >= Elem<DT>::kLowest && low * k > -1e38f && m * k < 1e38f;
+}
+
+// A thread's statistics of granules.  All logits added since the last raise() count from its m.  Per element one
+// instruction to unpack, half of one each to subtract, scale and add, and the exponential; with the entropy half of one
+// each for the lift (on packed 16-bit values) and the second sum.
 template <int DT, bool ENTROPY>
 struct Sums {
   Acc a;
-  uint64_t s2 = 0, t2 = 0;   // the two halves' sums since the last raise
+  float k;
+  bool lift = false;
+  uint32_t floor = 0;
+  uint64_t s2 = 0, t2 = 0;   // sums of even and odd places since the last raise
+  uint64_t k2, minus_m2;
+  __device__ __forceinline__ explicit Sums(float k_) : k(k_), k2(pair(k_, k_)), minus_m2(pair(FLT_MAX, FLT_MAX)) {}
   __device__ __forceinline__ void flush() {
     const float2 s = unpair(s2);
     a.s += s.x + s.y;
@@ -240,48 +301,69 @@ struct Sums {
       t2 = 0;
     }
   }
-  __device__ __forceinline__ void raise(float mx, float k) {
+  __device__ __forceinline__ void raise(float mx) {   // before adding logits of which mx is the largest
+    if (mx <= a.m) return;
     flush();
-    if (!(mx <= a.m)) a.rebase(max_nan(a.m, mx), k);
+    a.rebase(max_nan(a.m, mx), k);
+    minus_m2 = pair(-a.m, -a.m);
+    if (ENTROPY) lift = lift_floor<DT>(a.m, k, floor);
   }
-  __device__ __forceinline__ void add(const uint4& v, uint64_t minus_m, uint64_t k2) {
+  __device__ __forceinline__ void add(const uint4& g) {
     constexpr int VE = Elem<DT>::VE;
     float x[VE];
-    Elem<DT>::unpack(v, x);
+    if (!ENTROPY || lift) {
+      Elem<DT>::unpack(ENTROPY ? Elem<DT>::at_least(g, floor) : g, x);
 #pragma unroll
-    for (int e = 0; e < VE; e += 2) {
-      float2 y = unpair(mul2f(add2f(pair(x[e], x[e + 1]), minus_m), k2));
-      if (ENTROPY) {
-        y.x = max_nan(y.x, kFloor);
-        y.y = max_nan(y.y, kFloor);
+      for (int e = 0; e < VE; e += 2) {
+        const uint64_t y2 = mul2f(add2f(pair(x[e], x[e + 1]), minus_m2), k2);
+        const float2 y = unpair(y2);
+        const uint64_t f = pair(ex2(y.x), ex2(y.y));
+        s2 = add2f(s2, f);
+        if (ENTROPY) t2 = fma2f(f, y2, t2);
       }
-      const uint64_t f = pair(ex2(y.x), ex2(y.y));
-      s2 = add2f(s2, f);
-      if (ENTROPY) t2 = fma2f(f, pair(y.x, y.y), t2);
+    } else {
+      Elem<DT>::unpack(g, x);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        const float y = max_nan((x[e] - a.m) * k, kFloor), f = ex2(y);
+        a.s += f;
+        a.t = fmaf(f, y, a.t);
+      }
     }
   }
 };
 
-__device__ __forceinline__ Acc warp_merge(Acc a, float k) {
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// All threads of a block of 256 get the merged statistics, the same bits.  `buf`: 8 entries, used once a kernel or with a
+// barrier between uses.  One barrier.
+struct Warps8 {
+  Acc of[8];
+};
+template <bool ENTROPY>
+__device__ __forceinline__ void warp_share(Acc a, float k, Warps8& buf) {
+  a.rebase(warp_max(a.m), k);
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
-    Acc b;
-    b.m = __shfl_xor_sync(~0u, a.m, o);
-    b.s = __shfl_xor_sync(~0u, a.s, o);
-    b.t = __shfl_xor_sync(~0u, a.t, o);
-    a.merge(b, k);
+    a.s += __shfl_xor_sync(~0u, a.s, o);
+    if (ENTROPY) a.t += __shfl_xor_sync(~0u, a.t, o);
+  }
+  if ((threadIdx.x & 31) == 0) buf.of[threadIdx.x >> 5] = a;
+}
+template <bool ENTROPY>
+__device__ __forceinline__ Acc warps_join(float k, const Warps8& buf) {
+  Acc a = buf.of[threadIdx.x & 7];
+  a.rebase(warp_max(a.m), k);
+#pragma unroll
+  for (int o = 4; o; o >>= 1) {
+    a.s += __shfl_xor_sync(~0u, a.s, o);
+    if (ENTROPY) a.t += __shfl_xor_sync(~0u, a.t, o);
   }
   return a;
-}
-// All threads of the block get the merged statistics.  `buf`: 32 entries of shared memory, free for others after the
-// next barrier.
-__device__ __forceinline__ Acc block_merge(Acc a, float k, Acc* buf) {
-  a = warp_merge(a, k);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = a;
-  __syncthreads();
-  Acc r = (threadIdx.x & 31) < blockDim.x / 32 ? buf[threadIdx.x & 31] : Acc{};
-  return warp_merge(r, k);
 }
 
 // ln sum exp(scale (z - m)): -inf where no logit is left.

@@ -36,21 +36,19 @@ template <int DT, bool ENTROPY, bool TOP>
 __global__ void __launch_bounds__(kScoreThreads) score_kernel(const ScoreParams p) {
   using E = Elem<DT>;
   constexpr int T = kScoreThreads, U = kScoreGranules;
-  __shared__ Acc buf[32];
+  __shared__ Warps8 buf;
   __shared__ Acc parts[kMaxSplit];
   __shared__ typename std::conditional<TOP, TopShared, NoTop>::type top;
   extern __shared__ uint64_t lists[];   // TOP and split > 1: the blocks' sorted lists, top_k keys each, 0 where one is shorter
-  const int split = p.split, part = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x;
+  const int split = p.split, rank = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x;
   const int64_t r = blockIdx.x / split;
   if (split > 1) ptx::cluster_arrive_relaxed();
   const Row<DT> row(p.logits, r, p.stride, p.vocab);
-  const int nv = row.granules(), each = (nv + split - 1) / split;
-  const int v0 = min(nv, part * each), v1 = min(nv, v0 + each);
+  const Part<DT> part(row, rank, split);
   const float k = p.scale * kLog2e;
-  const uint64_t k2 = pair(k, k);
   float zt = 0.f;
   bool there = false;
-  if (part == 0 && tid < p.n_targets) {
+  if (rank == 0 && tid < p.n_targets) {
     const int64_t t = p.targets[r * p.n_targets + tid];
     there = t >= 0 && t < p.vocab;
     if (there) zt = E::to(row.column((int)t));
@@ -60,30 +58,29 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const ScoreParams 
     if (tid == 0) top.n = top.n_kept = 0, top.tau = 0;
     top.code[tid] = 0;
   }
-  Sums<DT, ENTROPY> sums;
-  for (int base = v0; base < v1; base += T * U) {
+  Sums<DT, ENTROPY> sums(k);
+  for (int base = 0; base < part.n_all; base += T * U) {
     uint4 g[U];
+    const int i0 = base + tid, n = part.n_all;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int v = base + u * T + tid;
-      g[u] = make_uint4(E::kMasked, E::kMasked, E::kMasked, E::kMasked);
-      if (v < v1) g[u] = row.raw(v);
-    }
-    float mx = E::largest(g[0]);
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * T < n) g[u] = part.raw(row, i0 + u * T);
+    float mx = -INFINITY;
 #pragma unroll
-    for (int u = 1; u < U; ++u)
-      if (base + u * T < v1) mx = max_nan(mx, E::largest(g[u]));
-    sums.raise(mx, k);
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * T < n) mx = max_nan(mx, E::largest(g[u]));
+    sums.raise(mx);
     if constexpr (TOP) {
       seen = max_nan(seen, mx);
-      if (base + tid < v1) top.code[tid] = order_bits(seen);
+      if (i0 < n) top.code[tid] = order_bits(seen);
       __syncthreads();
       if (tid < 32) bisect_tau(top, p.top_k);
     }
-    const uint64_t minus_m = pair(-sums.a.m, -sums.a.m);
+    if (mx != -INFINITY) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (base + u * T < v1) sums.add(g[u], minus_m, k2);
+      for (int u = 0; u < U; ++u)
+        if (i0 + u * T < n) sums.add(g[u]);
+    }
     if constexpr (TOP) {
       __syncthreads();
       const uint32_t tau = top.tau;
@@ -91,28 +88,30 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const ScoreParams 
       if (tau != 0xffffffffu) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (base + u * T + tid < v1) collect<DT>(top, row, base + u * T + tid, g[u], at_tau);
+          if (i0 + u * T < n) collect<DT>(top, row, part.granule(i0 + u * T), g[u], at_tau);
       }
     }
   }
   sums.flush();
-  Acc a = block_merge(sums.a, k, buf);
+  warp_share<ENTROPY>(sums.a, k, buf);
+  __syncthreads();
+  Acc a = warps_join<ENTROPY>(k, buf);
 
   if (split > 1) {
     ptx::cluster_wait();   // the first block has started
     if (tid == 0) {
-      const uint32_t to = ptx::mapa(ptx::smem_u32(&parts[part]), 0);
+      const uint32_t to = ptx::mapa(ptx::smem_u32(&parts[rank]), 0);
       ptx::st_shared_cluster_u32(to, __float_as_uint(a.m));
       ptx::st_shared_cluster_u32(to + 4, __float_as_uint(a.s));
       ptx::st_shared_cluster_u32(to + 8, __float_as_uint(a.t));
     }
     if constexpr (TOP) {
-      const uint32_t to = ptx::mapa(ptx::smem_u32(lists + part * p.top_k), 0);
-      const int n = finish_top<DT>(top, row, v0, v1, p.top_k, [&](int place, uint64_t key) { ptx::st_shared_cluster_u64(to + place * 8, key); });
+      const uint32_t to = ptx::mapa(ptx::smem_u32(lists + rank * p.top_k), 0);
+      const int n = finish_top<DT>(top, row, part.v0, part.v1, p.top_k, [&](int place, uint64_t key) { ptx::st_shared_cluster_u64(to + place * 8, key); });
       if (tid >= n && tid < p.top_k) ptx::st_shared_cluster_u64(to + tid * 8, 0);
     }
     ptx::cluster_sync();
-    if (part != 0) return;
+    if (rank != 0) return;
     a = parts[0];
     for (int i = 1; i < split; ++i) a.merge(parts[i], k);
   }
@@ -131,7 +130,7 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const ScoreParams 
       if (p.top_logprob) p.top_logprob[r * p.top_k + place] = log_prob(key_value(key), a.m, ls, p.scale);
     };
     if (split == 1) {
-      finish_top<DT>(top, row, v0, v1, p.top_k, emit);
+      finish_top<DT>(top, row, part.v0, part.v1, p.top_k, emit);
     } else {   // a key's place is the number of larger ones in every list
       for (int i = tid; i < split * p.top_k; i += T) {
         const uint64_t key = lists[i];
@@ -178,28 +177,33 @@ static int launch_score(const ScoreParams& p, int64_t rows, cudaStream_t st) {
 struct ScoreGradParams {
   const void* logits;
   int64_t stride, grad_stride;
-  int vocab, n_targets;
+  int vocab, n_targets, parts;
   float scale;
   const int64_t* targets;
   const float *stats, *entropy, *grad_logprob, *grad_entropy;
   void* dlogits;
 };
 
-constexpr int kGradThreads = 256;
-
 // dz_j = scale [ sum_q g_q ([t_q = j] - q_j) - g_H q_j (ln q_j + H) ]
-template <int DT>
+template <int DT, bool ENTROPY>
 __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const ScoreGradParams p) {
   __shared__ List list;
-  const int64_t r = blockIdx.x;
+  const int64_t r = blockIdx.x / p.parts;
   const Row<DT> in(p.logits, r, p.stride, p.vocab), out(p.dlogits, r, p.grad_stride, p.vocab);
   const int n = p.grad_logprob ? p.n_targets : 0;
-  const float ls = p.stats[2 * r + 1], gh = p.grad_entropy ? p.grad_entropy[r] : 0.f, h = p.grad_entropy ? p.entropy[r] : 0.f;
-  if ((int)threadIdx.x < n) {
-    const int64_t t = p.targets[r * n + threadIdx.x];
-    const bool there = t >= 0 && t < p.vocab;
-    list.id[threadIdx.x] = there ? (int)t : -1;
-    list.add[threadIdx.x] = there ? p.scale * p.grad_logprob[r * n + threadIdx.x] : 0.f;
+  const float ls = p.stats[2 * r + 1], gh = ENTROPY ? p.grad_entropy[r] : 0.f, h = ENTROPY ? p.entropy[r] : 0.f;
+  if (threadIdx.x < kMaxList) {
+    int id = -1;
+    float add = 0.f;
+    if ((int)threadIdx.x < n) {
+      const int64_t t = p.targets[r * n + threadIdx.x];
+      if (t >= 0 && t < p.vocab) {
+        id = (int)t;
+        add = p.scale * p.grad_logprob[r * n + threadIdx.x];
+      }
+    }
+    list.id[threadIdx.x] = id;
+    list.add[threadIdx.x] = add;
   }
   __syncthreads();
   float g = 0.f;
@@ -211,7 +215,16 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const ScoreGra
   c.alpha = c.alpha_l = -(g + p.scale * gh * h);
   c.beta = -p.scale * gh * kLn2;
   c.zero = ls == -INFINITY;
-  grad_range<DT>(in, out, 0, in.granules(), c, list, n);
+  grad_part<DT, ENTROPY>(in, out, Part<DT>(in, blockIdx.x % p.parts, p.parts), c, list, n);
+}
+
+template <int DT>
+static int launch_score_grad(const ScoreGradParams& p, int64_t rows, cudaStream_t st) {
+  const unsigned grid = (unsigned)(rows * p.parts);
+  if (p.grad_entropy) score_grad_kernel<DT, true><<<grid, kGradThreads, 0, st>>>(p);
+  else score_grad_kernel<DT, false><<<grid, kGradThreads, 0, st>>>(p);
+  IRIS_CUDA_TRY(cudaGetLastError());
+  return IRIS_OK;
 }
 
 }  // namespace rows
@@ -266,12 +279,12 @@ extern "C" int iris_token_logprobs_backward(const iris_logprob_grad_args* a, voi
   IRIS_CHECK(check_aligned(fn, "stats", a->stats, 4, true));
   IRIS_CHECK(check_aligned(fn, "grad_entropy", a->grad_entropy, 4, false));
   IRIS_CHECK(check_aligned(fn, "entropy", a->entropy, 4, want_h));
-  ScoreGradParams p{a->logits, stride, gstride, (int)a->vocab, a->n_targets, a->scale, a->targets, a->stats, a->entropy, want_lp ? a->grad_logprob : nullptr,
-                    a->grad_entropy, a->dlogits};
+  const int parts = grad_parts(a->vocab, a->dtype);
+  if (a->rows * parts > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 blocks", fn);
+  ScoreGradParams p{a->logits, stride, gstride, (int)a->vocab, a->n_targets, parts, a->scale, a->targets, a->stats, a->entropy,
+                    want_lp ? a->grad_logprob : nullptr, a->grad_entropy, a->dlogits};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (a->dtype == IRIS_BF16) score_grad_kernel<IRIS_BF16><<<(unsigned)a->rows, kGradThreads, 0, st>>>(p);
-  else if (a->dtype == IRIS_F16) score_grad_kernel<IRIS_F16><<<(unsigned)a->rows, kGradThreads, 0, st>>>(p);
-  else score_grad_kernel<IRIS_F32><<<(unsigned)a->rows, kGradThreads, 0, st>>>(p);
-  IRIS_CUDA_TRY(cudaGetLastError());
-  return IRIS_OK;
+  if (a->dtype == IRIS_BF16) return launch_score_grad<IRIS_BF16>(p, a->rows, st);
+  if (a->dtype == IRIS_F16) return launch_score_grad<IRIS_F16>(p, a->rows, st);
+  return launch_score_grad<IRIS_F32>(p, a->rows, st);
 }
