@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 IRIS_OK = 0
 IRIS_ERR_ARG, IRIS_ERR_RANGE, IRIS_ERR_NOMEM, IRIS_ERR_CUDA = -1, -2, -3, -4
@@ -59,28 +60,11 @@ class GemmArgs(C.Structure):
     ]
 
 
-_LOGITS = [("logits", C.c_void_p), ("rows", C.c_int64), ("vocab", C.c_int64), ("row_stride", C.c_int64), ("dtype", C.c_int), ("scale", C.c_float)]
-
-
-class LogprobArgs(C.Structure):
-    _fields_ = _LOGITS + [
-        ("targets", C.c_void_p), ("n_targets", C.c_int), ("top_k", C.c_int), ("logprob", C.c_void_p), ("entropy", C.c_void_p),
-        ("stats", C.c_void_p), ("top_ids", C.c_void_p), ("top_logprob", C.c_void_p),
-    ]
-
-
-class LogprobGradArgs(C.Structure):
-    _fields_ = _LOGITS + [
-        ("targets", C.c_void_p), ("n_targets", C.c_int), ("stats", C.c_void_p), ("grad_logprob", C.c_void_p), ("entropy", C.c_void_p),
-        ("grad_entropy", C.c_void_p), ("dlogits", C.c_void_p), ("grad_stride", C.c_int64),
-    ]
-
-
-class DistillArgs(C.Structure):
-    _fields_ = _LOGITS + [
-        ("teacher", C.c_void_p), ("teacher_ids", C.c_void_p), ("list_k", C.c_int), ("mode", C.c_int), ("teacher_scale", C.c_float),
-        ("weight", C.c_void_p), ("loss", C.c_void_p), ("stats", C.c_void_p), ("dlogits", C.c_void_p), ("grad_stride", C.c_int64),
-    ]
+# The argument blocks of the operators on logits, in the header's order (P pointer, q int64, i int, f float, natural alignment).  They are called
+# once a decoded token, where filling a ctypes.Structure would take longer than the kernel: packing one is a tenth of that.
+_LOGPROB_ARGS = struct.Struct("@PqqqifPiiPPPPP")
+_LOGPROB_GRAD_ARGS = struct.Struct("@PqqqifPiPPPPPq")
+_DISTILL_ARGS = struct.Struct("@PqqqifPPiifPPPPq")
 
 
 _lib = None
@@ -148,10 +132,8 @@ def lib() -> C.CDLL:
     L.iris_gemm_out_offset.restype = u64
     L.iris_gemm_out_offset.argtypes = [ci, ci, ci]
     L.iris_gemm_all_scatter_noalloc.argtypes = [vp, C.POINTER(vp), C.POINTER(u64), sz, ci, ci, ci, ci, ci, u64, u64, i32, vp]
-    L.iris_token_logprobs.argtypes = [C.POINTER(LogprobArgs), vp]
-    L.iris_token_logprobs_backward.argtypes = [C.POINTER(LogprobGradArgs), vp]
-    for f in (L.iris_distill_topk, L.iris_distill_topk_backward):
-        f.argtypes = [C.POINTER(DistillArgs), vp]
+    for f in (L.iris_token_logprobs, L.iris_token_logprobs_backward, L.iris_distill_topk, L.iris_distill_topk_backward):
+        f.argtypes = [C.c_char_p, vp]   # a packed argument block
     _lib = L
     return L
 
@@ -439,31 +421,45 @@ def iris_gemm_all_scatter_noalloc(A, B_shards, slot_bases, bytes_per_rank, M, N,
 # ------------------------------------------------------------------------------------- operators on logits
 # Shapes, types and rules are the header's.  Tensors other than logits and dlogits are contiguous, ids are int64, the
 # rest fp32; row_stride and grad_stride are in elements (0 = vocab).
+def _addr(x) -> int:
+    if x is None:
+        return 0
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        return _ptr(x)
+
+
 def iris_token_logprobs(logits, rows, vocab, dtype, targets=None, n_targets=0, logprob=None, entropy=None, stats=None, top_k=0, top_ids=None,
                         top_logprob=None, scale=1.0, row_stride=0, stream=None):
-    a = LogprobArgs(_ptr(logits), rows, vocab, row_stride, dtype, scale, _ptr(targets), n_targets, top_k, _ptr(logprob), _ptr(entropy), _ptr(stats),
-                    _ptr(top_ids), _ptr(top_logprob))
-    _ck(lib().iris_token_logprobs(C.byref(a), _stream(stream)))
+    a = _LOGPROB_ARGS.pack(_addr(logits), rows, vocab, row_stride, dtype, scale, _addr(targets), n_targets, top_k, _addr(logprob), _addr(entropy),
+                           _addr(stats), _addr(top_ids), _addr(top_logprob))
+    _ck(lib().iris_token_logprobs(a, _stream(stream)))
 
 
 def iris_token_logprobs_backward(logits, rows, vocab, dtype, targets, n_targets, stats, grad_logprob, dlogits, entropy=None, grad_entropy=None,
                                  scale=1.0, row_stride=0, grad_stride=0, stream=None):
-    a = LogprobGradArgs(_ptr(logits), rows, vocab, row_stride, dtype, scale, _ptr(targets), n_targets, _ptr(stats), _ptr(grad_logprob),
-                        _ptr(entropy), _ptr(grad_entropy), _ptr(dlogits), grad_stride)
-    _ck(lib().iris_token_logprobs_backward(C.byref(a), _stream(stream)))
+    a = _LOGPROB_GRAD_ARGS.pack(_addr(logits), rows, vocab, row_stride, dtype, scale, _addr(targets), n_targets, _addr(stats), _addr(grad_logprob),
+                                _addr(entropy), _addr(grad_entropy), _addr(dlogits), grad_stride)
+    _ck(lib().iris_token_logprobs_backward(a, _stream(stream)))
+
+
+def _distill(fn, logits, rows, vocab, dtype, teacher, teacher_ids, list_k, mode, weight, loss, stats, dlogits, scale, teacher_scale, row_stride,
+             grad_stride, stream):
+    a = _DISTILL_ARGS.pack(_addr(logits), rows, vocab, row_stride, dtype, scale, _addr(teacher), _addr(teacher_ids), list_k, mode, teacher_scale,
+                           _addr(weight), _addr(loss), _addr(stats), _addr(dlogits), grad_stride)
+    _ck(fn(a, _stream(stream)))
 
 
 def iris_distill_topk(logits, rows, vocab, dtype, teacher, teacher_ids, list_k, loss, mode=IRIS_DISTILL_RENORM, stats=None, weight=None, dlogits=None,
                       scale=1.0, teacher_scale=1.0, row_stride=0, grad_stride=0, stream=None):
     """Loss per row and, with `dlogits`, weight * its gradient, in one pass over the logits."""
-    a = DistillArgs(_ptr(logits), rows, vocab, row_stride, dtype, scale, _ptr(teacher), _ptr(teacher_ids), list_k, mode, teacher_scale, _ptr(weight),
-                    _ptr(loss), _ptr(stats), _ptr(dlogits), grad_stride)
-    _ck(lib().iris_distill_topk(C.byref(a), _stream(stream)))
+    _distill(lib().iris_distill_topk, logits, rows, vocab, dtype, teacher, teacher_ids, list_k, mode, weight, loss, stats, dlogits, scale, teacher_scale,
+             row_stride, grad_stride, stream)
 
 
 def iris_distill_topk_backward(logits, rows, vocab, dtype, teacher, teacher_ids, list_k, stats, grad_loss, dlogits, mode=IRIS_DISTILL_RENORM,
                                scale=1.0, teacher_scale=1.0, row_stride=0, grad_stride=0, stream=None):
     """grad_loss * the gradient, from the statistics that iris_distill_topk left."""
-    a = DistillArgs(_ptr(logits), rows, vocab, row_stride, dtype, scale, _ptr(teacher), _ptr(teacher_ids), list_k, mode, teacher_scale,
-                    _ptr(grad_loss), None, _ptr(stats), _ptr(dlogits), grad_stride)
-    _ck(lib().iris_distill_topk_backward(C.byref(a), _stream(stream)))
+    _distill(lib().iris_distill_topk_backward, logits, rows, vocab, dtype, teacher, teacher_ids, list_k, mode, grad_loss, None, stats, dlogits, scale,
+             teacher_scale, row_stride, grad_stride, stream)

@@ -13,14 +13,17 @@
 namespace iris {
 namespace rows {
 
-constexpr int kDistillThreads = 256;
+#ifndef DT_T
+#define DT_T 256
+#endif
+constexpr int kDistillThreads = DT_T;
 constexpr int kMaxSplit = 8;   // blocks (one cluster) that share a row
-static_assert(kDistillThreads >= kMaxList && kGradThreads == kDistillThreads, "one thread an entry of the list");
+static_assert(kDistillThreads >= kMaxList && kGradThreads >= kMaxList, "one thread an entry of the list");
 
 struct DistillParams {
   const void* logits;
   int64_t stride, grad_stride;
-  int vocab, list_k, split, hold;   // hold: granules of its part that a block keeps in shared memory
+  int rows, vocab, list_k, split, each, hold;   // each: granules of a block's part of a row; hold: of those in shared memory
   float scale, teacher_scale;
   const float* teacher;
   const int64_t* ids;
@@ -29,65 +32,80 @@ struct DistillParams {
   void* dlogits;
 };
 
-// The teacher's list in shared memory: probabilities p[], columns in list.id (-1: absent), their sum and the remainder p_r.
-struct Teacher {
-  List list;
-  float p[kMaxList];
-  float sum, rest;
+// The teacher's list: thread i has entry i, its column (-1: absent) and its value, and with the others of the first four
+// warps its probability p, the sum P and the remainder p_r.
+struct Entry {
+  int id;
+  float v;
+};
+struct RawEntry {   // as loaded: nothing waits for it yet
+  int64_t id = -1;
+  float v = 0.f;
+  template <bool TAIL>
+  __device__ __forceinline__ Entry checked(const DistillParams& p) const {
+    const bool there = id >= 0 && id < p.vocab;
+    return Entry{there ? (int)id : -1, there ? v * (TAIL ? 1.f : p.teacher_scale) : -INFINITY};
+  }
+};
+struct TeacherSums {
+  float m[kMaxList / 32], s[kMaxList / 32];
 };
 
-// Fills t from the row's list, by the first warp; visible to the others after the next barrier.
+__device__ __forceinline__ RawEntry load_entry(const DistillParams& p, int64_t r) {
+  RawEntry e;
+  if ((int)threadIdx.x < p.list_k) {
+    const int64_t at = r * p.list_k + threadIdx.x;
+    e.id = p.ids[at];
+    e.v = p.teacher[at];
+  }
+  return e;
+}
+
+// Before a barrier: what a warp of the list gives to the sum.  Returns exp(v - the warp's m).
 template <bool TAIL>
-__device__ __forceinline__ void load_teacher(const DistillParams& p, int64_t r, Teacher& t) {
-  if (threadIdx.x >= 32) return;
-  constexpr int N = kMaxList / 32;
-  const int lane = threadIdx.x, n = p.list_k;
-  float v[N];
-  float m = TAIL ? 0.f : -FLT_MAX;   // log probabilities are taken as they are
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int j = lane + 32 * i;
-    int id = -1;
-    v[i] = -INFINITY;
-    if (j < n) {
-      const int64_t id64 = p.ids[r * n + j];
-      if (id64 >= 0 && id64 < p.vocab) {
-        id = (int)id64;
-        v[i] = p.teacher[r * n + j] * (TAIL ? 1.f : p.teacher_scale);
-      }
-    }
-    t.list.id[j] = id;
-    if (!TAIL) m = fmaxf(m, v[i]);
-  }
-  if (!TAIL) m = warp_max(m);
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    v[i] = 32 * i < n ? expf(v[i] - m) : 0.f;
-    s += v[i];
-  }
+__device__ __forceinline__ float share_entry(const Entry& e, TeacherSums& t) {
+  if (threadIdx.x >= kMaxList) return 0.f;
+  const float m = TAIL ? 0.f : fmaxf(warp_max(e.v == e.v ? e.v : -FLT_MAX), -FLT_MAX);   // log probabilities are taken as they are
+  const float x = expf(e.v - m);
+  float s = x;
 #pragma unroll
   for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
-#pragma unroll
-  for (int i = 0; i < N; ++i) t.p[lane + 32 * i] = TAIL ? v[i] : s == 0.f ? 0.f : v[i] / s;   // a list with no token left asks for nothing
-  if (lane == 0) {
-    t.sum = TAIL ? s : s == 0.f ? 0.f : s == s ? 1.f : NAN;
-    t.rest = TAIL ? max_nan(0.f, 1.f - s) : 0.f;
+  if ((threadIdx.x & 31) == 0) {
+    t.m[threadIdx.x >> 5] = m;
+    t.s[threadIdx.x >> 5] = s;
   }
+  return x;
+}
+// Behind it: the entry's p, P and p_r, the latter two in all threads.
+template <bool TAIL>
+__device__ __forceinline__ float3 join_entries(float x, const TeacherSums& t) {
+  constexpr int N = kMaxList / 32;
+  if (TAIL) {
+    const float s = t.s[0] + t.s[1] + t.s[2] + t.s[3];
+    return make_float3(x, s, max_nan(0.f, 1.f - s));
+  }
+  float m = t.m[0], s = 0.f;
+#pragma unroll
+  for (int i = 1; i < N; ++i) m = fmaxf(m, t.m[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) s += t.s[i] * ex2((t.m[i] - m) * kLog2e);
+  if (s == 0.f) return make_float3(0.f, 0.f, 0.f);   // a list with no token left asks for nothing
+  const float own = threadIdx.x < kMaxList ? t.m[threadIdx.x >> 5] : m;
+  return make_float3(x * ex2((own - m) * kLog2e) / s, s == s ? 1.f : NAN, 0.f);
 }
 
 template <bool TAIL>
-__device__ __forceinline__ Coef distill_coef(const DistillParams& p, const Teacher& t, float m, float ls, float lr, float w) {
+__device__ __forceinline__ Coef distill_coef(const DistillParams& p, float sum, float rest, float m, float ls, float lr, float w) {
   Coef c;
   c.k = p.scale * kLog2e;
   c.m = m;
   c.beta = 0.f;
   c.off_l = ls * kLog2e;
-  c.alpha_l = w * p.scale * (t.sum + t.rest);
+  c.alpha_l = w * p.scale * (sum + rest);
   if (TAIL) {
     const bool some = lr != -INFINITY;
     c.off = some ? lr * kLog2e : 0.f;
-    c.alpha = some ? w * p.scale * ((t.sum + t.rest) * expf(lr - ls) - t.rest) : 0.f;
+    c.alpha = some ? w * p.scale * ((sum + rest) * ex2((lr - ls) * kLog2e) - rest) : 0.f;
   } else {
     c.off = c.off_l;
     c.alpha = c.alpha_l;
@@ -101,159 +119,260 @@ struct Found {
   Acc dense, listed;
 };
 
-// Rows are read once: every block of the cluster copies its part to shared memory, the blocks exchange their sums, and
-// the gradient is computed from the copy.  A part that does not fit is taken in pieces and read again for the gradient.
-template <int DT, bool TAIL>
-__global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillParams p) {
+// The one or two granules of a part that the row covers in part, held by threads 0 and 1 of the block.
+template <int DT>
+struct Edge {
+  using T = typename Elem<DT>::T;
+  T v[Elem<DT>::VE];
+  __device__ __forceinline__ void load(const Row<DT>& row, const Part<DT>& part) {   // bits as they are: nothing waits for them yet
+    if ((int)threadIdx.x >= part.n_all - part.n_int) return;
+    const int at = part.granule(part.n_int + threadIdx.x) * Elem<DT>::VE;
+#pragma unroll
+    for (int e = 0; e < Elem<DT>::VE; ++e) v[e] = at + e >= row.ph && at + e < row.end ? row.granule0[at + e] : Elem<DT>::from(-INFINITY);
+  }
+  __device__ __forceinline__ uint4 raw() const {
+    float x[Elem<DT>::VE];
+#pragma unroll
+    for (int e = 0; e < Elem<DT>::VE; ++e) x[e] = Elem<DT>::to(v[e]);
+    return Elem<DT>::pack(x);
+  }
+};
+
+// A cluster of `split` blocks takes rows one after the other; each block has a part of the row.  HELD: the part lies in
+// shared memory, where a thread uses only the granules that it copied itself, and the gradient is computed from there, so a row
+// is read once; as soon as a granule has been used for the last time its place takes the next row's, which is under way
+// while this one is finished.  A byte a granule (on_list) says which of its tokens are on the list: with a remainder they
+// leave the sum.  Not HELD: a part too large for that is read twice.
+template <int DT, bool TAIL, bool HELD>
+__global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const DistillParams p) {
   using E = Elem<DT>;
   constexpr int VE = E::VE, T = kDistillThreads, U = 4;
   extern __shared__ uint4 held[];
-  __shared__ Teacher t;
-  __shared__ Warps8 buf[2];
-  __shared__ Found found[kMaxSplit];
+  __shared__ List lists[2];          // of this row and the one before
+  __shared__ TeacherSums teacher;
+  __shared__ Warps<T / 32> buf[2];
+  __shared__ Found found[2][kMaxSplit];
   __shared__ float red[kMaxList / 32];
+  __shared__ int repeats[2];         // whether a column comes twice on the list
+  uint32_t* const on_list = reinterpret_cast<uint32_t*>(held + (HELD ? p.hold : 0));
+  const uint8_t* const marks = reinterpret_cast<const uint8_t*>(on_list);
+  uint4* const mine = held + threadIdx.x;
   const int split = p.split, rank = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x, n = p.list_k;
-  const int64_t r = blockIdx.x / split;
+  const int64_t step = gridDim.x / split;
+  int64_t r = blockIdx.x / split;
   if (split > 1) ptx::cluster_arrive_relaxed();
-  const Row<DT> in(p.logits, r, p.stride, p.vocab);
-  const Part<DT> part(in, rank, split);
   const float k = p.scale * kLog2e;
-  typename E::T* cells = reinterpret_cast<typename E::T*>(held);
+  const bool grad = p.dlogits != nullptr;
 
-  Sums<DT, false> sums(k);
-  Acc listed;
-  float zk = -INFINITY;   // the listed token's logit: of all tokens in the first block, of the part's own in the others
-  int id = -1;
-  bool first = false;     // not a repetition of an earlier entry
-  for (int b0 = 0; b0 < part.n_all || b0 == 0; b0 += p.hold) {
-    const int size = min(part.n_all - b0, p.hold);
-    if (b0 > 0) __syncthreads();   // the previous piece has been read
-    for (int i = tid; i < size; i += T) {
-      if (b0 + i < part.n_int) copy_async(&held[i], in.at(part.w0 + b0 + i));
-      else held[i] = part.raw(in, b0 + i);
-    }
-    if (b0 == 0) load_teacher<TAIL>(p, r, t);
-    copy_async_wait();
-    __syncthreads();
-    if (b0 == 0 && tid < n) {
-      id = t.list.id[tid];
-      if (rank == 0 && id >= 0) zk = E::to(in.column(id));
-      first = TAIL && id >= 0 && !repeated(t.list, n, tid, true);
-    }
-    bool here = id >= 0 && part.has(in.ph + id);
-    int at = 0;
-    if (here) {
-      at = (part.place((in.ph + id) / VE) - b0) * VE + (in.ph + id) % VE;
-      here = at >= 0 && at < size * VE;
-    }
-    if (here) {
-      zk = E::to(cells[at]);
-      if (first) listed.add_one(zk, k);
-    }
-    if (TAIL) {   // listed tokens leave the sum over the remainder
-      __syncthreads();
-      if (here) cells[at] = E::from(-INFINITY);
-      __syncthreads();
-    }
-    for (int i = tid; i < size; i += T * U) {
-      uint4 g[U];
-      float mx = -INFINITY;
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (i + u * T < size) {
-          g[u] = held[i + u * T];
-          mx = max_nan(mx, E::largest(g[u]));
-        }
-      sums.raise(mx);
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (i + u * T < size) sums.add(g[u]);
-    }
+  RawEntry ahead = load_entry(p, r);
+  float w = p.weight ? p.weight[r] : 1.f;
+  Row<DT> in(p.logits, r, p.stride, p.vocab);
+  Part<DT> part(in, rank, p.each);
+  Edge<DT> edge;
+  if (HELD) {
+    const uint4* const from = reinterpret_cast<const uint4*>(in.at(part.w0));
+#pragma unroll 4
+    for (int i = tid; i < part.n_int; i += T) copy_async(&held[i], from + i);
+    edge.load(in, part);
   }
-  sums.flush();
-  warp_share<false>(sums.a, k, buf[0]);
-  if (TAIL) warp_share<false>(listed, k, buf[1]);
+  for (int i = tid; i * 4 < p.hold; i += T) on_list[i] = 0;
+  if (tid == 0) repeats[0] = 0;
   __syncthreads();
-  Acc dense = warps_join<false>(k, buf[0]);
-  if (TAIL) listed = warps_join<false>(k, buf[1]);
-  if (split > 1) {
-    ptx::cluster_wait();   // all blocks have started
-    if (tid < split) {
-      const uint32_t to = ptx::mapa(ptx::smem_u32(&found[rank]), tid);
-      ptx::st_shared_cluster_u32(to, __float_as_uint(dense.m));
-      ptx::st_shared_cluster_u32(to + 4, __float_as_uint(dense.s));
-      if (TAIL) {
-        ptx::st_shared_cluster_u32(to + sizeof(Acc), __float_as_uint(listed.m));
-        ptx::st_shared_cluster_u32(to + sizeof(Acc) + 4, __float_as_uint(listed.s));
+  for (int turn = 0; r < p.rows; r += step, turn ^= 1) {
+    List& list = lists[turn];
+    const Entry entry = ahead.checked<TAIL>(p);
+    Sums<DT, false> sums(k);
+    const bool own = entry.id >= 0 && part.has(in.ph + entry.id);
+    float zk = -INFINITY;   // the listed token's logit: of all tokens in the first block, of the part's own in the others
+    if (own || (rank == 0 && entry.id >= 0)) zk = E::to(in.column(entry.id));
+    if (tid < kMaxList) list.id[tid] = entry.id;
+    const float x = share_entry<TAIL>(entry, teacher);
+    const int mark = own ? part.place((in.ph + entry.id) / VE) : -1;   // the listed token's granule and its bit in there
+    const uint32_t bit = own ? 1u << (mark % 4 * 8 + (in.ph + entry.id) % VE) : 0;
+    bool first = false;                                                // of entries with the same column
+    if (tid == 0) repeats[turn ^ 1] = 0;
+    const int64_t r_next = r + step;
+    const bool more = r_next < p.rows;
+    const Row<DT> next(p.logits, more ? r_next : r, p.stride, p.vocab);
+    const Part<DT> next_part(next, rank, p.each);
+    const uint4* const from = reinterpret_cast<const uint4*>(next.at(next_part.w0));
+    const int n_next = HELD && more ? next_part.n_int : 0;
+
+    if (HELD) {
+      if (own) {
+        first = !(atomicOr(&on_list[mark / 4], bit) & bit);
+        if (!first) repeats[turn] = 1;
       }
-    }
-    ptx::cluster_sync();
-    dense = listed = Acc{};
-    for (int i = 0; i < split; ++i) {
-      dense.merge(Acc{found[i].dense.m, found[i].dense.s, 0.f}, k);
-      if (TAIL) listed.merge(Acc{found[i].listed.m, found[i].listed.s, 0.f}, k);
-    }
-  }
-  Acc all = dense;
-  if (TAIL) all.merge(listed, k);
-  const float ls = log_sum(all);
-  const float lr = !TAIL ? 0.f : dense.s == 0.f ? -INFINITY : (dense.m - all.m) * p.scale + log_sum(dense);
-  const float pk = id >= 0 ? t.p[tid] : 0.f;
-  if (rank == 0 && tid < kMaxList) {
-    float l = 0.f;
-    if (!(pk == 0.f)) l = ls == -INFINITY && pk > 0.f ? INFINITY : pk * (logf(pk) - ((zk - all.m) * p.scale - ls));
-    if (TAIL && tid == 0 && !(t.rest == 0.f)) {
-      if (ls == -INFINITY && t.rest > 0.f) l = INFINITY;
-      else if (!(lr == -INFINITY && t.rest < 1e-5f)) l += t.rest * (logf(t.rest) - (lr - ls));
-    }
+      if (TAIL) __syncthreads();
+      copy_async_wait();
+      batches<T, U>(part.n_int, [&](int b, auto all) {
+        constexpr bool ALL = decltype(all)::value;
+        const int left = part.n_int - b - tid;
+        uint4 g[U];
+        uint32_t bits[U], any = 0;
+        float mx = -INFINITY;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
-    if ((tid & 31) == 0) red[tid >> 5] = l;
-  }
-  if (p.dlogits) {
-    const float w = p.weight ? p.weight[r] : 1.f;
-    const Coef c = distill_coef<TAIL>(p, t, all.m, ls, lr, w);
-    const Row<DT> out(p.dlogits, r, p.grad_stride, p.vocab);
-    if (tid < n) t.list.add[tid] = -w * p.scale * pk;
-    if (part.n_all > p.hold) {
-      __syncthreads();
-      grad_part<DT, false>(in, out, part, c, t.list, n);
-    } else {
-      const Dense<DT, false> of(c);
-      const bool alike = in.ph == out.ph;
-      for (int i = tid; i < part.n_all; i += T) {
-        float x[VE];
-        of(held[i], x);
-        store_granule<DT>(in, out, part, alike, i, x);
+        for (int u = 0; u < U; ++u)
+          if (ALL || u * T < left) {
+            g[u] = mine[b + u * T];
+            if (TAIL) any |= bits[u] = marks[b + u * T + tid];
+          }
+        if (TAIL && any) {
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (ALL || u * T < left) g[u] = without<DT>(g[u], bits[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (ALL || u * T < left) mx = max_nan(mx, E::largest(g[u]));
+        sums.template add<ALL>(g, mx, left, T);
+      });
+      if (tid < part.n_all - part.n_int) {
+        const uint4 g[1] = {without<DT>(edge.raw(), TAIL ? marks[part.n_int + tid] : 0)};
+        sums.template add<true>(g, E::largest(g[0]));
       }
-      __syncthreads();   // the dense part of the listed columns is written before what replaces it
-      if (id >= 0 && part.has(in.ph + id) && !c.zero) out.column(id) = E::from(grad_of(zk, c) + add_of_column(t.list, n, tid));
+      if (!grad)
+        for (int i = tid; i < n_next; i += T) copy_async(&held[i], from + i);
+    } else {
+      for (int b0 = 0; b0 < part.n_all; b0 += p.hold) {   // p.hold granules at a time have marks
+        const bool in_piece = TAIL && own && mark >= b0 && mark < b0 + p.hold;
+        if (TAIL) {
+          if (in_piece) first = !(atomicOr(&on_list[(mark - b0) / 4], bit) & bit);
+          __syncthreads();
+        }
+        for (int i = b0 + tid; i < min(part.n_all, b0 + p.hold); i += T) {
+          const uint4 g[1] = {without<DT>(part.raw(in, i), TAIL ? marks[i - b0] : 0)};
+          sums.template add<true>(g, E::largest(g[0]));
+        }
+        if (TAIL) {
+          __syncthreads();
+          if (in_piece) on_list[(mark - b0) / 4] = 0;
+          __syncthreads();
+        }
+      }
     }
-  } else {
+    sums.flush();
+    warp_share<false>(sums.a, k, buf[0]);
+    if (TAIL) {
+      Acc listed;
+      if (first) listed.add_one(zk, k);
+      warp_share<false>(listed, k, buf[1]);
+    }
     __syncthreads();
-  }
-  if (rank == 0 && tid == 0) {
-    p.loss[r] = red[0] + red[1] + red[2] + red[3];
-    if (p.stats) {
-      p.stats[3 * r] = ls == -INFINITY ? -INFINITY : all.m;
-      p.stats[3 * r + 1] = ls;
-      p.stats[3 * r + 2] = ls == -INFINITY && TAIL ? -INFINITY : lr;
+    if (HELD && own) on_list[mark / 4] = 0;
+    Acc dense = warps_join<false>(k, buf[0]), listed;
+    if (TAIL) listed = warps_join<false>(k, buf[1]);
+    const float3 teach = join_entries<TAIL>(x, teacher);
+    const float pk = entry.id >= 0 ? teach.x : 0.f;
+    if (split > 1) {
+      if (r < step) ptx::cluster_wait();   // the first row: all blocks have started
+      if (tid < split) {
+        const uint32_t to = ptx::mapa(ptx::smem_u32(&found[turn][rank]), tid);
+        ptx::st_shared_cluster_u32(to, __float_as_uint(dense.m));
+        ptx::st_shared_cluster_u32(to + 4, __float_as_uint(dense.s));
+        if (TAIL) {
+          ptx::st_shared_cluster_u32(to + sizeof(Acc), __float_as_uint(listed.m));
+          ptx::st_shared_cluster_u32(to + sizeof(Acc) + 4, __float_as_uint(listed.s));
+        }
+      }
+      ptx::cluster_sync();   // behind it no block reads logits of another's part, and the gradient may replace them
+      dense = listed = Acc{};
+      for (int i = 0; i < split; ++i) {
+        dense.merge(Acc{found[turn][i].dense.m, found[turn][i].dense.s, 0.f}, k);
+        if (TAIL) listed.merge(Acc{found[turn][i].listed.m, found[turn][i].listed.s, 0.f}, k);
+      }
     }
+    Acc all = dense;
+    if (TAIL) all.merge(listed, k);
+    const float ls = log_sum(all);
+    const float lr = !TAIL ? 0.f : dense.s == 0.f ? -INFINITY : (dense.m - all.m) * p.scale + log_sum(dense);
+    Coef coef;
+    const float w_row = w;
+    const Row<DT> out(p.dlogits, grad ? r : 0, p.grad_stride, p.vocab);
+    if (more) {
+      ahead = load_entry(p, r_next);
+      if (p.weight) w = p.weight[r_next];
+    }
+    bool rep = false;
+    if (grad) {
+      coef = distill_coef<TAIL>(p, teach.y, teach.z, all.m, ls, lr, w_row);
+      if (tid < n) list.add[tid] = -w_row * p.scale * pk;
+      rep = own && (HELD ? repeats[turn] != 0 : repeated(list, n, tid));
+      const Dense<DT, false> dense_part(coef);
+      if (HELD) {
+        if (tid < part.n_all - part.n_int) write_elements(in, out, dense_part, part.granule(part.n_int + tid), edge.raw());
+        if (more) edge.load(next, next_part);
+        const bool alike = in.ph == out.ph && dense_part.plain();
+        const int both = alike ? more ? min(part.n_int, n_next) : part.n_int : 0;
+        uint4* const to = reinterpret_cast<uint4*>(out.at(part.w0)) + tid;
+        int b = 0;
+        for (; b + T * U <= both; b += T * U) {
+          uint4 g[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) g[u] = mine[b + u * T];
+#pragma unroll
+          for (int u = 0; u < U; ++u) st_global_v4(to + b + u * T, dense_of(dense_part, g[u]));
+          if (more) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) copy_async(mine + b + u * T, from + b + u * T + tid);
+          }
+        }
+        for (int i = b + tid; i < max(part.n_int, n_next); i += T) {
+          if (i < part.n_int) {
+            if (alike) st_global_v4(to + i - tid, dense_of(dense_part, held[i]));
+            else write_elements(in, out, dense_part, part.w0 + i, held[i]);
+          }
+          if (i < n_next) copy_async(&held[i], from + i);
+        }
+      } else {
+        if (split == 1) __syncthreads();   // the listed logits have been read
+        for (int i = tid; i < part.n_all; i += T) write_elements(in, out, dense_part, part.granule(i), part.raw(in, i));
+      }
+    } else if (HELD && more) {
+      edge.load(next, next_part);
+    }
+    if (rank == 0 && tid < kMaxList) {
+      float l = 0.f;
+      if (!(pk == 0.f)) l = ls == -INFINITY && pk > 0.f ? INFINITY : pk * (logf(pk) - ((zk - all.m) * p.scale - ls));
+      if (TAIL && tid == 0 && !(teach.z == 0.f)) {
+        if (ls == -INFINITY && teach.z > 0.f) l = INFINITY;
+        else if (!(lr == -INFINITY && teach.z < 1e-5f)) l += teach.z * (logf(teach.z) - (lr - ls));
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
+      if ((tid & 31) == 0) red[tid >> 5] = l;
+    }
+    __syncthreads();   // the dense part of the listed columns is written before what replaces it
+    if (grad && own && !coef.zero) out.column(entry.id) = E::from(grad_of(zk, coef) + (rep ? sum_of_column(list, n, tid) : list.add[tid]));
+    if (rank == 0 && tid == 0) {
+      p.loss[r] = red[0] + red[1] + red[2] + red[3];
+      if (p.stats) {
+        p.stats[3 * r] = ls == -INFINITY ? -INFINITY : all.m;
+        p.stats[3 * r + 1] = ls;
+        p.stats[3 * r + 2] = ls == -INFINITY && TAIL ? -INFINITY : lr;
+      }
+    }
+    in = next;
+    part = next_part;
   }
 }
 
 template <int DT, bool TAIL>
-__global__ void __launch_bounds__(kDistillThreads) distill_grad_kernel(const DistillParams p) {
-  __shared__ Teacher t;
+__global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const DistillParams p) {
+  __shared__ List list;
+  __shared__ TeacherSums teacher;
   const int64_t r = blockIdx.x / p.split;
+  const int tid = threadIdx.x;
   const Row<DT> in(p.logits, r, p.stride, p.vocab), out(p.dlogits, r, p.grad_stride, p.vocab);
-  load_teacher<TAIL>(p, r, t);
+  const float w = p.weight[r], m = p.stats[3 * r], ls = p.stats[3 * r + 1], lr = p.stats[3 * r + 2];
+  const Entry e = load_entry(p, r).checked<TAIL>(p);
+  if (tid < kMaxList) list.id[tid] = e.id;
+  const float x = share_entry<TAIL>(e, teacher);
   __syncthreads();
-  const float w = p.weight[r];
-  const Coef c = distill_coef<TAIL>(p, t, p.stats[3 * r], p.stats[3 * r + 1], p.stats[3 * r + 2], w);
-  if (threadIdx.x < kMaxList) t.list.add[threadIdx.x] = -w * p.scale * t.p[threadIdx.x];
-  __syncthreads();
-  grad_part<DT, false>(in, out, Part<DT>(in, blockIdx.x % p.split, p.split), c, t.list, p.list_k);
+  const float3 teach = join_entries<TAIL>(x, teacher);
+  if (tid < kMaxList) list.add[tid] = -w * p.scale * (e.id >= 0 ? teach.x : 0.f);
+  const Coef c = distill_coef<TAIL>(p, teach.y, teach.z, m, ls, lr, w);
+  grad_part<DT, false>(in, out, Part<DT>(in, blockIdx.x % p.split, p.each), c, list, p.list_k);
 }
 
 }  // namespace rows
@@ -265,7 +384,7 @@ using namespace iris::rows;
 namespace {
 
 constexpr int kHoldBytes = 192 * 1024;   // of shared memory at most for a part
-static int part_kb() { const char* e = getenv("PARTKB"); return e ? atoi(e) : 56; }
+static int part_kb() { const char* e = getenv("PARTKB"); return e ? atoi(e) : 60; }
 #define kPartBytes (part_kb() * 1024)
 constexpr int kMaxDevices = 64;
 
@@ -294,6 +413,7 @@ DistillParams params_of(const iris_distill_args* a, int64_t stride, int64_t gstr
   p.logits = a->logits;
   p.stride = stride;
   p.grad_stride = gstride;
+  p.rows = (int)a->rows;
   p.vocab = (int)a->vocab;
   p.list_k = a->list_k;
   p.scale = a->scale;
@@ -307,41 +427,53 @@ DistillParams params_of(const iris_distill_args* a, int64_t stride, int64_t gstr
   return p;
 }
 
-template <int DT, bool TAIL>
-int launch_distill(DistillParams p, int64_t rows, cudaStream_t st) {
+template <int DT, bool TAIL, bool HELD>
+int launch_distill(const DistillParams& p, cudaStream_t st) {
+  const auto kernel = distill_kernel<DT, TAIL, HELD>;
+  const int bytes = (HELD ? p.hold * 16 : 0) + (p.hold + 3) / 4 * 4;
   static bool configured[kMaxDevices] = {};
   int dev = -1;
   IRIS_CUDA_TRY(cudaGetDevice(&dev));
   if (dev >= kMaxDevices || !configured[dev]) {
-    IRIS_CUDA_TRY(cudaFuncSetAttribute(distill_kernel<DT, TAIL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldBytes));
+    IRIS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldBytes + kHoldBytes / 16));
     if (dev < kMaxDevices) configured[dev] = true;
   }
-  // A row is shared by a cluster of blocks until a part is at most kPartBytes, or while the rows alone leave SMs without
-  // work and every thread still has a granule.
-  const int64_t granules = (p.vocab + 2 * Row<DT>::VE - 2) / Row<DT>::VE;   // of a row, wherever it starts
-  int split = 1;
-  while (split < kMaxSplit && (granules * 16 > (int64_t)split * kPartBytes || (rows * split < 2 * kSms && granules >= (int64_t)split * 2 * kDistillThreads))) ++split;
-  p.split = split;
-  const int64_t need = std::max<int64_t>(1, (granules + split - 1) / split);
-  p.hold = (int)std::min<int64_t>(need, kHoldBytes / 16);
+  // Blocks of 256 threads that an SM takes at a time: 4 by registers, fewer by shared memory (228 KB, 4 KB of it a block's
+  // own variables and reserve).
+  const int per_sm = std::max(1, std::min(4, (int)(228 * 1024 / (bytes + 5 * 1024))));
+  const int64_t clusters = std::min<int64_t>(p.rows, std::max(1, kSms * per_sm / p.split));
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(rows * split));
+  cfg.gridDim = dim3((unsigned)(clusters * p.split));
   cfg.blockDim = dim3(kDistillThreads);
-  cfg.dynamicSmemBytes = (size_t)p.hold * 16;
+  cfg.dynamicSmemBytes = (size_t)bytes;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)split;
+  at[0].val.clusterDim.x = (unsigned)p.split;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = split > 1 ? 1 : 0;
-  IRIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, distill_kernel<DT, TAIL>, p));
+  cfg.numAttrs = p.split > 1 ? 1 : 0;
+  IRIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
   return IRIS_OK;
+}
+
+template <int DT>
+int launch_distill(DistillParams p, bool tail, cudaStream_t st) {
+  // A row is shared by a cluster of blocks until a part is at most kPartBytes, or while the rows alone leave SMs without
+  // work and every thread still has a granule.
+  const int64_t granules = part_granules(p.vocab, DT, 1);
+  int split = 1;
+  while (split < kMaxSplit && (granules * 16 > (int64_t)split * kPartBytes || ((int64_t)p.rows * split < 2 * kSms && granules >= (int64_t)split * 2 * kDistillThreads))) ++split;
+  p.split = split;
+  p.each = part_granules(p.vocab, DT, split);
+  p.hold = std::max(1, std::min(p.each, kHoldBytes / 16));
+  if (p.each <= kHoldBytes / 16) return tail ? launch_distill<DT, true, true>(p, st) : launch_distill<DT, false, true>(p, st);
+  return tail ? launch_distill<DT, true, false>(p, st) : launch_distill<DT, false, false>(p, st);
 }
 
 template <int DT, bool TAIL>
 int launch_distill_grad(const DistillParams& p, int64_t rows, cudaStream_t st) {
-  distill_grad_kernel<DT, TAIL><<<(unsigned)(rows * p.split), kDistillThreads, 0, st>>>(p);
+  distill_grad_kernel<DT, TAIL><<<(unsigned)(rows * p.split), kGradThreads, 0, st>>>(p);
   IRIS_CUDA_TRY(cudaGetLastError());
   return IRIS_OK;
 }
@@ -356,12 +488,11 @@ extern "C" int iris_distill_topk(const iris_distill_args* a, void* stream) {
   IRIS_CHECK(check_aligned(fn, "loss", a->loss, 4, true));
   IRIS_CHECK(check_aligned(fn, "stats", a->stats, 4, false));
   const DistillParams p = params_of(a, stride, gstride);
-  if (a->rows > INT32_MAX / kMaxSplit) return fail(IRIS_ERR_UNSUPPORTED, "%s: more than 2^28 rows", fn);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool tail = a->mode == IRIS_DISTILL_TAIL;
-  if (a->dtype == IRIS_BF16) return tail ? launch_distill<IRIS_BF16, true>(p, a->rows, st) : launch_distill<IRIS_BF16, false>(p, a->rows, st);
-  if (a->dtype == IRIS_F16) return tail ? launch_distill<IRIS_F16, true>(p, a->rows, st) : launch_distill<IRIS_F16, false>(p, a->rows, st);
-  return tail ? launch_distill<IRIS_F32, true>(p, a->rows, st) : launch_distill<IRIS_F32, false>(p, a->rows, st);
+  if (a->dtype == IRIS_BF16) return launch_distill<IRIS_BF16>(p, tail, st);
+  if (a->dtype == IRIS_F16) return launch_distill<IRIS_F16>(p, tail, st);
+  return launch_distill<IRIS_F32>(p, tail, st);
 }
 
 extern "C" int iris_distill_topk_backward(const iris_distill_args* a, void* stream) {
@@ -374,6 +505,7 @@ extern "C" int iris_distill_topk_backward(const iris_distill_args* a, void* stre
   if (!a->dlogits) return fail(IRIS_ERR_ARG, "%s: dlogits is NULL", fn);
   DistillParams p = params_of(a, stride, gstride);
   p.split = grad_parts(a->vocab, a->dtype);
+  p.each = part_granules(a->vocab, a->dtype, p.split);
   if (a->rows * p.split > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 blocks", fn);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool tail = a->mode == IRIS_DISTILL_TAIL;

@@ -27,19 +27,17 @@ __device__ __forceinline__ float grad_of(float z, const Coef& c) {   // on the l
   return ex2(y) * fmaf(c.beta, max_nan(y, kFloor), c.alpha_l);
 }
 
-// Whether another entry of the first n has entry i's column; `before`: an earlier one.
-__device__ __forceinline__ bool repeated(const List& l, int n, int i, bool before) {
+// Whether another entry of the first n has entry i's column.
+__device__ __forceinline__ bool repeated(const List& l, int n, int i) {
   const int id = l.id[i];
   int same = 0;
   for (int j = 0; j < n; j += 4) {
     const int4 o = *reinterpret_cast<const int4*>(&l.id[j]);
-    same += (o.x == id && (!before || j < i)) + (o.y == id && (!before || j + 1 < i)) + (o.z == id && (!before || j + 2 < i)) +
-            (o.w == id && (!before || j + 3 < i));
+    same += (o.x == id) + (o.y == id) + (o.z == id) + (o.w == id);
   }
-  return same > (before ? 0 : 1);
+  return same > 1;
 }
-__device__ __forceinline__ float add_of_column(const List& l, int n, int i) {
-  if (!repeated(l, n, i, false)) return l.add[i];
+__device__ __forceinline__ float sum_of_column(const List& l, int n, int i) {
   float s = 0.f;
   const int id = l.id[i];
   for (int j = 0; j < n; ++j) s += l.id[j] == id ? l.add[j] : 0.f;
@@ -50,9 +48,10 @@ __device__ __forceinline__ float add_of_column(const List& l, int n, int i) {
 // subtract, scale, multiply and pack.
 template <int DT, bool BETA>
 struct Dense {
+  static constexpr int VE = Elem<DT>::VE;
   uint64_t k2, minus_m2, minus_off2, alpha2, beta2;
   uint32_t floor = 0;
-  bool lift = false;
+  bool lift = true;
   Coef c;
   __device__ __forceinline__ explicit Dense(const Coef& c_) : c(c_) {
     k2 = pair(c.k, c.k);
@@ -62,83 +61,87 @@ struct Dense {
     beta2 = pair(c.beta, c.beta);
     if (BETA) lift = lift_floor<DT>(c.m, c.k, floor);   // off >= 0 lowers the exponents further
   }
-  __device__ __forceinline__ void operator()(const uint4& g, float (&x)[Elem<DT>::VE]) const {
-    constexpr int VE = Elem<DT>::VE;
-    if (c.zero) {
+  __device__ __forceinline__ bool plain() const { return c.zero || lift; }
+  __device__ __forceinline__ void operator()(const uint4& g, float (&x)[VE]) const {   // where lift and not zero
+    Elem<DT>::unpack(BETA ? Elem<DT>::at_least(g, floor) : g, x);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) x[e] = 0.f;
-    } else if (!BETA || lift) {
-      Elem<DT>::unpack(BETA ? Elem<DT>::at_least(g, floor) : g, x);
+    for (int e = 0; e < VE; e += 2) {
+      const uint64_t y2 = fma2f(add2f(pair(x[e], x[e + 1]), minus_m2), k2, minus_off2);
+      const float2 y = unpair(y2);
+      const float2 d = unpair(mul2f(pair(ex2(y.x), ex2(y.y)), BETA ? fma2f(beta2, y2, alpha2) : alpha2));
+      x[e] = d.x;
+      x[e + 1] = d.y;
+    }
+  }
+  __device__ __forceinline__ void one_by_one(const uint4& g, float (&x)[VE]) const {
+    Elem<DT>::unpack(g, x);
 #pragma unroll
-      for (int e = 0; e < VE; e += 2) {
-        const uint64_t y2 = fma2f(add2f(pair(x[e], x[e + 1]), minus_m2), k2, minus_off2);
-        const float2 y = unpair(y2);
-        const float2 d = unpair(mul2f(pair(ex2(y.x), ex2(y.y)), BETA ? fma2f(beta2, y2, alpha2) : alpha2));
-        x[e] = d.x;
-        x[e + 1] = d.y;
-      }
-    } else {
-      Elem<DT>::unpack(g, x);
-#pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        const float y = (x[e] - c.m) * c.k - c.off;
-        x[e] = ex2(y) * fmaf(c.beta, max_nan(y, kFloor), c.alpha);
-      }
+    for (int e = 0; e < VE; ++e) {
+      const float y = (x[e] - c.m) * c.k - c.off;
+      x[e] = c.zero ? 0.f : ex2(y) * fmaf(c.beta, max_nan(y, kFloor), c.alpha);
     }
   }
 };
 
-// Granule i of a part of the gradient: at once where it lies inside the row and the two matrices' rows lie alike in
-// memory, else element by element.
-template <int DT>
-__device__ __forceinline__ void store_granule(const Row<DT>& in, const Row<DT>& out, const Part<DT>& part, bool alike, int i,
-                                              const float (&x)[Elem<DT>::VE]) {
-  using E = Elem<DT>;
-  if (alike && i < part.n_int) {
-    st_global_v4(out.at(part.w0 + i), E::pack(x));
-  } else {
-    const int at = part.granule(i) * E::VE;
-#pragma unroll
-    for (int e = 0; e < E::VE; ++e)
-      if (at + e >= in.ph && at + e < in.end) out.column(at + e - in.ph) = E::from(x[e]);
-  }
-}
-
 constexpr int kGradThreads = 256;
 constexpr int kGradGranules = 4;   // that a thread has in flight
 
-// A part of a row, by all kGradThreads threads of the block; listed columns outside it are another block's.
+// The dense gradient of a granule element by element, for what the row covers in part and where the rows of the gradient
+// do not lie in memory as those of the logits.
+template <int DT, bool BETA>
+__device__ __forceinline__ void write_elements(const Row<DT>& in, const Row<DT>& out, const Dense<DT, BETA>& dense, int granule, const uint4& g) {
+  using E = Elem<DT>;
+  float x[E::VE];
+  dense.one_by_one(g, x);
+  const int at = granule * E::VE;
+#pragma unroll
+  for (int e = 0; e < E::VE; ++e)
+    if (at + e >= in.ph && at + e < in.end) out.column(at + e - in.ph) = E::from(x[e]);
+}
+template <int DT, bool BETA>
+__device__ __forceinline__ uint4 dense_of(const Dense<DT, BETA>& dense, const uint4& g) {
+  if (dense.c.zero) return make_uint4(0, 0, 0, 0);
+  float x[Elem<DT>::VE];
+  dense(g, x);
+  return Elem<DT>::pack(x);
+}
+
+// A part of a row; listed columns outside it are another block's.  The list has been written before the last barrier
+// (id) or the next one (add).
 template <int DT, bool BETA>
 __device__ __forceinline__ void grad_part(const Row<DT>& in, const Row<DT>& out, const Part<DT>& part, const Coef& c, const List& list, int n) {
-  constexpr int VE = Elem<DT>::VE, U = kGradGranules, T = kGradThreads;
   const int tid = threadIdx.x;
-  float zl = 0.f, add = 0.f;
-  bool mine = false;
-  if (tid < n && !c.zero) {
-    mine = list.id[tid] >= 0 && part.has(in.ph + list.id[tid]);
-    if (mine) {
-      zl = Elem<DT>::to(in.column(list.id[tid]));
-      add = add_of_column(list, n, tid);
-    }
+  float zl = 0.f;
+  bool rep = false;
+  const bool mine = tid < n && !c.zero && list.id[tid] >= 0 && part.has(in.ph + list.id[tid]);
+  if (mine) {
+    zl = Elem<DT>::to(in.column(list.id[tid]));
+    rep = repeated(list, n, tid);
   }
-  const Dense<DT, BETA> dense(c);
-  const bool alike = in.ph == out.ph;
   __syncthreads();   // the gradient may replace the logits: listed ones have been read
-  for (int i = tid; i < part.n_all; i += T * U) {
-    uint4 g[U];
+  const Dense<DT, BETA> dense(c);
+  constexpr int T = kGradThreads, U = kGradGranules;
+  if (in.ph == out.ph && dense.plain()) {
+    const uint4* const from = reinterpret_cast<const uint4*>(in.at(part.w0)) + tid;
+    uint4* const to = reinterpret_cast<uint4*>(out.at(part.w0)) + tid;
+    batches<T, U>(part.n_int, [&](int b, auto all) {
+      constexpr bool ALL = decltype(all)::value;
+      const int left = part.n_int - b - tid;
+      uint4 g[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * T < part.n_all) g[u] = part.raw(in, i + u * T);
+      for (int u = 0; u < U; ++u)
+        if ((ALL || u * T < left) && !c.zero) g[u] = ld_once(from + b + u * T);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * T < part.n_all) {
-        float x[VE];
-        dense(g[u], x);
-        store_granule<DT>(in, out, part, alike, i + u * T, x);
-      }
+      for (int u = 0; u < U; ++u)
+        if (ALL || u * T < left) st_global_v4(to + b + u * T, dense_of(dense, g[u]));
+    });
+    if (tid < part.n_all - part.n_int) write_elements(in, out, dense, part.granule(part.n_int + tid), part.raw(in, part.n_int + tid));
+  } else {
+#pragma unroll 1
+    for (int i = tid; i < part.n_all; i += T) write_elements(in, out, dense, part.granule(i), part.raw(in, i));
   }
   __syncthreads();   // the dense part of the listed columns is written before what replaces it
-  if (mine) out.column(list.id[tid]) = Elem<DT>::from(grad_of(zl, c) + add);
+  if (mine) out.column(list.id[tid]) = Elem<DT>::from(grad_of(zl, c) + (rep ? sum_of_column(list, n, tid) : list.add[tid]));
 }
 
 // Blocks a row is cut into for a streamed gradient: about 8 granules a thread.

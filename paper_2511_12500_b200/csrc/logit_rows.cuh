@@ -9,6 +9,7 @@
 
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "iris_device.cuh"
 
@@ -189,6 +190,16 @@ template <> struct Elem<IRIS_F32> {
   }
 };
 
+// The granule with -inf in the places whose bit is set.
+template <int DT>
+__device__ __forceinline__ uint4 without(const uint4& g, uint32_t bits) {
+  float x[Elem<DT>::VE];
+  Elem<DT>::unpack(g, x);
+#pragma unroll
+  for (int e = 0; e < Elem<DT>::VE; ++e) x[e] = bits >> e & 1 ? -INFINITY : x[e];
+  return Elem<DT>::pack(x);
+}
+
 // A row of the logits (or of the gradient) as granules.
 template <int DT>
 struct Row {
@@ -234,8 +245,8 @@ template <int DT>
 struct Part {
   static constexpr int VE = Elem<DT>::VE;
   int v0, v1, w0, n_int, n_all;
-  __device__ __forceinline__ Part(const Row<DT>& row, int part, int parts) {
-    const int nv = row.granules(), each = (nv + parts - 1) / parts;
+  __device__ __forceinline__ Part(const Row<DT>& row, int part, int each) {   // each: granules of a part, the last ones have fewer
+    const int nv = row.granules();
     v0 = min(nv, part * each);
     v1 = min(nv, v0 + each);
     w0 = v0 + (v0 < v1 && v0 * VE < row.ph);
@@ -308,30 +319,54 @@ struct Sums {
     minus_m2 = pair(-a.m, -a.m);
     if (ENTROPY) lift = lift_floor<DT>(a.m, k, floor);
   }
-  __device__ __forceinline__ void add(const uint4& g) {
+  __device__ __forceinline__ void add_lifted(const uint4& g) {
     constexpr int VE = Elem<DT>::VE;
     float x[VE];
+    Elem<DT>::unpack(ENTROPY ? Elem<DT>::at_least(g, floor) : g, x);
+#pragma unroll
+    for (int e = 0; e < VE; e += 2) {
+      const uint64_t y2 = mul2f(add2f(pair(x[e], x[e + 1]), minus_m2), k2);
+      const float2 y = unpair(y2);
+      const uint64_t f = pair(ex2(y.x), ex2(y.y));
+      s2 = add2f(s2, f);
+      if (ENTROPY) t2 = fma2f(f, y2, t2);
+    }
+  }
+  __device__ __forceinline__ void add_cut(const uint4& g) {
+    constexpr int VE = Elem<DT>::VE;
+    float x[VE];
+    Elem<DT>::unpack(g, x);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      const float y = max_nan((x[e] - a.m) * k, kFloor), f = ex2(y);
+      a.s += f;
+      a.t = fmaf(f, y, a.t);
+    }
+  }
+  // Granules g[0 .. U), the first `left` of every T-th (all of them if ALL), of which mx is the largest logit.
+  template <bool ALL, int U>
+  __device__ __forceinline__ void add(const uint4 (&g)[U], float mx, int left = 0, int T = 1) {
+    raise(mx);
     if (!ENTROPY || lift) {
-      Elem<DT>::unpack(ENTROPY ? Elem<DT>::at_least(g, floor) : g, x);
 #pragma unroll
-      for (int e = 0; e < VE; e += 2) {
-        const uint64_t y2 = mul2f(add2f(pair(x[e], x[e + 1]), minus_m2), k2);
-        const float2 y = unpair(y2);
-        const uint64_t f = pair(ex2(y.x), ex2(y.y));
-        s2 = add2f(s2, f);
-        if (ENTROPY) t2 = fma2f(f, y2, t2);
-      }
-    } else {
-      Elem<DT>::unpack(g, x);
+      for (int u = 0; u < U; ++u)
+        if (ALL || u * T < left) add_lifted(g[u]);
+    } else if (mx != -INFINITY) {
 #pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        const float y = max_nan((x[e] - a.m) * k, kFloor), f = ex2(y);
-        a.s += f;
-        a.t = fmaf(f, y, a.t);
-      }
+      for (int u = 0; u < U; ++u)
+        if (ALL || u * T < left) add_cut(g[u]);
     }
   }
 };
+
+// Calls f(b, all) for batches b of T * U consecutive granules until n: with std::true_type for whole ones, of which thread
+// tid has granules b + u * T + tid, then with std::false_type for the rest, where f looks which of its own are below n.
+template <int T, int U, class F>
+__device__ __forceinline__ void batches(int n, F f) {
+  int b = 0;
+  for (; b + T * U <= n; b += T * U) f(b, std::true_type{});
+  if (b < n) f(b, std::false_type{});
+}
 
 __device__ __forceinline__ float warp_max(float x) {
   float y;
@@ -339,13 +374,14 @@ __device__ __forceinline__ float warp_max(float x) {
   return y;
 }
 
-// All threads of a block of 256 get the merged statistics, the same bits.  `buf`: 8 entries, used once a kernel or with a
-// barrier between uses.  One barrier.
-struct Warps8 {
-  Acc of[8];
+// All threads of a block of W warps (a power of two) get the merged statistics, the same bits: warp_share, a barrier,
+// warps_join.
+template <int W>
+struct Warps {
+  Acc of[W];
 };
-template <bool ENTROPY>
-__device__ __forceinline__ void warp_share(Acc a, float k, Warps8& buf) {
+template <bool ENTROPY, int W>
+__device__ __forceinline__ void warp_share(Acc a, float k, Warps<W>& buf) {
   a.rebase(warp_max(a.m), k);
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
@@ -354,12 +390,12 @@ __device__ __forceinline__ void warp_share(Acc a, float k, Warps8& buf) {
   }
   if ((threadIdx.x & 31) == 0) buf.of[threadIdx.x >> 5] = a;
 }
-template <bool ENTROPY>
-__device__ __forceinline__ Acc warps_join(float k, const Warps8& buf) {
-  Acc a = buf.of[threadIdx.x & 7];
+template <bool ENTROPY, int W>
+__device__ __forceinline__ Acc warps_join(float k, const Warps<W>& buf) {
+  Acc a = buf.of[threadIdx.x & (W - 1)];
   a.rebase(warp_max(a.m), k);
 #pragma unroll
-  for (int o = 4; o; o >>= 1) {
+  for (int o = W / 2; o; o >>= 1) {
     a.s += __shfl_xor_sync(~0u, a.s, o);
     if (ENTROPY) a.t += __shfl_xor_sync(~0u, a.t, o);
   }
@@ -397,6 +433,11 @@ inline int check_logits(const char* fn, const char* what, const void* p, int dty
   if (!p) return fail(IRIS_ERR_ARG, "%s: %s is NULL", fn, what);
   if (reinterpret_cast<uintptr_t>(p) % elem_size(dtype)) return fail(IRIS_ERR_ARG, "%s: %s is not aligned to its elements", fn, what);
   return IRIS_OK;
+}
+// Granules of a row, wherever it starts, in equal parts.
+inline int part_granules(int64_t vocab, int dtype, int parts) {
+  const int64_t ve = 16 / (int64_t)elem_size(dtype), granules = (vocab + 2 * ve - 2) / ve;
+  return (int)((granules + parts - 1) / parts);
 }
 inline int check_scale(const char* fn, const char* what, float s) {
   if (!(s > 0.f) || std::isinf(s)) return fail(IRIS_ERR_ARG, "%s: %s has to be positive and finite", fn, what);

@@ -18,7 +18,7 @@ static_assert(kScoreThreads == kTopThreads, "the list is kept by all threads of 
 struct ScoreParams {
   const void* logits;
   int64_t stride;
-  int vocab, n_targets, top_k, split;
+  int vocab, n_targets, top_k, split, each;   // each: granules of a block's part of a row
   float scale;
   const int64_t* targets;
   float *logprob, *entropy, *stats, *top_logprob;
@@ -33,10 +33,10 @@ struct NoTop {};
 
 // One cluster of `split` blocks a row; each takes an equal run of granules and the first one joins what they found.
 template <int DT, bool ENTROPY, bool TOP>
-__global__ void __launch_bounds__(kScoreThreads) score_kernel(const ScoreParams p) {
+__global__ void __launch_bounds__(kScoreThreads, TOP ? 3 : 4) score_kernel(const ScoreParams p) {
   using E = Elem<DT>;
   constexpr int T = kScoreThreads, U = kScoreGranules;
-  __shared__ Warps8 buf;
+  __shared__ Warps<T / 32> buf;
   __shared__ Acc parts[kMaxSplit];
   __shared__ typename std::conditional<TOP, TopShared, NoTop>::type top;
   extern __shared__ uint64_t lists[];   // TOP and split > 1: the blocks' sorted lists, top_k keys each, 0 where one is shorter
@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const ScoreParams 
   const int64_t r = blockIdx.x / split;
   if (split > 1) ptx::cluster_arrive_relaxed();
   const Row<DT> row(p.logits, r, p.stride, p.vocab);
-  const Part<DT> part(row, rank, split);
+  const Part<DT> part(row, rank, p.each);
   const float k = p.scale * kLog2e;
   float zt = 0.f;
   bool there = false;
@@ -59,39 +59,43 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const ScoreParams 
     top.code[tid] = 0;
   }
   Sums<DT, ENTROPY> sums(k);
-  for (int base = 0; base < part.n_all; base += T * U) {
+  const uint4* const from = reinterpret_cast<const uint4*>(row.at(part.w0)) + tid;
+  const int n = part.n_all;
+  const auto batch = [&](int b, auto all) {
+    constexpr bool ALL = decltype(all)::value;
+    const int left = n - b - tid;   // this thread has granules u with u * T < left
     uint4 g[U];
-    const int i0 = base + tid, n = part.n_all;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i0 + u * T < n) g[u] = part.raw(row, i0 + u * T);
     float mx = -INFINITY;
 #pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (ALL) g[u] = ld_once(from + b + u * T);
+      else if (u * T < left) g[u] = part.raw(row, b + u * T + tid);
+    }
+#pragma unroll
     for (int u = 0; u < U; ++u)
-      if (i0 + u * T < n) mx = max_nan(mx, E::largest(g[u]));
-    sums.raise(mx);
+      if (ALL || u * T < left) mx = max_nan(mx, E::largest(g[u]));
     if constexpr (TOP) {
       seen = max_nan(seen, mx);
-      if (i0 < n) top.code[tid] = order_bits(seen);
+      if (ALL || left > 0) top.code[tid] = order_bits(seen);
       __syncthreads();
       if (tid < 32) bisect_tau(top, p.top_k);
     }
-    if (mx != -INFINITY) {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (i0 + u * T < n) sums.add(g[u]);
-    }
+    sums.template add<ALL>(g, mx, left, T);
     if constexpr (TOP) {
       __syncthreads();
       const uint32_t tau = top.tau;
       const float at_tau = tau ? key_value((uint64_t)tau << 32) : NAN;
-      if (tau != 0xffffffffu) {
+      if (tau != 0xffffffffu && !(mx <= at_tau)) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (i0 + u * T < n) collect<DT>(top, row, part.granule(i0 + u * T), g[u], at_tau);
+          if ((ALL || u * T < left) && !(E::largest(g[u]) <= at_tau))
+            collect<DT>(top, row.ph, row.end, part.granule(b + u * T + tid), g[u], at_tau);
       }
     }
-  }
+  };
+  int b = 0;
+  for (; b + T * U <= part.n_int; b += T * U) batch(b, std::true_type{});
+  for (; b < n; b += T * U) batch(b, std::false_type{});
   sums.flush();
   warp_share<ENTROPY>(sums.a, k, buf);
   __syncthreads();
@@ -107,8 +111,8 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const ScoreParams 
     }
     if constexpr (TOP) {
       const uint32_t to = ptx::mapa(ptx::smem_u32(lists + rank * p.top_k), 0);
-      const int n = finish_top<DT>(top, row, part.v0, part.v1, p.top_k, [&](int place, uint64_t key) { ptx::st_shared_cluster_u64(to + place * 8, key); });
-      if (tid >= n && tid < p.top_k) ptx::st_shared_cluster_u64(to + tid * 8, 0);
+      const int found = finish_top<DT>(top, row, part.v0, part.v1, p.top_k, [&](int place, uint64_t key) { ptx::st_shared_cluster_u64(to + place * 8, key); });
+      if (tid >= found && tid < p.top_k) ptx::st_shared_cluster_u64(to + tid * 8, 0);
     }
     ptx::cluster_sync();
     if (rank != 0) return;
@@ -177,7 +181,7 @@ static int launch_score(const ScoreParams& p, int64_t rows, cudaStream_t st) {
 struct ScoreGradParams {
   const void* logits;
   int64_t stride, grad_stride;
-  int vocab, n_targets, parts;
+  int vocab, n_targets, parts, each;
   float scale;
   const int64_t* targets;
   const float *stats, *entropy, *grad_logprob, *grad_entropy;
@@ -215,7 +219,7 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const ScoreGra
   c.alpha = c.alpha_l = -(g + p.scale * gh * h);
   c.beta = -p.scale * gh * kLn2;
   c.zero = ls == -INFINITY;
-  grad_part<DT, ENTROPY>(in, out, Part<DT>(in, blockIdx.x % p.parts, p.parts), c, list, n);
+  grad_part<DT, ENTROPY>(in, out, Part<DT>(in, blockIdx.x % p.parts, p.each), c, list, n);
 }
 
 template <int DT>
@@ -255,7 +259,7 @@ extern "C" int iris_token_logprobs(const iris_logprob_args* a, void* stream) {
   const int64_t granules = a->vocab * (int64_t)elem_size(a->dtype) / 16;
   int split = 1;
   while (split < kMaxSplit && a->rows * split < 2 * kSms && granules >= (int64_t)split * 2 * kScoreThreads) split *= 2;
-  ScoreParams p{a->logits, stride, (int)a->vocab, want_lp ? a->n_targets : 0, a->top_k, split, a->scale, a->targets, a->logprob, a->entropy, a->stats,
+  ScoreParams p{a->logits, stride, (int)a->vocab, want_lp ? a->n_targets : 0, a->top_k, split, part_granules(a->vocab, a->dtype, split), a->scale, a->targets, a->logprob, a->entropy, a->stats,
                 a->top_logprob, a->top_ids};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (a->dtype == IRIS_BF16) return launch_score<IRIS_BF16>(p, a->rows, st);
@@ -281,7 +285,7 @@ extern "C" int iris_token_logprobs_backward(const iris_logprob_grad_args* a, voi
   IRIS_CHECK(check_aligned(fn, "entropy", a->entropy, 4, want_h));
   const int parts = grad_parts(a->vocab, a->dtype);
   if (a->rows * parts > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 blocks", fn);
-  ScoreGradParams p{a->logits, stride, gstride, (int)a->vocab, a->n_targets, parts, a->scale, a->targets, a->stats, a->entropy,
+  ScoreGradParams p{a->logits, stride, gstride, (int)a->vocab, a->n_targets, parts, part_granules(a->vocab, a->dtype, parts), a->scale, a->targets, a->stats, a->entropy,
                     want_lp ? a->grad_logprob : nullptr, a->grad_entropy, a->dlogits};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (a->dtype == IRIS_BF16) return launch_score_grad<IRIS_BF16>(p, a->rows, st);

@@ -57,21 +57,21 @@ __device__ __forceinline__ void bisect_tau(TopShared& sh, int k) {
   if (lane == 0) sh.tau = max(sh.tau, lo);   // never back: what was left out was not above the earlier one
 }
 
-// Puts granule v's logits above tau on the list; at_tau: tau as a float, NaN for tau = 0 (every logit is above it).
+// Puts granule v's logits above tau on the list; at_tau: tau as a float, NaN for tau = 0 (every logit is above it).  Not
+// inlined: few granules have such a logit, and the pass over the row keeps its registers.
 template <int DT>
-__device__ __forceinline__ void collect(TopShared& sh, const Row<DT>& row, int v, const uint4& g, float at_tau) {
+__device__ __noinline__ void collect(TopShared& sh, int ph, int end, int v, uint4 g, float at_tau) {
   using E = Elem<DT>;
   constexpr int VE = E::VE;
-  if (E::largest(g) <= at_tau) return;
   float x[VE];
   E::unpack(g, x);
 #pragma unroll
   for (int e = 0; e < VE; ++e) {
     if (!(x[e] <= at_tau)) {
       const int i = v * VE + e;
-      if (i >= row.ph && i < row.end) {
+      if (i >= ph && i < end) {
         const int at = atomicAdd(&sh.n, 1);
-        if (at < kTopCap) sh.key[at] = order_key(x[e], i - row.ph);
+        if (at < kTopCap) sh.key[at] = order_key(x[e], i - ph);
       }
     }
   }
