@@ -6,6 +6,7 @@
 //   dL/dz_j = scale (P q_j - p_j) in the first form; in the second scale ((P + p_r) q_j - p_j) on the list and
 //   scale ((P + p_r) q_j - p_r q_j / q_r) off it;  P = sum p_k.
 #include <algorithm>
+#include <atomic>
 
 #include "logit_grad.cuh"
 #include "sm100_ptx.cuh"
@@ -13,10 +14,8 @@
 namespace iris {
 namespace rows {
 
-#ifndef DT_T
-#define DT_T 256
-#endif
-constexpr int kDistillThreads = DT_T;
+constexpr int kDistillThreads = 128;
+constexpr int kDistillBlocks = 4;   // an SM's registers are shared out for
 constexpr int kMaxSplit = 8;   // blocks (one cluster) that share a row
 static_assert(kDistillThreads >= kMaxList && kGradThreads >= kMaxList, "one thread an entry of the list");
 
@@ -144,9 +143,9 @@ struct Edge {
 // while this one is finished.  A byte a granule (on_list) says which of its tokens are on the list: with a remainder they
 // leave the sum.  Not HELD: a part too large for that is read twice.
 template <int DT, bool TAIL, bool HELD>
-__global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const DistillParams p) {
+__global__ void __launch_bounds__(kDistillThreads, kDistillBlocks) distill_kernel(const DistillParams p) {
   using E = Elem<DT>;
-  constexpr int VE = E::VE, T = kDistillThreads, U = 4;
+  constexpr int VE = E::VE, T = kDistillThreads, U = 4;   // granules of a batch
   extern __shared__ uint4 held[];
   __shared__ List lists[2];          // of this row and the one before
   __shared__ TeacherSums teacher;
@@ -157,6 +156,7 @@ __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const Disti
   uint32_t* const on_list = reinterpret_cast<uint32_t*>(held + (HELD ? p.hold : 0));
   const uint8_t* const marks = reinterpret_cast<const uint8_t*>(on_list);
   uint4* const mine = held + threadIdx.x;
+  const uint32_t held_at = ptx::smem_u32(held), mine_at = held_at + threadIdx.x * 16;
   const int split = p.split, rank = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x, n = p.list_k;
   const int64_t step = gridDim.x / split;
   int64_t r = blockIdx.x / split;
@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const Disti
   if (HELD) {
     const uint4* const from = reinterpret_cast<const uint4*>(in.at(part.w0));
 #pragma unroll 4
-    for (int i = tid; i < part.n_int; i += T) copy_async(&held[i], from + i);
+    for (int i = tid; i < part.n_int; i += T) copy_async(held_at + i * 16, from + i);
     edge.load(in, part);
   }
   for (int i = tid; i * 4 < p.hold; i += T) on_list[i] = 0;
@@ -183,8 +183,8 @@ __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const Disti
     const Entry entry = ahead.checked<TAIL>(p);
     Sums<DT, false> sums(k);
     const bool own = entry.id >= 0 && part.has(in.ph + entry.id);
-    float zk = -INFINITY;   // the listed token's logit: of all tokens in the first block, of the part's own in the others
-    if (own || (rank == 0 && entry.id >= 0)) zk = E::to(in.column(entry.id));
+    typename E::T z_listed = E::from(-INFINITY);   // the listed token's logit: of all tokens in the first block, of the part's own in the others
+    if (own || (rank == 0 && entry.id >= 0)) z_listed = in.column(entry.id);
     if (tid < kMaxList) list.id[tid] = entry.id;
     const float x = share_entry<TAIL>(entry, teacher);
     const int mark = own ? part.place((in.ph + entry.id) / VE) : -1;   // the listed token's granule and its bit in there
@@ -210,7 +210,6 @@ __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const Disti
         const int left = part.n_int - b - tid;
         uint4 g[U];
         uint32_t bits[U], any = 0;
-        float mx = -INFINITY;
 #pragma unroll
         for (int u = 0; u < U; ++u)
           if (ALL || u * T < left) {
@@ -222,17 +221,14 @@ __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const Disti
           for (int u = 0; u < U; ++u)
             if (ALL || u * T < left) g[u] = without<DT>(g[u], bits[u]);
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (ALL || u * T < left) mx = max_nan(mx, E::largest(g[u]));
-        sums.template add<ALL>(g, mx, left, T);
+        sums.template add<ALL>(g, largest<DT, ALL>(g, left, T), left, T);
       });
       if (tid < part.n_all - part.n_int) {
         const uint4 g[1] = {without<DT>(edge.raw(), TAIL ? marks[part.n_int + tid] : 0)};
-        sums.template add<true>(g, E::largest(g[0]));
+        sums.template add<true>(g, largest<DT>(g[0]));
       }
       if (!grad)
-        for (int i = tid; i < n_next; i += T) copy_async(&held[i], from + i);
+        for (int i = tid; i < n_next; i += T) copy_async(held_at + i * 16, from + i);
     } else {
       for (int b0 = 0; b0 < part.n_all; b0 += p.hold) {   // p.hold granules at a time have marks
         const bool in_piece = TAIL && own && mark >= b0 && mark < b0 + p.hold;
@@ -242,7 +238,7 @@ __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const Disti
         }
         for (int i = b0 + tid; i < min(part.n_all, b0 + p.hold); i += T) {
           const uint4 g[1] = {without<DT>(part.raw(in, i), TAIL ? marks[i - b0] : 0)};
-          sums.template add<true>(g, E::largest(g[0]));
+          sums.template add<true>(g, largest<DT>(g[0]));
         }
         if (TAIL) {
           __syncthreads();
@@ -251,11 +247,10 @@ __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const Disti
         }
       }
     }
-    sums.flush();
-    warp_share<false>(sums.a, k, buf[0]);
+    warp_share<false>(sums.done(), k, buf[0]);
     if (TAIL) {
       Acc listed;
-      if (first) listed.add_one(zk, k);
+      if (first) listed.add_one(E::to(z_listed), k);
       warp_share<false>(listed, k, buf[1]);
     }
     __syncthreads();
@@ -286,6 +281,7 @@ __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const Disti
     if (TAIL) all.merge(listed, k);
     const float ls = log_sum(all);
     const float lr = !TAIL ? 0.f : dense.s == 0.f ? -INFINITY : (dense.m - all.m) * p.scale + log_sum(dense);
+    const float zk = E::to(z_listed);
     Coef coef;
     const float w_row = w;
     const Row<DT> out(p.dlogits, grad ? r : 0, p.grad_stride, p.vocab);
@@ -294,9 +290,12 @@ __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const Disti
       if (p.weight) w = p.weight[r_next];
     }
     bool rep = false;
+    float listed_grad = 0.f, add = 0.f;
     if (grad) {
       coef = distill_coef<TAIL>(p, teach.y, teach.z, all.m, ls, lr, w_row);
-      if (tid < n) list.add[tid] = -w_row * p.scale * pk;
+      add = -w_row * p.scale * pk;
+      listed_grad = grad_of(zk, coef);
+      if (tid < n) list.add[tid] = add;
       rep = own && (HELD ? repeats[turn] != 0 : repeated(list, n, tid));
       const Dense<DT, false> dense_part(coef);
       if (HELD) {
@@ -314,7 +313,7 @@ __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const Disti
           for (int u = 0; u < U; ++u) st_global_v4(to + b + u * T, dense_of(dense_part, g[u]));
           if (more) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) copy_async(mine + b + u * T, from + b + u * T + tid);
+            for (int u = 0; u < U; ++u) copy_async(mine_at + (b + u * T) * 16, from + b + u * T + tid);
           }
         }
         for (int i = b + tid; i < max(part.n_int, n_next); i += T) {
@@ -322,7 +321,7 @@ __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const Disti
             if (alike) st_global_v4(to + i - tid, dense_of(dense_part, held[i]));
             else write_elements(in, out, dense_part, part.w0 + i, held[i]);
           }
-          if (i < n_next) copy_async(&held[i], from + i);
+          if (i < n_next) copy_async(held_at + i * 16, from + i);
         }
       } else {
         if (split == 1) __syncthreads();   // the listed logits have been read
@@ -343,7 +342,7 @@ __global__ void __launch_bounds__(kDistillThreads, 3) distill_kernel(const Disti
       if ((tid & 31) == 0) red[tid >> 5] = l;
     }
     __syncthreads();   // the dense part of the listed columns is written before what replaces it
-    if (grad && own && !coef.zero) out.column(entry.id) = E::from(grad_of(zk, coef) + (rep ? sum_of_column(list, n, tid) : list.add[tid]));
+    if (grad && own && !coef.zero) out.column(entry.id) = E::from(listed_grad + (rep ? sum_of_column(list, n, tid) : add));
     if (rank == 0 && tid == 0) {
       p.loss[r] = red[0] + red[1] + red[2] + red[3];
       if (p.stats) {
@@ -384,8 +383,7 @@ using namespace iris::rows;
 namespace {
 
 constexpr int kHoldBytes = 192 * 1024;   // of shared memory at most for a part
-static int part_kb() { const char* e = getenv("PARTKB"); return e ? atoi(e) : 60; }
-#define kPartBytes (part_kb() * 1024)
+constexpr int kPartBytes = 60 * 1024;    // ... and where the row can be split further: three blocks' worth in an SM
 constexpr int kMaxDevices = 64;
 
 int check_distill(const char* fn, const iris_distill_args* a, int64_t* stride, int64_t* gstride) {
@@ -438,12 +436,8 @@ int launch_distill(const DistillParams& p, cudaStream_t st) {
     IRIS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldBytes + kHoldBytes / 16));
     if (dev < kMaxDevices) configured[dev] = true;
   }
-  // Blocks of 256 threads that an SM takes at a time: 4 by registers, fewer by shared memory (228 KB, 4 KB of it a block's
-  // own variables and reserve).
-  const int per_sm = std::max(1, std::min(4, (int)(228 * 1024 / (bytes + 5 * 1024))));
-  const int64_t clusters = std::min<int64_t>(p.rows, std::max(1, kSms * per_sm / p.split));
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(clusters * p.split));
+  cfg.gridDim = dim3((unsigned)p.split);
   cfg.blockDim = dim3(kDistillThreads);
   cfg.dynamicSmemBytes = (size_t)bytes;
   cfg.stream = st;
@@ -453,6 +447,22 @@ int launch_distill(const DistillParams& p, cudaStream_t st) {
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = p.split > 1 ? 1 : 0;
+  // As many clusters as the device holds at a time: one more would run after the others have done all their rows.  The
+  // answer is kept (it depends on the kernel, the split and the bytes alone), as asking takes longer than a small launch.
+  int clusters = 0;
+  static std::atomic<uint64_t> known[kMaxSplit + 1];
+  const uint64_t key = (uint64_t)(dev + 1) << 48 | (uint64_t)bytes << 16;
+  const uint64_t was = known[p.split].load(std::memory_order_relaxed);
+  if ((was & ~0xffffull) == key) {
+    clusters = (int)(was & 0xffff);
+  } else {
+    if (p.split > 1) IRIS_CUDA_TRY(cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg));
+    else IRIS_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&clusters, kernel, kDistillThreads, (size_t)bytes));
+    if (p.split == 1) clusters *= kSms;
+    clusters = std::max(1, std::min(clusters, 0xffff));
+    known[p.split].store(key | (uint64_t)clusters, std::memory_order_relaxed);
+  }
+  cfg.gridDim = dim3((unsigned)(std::min(clusters, p.rows) * p.split));
   IRIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
   return IRIS_OK;
 }

@@ -62,8 +62,8 @@ __device__ __forceinline__ uint4 ld_once(const void* p) {
 }
 // 16 bytes to shared memory without passing through registers; visible to the copying thread after copy_async_wait, to
 // the block after a barrier behind that.
-__device__ __forceinline__ void copy_async(void* shared, const void* global) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(global) : "memory");
+__device__ __forceinline__ void copy_async(uint32_t shared, const void* global) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(shared), "l"(global) : "memory");
 }
 __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // The larger of two, NaN if either is.
@@ -73,7 +73,8 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return y;
 }
 
-template <int DT> struct Elem;   // kMasked: 32 bits of -inf; largest(): of a granule's values, NaN if one is;
+template <int DT> struct Elem;   // kMasked: 32 bits of -inf; fold(): a granule's largest values in two halves, larger() of two such, unfold() the larger
+// half, NaN if one is;
 // at_least(): none below twice(floor), NaN stays
 template <> struct Elem<IRIS_F16> {
   using T = __half;
@@ -84,6 +85,25 @@ template <> struct Elem<IRIS_F16> {
     const __half2 h = __floats2half2_rn(x, x);
     return *reinterpret_cast<const uint32_t*>(&h);
   }
+  // A number that orders the type's values, 0 below all of them, the largest for NaN, and back.
+  static __device__ __forceinline__ uint32_t ordinal(float x) {
+    const uint32_t b = (uint32_t)__half_as_ushort(__float2half_rn(x + 0.f));   // -0 counts as +0
+    return x != x ? 0xffffu : b & 0x8000u ? ~b & 0xffffu : b | 0x8000u;
+  }
+  static __device__ __forceinline__ float value(uint32_t n) {
+    const uint32_t b = n & 0x8000u ? n & 0x7fffu : ~n & 0xffffu;
+    return n == 0xffffu ? NAN : __half2float(__ushort_as_half((unsigned short)b));
+  }
+  // Of granules g[0 .. 8): bit 4 (u % 4) + w + 16 h of word u / 4 says that element 2 w + h of granule u is above tau or NaN.
+  static constexpr int kMarkWords = 2;
+  static __device__ __forceinline__ void mark(const uint4& g, int u, uint32_t tau2, uint32_t (&m)[2]) {
+    const __half2 t = *reinterpret_cast<const __half2*>(&tau2);
+    const uint32_t w[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[u / 4] |= __hgtu2_mask(*reinterpret_cast<const __half2*>(&w[i]), t) & (0x10001u << (4 * (u % 4) + i));
+  }
+  static __device__ __forceinline__ int marked_granule(int word, int bit) { return word * 4 + bit % 16 / 4; }
+  static __device__ __forceinline__ int marked_element(int bit) { return 2 * (bit % 4) + bit / 16; }
   static __device__ __forceinline__ uint4 at_least(uint4 v, uint32_t floor) {
     asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(v.x) : "r"(floor));
     asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(v.y) : "r"(floor));
@@ -91,11 +111,13 @@ template <> struct Elem<IRIS_F16> {
     asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(v.w) : "r"(floor));
     return v;
   }
-  static __device__ __forceinline__ float largest(const uint4& v) {
-    uint32_t a, b, m;
-    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
-    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    uint32_t m;
     asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return m;
+  }
+  static __device__ __forceinline__ uint32_t fold(const uint4& v) { return larger(larger(v.x, v.y), larger(v.z, v.w)); }
+  static __device__ __forceinline__ float unfold(uint32_t m) {
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&m));
     return max_nan(f.x, f.y);
   }
@@ -129,6 +151,25 @@ template <> struct Elem<IRIS_BF16> {
     const __nv_bfloat162 h = __floats2bfloat162_rn(x, x);
     return *reinterpret_cast<const uint32_t*>(&h);
   }
+  // A number that orders the type's values, 0 below all of them, the largest for NaN, and back.
+  static __device__ __forceinline__ uint32_t ordinal(float x) {
+    const uint32_t b = __float_as_uint(x + 0.f) >> 16;   // -0 counts as +0
+    return x != x ? 0xffffu : b & 0x8000u ? ~b & 0xffffu : b | 0x8000u;
+  }
+  static __device__ __forceinline__ float value(uint32_t n) {
+    const uint32_t b = n & 0x8000u ? n & 0x7fffu : ~n & 0xffffu;
+    return n == 0xffffu ? NAN : __uint_as_float(b << 16);
+  }
+  // Of granules g[0 .. 8): bit 4 (u % 4) + w + 16 h of word u / 4 says that element 2 w + h of granule u is above tau or NaN.
+  static constexpr int kMarkWords = 2;
+  static __device__ __forceinline__ void mark(const uint4& g, int u, uint32_t tau2, uint32_t (&m)[2]) {
+    const __nv_bfloat162 t = *reinterpret_cast<const __nv_bfloat162*>(&tau2);
+    const uint32_t w[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[u / 4] |= __hgtu2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[i]), t) & (0x10001u << (4 * (u % 4) + i));
+  }
+  static __device__ __forceinline__ int marked_granule(int word, int bit) { return word * 4 + bit % 16 / 4; }
+  static __device__ __forceinline__ int marked_element(int bit) { return 2 * (bit % 4) + bit / 16; }
   static __device__ __forceinline__ uint4 at_least(uint4 v, uint32_t floor) {
     asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(v.x) : "r"(floor));
     asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(v.y) : "r"(floor));
@@ -136,11 +177,13 @@ template <> struct Elem<IRIS_BF16> {
     asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(v.w) : "r"(floor));
     return v;
   }
-  static __device__ __forceinline__ float largest(const uint4& v) {
-    uint32_t a, b, m;
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    uint32_t m;
     asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return m;
+  }
+  static __device__ __forceinline__ uint32_t fold(const uint4& v) { return larger(larger(v.x, v.y), larger(v.z, v.w)); }
+  static __device__ __forceinline__ float unfold(uint32_t m) {
     return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
   }
   static __device__ __forceinline__ float to(T x) { return __bfloat162float(x); }
@@ -169,14 +212,29 @@ template <> struct Elem<IRIS_F32> {
   static constexpr uint32_t kMasked = 0xff800000u;
   static constexpr float kLowest = -3.38e38f;
   static __device__ __forceinline__ uint32_t twice(float x) { return __float_as_uint(x); }
+  static __device__ __forceinline__ uint32_t ordinal(float x) {
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return x != x ? ~0u : b & 0x80000000u ? ~b : b | 0x80000000u;
+  }
+  static __device__ __forceinline__ float value(uint32_t n) { return n == ~0u ? NAN : __uint_as_float(n & 0x80000000u ? n & 0x7fffffffu : ~n); }
+  // Bit 4 u + e: element e of granule u is above tau or NaN.
+  static constexpr int kMarkWords = 1;
+  static __device__ __forceinline__ void mark(const uint4& g, int u, uint32_t tau2, uint32_t (&m)[1]) {
+    const float t = __uint_as_float(tau2);
+    const uint32_t w[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m[0] |= !(__uint_as_float(w[e]) <= t) ? 1u << (4 * u + e) : 0u;
+  }
+  static __device__ __forceinline__ int marked_granule(int, int bit) { return bit / 4; }
+  static __device__ __forceinline__ int marked_element(int bit) { return bit % 4; }
   static __device__ __forceinline__ uint4 at_least(const uint4& v, uint32_t floor) {
     const float f = __uint_as_float(floor);
     return make_uint4(__float_as_uint(max_nan(__uint_as_float(v.x), f)), __float_as_uint(max_nan(__uint_as_float(v.y), f)),
                       __float_as_uint(max_nan(__uint_as_float(v.z), f)), __float_as_uint(max_nan(__uint_as_float(v.w), f)));
   }
-  static __device__ __forceinline__ float largest(const uint4& v) {
-    return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)), max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
-  }
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b))); }
+  static __device__ __forceinline__ uint32_t fold(const uint4& v) { return larger(larger(v.x, v.y), larger(v.z, v.w)); }
+  static __device__ __forceinline__ float unfold(uint32_t m) { return __uint_as_float(m); }
   static __device__ __forceinline__ float to(T x) { return x; }
   static __device__ __forceinline__ T from(float x) { return x; }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
@@ -189,6 +247,20 @@ template <> struct Elem<IRIS_F32> {
     return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
   }
 };
+
+template <int DT>
+__device__ __forceinline__ float largest(const uint4& g) {
+  return Elem<DT>::unfold(Elem<DT>::fold(g));
+}
+// Of the granules g[u] with u * T < left (all of them if ALL); -inf if there are none.
+template <int DT, bool ALL, int U>
+__device__ __forceinline__ float largest(const uint4 (&g)[U], int left, int T) {
+  uint32_t m = Elem<DT>::kMasked;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (ALL || u * T < left) m = ALL && u == 0 ? Elem<DT>::fold(g[0]) : Elem<DT>::larger(m, Elem<DT>::fold(g[u]));
+  return Elem<DT>::unfold(m);
+}
 
 // The granule with -inf in the places whose bit is set.
 template <int DT>
@@ -263,7 +335,7 @@ struct Part {
 // a masked z), s = sum 2^y, t = sum y 2^y, y = (z - m) k cut at about kFloor, k = scale log2(e).
 struct Acc {
   float m = -FLT_MAX, s = 0.f, t = 0.f;
-  __device__ __forceinline__ void rebase(float mx, float k) {   // to a larger m
+  __device__ __forceinline__ void rebase(float mx, float k) {   // to another m, if not too far below
     const float d = max_nan((m - mx) * k, kFloor), f = ex2(d);
     t = __fmul_rn(fmaf(s, d, t), f);
     s = __fmul_rn(s, f);
@@ -290,13 +362,16 @@ __device__ __forceinline__ bool lift_floor(float m, float k, uint32_t& word) {
   return low >= Elem<DT>::kLowest && low * k > -1e38f && m * k < 1e38f;
 }
 
-// A thread's statistics of granules.  All logits added since the last raise() count from its m.  Per element one
-// instruction to unpack, half of one each to subtract, scale and add, and the exponential; with the entropy half of one
-// each for the lift (on packed 16-bit values) and the second sum.
+// A thread's statistics of granules, counted from a logit near the largest: it is raised only when one comes that is
+// 2^kSlack times as probable, so that in most rows it is the largest of the first batch and the sums need no further care
+// (2^kSlack times 2^30 columns is far from overflow, and nothing is lost by larger terms).  Per element one instruction to
+// unpack, half of one each to subtract, scale and add, and the exponential; with the entropy half of one each for the lift
+// (on packed 16-bit values) and the second sum.
 template <int DT, bool ENTROPY>
 struct Sums {
+  static constexpr float kSlack = 24.f;
   Acc a;
-  float k;
+  float k, top = -FLT_MAX;   // top: the largest logit so far
   bool lift = false;
   uint32_t floor = 0;
   uint64_t s2 = 0, t2 = 0;   // sums of even and odd places since the last raise
@@ -313,11 +388,17 @@ struct Sums {
     }
   }
   __device__ __forceinline__ void raise(float mx) {   // before adding logits of which mx is the largest
-    if (mx <= a.m) return;
+    top = max_nan(top, mx);
+    if ((mx - a.m) * k <= kSlack) return;
     flush();
     a.rebase(max_nan(a.m, mx), k);
     minus_m2 = pair(-a.m, -a.m);
     if (ENTROPY) lift = lift_floor<DT>(a.m, k, floor);
+  }
+  __device__ __forceinline__ Acc done() {   // counted from the largest logit
+    flush();
+    a.rebase(top, k);
+    return a;
   }
   __device__ __forceinline__ void add_lifted(const uint4& g) {
     constexpr int VE = Elem<DT>::VE;
@@ -405,17 +486,15 @@ __device__ __forceinline__ Acc warps_join(float k, const Warps<W>& buf) {
 // ln sum exp(scale (z - m)): -inf where no logit is left.
 __device__ __forceinline__ float log_sum(const Acc& a) { return a.s > 0.f ? logf(a.s) : a.s == 0.f ? -INFINITY : NAN; }
 
-// A larger logit, and among equal ones the lower column, has the larger key.  NaN comes above +inf.
-__device__ __forceinline__ uint32_t order_bits(float x) {
-  if (x != x) return 0xffffffffu;
-  const uint32_t b = __float_as_uint(x + 0.f);   // -0 counts as +0
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+// A larger logit, and among equal ones the lower column, has the larger key; 0 is no logit's.  NaN comes above +inf.
+template <int DT>
+__device__ __forceinline__ uint64_t order_key(float x, int column) {
+  return (uint64_t)Elem<DT>::ordinal(x) << 32 | (0xffffffffu - (uint32_t)column);
 }
-__device__ __forceinline__ uint64_t order_key(float x, int column) { return (uint64_t)order_bits(x) << 32 | (0xffffffffu - (uint32_t)column); }
 __device__ __forceinline__ int key_column(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
+template <int DT>
 __device__ __forceinline__ float key_value(uint64_t key) {
-  const uint32_t b = (uint32_t)(key >> 32);
-  return b == 0xffffffffu ? NAN : __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
+  return Elem<DT>::value((uint32_t)(key >> 32));
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------

@@ -33,7 +33,7 @@ struct NoTop {};
 
 // One cluster of `split` blocks a row; each takes an equal run of granules and the first one joins what they found.
 template <int DT, bool ENTROPY, bool TOP>
-__global__ void __launch_bounds__(kScoreThreads, TOP ? 3 : 4) score_kernel(const ScoreParams p) {
+__global__ void __launch_bounds__(kScoreThreads, 4) score_kernel(const ScoreParams p) {
   using E = Elem<DT>;
   constexpr int T = kScoreThreads, U = kScoreGranules;
   __shared__ Warps<T / 32> buf;
@@ -53,51 +53,41 @@ __global__ void __launch_bounds__(kScoreThreads, TOP ? 3 : 4) score_kernel(const
     there = t >= 0 && t < p.vocab;
     if (there) zt = E::to(row.column((int)t));
   }
-  float seen = -INFINITY;
-  if constexpr (TOP) {
-    if (tid == 0) top.n = top.n_kept = 0, top.tau = 0;
-    top.code[tid] = 0;
-  }
   Sums<DT, ENTROPY> sums(k);
   const uint4* const from = reinterpret_cast<const uint4*>(row.at(part.w0)) + tid;
-  const int n = part.n_all;
+  const int n = part.n_all, piece = TOP ? max(1, ((n + T * U - 1) / (T * U) + kTopPieces - 1) / kTopPieces) : 1;   // batches of one
+  float best = -INFINITY, of_piece = -INFINITY;
+  int done = 0, q = 0;
   const auto batch = [&](int b, auto all) {
     constexpr bool ALL = decltype(all)::value;
     const int left = n - b - tid;   // this thread has granules u with u * T < left
     uint4 g[U];
-    float mx = -INFINITY;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (ALL) g[u] = ld_once(from + b + u * T);
       else if (u * T < left) g[u] = part.raw(row, b + u * T + tid);
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (ALL || u * T < left) mx = max_nan(mx, E::largest(g[u]));
-    if constexpr (TOP) {
-      seen = max_nan(seen, mx);
-      if (ALL || left > 0) top.code[tid] = order_bits(seen);
-      __syncthreads();
-      if (tid < 32) bisect_tau(top, p.top_k);
-    }
+    const float mx = largest<DT, ALL>(g, left, T);
     sums.template add<ALL>(g, mx, left, T);
     if constexpr (TOP) {
-      __syncthreads();
-      const uint32_t tau = top.tau;
-      const float at_tau = tau ? key_value((uint64_t)tau << 32) : NAN;
-      if (tau != 0xffffffffu && !(mx <= at_tau)) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          if ((ALL || u * T < left) && !(E::largest(g[u]) <= at_tau))
-            collect<DT>(top, row.ph, row.end, part.granule(b + u * T + tid), g[u], at_tau);
+      of_piece = max_nan(of_piece, mx);
+      top.largest[q][tid] = of_piece;
+      if (++done == piece) {
+        best = max_nan(best, of_piece);
+        of_piece = -INFINITY;
+        done = 0;
+        ++q;
       }
     }
   };
   int b = 0;
   for (; b + T * U <= part.n_int; b += T * U) batch(b, std::true_type{});
   for (; b < n; b += T * U) batch(b, std::false_type{});
-  sums.flush();
-  warp_share<ENTROPY>(sums.a, k, buf);
+  warp_share<ENTROPY>(sums.done(), k, buf);
+  if constexpr (TOP) {
+    top.ordinal[tid] = tid < n ? E::ordinal(max_nan(best, of_piece)) : 0;
+    if (tid == 0) top.n = 0;
+  }
   __syncthreads();
   Acc a = warps_join<ENTROPY>(k, buf);
 
@@ -111,7 +101,7 @@ __global__ void __launch_bounds__(kScoreThreads, TOP ? 3 : 4) score_kernel(const
     }
     if constexpr (TOP) {
       const uint32_t to = ptx::mapa(ptx::smem_u32(lists + rank * p.top_k), 0);
-      const int found = finish_top<DT>(top, row, part.v0, part.v1, p.top_k, [&](int place, uint64_t key) { ptx::st_shared_cluster_u64(to + place * 8, key); });
+      const int found = find_top<DT, U>(top, row, part, piece * U, p.top_k, [&](int place, uint64_t key) { ptx::st_shared_cluster_u64(to + place * 8, key); });
       if (tid >= found && tid < p.top_k) ptx::st_shared_cluster_u64(to + tid * 8, 0);
     }
     ptx::cluster_sync();
@@ -131,10 +121,10 @@ __global__ void __launch_bounds__(kScoreThreads, TOP ? 3 : 4) score_kernel(const
   if constexpr (TOP) {
     const auto emit = [&](int place, uint64_t key) {
       p.top_ids[r * p.top_k + place] = key_column(key);
-      if (p.top_logprob) p.top_logprob[r * p.top_k + place] = log_prob(key_value(key), a.m, ls, p.scale);
+      if (p.top_logprob) p.top_logprob[r * p.top_k + place] = log_prob(key_value<DT>(key), a.m, ls, p.scale);
     };
     if (split == 1) {
-      finish_top<DT>(top, row, part.v0, part.v1, p.top_k, emit);
+      find_top<DT, U>(top, row, part, piece * U, p.top_k, emit);
     } else {   // a key's place is the number of larger ones in every list
       for (int i = tid; i < split * p.top_k; i += T) {
         const uint64_t key = lists[i];
