@@ -94,16 +94,6 @@ template <> struct Elem<IRIS_F16> {
     const uint32_t b = n & 0x8000u ? n & 0x7fffu : ~n & 0xffffu;
     return n == 0xffffu ? NAN : __half2float(__ushort_as_half((unsigned short)b));
   }
-  // Of granules g[0 .. 8): bit 4 (u % 4) + w + 16 h of word u / 4 says that element 2 w + h of granule u is above tau or NaN.
-  static constexpr int kMarkWords = 2;
-  static __device__ __forceinline__ void mark(const uint4& g, int u, uint32_t tau2, uint32_t (&m)[2]) {
-    const __half2 t = *reinterpret_cast<const __half2*>(&tau2);
-    const uint32_t w[4] = {g.x, g.y, g.z, g.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m[u / 4] |= __hgtu2_mask(*reinterpret_cast<const __half2*>(&w[i]), t) & (0x10001u << (4 * (u % 4) + i));
-  }
-  static __device__ __forceinline__ int marked_granule(int word, int bit) { return word * 4 + bit % 16 / 4; }
-  static __device__ __forceinline__ int marked_element(int bit) { return 2 * (bit % 4) + bit / 16; }
   static __device__ __forceinline__ uint4 at_least(uint4 v, uint32_t floor) {
     asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(v.x) : "r"(floor));
     asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(v.y) : "r"(floor));
@@ -160,16 +150,6 @@ template <> struct Elem<IRIS_BF16> {
     const uint32_t b = n & 0x8000u ? n & 0x7fffu : ~n & 0xffffu;
     return n == 0xffffu ? NAN : __uint_as_float(b << 16);
   }
-  // Of granules g[0 .. 8): bit 4 (u % 4) + w + 16 h of word u / 4 says that element 2 w + h of granule u is above tau or NaN.
-  static constexpr int kMarkWords = 2;
-  static __device__ __forceinline__ void mark(const uint4& g, int u, uint32_t tau2, uint32_t (&m)[2]) {
-    const __nv_bfloat162 t = *reinterpret_cast<const __nv_bfloat162*>(&tau2);
-    const uint32_t w[4] = {g.x, g.y, g.z, g.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m[u / 4] |= __hgtu2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[i]), t) & (0x10001u << (4 * (u % 4) + i));
-  }
-  static __device__ __forceinline__ int marked_granule(int word, int bit) { return word * 4 + bit % 16 / 4; }
-  static __device__ __forceinline__ int marked_element(int bit) { return 2 * (bit % 4) + bit / 16; }
   static __device__ __forceinline__ uint4 at_least(uint4 v, uint32_t floor) {
     asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(v.x) : "r"(floor));
     asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(v.y) : "r"(floor));
@@ -217,16 +197,6 @@ template <> struct Elem<IRIS_F32> {
     return x != x ? ~0u : b & 0x80000000u ? ~b : b | 0x80000000u;
   }
   static __device__ __forceinline__ float value(uint32_t n) { return n == ~0u ? NAN : __uint_as_float(n & 0x80000000u ? n & 0x7fffffffu : ~n); }
-  // Bit 4 u + e: element e of granule u is above tau or NaN.
-  static constexpr int kMarkWords = 1;
-  static __device__ __forceinline__ void mark(const uint4& g, int u, uint32_t tau2, uint32_t (&m)[1]) {
-    const float t = __uint_as_float(tau2);
-    const uint32_t w[4] = {g.x, g.y, g.z, g.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) m[0] |= !(__uint_as_float(w[e]) <= t) ? 1u << (4 * u + e) : 0u;
-  }
-  static __device__ __forceinline__ int marked_granule(int, int bit) { return bit / 4; }
-  static __device__ __forceinline__ int marked_element(int bit) { return bit % 4; }
   static __device__ __forceinline__ uint4 at_least(const uint4& v, uint32_t floor) {
     const float f = __uint_as_float(floor);
     return make_uint4(__float_as_uint(max_nan(__uint_as_float(v.x), f)), __float_as_uint(max_nan(__uint_as_float(v.y), f)),

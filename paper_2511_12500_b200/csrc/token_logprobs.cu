@@ -11,7 +11,8 @@ namespace iris {
 namespace rows {
 
 constexpr int kScoreThreads = 256;
-constexpr int kScoreGranules = 8;       // of 16 bytes a thread holds at once
+constexpr int kScoreGranules = 4;       // of 16 bytes a thread holds at once
+constexpr int kScoreBlocks = 5;         // an SM's registers are shared out for
 constexpr int kMaxSplit = 8;            // blocks (one cluster) that share a row
 static_assert(kScoreThreads == kTopThreads, "the list is kept by all threads of the block");
 
@@ -31,18 +32,21 @@ __device__ __forceinline__ float log_prob(float z, float m, float ls, float scal
 
 struct NoTop {};
 
-// One cluster of `split` blocks a row; each takes an equal run of granules and the first one joins what they found.
+// One cluster of `split` blocks a row; each takes an equal run of granules, and all get what each found.
 template <int DT, bool ENTROPY, bool TOP>
-__global__ void __launch_bounds__(kScoreThreads, 4) score_kernel(const ScoreParams p) {
+__global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) score_kernel(const ScoreParams p) {
   using E = Elem<DT>;
   constexpr int T = kScoreThreads, U = kScoreGranules;
   __shared__ Warps<T / 32> buf;
-  __shared__ Acc parts[kMaxSplit];
+  __shared__ Warps<kMaxSplit> parts;   // of the cluster's blocks
   __shared__ typename std::conditional<TOP, TopShared, NoTop>::type top;
   extern __shared__ uint64_t lists[];   // TOP and split > 1: the blocks' sorted lists, top_k keys each, 0 where one is shorter
   const int split = p.split, rank = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x;
   const int64_t r = blockIdx.x / split;
-  if (split > 1) ptx::cluster_arrive_relaxed();
+  if (split > 1) {
+    if (tid < kMaxSplit) parts.of[tid] = Acc{};
+    ptx::cluster_arrive_relaxed();
+  }
   const Row<DT> row(p.logits, r, p.stride, p.vocab);
   const Part<DT> part(row, rank, p.each);
   const float k = p.scale * kLog2e;
@@ -86,61 +90,55 @@ __global__ void __launch_bounds__(kScoreThreads, 4) score_kernel(const ScorePara
   warp_share<ENTROPY>(sums.done(), k, buf);
   if constexpr (TOP) {
     top.ordinal[tid] = tid < n ? E::ordinal(max_nan(best, of_piece)) : 0;
-    if (tid == 0) top.n = 0;
+    if (tid == 0) top.n = top.n_again = 0;
   }
   __syncthreads();
   Acc a = warps_join<ENTROPY>(k, buf);
 
   if (split > 1) {
-    ptx::cluster_wait();   // the first block has started
-    if (tid == 0) {
-      const uint32_t to = ptx::mapa(ptx::smem_u32(&parts[rank]), 0);
+    ptx::cluster_wait();   // all blocks have started
+    if (tid < split) {
+      const uint32_t to = ptx::mapa(ptx::smem_u32(&parts.of[rank]), tid);
       ptx::st_shared_cluster_u32(to, __float_as_uint(a.m));
       ptx::st_shared_cluster_u32(to + 4, __float_as_uint(a.s));
       ptx::st_shared_cluster_u32(to + 8, __float_as_uint(a.t));
     }
     if constexpr (TOP) {
-      const uint32_t to = ptx::mapa(ptx::smem_u32(lists + rank * p.top_k), 0);
-      const int found = find_top<DT, U>(top, row, part, piece * U, p.top_k, [&](int place, uint64_t key) { ptx::st_shared_cluster_u64(to + place * 8, key); });
-      if (tid >= found && tid < p.top_k) ptx::st_shared_cluster_u64(to + tid * 8, 0);
+      const uint32_t own = ptx::smem_u32(lists + rank * p.top_k);
+      const auto share = [&](int place, uint64_t key) {
+        for (int s = 0; s < split; ++s) ptx::st_shared_cluster_u64(ptx::mapa(own + place * 8, s), key);
+      };
+      const int found = find_top<DT, U>(top, row, part, piece, p.top_k, share);
+      if (tid >= found && tid < p.top_k) share(tid, 0);
     }
     ptx::cluster_sync();
-    if (rank != 0) return;
-    a = parts[0];
-    for (int i = 1; i < split; ++i) a.merge(parts[i], k);
+    a = warps_join<ENTROPY>(k, parts);
   }
   const float ls = log_sum(a);
-  if (tid == 0) {
+  if (rank == 0 && tid == 0) {
     if (p.stats) {
       p.stats[2 * r] = ls == -INFINITY ? -INFINITY : a.m;
       p.stats[2 * r + 1] = ls;
     }
     if (ENTROPY) p.entropy[r] = a.s == 0.f ? 0.f : ls - a.t / a.s * kLn2;
   }
-  if (tid < p.n_targets) p.logprob[r * p.n_targets + tid] = there ? log_prob(zt, a.m, ls, p.scale) : 0.f;
+  if (rank == 0 && tid < p.n_targets) p.logprob[r * p.n_targets + tid] = there ? log_prob(zt, a.m, ls, p.scale) : 0.f;
   if constexpr (TOP) {
     const auto emit = [&](int place, uint64_t key) {
       p.top_ids[r * p.top_k + place] = key_column(key);
       if (p.top_logprob) p.top_logprob[r * p.top_k + place] = log_prob(key_value<DT>(key), a.m, ls, p.scale);
     };
     if (split == 1) {
-      find_top<DT, U>(top, row, part, piece * U, p.top_k, emit);
-    } else {   // a key's place is the number of larger ones in every list
-      for (int i = tid; i < split * p.top_k; i += T) {
-        const uint64_t key = lists[i];
-        if (key == 0) continue;
-        int place = 0;
-        for (int s = 0; s < split; ++s) {
-          int lo = 0, hi = p.top_k;
-          while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (lists[s * p.top_k + mid] > key) lo = mid + 1;
-            else hi = mid;
-          }
-          place += lo;
-        }
-        if (place < p.top_k) emit(place, key);
-      }
+      find_top<DT, U>(top, row, part, piece, p.top_k, emit);
+    } else {   // every block finds the places of its own keys, with a group of threads each
+      int group = 32;
+      while (group * p.top_k > T) group /= 2;   // >= 2: top_k <= 128
+      const int i = tid / group, n_all = split * p.top_k;
+      const uint64_t key = i < p.top_k ? lists[rank * p.top_k + i] : 0;
+      int place = 0;
+      for (int j = tid % group; j < n_all; j += group) place += lists[j] > key;
+      for (int o = group / 2; o; o /= 2) place += __shfl_xor_sync(~0u, place, o);
+      if (key && tid % group == 0 && place < p.top_k) emit(place, key);
     }
   }
 }
@@ -244,11 +242,11 @@ extern "C" int iris_token_logprobs(const iris_logprob_args* a, void* stream) {
   IRIS_CHECK(check_aligned(fn, "stats", a->stats, 4, false));
   IRIS_CHECK(check_aligned(fn, "top_ids", a->top_ids, 8, a->top_k > 0));
   IRIS_CHECK(check_aligned(fn, "top_logprob", a->top_logprob, 4, false));
-  // A row is shared by a cluster of blocks while the rows alone leave SMs without work and every thread of each block
-  // still has a granule.
-  const int64_t granules = a->vocab * (int64_t)elem_size(a->dtype) / 16;
+  // A row is shared by a cluster of blocks while the rows alone leave SMs without work and every block still has a batch
+  // of granules.
+  const int64_t granules = part_granules(a->vocab, a->dtype, 1);
   int split = 1;
-  while (split < kMaxSplit && a->rows * split < 2 * kSms && granules >= (int64_t)split * 2 * kScoreThreads) split *= 2;
+  while (split < kMaxSplit && a->rows * split < 2 * kSms && granules >= (int64_t)split * 2 * kScoreThreads * kScoreGranules) split *= 2;
   ScoreParams p{a->logits, stride, (int)a->vocab, want_lp ? a->n_targets : 0, a->top_k, split, part_granules(a->vocab, a->dtype, split), a->scale, a->targets, a->logprob, a->entropy, a->stats,
                 a->top_logprob, a->top_ids};
   cudaStream_t st = static_cast<cudaStream_t>(stream);

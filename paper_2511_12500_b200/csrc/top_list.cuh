@@ -1,11 +1,12 @@
 // The k largest of a row's logits.  The pass over the row keeps every thread's largest logits, by pieces of the row.  If k
 // threads hold a logit >= tau, then k logits are >= tau: the largest such tau that a few halvings find leaves little more
-// than k logits above it (each of 256 threads has a share of the row, and few hold two of the k largest).  Threads read the
-// pieces again whose largest logit is above tau (from L2: about k of them) and list what is; a key's place among the k is
-// the number of larger keys on the list.
+// than k logits from it up (each of 256 threads has a share of the row, and few hold two of the k largest).  The pieces with
+// such logits, about k of them, are read again, from L2, a granule a thread, and the logits are listed; a key's place among
+// the k is the number of larger keys on the list.
 //
-// Ties are cut by the column, so logits equal to tau may be needed too (a row whose mask leaves fewer than k logits always
-// needs some); those are fetched in column order.  A row laid out so that the list overflows is selected digit by digit.
+// Where far more than k threads hold tau or more (equal logits; a mask that leaves fewer than k, in which case tau is the
+// mask's value), the list takes what is above tau, and the ties it lacks are fetched in column order.  A row laid out so that
+// the list overflows is selected digit by digit.
 #pragma once
 
 #include "logit_rows.cuh"
@@ -20,18 +21,21 @@ constexpr int kTopCap = 1024;   // > 127 granules of 8, what a block can hold wi
 static_assert(kTopThreads >= kMaxList && kTopCap >= (kMaxList - 1) * 8, "the list holds all of a part that has fewer granules than k");
 
 struct TopShared {
-  uint64_t key[kTopCap];
+  alignas(16) uint64_t key[kTopCap];
   float largest[kTopPieces][kTopThreads];   // of a thread's logits in a piece of the row
   uint32_t ordinal[kTopThreads];            // of a thread's largest logit; 0 = it has none
+  uint16_t again[kTopPieces * kTopThreads]; // pieces to be read again: piece * kTopThreads + thread
   uint32_t hist[256];
   uint32_t tau;
-  int n, warp_sum[kTopThreads / 32];
+  int with_tau;   // logits equal to tau are listed too
+  int n, n_again, warp_sum[kTopThreads / 32];
 };
 
-// By one warp: the largest tau it finds in 16 halvings with at least k of sh.ordinal >= tau (0 if fewer than k are not 0);
-// a count within an eighth of k is near enough.
-__device__ __forceinline__ void bisect_tau(TopShared& sh, int k) {
-  const int lane = threadIdx.x & 31;
+// By one warp: the largest tau it finds with at least k of sh.ordinal >= tau (0 if fewer than k are not 0), by quartering;
+// a few more than k are near enough.
+__device__ __forceinline__ void find_tau(TopShared& sh, int k) {
+  const int lane = threadIdx.x & 31, enough = k + max(8, k / 8);
+  int above = kTopThreads;   // threads that hold lo or more
   uint32_t c[kTopThreads / 32], lo = ~0u, hi = 0;
 #pragma unroll
   for (int i = 0; i < kTopThreads / 32; ++i) {
@@ -41,42 +45,23 @@ __device__ __forceinline__ void bisect_tau(TopShared& sh, int k) {
   }
   lo = __reduce_min_sync(~0u, lo);   // all kTopThreads >= k are at least this large
   hi = __reduce_max_sync(~0u, hi);
-  for (int it = 0; it < 16 && lo < hi; ++it) {
-    const uint32_t mid = lo + (hi - lo - 1) / 2 + 1;   // in (lo, hi]
-    int cnt = 0;
+  for (int it = 0; it < 10 && lo < hi; ++it) {
+    const uint32_t step = (hi - lo) / 4, m1 = lo + max(1u, step), m2 = max(m1, lo + 2 * step), m3 = max(m2, lo + 3 * step);   // in (lo, hi]
+    uint32_t cnt = 0;   // three counts up to 256, 10 bits each
 #pragma unroll
-    for (int i = 0; i < kTopThreads / 32; ++i) cnt += c[i] >= mid;
+    for (int i = 0; i < kTopThreads / 32; ++i) cnt += (c[i] >= m1 ? 1u : 0u) + (c[i] >= m2 ? 1u << 10 : 0u) + (c[i] >= m3 ? 1u << 20 : 0u);
     cnt = __reduce_add_sync(~0u, cnt);
-    if (cnt >= k) {
-      lo = mid;
-      if (cnt <= k + k / 8) break;
-    } else {
-      hi = mid - 1;
-    }
+    const int n1 = cnt & 1023, n2 = cnt >> 10 & 1023, n3 = cnt >> 20;
+    if (n3 >= k) lo = m3, above = n3;
+    else if (n2 >= k) lo = m2, hi = m3 - 1, above = n2;
+    else if (n1 >= k) lo = m1, hi = m2 - 1, above = n1;
+    else hi = m1 - 1;
+    if (above <= enough) break;
   }
-  if (lane == 0) sh.tau = lo;
-}
-
-// Lists the columns of the logits above tau among this thread's granules g[0 .. U), granule u being the part's
-// i0 + u * T-th, where u * T < left: one mark a logit, made two at a time, and few that are set.
-template <int DT, int U>
-__device__ __forceinline__ void collect(TopShared& sh, const Row<DT>& row, const Part<DT>& part, const uint4 (&g)[U], int i0, int left, uint32_t tau2) {
-  using E = Elem<DT>;
-  uint32_t m[E::kMarkWords] = {};
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (u * kTopThreads < left) E::mark(g[u], u, tau2, m);
-#pragma unroll
-  for (int w = 0; w < E::kMarkWords; ++w)
-    while (m[w]) {
-      const int bit = __ffs(m[w]) - 1;
-      m[w] &= m[w] - 1;
-      const int i = part.granule(i0 + E::marked_granule(w, bit) * kTopThreads) * E::VE + E::marked_element(bit);
-      if (i >= row.ph && i < row.end) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < kTopCap) sh.key[at] = (uint32_t)(i - row.ph);
-      }
-    }
+  if (lane == 0) {
+    sh.tau = lo;
+    sh.with_tau = lo == 0 || above <= 2 * enough;
+  }
 }
 
 // Exact tau by passes over 8 bits each, and the keys above it (fewer than k) on the list.
@@ -172,49 +157,64 @@ __device__ __noinline__ void fetch_ties(TopShared& sh, const Row<DT>& row, int v
   __syncthreads();
 }
 
-// After the pass, sh.largest and sh.ordinal written and sh.n 0 behind a barrier: emit(place, key) for the part's largest,
-// place = 0 .. min(k, its length) - 1.  Returns that count.  `piece`: granules of a thread in a piece, a multiple of U.
+// After the pass, sh.largest and sh.ordinal written, sh.n and sh.n_again 0, behind a barrier: emit(place, key) for the
+// part's largest, place = 0 .. min(k, its length) - 1.  Returns that count.  A piece of a thread is `piece` batches of U
+// granules.
 template <int DT, int U, class Emit>
 __device__ __forceinline__ int find_top(TopShared& sh, const Row<DT>& row, const Part<DT>& part, int piece, int k, Emit emit) {
   using E = Elem<DT>;
-  constexpr int T = kTopThreads;
-  const int tid = threadIdx.x;
-  if (tid < 32) bisect_tau(sh, k);
+  constexpr int T = kTopThreads, VE = E::VE;
+  const int tid = threadIdx.x, lane = tid & 31;
+  if (tid < 32) find_tau(sh, k);
   __syncthreads();
   uint32_t tau = sh.tau;
+  const bool with_tau = sh.with_tau && tau != E::ordinal(NAN);   // NaN are ties
+  const float at_tau = tau ? E::value(tau) : NAN;
+  const auto wanted = [&](float x) { return with_tau ? !(x < at_tau) : !(x <= at_tau); };   // NaN is, and everything for tau = 0
   if (tau != E::ordinal(NAN)) {   // nothing is above NaN
-    const float at_tau = tau ? E::value(tau) : NAN;   // everything is above tau = 0
-    const uint32_t tau2 = E::twice(at_tau);
-    for (int q = 0, i0 = tid; i0 < part.n_all; ++q, i0 += T * piece) {
-      if (sh.largest[q][tid] <= at_tau) continue;
-      for (int i = i0; i < min(i0 + T * piece, part.n_all); i += T * U) {
-        uint4 g[U];
-        const int left = part.n_all - i;
+    for (int q = 0; q * T * U * piece < part.n_all; ++q) {
+      const bool w = q * T * U * piece + tid < part.n_all && wanted(sh.largest[q][tid]);
+      const uint32_t all = __ballot_sync(~0u, w);
+      if (!all) continue;
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&sh.n_again, __popc(all));
+      at = __shfl_sync(~0u, at, 0) + __popc(all & ((1u << lane) - 1));
+      if (w) sh.again[at] = (uint16_t)(q * T + tid);
+    }
+  }
+  __syncthreads();
+  for (int j = tid; j < sh.n_again * U; j += T) {
+    const int which = sh.again[j / U], i0 = (which / T * piece * U + j % U) * T + which % T;
+    for (int i = i0; i < min(part.n_all, i0 + piece * U * T); i += U * T) {
+      const uint4 g = part.raw(row, i);
+      if (!wanted(largest<DT>(g))) continue;
+      float x[VE];
+      E::unpack(g, x);
+      const int first = part.granule(i) * VE;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (u * T < left) g[u] = part.raw(row, i + u * T);
-        collect<DT>(sh, row, part, g, i, left, tau2);
-      }
+      for (int e = 0; e < VE; ++e)
+        if (wanted(x[e]) && first + e >= row.ph && first + e < row.end) {
+          const int at = atomicAdd(&sh.n, 1);
+          if (at < kTopCap) sh.key[at] = order_key<DT>(x[e], first + e - row.ph);
+        }
     }
   }
   __syncthreads();
   if (sh.n > kTopCap) {
     select_by_digits<DT>(sh, row, part.v0, part.v1, k);
     tau = sh.tau;
-  } else {   // the listed logits once more, for their keys
-    for (int i = tid; i < sh.n; i += T) {
-      const int column = (int)sh.key[i];
-      sh.key[i] = order_key<DT>(E::to(row.column(column)), column);
-    }
-    __syncthreads();
   }
   if (tau && sh.n < k) fetch_ties<DT>(sh, row, part.v0, part.v1, tau, k - sh.n);
   const int n = sh.n;
-  for (int i = tid; i < n; i += T) {
-    const uint64_t key = sh.key[i];
+  int group = 32;   // threads that share a key's comparisons
+  while (group > 1 && group * n > T) group /= 2;
+  for (int b = 0; b < n; b += T / group) {
+    const int i = b + tid / group;
+    const uint64_t key = i < n ? sh.key[i] : ~0ull;
     int place = 0;
-    for (int j = 0; j < n; ++j) place += sh.key[j] > key;
-    if (place < k) emit(place, key);
+    for (int j = tid % group; j < n; j += group) place += sh.key[j] > key;
+    for (int o = group / 2; o; o /= 2) place += __shfl_xor_sync(~0u, place, o);
+    if (i < n && tid % group == 0 && place < k) emit(place, key);
   }
   return min(n, k);
 }
