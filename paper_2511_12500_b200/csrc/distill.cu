@@ -161,6 +161,7 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillBlocks) distill_kerne
   const int64_t step = gridDim.x / split;
   int64_t r = blockIdx.x / split;
   if (split > 1) ptx::cluster_arrive_relaxed();
+  ptx::begin_after_previous();
   const float k = p.scale * kLog2e;
   const bool grad = p.dlogits != nullptr;
 
@@ -354,6 +355,7 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillBlocks) distill_kerne
     in = next;
     part = next_part;
   }
+  ptx::let_next_begin();
 }
 
 template <int DT, bool TAIL>
@@ -362,6 +364,8 @@ __global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const Distil
   __shared__ TeacherSums teacher;
   const int64_t r = blockIdx.x / p.split;
   const int tid = threadIdx.x;
+  ptx::let_next_begin();
+  ptx::begin_after_previous();
   const Row<DT> in(p.logits, r, p.stride, p.vocab), out(p.dlogits, r, p.grad_stride, p.vocab);
   const float w = p.weight[r], m = p.stats[3 * r], ls = p.stats[3 * r + 1], lr = p.stats[3 * r + 2];
   const Entry e = load_entry(p, r).checked<TAIL>(p);
@@ -436,17 +440,6 @@ int launch_distill(const DistillParams& p, cudaStream_t st) {
     IRIS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldBytes + kHoldBytes / 16));
     if (dev < kMaxDevices) configured[dev] = true;
   }
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)p.split);
-  cfg.blockDim = dim3(kDistillThreads);
-  cfg.dynamicSmemBytes = (size_t)bytes;
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)p.split;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = p.split > 1 ? 1 : 0;
   // As many clusters as the device holds at a time: one more would run after the others have done all their rows.  The
   // answer is kept (it depends on the kernel, the split and the bytes alone), as asking takes longer than a small launch.
   int clusters = 0;
@@ -456,26 +449,35 @@ int launch_distill(const DistillParams& p, cudaStream_t st) {
   if ((was & ~0xffffull) == key) {
     clusters = (int)(was & 0xffff);
   } else {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)p.split);
+    cfg.blockDim = dim3(kDistillThreads);
+    cfg.dynamicSmemBytes = (size_t)bytes;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)p.split;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = p.split > 1 ? 1 : 0;
     if (p.split > 1) IRIS_CUDA_TRY(cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg));
     else IRIS_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&clusters, kernel, kDistillThreads, (size_t)bytes));
     if (p.split == 1) clusters *= kSms;
     clusters = std::max(1, std::min(clusters, 0xffff));
     known[p.split].store(key | (uint64_t)clusters, std::memory_order_relaxed);
   }
-  cfg.gridDim = dim3((unsigned)(std::min(clusters, p.rows) * p.split));
-  IRIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
-  return IRIS_OK;
+  return launch_rows(kernel, p, (unsigned)(std::min(clusters, p.rows) * p.split), p.split, kDistillThreads, (size_t)bytes, st);
 }
 
 template <int DT>
 int launch_distill(DistillParams p, bool tail, cudaStream_t st) {
   // A row is shared by a cluster of blocks until a part is at most kPartBytes, or while the rows alone leave SMs without
   // work and every thread still has a granule.
-  const int64_t granules = part_granules(p.vocab, DT, 1);
+  const int64_t granules = part_granules(p.logits, p.stride, p.vocab, DT, 1);
   int split = 1;
   while (split < kMaxSplit && (granules * 16 > (int64_t)split * kPartBytes || ((int64_t)p.rows * split < 2 * kSms && granules >= (int64_t)split * 2 * kDistillThreads))) ++split;
   p.split = split;
-  p.each = part_granules(p.vocab, DT, split);
+  p.each = part_granules(p.logits, p.stride, p.vocab, DT, split);
   p.hold = std::max(1, std::min(p.each, kHoldBytes / 16));
   if (p.each <= kHoldBytes / 16) return tail ? launch_distill<DT, true, true>(p, st) : launch_distill<DT, false, true>(p, st);
   return tail ? launch_distill<DT, true, false>(p, st) : launch_distill<DT, false, false>(p, st);
@@ -483,9 +485,7 @@ int launch_distill(DistillParams p, bool tail, cudaStream_t st) {
 
 template <int DT, bool TAIL>
 int launch_distill_grad(const DistillParams& p, int64_t rows, cudaStream_t st) {
-  distill_grad_kernel<DT, TAIL><<<(unsigned)(rows * p.split), kGradThreads, 0, st>>>(p);
-  IRIS_CUDA_TRY(cudaGetLastError());
-  return IRIS_OK;
+  return launch_rows(distill_grad_kernel<DT, TAIL>, p, (unsigned)(rows * p.split), 1, kGradThreads, 0, st);
 }
 
 }  // namespace
@@ -515,7 +515,7 @@ extern "C" int iris_distill_topk_backward(const iris_distill_args* a, void* stre
   if (!a->dlogits) return fail(IRIS_ERR_ARG, "%s: dlogits is NULL", fn);
   DistillParams p = params_of(a, stride, gstride);
   p.split = grad_parts(a->vocab, a->dtype);
-  p.each = part_granules(a->vocab, a->dtype, p.split);
+  p.each = part_granules(a->logits, stride, a->vocab, a->dtype, p.split);
   if (a->rows * p.split > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 blocks", fn);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool tail = a->mode == IRIS_DISTILL_TAIL;

@@ -12,6 +12,7 @@
 #include <type_traits>
 
 #include "iris_device.cuh"
+#include "sm100_ptx.cuh"
 
 namespace iris {
 namespace rows {
@@ -484,8 +485,10 @@ inline int check_logits(const char* fn, const char* what, const void* p, int dty
   return IRIS_OK;
 }
 // Granules of a row, wherever it starts, in equal parts.
-inline int part_granules(int64_t vocab, int dtype, int parts) {
-  const int64_t ve = 16 / (int64_t)elem_size(dtype), granules = (vocab + 2 * ve - 2) / ve;
+inline int part_granules(const void* p, int64_t stride, int64_t vocab, int dtype, int parts) {
+  const int64_t es = (int64_t)elem_size(dtype), ve = 16 / es;
+  const bool aligned = reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % ve == 0;
+  const int64_t granules = (vocab + (aligned ? ve - 1 : 2 * ve - 2)) / ve;
   return (int)((granules + parts - 1) / parts);
 }
 inline int check_scale(const char* fn, const char* what, float s) {
@@ -510,6 +513,26 @@ inline int check_in_place(const char* fn, const void* logits, int64_t stride, co
     if (d >= row && s - d >= row) return IRIS_OK;
   }
   return fail(IRIS_ERR_ARG, "%s: dlogits overlaps logits and is not the same matrix", fn);
+}
+// Launches clusters of `split` blocks.  A kernel may begin while the one before it in the stream ends (it waits for that
+// one before it reads anything): a decoding step's calls are about as long as the gap between two launches.
+template <class P>
+inline int launch_rows(void (*kernel)(P), const P& p, unsigned blocks, int split, int threads, size_t bytes, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)split;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = split > 1 ? 2 : 1;
+  IRIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
+  return IRIS_OK;
 }
 #define IRIS_CHECK(expr)              \
   do {                                \

@@ -224,6 +224,11 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t bar, uint16_t mask) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(mask) : "memory");
 }
 
+// Launches that may begin while the kernel before them in the stream ends: begin_after_previous() waits until that one is
+// done and its writes are visible; let_next_begin() says that this kernel's blocks have all the SM room that they will take.
+__device__ __forceinline__ void begin_after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Named barrier among `count` threads that also ORs a predicate over them.
 __device__ __forceinline__ bool bar_red_or(int id, int count, bool pred) {
   uint32_t out;

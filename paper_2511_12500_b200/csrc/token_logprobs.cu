@@ -11,8 +11,8 @@ namespace iris {
 namespace rows {
 
 constexpr int kScoreThreads = 256;
-constexpr int kScoreGranules = 4;       // of 16 bytes a thread holds at once
-constexpr int kScoreBlocks = 5;         // an SM's registers are shared out for
+constexpr int kOneBatch = 2048;         // granules of a part that its block holds in registers, 8 a thread
+enum { kNoTop, kTopPiecewise, kTopOneBatch };
 constexpr int kMaxSplit = 8;            // blocks (one cluster) that share a row
 static_assert(kScoreThreads == kTopThreads, "the list is kept by all threads of the block");
 
@@ -33,13 +33,15 @@ __device__ __forceinline__ float log_prob(float z, float m, float ls, float scal
 struct NoTop {};
 
 // One cluster of `split` blocks a row; each takes an equal run of granules, and all get what each found.
-template <int DT, bool ENTROPY, bool TOP>
-__global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) score_kernel(const ScoreParams p) {
+// TOP: no alternatives; alternatives of a part of any length, of which pieces are read again; of a part of at most
+// kOneBatch granules, which stays in registers.
+template <int DT, bool ENTROPY, int TOP>
+__global__ void __launch_bounds__(kScoreThreads, TOP == kTopOneBatch ? 4 : 5) score_kernel(const ScoreParams p) {
   using E = Elem<DT>;
-  constexpr int T = kScoreThreads, U = kScoreGranules;
+  constexpr int T = kScoreThreads, U = TOP == kTopOneBatch ? kOneBatch / T : 4;
   __shared__ Warps<T / 32> buf;
   __shared__ Warps<kMaxSplit> parts;   // of the cluster's blocks
-  __shared__ typename std::conditional<TOP, TopShared, NoTop>::type top;
+  __shared__ typename std::conditional<TOP != kNoTop, TopShared, NoTop>::type top;
   extern __shared__ uint64_t lists[];   // TOP and split > 1: the blocks' sorted lists, top_k keys each, 0 where one is shorter
   const int split = p.split, rank = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x;
   const int64_t r = blockIdx.x / split;
@@ -50,6 +52,7 @@ __global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) score_kernel(cons
   const Row<DT> row(p.logits, r, p.stride, p.vocab);
   const Part<DT> part(row, rank, p.each);
   const float k = p.scale * kLog2e;
+  ptx::begin_after_previous();
   float zt = 0.f;
   bool there = false;
   if (rank == 0 && tid < p.n_targets) {
@@ -59,41 +62,84 @@ __global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) score_kernel(cons
   }
   Sums<DT, ENTROPY> sums(k);
   const uint4* const from = reinterpret_cast<const uint4*>(row.at(part.w0)) + tid;
-  const int n = part.n_all, piece = TOP ? max(1, ((n + T * U - 1) / (T * U) + kTopPieces - 1) / kTopPieces) : 1;   // batches of one
+  const int n = part.n_all, shift = TOP == kTopPiecewise ? piece_shift(n) : 0;
   float best = -INFINITY, of_piece = -INFINITY;
-  int done = 0, q = 0;
-  const auto batch = [&](int b, auto all) {
+  uint4 g[U];
+  const auto load = [&](int b, auto all) {
     constexpr bool ALL = decltype(all)::value;
     const int left = n - b - tid;   // this thread has granules u with u * T < left
-    uint4 g[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (ALL) g[u] = ld_once(from + b + u * T);
       else if (u * T < left) g[u] = part.raw(row, b + u * T + tid);
     }
+  };
+  const auto batch = [&](int b, auto all) {
+    constexpr bool ALL = decltype(all)::value;
+    const int left = n - b - tid;
+    load(b, all);
     const float mx = largest<DT, ALL>(g, left, T);
     sums.template add<ALL>(g, mx, left, T);
-    if constexpr (TOP) {
-      of_piece = max_nan(of_piece, mx);
-      top.largest[q][tid] = of_piece;
-      if (++done == piece) {
-        best = max_nan(best, of_piece);
-        of_piece = -INFINITY;
-        done = 0;
-        ++q;
+    if constexpr (TOP == kTopPiecewise) {   // the largest of each piece: 1 or 2 granules of the batch, all of them, or those of several batches
+      static_assert(TOP != kTopPiecewise || U == 4, "pieces of 1, 2 and 4 granules lie in a batch");
+      const int u0 = b / T, q = u0 >> shift;   // the batch's first granule of the thread, and its piece
+      best = max_nan(best, mx);
+      if (shift == 0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (ALL || u * T < left) top.largest[q + u][tid] = largest<DT>(g[u]);
+      } else if (shift == 1) {
+#pragma unroll
+        for (int u = 0; u < U; u += 2)
+          if (ALL || u * T < left)
+            top.largest[q + u / 2][tid] = E::unfold(ALL || (u + 1) * T < left ? E::larger(E::fold(g[u]), E::fold(g[u + 1])) : E::fold(g[u]));
+      } else {
+        of_piece = u0 & ((1 << shift) - 1) ? max_nan(of_piece, mx) : mx;
+        if (ALL || left > 0) top.largest[q][tid] = of_piece;
       }
     }
   };
-  int b = 0;
-  for (; b + T * U <= part.n_int; b += T * U) batch(b, std::true_type{});
-  for (; b < n; b += T * U) batch(b, std::false_type{});
-  warp_share<ENTROPY>(sums.done(), k, buf);
-  if constexpr (TOP) {
-    top.ordinal[tid] = tid < n ? E::ordinal(max_nan(best, of_piece)) : 0;
-    if (tid == 0) top.n = top.n_again = 0;
+  if constexpr (TOP == kTopOneBatch) {
+    load(0, std::false_type{});
+    best = largest<DT, false>(g, n - tid, T);
+    top.ordinal[tid] = tid < n ? E::ordinal(best) : 0;
+    if (tid == 0) top.n = top.n_queue = 0;
+    __syncthreads();
+    if (tid < 32) find_tau(top, p.top_k);   // while the other warps go on
+    sums.template add<false>(g, best, n - tid, T);
+  } else {
+    int b = 0;
+    for (; b + T * U <= part.n_int; b += T * U) batch(b, std::true_type{});
+    for (; b < n; b += T * U) batch(b, std::false_type{});
+    if constexpr (TOP) {
+      top.ordinal[tid] = tid < n ? E::ordinal(best) : 0;
+      if (tid == 0) top.n = top.n_again = top.n_queue = 0;
+    }
   }
+  ptx::let_next_begin();
+  warp_share<ENTROPY>(sums.done(), k, buf);
   __syncthreads();
   Acc a = warps_join<ENTROPY>(k, buf);
+  const auto find_top = [&](auto emit) -> int {
+    if constexpr (TOP == kTopPiecewise) {
+      if (tid < 32) find_tau(top, p.top_k);
+      __syncthreads();
+    }
+    if constexpr (TOP != kNoTop) {
+      const Wanted<DT> wanted(top);
+      if constexpr (TOP == kTopPiecewise) {
+        queue_pieces<DT>(top, row, part, shift, wanted);
+      } else if (!wanted.none && wanted(best)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (u * T < n - tid && wanted(largest<DT>(g[u]))) queue_granule(top, part.granule(u * T + tid), g[u]);
+      }
+      __syncthreads();
+      list_queue<DT>(top, row, wanted);
+      return finish_top<DT>(top, row, part, wanted.tau, p.top_k, emit);
+    }
+    return 0;
+  };
 
   if (split > 1) {
     ptx::cluster_wait();   // all blocks have started
@@ -108,7 +154,7 @@ __global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) score_kernel(cons
       const auto share = [&](int place, uint64_t key) {
         for (int s = 0; s < split; ++s) ptx::st_shared_cluster_u64(ptx::mapa(own + place * 8, s), key);
       };
-      const int found = find_top<DT, U>(top, row, part, piece, p.top_k, share);
+      const int found = find_top(share);
       if (tid >= found && tid < p.top_k) share(tid, 0);
     }
     ptx::cluster_sync();
@@ -129,7 +175,7 @@ __global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) score_kernel(cons
       if (p.top_logprob) p.top_logprob[r * p.top_k + place] = log_prob(key_value<DT>(key), a.m, ls, p.scale);
     };
     if (split == 1) {
-      find_top<DT, U>(top, row, part, piece, p.top_k, emit);
+      find_top(emit);
     } else {   // every block finds the places of its own keys, with a group of threads each
       int group = 32;
       while (group * p.top_k > T) group /= 2;   // >= 2: top_k <= 128
@@ -143,27 +189,17 @@ __global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) score_kernel(cons
   }
 }
 
-template <int DT, bool ENTROPY, bool TOP>
+template <int DT, bool ENTROPY>
 static int launch_score(const ScoreParams& p, int64_t rows, cudaStream_t st) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(rows * p.split));
-  cfg.blockDim = dim3(kScoreThreads);
-  cfg.dynamicSmemBytes = TOP && p.split > 1 ? (size_t)p.split * p.top_k * 8 : 0;
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)p.split;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = p.split > 1 ? 1 : 0;
-  IRIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, score_kernel<DT, ENTROPY, TOP>, p));
-  return IRIS_OK;
+  const auto kernel = !p.top_k             ? score_kernel<DT, ENTROPY, kNoTop>
+                      : p.each > kOneBatch ? score_kernel<DT, ENTROPY, kTopPiecewise>
+                                           : score_kernel<DT, ENTROPY, kTopOneBatch>;
+  return launch_rows(kernel, p, (unsigned)(rows * p.split), p.split, kScoreThreads, p.split > 1 ? (size_t)p.split * p.top_k * 8 : 0, st);
 }
 
 template <int DT>
 static int launch_score(const ScoreParams& p, int64_t rows, cudaStream_t st) {
-  if (p.entropy) return p.top_k ? launch_score<DT, true, true>(p, rows, st) : launch_score<DT, true, false>(p, rows, st);
-  return p.top_k ? launch_score<DT, false, true>(p, rows, st) : launch_score<DT, false, false>(p, rows, st);
+  return p.entropy ? launch_score<DT, true>(p, rows, st) : launch_score<DT, false>(p, rows, st);
 }
 
 struct ScoreGradParams {
@@ -180,6 +216,8 @@ struct ScoreGradParams {
 template <int DT, bool ENTROPY>
 __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const ScoreGradParams p) {
   __shared__ List list;
+  ptx::let_next_begin();
+  ptx::begin_after_previous();
   const int64_t r = blockIdx.x / p.parts;
   const Row<DT> in(p.logits, r, p.stride, p.vocab), out(p.dlogits, r, p.grad_stride, p.vocab);
   const int n = p.grad_logprob ? p.n_targets : 0;
@@ -212,11 +250,9 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const ScoreGra
 
 template <int DT>
 static int launch_score_grad(const ScoreGradParams& p, int64_t rows, cudaStream_t st) {
-  const unsigned grid = (unsigned)(rows * p.parts);
-  if (p.grad_entropy) score_grad_kernel<DT, true><<<grid, kGradThreads, 0, st>>>(p);
-  else score_grad_kernel<DT, false><<<grid, kGradThreads, 0, st>>>(p);
-  IRIS_CUDA_TRY(cudaGetLastError());
-  return IRIS_OK;
+  const unsigned blocks = (unsigned)(rows * p.parts);
+  if (p.grad_entropy) return launch_rows(score_grad_kernel<DT, true>, p, blocks, 1, kGradThreads, 0, st);
+  return launch_rows(score_grad_kernel<DT, false>, p, blocks, 1, kGradThreads, 0, st);
 }
 
 }  // namespace rows
@@ -242,12 +278,11 @@ extern "C" int iris_token_logprobs(const iris_logprob_args* a, void* stream) {
   IRIS_CHECK(check_aligned(fn, "stats", a->stats, 4, false));
   IRIS_CHECK(check_aligned(fn, "top_ids", a->top_ids, 8, a->top_k > 0));
   IRIS_CHECK(check_aligned(fn, "top_logprob", a->top_logprob, 4, false));
-  // A row is shared by a cluster of blocks while the rows alone leave SMs without work and every block still has a batch
-  // of granules.
-  const int64_t granules = part_granules(a->vocab, a->dtype, 1);
+  // A row is shared by a cluster of blocks while the rows alone leave SMs without work, until a part fits registers.
+  const int64_t granules = part_granules(a->logits, stride, a->vocab, a->dtype, 1);
   int split = 1;
-  while (split < kMaxSplit && a->rows * split < 2 * kSms && granules >= (int64_t)split * 2 * kScoreThreads * kScoreGranules) split *= 2;
-  ScoreParams p{a->logits, stride, (int)a->vocab, want_lp ? a->n_targets : 0, a->top_k, split, part_granules(a->vocab, a->dtype, split), a->scale, a->targets, a->logprob, a->entropy, a->stats,
+  while (split < kMaxSplit && a->rows * split < 2 * kSms && granules > (int64_t)split * kOneBatch) split *= 2;
+  ScoreParams p{a->logits, stride, (int)a->vocab, want_lp ? a->n_targets : 0, a->top_k, split, part_granules(a->logits, stride, a->vocab, a->dtype, split), a->scale, a->targets, a->logprob, a->entropy, a->stats,
                 a->top_logprob, a->top_ids};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (a->dtype == IRIS_BF16) return launch_score<IRIS_BF16>(p, a->rows, st);
@@ -273,7 +308,7 @@ extern "C" int iris_token_logprobs_backward(const iris_logprob_grad_args* a, voi
   IRIS_CHECK(check_aligned(fn, "entropy", a->entropy, 4, want_h));
   const int parts = grad_parts(a->vocab, a->dtype);
   if (a->rows * parts > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 blocks", fn);
-  ScoreGradParams p{a->logits, stride, gstride, (int)a->vocab, a->n_targets, parts, part_granules(a->vocab, a->dtype, parts), a->scale, a->targets, a->stats, a->entropy,
+  ScoreGradParams p{a->logits, stride, gstride, (int)a->vocab, a->n_targets, parts, part_granules(a->logits, stride, a->vocab, a->dtype, parts), a->scale, a->targets, a->stats, a->entropy,
                     want_lp ? a->grad_logprob : nullptr, a->grad_entropy, a->dlogits};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (a->dtype == IRIS_BF16) return launch_score_grad<IRIS_BF16>(p, a->rows, st);

@@ -20,15 +20,23 @@ constexpr int kTopPieces = 16;
 constexpr int kTopCap = 1024;   // > 127 granules of 8, what a block can hold with fewer than k threads at work
 static_assert(kTopThreads >= kMaxList && kTopCap >= (kMaxList - 1) * 8, "the list holds all of a part that has fewer granules than k");
 
+constexpr int kTopQueue = 768;   // granules with wanted logits
+
 struct TopShared {
   alignas(16) uint64_t key[kTopCap];
-  float largest[kTopPieces][kTopThreads];   // of a thread's logits in a piece of the row
+  union {
+    float largest[kTopPieces][kTopThreads];   // of a thread's logits in a piece
+    struct {
+      uint4 granule[kTopQueue];
+      int index[kTopQueue];
+    } queue;
+  };
   uint32_t ordinal[kTopThreads];            // of a thread's largest logit; 0 = it has none
   uint16_t again[kTopPieces * kTopThreads]; // pieces to be read again: piece * kTopThreads + thread
   uint32_t hist[256];
   uint32_t tau;
   int with_tau;   // logits equal to tau are listed too
-  int n, n_again, warp_sum[kTopThreads / 32];
+  int n, n_again, n_queue, warp_sum[kTopThreads / 32];
 };
 
 // By one warp: the largest tau it finds with at least k of sh.ordinal >= tau (0 if fewer than k are not 0), by quartering;
@@ -157,48 +165,91 @@ __device__ __noinline__ void fetch_ties(TopShared& sh, const Row<DT>& row, int v
   __syncthreads();
 }
 
-// After the pass, sh.largest and sh.ordinal written, sh.n and sh.n_again 0, behind a barrier: emit(place, key) for the
-// part's largest, place = 0 .. min(k, its length) - 1.  Returns that count.  A piece of a thread is `piece` batches of U
-// granules.
-template <int DT, int U, class Emit>
-__device__ __forceinline__ int find_top(TopShared& sh, const Row<DT>& row, const Part<DT>& part, int piece, int k, Emit emit) {
+// Granules of a thread in a piece, as a power of two: at most kTopPieces pieces.
+__device__ __forceinline__ int piece_shift(int n_all) {
+  const int each = (n_all + kTopThreads - 1) / kTopThreads;
+  int s = 0;
+  while ((each + (1 << s) - 1) >> s > kTopPieces) ++s;
+  return s;
+}
+
+// Which logits the list takes; NaN is wanted, and everything for tau = 0.
+template <int DT>
+struct Wanted {
+  uint32_t tau;
+  float at_tau;
+  bool with_tau, none;
+  __device__ __forceinline__ explicit Wanted(const TopShared& sh) : tau(sh.tau) {
+    using E = Elem<DT>;
+    none = tau == E::ordinal(NAN);   // nothing is above NaN: they are fetched as ties
+    with_tau = sh.with_tau && !none;
+    at_tau = tau ? E::value(tau) : NAN;
+  }
+  __device__ __forceinline__ bool operator()(float x) const { return with_tau ? !(x < at_tau) : !(x <= at_tau); }
+};
+
+// Granules with wanted logits are queued with their bits, and then looked through an element a thread: inside the pass, or
+// where a thread has read a granule again, one that holds a wanted logit would stop its warp for all its elements.
+__device__ __forceinline__ void queue_granule(TopShared& sh, int v, const uint4& g) {
+  const int at = atomicAdd(&sh.n_queue, 1);
+  if (at < kTopQueue) {
+    sh.queue.granule[at] = g;
+    sh.queue.index[at] = v;
+  }
+}
+template <int DT>
+__device__ __forceinline__ void list_queue(TopShared& sh, const Row<DT>& row, const Wanted<DT>& wanted) {   // behind a barrier
   using E = Elem<DT>;
-  constexpr int T = kTopThreads, VE = E::VE;
+  constexpr int VE = E::VE;
+  const int n = sh.n_queue;
+  if (n > kTopQueue) {
+    if (threadIdx.x == 0) sh.n = kTopCap + 1;   // too many for the list, too
+    return;
+  }
+  for (int j = threadIdx.x; j < n * VE; j += kTopThreads) {
+    const int i = sh.queue.index[j / VE] * VE + j % VE;
+    const float x = E::to(reinterpret_cast<const typename E::T*>(&sh.queue.granule[j / VE])[j % VE]);
+    if (wanted(x) && i >= row.ph && i < row.end) {
+      const int at = atomicAdd(&sh.n, 1);
+      if (at < kTopCap) sh.key[at] = order_key<DT>(x, i - row.ph);
+    }
+  }
+}
+
+// Queues what is wanted of a part, of which sh.largest has the pieces' largest logits.  One barrier.
+template <int DT>
+__device__ __forceinline__ void queue_pieces(TopShared& sh, const Row<DT>& row, const Part<DT>& part, int shift, const Wanted<DT>& wanted) {
+  constexpr int T = kTopThreads;
   const int tid = threadIdx.x, lane = tid & 31;
-  if (tid < 32) find_tau(sh, k);
-  __syncthreads();
-  uint32_t tau = sh.tau;
-  const bool with_tau = sh.with_tau && tau != E::ordinal(NAN);   // NaN are ties
-  const float at_tau = tau ? E::value(tau) : NAN;
-  const auto wanted = [&](float x) { return with_tau ? !(x < at_tau) : !(x <= at_tau); };   // NaN is, and everything for tau = 0
-  if (tau != E::ordinal(NAN)) {   // nothing is above NaN
-    for (int q = 0; q * T * U * piece < part.n_all; ++q) {
-      const bool w = q * T * U * piece + tid < part.n_all && wanted(sh.largest[q][tid]);
-      const uint32_t all = __ballot_sync(~0u, w);
-      if (!all) continue;
-      int at = 0;
-      if (lane == 0) at = atomicAdd(&sh.n_again, __popc(all));
-      at = __shfl_sync(~0u, at, 0) + __popc(all & ((1u << lane) - 1));
-      if (w) sh.again[at] = (uint16_t)(q * T + tid);
-    }
-  }
-  __syncthreads();
-  for (int j = tid; j < sh.n_again * U; j += T) {
-    const int which = sh.again[j / U], i0 = (which / T * piece * U + j % U) * T + which % T;
-    for (int i = i0; i < min(part.n_all, i0 + piece * U * T); i += U * T) {
-      const uint4 g = part.raw(row, i);
-      if (!wanted(largest<DT>(g))) continue;
-      float x[VE];
-      E::unpack(g, x);
-      const int first = part.granule(i) * VE;
+  uint32_t pieces = 0;
+  if (!wanted.none)
+    for (int q = 0; (q << shift) * T + tid < part.n_all; ++q) pieces |= wanted(sh.largest[q][tid]) ? 1u << q : 0u;
+  const int mine = __popc(pieces);
+  int upto = mine;
 #pragma unroll
-      for (int e = 0; e < VE; ++e)
-        if (wanted(x[e]) && first + e >= row.ph && first + e < row.end) {
-          const int at = atomicAdd(&sh.n, 1);
-          if (at < kTopCap) sh.key[at] = order_key<DT>(x[e], first + e - row.ph);
-        }
-    }
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(~0u, upto, o);
+    if (lane >= o) upto += y;
   }
+  int at = 0;
+  if (lane == 31 && upto) at = atomicAdd(&sh.n_again, upto);
+  at = __shfl_sync(~0u, at, 31) + upto - mine;
+  for (; pieces; pieces &= pieces - 1) sh.again[at++] = (uint16_t)((__ffs(pieces) - 1) * T + tid);
+  __syncthreads();
+  for (int j = tid; j < sh.n_again << shift; j += T) {
+    const int which = sh.again[j >> shift], i = ((which / T << shift) + (j & ((1 << shift) - 1))) * T + which % T;
+    if (i >= part.n_all) continue;
+    const uint4 g = part.raw(row, i);
+    if (wanted(largest<DT>(g))) queue_granule(sh, part.granule(i), g);
+  }
+}
+
+// Once all threads have listed what is wanted: emit(place, key) for the part's largest, place = 0 ..
+// min(k, its length) - 1.  Returns that count.
+template <int DT, class Emit>
+__device__ __forceinline__ int finish_top(TopShared& sh, const Row<DT>& row, const Part<DT>& part, uint32_t tau, int k, Emit emit) {
+  constexpr int T = kTopThreads;
+  const int tid = threadIdx.x;
   __syncthreads();
   if (sh.n > kTopCap) {
     select_by_digits<DT>(sh, row, part.v0, part.v1, k);
