@@ -16,6 +16,8 @@ namespace rows {
 
 constexpr int kDistillThreads = 128;
 constexpr int kDistillBlocks = 4;   // an SM's registers are shared out for
+constexpr int kLossBlocks = 8;
+enum { kLossOnly, kHeld, kReadTwice };
 constexpr int kMaxSplit = 8;   // blocks (one cluster) that share a row
 static_assert(kDistillThreads >= kMaxList && kGradThreads >= kMaxList, "one thread an entry of the list");
 
@@ -137,15 +139,18 @@ struct Edge {
   }
 };
 
-// A cluster of `split` blocks takes rows one after the other; each block has a part of the row.  HELD: the part lies in
-// shared memory, where a thread uses only the granules that it copied itself, and the gradient is computed from there, so a row
-// is read once; as soon as a granule has been used for the last time its place takes the next row's, which is under way
-// while this one is finished.  A byte a granule (on_list) says which of its tokens are on the list: with a remainder they
-// leave the sum.  Not HELD: a part too large for that is read twice.
-template <int DT, bool TAIL, bool HELD>
-__global__ void __launch_bounds__(kDistillThreads, kDistillBlocks) distill_kernel(const DistillParams p) {
+// A cluster of `split` blocks takes rows one after the other; each block has a part of the row.
+//   kHeld       The part lies in shared memory, where a thread uses only the granules that it copied itself, and the
+//               gradient is computed from there, so a row is read once.  As soon as a granule has been used for the last
+//               time its place takes the next row's, which is under way while this one is finished.
+//   kLossOnly   Nothing has to be held; a cluster for every row.
+//   kReadTwice  The gradient of a part too large for shared memory.
+// A byte a granule (on_list) says which of its tokens are on the list: with a remainder they leave the sum.
+template <int DT, bool TAIL, int MODE>
+__global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBlocks : kDistillBlocks) distill_kernel(const DistillParams p) {
   using E = Elem<DT>;
   constexpr int VE = E::VE, T = kDistillThreads, U = 4;   // granules of a batch
+  constexpr bool HELD = MODE == kHeld, grad = MODE != kLossOnly;
   extern __shared__ uint4 held[];
   __shared__ List lists[2];          // of this row and the one before
   __shared__ TeacherSums teacher;
@@ -163,7 +168,6 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillBlocks) distill_kerne
   if (split > 1) ptx::cluster_arrive_relaxed();
   ptx::begin_after_previous();
   const float k = p.scale * kLog2e;
-  const bool grad = p.dlogits != nullptr;
 
   RawEntry ahead = load_entry(p, r);
   float w = p.weight ? p.weight[r] : 1.f;
@@ -193,7 +197,7 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillBlocks) distill_kerne
     bool first = false;                                                // of entries with the same column
     if (tid == 0) repeats[turn ^ 1] = 0;
     const int64_t r_next = r + step;
-    const bool more = r_next < p.rows;
+    const bool more = MODE != kLossOnly && r_next < p.rows;
     const Row<DT> next(p.logits, more ? r_next : r, p.stride, p.vocab);
     const Part<DT> next_part(next, rank, p.each);
     const uint4* const from = reinterpret_cast<const uint4*>(next.at(next_part.w0));
@@ -228,8 +232,6 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillBlocks) distill_kerne
         const uint4 g[1] = {without<DT>(edge.raw(), TAIL ? marks[part.n_int + tid] : 0)};
         sums.template add<true>(g, largest<DT>(g[0]));
       }
-      if (!grad)
-        for (int i = tid; i < n_next; i += T) copy_async(held_at + i * 16, from + i);
     } else {
       for (int b0 = 0; b0 < part.n_all; b0 += p.hold) {   // p.hold granules at a time have marks
         const bool in_piece = TAIL && own && mark >= b0 && mark < b0 + p.hold;
@@ -237,10 +239,33 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillBlocks) distill_kerne
           if (in_piece) first = !(atomicOr(&on_list[(mark - b0) / 4], bit) & bit);
           __syncthreads();
         }
-        for (int i = b0 + tid; i < min(part.n_all, b0 + p.hold); i += T) {
-          const uint4 g[1] = {without<DT>(part.raw(in, i), TAIL ? marks[i - b0] : 0)};
-          sums.template add<true>(g, largest<DT>(g[0]));
-        }
+        const int size = min(part.n_all - b0, p.hold), inside = min(part.n_int - b0, size);
+        const uint4* const at = reinterpret_cast<const uint4*>(in.at(part.w0)) + b0 + tid;
+        const auto batch = [&](int b, auto all) {
+          constexpr bool ALL = decltype(all)::value;
+          const int left = size - b - tid;
+          uint4 g[U];
+          uint32_t bits[U], any = 0;
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            if (ALL) g[u] = ld_once(at + b + u * T);
+            else if (u * T < left) g[u] = part.raw(in, b0 + b + u * T + tid);
+          }
+          if (TAIL) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+              if (ALL || u * T < left) any |= bits[u] = marks[b + u * T + tid];
+            if (any) {
+#pragma unroll
+              for (int u = 0; u < U; ++u)
+                if (ALL || u * T < left) g[u] = without<DT>(g[u], bits[u]);
+            }
+          }
+          sums.template add<ALL>(g, largest<DT, ALL>(g, left, T), left, T);
+        };
+        int b = 0;
+        for (; b + T * U <= inside; b += T * U) batch(b, std::true_type{});
+        for (; b < size; b += T * U) batch(b, std::false_type{});
         if (TAIL) {
           __syncthreads();
           if (in_piece) on_list[(mark - b0) / 4] = 0;
@@ -292,7 +317,7 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillBlocks) distill_kerne
     }
     bool rep = false;
     float listed_grad = 0.f, add = 0.f;
-    if (grad) {
+    if constexpr (grad) {
       coef = distill_coef<TAIL>(p, teach.y, teach.z, all.m, ls, lr, w_row);
       add = -w_row * p.scale * pk;
       listed_grad = grad_of(zk, coef);
@@ -326,10 +351,25 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillBlocks) distill_kerne
         }
       } else {
         if (split == 1) __syncthreads();   // the listed logits have been read
-        for (int i = tid; i < part.n_all; i += T) write_elements(in, out, dense_part, part.granule(i), part.raw(in, i));
+        if (in.ph == out.ph && dense_part.plain()) {
+          const uint4* const at = reinterpret_cast<const uint4*>(in.at(part.w0)) + tid;
+          uint4* const to = reinterpret_cast<uint4*>(out.at(part.w0)) + tid;
+          batches<T, U>(part.n_int, [&](int b, auto all) {
+            constexpr bool ALL = decltype(all)::value;
+            const int left = part.n_int - b - tid;
+            uint4 g[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+              if ((ALL || u * T < left) && !coef.zero) g[u] = ld_once(at + b + u * T);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+              if (ALL || u * T < left) st_global_v4(to + b + u * T, dense_of(dense_part, g[u]));
+          });
+          if (tid < part.n_all - part.n_int) write_elements(in, out, dense_part, part.granule(part.n_int + tid), part.raw(in, part.n_int + tid));
+        } else {
+          for (int i = tid; i < part.n_all; i += T) write_elements(in, out, dense_part, part.granule(i), part.raw(in, i));
+        }
       }
-    } else if (HELD && more) {
-      edge.load(next, next_part);
     }
     if (rank == 0 && tid < kMaxList) {
       float l = 0.f;
@@ -352,6 +392,7 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillBlocks) distill_kerne
         p.stats[3 * r + 2] = ls == -INFINITY && TAIL ? -INFINITY : lr;
       }
     }
+    if (MODE == kLossOnly) break;
     in = next;
     part = next_part;
   }
@@ -429,10 +470,10 @@ DistillParams params_of(const iris_distill_args* a, int64_t stride, int64_t gstr
   return p;
 }
 
-template <int DT, bool TAIL, bool HELD>
+template <int DT, bool TAIL, int MODE>
 int launch_distill(const DistillParams& p, cudaStream_t st) {
-  const auto kernel = distill_kernel<DT, TAIL, HELD>;
-  const int bytes = (HELD ? p.hold * 16 : 0) + (p.hold + 3) / 4 * 4;
+  const auto kernel = distill_kernel<DT, TAIL, MODE>;
+  const int bytes = (MODE == kHeld ? p.hold * 16 : 0) + (p.hold + 3) / 4 * 4;
   static bool configured[kMaxDevices] = {};
   int dev = -1;
   IRIS_CUDA_TRY(cudaGetDevice(&dev));
@@ -440,6 +481,7 @@ int launch_distill(const DistillParams& p, cudaStream_t st) {
     IRIS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldBytes + kHoldBytes / 16));
     if (dev < kMaxDevices) configured[dev] = true;
   }
+  if (MODE == kLossOnly) return launch_rows(kernel, p, (unsigned)((int64_t)p.rows * p.split), p.split, kDistillThreads, (size_t)bytes, st);
   // As many clusters as the device holds at a time: one more would run after the others have done all their rows.  The
   // answer is kept (it depends on the kernel, the split and the bytes alone), as asking takes longer than a small launch.
   int clusters = 0;
@@ -471,16 +513,19 @@ int launch_distill(const DistillParams& p, cudaStream_t st) {
 
 template <int DT>
 int launch_distill(DistillParams p, bool tail, cudaStream_t st) {
-  // A row is shared by a cluster of blocks until a part is at most kPartBytes, or while the rows alone leave SMs without
-  // work and every thread still has a granule.
+  // With a gradient a row is shared by a cluster of blocks until a part is at most kPartBytes of shared memory; with or
+  // without one, while the rows alone leave SMs without work and every thread still has a granule.
   const int64_t granules = part_granules(p.logits, p.stride, p.vocab, DT, 1);
   int split = 1;
-  while (split < kMaxSplit && (granules * 16 > (int64_t)split * kPartBytes || ((int64_t)p.rows * split < 2 * kSms && granules >= (int64_t)split * 2 * kDistillThreads))) ++split;
+  while (split < kMaxSplit && ((p.dlogits && granules * 16 > (int64_t)split * kPartBytes) ||
+                               ((int64_t)p.rows * split < 2 * kSms && granules >= (int64_t)split * 2 * kDistillThreads)))
+    ++split;
   p.split = split;
   p.each = part_granules(p.logits, p.stride, p.vocab, DT, split);
   p.hold = std::max(1, std::min(p.each, kHoldBytes / 16));
-  if (p.each <= kHoldBytes / 16) return tail ? launch_distill<DT, true, true>(p, st) : launch_distill<DT, false, true>(p, st);
-  return tail ? launch_distill<DT, true, false>(p, st) : launch_distill<DT, false, false>(p, st);
+  if (!p.dlogits) return tail ? launch_distill<DT, true, kLossOnly>(p, st) : launch_distill<DT, false, kLossOnly>(p, st);
+  if (p.each <= kHoldBytes / 16) return tail ? launch_distill<DT, true, kHeld>(p, st) : launch_distill<DT, false, kHeld>(p, st);
+  return tail ? launch_distill<DT, true, kReadTwice>(p, st) : launch_distill<DT, false, kReadTwice>(p, st);
 }
 
 template <int DT, bool TAIL>

@@ -281,7 +281,7 @@ extern "C" int iris_token_logprobs(const iris_logprob_args* a, void* stream) {
   // A row is shared by a cluster of blocks while the rows alone leave SMs without work, until a part fits registers.
   const int64_t granules = part_granules(a->logits, stride, a->vocab, a->dtype, 1);
   int split = 1;
-  while (split < kMaxSplit && a->rows * split < 2 * kSms && granules > (int64_t)split * kOneBatch) split *= 2;
+  while (split < kMaxSplit && a->rows * split < kSms * 5 / 2 && granules > (int64_t)split * kOneBatch) split *= 2;
   ScoreParams p{a->logits, stride, (int)a->vocab, want_lp ? a->n_targets : 0, a->top_k, split, part_granules(a->logits, stride, a->vocab, a->dtype, split), a->scale, a->targets, a->logprob, a->entropy, a->stats,
                 a->top_logprob, a->top_ids};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
