@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
         if (TAIL && any) {
 #pragma unroll
           for (int u = 0; u < U; ++u)
-            if (ALL || u * T < left) g[u] = without<DT>(g[u], bits[u]);
+            if ((ALL || u * T < left) && bits[u]) g[u] = without<DT>(g[u], bits[u]);
         }
         sums.template add<ALL>(g, largest<DT, ALL>(g, left, T), left, T);
       });
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
             if (any) {
 #pragma unroll
               for (int u = 0; u < U; ++u)
-                if (ALL || u * T < left) g[u] = without<DT>(g[u], bits[u]);
+                if ((ALL || u * T < left) && bits[u]) g[u] = without<DT>(g[u], bits[u]);
             }
           }
           sums.template add<ALL>(g, largest<DT, ALL>(g, left, T), left, T);
