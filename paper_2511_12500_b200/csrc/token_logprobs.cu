@@ -151,11 +151,11 @@ __global__ void __launch_bounds__(kScoreThreads, TOP == kTopOneBatch ? 4 : 5) sc
     }
     if constexpr (TOP) {
       const uint32_t own = ptx::smem_u32(lists + rank * p.top_k);
-      const auto share = [&](int place, uint64_t key) {
-        for (int s = 0; s < split; ++s) ptx::st_shared_cluster_u64(ptx::mapa(own + place * 8, s), key);
+      const auto share = [&](int place, uint64_t key, int sub, int group) {
+        for (int s = sub; s < split; s += group) ptx::st_shared_cluster_u64(ptx::mapa(own + place * 8, s), key);
       };
       const int found = find_top(share);
-      if (tid >= found && tid < p.top_k) share(tid, 0);
+      if (tid >= found && tid < p.top_k) share(tid, 0, 0, 1);
     }
     ptx::cluster_sync();
     a = warps_join<ENTROPY>(k, parts);
@@ -170,7 +170,8 @@ __global__ void __launch_bounds__(kScoreThreads, TOP == kTopOneBatch ? 4 : 5) sc
   }
   if (rank == 0 && tid < p.n_targets) p.logprob[r * p.n_targets + tid] = there ? log_prob(zt, a.m, ls, p.scale) : 0.f;
   if constexpr (TOP) {
-    const auto emit = [&](int place, uint64_t key) {
+    const auto emit = [&](int place, uint64_t key, int sub, int) {
+      if (sub) return;
       p.top_ids[r * p.top_k + place] = key_column(key);
       if (p.top_logprob) p.top_logprob[r * p.top_k + place] = log_prob(key_value<DT>(key), a.m, ls, p.scale);
     };
@@ -184,7 +185,7 @@ __global__ void __launch_bounds__(kScoreThreads, TOP == kTopOneBatch ? 4 : 5) sc
       int place = 0;
       for (int j = tid % group; j < n_all; j += group) place += lists[j] > key;
       for (int o = group / 2; o; o /= 2) place += __shfl_xor_sync(~0u, place, o);
-      if (key && tid % group == 0 && place < p.top_k) emit(place, key);
+      if (key && place < p.top_k) emit(place, key, tid % group, group);
     }
   }
 }

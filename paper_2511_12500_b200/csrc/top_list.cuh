@@ -244,8 +244,8 @@ __device__ __forceinline__ void queue_pieces(TopShared& sh, const Row<DT>& row, 
   }
 }
 
-// Once all threads have listed what is wanted: emit(place, key) for the part's largest, place = 0 ..
-// min(k, its length) - 1.  Returns that count.
+// Once all threads have listed what is wanted: emit(place, key, sub, group) for the part's largest, place = 0 ..
+// min(k, its length) - 1, by threads sub = 0 .. group - 1 each.  Returns that count.
 template <int DT, class Emit>
 __device__ __forceinline__ int finish_top(TopShared& sh, const Row<DT>& row, const Part<DT>& part, uint32_t tau, int k, Emit emit) {
   constexpr int T = kTopThreads;
@@ -260,12 +260,18 @@ __device__ __forceinline__ int finish_top(TopShared& sh, const Row<DT>& row, con
   int group = 32;   // threads that share a key's comparisons
   while (group > 1 && group * n > T) group /= 2;
   for (int b = 0; b < n; b += T / group) {
-    const int i = b + tid / group;
-    const uint64_t key = i < n ? sh.key[i] : ~0ull;
+    const int i = b + tid / group, sub = tid % group;
+    uint64_t key = 0;
     int place = 0;
-    for (int j = tid % group; j < n; j += group) place += sh.key[j] > key;
+    if (i < n) {
+      key = sh.key[i];
+      for (int j = 2 * sub; j < n; j += 2 * group) {
+        const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(&sh.key[j]);
+        place += (two.x > key) + (two.y > key && j + 1 < n);
+      }
+    }
     for (int o = group / 2; o; o /= 2) place += __shfl_xor_sync(~0u, place, o);
-    if (i < n && tid % group == 0 && place < k) emit(place, key);
+    if (i < n && place < k) emit(place, key, sub, group);
   }
   return min(n, k);
 }
