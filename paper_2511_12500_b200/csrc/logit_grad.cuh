@@ -22,9 +22,13 @@ struct List {
   float add[kMaxList];
 };
 
+// ex2 gives 0 below 2^-126, and alpha + beta y may be large: exponents are raised by 32 and the factor lowered by 2^-32, a
+// power of two, so that a y of 0 still gives alpha.
+constexpr float kRaise = 32.f, kLower = 1.f / 4294967296.f;
+
 __device__ __forceinline__ float grad_of(float z, const Coef& c) {   // on the list
   const float y = (z - c.m) * c.k - c.off_l;
-  return ex2(y) * fmaf(c.beta, max_nan(y, kFloor), c.alpha_l);
+  return ex2(y + kRaise) * fmaf(c.beta, max_nan(y, kFloor), c.alpha_l) * kLower;
 }
 
 // Whether another entry of the first n has entry i's column.
@@ -56,9 +60,10 @@ struct Dense {
   __device__ __forceinline__ explicit Dense(const Coef& c_) : c(c_) {
     k2 = pair(c.k, c.k);
     minus_m2 = pair(-c.m, -c.m);
-    minus_off2 = pair(-c.off, -c.off);
-    alpha2 = pair(c.alpha, c.alpha);
-    beta2 = pair(c.beta, c.beta);
+    const float off = c.off - kRaise, alpha = (c.alpha - kRaise * c.beta) * kLower, beta = c.beta * kLower;
+    minus_off2 = pair(-off, -off);
+    alpha2 = pair(alpha, alpha);
+    beta2 = pair(beta, beta);
     if (BETA) lift = lift_floor<DT>(c.m, c.k, floor);   // off >= 0 lowers the exponents further
   }
   __device__ __forceinline__ bool plain() const { return c.zero || lift; }
@@ -78,7 +83,7 @@ struct Dense {
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
       const float y = (x[e] - c.m) * c.k - c.off;
-      x[e] = c.zero ? 0.f : ex2(y) * fmaf(c.beta, max_nan(y, kFloor), c.alpha);
+      x[e] = c.zero ? 0.f : ex2(y + kRaise) * fmaf(c.beta, max_nan(y, kFloor), c.alpha) * kLower;
     }
   }
 };

@@ -55,10 +55,11 @@ __device__ __forceinline__ uint64_t fma2f(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
-// 16 bytes that are read once: not kept in L1.
+// 16 bytes that are read once: not kept in L1.  Volatile, with memory clobbered: it must not move ahead of the wait for the
+// kernel before, nor behind a store where the gradient replaces the logits.
 __device__ __forceinline__ uint4 ld_once(const void* p) {
   uint4 v;
-  asm("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
   return v;
 }
 // 16 bytes to shared memory without passing through registers; visible to the copying thread after copy_async_wait, to
@@ -324,13 +325,14 @@ struct Acc {
 };
 
 // The lowest logit that has to be told apart: one below low(m, k) has 2^y = 0 and is lifted to it, so that y 2^y is 0 and
-// not NaN for -inf.  Rounding to the type stays below m + kFloor / k.  False where the type has no such value (masks of
-// the lowest finite value and nothing above them, temperatures beyond the type's range): then y is cut instead.
+// not NaN for -inf.  Rounding to the type leaves it well below m (by 1000 / k and 1 / 64 of itself).  False where the type
+// has no such value (masks of the lowest finite value and nothing above them, scales beyond the type's range): then y is
+// cut instead.
 template <int DT>
 __device__ __forceinline__ bool lift_floor(float m, float k, uint32_t& word) {
   const float z = m + kFloor / k, low = z - fabsf(z) * (1.f / 64);
   word = Elem<DT>::twice(low);
-  return low >= Elem<DT>::kLowest && low * k > -1e38f && m * k < 1e38f;
+  return low >= Elem<DT>::kLowest && low * k > -1e38f && m * k < 1e38f && k < 1e8f;
 }
 
 // A thread's statistics of granules, counted from a logit near the largest: it is raised only when one comes that is
@@ -423,7 +425,7 @@ __device__ __forceinline__ void batches(int n, F f) {
 
 __device__ __forceinline__ float warp_max(float x) {
   float y;
-  asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
 }
 
@@ -532,7 +534,10 @@ inline int launch_rows(void (*kernel)(P), const P& p, unsigned blocks, int split
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = split > 1 ? 2 : 1;
-  IRIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
+  if (cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p)) {
+    cudaGetLastError();   // reported here, not by the next call
+    return fail(IRIS_ERR_CUDA, "kernel launch: %s", cudaGetErrorString(e));
+  }
   return IRIS_OK;
 }
 #define IRIS_CHECK(expr)              \

@@ -485,3 +485,75 @@ def test_gradient_into_other_columns_of_the_same_matrix():
     ids, tv = teacher_of(rng, v, 6, False)
     run_distill(z, "bf16", torch.from_numpy(ids).cuda(), torch.from_numpy(tv).cuda(), False, dz=dz)
     check_distill(v, "bf16", ids, tv, False, 1.0, 1.0, None, None, None, as64(dz))
+
+
+# ------------------------------------------------------------------------------------------------ scales, and calls in a row
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("scale", [1e-6, 0.01, 30.0, 1e4, 1e9])
+def test_scales_far_from_one(dtype, scale):
+    """Exponents y = scale (z - max) log2(e) carry 3 roundings of 2^-24 each; what they weigh falls as 2^y: errors as in the other tests, except
+    that log probabilities scale with y (1e-6 of the value)."""
+    rng = np.random.default_rng(21)
+    values = logits_like(rng, 3, 3001)
+    values[1, rng.random(3001) < 0.5] = -np.inf
+    _, z = strided(values, dtype, 0, 1)
+    t = torch.from_numpy(rng.integers(0, 3001, (3, 2))).cuda()
+    out = score(z, dtype, t, 9, True, scale)
+    check_score(z, out, t, 9, scale)
+    v = as64(z)
+    g, gh = torch.ones(3, 2, device="cuda") / scale, torch.ones(3, device="cuda") / scale
+    dz = torch.empty_like(z)
+    run_score_grad(z, dtype, t, g, gh, scale, dz, out["stats"], out["entropy"])
+    for r in range(3):
+        want, size = ref.score_grad(v[r], scale, t[r].cpu().numpy(), as64(g[r]), gh[r].item())
+        close(as64(dz[r]), want, HALF_UNIT[dtype] * np.abs(want) + 3e-5 * size + SMALLEST[dtype], "dz")
+
+
+def test_calls_in_a_row_wait_for_one_another():
+    """Kernels may begin while the one before them ends; each has to see all that was written before it in the stream."""
+    rng = np.random.default_rng(22)
+    vocab, rows = 20000, 40
+    zs = [torch.from_numpy(logits_like(rng, rows, vocab)).cuda().bfloat16() for _ in range(2)]
+    t = torch.from_numpy(rng.integers(0, vocab, (rows, 1))).cuda()
+    g = torch.ones(rows, 1, device="cuda")
+    ids = [z.float().topk(16, dim=1).indices for z in zs]
+    tv = torch.zeros(rows, 16, device="cuda")
+    st, lp, loss, st3 = (torch.empty(rows, n, device="cuda") for n in (2, 1, 1, 3))
+    ones = torch.ones(rows, device="cuda")
+
+    def chain(z, i, buf, dz, sync):
+        steps = [
+            lambda: buf.copy_(z),
+            lambda: iris.iris_token_logprobs(buf, rows, vocab, iris.IRIS_BF16, targets=t, n_targets=1, logprob=lp, stats=st),
+            lambda: iris.iris_token_logprobs_backward(buf, rows, vocab, iris.IRIS_BF16, t, 1, st, g, buf),      # in place
+            lambda: iris.iris_distill_topk(buf, rows, vocab, iris.IRIS_BF16, tv, i, 16, loss, stats=st3),       # of the gradient, as logits
+            lambda: iris.iris_distill_topk_backward(buf, rows, vocab, iris.IRIS_BF16, tv, i, 16, st3, ones, dz),
+            lambda: iris.iris_distill_topk(dz, rows, vocab, iris.IRIS_BF16, tv, i, 16, loss, dlogits=dz),       # in place
+        ]
+        for s in steps:
+            s()
+            if sync:
+                torch.cuda.synchronize()
+        return dz.clone(), loss.clone()
+
+    buf, dz = torch.empty_like(zs[0]), torch.empty_like(zs[0])
+    want = [chain(z, i, buf, dz, True) for z, i in zip(zs, ids)]
+    got = [chain(zs[n % 2], ids[n % 2], buf, dz, False) for n in range(60)]
+    torch.cuda.synchronize()
+    for n, (a, b) in enumerate(got):
+        assert torch.equal(a, want[n % 2][0]) and torch.equal(b, want[n % 2][1]), n
+
+
+def test_calls_in_a_cuda_graph():
+    rng = np.random.default_rng(23)
+    _, z = strided(logits_like(rng, 8, 40000), "bf16")
+    want = score(z, "bf16", None, 20)
+    out = {k: torch.zeros_like(v) for k, v in want.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(3):
+            iris.iris_token_logprobs(z, 8, 40000, iris.IRIS_BF16, top_k=20, entropy=out["entropy"], stats=out["stats"], top_ids=out["top_ids"],
+                                     top_logprob=out["top_logprob"])
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out["top_ids"], want["top_ids"]) and torch.equal(out["stats"], want["stats"]) and torch.equal(out["entropy"], want["entropy"])
