@@ -488,6 +488,9 @@ int iris_gemm_all_scatter_noalloc(const void* A, const void* const* B_shards, co
  * lowest finite value is an ordinary value, also where a row holds nothing else.  A row with no finite logit has log
  * probabilities -inf, entropy 0, statistics -inf, a loss of +inf where its teacher asks for anything, and gradient 0.
  * A row that holds +inf or NaN gives NaN; other rows do not notice.
+ * In a stream the kernels may be set up while the kernel before them ends (programmatic launch); they wait for it before
+ * they read or write memory, so the order of a stream is what it always is.  The calls may be captured in a CUDA graph.
+ * Results do not depend on scheduling: the same call on the same inputs gives the same bits.
  * Errors: IRIS_ERR_ARG for what the comments below exclude, before anything is launched. */
 
 /* Log probabilities of given tokens, entropy, and the largest alternatives. */

@@ -33,10 +33,18 @@ __device__ __forceinline__ float log_prob(float z, float m, float ls, float scal
 struct NoTop {};
 
 // One cluster of `split` blocks a row; each takes an equal run of granules, and all get what each found.
+//
+// Bound by memory where a row is long and there are many (4096 x 128000 bf16: 174 us, 6.0 TB/s, 92 % of the copy rate; 6.6
+// instructions an element, a third of the issue slots): without alternatives a batch of four granules a thread is fetched
+// while one is summed, in four blocks an SM (178 us without, 194 with five blocks, whose registers spill).  With
+// alternatives five blocks of single batches hide the end of one row, about half of a block's time, behind the others'
+// passes (4096 x 36864 fp16, 64 alternatives: 87 us; four blocks 91).  Short rows are bound by the chain of latencies: load,
+// bound, list, places (1 x 16384: 4.6 us from first to last instruction).
+//
 // TOP: no alternatives; alternatives of a part of any length, of which pieces are read again; of a part of at most
 // kOneBatch granules, which stays in registers.
 template <int DT, bool ENTROPY, int TOP>
-__global__ void __launch_bounds__(kScoreThreads, TOP == kTopOneBatch ? 4 : 5) score_kernel(const ScoreParams p) {
+__global__ void __launch_bounds__(kScoreThreads, TOP == kTopPiecewise ? 5 : 4) score_kernel(const ScoreParams p) {
   using E = Elem<DT>;
   constexpr int T = kScoreThreads, U = TOP == kTopOneBatch ? kOneBatch / T : 4;
   __shared__ Warps<T / 32> buf;
@@ -109,6 +117,30 @@ __global__ void __launch_bounds__(kScoreThreads, TOP == kTopOneBatch ? 4 : 5) sc
     sums.template add<false>(g, best, n - tid, T);
   } else {
     int b = 0;
+    if constexpr (TOP == kNoTop) {   // the next batch is under way while one is summed
+      constexpr int B = T * U;
+      uint4 h[U];
+      const auto fetch = [&](int at, uint4(&to)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) to[u] = ld_once(from + at + u * T);
+      };
+      if (B <= part.n_int) fetch(0, g);
+      for (; b + 3 * B <= part.n_int; b += 2 * B) {
+        fetch(b + B, h);
+        sums.template add<true>(g, largest<DT, true>(g, 0, T));
+        fetch(b + 2 * B, g);
+        sums.template add<true>(h, largest<DT, true>(h, 0, T));
+      }
+      if (b + 2 * B <= part.n_int) {
+        fetch(b + B, h);
+        sums.template add<true>(g, largest<DT, true>(g, 0, T));
+        sums.template add<true>(h, largest<DT, true>(h, 0, T));
+        b += 2 * B;
+      } else if (b + B <= part.n_int) {
+        sums.template add<true>(g, largest<DT, true>(g, 0, T));
+        b += B;
+      }
+    }
     for (; b + T * U <= part.n_int; b += T * U) batch(b, std::true_type{});
     for (; b < n; b += T * U) batch(b, std::false_type{});
     if constexpr (TOP) {
