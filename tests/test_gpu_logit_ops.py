@@ -557,3 +557,75 @@ def test_calls_in_a_cuda_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out["top_ids"], want["top_ids"]) and torch.equal(out["stats"], want["stats"]) and torch.equal(out["entropy"], want["entropy"])
+
+
+# ------------------------------------------------------------------------------------------------ many rows, and rows beyond shared memory
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("vocab,top,pad", [(9000, 128, 0), (20001, 5, 0), (36864, 64, 3), (70000, 128, 0)])
+@pytest.mark.parametrize("kind", ["random", "masked", "few_left", "four_threads", "constant", "rising"])
+def test_alternatives_of_many_rows(dtype, vocab, top, pad, kind):
+    """As many rows as keep a block for each: against a stable sort of all rows, and the definition for three."""
+    rows = 380
+    gen = torch.Generator(device="cuda").manual_seed(vocab + top)
+    x = torch.randn(rows, vocab, device="cuda", generator=gen) * 3
+    j = torch.arange(vocab, device="cuda")
+    if kind == "masked":
+        x[torch.rand(x.shape, device="cuda", generator=gen) < 0.99] = -math.inf
+    elif kind == "few_left":
+        x[:, torch.rand(vocab, device="cuda", generator=gen) > 3 / vocab] = -math.inf
+    elif kind == "four_threads":                       # what a block's threads 3 .. 6 read holds all that is large
+        x = torch.where((j // (16 // TORCH[dtype].itemsize) % 256 - 3).clamp(0, 3) == j // (16 // TORCH[dtype].itemsize) % 256 - 3, 20.0, 0.0) + x * 1e-2
+    elif kind == "constant":
+        x[:] = 0.5
+    elif kind == "rising":
+        x = (j * 1e-3).expand(rows, vocab)
+    store = torch.zeros(rows, vocab + pad, dtype=TORCH[dtype], device="cuda")
+    z = store[:, :vocab]
+    z.copy_(x)
+    out = score(z, dtype, None, top)
+    want = torch.sort(z.float(), dim=1, descending=True, stable=True).indices[:, :top]
+    assert torch.equal(out["top_ids"], want)
+    few = torch.tensor([0, rows // 2, rows - 1], device="cuda")
+    check_score(z[few], {k: v[few] for k, v in out.items()}, None, top, 1.0)
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("dtype,vocab,offset", [("fp32", 400003, 1), ("bf16", 900001, 0), ("bf16", 800000, 0)])
+def test_distill_rows_beyond_shared_memory(tail, dtype, vocab, offset):
+    rng = np.random.default_rng(31)
+    store, z = strided(logits_like(rng, 2, vocab), dtype, 0, offset)
+    v = as64(z)
+    ids, tv = teacher_of(rng, v, 50, tail)
+    ids[1, 3] = ids[1, 4]
+    d = [torch.from_numpy(a).cuda() for a in (ids, tv)]
+    w = np.array([1.0, 0.25], np.float32)
+    dz = torch.empty_like(z)
+    for target in (dz, z):                             # apart, then in place
+        loss, stats = run_distill(z, dtype, d[0], d[1], tail, weight=torch.from_numpy(w).cuda(), dz=target)
+        check_distill(v, dtype, ids, tv, tail, 1.0, 1.0, w, loss, stats, as64(target))
+    outside_untouched(store, z, offset)
+
+
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_many_rows_of_unlike_places(tail):
+    """Enough rows that each block takes several, every row at another place in its 16 bytes, the gradient's rows elsewhere."""
+    rng = np.random.default_rng(32)
+    rows, vocab, k = 1500, 5003, 12
+    values = logits_like(rng, rows, vocab)
+    for gpad in (2, 3):                                # as the logits' rows, and not
+        store, z = strided(values, "fp16", 2, 1)
+        v = as64(z)
+        ids, tv = teacher_of(rng, v, k, tail)
+        ids[::3, -1] = -1
+        ids[7, 0] = ids[7, 1]
+        gstore, dz = strided(np.full((rows, vocab), SENTINEL), "fp16", gpad, 1)
+        w = (rng.random(rows) * 64).astype(np.float32)
+        w[::5] = 0
+        d = [torch.from_numpy(a).cuda() for a in (ids, tv, w)]
+        loss, stats = run_distill(z, "fp16", d[0], d[1], tail, weight=d[2], dz=dz)
+        check_distill(v, "fp16", ids, tv, tail, 1.0, 1.0, w, loss, stats, as64(dz))
+        outside_untouched(gstore, dz, 1)
+        if gpad == 2:
+            run_distill(z, "fp16", d[0], d[1], tail, weight=d[2], dz=z)
+            check_distill(v, "fp16", ids, tv, tail, 1.0, 1.0, w, None, None, as64(z))
+            outside_untouched(store, z, 1)
