@@ -115,9 +115,9 @@ __device__ __forceinline__ Coef distill_coef(const DistillParams& p, float sum, 
   return c;
 }
 
-// What a block of the cluster found in its part: the tokens off the list (all, without remainder) and those on it.
+// What the blocks of the cluster found in their parts: of the tokens off the list (all, without remainder) and of those on it.
 struct Found {
-  Acc dense, listed;
+  Warps<kMaxSplit> dense, listed;
 };
 
 // The one or two granules of a part that the row covers in part, held by threads 0 and 1 of the block.
@@ -153,7 +153,7 @@ struct Edge {
 // better.  Blocks of 128 threads: what a row costs besides its elements is 670 instructions a warp, so few warps (256
 // threads: 195 us), with four blocks' worth of registers; rows of one block up to 60 KB (two blocks of 28 KB: 236 us), as
 // many clusters as fit at once (one wave more, as an SM count would give for clusters of four, is twice the time).
-// 4096 x 128000 with remainder, clusters of four: 455 us, 71 %; 2.4 us of a row's 12.5 wait for the exchange.
+// 4096 x 128000 with remainder, clusters of five: 432 us, 74 %; about 2 us of a row's 12 wait for the exchange.
 template <int DT, bool TAIL, int MODE>
 __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBlocks : kDistillBlocks) distill_kernel(const DistillParams p) {
   using E = Elem<DT>;
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
   __shared__ List lists[2];          // of this row and the one before
   __shared__ TeacherSums teacher;
   __shared__ Warps<T / 32> buf[2];
-  __shared__ Found found[2][kMaxSplit];
+  __shared__ Found found[2];         // as the lists
   __shared__ float red[kMaxList / 32];
   __shared__ int repeats[2];         // whether a column comes twice on the list
   uint32_t* const on_list = reinterpret_cast<uint32_t*>(held + (HELD ? p.hold : 0));
@@ -173,7 +173,10 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
   const int split = p.split, rank = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x, n = p.list_k;
   const int64_t step = gridDim.x / split;
   int64_t r = blockIdx.x / split;
-  if (split > 1) ptx::cluster_arrive_relaxed();
+  if (split > 1) {
+    if (tid < kMaxSplit) found[0].dense.of[tid] = found[0].listed.of[tid] = found[1].dense.of[tid] = found[1].listed.of[tid] = Acc{};
+    ptx::cluster_arrive_release();
+  }
   ptx::begin_after_previous();
   const float k = p.scale * kLog2e;
 
@@ -190,6 +193,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
   }
   for (int i = tid; i * 4 < p.hold; i += T) on_list[i] = 0;
   if (tid == 0) repeats[0] = 0;
+  if (split > 1) ptx::cluster_wait();   // all blocks have started and have cleared their places for the others' sums
   __syncthreads();
   for (int turn = 0; r < p.rows; r += step, turn ^= 1) {
     List& list = lists[turn];
@@ -291,25 +295,29 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
     if (HELD && own) on_list[mark / 4] = 0;
     Acc dense = warps_join<false>(k, buf[0]), listed;
     if (TAIL) listed = warps_join<false>(k, buf[1]);
-    const float3 teach = join_entries<TAIL>(x, teacher);
-    const float pk = entry.id >= 0 ? teach.x : 0.f;
     if (split > 1) {
-      if (r < step) ptx::cluster_wait();   // the first row: all blocks have started
       if (tid < split) {
-        const uint32_t to = ptx::mapa(ptx::smem_u32(&found[turn][rank]), tid);
+        const uint32_t to = ptx::mapa(ptx::smem_u32(&found[turn].dense.of[rank]), tid), to_listed = ptx::mapa(ptx::smem_u32(&found[turn].listed.of[rank]), tid);
         ptx::st_shared_cluster_u32(to, __float_as_uint(dense.m));
         ptx::st_shared_cluster_u32(to + 4, __float_as_uint(dense.s));
         if (TAIL) {
-          ptx::st_shared_cluster_u32(to + sizeof(Acc), __float_as_uint(listed.m));
-          ptx::st_shared_cluster_u32(to + sizeof(Acc) + 4, __float_as_uint(listed.s));
+          ptx::st_shared_cluster_u32(to_listed, __float_as_uint(listed.m));
+          ptx::st_shared_cluster_u32(to_listed + 4, __float_as_uint(listed.s));
         }
       }
-      ptx::cluster_sync();   // behind it no block reads logits of another's part, and the gradient may replace them
-      dense = listed = Acc{};
-      for (int i = 0; i < split; ++i) {
-        dense.merge(Acc{found[turn][i].dense.m, found[turn][i].dense.s, 0.f}, k);
-        if (TAIL) listed.merge(Acc{found[turn][i].listed.m, found[turn][i].listed.s, 0.f}, k);
-      }
+      ptx::cluster_arrive_release();
+    }
+    const float w_row = w;
+    if (more) {
+      ahead = load_entry(p, r_next);
+      if (p.weight) w = p.weight[r_next];
+    }
+    const float3 teach = join_entries<TAIL>(x, teacher);
+    const float pk = entry.id >= 0 ? teach.x : 0.f;
+    if (split > 1) {
+      ptx::cluster_wait();   // behind it no block reads logits of another's part, and the gradient may replace them
+      dense = warps_join<false>(k, found[turn].dense);
+      if (TAIL) listed = warps_join<false>(k, found[turn].listed);
     }
     Acc all = dense;
     if (TAIL) all.merge(listed, k);
@@ -317,12 +325,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
     const float lr = !TAIL ? 0.f : dense.s == 0.f ? -INFINITY : (dense.m - all.m) * p.scale + log_sum(dense);
     const float zk = E::to(z_listed);
     Coef coef;
-    const float w_row = w;
     const Row<DT> out(p.dlogits, grad ? r : 0, p.grad_stride, p.vocab);
-    if (more) {
-      ahead = load_entry(p, r_next);
-      if (p.weight) w = p.weight[r_next];
-    }
     bool rep = false;
     float listed_grad = 0.f, add = 0.f;
     if constexpr (grad) {
