@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(kScoreThreads, TOP == kTopPiecewise ? 5 : 4) s
   const int64_t r = blockIdx.x / split;
   if (split > 1) {
     if (tid < kMaxSplit) parts.of[tid] = Acc{};
-    ptx::cluster_arrive_relaxed();
+    ptx::cluster_arrive_release();   // behind the wait the others may write there
   }
   const Row<DT> row(p.logits, r, p.stride, p.vocab);
   const Part<DT> part(row, rank, p.each);
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kScoreThreads, TOP == kTopPiecewise ? 5 : 4) s
   };
 
   if (split > 1) {
-    ptx::cluster_wait();   // all blocks have started
+    ptx::cluster_wait();   // all blocks have started and cleared their places
     if (tid < split) {
       const uint32_t to = ptx::mapa(ptx::smem_u32(&parts.of[rank]), tid);
       ptx::st_shared_cluster_u32(to, __float_as_uint(a.m));
