@@ -22,9 +22,9 @@ struct List {
   float add[kMaxList];
 };
 
-// ex2 gives 0 below 2^-126, and alpha + beta y may be large: exponents are raised by 32 and the factor lowered by 2^-32, a
-// power of two, so that a y of 0 still gives alpha.
-constexpr float kRaise = 32.f, kLower = 1.f / 4294967296.f;
+// ex2 gives 0 below 2^-126, and alpha + beta y may be large: exponents are raised by 8 and the factor lowered by 2^-8, a
+// power of two, so that a y of 0 still gives alpha.  (By 32, the rounding of exponents near 32 was 1e-6 of the result.)
+constexpr float kRaise = 8.f, kLower = 1.f / 256.f;
 
 __device__ __forceinline__ float grad_of(float z, const Coef& c) {   // on the list
   const float y = (z - c.m) * c.k - c.off_l;

@@ -75,9 +75,10 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return y;
 }
 
-template <int DT> struct Elem;   // kMasked: 32 bits of -inf; fold(): a granule's largest values in two halves, larger() of two such, unfold() the larger
-// half, NaN if one is;
-// at_least(): none below twice(floor), NaN stays
+// An element type.  VE: elements of a granule; kMasked: 32 bits of -inf; kLowest: about the lowest finite value; fold(): a
+// granule's largest values in two halves, larger() of two such, unfold() the larger half, NaN if one is; at_least(): none
+// below floor, which is twice() a value, NaN stays; ordinal() and value(): below.
+template <int DT> struct Elem;
 template <> struct Elem<IRIS_F16> {
   using T = __half;
   static constexpr int VE = 8;
