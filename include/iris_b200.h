@@ -538,7 +538,8 @@ int iris_token_logprobs_backward(const iris_logprob_grad_args* args, void* strea
  *                        p_r = max(0, 1 - sum p_k), is one more token, compared with the student's probability of all
  *                        tokens off the list:                 loss = sum p_k (ln p_k - ln q_k) + p_r (ln p_r - ln q_r)
  *                        (teacher_scale is not used; p_r < 1e-5 is dropped where no token off the list has mass)
- * Terms with p = 0 are 0; p > 0 against q = 0 gives a loss of +inf and a finite gradient. */
+ * Terms with p = 0 are 0; p > 0 against q = 0 gives a loss of +inf and a finite gradient.  Where all tokens off the list are
+ * masked by finite values, the remainder's gradient is spread over them by their own softmax. */
 enum { IRIS_DISTILL_RENORM = 0, IRIS_DISTILL_TAIL = 1 };
 typedef struct iris_distill_args {
   const void* logits;
@@ -554,7 +555,7 @@ typedef struct iris_distill_args {
                                  whatever its logits are                                                              */
   float* loss;                /* [rows], not multiplied by weight                                                     */
   float* stats;               /* [rows, 3]: max z, ln sum exp(scale (z - max z)), the same sum over the tokens off the
-                                 list (0 in RENORM)                                                                   */
+                                 list (0 in RENORM; -FLT_MAX where it is below that, -inf where no such token is left) */
   void* dlogits;              /* weight * dloss/dz, type and rules as above; NULL = loss only                         */
   int64_t grad_stride;
 } iris_distill_args;

@@ -7,6 +7,7 @@
 //   scale ((P + p_r) q_j - p_r q_j / q_r) off it;  P = sum p_k.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "logit_grad.cuh"
 #include "sm100_ptx.cuh"
@@ -95,17 +96,26 @@ __device__ __forceinline__ float3 join_entries(float x, const TeacherSums& t) {
   return make_float3(x * ex2((own - m) * kLog2e) / s, s == s ? 1.f : NAN, 0.f);
 }
 
+// ln of the sum of the tokens off the list (`dense`), counted from m; what is less than the type holds is its lowest value, as -inf says
+// that there is no such token.
+__device__ __forceinline__ float log_rest(const Acc& dense, float m, float scale) {
+  return dense.s == 0.f ? -INFINITY : max_nan((dense.m - m) * scale + log_sum(dense), -FLT_MAX);
+}
+
+// m_off, ls_off: with a remainder, a logit and ln of the sum of the tokens off the list counted from it.  Their largest one, or (m, lr): but where
+// they are all masked by a finite value, (z - m) k and lr are so far below 0 that their difference, the logarithm of a share, is lost.
 template <bool TAIL>
-__device__ __forceinline__ Coef distill_coef(const DistillParams& p, float sum, float rest, float m, float ls, float lr, float w) {
+__device__ __forceinline__ Coef distill_coef(const DistillParams& p, float sum, float rest, float m, float ls, float lr, float m_off, float ls_off, float w) {
   Coef c;
   c.k = p.scale * kLog2e;
-  c.m = m;
+  c.m = c.m_l = m;
   c.beta = 0.f;
   c.off_l = ls * kLog2e;
   c.alpha_l = w * p.scale * (sum + rest);
   if (TAIL) {
-    const bool some = lr != -INFINITY;
-    c.off = some ? lr * kLog2e : 0.f;
+    const bool some = ls_off != -INFINITY;
+    if (some) c.m = m_off;
+    c.off = some ? ls_off * kLog2e : 0.f;
     c.alpha = some ? w * p.scale * ((sum + rest) * ex2((lr - ls) * kLog2e) - rest) : 0.f;
   } else {
     c.off = c.off_l;
@@ -322,14 +332,14 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
     Acc all = dense;
     if (TAIL) all.merge(listed, k);
     const float ls = log_sum(all);
-    const float lr = !TAIL ? 0.f : dense.s == 0.f ? -INFINITY : (dense.m - all.m) * p.scale + log_sum(dense);
+    const float lr = TAIL ? log_rest(dense, all.m, p.scale) : 0.f;
     const float zk = E::to(z_listed);
     Coef coef;
     const Row<DT> out(p.dlogits, grad ? r : 0, p.grad_stride, p.vocab);
     bool rep = false;
     float listed_grad = 0.f, add = 0.f;
     if constexpr (grad) {
-      coef = distill_coef<TAIL>(p, teach.y, teach.z, all.m, ls, lr, w_row);
+      coef = distill_coef<TAIL>(p, teach.y, teach.z, all.m, ls, lr, dense.m, log_sum(dense), w_row);
       add = -w_row * p.scale * pk;
       listed_grad = grad_of(zk, coef);
       if (tid < n) list.add[tid] = add;
@@ -410,10 +420,51 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
   ptx::let_next_begin();
 }
 
+// The statistics of a whole row's tokens off the list, by all threads of a block of kGradThreads.  list.id has been written before the last barrier.
+constexpr int kSieve = 4096;   // granules are looked up on the list where granule mod kSieve is that of a listed token
+struct OffList {
+  uint32_t sieve[kSieve / 32];
+  Warps<kGradThreads / 32> buf;
+};
+struct NoOffList {};
+template <int DT>
+__device__ __forceinline__ Acc sum_off_list(const Row<DT> row, const List& list, int n, float k, OffList& sh) {
+  constexpr int VE = Elem<DT>::VE, T = kGradThreads;
+  const int tid = threadIdx.x;
+  for (int i = tid; i < kSieve / 32; i += T) sh.sieve[i] = 0;
+  __syncthreads();
+  if (tid < n && list.id[tid] >= 0) {
+    const int v = (row.ph + list.id[tid]) / VE % kSieve;
+    atomicOr(&sh.sieve[v / 32], 1u << v % 32);
+  }
+  __syncthreads();
+  const Part<DT> whole(row, 0, row.granules());
+  Sums<DT, false> sums(k);
+  for (int i = tid; i < whole.n_all; i += T) {
+    uint4 g[1] = {whole.raw(row, i)};
+    const int v = whole.granule(i);
+    if (sh.sieve[v % kSieve / 32] >> v % 32 & 1) {
+      uint32_t bits = 0;
+      for (int j = 0; j < n; ++j) {
+        const int at = row.ph + list.id[j];
+        if (list.id[j] >= 0 && at / VE == v) bits |= 1u << at % VE;
+      }
+      g[0] = without<DT>(g[0], bits);
+    }
+    sums.template add<true>(g, largest<DT>(g[0]));
+  }
+  warp_share<false>(sums.done(), k, sh.buf);
+  __syncthreads();
+  return warps_join<false>(k, sh.buf);
+}
+
+// A row whose student gives the tokens off the list no probability in 32 bits, but not -inf, is one block's: saved statistics do not hold how its
+// remainder is spread (distill_coef), so the row is summed again, before any of it is replaced.  Six blocks an SM, as the other form has by itself.
 template <int DT, bool TAIL>
-__global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const DistillParams p) {
+__global__ void __launch_bounds__(kGradThreads, TAIL ? 6 : 0) distill_grad_kernel(const DistillParams p) {
   __shared__ List list;
   __shared__ TeacherSums teacher;
+  __shared__ typename std::conditional<TAIL, OffList, NoOffList>::type off;
   const int64_t r = blockIdx.x / p.split;
   const int tid = threadIdx.x;
   ptx::let_next_begin();
@@ -426,8 +477,19 @@ __global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const Distil
   __syncthreads();
   const float3 teach = join_entries<TAIL>(x, teacher);
   if (tid < kMaxList) list.add[tid] = -w * p.scale * (e.id >= 0 ? teach.x : 0.f);
-  const Coef c = distill_coef<TAIL>(p, teach.y, teach.z, m, ls, lr, w);
-  grad_part<DT, false>(in, out, Part<DT>(in, blockIdx.x % p.split, p.each), c, list, p.list_k);
+  int part = blockIdx.x % p.split, each = p.each;
+  float m_off = m, ls_off = lr;
+  if constexpr (TAIL) {
+    if (!(teach.z == 0.f) && w != 0.f && lr != -INFINITY && ex2((lr - ls) * kLog2e) == 0.f) {   // alike in all blocks of the row
+      if (part) return;
+      each = in.granules();
+      const Acc dense = sum_off_list<DT>(in, list, p.list_k, p.scale * kLog2e, off);
+      m_off = dense.m;
+      ls_off = log_sum(dense);
+    }
+  }
+  const Coef c = distill_coef<TAIL>(p, teach.y, teach.z, m, ls, lr, m_off, ls_off, w);
+  grad_part<DT, false>(in, out, Part<DT>(in, part, each), c, list, p.list_k);
 }
 
 }  // namespace rows

@@ -7,11 +7,11 @@
 namespace iris {
 namespace rows {
 
-// dz_j = 2^(y_j - off) (alpha + beta max(y_j - off, kFloor)) for columns off the list,
-//        2^(y_j - off_l) (alpha_l + beta max(y_j - off_l, kFloor)) + add for those on it,   y_j = (z_j - m) k.
+// dz_j = 2^(y_j - off) (alpha + beta max(y_j - off, kFloor)) for columns off the list, y_j = (z_j - m) k,
+//        2^(y_j - off_l) (alpha_l + beta max(y_j - off_l, kFloor)) + add for those on it, y_j = (z_j - m_l) k.
 // zero: the whole row is 0, whatever its logits are.
 struct Coef {
-  float k, m, off, alpha, off_l, alpha_l, beta;
+  float k, m, off, alpha, m_l, off_l, alpha_l, beta;
   bool zero;
 };
 
@@ -27,7 +27,7 @@ struct List {
 constexpr float kRaise = 8.f, kLower = 1.f / 256.f;
 
 __device__ __forceinline__ float grad_of(float z, const Coef& c) {   // on the list
-  const float y = (z - c.m) * c.k - c.off_l;
+  const float y = (z - c.m_l) * c.k - c.off_l;
   return ex2(y + kRaise) * fmaf(c.beta, max_nan(y, kFloor), c.alpha_l) * kLower;
 }
 

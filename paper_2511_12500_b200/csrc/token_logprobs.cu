@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const ScoreGra
   for (int i = 0; i < n; ++i) g += list.add[i];
   Coef c;
   c.k = p.scale * kLog2e;
-  c.m = p.stats[2 * r];
+  c.m = c.m_l = p.stats[2 * r];
   c.off = c.off_l = ls * kLog2e;
   c.alpha = c.alpha_l = -(g + p.scale * gh * h);
   c.beta = -p.scale * gh * kLn2;

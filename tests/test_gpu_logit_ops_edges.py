@@ -1,0 +1,117 @@
+"""Operators on logits where they went wrong once: finite masks off the teacher's list, long rows, tokens listed twice, scales near
+the type's largest, rows of NaN, 32-bit gradients, graphs.
+
+Tolerances are those of test_gpu_logit_ops.py unless a test derives its own.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import logit_ref as ref
+import paper_2511_12500_b200 as iris
+from test_gpu_logit_ops import HALF_UNIT, SMALLEST, TORCH, as64, check_score, close, logits_like, run_distill, run_score_grad, score, strided
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ finite masks off the teacher's list
+def masked_off_list(z, scale, ids, tv):
+    """Loss, gradient, ln of the sum off the list and the sizes of the first two's terms, in 64 bits, with the tokens off the list counted from
+    their own largest (64 bits do not hold ln n beside 1e38).  A remainder below 1e-5 is dropped where the probability off the list is below
+    2^-126."""
+    m, ls, lq = ref.log_softmax(z, scale)
+    there = ids >= 0
+    p = np.where(there, np.exp(tv.astype(np.float64)), 0.0)
+    rest = max(0.0, 1.0 - p.sum())
+    off = np.ones(z.size, dtype=bool)
+    off[ids[there]] = False
+    top = z[off].max()
+    y = np.exp(scale * (z - top), where=off, out=np.zeros(z.size))
+    down, lo = scale * (m - top), np.log(y.sum())                      # ln of the sum off the list = lo - down
+    if rest < 1e-5 and lo - down - ls < -126 * math.log(2):
+        rest = 0.0
+    q = np.exp(lq)
+    dz, dsize = (p.sum() + rest) * q - rest * y / y.sum(), (p.sum() + rest) * q + rest * y / y.sum()
+    dz[ids[there]] -= p[there]
+    dsize[ids[there]] += p[there]
+    terms = np.array([x * (np.log(x) - lq[j]) for j, x in zip(ids, p) if j >= 0 and x > 0] + ([rest * np.log(rest), rest * ls, -rest * lo, rest * down] if rest else []))
+    return terms.sum(), scale * dz, lo - down, np.abs(terms).sum(), scale * dsize
+
+
+MASK_VALUES = [(d, m) for d in ("bf16", "fp16", "fp32") for m in (None, -1e9, -1e4) if (d, m) != ("fp16", -1e9)]   # None: the type's lowest
+
+
+def rows_with_masked_rest(dtype, mask, rows, vocab, k, p_rest, offset, others):
+    """Rows in which all tokens off the list are masked, by one value or by three."""
+    rng = np.random.default_rng(vocab)
+    low = float(torch.finfo(TORCH[dtype]).min) if mask is None else mask
+    values = np.full((rows, vocab), low)
+    if others:
+        values[:, ::3] = low / 2
+        values[:, 1::7] = -np.inf
+    ids = np.stack([rng.permutation(vocab)[:k] for _ in range(rows)]).astype(np.int64)
+    np.put_along_axis(values, ids, rng.normal(0, 2, (rows, k)), 1)
+    p = rng.random((rows, k)) + 0.1
+    tv = np.log(p / p.sum(1, keepdims=True) * (1 - p_rest)).astype(np.float32)
+    absent = rng.permutation(k)[0]
+    if p_rest > 1e-3:
+        values[0, ids[0, absent]] = low                                # an absent entry's token is off the list too
+        ids[0, absent] = -1
+    store, z = strided(values, dtype, 0, offset)
+    return store, z, ids, tv
+
+
+def check_masked_rest(dtype, z, v, ids, tv, scale, weight, what, loss=None, stats=None, dz=None):
+    for r in range(v.shape[0]):
+        want, dwant, lr, size, dsize = masked_off_list(v[r], scale, ids[r], tv[r])
+        w = float(weight[r])
+        if loss is not None:
+            close(loss[r].item(), want, 1e-5 + 1e-5 * size, what + " loss")
+        if stats is not None:
+            lr = max(lr, -float(np.finfo(np.float32).max))
+            close(as64(stats[r]), [*ref.log_softmax(v[r], scale)[:2], lr], [0.0, 1e-5, 1e-5 + 1e-6 * abs(lr)], what + " stats")
+        if dz is not None:
+            close(dz[r], w * dwant, HALF_UNIT[dtype] * np.abs(w * dwant) + 3e-5 * abs(w) * dsize + SMALLEST[dtype], what + " dz")
+
+
+def run_masked_rest(dtype, mask, scale, p_rest, rows, vocab, offset, others, gradients, losses):
+    k = 12
+    store, z, ids, tv = rows_with_masked_rest(dtype, mask, rows, vocab, k, p_rest, offset, others)
+    v = as64(z)
+    weight = np.linspace(0.5, 64 if dtype == "fp16" else 1.5, rows).astype(np.float32)
+    i, t, w = [torch.from_numpy(x).cuda() for x in (ids, tv, weight)]
+    dz = torch.empty_like(z)
+    loss, stats = run_distill(z, dtype, i, t, True, scale, weight=w, dz=dz)
+    alone, saved = run_distill(z, dtype, i, t, True, scale)
+    if losses:
+        check_masked_rest(dtype, z, v, ids, tv, scale, weight, "fused", loss=loss, stats=stats)
+        check_masked_rest(dtype, z, v, ids, tv, scale, weight, "alone", loss=alone, stats=saved)
+    if gradients:
+        check_masked_rest(dtype, z, v, ids, tv, scale, weight, "fused", dz=as64(dz))
+        where = (z, rows, vocab, iris.LOGIT_DTYPES[dtype], t, i, k, saved, w)
+        strides = dict(row_stride=z.stride(0), grad_stride=z.stride(0)) if rows > 1 else {}
+        iris.iris_distill_topk_backward(*where, dz, mode=iris.IRIS_DISTILL_TAIL, scale=scale, **strides)
+        check_masked_rest(dtype, z, v, ids, tv, scale, weight, "backward", dz=as64(dz))
+        keep = z.clone()
+        iris.iris_distill_topk_backward(*where, z, mode=iris.IRIS_DISTILL_TAIL, scale=scale, **strides)
+        check_masked_rest(dtype, z, v, ids, tv, scale, weight, "backward in place", dz=as64(z))
+        z.copy_(keep)
+        run_distill(z, dtype, i, t, True, scale, weight=w, dz=z)
+        check_masked_rest(dtype, z, v, ids, tv, scale, weight, "fused in place", dz=as64(z))
+
+
+@pytest.mark.parametrize("dtype,mask", MASK_VALUES)
+@pytest.mark.parametrize("scale", [0.5, 1.0, 2.0])
+@pytest.mark.parametrize("p_rest", [0.1, 0.6])
+@pytest.mark.parametrize("rows,vocab,offset,others", [(4, 3001, 3, False), (3, 20000, 0, True), (1, 128000, 0, False), (2, 60001, 1, True)])
+def test_remainder_over_finite_masks(dtype, mask, scale, p_rest, rows, vocab, offset, others):
+    """A student whose tokens off the list are all masked by a finite value: the remainder's gradient is spread over them by their own softmax."""
+    run_masked_rest(dtype, mask, scale, p_rest, rows, vocab, offset, others, True, False)
+
+
+@pytest.mark.parametrize("dtype,vocab", [("fp32", 400003), ("bf16", 900001)])
+@pytest.mark.parametrize("mask", [None, -1e9])
+def test_remainder_over_finite_masks_beyond_shared_memory(dtype, vocab, mask):
+    run_masked_rest(dtype, mask, 1.0, 0.1, 2, vocab, 1, True, True, False)
