@@ -537,7 +537,8 @@ int iris_token_logprobs_backward(const iris_logprob_grad_args* args, void* strea
  *   IRIS_DISTILL_TAIL    values are log probabilities over the whole vocabulary, p_k = exp(value), and what is left,
  *                        p_r = max(0, 1 - sum p_k), is one more token, compared with the student's probability of all
  *                        tokens off the list:                 loss = sum p_k (ln p_k - ln q_k) + p_r (ln p_r - ln q_r)
- *                        (teacher_scale is not used; p_r < 1e-5 is dropped where no token off the list has mass)
+ *                        (teacher_scale is not used; p_r < 1e-5 is taken as 0 where the student's probability off the
+ *                        list is below 2^-126, be its tokens masked by -inf or by a finite value)
  * Terms with p = 0 are 0; p > 0 against q = 0 gives a loss of +inf and a finite gradient.  Where all tokens off the list are
  * masked by finite values, the remainder's gradient is spread over them by their own softmax. */
 enum { IRIS_DISTILL_RENORM = 0, IRIS_DISTILL_TAIL = 1 };

@@ -98,8 +98,14 @@ __device__ __forceinline__ float3 join_entries(float x, const TeacherSums& t) {
 
 // ln of the sum of the tokens off the list (`dense`), counted from m; what is less than the type holds is its lowest value, as -inf says
 // that there is no such token.
-__device__ __forceinline__ float log_rest(const Acc& dense, float m, float scale) {
-  return dense.s == 0.f ? -INFINITY : max_nan((dense.m - m) * scale + log_sum(dense), -FLT_MAX);
+__device__ __forceinline__ float log_rest(const Acc& dense, float ls_off, float m, float scale) {
+  return dense.s == 0.f ? -INFINITY : max_nan((dense.m - m) * scale + ls_off, -FLT_MAX);
+}
+
+// The remainder that counts: against tokens off the list that have no probability in 32 bits (the largest is masked, by -inf or by a finite value),
+// what rounding may have left of 1 - sum p is no remainder.  The rows of -inf (ls) keep theirs.
+__device__ __forceinline__ float kept_rest(float rest, float ls, float lr) {
+  return rest < 1e-5f && ex2((lr - ls) * kLog2e) == 0.f ? 0.f : rest;
 }
 
 // m_off, ls_off: with a remainder, a logit and ln of the sum of the tokens off the list counted from it.  Their largest one, or (m, lr): but where
@@ -112,7 +118,7 @@ __device__ __forceinline__ Coef distill_coef(const DistillParams& p, float sum, 
   c.beta = 0.f;
   c.off_l = ls * kLog2e;
   c.alpha_l = w * p.scale * (sum + rest);
-  if (TAIL) {
+  if (TAIL && !(rest == 0.f)) {
     const bool some = ls_off != -INFINITY;
     if (some) c.m = m_off;
     c.off = some ? ls_off * kLog2e : 0.f;
@@ -332,14 +338,15 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
     Acc all = dense;
     if (TAIL) all.merge(listed, k);
     const float ls = log_sum(all);
-    const float lr = TAIL ? log_rest(dense, all.m, p.scale) : 0.f;
+    const float ls_off = TAIL ? log_sum(dense) : 0.f, lr = TAIL ? log_rest(dense, ls_off, all.m, p.scale) : 0.f;
+    const float rest = TAIL ? kept_rest(teach.z, ls, lr) : 0.f;
     const float zk = E::to(z_listed);
     Coef coef;
     const Row<DT> out(p.dlogits, grad ? r : 0, p.grad_stride, p.vocab);
     bool rep = false;
     float listed_grad = 0.f, add = 0.f;
     if constexpr (grad) {
-      coef = distill_coef<TAIL>(p, teach.y, teach.z, all.m, ls, lr, dense.m, log_sum(dense), w_row);
+      coef = distill_coef<TAIL>(p, teach.y, rest, all.m, ls, lr, dense.m, ls_off, w_row);
       add = -w_row * p.scale * pk;
       listed_grad = grad_of(zk, coef);
       if (tid < n) list.add[tid] = add;
@@ -395,9 +402,9 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
     if (rank == 0 && tid < kMaxList) {
       float l = 0.f;
       if (!(pk == 0.f)) l = ls == -INFINITY && pk > 0.f ? INFINITY : pk * (logf(pk) - ((zk - all.m) * p.scale - ls));
-      if (TAIL && tid == 0 && !(teach.z == 0.f)) {
-        if (ls == -INFINITY && teach.z > 0.f) l = INFINITY;
-        else if (!(lr == -INFINITY && teach.z < 1e-5f)) l += teach.z * (logf(teach.z) - (lr - ls));
+      if (TAIL && tid == 0 && !(rest == 0.f)) {   // lr - ls in parts: their products with rest are in range where lr itself is not
+        if (ls == -INFINITY && rest > 0.f) l = INFINITY;
+        else l += rest * (logf(rest) - ls_off + ls) + rest * p.scale * (all.m - dense.m);
       }
 #pragma unroll
       for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
@@ -477,10 +484,11 @@ __global__ void __launch_bounds__(kGradThreads, TAIL ? 6 : 0) distill_grad_kerne
   __syncthreads();
   const float3 teach = join_entries<TAIL>(x, teacher);
   if (tid < kMaxList) list.add[tid] = -w * p.scale * (e.id >= 0 ? teach.x : 0.f);
+  const float rest = TAIL ? kept_rest(teach.z, ls, lr) : 0.f;
   int part = blockIdx.x % p.split, each = p.each;
   float m_off = m, ls_off = lr;
   if constexpr (TAIL) {
-    if (!(teach.z == 0.f) && w != 0.f && lr != -INFINITY && ex2((lr - ls) * kLog2e) == 0.f) {   // alike in all blocks of the row
+    if (!(rest == 0.f) && w != 0.f && lr != -INFINITY && ex2((lr - ls) * kLog2e) == 0.f) {   // alike in all blocks of the row
       if (part) return;
       each = in.granules();
       const Acc dense = sum_off_list<DT>(in, list, p.list_k, p.scale * kLog2e, off);
@@ -488,7 +496,7 @@ __global__ void __launch_bounds__(kGradThreads, TAIL ? 6 : 0) distill_grad_kerne
       ls_off = log_sum(dense);
     }
   }
-  const Coef c = distill_coef<TAIL>(p, teach.y, teach.z, m, ls, lr, m_off, ls_off, w);
+  const Coef c = distill_coef<TAIL>(p, teach.y, rest, m, ls, lr, m_off, ls_off, w);
   grad_part<DT, false>(in, out, Part<DT>(in, part, each), c, list, p.list_k);
 }
 

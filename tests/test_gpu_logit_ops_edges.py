@@ -115,3 +115,13 @@ def test_remainder_over_finite_masks(dtype, mask, scale, p_rest, rows, vocab, of
 @pytest.mark.parametrize("mask", [None, -1e9])
 def test_remainder_over_finite_masks_beyond_shared_memory(dtype, vocab, mask):
     run_masked_rest(dtype, mask, 1.0, 0.1, 2, vocab, 1, True, True, False)
+
+
+# ------------------------------------------------------------------------------------------------ what rounding leaves of no remainder
+@pytest.mark.parametrize("dtype,mask", MASK_VALUES)
+@pytest.mark.parametrize("scale", [0.5, 1.0, 2.0])
+@pytest.mark.parametrize("p_rest", [0.0, 6e-8, 0.1])
+@pytest.mark.parametrize("rows,vocab", [(4, 3001), (1, 128000)])
+def test_no_remainder_over_finite_masks(dtype, mask, scale, p_rest, rows, vocab):
+    """A list that holds all of the teacher's mass: what rounding leaves of 1 - sum p must not meet ln q_r of -1e9."""
+    run_masked_rest(dtype, mask, scale, p_rest, rows, vocab, 0, False, True, True)
