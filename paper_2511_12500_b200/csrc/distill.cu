@@ -111,18 +111,18 @@ __device__ __forceinline__ float kept_rest(float rest, float ls, float lr) {
 // m_off, ls_off: with a remainder, a logit and ln of the sum of the tokens off the list counted from it.  Their largest one, or (m, lr): but where
 // they are all masked by a finite value, (z - m) k and lr are so far below 0 that their difference, the logarithm of a share, is lost.
 template <bool TAIL>
-__device__ __forceinline__ Coef distill_coef(const DistillParams& p, float sum, float rest, float m, float ls, float lr, float m_off, float ls_off, float w) {
+__device__ __forceinline__ Coef distill_coef(float scale, float sum, float rest, float m, float ls, float lr, float m_off, float ls_off, float w) {
   Coef c;
-  c.k = p.scale * kLog2e;
+  c.k = scale * kLog2e;
   c.m = c.m_l = m;
   c.beta = 0.f;
   c.off_l = ls * kLog2e;
-  c.alpha_l = w * p.scale * (sum + rest);
+  c.alpha_l = w * scale * (sum + rest);
   if (TAIL && !(rest == 0.f)) {
     const bool some = ls_off != -INFINITY;
     if (some) c.m = m_off;
     c.off = some ? ls_off * kLog2e : 0.f;
-    c.alpha = some ? w * p.scale * ((sum + rest) * ex2((lr - ls) * kLog2e) - rest) : 0.f;
+    c.alpha = some ? w * scale * ((sum + rest) * ex2((lr - ls) * kLog2e) - rest) : 0.f;
   } else {
     c.off = c.off_l;
     c.alpha = c.alpha_l;
@@ -181,6 +181,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
   __shared__ Warps<T / 32> buf[2];
   __shared__ Found found[2];         // as the lists
   __shared__ float red[kMaxList / 32];
+  __shared__ float4 upper[HELD ? 1 : T];
   __shared__ int repeats[2];         // whether a column comes twice on the list
   uint32_t* const on_list = reinterpret_cast<uint32_t*>(held + (HELD ? p.hold : 0));
   const uint8_t* const marks = reinterpret_cast<const uint8_t*>(on_list);
@@ -214,7 +215,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
   for (int turn = 0; r < p.rows; r += step, turn ^= 1) {
     List& list = lists[turn];
     const Entry entry = ahead.checked<TAIL>(p);
-    Sums<DT, false> sums(k);
+    Sums<DT, false, !HELD> sums(k, upper + (HELD ? 0 : tid));
     const bool own = entry.id >= 0 && part.has(in.ph + entry.id);
     typename E::T z_listed = E::from(-INFINITY);   // the listed token's logit: of all tokens in the first block, of the part's own in the others
     if (own || (rank == 0 && entry.id >= 0)) z_listed = in.column(entry.id);
@@ -254,6 +255,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
           for (int u = 0; u < U; ++u)
             if ((ALL || u * T < left) && bits[u]) g[u] = without<DT>(g[u], bits[u]);
         }
+        sums.template pace<T, U>(b);
         sums.template add<ALL>(g, largest<DT, ALL>(g, left, T), left, T);
       });
       if (tid < part.n_all - part.n_int) {
@@ -289,6 +291,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
                 if ((ALL || u * T < left) && bits[u]) g[u] = without<DT>(g[u], bits[u]);
             }
           }
+          sums.template pace<T, U>(b);
           sums.template add<ALL>(g, largest<DT, ALL>(g, left, T), left, T);
         };
         int b = 0;
@@ -346,7 +349,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
     bool rep = false;
     float listed_grad = 0.f, add = 0.f;
     if constexpr (grad) {
-      coef = distill_coef<TAIL>(p, teach.y, rest, all.m, ls, lr, dense.m, ls_off, w_row);
+      coef = distill_coef<TAIL>(p.scale, teach.y, rest, all.m, ls, lr, dense.m, ls_off, w_row);
       add = -w_row * p.scale * pk;
       listed_grad = grad_of(zk, coef);
       if (tid < n) list.add[tid] = add;
@@ -432,6 +435,7 @@ constexpr int kSieve = 4096;   // granules are looked up on the list where granu
 struct OffList {
   uint32_t sieve[kSieve / 32];
   Warps<kGradThreads / 32> buf;
+  float4 upper[kGradThreads];
 };
 struct NoOffList {};
 template <int DT>
@@ -446,7 +450,7 @@ __device__ __forceinline__ Acc sum_off_list(const Row<DT> row, const List& list,
   }
   __syncthreads();
   const Part<DT> whole(row, 0, row.granules());
-  Sums<DT, false> sums(k);
+  Sums<DT, false, true> sums(k, sh.upper + tid);
   for (int i = tid; i < whole.n_all; i += T) {
     uint4 g[1] = {whole.raw(row, i)};
     const int v = whole.granule(i);
@@ -458,6 +462,7 @@ __device__ __forceinline__ Acc sum_off_list(const Row<DT> row, const List& list,
       }
       g[0] = without<DT>(g[0], bits);
     }
+    sums.template pace<T, 1>(i - tid);
     sums.template add<true>(g, largest<DT>(g[0]));
   }
   warp_share<false>(sums.done(), k, sh.buf);
@@ -466,9 +471,21 @@ __device__ __forceinline__ Acc sum_off_list(const Row<DT> row, const List& list,
 }
 
 // A row whose student gives the tokens off the list no probability in 32 bits, but not -inf, is one block's: saved statistics do not hold how its
-// remainder is spread (distill_coef), so the row is summed again, before any of it is replaced.  Six blocks an SM, as the other form has by itself.
+// remainder is spread (distill_coef), so the row is summed again, before any of it is replaced.  Not inlined, so that
+// its registers are not other rows'.
+template <int DT>
+__device__ __noinline__ void grad_of_masked_rest(const DistillParams& p, int64_t r, const List& list, OffList& sh, float sum, float rest) {
+  const Row<DT> in(p.logits, r, p.stride, p.vocab), out(p.dlogits, r, p.grad_stride, p.vocab);
+  const int n = p.list_k;
+  const float scale = p.scale, w = p.weight[r], m = p.stats[3 * r], ls = p.stats[3 * r + 1], lr = p.stats[3 * r + 2];
+  const Acc dense = sum_off_list<DT>(in, list, n, scale * kLog2e, sh);
+  const Coef c = distill_coef<true>(scale, sum, rest, m, ls, lr, dense.m, log_sum(dense), w);
+  grad_part<DT, false>(in, out, Part<DT>(in, 0, in.granules()), c, list, n);
+}
+
+// With a remainder as many blocks an SM as the other form has by itself.
 template <int DT, bool TAIL>
-__global__ void __launch_bounds__(kGradThreads, TAIL ? 6 : 0) distill_grad_kernel(const DistillParams p) {
+__global__ void __launch_bounds__(kGradThreads, TAIL ? 6 : 0) distill_grad_kernel(const __grid_constant__ DistillParams p) {
   __shared__ List list;
   __shared__ TeacherSums teacher;
   __shared__ typename std::conditional<TAIL, OffList, NoOffList>::type off;
@@ -485,19 +502,15 @@ __global__ void __launch_bounds__(kGradThreads, TAIL ? 6 : 0) distill_grad_kerne
   const float3 teach = join_entries<TAIL>(x, teacher);
   if (tid < kMaxList) list.add[tid] = -w * p.scale * (e.id >= 0 ? teach.x : 0.f);
   const float rest = TAIL ? kept_rest(teach.z, ls, lr) : 0.f;
-  int part = blockIdx.x % p.split, each = p.each;
-  float m_off = m, ls_off = lr;
+  const int part = blockIdx.x % p.split;
   if constexpr (TAIL) {
     if (!(rest == 0.f) && w != 0.f && lr != -INFINITY && ex2((lr - ls) * kLog2e) == 0.f) {   // alike in all blocks of the row
-      if (part) return;
-      each = in.granules();
-      const Acc dense = sum_off_list<DT>(in, list, p.list_k, p.scale * kLog2e, off);
-      m_off = dense.m;
-      ls_off = log_sum(dense);
+      if (part == 0) grad_of_masked_rest<DT>(p, r, list, off, teach.y, rest);
+      return;
     }
   }
-  const Coef c = distill_coef<TAIL>(p, teach.y, rest, m, ls, lr, m_off, ls_off, w);
-  grad_part<DT, false>(in, out, Part<DT>(in, part, each), c, list, p.list_k);
+  const Coef c = distill_coef<TAIL>(p.scale, teach.y, rest, m, ls, lr, m, lr, w);
+  grad_part<DT, false>(in, out, Part<DT>(in, part, p.each), c, list, p.list_k);
 }
 
 }  // namespace rows

@@ -342,37 +342,67 @@ __device__ __forceinline__ bool lift_floor(float m, float k, uint32_t& word) {
 // the end: its slack is 8 (entropies of 4096 x 128000: 1.1e-6 off with a slack of 24, 1e-7 with 8; 2 takes 4 % longer).  Per element one
 // instruction to unpack, half of one each to subtract, scale and add, and the exponential; with the entropy half of one each
 // for the lift (on packed 16-bit values) and the second sum.
-template <int DT, bool ENTROPY>
+//
+// Sums are taken in two levels, as each addition rounds, and equal terms round to the same side (a chain of 4096 terms 0.7: 3e-5 off): pace() ends
+// a chain of at most 128 terms in each of two halves.  LONG, for parts of any length: the sums above them keep what their additions lose, so that a
+// row of 2^30 columns is as near as a short one.  They lie in shared memory, as they are seldom touched: in registers they made the kernels spill
+// (1 to 4 %).
+template <int DT, bool ENTROPY, bool LONG>
 struct Sums {
   static constexpr float kSlack = ENTROPY ? 8.f : 24.f;
-  Acc a;
+  Acc a;           // LONG: s and t in the end
+  float4* upper;   // LONG: s, t, and what the additions to them lost
   float k, top = -FLT_MAX;   // top: the largest logit so far
   bool lift = false;
   uint32_t floor = 0;
   uint64_t s2 = 0, t2 = 0;   // sums of even and odd places since the last raise
   uint64_t k2, minus_m2;
-  __device__ __forceinline__ explicit Sums(float k_) : k(k_), k2(pair(k_, k_)), minus_m2(pair(FLT_MAX, FLT_MAX)) {}
+  __device__ __forceinline__ Sums(float k_, float4* upper_) : upper(upper_), k(k_), k2(pair(k_, k_)), minus_m2(pair(FLT_MAX, FLT_MAX)) {
+    if (LONG) *upper = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  static __device__ __forceinline__ void add_exactly(float& sum, float& lost, float x) {
+    const float more = __fadd_rn(x, lost), to = __fadd_rn(sum, more);
+    lost = __fsub_rn(more, __fsub_rn(to, sum));
+    sum = to;
+  }
   __device__ __forceinline__ void flush() {
-    const float2 s = unpair(s2);
-    a.s += s.x + s.y;
-    s2 = 0;
-    if (ENTROPY) {
-      const float2 t = unpair(t2);
-      a.t += t.x + t.y;
-      t2 = 0;
+    const float2 s = unpair(s2), t = unpair(t2);
+    s2 = t2 = 0;
+    if (LONG) {
+      float4 u = *upper;
+      add_exactly(u.x, u.z, s.x + s.y);
+      if (ENTROPY) add_exactly(u.y, u.w, t.x + t.y);
+      *upper = u;
+    } else {
+      a.s += s.x + s.y;
+      if (ENTROPY) a.t += t.x + t.y;
     }
+  }
+  __device__ __forceinline__ void rebase(float mx) {
+    flush();
+    if (LONG) {
+      a.s = upper->x;
+      a.t = upper->y;
+    }
+    a.rebase(mx, k);
+    if (LONG) *upper = make_float4(a.s, a.t, 0.f, 0.f);
+  }
+  // Before a batch of U granules of every thread that begins at granule b = i T U of its loop.
+  template <int T, int U>
+  __device__ __forceinline__ void pace(int b) {
+    constexpr int kBatches = 128 / (U * Elem<DT>::VE / 2);
+    static_assert((kBatches & (kBatches - 1)) == 0 && (T * U & (T * U - 1)) == 0, "powers of two");
+    if ((b & (kBatches * T * U - 1)) == 0) flush();
   }
   __device__ __forceinline__ void raise(float mx) {   // before adding logits of which mx is the largest
     top = max_nan(top, mx);
     if ((mx - a.m) * k <= kSlack) return;
-    flush();
-    a.rebase(max_nan(a.m, mx), k);
+    rebase(max_nan(a.m, mx));
     minus_m2 = pair(-a.m, -a.m);
     if (ENTROPY) lift = lift_floor<DT>(a.m, k, floor);
   }
   __device__ __forceinline__ Acc done() {   // counted from the largest logit
-    flush();
-    a.rebase(top, k);
+    rebase(top);
     return a;
   }
   __device__ __forceinline__ void add_lifted(const uint4& g) {
@@ -393,10 +423,11 @@ struct Sums {
     float x[VE];
     Elem<DT>::unpack(g, x);
 #pragma unroll
-    for (int e = 0; e < VE; ++e) {
-      const float y = max_nan((x[e] - a.m) * k, kFloor), f = ex2(y);
-      a.s += f;
-      a.t = fmaf(f, y, a.t);
+    for (int e = 0; e < VE; e += 2) {
+      const float y0 = max_nan((x[e] - a.m) * k, kFloor), y1 = max_nan((x[e + 1] - a.m) * k, kFloor);
+      const uint64_t f = pair(ex2(y0), ex2(y1));
+      s2 = add2f(s2, f);
+      t2 = fma2f(f, pair(y0, y1), t2);
     }
   }
   // Granules g[0 .. U), the first `left` of every T-th (all of them if ALL), of which mx is the largest logit.

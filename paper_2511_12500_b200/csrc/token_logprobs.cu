@@ -31,6 +31,12 @@ __device__ __forceinline__ float log_prob(float z, float m, float ls, float scal
 }
 
 struct NoTop {};
+// Where a thread's upper sums lie: the list is filled behind the pass (the kernel with pieces has shared memory for five blocks an SM and no more).
+__device__ __forceinline__ float4* upper_of(NoTop&, float4* upper) { return upper + threadIdx.x; }
+__device__ __forceinline__ float4* upper_of(TopShared& top, float4*) {
+  static_assert(sizeof(top.key) >= kScoreThreads * sizeof(float4), "one for each thread");
+  return reinterpret_cast<float4*>(top.key) + threadIdx.x;
+}
 
 // One cluster of `split` blocks a row; each takes an equal run of granules, and all get what each found.
 //
@@ -49,6 +55,7 @@ __global__ void __launch_bounds__(kScoreThreads, TOP == kTopPiecewise ? 5 : 4) s
   constexpr int T = kScoreThreads, U = TOP == kTopOneBatch ? kOneBatch / T : 4;
   __shared__ Warps<T / 32> buf;
   __shared__ Warps<kMaxSplit> parts;   // of the cluster's blocks
+  __shared__ float4 upper[TOP == kNoTop ? T : 1];
   __shared__ typename std::conditional<TOP != kNoTop, TopShared, NoTop>::type top;
   extern __shared__ uint64_t lists[];   // TOP and split > 1: the blocks' sorted lists, top_k keys each, 0 where one is shorter
   const int split = p.split, rank = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x;
@@ -68,7 +75,7 @@ __global__ void __launch_bounds__(kScoreThreads, TOP == kTopPiecewise ? 5 : 4) s
     there = t >= 0 && t < p.vocab;
     if (there) zt = E::to(row.column((int)t));
   }
-  Sums<DT, ENTROPY> sums(k);
+  Sums<DT, ENTROPY, TOP != kTopOneBatch> sums(k, upper_of(top, upper));
   const uint4* const from = reinterpret_cast<const uint4*>(row.at(part.w0)) + tid;
   const int n = part.n_all, shift = TOP == kTopPiecewise ? piece_shift(n) : 0;
   float best = -INFINITY, of_piece = -INFINITY;
@@ -87,6 +94,7 @@ __global__ void __launch_bounds__(kScoreThreads, TOP == kTopPiecewise ? 5 : 4) s
     const int left = n - b - tid;
     load(b, all);
     const float mx = largest<DT, ALL>(g, left, T);
+    sums.template pace<T, U>(b);
     sums.template add<ALL>(g, mx, left, T);
     if constexpr (TOP == kTopPiecewise) {   // the largest of each piece: 1 or 2 granules of the batch, all of them, or those of several batches
       static_assert(TOP != kTopPiecewise || U == 4, "pieces of 1, 2 and 4 granules lie in a batch");
@@ -127,6 +135,7 @@ __global__ void __launch_bounds__(kScoreThreads, TOP == kTopPiecewise ? 5 : 4) s
       if (B <= part.n_int) fetch(0, g);
       for (; b + 3 * B <= part.n_int; b += 2 * B) {
         fetch(b + B, h);
+        sums.template pace<T, U>(b);
         sums.template add<true>(g, largest<DT, true>(g, 0, T));
         fetch(b + 2 * B, g);
         sums.template add<true>(h, largest<DT, true>(h, 0, T));

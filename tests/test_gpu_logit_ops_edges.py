@@ -125,3 +125,33 @@ def test_remainder_over_finite_masks_beyond_shared_memory(dtype, vocab, mask):
 def test_no_remainder_over_finite_masks(dtype, mask, scale, p_rest, rows, vocab):
     """A list that holds all of the teacher's mass: what rounding leaves of 1 - sum p must not meet ln q_r of -1e9."""
     run_masked_rest(dtype, mask, scale, p_rest, rows, vocab, 0, False, True, True)
+
+
+# ------------------------------------------------------------------------------------------------ long rows
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_sums_of_long_rows(dtype):
+    """2^24 columns of which seven in eight are 0.7 times as probable as the eighth: a chain of all of a thread's terms (4096 in a lane) rounds
+    each to the same side and is 3e-5 off; the tolerance is that of short rows."""
+    vocab, rows = 1 << 24, 1
+    z = torch.full((rows, vocab), math.log(0.7), dtype=TORCH[dtype], device="cuda")
+    z[:, ::8] = 0.0
+    x = z.double()
+    ls = float(torch.logsumexp(x, 1)[0])
+    lq = x[0] - ls
+    h = float(-(lq.exp() * lq).sum())
+    t = torch.tensor([[0, 1]], device="cuda")
+    for entropy in (True, False):
+        for top in (0, 5):
+            out = score(z, dtype, t, top, entropy)
+            close(as64(out["stats"][0]), [0.0, ls], [0.0, 1e-5], "stats")
+            close(as64(out["logprob"][0]), as64(lq[:2]), 1e-5 + 1e-6 * ls, "logprob")
+            if entropy:
+                close(out["entropy"][0].item(), h, 3e-5 + 1e-6 * h, "entropy")
+    ids = torch.arange(16, device="cuda")[None]
+    tv = torch.log_softmax(torch.arange(16, device="cuda") * -0.1, 0)[None].float().contiguous()
+    for tail in (False, True):
+        for dz in (None, torch.empty_like(z)):
+            loss, st = run_distill(z, dtype, ids, tv, tail, dz=dz)
+            close(as64(st[0, :2]), [0.0, ls], [0.0, 1e-5], "stats")
+            want = float((tv.double().exp() * (tv.double() - lq[:16])).sum())
+            close(loss[0].item(), want, 1e-5 + 1e-5 * 20, "loss")
