@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
     const float x = share_entry<TAIL>(entry, teacher);
     const int mark = own ? part.place((in.ph + entry.id) / VE) : -1;   // the listed token's granule and its bit in there
     const uint32_t bit = own ? 1u << (mark % 4 * 8 + (in.ph + entry.id) % VE) : 0;
-    bool first = false;                                                // of entries with the same column
+    bool first = false;                                                // of entries with the same column: the one whose logit is summed
     if (tid == 0) repeats[turn ^ 1] = 0;
     const int64_t r_next = r + step;
     const bool more = MODE != kLossOnly && r_next < p.rows;
@@ -266,7 +266,10 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
       for (int b0 = 0; b0 < part.n_all; b0 += p.hold) {   // p.hold granules at a time have marks
         const bool in_piece = TAIL && own && mark >= b0 && mark < b0 + p.hold;
         if (TAIL) {
-          if (in_piece) first = !(atomicOr(&on_list[(mark - b0) / 4], bit) & bit);
+          if (in_piece) {
+            first = !(atomicOr(&on_list[(mark - b0) / 4], bit) & bit);
+            if (!first) repeats[turn] = 1;
+          }
           __syncthreads();
         }
         const int size = min(part.n_all - b0, p.hold), inside = min(part.n_int - b0, size);
@@ -307,6 +310,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
     warp_share<false>(sums.done(), k, buf[0]);
     if (TAIL) {
       Acc listed;
+      if (repeats[turn] && own) first = !comes_again(list, tid);   // not the one that came first: sums must not depend on that
       if (first) listed.add_one(E::to(z_listed), k);
       warp_share<false>(listed, k, buf[1]);
     }

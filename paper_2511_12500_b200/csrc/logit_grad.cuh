@@ -41,6 +41,16 @@ __device__ __forceinline__ bool repeated(const List& l, int n, int i) {
   }
   return same > 1;
 }
+// Whether an entry before entry i has its column.
+__device__ __forceinline__ bool comes_again(const List& l, int i) {
+  const int id = l.id[i];
+  int same = 0;
+  for (int j = 0; j < i; j += 4) {
+    const int4 o = *reinterpret_cast<const int4*>(&l.id[j]);
+    same += (o.x == id) + (o.y == id && j + 1 < i) + (o.z == id && j + 2 < i) + (o.w == id && j + 3 < i);
+  }
+  return same > 0;
+}
 __device__ __forceinline__ float sum_of_column(const List& l, int n, int i) {
   float s = 0.f;
   const int id = l.id[i];

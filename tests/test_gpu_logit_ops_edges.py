@@ -155,3 +155,22 @@ def test_sums_of_long_rows(dtype):
             close(as64(st[0, :2]), [0.0, ls], [0.0, 1e-5], "stats")
             want = float((tv.double().exp() * (tv.double() - lq[:16])).sum())
             close(loss[0].item(), want, 1e-5 + 1e-5 * 20, "loss")
+
+
+# ------------------------------------------------------------------------------------------------ tokens listed twice
+@pytest.mark.parametrize("rows,vocab", [(600, 5000), (40, 60000)])
+@pytest.mark.parametrize("grad", [True, False])
+def test_tokens_listed_twice_give_the_same_bits(rows, vocab, grad):
+    """Every token is listed by two warps: which of them is counted must not depend on which comes first."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    z = torch.randn(rows, vocab, device="cuda", generator=gen) * 2
+    half = torch.rand(rows, vocab, device="cuda", generator=gen).topk(64, dim=1).indices
+    ids = torch.cat([half, half.flip(1)], 1).contiguous()
+    tv = torch.log_softmax(torch.randn(rows, 128, device="cuda", generator=gen), 1).sub(0.3).contiguous()
+    dz = torch.empty_like(z) if grad else None
+    loss, stats = run_distill(z, "fp32", ids, tv, True, dz=dz)
+    first = [x.clone() for x in (loss, stats, dz) if x is not None]
+    for _ in range(60):
+        loss, stats = run_distill(z, "fp32", ids, tv, True, dz=dz)
+        for a, b in zip(first, [x for x in (loss, stats, dz) if x is not None]):
+            assert torch.equal(a, b)
