@@ -482,7 +482,7 @@ int iris_gemm_all_scatter_noalloc(const void* A, const void* const* B_shards, co
  *               IRIS_BF16 or IRIS_F32).  row_stride in elements, >= vocab; 0 = vocab.  Rows may start at any element
  *               (16-bit logits at any even address); 16-byte aligned rows are the fast case.  Nothing outside a row is
  *               read or written.  rows < 2^31, vocab <= 2^30 (IRIS_ERR_UNSUPPORTED beyond that).
- *   scale       > 0: the softmax is taken of scale * z (1 / temperature).
+ *   scale       > 0, at most 2e38: the softmax is taken of scale * z (1 / temperature).
  *   targets, teacher_ids, top_ids   int64 column indices.
  * Statistics, probabilities and sums are fp32.  -inf logits are masked tokens (probability 0); a mask of the type's
  * lowest finite value is an ordinary value, also where a row holds nothing else.  A row with no finite logit has log

@@ -533,7 +533,7 @@ int check_distill(const char* fn, const iris_distill_args* a, int64_t* stride, i
   if (!a) return fail(IRIS_ERR_ARG, "%s: args is NULL", fn);
   *stride = a->row_stride;
   IRIS_CHECK(check_logits(fn, "logits", a->logits, a->dtype, a->rows, a->vocab, stride));
-  IRIS_CHECK(check_scale(fn, "scale", a->scale));
+  IRIS_CHECK(check_scale(fn, "scale", a->scale, kMaxScale));
   IRIS_CHECK(check_scale(fn, "teacher_scale", a->teacher_scale));
   if (a->mode != IRIS_DISTILL_RENORM && a->mode != IRIS_DISTILL_TAIL) return fail(IRIS_ERR_ARG, "%s: unknown mode %d", fn, a->mode);
   if (a->list_k < 0 || a->list_k > kMaxList) return fail(IRIS_ERR_ARG, "%s: list_k=%d not in [0, %d]", fn, a->list_k, kMaxList);

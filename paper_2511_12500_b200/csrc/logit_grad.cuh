@@ -26,9 +26,14 @@ struct List {
 // power of two, so that a y of 0 still gives alpha.  (By 32, the rounding of exponents near 32 was 1e-6 of the result.)
 constexpr float kRaise = 8.f, kLower = 1.f / 256.f;
 
+// 2^y (alpha + beta y): beta y would overflow for a large beta where 2^y is 0.
+__device__ __forceinline__ float raised(float y, float alpha, float beta) {
+  const float e = ex2(y + kRaise);
+  return fmaf(e * max_nan(y, kFloor), beta, e * alpha) * kLower;
+}
 __device__ __forceinline__ float grad_of(float z, const Coef& c) {   // on the list
   const float y = (z - c.m_l) * c.k - c.off_l;
-  return ex2(y + kRaise) * fmaf(c.beta, max_nan(y, kFloor), c.alpha_l) * kLower;
+  return raised(y, c.alpha_l, c.beta);
 }
 
 // Whether another entry of the first n has entry i's column.
@@ -93,7 +98,7 @@ struct Dense {
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
       const float y = (x[e] - c.m) * c.k - c.off;
-      x[e] = c.zero ? 0.f : ex2(y + kRaise) * fmaf(c.beta, max_nan(y, kFloor), c.alpha) * kLower;
+      x[e] = c.zero ? 0.f : raised(y, c.alpha, c.beta);
     }
   }
 };

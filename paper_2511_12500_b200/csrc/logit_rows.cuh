@@ -22,6 +22,7 @@ constexpr int64_t kMaxVocab = 1 << 30;      // columns are counted in 32 bits in
 constexpr int kSms = 148;                    // of a B200
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kMaxScale = 2e38f;           // times log2(e) it is in the type's range, so that times a difference of 0 it is 0
 constexpr float kFloor = -1024.f;           // exponents (base 2) are cut here: 2^-1024 is 0 in 32 bits, and 0 * -1024 is not NaN
 
 __device__ __forceinline__ float ex2(float x) {
@@ -526,8 +527,9 @@ inline int part_granules(const void* p, int64_t stride, int64_t vocab, int dtype
   const int64_t granules = (vocab + (aligned ? ve - 1 : 2 * ve - 2)) / ve;
   return (int)((granules + parts - 1) / parts);
 }
-inline int check_scale(const char* fn, const char* what, float s) {
+inline int check_scale(const char* fn, const char* what, float s, float most = FLT_MAX) {
   if (!(s > 0.f) || std::isinf(s)) return fail(IRIS_ERR_ARG, "%s: %s has to be positive and finite", fn, what);
+  if (s > most) return fail(IRIS_ERR_ARG, "%s: %s is at most %g", fn, what, most);
   return IRIS_OK;
 }
 inline int check_aligned(const char* fn, const char* what, const void* p, size_t a, bool needed) {

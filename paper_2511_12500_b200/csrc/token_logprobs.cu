@@ -308,7 +308,7 @@ extern "C" int iris_token_logprobs(const iris_logprob_args* a, void* stream) {
   if (!a) return fail(IRIS_ERR_ARG, "%s: args is NULL", fn);
   int64_t stride = a->row_stride;
   IRIS_CHECK(check_logits(fn, "logits", a->logits, a->dtype, a->rows, a->vocab, &stride));
-  IRIS_CHECK(check_scale(fn, "scale", a->scale));
+  IRIS_CHECK(check_scale(fn, "scale", a->scale, kMaxScale));
   if (a->n_targets < 0 || a->n_targets > kMaxList) return fail(IRIS_ERR_ARG, "%s: n_targets=%d not in [0, %d]", fn, a->n_targets, kMaxList);
   if (a->top_k < 0 || a->top_k > kMaxList) return fail(IRIS_ERR_ARG, "%s: top_k=%d not in [0, %d]", fn, a->top_k, kMaxList);
   if (a->top_k > a->vocab) return fail(IRIS_ERR_ARG, "%s: top_k=%d exceeds vocab=%lld", fn, a->top_k, (long long)a->vocab);
@@ -338,7 +338,7 @@ extern "C" int iris_token_logprobs_backward(const iris_logprob_grad_args* a, voi
   int64_t stride = a->row_stride, gstride = a->grad_stride;
   IRIS_CHECK(check_logits(fn, "logits", a->logits, a->dtype, a->rows, a->vocab, &stride));
   IRIS_CHECK(check_logits(fn, "dlogits", a->dlogits, a->dtype, a->rows, a->vocab, &gstride));
-  IRIS_CHECK(check_scale(fn, "scale", a->scale));
+  IRIS_CHECK(check_scale(fn, "scale", a->scale, kMaxScale));
   if (a->n_targets < 0 || a->n_targets > kMaxList) return fail(IRIS_ERR_ARG, "%s: n_targets=%d not in [0, %d]", fn, a->n_targets, kMaxList);
   IRIS_CHECK(check_in_place(fn, a->logits, stride, a->dlogits, gstride, a->rows, a->vocab, a->dtype));
   if (a->rows == 0 || a->vocab == 0) return IRIS_OK;

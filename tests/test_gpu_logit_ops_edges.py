@@ -174,3 +174,29 @@ def test_tokens_listed_twice_give_the_same_bits(rows, vocab, grad):
         loss, stats = run_distill(z, "fp32", ids, tv, True, dz=dz)
         for a, b in zip(first, [x for x in (loss, stats, dz) if x is not None]):
             assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------------------------------------ scales near the type's largest
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("scale", [1e30, 1e36, 2e38])
+def test_scales_near_the_largest(dtype, scale):
+    """Differences of half a unit become 1e30 and more: one token, or equal ones, have all the probability, and
+    scale g_H ln 2 times a cut exponent overflows.  (scale log2(e) itself does from 2.4e38 on: refused.)"""
+    values = np.full((3, 900), -1.0)
+    values[0, 400], values[1, [5, 6, 700]], values[2, ::2] = -0.5, -0.5, -np.inf
+    values[2, 31] = -0.75
+    _, z = strided(values, dtype)
+    t = torch.tensor([[400, 3], [6, 7], [31, 0]], device="cuda")
+    out = score(z, dtype, t, 5, True, scale)
+    check_score(z, out, t, 5, scale)
+    g, gh = torch.full((3, 2), 1 / scale, device="cuda"), torch.ones(3, device="cuda")
+    dz = torch.empty_like(z)
+    run_score_grad(z, dtype, t, g, gh, scale, dz, out["stats"], out["entropy"])
+    g64, v = as64(g), as64(z)
+    for r in (0, 2):                                       # row 1 has entropy, whose gradient is rounding times the scale
+        want, _ = ref.score_grad(v[r], scale, t[r].cpu().numpy(), g64[r], 1.0)
+        close(as64(dz[r]), want, HALF_UNIT[dtype] * np.abs(want) + 3e-5, "dz")
+    ids, tv = t.clone(), torch.zeros(3, 2, device="cuda")
+    loss, st = run_distill(z, dtype, ids[:, :1].contiguous(), tv[:, :1].contiguous(), False, scale, dz=dz, weight=torch.full((3,), 1 / scale, device="cuda"))
+    close(as64(loss), [0.0, math.log(3), 0.0], 1e-5, "loss")
+    close(as64(dz[1, [5, 6, 700]]), [1 / 3, -2 / 3, 1 / 3], 2.0 ** -8 if dtype == "bf16" else 3e-5, "dz")
