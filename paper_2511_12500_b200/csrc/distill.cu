@@ -43,10 +43,9 @@ struct Entry {
 struct RawEntry {   // as loaded: nothing waits for it yet
   int64_t id = -1;
   float v = 0.f;
-  template <bool TAIL>
   __device__ __forceinline__ Entry checked(const DistillParams& p) const {
     const bool there = id >= 0 && id < p.vocab;
-    return Entry{there ? (int)id : -1, there ? v * (TAIL ? 1.f : p.teacher_scale) : -INFINITY};
+    return Entry{there ? (int)id : -1, there ? v : -INFINITY};
   }
 };
 struct TeacherSums {
@@ -63,12 +62,13 @@ __device__ __forceinline__ RawEntry load_entry(const DistillParams& p, int64_t r
   return e;
 }
 
-// Before a barrier: what a warp of the list gives to the sum.  Returns exp(v - the warp's m).
+// Before a barrier: what a warp of the list gives to the sum.  Returns exp(scale (v - the warp's m)): differences are scaled, as a mask's finite value
+// times the scale may overflow.
 template <bool TAIL>
-__device__ __forceinline__ float share_entry(const Entry& e, TeacherSums& t) {
+__device__ __forceinline__ float share_entry(const Entry& e, float scale, TeacherSums& t) {
   if (threadIdx.x >= kMaxList) return 0.f;
   const float m = TAIL ? 0.f : fmaxf(warp_max(e.v == e.v ? e.v : -FLT_MAX), -FLT_MAX);   // log probabilities are taken as they are
-  const float x = expf(e.v - m);
+  const float x = expf(TAIL ? e.v : (e.v - m) * scale);
   float s = x;
 #pragma unroll
   for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
@@ -80,7 +80,7 @@ __device__ __forceinline__ float share_entry(const Entry& e, TeacherSums& t) {
 }
 // Behind it: the entry's p, P and p_r, the latter two in all threads.
 template <bool TAIL>
-__device__ __forceinline__ float3 join_entries(float x, const TeacherSums& t) {
+__device__ __forceinline__ float3 join_entries(float x, float scale, const TeacherSums& t) {
   constexpr int N = kMaxList / 32;
   if (TAIL) {
     const float s = t.s[0] + t.s[1] + t.s[2] + t.s[3];
@@ -90,10 +90,10 @@ __device__ __forceinline__ float3 join_entries(float x, const TeacherSums& t) {
 #pragma unroll
   for (int i = 1; i < N; ++i) m = fmaxf(m, t.m[i]);
 #pragma unroll
-  for (int i = 0; i < N; ++i) s += t.s[i] * ex2((t.m[i] - m) * kLog2e);
+  for (int i = 0; i < N; ++i) s += t.s[i] * ex2((t.m[i] - m) * scale * kLog2e);
   if (s == 0.f) return make_float3(0.f, 0.f, 0.f);   // a list with no token left asks for nothing
   const float own = threadIdx.x < kMaxList ? t.m[threadIdx.x >> 5] : m;
-  return make_float3(x * ex2((own - m) * kLog2e) / s, s == s ? 1.f : NAN, 0.f);
+  return make_float3(x * ex2((own - m) * scale * kLog2e) / s, s == s ? 1.f : NAN, 0.f);
 }
 
 // ln of the sum of the tokens off the list (`dense`), counted from m; what is less than the type holds is its lowest value, as -inf says
@@ -214,13 +214,13 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
   __syncthreads();
   for (int turn = 0; r < p.rows; r += step, turn ^= 1) {
     List& list = lists[turn];
-    const Entry entry = ahead.checked<TAIL>(p);
+    const Entry entry = ahead.checked(p);
     Sums<DT, false, !HELD> sums(k, upper + (HELD ? 0 : tid));
     const bool own = entry.id >= 0 && part.has(in.ph + entry.id);
     typename E::T z_listed = E::from(-INFINITY);   // the listed token's logit: of all tokens in the first block, of the part's own in the others
     if (own || (rank == 0 && entry.id >= 0)) z_listed = in.column(entry.id);
     if (tid < kMaxList) list.id[tid] = entry.id;
-    const float x = share_entry<TAIL>(entry, teacher);
+    const float x = share_entry<TAIL>(entry, p.teacher_scale, teacher);
     const int mark = own ? part.place((in.ph + entry.id) / VE) : -1;   // the listed token's granule and its bit in there
     const uint32_t bit = own ? 1u << (mark % 4 * 8 + (in.ph + entry.id) % VE) : 0;
     bool first = false;                                                // of entries with the same column: the one whose logit is summed
@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
       ahead = load_entry(p, r_next);
       if (p.weight) w = p.weight[r_next];
     }
-    const float3 teach = join_entries<TAIL>(x, teacher);
+    const float3 teach = join_entries<TAIL>(x, p.teacher_scale, teacher);
     const float pk = entry.id >= 0 ? teach.x : 0.f;
     if (split > 1) {
       ptx::cluster_wait();   // behind it no block reads logits of another's part, and the gradient may replace them
@@ -499,11 +499,11 @@ __global__ void __launch_bounds__(kGradThreads, TAIL ? 6 : 0) distill_grad_kerne
   ptx::begin_after_previous();
   const Row<DT> in(p.logits, r, p.stride, p.vocab), out(p.dlogits, r, p.grad_stride, p.vocab);
   const float w = p.weight[r], m = p.stats[3 * r], ls = p.stats[3 * r + 1], lr = p.stats[3 * r + 2];
-  const Entry e = load_entry(p, r).checked<TAIL>(p);
+  const Entry e = load_entry(p, r).checked(p);
   if (tid < kMaxList) list.id[tid] = e.id;
-  const float x = share_entry<TAIL>(e, teacher);
+  const float x = share_entry<TAIL>(e, p.teacher_scale, teacher);
   __syncthreads();
-  const float3 teach = join_entries<TAIL>(x, teacher);
+  const float3 teach = join_entries<TAIL>(x, p.teacher_scale, teacher);
   if (tid < kMaxList) list.add[tid] = -w * p.scale * (e.id >= 0 ? teach.x : 0.f);
   const float rest = TAIL ? kept_rest(teach.z, ls, lr) : 0.f;
   const int part = blockIdx.x % p.split;

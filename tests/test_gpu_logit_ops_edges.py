@@ -200,3 +200,30 @@ def test_scales_near_the_largest(dtype, scale):
     loss, st = run_distill(z, dtype, ids[:, :1].contiguous(), tv[:, :1].contiguous(), False, scale, dz=dz, weight=torch.full((3,), 1 / scale, device="cuda"))
     close(as64(loss), [0.0, math.log(3), 0.0], 1e-5, "loss")
     close(as64(dz[1, [5, 6, 700]]), [1 / 3, -2 / 3, 1 / 3], 2.0 ** -8 if dtype == "bf16" else 3e-5, "dz")
+
+
+@pytest.mark.parametrize("tscale", [2.0, 1e30, 3e38])
+def test_teacher_values_times_teacher_scale_beyond_the_type(tscale):
+    """p = softmax(teacher_scale v): only differences of the values count, also where the products would overflow."""
+    low = float(np.finfo(np.float32).min)
+    v = np.array([[2.0, 1.0, 2.0, -3.0], [low, low, low, low], [low, 3.0, low, -np.inf], [3e38, 3e38, -3e38, 0.0]], np.float32)
+    want = np.array([[0.5, 0, 0.5, 0], [0.25] * 4, [0, 1, 0, 0], [0.5, 0.5, 0, 0]])
+    if tscale == 2.0:
+        e = np.exp(2.0 * (v[0].astype(np.float64) - 2))
+        want[0] = e / e.sum()
+    rng = np.random.default_rng(1)
+    _, z = strided(rng.normal(0, 1, (4, 300)), "fp32")
+    x = as64(z)
+    ids = torch.arange(4, device="cuda").repeat(4, 1).contiguous()
+    dz = torch.empty_like(z)
+    loss, st = run_distill(z, "fp32", ids, torch.from_numpy(v).cuda(), False, 1.0, tscale, dz=dz)
+    back = torch.empty_like(z)
+    iris.iris_distill_topk_backward(z, 4, 300, iris.IRIS_F32, torch.from_numpy(v).cuda(), ids, 4, st, torch.ones(4, device="cuda"), back, teacher_scale=tscale)
+    for r in range(4):
+        lq = ref.log_softmax(x[r], 1.0)[2]
+        p = want[r]
+        close(loss[r].item(), sum(a * (math.log(a) - b) for a, b in zip(p, lq) if a > 0), 1e-4, "loss")
+        dwant = np.exp(lq)
+        dwant[:4] -= p
+        close(as64(dz[r]), dwant, 1e-4 * np.abs(dwant) + 3e-5, "dz")
+        close(as64(back[r]), dwant, 1e-4 * np.abs(dwant) + 3e-5, "backward")
