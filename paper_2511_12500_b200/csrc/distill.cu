@@ -408,7 +408,8 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
     }
     if (rank == 0 && tid < kMaxList) {
       float l = 0.f;
-      if (!(pk == 0.f)) l = ls == -INFINITY && pk > 0.f ? INFINITY : pk * (logf(pk) - ((zk - all.m) * p.scale - ls));
+      if (ls != ls) l = NAN;   // also where nothing is asked of the row
+      else if (!(pk == 0.f)) l = ls == -INFINITY && pk > 0.f ? INFINITY : pk * (logf(pk) - ((zk - all.m) * p.scale - ls));
       if (TAIL && tid == 0 && !(rest == 0.f)) {   // lr - ls in parts: their products with rest are in range where lr itself is not
         if (ls == -INFINITY && rest > 0.f) l = INFINITY;
         else l += rest * (logf(rest) - ls_off + ls) + rest * p.scale * (all.m - dense.m);

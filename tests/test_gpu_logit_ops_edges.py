@@ -227,3 +227,18 @@ def test_teacher_values_times_teacher_scale_beyond_the_type(tscale):
         dwant[:4] -= p
         close(as64(dz[r]), dwant, 1e-4 * np.abs(dwant) + 3e-5, "dz")
         close(as64(back[r]), dwant, 1e-4 * np.abs(dwant) + 3e-5, "backward")
+
+
+# ------------------------------------------------------------------------------------------------ rows of NaN
+@pytest.mark.parametrize("grad", [True, False])
+def test_a_row_of_nan_gives_a_loss_of_nan_whatever_is_asked(grad):
+    z = torch.zeros(4, 700, device="cuda")
+    z[0, 600], z[1, 600], z[2, 600] = math.nan, math.inf, math.nan
+    ids = torch.tensor([[-1, -1], [3, 5], [3, 600], [-1, -1]], device="cuda")
+    tv = torch.zeros(4, 2, device="cuda")
+    tv[1] = -math.inf                                      # listed, nothing asked
+    dz = torch.empty_like(z) if grad else None
+    loss, _ = run_distill(z, "fp32", ids, tv, False, dz=dz)
+    assert torch.isnan(loss).tolist() == [True, True, True, False] and loss[3].item() == 0
+    if grad:
+        assert bool(torch.isnan(dz[:3]).all()) and bool((dz[3] == 0).all())
