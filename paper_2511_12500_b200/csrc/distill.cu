@@ -573,12 +573,12 @@ template <int DT, bool TAIL, int MODE>
 int launch_distill(const DistillParams& p, cudaStream_t st) {
   const auto kernel = distill_kernel<DT, TAIL, MODE>;
   const int bytes = (MODE == kHeld ? p.hold * 16 : 0) + (p.hold + 3) / 4 * 4;
-  static bool configured[kMaxDevices] = {};
+  static std::atomic<bool> configured[kMaxDevices] = {};   // calls may come from several threads; the setting may be made twice
   int dev = -1;
   IRIS_CUDA_TRY(cudaGetDevice(&dev));
-  if (dev >= kMaxDevices || !configured[dev]) {
+  if (dev >= kMaxDevices || !configured[dev].load(std::memory_order_acquire)) {
     IRIS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldBytes + kHoldBytes / 16));
-    if (dev < kMaxDevices) configured[dev] = true;
+    if (dev < kMaxDevices) configured[dev].store(true, std::memory_order_release);
   }
   if (MODE == kLossOnly) return launch_rows(kernel, p, (unsigned)((int64_t)p.rows * p.split), p.split, kDistillThreads, (size_t)bytes, st);
   // As many clusters as the device holds at a time: one more would run after the others have done all their rows.  The

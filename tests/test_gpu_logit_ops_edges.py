@@ -4,6 +4,7 @@ the type's largest, rows of NaN, 32-bit gradients, graphs.
 Tolerances are those of test_gpu_logit_ops.py unless a test derives its own.
 """
 import math
+from concurrent.futures import ThreadPoolExecutor
 
 import numpy as np
 import pytest
@@ -242,3 +243,30 @@ def test_a_row_of_nan_gives_a_loss_of_nan_whatever_is_asked(grad):
     assert torch.isnan(loss).tolist() == [True, True, True, False] and loss[3].item() == 0
     if grad:
         assert bool(torch.isnan(dz[:3]).all()) and bool((dz[3] == 0).all())
+
+
+# ------------------------------------------------------------------------------------------------ graphs and threads
+@pytest.mark.parametrize("vocab", [700, 9000, 41000])
+def test_calls_from_several_threads(vocab):
+    """Each thread with its own stream and outputs; the first of them sets up the kernels while the others call them."""
+    rows, k, n = 6, 8, 8
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    zs = [torch.randn(rows, vocab, device="cuda", generator=gen).half() for _ in range(n)]
+    ids = [z.float().topk(k, dim=1).indices.contiguous() for z in zs]
+    tv = torch.log_softmax(torch.randn(rows, k, device="cuda", generator=gen), 1).sub(0.1).contiguous()
+    losses, grads = torch.zeros(2, n, rows, device="cuda"), [[torch.zeros_like(z) for z in zs] for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(n)]
+    torch.cuda.synchronize()
+
+    def call(turn, i):
+        for _ in range(20):
+            iris.iris_distill_topk(zs[i], rows, vocab, iris.IRIS_F16, tv, ids[i], k, losses[turn, i], mode=iris.IRIS_DISTILL_TAIL, dlogits=grads[turn][i],
+                                   stream=streams[i])
+
+    with ThreadPoolExecutor(n) as pool:
+        list(pool.map(lambda i: call(0, i), range(n)))
+    torch.cuda.synchronize()
+    for i in range(n):
+        call(1, i)
+    torch.cuda.synchronize()
+    assert torch.equal(losses[0], losses[1]) and all(torch.equal(a, b) for a, b in zip(*grads)) and float(losses.abs().min()) > 0
