@@ -245,7 +245,67 @@ def test_a_row_of_nan_gives_a_loss_of_nan_whatever_is_asked(grad):
         assert bool(torch.isnan(dz[:3]).all()) and bool((dz[3] == 0).all())
 
 
+# ------------------------------------------------------------------------------------------------ 32-bit gradients
+def test_32_bit_gradients_to_a_few_roundings():
+    """Root mean square of relative errors where q > 2^-8, statistics given to half a unit.  The exponent y (|y| < 8, raised by 8: a result below 8)
+    carries the roundings of z - m (< 8), y and the offset (< 4), half units 2^-22, 2^-22 and 2^-23 of 2^y's ln 2, root mean squares 1 / sqrt 3 of that;
+    2^y and three products 2^-22 and 2^-24 likewise: 2e-7 together in the mean.  Exponents near 32 would carry 2^-20: 5e-7."""
+    rng = np.random.default_rng(40)
+    rows, vocab = 60, 2000
+    values = rng.normal(0, 2.5, (rows, vocab))
+    for r in range(rows):
+        values[r, rng.integers(0, vocab, 40)] += 6
+    _, z = strided(values, "fp32")
+    v = as64(z)
+    stats, lqs = zip(*[((m, ls), lq) for m, ls, lq in (ref.log_softmax(x, 1.0) for x in v)])
+    st = torch.tensor(stats, dtype=torch.float32, device="cuda")
+    t = torch.zeros(rows, 1, dtype=torch.int64, device="cuda")
+    dz = torch.empty_like(z)
+    iris.iris_token_logprobs_backward(z, rows, vocab, iris.IRIS_F32, t, 1, st, torch.full((rows, 1), -1.0, device="cuda"), dz)
+    st3 = torch.cat([st, torch.zeros(rows, 1, device="cuda")], 1).contiguous()
+    kd = torch.empty_like(z)
+    iris.iris_distill_topk_backward(z, rows, vocab, iris.IRIS_F32, torch.zeros(rows, 1, device="cuda"), t, 1, st3, torch.ones(rows, device="cuda"), kd)
+    q = np.exp(np.stack(lqs))
+    sel = q > 2.0 ** -8
+    sel[:, 0] = False
+    assert sel.sum() > 500
+    for got in (as64(dz), as64(kd)):
+        assert np.sqrt(np.mean((got[sel] / q[sel] - 1) ** 2)) < 3e-7
+
+
 # ------------------------------------------------------------------------------------------------ graphs and threads
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 3000), ("fp16", 40000), ("fp32", 400003)])
+@pytest.mark.parametrize("tail", [False, True])
+def test_distillation_in_a_cuda_graph(dtype, vocab, tail):
+    rng = np.random.default_rng(41)
+    rows, k = 5, 16
+    _, z = strided(logits_like(rng, rows, vocab), dtype)
+    ids = z.float().topk(k, dim=1).indices.contiguous()
+    tv = torch.log_softmax(torch.randn(rows, k, device="cuda"), 1).sub(0.1).contiguous()
+    w = torch.rand(rows, device="cuda")
+    loss, st, alone = torch.zeros(rows, device="cuda"), torch.zeros(rows, 3, device="cuda"), torch.zeros(rows, device="cuda")
+    dz, back = torch.zeros_like(z), torch.zeros_like(z)
+
+    def calls():
+        where = (z, rows, vocab, iris.LOGIT_DTYPES[dtype], tv, ids, k)
+        iris.iris_distill_topk(*where, loss, mode=int(tail), stats=st, weight=w, dlogits=dz)
+        iris.iris_distill_topk(*where, alone, mode=int(tail))
+        iris.iris_distill_topk_backward(*where, st, w, back, mode=int(tail))
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):                          # the first calls of these sizes: their queries run while the stream is captured
+        calls()
+    graph.replay()
+    torch.cuda.synchronize()
+    got = [x.clone() for x in (loss, st, alone, dz, back)]
+    for x in (loss, st, alone, dz, back):
+        x.zero_()
+    calls()
+    torch.cuda.synchronize()
+    for a, b in zip(got, (loss, st, alone, dz, back)):
+        assert torch.equal(a, b) and float(a.float().abs().max()) > 0
+
+
 @pytest.mark.parametrize("vocab", [700, 9000, 41000])
 def test_calls_from_several_threads(vocab):
     """Each thread with its own stream and outputs; the first of them sets up the kernels while the others call them."""
