@@ -1,4 +1,5 @@
-"""Thin ctypes binding of libiris_b200.so: same names as include/iris_b200.h, argument marshalling only.
+"""Thin ctypes binding of libiris_b200.so: same names as include/iris_b200.h, argument marshalling, and for the operators on
+logits checks of the tensors that they are given.
 
 PyTorch appears here only to obtain device pointers and the current stream.  There is no fallback:
 if the shared library is missing or cannot be loaded, importing a symbol raises.
@@ -8,6 +9,11 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+
+try:
+    from . import _tensors
+except ImportError:
+    _tensors = None   # not built: its checks are made in Python
 
 IRIS_OK = 0
 IRIS_ERR_ARG, IRIS_ERR_RANGE, IRIS_ERR_NOMEM, IRIS_ERR_CUDA = -1, -2, -3, -4
@@ -421,46 +427,126 @@ def iris_gemm_all_scatter_noalloc(A, B_shards, slot_bases, bytes_per_rank, M, N,
 
 # ------------------------------------------------------------------------------------- operators on logits
 # Shapes, types and rules are the header's.  Tensors other than logits and dlogits are contiguous, ids are int64, the
-# rest fp32; row_stride and grad_stride are in elements (0 = vocab).
-def _addr(x) -> int:
-    if x is None:
-        return 0
-    try:
-        return x.data_ptr()
-    except AttributeError:
-        return _ptr(x)
+# rest fp32; row_stride and grad_stride are in elements (0 = vocab).  What is given as a tensor is checked against the
+# sizes of the call: its type, its layout, that it is long enough and that the GPU can read it (IRIS_ERR_ARG).  Addresses are
+# taken as they are.  _accept (csrc/py_tensors.c) passes what is right in the usual way, in half a microsecond; anything else, and everything
+# where that extension is not built or the tensors have no C interface, is looked at by _look.
+_accept = None
+_LOGITS = {}   # dtype -> torch type
+
+
+def _first_call():
+    global _accept
+    import torch
+    _LOGITS.update({IRIS_F16: torch.float16, IRIS_BF16: torch.bfloat16, IRIS_F32: torch.float32})
+    interface = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
+    if _tensors is not None and interface is not None and _tensors.setup(interface, torch.Tensor):
+        _accept = _tensors.addresses
+    else:
+        _accept = _none
+
+
+def _none(*args):
+    return None
+
+
+def _refuse(what, why):
+    raise IrisError(IRIS_ERR_ARG, f"{what} {why}")
+
+
+def _look_at_type(x, dtype, what):
+    if not hasattr(x, "data_ptr"):
+        _refuse(what, f"is a {type(x).__name__}, neither a tensor nor an address")
+    if x.dtype is not dtype:
+        _refuse(what, f"is {x.dtype}, not {dtype}")
+
+
+def _look_at_place(x, what):
+    if not x.is_cuda and not x.is_pinned():
+        _refuse(what, "is not on the GPU")
+
+
+def _look_at_buffer(x, size, count, what):
+    import torch
+    if x is None or isinstance(x, int) or count <= 0:   # nothing is read or written of 0 elements
+        return
+    _look_at_type(x, torch.int64 if size == 8 else torch.float32, what)
+    if not x.is_contiguous():
+        _refuse(what, "is not contiguous")
+    if x.numel() < count:
+        _refuse(what, f"has {x.numel()} elements, the call needs {count}")
+    _look_at_place(x, what)
+
+
+def _look_at_rows(x, rows, vocab, dtype, stride, what):
+    if x is None or isinstance(x, int) or rows <= 0 or vocab <= 0 or dtype not in _LOGITS:   # nothing to read, or refused by the library
+        return
+    _look_at_type(x, _LOGITS[dtype], what)
+    shape, strides = tuple(x.shape), x.stride()
+    if not x.is_contiguous() and vocab > 1 and strides[-1] != 1:
+        _refuse(what, f"has a row's elements {strides[-1]} elements apart")
+    if stride == 0 and rows > 1 and not (x.is_contiguous() and (len(shape) == 1 or shape and shape[-1] == vocab)):
+        _refuse(what, f"of shape {shape}, strides {strides}, has other rows than {rows} of {vocab} one after the other, and the row stride is not given")
+    last = sum((n - 1) * s for n, s in zip(shape, strides)) if x.numel() else -1
+    if (rows - 1) * (stride or vocab) + vocab - 1 > last:
+        _refuse(what, f"of shape {shape}, strides {strides}, does not hold {rows} rows of {vocab}, {stride or vocab} elements apart")
+    _look_at_place(x, what)
+
+
+def _look(names, rows, vocab, dtype, logits, row_stride, dlogits, grad_stride, *buffers):
+    """What _accept does, a question at a time."""
+    _look_at_rows(logits, rows, vocab, dtype, row_stride, "logits")
+    _look_at_rows(dlogits, rows, vocab, dtype, grad_stride, "dlogits")
+    for what, x, size, each in zip(names, buffers[::3], buffers[1::3], buffers[2::3]):
+        _look_at_buffer(x, size, rows * each, what)
+    return [_ptr(x) or 0 for x in (logits, dlogits, *buffers[::3])]
 
 
 def iris_token_logprobs(logits, rows, vocab, dtype, targets=None, n_targets=0, logprob=None, entropy=None, stats=None, top_k=0, top_ids=None,
                         top_logprob=None, scale=1.0, row_stride=0, stream=None):
-    a = _LOGPROB_ARGS.pack(_addr(logits), rows, vocab, row_stride, dtype, scale, _addr(targets), n_targets, top_k, _addr(logprob), _addr(entropy),
-                           _addr(stats), _addr(top_ids), _addr(top_logprob))
-    _ck(lib().iris_token_logprobs(a, _stream(stream)))
+    if _accept is None:
+        _first_call()
+    args = (rows, vocab, dtype, logits, row_stride, None, 0, targets, 8, n_targets, logprob, 4, n_targets, entropy, 4, 1, stats, 4, 2, top_ids, 8, top_k,
+            top_logprob, 4, top_k)
+    z, _, t, lp, en, st, ti, tl = _accept(*args) or _look(("targets", "logprob", "entropy", "stats", "top_ids", "top_logprob"), *args)
+    rc = lib().iris_token_logprobs(_LOGPROB_ARGS.pack(z, rows, vocab, row_stride, dtype, scale, t, n_targets, top_k, lp, en, st, ti, tl), _stream(stream))
+    if rc:
+        _ck(rc)
 
 
 def iris_token_logprobs_backward(logits, rows, vocab, dtype, targets, n_targets, stats, grad_logprob, dlogits, entropy=None, grad_entropy=None,
                                  scale=1.0, row_stride=0, grad_stride=0, stream=None):
-    a = _LOGPROB_GRAD_ARGS.pack(_addr(logits), rows, vocab, row_stride, dtype, scale, _addr(targets), n_targets, _addr(stats), _addr(grad_logprob),
-                                _addr(entropy), _addr(grad_entropy), _addr(dlogits), grad_stride)
-    _ck(lib().iris_token_logprobs_backward(a, _stream(stream)))
+    if _accept is None:
+        _first_call()
+    args = (rows, vocab, dtype, logits, row_stride, dlogits, grad_stride, targets, 8, n_targets, stats, 4, 2, grad_logprob, 4, n_targets, entropy, 4, 1,
+            grad_entropy, 4, 1)
+    z, dz, t, st, g, en, gh = _accept(*args) or _look(("targets", "stats", "grad_logprob", "entropy", "grad_entropy"), *args)
+    rc = lib().iris_token_logprobs_backward(_LOGPROB_GRAD_ARGS.pack(z, rows, vocab, row_stride, dtype, scale, t, n_targets, st, g, en, gh, dz, grad_stride),
+                                            _stream(stream))
+    if rc:
+        _ck(rc)
 
 
-def _distill(fn, logits, rows, vocab, dtype, teacher, teacher_ids, list_k, mode, weight, loss, stats, dlogits, scale, teacher_scale, row_stride,
+def _distill(fn, weight_name, logits, rows, vocab, dtype, teacher, teacher_ids, list_k, mode, weight, loss, stats, dlogits, scale, teacher_scale, row_stride,
              grad_stride, stream):
-    a = _DISTILL_ARGS.pack(_addr(logits), rows, vocab, row_stride, dtype, scale, _addr(teacher), _addr(teacher_ids), list_k, mode, teacher_scale,
-                           _addr(weight), _addr(loss), _addr(stats), _addr(dlogits), grad_stride)
-    _ck(fn(a, _stream(stream)))
+    if _accept is None:
+        _first_call()
+    args = (rows, vocab, dtype, logits, row_stride, dlogits, grad_stride, teacher, 4, list_k, teacher_ids, 8, list_k, weight, 4, 1, loss, 4, 1, stats, 4, 3)
+    z, dz, v, ids, w, lo, st = _accept(*args) or _look(("teacher", "teacher_ids", weight_name, "loss", "stats"), *args)
+    rc = fn(_DISTILL_ARGS.pack(z, rows, vocab, row_stride, dtype, scale, v, ids, list_k, mode, teacher_scale, w, lo, st, dz, grad_stride), _stream(stream))
+    if rc:
+        _ck(rc)
 
 
 def iris_distill_topk(logits, rows, vocab, dtype, teacher, teacher_ids, list_k, loss, mode=IRIS_DISTILL_RENORM, stats=None, weight=None, dlogits=None,
                       scale=1.0, teacher_scale=1.0, row_stride=0, grad_stride=0, stream=None):
     """Loss per row and, with `dlogits`, weight * its gradient, in one pass over the logits."""
-    _distill(lib().iris_distill_topk, logits, rows, vocab, dtype, teacher, teacher_ids, list_k, mode, weight, loss, stats, dlogits, scale, teacher_scale,
-             row_stride, grad_stride, stream)
+    _distill(lib().iris_distill_topk, "weight", logits, rows, vocab, dtype, teacher, teacher_ids, list_k, mode, weight, loss, stats, dlogits, scale,
+             teacher_scale, row_stride, grad_stride, stream)
 
 
 def iris_distill_topk_backward(logits, rows, vocab, dtype, teacher, teacher_ids, list_k, stats, grad_loss, dlogits, mode=IRIS_DISTILL_RENORM,
                                scale=1.0, teacher_scale=1.0, row_stride=0, grad_stride=0, stream=None):
     """grad_loss * the gradient, from the statistics that iris_distill_topk left."""
-    _distill(lib().iris_distill_topk_backward, logits, rows, vocab, dtype, teacher, teacher_ids, list_k, mode, grad_loss, None, stats, dlogits, scale,
-             teacher_scale, row_stride, grad_stride, stream)
+    _distill(lib().iris_distill_topk_backward, "grad_loss", logits, rows, vocab, dtype, teacher, teacher_ids, list_k, mode, grad_loss, None, stats, dlogits,
+             scale, teacher_scale, row_stride, grad_stride, stream)

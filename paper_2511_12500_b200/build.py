@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -13,6 +14,11 @@ SOURCES = ["heap.cu", "tile_ops.cu", "gemm_all_scatter.cu", "consumer.cu", "toke
 HEADERS = ["iris_internal.h", "iris_device.cuh", "sm100_ptx.cuh", "logit_rows.cuh", "logit_grad.cuh", "top_list.cuh"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-O3", "-lineinfo", "-Xcompiler", "-fPIC",
               "-Xptxas", "-v", "--expt-relaxed-constexpr"]
+
+
+# The binding's checks of tensors (a CPython extension; built where Python's headers are, the checks are slower without it).
+EXT_SOURCE = os.path.join(CSRC, "py_tensors.c")
+EXT = os.path.join(PKG, "_tensors" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 
 def _nvcc() -> str:
@@ -42,7 +48,20 @@ def _stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_ext(force: bool = False) -> None:
+    include = sysconfig.get_path("include")
+    if not os.path.exists(os.path.join(include, "Python.h")):
+        print("no Python.h: the binding checks tensors in Python", file=sys.stderr)
+        return
+    if not force and os.path.exists(EXT) and all(os.path.getmtime(f) <= os.path.getmtime(EXT) for f in (EXT_SOURCE, __file__)):
+        return
+    tmp = EXT + f".{os.getpid()}.tmp"
+    subprocess.check_call([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I", include, EXT_SOURCE, "-o", tmp])
+    os.replace(tmp, EXT)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_ext(force)
     if not force and not _stale():
         return LIB
     os.makedirs(os.path.dirname(LIB), exist_ok=True)

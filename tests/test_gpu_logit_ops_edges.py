@@ -12,6 +12,7 @@ import torch
 
 import logit_ref as ref
 import paper_2511_12500_b200 as iris
+from paper_2511_12500_b200 import binding
 from test_gpu_logit_ops import HALF_UNIT, SMALLEST, TORCH, as64, check_score, close, logits_like, run_distill, run_score_grad, score, strided
 
 pytestmark = pytest.mark.gpu
@@ -330,3 +331,41 @@ def test_calls_from_several_threads(vocab):
         call(1, i)
     torch.cuda.synchronize()
     assert torch.equal(losses[0], losses[1]) and all(torch.equal(a, b) for a, b in zip(*grads)) and float(losses.abs().min()) > 0
+
+
+# ------------------------------------------------------------------------------------------------ tensors of a call
+def test_tensors_that_are_right_pass_at_once_and_by_the_slower_look(monkeypatch):
+    """Contiguous, strided, of more dimensions, longer than needed, parameters, addresses: the same answers from the extension and without it."""
+    rng = np.random.default_rng(50)
+    rows, vocab = 6, 500
+    full = torch.from_numpy(rng.normal(0, 2, (rows + 1, vocab + 36)).astype(np.float32)).cuda().bfloat16()
+    view = full[1:, 5:vocab + 5]
+    t = torch.from_numpy(rng.integers(0, vocab, (rows + 2, 2))).cuda()
+    some = view.contiguous()
+    forms = [(view, vocab + 36), (some, 0), (some, vocab), (some.view(2, 3, vocab), 0), (some.view(-1), 0), (some.data_ptr(), 0),
+             (torch.nn.Parameter(some, requires_grad=False), 0), (some.clone().requires_grad_(), 0), (full.view(-1)[vocab + 41:], vocab + 36)]
+    look = binding._look
+    slow = []
+    monkeypatch.setattr(binding, "_look", lambda *a: slow.append(1) or look(*a))
+    for accept in (binding._accept, binding._none):
+        monkeypatch.setattr(binding, "_accept", accept)
+        for z, stride in forms:
+            want = score(view, "bf16", t[:rows], 7, stride=vocab + 36) if stride == vocab + 36 else score(some, "bf16", t[:rows], 7)
+            slow.clear()
+            out = {k: torch.zeros_like(v) for k, v in want.items()}
+            iris.iris_token_logprobs(z, rows, vocab, iris.IRIS_BF16, targets=t, n_targets=2, top_k=7, row_stride=stride, **out)
+            assert all(torch.equal(out[k], want[k]) for k in want)
+            assert len(slow) == (accept is binding._none or type(z) is torch.nn.Parameter)      # a parameter is not of the type itself
+
+
+def test_tensors_that_are_wrong_are_refused_on_the_gpu():
+    rows, vocab = 4, 300
+    z, t = torch.zeros(rows, vocab, device="cuda"), torch.zeros(rows, 1, dtype=torch.int64, device="cuda")
+    st, g, dz = torch.zeros(rows, 2, device="cuda"), torch.ones(rows, 1, device="cuda"), torch.zeros(rows, vocab, device="cuda")
+    one = torch.ones(1, device="cuda").expand(rows, 1)                                   # what autograd hands to the backward of a sum
+    for change in (dict(targets=t.int()), dict(grad_logprob=one), dict(grad_logprob=g[:3]), dict(stats=st.double()), dict(stats=st[:, :1]),
+                   dict(dlogits=dz.half()), dict(dlogits=torch.zeros(rows, vocab + 4, device="cuda")[:, :vocab]), dict(logits=z[:3]), dict(logits=z.cpu())):
+        with pytest.raises(iris.IrisError) as e:
+            iris.iris_token_logprobs_backward(**{**dict(logits=z, rows=rows, vocab=vocab, dtype=iris.IRIS_F32, targets=t, n_targets=1, stats=st, grad_logprob=g,
+                                                        dlogits=dz), **change})
+        assert e.value.code == iris.IRIS_ERR_ARG and next(iter(change)) in str(e.value)
