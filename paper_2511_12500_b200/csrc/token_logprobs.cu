@@ -135,10 +135,10 @@ __global__ void __launch_bounds__(kScoreThreads, TOP == kTopPiecewise ? 5 : 4) s
       if (B <= part.n_int) fetch(0, g);
       for (; b + 3 * B <= part.n_int; b += 2 * B) {
         fetch(b + B, h);
-        sums.template pace<T, U>(b);
         sums.template add<true>(g, largest<DT, true>(g, 0, T));
         fetch(b + 2 * B, g);
         sums.template add<true>(h, largest<DT, true>(h, 0, T));
+        sums.template pace<T, U>(b);
       }
       if (b + 2 * B <= part.n_int) {
         fetch(b + B, h);
