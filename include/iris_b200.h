@@ -480,8 +480,9 @@ int iris_gemm_all_scatter_noalloc(const void* A, const void* const* B_shards, co
  * Common arguments:
  *   logits      row r starts at logits + r * row_stride elements, `vocab` elements each, of type `dtype` (IRIS_F16,
  *               IRIS_BF16 or IRIS_F32).  row_stride in elements, >= vocab; 0 = vocab.  Rows may start at any element
- *               (16-bit logits at any even address); 16-byte aligned rows are the fast case.  Nothing outside a row is
- *               read or written.  rows < 2^31, vocab <= 2^30 (IRIS_ERR_UNSUPPORTED beyond that).
+ *               (16-bit logits at any even address); 16-byte aligned rows are the fast case.  A gradient is fast where its
+ *               rows lie at the same places of 16 bytes as the logits' (equal strides and alignment), and stored element by
+ *               element otherwise, at a quarter of the speed.  Nothing outside a row is read or written.  rows < 2^31, vocab <= 2^30 (IRIS_ERR_UNSUPPORTED beyond that).
  *   scale       > 0, at most 2e38: the softmax is taken of scale * z (1 / temperature).
  *   targets, teacher_ids, top_ids   int64 column indices.
  * Statistics, probabilities and sums are fp32.  -inf logits are masked tokens (probability 0); a mask of the type's

@@ -40,12 +40,12 @@ __device__ __forceinline__ float4* upper_of(TopShared& top, float4*) {
 
 // One cluster of `split` blocks a row; each takes an equal run of granules, and all get what each found.
 //
-// Bound by memory where a row is long and there are many (4096 x 128000 bf16: 174 us, 6.0 TB/s, 92 % of the copy rate; 6.6
-// instructions an element, a third of the issue slots): without alternatives a batch of four granules a thread is fetched
-// while one is summed, in four blocks an SM (178 us without, 194 with five blocks, whose registers spill).  With
-// alternatives five blocks of single batches hide the end of one row, about half of a block's time, behind the others'
-// passes (4096 x 36864 fp16, 64 alternatives: 87 us; four blocks 91).  Short rows are bound by the chain of latencies: load,
-// bound, list, places (1 x 16384: 4.6 us from first to last instruction).
+// Bound by memory where a row is long and there are many (4096 x 128000 bf16: 187 us, 5.6 TB/s, 86 % of the copy rate; 7.0
+// instructions an element, 60 % of the issue slots): without alternatives a batch of four granules a thread is fetched
+// while one is summed, in four blocks an SM (without that 4 to 6 % more; five blocks spill far more registers than the 8 bytes
+// that bf16 with entropy does with four: 194 us).  With alternatives five blocks of single batches hide the end of one row, about half of a
+// block's time, behind the others' passes (4096 x 36864 fp16, 64 alternatives: 86 us; four blocks 91).  Short rows are bound by the
+// chain of latencies: load, bound, list, places (1 x 16384: 4.6 us from first to last instruction).
 //
 // TOP: no alternatives; alternatives of a part of any length, of which pieces are read again; of a part of at most
 // kOneBatch granules, which stays in registers.
