@@ -409,12 +409,12 @@ __global__ void __launch_bounds__(kDistillThreads, MODE == kLossOnly ? kLossBloc
       }
     }
     if (rank == 0 && tid < kMaxList) {
-      float l = 0.f;
+      float l = 0.f;   // log probabilities in parts: their products with p are in range where a mask's own is not
       if (ls != ls) l = NAN;   // also where nothing is asked of the row
-      else if (!(pk == 0.f)) l = ls == -INFINITY && pk > 0.f ? INFINITY : pk * (logf(pk) - ((zk - all.m) * p.scale - ls));
-      if (TAIL && tid == 0 && !(rest == 0.f)) {   // lr - ls in parts: their products with rest are in range where lr itself is not
+      else if (!(pk == 0.f)) l = ls == -INFINITY && pk > 0.f ? INFINITY : pk * (logf(pk) + ls) + pk * (all.m - zk) * p.scale;
+      if (TAIL && tid == 0 && !(rest == 0.f)) {
         if (ls == -INFINITY && rest > 0.f) l = INFINITY;
-        else l += rest * (logf(rest) - ls_off + ls) + rest * p.scale * (all.m - dense.m);
+        else l += rest * (logf(rest) - ls_off + ls) + rest * (all.m - dense.m) * p.scale;
       }
 #pragma unroll
       for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);

@@ -231,6 +231,28 @@ def test_teacher_values_times_teacher_scale_beyond_the_type(tscale):
         close(as64(back[r]), dwant, 1e-4 * np.abs(dwant) + 3e-5, "backward")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tail", [False, True])
+def test_listed_tokens_masked_by_the_lowest_value(dtype, tail):
+    """p times a log probability of -4.8e38 is in range where p is 0.1."""
+    scale, low = 1 / 0.7, float(torch.finfo(TORCH[dtype]).min)
+    rng = np.random.default_rng(60)
+    values = rng.normal(0, 1, (2, 400))
+    values[:, [7, 9]] = low
+    _, z = strided(values, dtype)
+    v = as64(z)
+    ids = np.array([[1, 2, 7, 9]] * 2)
+    p = np.array([0.5, 0.3, 0.1, 0.05])
+    tv = np.log(p).astype(np.float32)[None].repeat(2, 0)
+    dz = torch.empty_like(z)
+    loss, st = run_distill(z, dtype, torch.from_numpy(ids).cuda(), torch.from_numpy(tv).cuda(), tail, scale, 1.0, dz=dz)
+    for r in range(2):
+        want, dwant, size, dsize, _ = ref.distill(v[r], scale, ids[r], tv[r], 1.0, tail)
+        assert 1e37 < want < 3e38
+        close(loss[r].item(), want, 1e-5 * size, "loss")
+        close(as64(dz[r]), dwant, HALF_UNIT[dtype] * np.abs(dwant) + 3e-5 * dsize + SMALLEST[dtype], "dz")
+
+
 # ------------------------------------------------------------------------------------------------ rows of NaN
 @pytest.mark.parametrize("grad", [True, False])
 def test_a_row_of_nan_gives_a_loss_of_nan_whatever_is_asked(grad):
