@@ -7,13 +7,9 @@ if the shared library is missing or cannot be loaded, importing a symbol raises.
 from __future__ import annotations
 
 import ctypes as C
+import importlib
 import os
 import struct
-
-try:
-    from . import _tensors
-except ImportError:
-    _tensors = None   # not built: its checks are made in Python
 
 IRIS_OK = 0
 IRIS_ERR_ARG, IRIS_ERR_RANGE, IRIS_ERR_NOMEM, IRIS_ERR_CUDA = -1, -2, -3, -4
@@ -440,10 +436,14 @@ def _first_call():
     import torch
     _LOGITS.update({IRIS_F16: torch.float16, IRIS_BF16: torch.bfloat16, IRIS_F32: torch.float32})
     interface = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
-    if _tensors is not None and interface is not None and _tensors.setup(interface, torch.Tensor):
+    _accept = _none
+    importlib.invalidate_caches()   # it may have been built since this process began
+    try:
+        from . import _tensors
+    except ImportError:
+        return
+    if interface is not None and _tensors.setup(interface, torch.Tensor):
         _accept = _tensors.addresses
-    else:
-        _accept = _none
 
 
 def _none(*args):
