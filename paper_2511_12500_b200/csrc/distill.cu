@@ -163,13 +163,13 @@ struct Edge {
 //   kReadTwice  The gradient of a part too large for shared memory.
 // A byte a granule (on_list) says which of its tokens are on the list: with a remainder they leave the sum.
 //
-// What bounds it: 8192 x 28672 bf16 with 64 teacher's tokens takes 192 us, 4.9 TB/s read and written, 75 % of the copy rate;
+// What bounds it: 8192 x 28672 bf16 with 64 teacher's tokens takes 193 us, 4.9 TB/s read and written, 74 % of the copy rate;
 // 2 exponentials an element keep the special function unit 60 % busy and 12.7 instructions an element the issue slots 50 %.
 // Without its loads and stores the kernel takes 170 us, without its arithmetic 175: three rows in an SM do not overlap them
 // better.  Blocks of 128 threads: what a row costs besides its elements is 670 instructions a warp, so few warps (256
 // threads: 195 us), with four blocks' worth of registers; rows of one block up to 60 KB (two blocks of 28 KB: 236 us), as
 // many clusters as fit at once (one wave more, as an SM count would give for clusters of four, is twice the time).
-// 4096 x 128000 with remainder, clusters of five: 452 us, 71 %; about 2 us of a row's 12 wait for the exchange.
+// 4096 x 128000 with remainder, clusters of five: 455 us, 70 %; about 2 us of a row's 12 wait for the exchange.
 // The loss alone streams: 1024 x 50021 fp32 with remainder 37 us, 85 %; 4096 x 36864 bf16 54 us renormalised, 60 with remainder (86 and 77 %).  Of its
 // eight blocks an SM only fp32 renormalised spills registers (84 bytes; 36 us, 86 %).
 template <int DT, bool TAIL, int MODE>

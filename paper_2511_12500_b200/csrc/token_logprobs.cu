@@ -40,7 +40,7 @@ __device__ __forceinline__ float4* upper_of(TopShared& top, float4*) {
 
 // One cluster of `split` blocks a row; each takes an equal run of granules, and all get what each found.
 //
-// Bound by memory where a row is long and there are many (4096 x 128000 bf16: 187 us, 5.6 TB/s, 86 % of the copy rate; 7.0
+// Bound by memory where a row is long and there are many (4096 x 128000 bf16: 189 us, 5.5 TB/s, 85 % of the copy rate; 7.0
 // instructions an element, 60 % of the issue slots): without alternatives a batch of four granules a thread is fetched
 // while one is summed, in four blocks an SM (without that 4 to 6 % more; five blocks spill far more registers than the 8 bytes
 // that bf16 with entropy does with four: 194 us).  With alternatives five blocks of single batches hide the end of one row, about half of a
