@@ -568,6 +568,115 @@ int iris_distill_topk(const iris_distill_args* args, void* stream);
  * used. */
 int iris_distill_topk_backward(const iris_distill_args* args, void* stream);
 
+/* Verification of drafted tokens (speculative sampling).  Each sequence has `drafts` drafted tokens and drafts + 1 rows of target logits: row
+ * b * (drafts + 1) + i is the distribution p_i of the token at place i, given the drafts before it.  q_i = softmax of draft_logits' row
+ * b * drafts + i, with the same scale; without draft_logits a drafted token was certain (q_i = 1 there).
+ *   Draft i is accepted while u_i q_i(d_i) < p_i(d_i).  At the first place where it is not, the next token is drawn from max(0, p_i - q_i)
+ *   (from p_i where that leaves nothing), behind the last draft from p.  A sequence's drafts end at the first id outside [0, vocab).
+ * Tokens drawn this way are distributed as if the target alone had drawn them.  Drawn by a race: the token with the largest weight / noise, the
+ * lowest column among equals, so that with exponential noise (-ln of a uniform number) a token has its weight's probability.
+ * A scale of +inf, or above 2e38, is greedy: p is 1 at the largest logit (the lowest column among equals), drafts are compared with it, and
+ * uniform, noise and draft_logits are not read.  A row of target logits with nothing left, or with NaN or +inf, accepts nothing and its next token is
+ * -1; a row of draft logits with NaN or +inf rejects its draft, and the next token is drawn from p. */
+typedef struct iris_verify_args {
+  const void* logits;        /* [sequences * (drafts + 1)] rows: see "Common arguments"                              */
+  int64_t sequences, vocab, row_stride;
+  int drafts;                /* 0 .. 128; 0 draws a token for each row                                               */
+  int dtype;                 /* of logits and draft_logits                                                           */
+  float scale;               /* > 0, +inf for greedy                                                                 */
+  const float* scales;       /* [sequences]: a scale for each sequence instead; NULL = scale.  One that is not > 0 is as a row of NaN */
+  const void* draft_logits;  /* [sequences * drafts] rows, or NULL                                                   */
+  int64_t draft_stride;      /* 0 = vocab                                                                            */
+  const int64_t* draft_ids;  /* [sequences, drafts]                                                                  */
+  const float* uniform;      /* [sequences, drafts]: uniform random numbers in [0, 1)                                */
+  const float* noise;        /* [sequences, vocab]: exponential random numbers; one that is not > 0 never wins, but 0 against weight > 0 */
+  int64_t* tokens;           /* [sequences, drafts + 1]: the accepted drafts, the next token, -1 behind it           */
+  int64_t* accepted;         /* [sequences]: how many drafts                                                         */
+  float* logprob;            /* [sequences, drafts + 1]: ln p of `tokens` (0 where greedy, and for -1); may be NULL  */
+  void* workspace;           /* iris_verify_workspace_bytes(sequences, drafts) bytes, 16-byte aligned (see below)    */
+  size_t workspace_bytes;
+} iris_verify_args;
+int iris_verify_drafts(const iris_verify_args* args, void* stream);
+size_t iris_verify_workspace_bytes(int64_t sequences, int drafts);
+
+/* ------------------------------------------------------------------------------------------ */
+/* In front of the head: embedding lookup and layer norm                                       */
+/* ------------------------------------------------------------------------------------------ */
+
+/* What the operators on logits say of scheduling, streams and errors holds here too: nothing is allocated, the order of a stream is what it always
+ * is, calls may be captured in a CUDA graph, the same call on the same inputs gives the same bits, sums are fp32.
+ * Workspaces: device memory of the caller's whose contents neither have to be prepared nor are of use afterwards.  Calls that may
+ * run at the same time (on different streams, in graphs that are replayed at the same time) need one each.
+ * Rows: row r starts at its matrix + r * stride elements of type `dtype` (IRIS_F16, IRIS_BF16, IRIS_F32); strides are in elements, 0 = rows one after the
+ * other.  Rows may start at any element; nothing outside a row is read or written. */
+
+/* Embedding lookup: out row i = scale * table row tokens[i], rounded once.  The table is cut by rows into `world` shards of vocab / world rows: the
+ * B shards of gemm_all_scatter are such a table (tied embeddings), in this process's memory or mapped from another's.
+ * A token outside [0, vocab) gives a row of 0, and so does one whose shard is NULL (a process that has its own shard only: the sum of
+ * all processes' rows is then the lookup). */
+typedef struct iris_embed_args {
+  const void* shards[IRIS_MAX_WORLD]; /* device pointers; [vocab / world, dim] each                       */
+  int world, dtype;                   /* vocab % world == 0                                               */
+  int64_t vocab, dim, shard_stride;   /* vocab <= 2^30, dim <= 2^24 (IRIS_ERR_UNSUPPORTED beyond that)    */
+  const int64_t* tokens;              /* [n]                                                              */
+  int64_t n;                          /* < 2^31                                                           */
+  void* out;                          /* [n, dim]                                                         */
+  int64_t out_stride;
+  float scale;
+} iris_embed_args;
+int iris_embed_tokens(const iris_embed_args* args, void* stream);
+
+/* Its gradient for the table: row v = scale * sum of the rows i of grad_out with tokens[i] = v, summed in the order of the places whatever the
+ * scheduling, in fp32, and rounded once to grad_dtype (dtype or IRIS_F32).  accumulate == 0 writes every row of every shard (0 where no token
+ * names it); otherwise the sums are added to the rows that tokens name, and the others are not touched.  A NULL shard and its tokens are
+ * left out.  The shards must not overlap grad_out or one another. */
+typedef struct iris_embed_grad_args {
+  const void* grad_out;                /* [n, dim] of dtype                                               */
+  int64_t n, dim, grad_out_stride;
+  int dtype, grad_dtype;
+  const int64_t* tokens;
+  void* grad_shards[IRIS_MAX_WORLD];   /* [vocab / world, dim] each, of grad_dtype                        */
+  int world, accumulate;
+  int64_t vocab, shard_stride;
+  float scale;
+  void* workspace;                     /* iris_embed_workspace_bytes(n, vocab, dim) bytes, 16-byte aligned */
+  size_t workspace_bytes;
+} iris_embed_grad_args;
+int iris_embed_tokens_backward(const iris_embed_grad_args* args, void* stream);
+size_t iris_embed_workspace_bytes(int64_t n, int64_t vocab, int64_t dim);
+
+/* Layer norm: y = (x - mean) / sqrt(var + eps) * weight + bias over each row of `dim` elements (1 <= dim <= 65536, IRIS_ERR_UNSUPPORTED beyond
+ * that), var the mean of (x - mean)^2.  y may be x itself (same address and stride) and must not overlap it otherwise.  A row that holds NaN or an
+ * infinity gives NaN; so does one of equal values with eps = 0. */
+typedef struct iris_layer_norm_args {
+  const void* x;
+  int64_t rows, dim, row_stride;
+  int dtype, param_dtype;      /* param_dtype: of weight and bias; dtype or IRIS_F32                       */
+  const void *weight, *bias;   /* [dim]; NULL = 1, NULL = 0                                                */
+  void* y;
+  int64_t out_stride;
+  float* stats;                /* [rows, 2]: mean, 1 / sqrt(var + eps): what the backward call needs; may be NULL */
+  float eps;                   /* >= 0                                                                     */
+} iris_layer_norm_args;
+int iris_layer_norm(const iris_layer_norm_args* args, void* stream);
+
+/* Gradients from dy.  dx may be x or dy itself (same address and stride) and must not overlap them otherwise.  dweight and dbias are sums over all
+ * rows, of param_dtype, written, not added to. */
+typedef struct iris_layer_norm_grad_args {
+  const void *x, *dy;
+  int64_t rows, dim, row_stride, dy_stride;
+  int dtype, param_dtype;
+  const void* weight;          /* as in the forward call                                                   */
+  const float* stats;          /* [rows, 2] of the forward call                                            */
+  void* dx;                    /* NULL = not wanted                                                        */
+  int64_t dx_stride;
+  void *dweight, *dbias;       /* NULL = not wanted                                                        */
+  void* workspace;             /* iris_layer_norm_workspace_bytes(rows, dim) bytes, 16-byte aligned; not needed without dweight and dbias */
+  size_t workspace_bytes;
+} iris_layer_norm_grad_args;
+int iris_layer_norm_backward(const iris_layer_norm_grad_args* args, void* stream);
+size_t iris_layer_norm_workspace_bytes(int64_t rows, int64_t dim);
+
 #ifdef __cplusplus
 }
 #endif

@@ -42,6 +42,8 @@ EXPORTS = [
     "iris_gemm_all_scatter_noalloc", "iris_heap_create_from_bases", "iris_heap_local_rank", "iris_ipc_alloc", "iris_ipc_free", "iris_ipc_export",
     "iris_ipc_open", "iris_ipc_close", "iris_atomic_add_u64", "iris_atomic_cas_u64", "iris_copy_tile", "iris_load_tile", "iris_store_tile", "iris_atomic_rmw",
     "iris_token_logprobs", "iris_token_logprobs_backward", "iris_distill_topk", "iris_distill_topk_backward",
+    "iris_verify_drafts", "iris_verify_workspace_bytes", "iris_embed_tokens", "iris_embed_tokens_backward", "iris_embed_workspace_bytes",
+    "iris_layer_norm", "iris_layer_norm_backward", "iris_layer_norm_workspace_bytes",
 ]
 
 
@@ -67,6 +69,12 @@ class GemmArgs(C.Structure):
 _LOGPROB_ARGS = struct.Struct("@PqqqifPiiPPPPP")
 _LOGPROB_GRAD_ARGS = struct.Struct("@PqqqifPiPPPPPq")
 _DISTILL_ARGS = struct.Struct("@PqqqifPPiifPPPPq")
+# And of those around the head (N size_t).
+_VERIFY_ARGS = struct.Struct("@PqqqiifPPqPPPPPPPN")
+_EMBED_ARGS = struct.Struct("@8PiiqqqPqPqf0q")
+_EMBED_GRAD_ARGS = struct.Struct("@PqqqiiP8PiiqqfPN")
+_LAYER_NORM_ARGS = struct.Struct("@PqqqiiPPPqPf0q")
+_LAYER_NORM_GRAD_ARGS = struct.Struct("@PPqqqqiiPPPqPPPN")
 
 
 _lib = None
@@ -136,6 +144,12 @@ def lib() -> C.CDLL:
     L.iris_gemm_all_scatter_noalloc.argtypes = [vp, C.POINTER(vp), C.POINTER(u64), sz, ci, ci, ci, ci, ci, u64, u64, i32, vp]
     for f in (L.iris_token_logprobs, L.iris_token_logprobs_backward, L.iris_distill_topk, L.iris_distill_topk_backward):
         f.argtypes = [C.c_char_p, vp]   # a packed argument block
+    for f in (L.iris_verify_drafts, L.iris_embed_tokens, L.iris_embed_tokens_backward, L.iris_layer_norm, L.iris_layer_norm_backward):
+        f.argtypes = [C.c_char_p, vp]
+    i64 = C.c_int64
+    L.iris_verify_workspace_bytes.argtypes, L.iris_verify_workspace_bytes.restype = [i64, ci], sz
+    L.iris_embed_workspace_bytes.argtypes, L.iris_embed_workspace_bytes.restype = [i64, i64, i64], sz
+    L.iris_layer_norm_workspace_bytes.argtypes, L.iris_layer_norm_workspace_bytes.restype = [i64, i64], sz
     _lib = L
     return L
 
@@ -427,23 +441,23 @@ def iris_gemm_all_scatter_noalloc(A, B_shards, slot_bases, bytes_per_rank, M, N,
 # sizes of the call: its type, its layout, that it is long enough and that the GPU can read it (IRIS_ERR_ARG).  Addresses are
 # taken as they are.  _accept (csrc/py_tensors.c) passes what is right in the usual way, in half a microsecond; anything else, and everything
 # where that extension is not built or the tensors have no C interface, is looked at by _look.
-_accept = None
+_accept = _accept_rows = None
 _LOGITS = {}   # dtype -> torch type
 
 
 def _first_call():
-    global _accept
+    global _accept, _accept_rows
     import torch
     _LOGITS.update({IRIS_F16: torch.float16, IRIS_BF16: torch.bfloat16, IRIS_F32: torch.float32})
     interface = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
-    _accept = _none
+    _accept = _accept_rows = _none
     importlib.invalidate_caches()   # it may have been built since this process began
     try:
         from . import _tensors
     except ImportError:
         return
     if interface is not None and _tensors.setup(interface, torch.Tensor):
-        _accept = _tensors.addresses
+        _accept, _accept_rows = _tensors.addresses, _tensors.rows
 
 
 def _none(*args):
@@ -550,3 +564,145 @@ def iris_distill_topk_backward(logits, rows, vocab, dtype, teacher, teacher_ids,
     """grad_loss * the gradient, from the statistics that iris_distill_topk left."""
     _distill(lib().iris_distill_topk_backward, "grad_loss", logits, rows, vocab, dtype, teacher, teacher_ids, list_k, mode, grad_loss, None, stats, dlogits,
              scale, teacher_scale, row_stride, grad_stride, stream)
+
+
+# ------------------------------------------------------------------------------------- around the head
+# Shapes, types and rules are the header's; strides are in elements (0: the rows lie one after the other).  Vectors, ids, statistics and random numbers are
+# contiguous.  Tensors are checked as above, and they have to be on the current device.  `workspace` is a contiguous tensor of bytes (torch.uint8).
+_INT64, _BYTES = 3, 4
+_BUFFER = -1
+
+
+def _device():
+    import torch
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else 0   # no tensor is on a GPU before that
+
+
+def _look_at_rows_of(x, kind, rows, columns, stride, what):
+    """What _accept_rows does, a question at a time."""
+    import torch
+    if x is None or isinstance(x, int) or rows <= 0 or columns <= 0:
+        return
+    kinds = {IRIS_F16: torch.float16, IRIS_BF16: torch.bfloat16, IRIS_F32: torch.float32, _INT64: torch.int64, _BYTES: torch.uint8}
+    if kind not in kinds:   # refused by the library
+        return
+    _look_at_type(x, kinds[kind], what)
+    shape, strides = tuple(x.shape), x.stride()
+    if stride == _BUFFER:
+        if not x.is_contiguous():
+            _refuse(what, "is not contiguous")
+        if x.numel() < rows * columns:
+            _refuse(what, f"has {x.numel()} elements, the call needs {rows * columns}")
+    else:
+        if not x.is_contiguous() and columns > 1 and strides[-1] != 1:
+            _refuse(what, f"has a row's elements {strides[-1]} elements apart")
+        if stride == 0 and rows > 1 and not (x.is_contiguous() and (len(shape) == 1 or shape and shape[-1] == columns)):
+            _refuse(what, f"of shape {shape}, strides {strides}, has other rows than {rows} of {columns} one after the other, and the row stride is not given")
+        last = sum((n - 1) * s for n, s in zip(shape, strides)) if x.numel() else -1
+        if (rows - 1) * (stride or columns) + columns - 1 > last:
+            _refuse(what, f"of shape {shape}, strides {strides}, does not hold {rows} rows of {columns}, {stride or columns} elements apart")
+    _look_at_place(x, what)
+    if x.is_cuda and x.device.index != _device():
+        _refuse(what, f"is on {x.device}, not on the current device")
+
+
+def _rows(names, *specs):
+    if _accept is None:
+        _first_call()
+    at = _accept_rows(_device(), *specs)
+    if at is None:
+        for i, what in enumerate(names):
+            _look_at_rows_of(*specs[5 * i: 5 * i + 5], what)
+        at = [_ptr(x) or 0 for x in specs[::5]]
+    return at
+
+
+def _size_of(workspace):
+    """Bytes of a workspace.  (An address says nothing of its size: the caller vouches for it.)"""
+    return 0 if workspace is None else (1 << 62) if isinstance(workspace, int) else workspace.numel() if hasattr(workspace, "numel") else 0
+
+
+def iris_verify_workspace_bytes(sequences, drafts):
+    return lib().iris_verify_workspace_bytes(sequences, drafts)
+
+
+def iris_verify_drafts(logits, sequences, drafts, vocab, dtype, draft_ids, uniform, noise, tokens, accepted, workspace, draft_logits=None, logprob=None,
+                       scale=1.0, scales=None, row_stride=0, draft_stride=0, stream=None):
+    """Accepts drafted tokens and draws the next one (see the header)."""
+    size = _size_of(workspace)
+    z, q, ids, u, e, t, a, lp, s, w = _rows(
+        ("logits", "draft_logits", "draft_ids", "uniform", "noise", "tokens", "accepted", "logprob", "scales", "workspace"),
+        logits, dtype, sequences * (drafts + 1), vocab, row_stride, draft_logits, dtype, sequences * drafts, vocab, draft_stride,
+        draft_ids, _INT64, sequences, drafts, _BUFFER, uniform, IRIS_F32, sequences, drafts, _BUFFER, noise, IRIS_F32, sequences, vocab, _BUFFER,
+        tokens, _INT64, sequences, drafts + 1, _BUFFER, accepted, _INT64, sequences, 1, _BUFFER, logprob, IRIS_F32, sequences, drafts + 1, _BUFFER,
+        scales, IRIS_F32, sequences, 1, _BUFFER, workspace, _BYTES, 1, size, _BUFFER)
+    rc = lib().iris_verify_drafts(_VERIFY_ARGS.pack(z, sequences, vocab, row_stride, drafts, dtype, scale, s, q, draft_stride, ids, u, e, t, a, lp, w, size),
+                                  _stream(stream))
+    if rc:
+        _ck(rc)
+
+
+_NO_SHARDS = [(0,) * i for i in range(IRIS_MAX_WORLD + 1)]
+
+
+def _world(shards):
+    if not 1 <= len(shards) <= IRIS_MAX_WORLD:
+        raise IrisError(IRIS_ERR_ARG, f"world={len(shards)} not in [1, {IRIS_MAX_WORLD}]")
+    return len(shards)
+
+
+def iris_embed_tokens(shards, vocab, dim, dtype, tokens, n, out, scale=1.0, shard_stride=0, out_stride=0, stream=None):
+    """out[i] = scale * the table's row tokens[i]; shards: the table's rows in equal parts, one after the other (None: not here)."""
+    world = _world(shards)
+    specs = []
+    for x in shards:
+        specs += (x, dtype, vocab // world, dim, shard_stride)
+    t, o, *at = _rows(("tokens", "out") + ("shard",) * world, tokens, _INT64, n, 1, _BUFFER, out, dtype, n, dim, out_stride, *specs)
+    rc = lib().iris_embed_tokens(_EMBED_ARGS.pack(*at, *_NO_SHARDS[IRIS_MAX_WORLD - world], world, dtype, vocab, dim, shard_stride, t, n, o, out_stride, scale),
+                                 _stream(stream))
+    if rc:
+        _ck(rc)
+
+
+def iris_embed_workspace_bytes(n, vocab, dim):
+    return lib().iris_embed_workspace_bytes(n, vocab, dim)
+
+
+def iris_embed_tokens_backward(grad_out, n, dim, dtype, tokens, grad_shards, vocab, grad_dtype, workspace, scale=1.0, accumulate=False, grad_out_stride=0,
+                               shard_stride=0, stream=None):
+    """The table's gradient, into shards of its own layout."""
+    world, size = _world(grad_shards), _size_of(workspace)
+    specs = []
+    for x in grad_shards:
+        specs += (x, grad_dtype, vocab // world, dim, shard_stride)
+    t, g, w, *at = _rows(("tokens", "grad_out", "workspace") + ("grad_shard",) * world, tokens, _INT64, n, 1, _BUFFER,
+                         grad_out, dtype, n, dim, grad_out_stride, workspace, _BYTES, 1, size, _BUFFER, *specs)
+    rc = lib().iris_embed_tokens_backward(_EMBED_GRAD_ARGS.pack(g, n, dim, grad_out_stride, dtype, grad_dtype, t, *at, *_NO_SHARDS[IRIS_MAX_WORLD - world], world,
+                                                                bool(accumulate), vocab, shard_stride, scale, w, size), _stream(stream))
+    if rc:
+        _ck(rc)
+
+
+def iris_layer_norm(x, rows, dim, dtype, y, weight=None, bias=None, param_dtype=IRIS_F32, stats=None, eps=1e-5, row_stride=0, out_stride=0, stream=None):
+    a, o, w, b, s = _rows(("x", "y", "weight", "bias", "stats"), x, dtype, rows, dim, row_stride, y, dtype, rows, dim, out_stride,
+                          weight, param_dtype, 1, dim, _BUFFER, bias, param_dtype, 1, dim, _BUFFER, stats, IRIS_F32, rows, 2, _BUFFER)
+    rc = lib().iris_layer_norm(_LAYER_NORM_ARGS.pack(a, rows, dim, row_stride, dtype, param_dtype, w, b, o, out_stride, s, eps), _stream(stream))
+    if rc:
+        _ck(rc)
+
+
+def iris_layer_norm_workspace_bytes(rows, dim):
+    return lib().iris_layer_norm_workspace_bytes(rows, dim)
+
+
+def iris_layer_norm_backward(x, rows, dim, dtype, dy, stats, workspace=None, weight=None, param_dtype=IRIS_F32, dx=None, dweight=None, dbias=None, row_stride=0,
+                             dy_stride=0, dx_stride=0, stream=None):
+    size = _size_of(workspace)
+    a, g, d, w, dw, db, s, ws = _rows(("x", "dy", "dx", "weight", "dweight", "dbias", "stats", "workspace"), x, dtype, rows, dim, row_stride,
+                                      dy, dtype, rows, dim, dy_stride, dx, dtype, rows, dim, dx_stride, weight, param_dtype, 1, dim, _BUFFER,
+                                      dweight, param_dtype, 1, dim, _BUFFER, dbias, param_dtype, 1, dim, _BUFFER, stats, IRIS_F32, rows, 2, _BUFFER,
+                                      workspace, _BYTES, 1, size, _BUFFER)
+    rc = lib().iris_layer_norm_backward(_LAYER_NORM_GRAD_ARGS.pack(a, g, rows, dim, row_stride, dy_stride, dtype, param_dtype, w, s, d, dx_stride, dw, db, ws, size),
+                                        _stream(stream))
+    if rc:
+        _ck(rc)

@@ -537,19 +537,23 @@ inline int check_aligned(const char* fn, const char* what, const void* p, size_t
   if (reinterpret_cast<uintptr_t>(p) % a) return fail(IRIS_ERR_ARG, "%s: %s is not %zu-byte aligned", fn, what, a);
   return IRIS_OK;
 }
-// The gradient may be the logits themselves (same address and stride) or share no element with them.
-inline int check_in_place(const char* fn, const void* logits, int64_t stride, const void* grad, int64_t gstride, int64_t rows, int64_t vocab, int dtype) {
-  if (rows == 0 || vocab == 0) return IRIS_OK;
+// `out` may be `in` itself (same address and stride) or share no element with it.
+inline int check_overlap(const char* fn, const char* out_name, const char* in_name, const void* in, int64_t stride, const void* out, int64_t ostride,
+                         int64_t rows, int64_t columns, int dtype) {
+  if (rows == 0 || columns == 0) return IRIS_OK;
   const size_t es = elem_size(dtype);
-  const uint64_t a = reinterpret_cast<uint64_t>(logits), b = reinterpret_cast<uint64_t>(grad);
-  if (a == b && (stride == gstride || rows == 1)) return IRIS_OK;
-  const uint64_t row = vocab * es, ea = a + (uint64_t)(rows - 1) * stride * es + row, eb = b + (uint64_t)(rows - 1) * gstride * es + row;
+  const uint64_t a = reinterpret_cast<uint64_t>(in), b = reinterpret_cast<uint64_t>(out);
+  if (a == b && (stride == ostride || rows == 1)) return IRIS_OK;
+  const uint64_t row = columns * es, ea = a + (uint64_t)(rows - 1) * stride * es + row, eb = b + (uint64_t)(rows - 1) * ostride * es + row;
   if (ea <= b || eb <= a) return IRIS_OK;
-  if (stride == gstride && rows > 1) {   // two column ranges of one matrix
+  if (stride == ostride && rows > 1) {   // two column ranges of one matrix
     const uint64_t s = stride * es, d = (a < b ? b - a : a - b) % s;
     if (d >= row && s - d >= row) return IRIS_OK;
   }
-  return fail(IRIS_ERR_ARG, "%s: dlogits overlaps logits and is not the same matrix", fn);
+  return fail(IRIS_ERR_ARG, "%s: %s overlaps %s and is not the same matrix", fn, out_name, in_name);
+}
+inline int check_in_place(const char* fn, const void* logits, int64_t stride, const void* grad, int64_t gstride, int64_t rows, int64_t vocab, int dtype) {
+  return check_overlap(fn, "dlogits", "logits", logits, stride, grad, gstride, rows, vocab, dtype);
 }
 // Launches clusters of `split` blocks.  A kernel may begin while the one before it in the stream ends (it waits for that
 // one before it reads anything): a decoding step's calls are about as long as the gap between two launches.
@@ -574,9 +578,9 @@ inline int launch_rows(void (*kernel)(P), const P& p, unsigned blocks, int split
   }
   return IRIS_OK;
 }
-#define IRIS_CHECK(expr)              \
-  do {                                \
-    if (int rc_ = (expr)) return rc_; \
+#define IRIS_CHECK(...)                      \
+  do {                                       \
+    if (int rc_ = (__VA_ARGS__)) return rc_; \
   } while (0)
 
 }  // namespace rows

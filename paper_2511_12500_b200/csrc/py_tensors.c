@@ -29,7 +29,7 @@ typedef struct {
   int (*describe)(void* tensor, Description* out);
   void* current_stream;
 } Exchange;
-enum { ON_GPU = 2, PINNED_HOST = 3, MANAGED = 13, INTEGER = 0, FLOATING = 2, BFLOAT = 4 };
+enum { ON_GPU = 2, PINNED_HOST = 3, MANAGED = 13, INTEGER = 0, UNSIGNED = 1, FLOATING = 2, BFLOAT = 4 };
 
 static const Exchange* exchange;
 static PyTypeObject* tensor_type;
@@ -153,8 +153,73 @@ again:
   Py_RETURN_NONE;
 }
 
+/* Elements of kind 0 .. 4: fp16, bf16, fp32, int64, bytes. */
+static int of_kind(const Description* t, long long kind) {
+  static const struct {
+    uint8_t code, bits;
+  } kinds[] = {{FLOATING, 16}, {BFLOAT, 16}, {FLOATING, 32}, {INTEGER, 64}, {UNSIGNED, 8}};
+  return kind >= 0 && kind <= 4 && t->type_code == kinds[kind].code && t->type_bits == kinds[kind].bits && t->type_lanes == 1;
+}
+
+/* rows(device, {tensor, kind, rows, columns, stride} ...) -> the addresses (0 for None), or None: look again.  Each is a matrix of rows `stride`
+ * elements apart (0: the tensor's own rows, one after the other; -1: a contiguous buffer of rows * columns elements).  Tensors are on GPU `device`
+ * or in pinned or managed memory. */
+static PyObject* rows(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  unsigned long long at[40];
+  Py_ssize_t k = 0;
+  if (!exchange || n < 1 || (n - 1) % 5 || (n - 1) / 5 > 40) Py_RETURN_NONE;
+  const long long device = PyLong_AsLongLong(args[0]);
+  for (Py_ssize_t i = 1; i < n; i += 5, ++k) {
+    Description t;
+    int is_tensor;
+    int64_t count;
+    long long v[4];
+    if (!address(args[i], &at[k], &t, &is_tensor)) Py_RETURN_NONE;
+    if (!is_tensor) continue;
+    for (int j = 0; j < 4; ++j) v[j] = PyLong_AsLongLong(args[i + 1 + j]);
+    if (PyErr_Occurred()) goto again;
+    const long long rows = v[1], columns = v[2];
+    long long stride = v[3];
+    if (rows <= 0 || columns <= 0) continue;
+    if (!of_kind(&t, v[0]) || rows > INT32_MAX || columns > INT64_MAX / 4 / rows || (t.device_type == ON_GPU && t.device_id != device)) Py_RETURN_NONE;
+    const int whole = contiguous(&t, &count);
+    if (stride < 0) {
+      if (!whole || count < rows * columns) Py_RETURN_NONE;
+      continue;
+    }
+    if (whole) {
+      if (stride == 0 && rows > 1 && (t.ndim == 0 || (t.ndim > 1 && t.shape[t.ndim - 1] != columns))) Py_RETURN_NONE;
+    } else {
+      if ((stride == 0 && rows > 1) || t.ndim < 1 || (columns > 1 && t.strides[t.ndim - 1] != 1)) Py_RETURN_NONE;
+      count = 1;
+      for (int j = 0; j < t.ndim; ++j) {
+        if (t.shape[j] == 0) Py_RETURN_NONE;
+        count += (t.shape[j] - 1) * t.strides[j];
+      }
+    }
+    if (stride == 0) stride = columns;
+    if (stride > INT64_MAX / 4 / rows || (rows - 1) * stride + columns > count) Py_RETURN_NONE;
+  }
+  if (PyErr_Occurred()) goto again;
+  PyObject* out = PyTuple_New(k);
+  if (!out) return NULL;
+  for (Py_ssize_t i = 0; i < k; ++i) {
+    PyObject* a = PyLong_FromUnsignedLongLong(at[i]);
+    if (!a) {
+      Py_DECREF(out);
+      return NULL;
+    }
+    PyTuple_SET_ITEM(out, i, a);
+  }
+  return out;
+again:
+  PyErr_Clear();
+  Py_RETURN_NONE;
+}
+
 static PyMethodDef methods[] = {
     {"setup", (PyCFunction)(void (*)(void))setup, METH_FASTCALL, "setup(capsule, type) -> bool"},
+    {"rows", (PyCFunction)(void (*)(void))rows, METH_FASTCALL, "addresses of checked matrices and buffers, or None"},
     {"addresses", (PyCFunction)(void (*)(void))addresses, METH_FASTCALL, "addresses of checked tensors, or None"},
     {NULL, NULL, 0, NULL},
 };
