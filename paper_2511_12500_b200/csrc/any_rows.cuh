@@ -1,10 +1,10 @@
-// Rows that start at any element, seen in pieces of 16 bytes counted from the row's first element (not from a 16-byte boundary as in
-// logit_rows.cuh), so that a thread has the same columns of every row: what the operators on embeddings and norms need, whose weights and sums
-// belong to columns.
+// Rows that start at any element, seen by columns (not by 16-byte granules as in logit_rows.cuh), so that a thread has the same columns of every row:
+// what the operators on embeddings and norms need, whose weights and sums belong to columns.
 //
-// A piece that does not start on a 16-byte boundary is cut out of the two aligned 16 bytes that it touches (the second is the next thread's
-// first and comes from L1).  Stores go the other way: a warp holds consecutive pieces, and each thread joins the end of its neighbour's piece
-// with the start of its own.  Nothing outside a row is read or written: at a row's ends, elements are moved one at a time.
+// A warp takes 256 columns of a row, or a few times that, through shared memory of its own.  Aligned 16 bytes are copied asynchronously, several rows
+// ahead, without passing through registers; where the row begins elsewhere than at 16 bytes, each thread cuts its columns out of two of
+// them there, and results go the same way back.  Nothing outside a row is read or written: its first elements are copied by words (and one by itself,
+// where it begins at half a word), the copy of its last 16 bytes is cut short, and what does not fill 16 bytes is stored by elements.
 #pragma once
 
 #include <atomic>
@@ -14,6 +14,7 @@
 namespace iris {
 namespace rows {
 
+constexpr int64_t kMaxDim = 1 << 24;             // bytes of a row are counted in 32 bits
 constexpr int kLaneColumns = 8;                  // of a thread: one piece of 16-bit elements, two of 32-bit ones
 constexpr int kWarpColumns = 32 * kLaneColumns;  // that the threads of a warp hold at a time
 
@@ -33,31 +34,29 @@ __device__ __forceinline__ uint4 cut(const uint4& lo, const uint4& hi, uint32_t 
                     __funnelshift_r(w[3], w[4], bits));
 }
 
-// The 16 bytes at `at` of which [lo, hi) may be read; zeros elsewhere.  ES: bytes of an element.
+// The 16 bytes at `at` of which [lo, hi) may be read; zeros elsewhere.  ES: bytes of an element.  (Loops, as these are rare: unrolled they cost
+// the kernels registers.)
 template <int ES>
 __device__ __forceinline__ uint4 load_elements(const char* at, const char* lo, const char* hi) {
-  uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-  for (int e = 0; e < 16 / ES; ++e) {
-    const char* p = at + e * ES;
-    if (p >= lo && p < hi) {
-      const uint32_t v = ES == 4 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
-      w[e * ES / 4] |= v << (e * ES % 4 * 8);
-    }
+  uint4 v = make_uint4(0, 0, 0, 0);
+#pragma unroll 1
+  for (const char* p = at + 16 - ES; p >= at; p -= ES) {
+    const uint32_t x = p < lo || p >= hi ? 0 : ES == 4 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
+    v = ES == 4 ? make_uint4(x, v.x, v.y, v.z)
+                : make_uint4(v.x << 16 | x, __funnelshift_l(v.x, v.y, 16), __funnelshift_l(v.y, v.z, 16), __funnelshift_l(v.z, v.w, 16));
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  return v;
 }
 template <int ES>
-__device__ __forceinline__ void store_elements(char* at, const char* lo, const char* hi, const uint4& v) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int e = 0; e < 16 / ES; ++e) {
-    char* p = at + e * ES;
+__device__ __forceinline__ void store_elements(char* at, const char* lo, const char* hi, uint4 v) {
+#pragma unroll 1
+  for (char* p = at; p < at + 16; p += ES) {
     if (p >= lo && p < hi) {
-      const uint32_t x = w[e * ES / 4] >> (e * ES % 4 * 8);
-      if (ES == 4) *reinterpret_cast<uint32_t*>(p) = x;
-      else *reinterpret_cast<uint16_t*>(p) = (uint16_t)x;
+      if (ES == 4) *reinterpret_cast<uint32_t*>(p) = v.x;
+      else *reinterpret_cast<uint16_t*>(p) = (uint16_t)v.x;
     }
+    v = ES == 4 ? make_uint4(v.y, v.z, v.w, 0)
+                : make_uint4(__funnelshift_r(v.x, v.y, 16), __funnelshift_r(v.y, v.z, 16), __funnelshift_r(v.z, v.w, 16), v.w >> 16);
   }
 }
 // Aligned 16 bytes, as above.
@@ -68,42 +67,48 @@ __device__ __forceinline__ void store16(char* at, const char* lo, const char* hi
 }
 __device__ __forceinline__ uint32_t phase(const void* p) { return (uint32_t)reinterpret_cast<uintptr_t>(p) & 15; }
 
-// N pieces: piece i at `at` + i * step, of the row [lo, hi).  All loads are under way before the first result is used.
-template <int ES, int N>
-__device__ __forceinline__ void load_pieces(const char* at, int step, const char* lo, const char* hi, uint4 (&v)[N]) {
-  const uint32_t a = phase(at);   // of every piece: step is a multiple of 16
-  if (a == 0) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const char* p = at + (int64_t)i * step;
-      if (p >= lo && p + 16 <= hi) v[i] = ld_global_v4(p);
-      else v[i] = load_elements<ES>(p, lo, hi);
-    }
-    return;
-  }
-  uint4 next[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const char* p = at + (int64_t)i * step - a;
-    const bool inside = p >= lo && p + 32 <= hi;
-    v[i] = inside ? ld_global_v4(p) : load_elements<ES>(p, lo, hi);
-    next[i] = inside ? ld_global_v4(p + 16) : load_elements<ES>(p + 16, lo, hi);
-  }
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = cut(v[i], next[i], a);
-}
+// The piece at `at` of the row [lo, hi), by one thread alone.
 template <int ES>
 __device__ __forceinline__ uint4 load_piece(const char* at, const char* lo, const char* hi) {
-  uint4 v[1];
-  load_pieces<ES, 1>(at, 16, lo, hi, v);
-  return v[0];
+  const uint32_t a = phase(at);
+  const char* p = at - a;
+  if (a == 0) return p >= lo && p + 16 <= hi ? ld_global_v4(p) : load_elements<ES>(p, lo, hi);
+  const bool inside = p >= lo && p + 32 <= hi;
+  const uint4 v = inside ? ld_global_v4(p) : load_elements<ES>(p, lo, hi), next = inside ? ld_global_v4(p + 16) : load_elements<ES>(p + 16, lo, hi);
+  return cut(v, next, a);
 }
 
-// A thread's 8 columns of a type: 1 piece or 2.
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+// `bytes` <= 16 of 16, the rest zeros.
+__device__ __forceinline__ void copy_async_part(uint32_t shared, const void* global, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(shared), "l"(global), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_async_word(uint32_t shared, const void* global) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(shared), "l"(global) : "memory");
+}
+__device__ __forceinline__ void copy_async_pair(uint32_t shared, const float* global) {   // 8-byte aligned
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(shared), "l"(global) : "memory");
+}
+__device__ __forceinline__ uint64_t ld_shared_u64(uint32_t at) {
+  uint64_t v;
+  asm volatile("ld.shared.u64 %0, [%1];" : "=l"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_async_wait_but() {   // until at most N groups of this thread are under way
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// A thread's 8 columns of a type.
 template <int DT>
 struct Columns {
   using E = Elem<DT>;
-  static constexpr int ES = sizeof(typename E::T), N = kLaneColumns / E::VE;   // N: pieces
+  static constexpr int ES = sizeof(typename E::T), N = kLaneColumns / E::VE;   // N: times 16 bytes
   static __device__ __forceinline__ void unpack(const uint4* v, float (&x)[kLaneColumns]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -122,50 +127,141 @@ struct Columns {
       v[i] = E::pack(y);
     }
   }
-  // Columns first + i * kWarpColumns ... of the row's `dim`; zeros behind its end.
-  template <int I>
-  static __device__ __forceinline__ void load(const char* row, int first, int dim, uint4 (&v)[I * N]) {
-    const char* hi = row + (int64_t)dim * ES;
-    const char* at = row + (int64_t)first * ES;
-    if constexpr (N == 1) {
-      load_pieces<ES, I>(at, kWarpColumns * ES, row, hi, v);
-    } else {
-      uint4 a[I], b[I];
-      load_pieces<ES, I>(at, kWarpColumns * ES, row, hi, a);
-      load_pieces<ES, I>(at + 16, kWarpColumns * ES, row, hi, b);
+  // As pairs, for arithmetic on two at once.
+  static __device__ __forceinline__ void unpack2(const uint4* v, uint64_t (&x)[kLaneColumns / 2]) {
+    float y[kLaneColumns];
+    unpack(v, y);
 #pragma unroll
-      for (int i = 0; i < I; ++i) {
-        v[2 * i] = a[i];
-        v[2 * i + 1] = b[i];
+    for (int e = 0; e < kLaneColumns / 2; ++e) x[e] = pair(y[2 * e], y[2 * e + 1]);
+  }
+  static __device__ __forceinline__ void pack2(const uint64_t (&x)[kLaneColumns / 2], uint4* v) {
+    float y[kLaneColumns];
+#pragma unroll
+    for (int e = 0; e < kLaneColumns / 2; ++e) {
+      const float2 f = unpair(x[e]);
+      y[2 * e] = f.x;
+      y[2 * e + 1] = f.y;
+    }
+    pack(y, v);
+  }
+  // Straight from memory: columns `first` ... of a vector of `dim`, zeros behind its end.
+  static __device__ __forceinline__ void load(const char* row, int first, int dim, float (&x)[kLaneColumns]) {
+    uint4 v[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = load_piece<ES>(row + first * ES + n * 16, row, row + dim * ES);
+    unpack(v, x);
+  }
+};
+
+// I times 256 columns of a row, from column `begin`, in a warp's shared memory at `at` (16-byte aligned, kBytes): bytes from the aligned 16
+// in which they begin.
+template <int DT, int I>
+struct Segment {
+  using C = Columns<DT>;
+  static constexpr int ES = C::ES, N = C::N, kColumns = I * kWarpColumns, kBytes = kColumns * ES + 32;
+  // Starts the copies.  An element that begins at half a word, if there is one, comes back with its place in shared memory, where `settle` puts it; later,
+  // so that nobody waits for it here.
+  struct Lone {
+    uint32_t at = 0;   // 0: none
+    uint16_t value;
+    __device__ __forceinline__ void settle() {
+      if (at) asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(value) : "memory");
+      at = 0;
+    }
+  };
+  static __device__ __forceinline__ void fetch(uint32_t at, const char* row, int begin, int dim, Lone& lone) {
+    const int lane = threadIdx.x & 31, bytes = dim * ES, start = begin * ES;
+    const int a = (int)phase(row + start);
+    const char* const somewhere = row - phase(row);   // aligned, for copies of 0 bytes
+    if (begin + kColumns <= dim) {
+      const char* const p = row + (start - a + lane * 16);
+#pragma unroll
+      for (int k = 0; k < I * N; ++k)
+        if (k || start - a + lane * 16 >= 0) copy_async(at + (k * 32 + lane) * 16, p + k * 512);
+    } else {
+#pragma unroll
+      for (int k = 0; k < I * N; ++k) {
+        const int g = k * 32 + lane, from = start - a + g * 16;   // counted from the row's first byte
+        if (from >= 0) copy_async_part(at + g * 16, from < bytes ? row + from : somewhere, max(0, min(16, bytes - from)));
+      }
+    }
+    if (a == 0) return;
+    if (lane == 0) {
+      const int from = start - a + I * N * 512;
+      copy_async_part(at + I * N * 512, from < bytes ? row + from : somewhere, max(0, min(16, bytes - from)));
+    }
+    if (begin == 0) {   // the row's first elements
+      const int word = (a + 3) / 4 + lane, from = word * 4 - a;
+      if (word < 4) {
+        if (from + 4 <= bytes) copy_async_word(at + word * 4, row + from);
+        else if (from < bytes) asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + word * 4), "h"(*reinterpret_cast<const uint16_t*>(row + from)) : "memory");
+      }
+      if (ES == 2 && lane == 0 && (a & 2)) {
+        lone.at = at + a;
+        lone.value = *reinterpret_cast<const uint16_t*>(row);
       }
     }
   }
-  // The other way; all threads of a warp, whose columns are lane * kLaneColumns on from the first one's.
-  template <int I>
-  static __device__ __forceinline__ void store(char* row, int first, int dim, const uint4 (&v)[I * N]) {
-    const int lane = threadIdx.x & 31, begin = first - lane * kLaneColumns;
-    const char* lo = row + (int64_t)begin * ES;
-    const char* hi = row + (int64_t)min(dim, begin + I * kWarpColumns) * ES;
-    char* at = row + (int64_t)first * ES;
-    const uint32_t a = phase(at);
-    if (a == 0) {
+  // Run i of the thread's columns; zeros behind the row's end.  After a barrier of the warp behind the copies and `settle`.
+  static __device__ __forceinline__ void read(uint32_t at, const char* row, int begin, int dim, int i, uint64_t (&x)[kLaneColumns / 2]) {
+    const uint32_t a = phase(row + begin * ES);
+    uint4 v[N];
 #pragma unroll
-      for (int i = 0; i < I * N; ++i) store16<ES>(at + (int64_t)(i / N) * kWarpColumns * ES + i % N * 16, lo, hi, v[i]);
+    for (int n = 0; n < N; ++n) {
+      const uint32_t g = at + (i * 32 + (threadIdx.x & 31)) * N * 16 + n * 16;
+      v[n] = ld_shared_v4(g);
+      if (a) v[n] = cut(v[n], ld_shared_v4(g + 16), a);
+    }
+    if (a && dim * ES < 16) {   // the copies have left nothing behind the end of such a row
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        uint32_t w[4] = {v[n].x, v[n].y, v[n].z, v[n].w};
+        const int there = dim - begin - i * kWarpColumns - (int)(threadIdx.x & 31) * kLaneColumns - n * C::E::VE;
+#pragma unroll
+        for (int e = 0; e < C::E::VE; ++e)
+          if (e >= there) w[e * ES / 4] &= ES == 4 ? 0u : e % 2 ? 0xffffu : 0xffff0000u;
+        v[n] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    C::unpack2(v, x);
+  }
+  // Stores the threads' columns; `at`: kBytes of the warp's shared memory that nobody reads any more.
+  static __device__ __forceinline__ void write(uint32_t at, char* row, int begin, int dim, const uint4 (&v)[I * N]) {
+    const int lane = threadIdx.x & 31, bytes = min(dim - begin, kColumns) * ES;   // of the segment
+    if (bytes <= 0) return;
+    char* const to = row + begin * ES;
+    const int a = (int)phase(to);
+    if (a == 0 && bytes % 16 == 0) {
+#pragma unroll
+      for (int k = 0; k < I * N; ++k) {
+        const int b = ((k / N * 32 + lane) * N + k % N) * 16;
+        if (b < bytes) st_global_v4(to + b, v[k]);
+      }
       return;
     }
-    uint4 carry = make_uint4(0, 0, 0, 0);   // the piece in front of the warp's next 256 columns
+    __syncwarp();
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-      const uint4 last = v[i * N + N - 1];
-      uint4 before = make_uint4(__shfl_up_sync(~0u, last.x, 1), __shfl_up_sync(~0u, last.y, 1), __shfl_up_sync(~0u, last.z, 1),
-                                __shfl_up_sync(~0u, last.w, 1));
-      if (lane == 0) before = carry;
-      carry = make_uint4(__shfl_sync(~0u, last.x, 31), __shfl_sync(~0u, last.y, 31), __shfl_sync(~0u, last.z, 31), __shfl_sync(~0u, last.w, 31));
+    for (int k = 0; k < I * N; ++k) ptx::st_shared_v4(at + 16 + ((k / N * 32 + lane) * N + k % N) * 16, v[k]);
+    __syncwarp();
 #pragma unroll
-      for (int n = 0; n < N; ++n)
-        store16<ES>(at + (int64_t)i * kWarpColumns * ES + n * 16 - a, lo, hi, cut(n ? v[i * N + n - 1] : before, v[i * N + n], 16 - a));
+    for (int k = 0; k < I * N; ++k) {
+      const int g = k * 32 + lane, b = g * 16 - a;
+      if (b >= 0 && b + 16 <= bytes) st_global_v4(to + b, a ? cut(ld_shared_v4(at + g * 16), ld_shared_v4(at + g * 16 + 16), 16 - a) : ld_shared_v4(at + g * 16 + 16));
     }
-    if (lane == 31) store16<ES>(at + (int64_t)(I - 1) * kWarpColumns * ES + N * 16 - a, lo, hi, cut(carry, carry, 16 - a));
+    // what does not fill 16 bytes: at the begin (if it is not aligned) and at the end, an element a thread
+    const int head = a ? min(16 - a, bytes) : 0, end = ((bytes + a) & ~15) - a;
+    const int b = lane < 8 ? lane * ES : end + (lane - 8) * ES;
+    if (lane < 8 ? b < head : end >= 0 && lane < 16 && b < bytes) {
+      if (ES == 4) {
+        uint32_t x;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at + 16 + b) : "memory");
+        *reinterpret_cast<uint32_t*>(to + b) = x;
+      } else {
+        uint16_t x;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(at + 16 + b) : "memory");
+        *reinterpret_cast<uint16_t*>(to + b) = x;
+      }
+    }
   }
 };
 

@@ -6,8 +6,6 @@
 namespace iris {
 namespace rows {
 
-constexpr int64_t kMaxDim = 1 << 24;
-
 // ---- lookup --------------------------------------------------------------------------------------------------------
 constexpr int kEmbedThreads = 256;
 
@@ -215,9 +213,9 @@ __device__ __forceinline__ char* table_row(const EmbedGradParams& p, uint32_t v)
   const uint32_t r = v / p.per;
   return p.shard[r] ? p.shard[r] + (int64_t)(v - r * p.per) * p.shard_stride : nullptr;
 }
-// All threads of a warp: their columns of row v.
+// All threads of a warp: their columns of row v, from column `begin` on; `at`: shared memory of the warp's, Segment<GT, 1>::kBytes.
 template <int GT>
-__device__ __forceinline__ void write_row(const EmbedGradParams& p, uint32_t v, int first, const float (&sum)[kLaneColumns]) {
+__device__ __forceinline__ void write_row(const EmbedGradParams& p, uint32_t v, uint32_t at, int begin, const float (&sum)[kLaneColumns]) {
   using C = Columns<GT>;
   char* const row = table_row<GT>(p, v);
   float x[kLaneColumns];
@@ -226,13 +224,13 @@ __device__ __forceinline__ void write_row(const EmbedGradParams& p, uint32_t v, 
   uint4 w[C::N];
   if (p.accumulate) {
     float old[kLaneColumns];
-    C::template load<1>(row, first, p.dim, w);
-    C::unpack(w, old);
+    C::load(row, begin + (threadIdx.x & 31) * kLaneColumns, p.dim, old);
 #pragma unroll
     for (int e = 0; e < kLaneColumns; ++e) x[e] += old[e];
   }
   C::pack(x, w);
-  C::template store<1>(row, first, p.dim, w);
+  __syncwarp();
+  Segment<GT, 1>::write(at, row, begin, p.dim, w);
 }
 
 // Zeros in the rows that no token names: a warp has 32 rows and kFillBytes of each.
@@ -257,10 +255,18 @@ __device__ __forceinline__ void fill_rows(const EmbedGradParams& p, int64_t unit
 
 // A warp adds up a chunk of the sorted places over 256 columns.  A run of equal tokens that lies inside a chunk is finished here; one that goes on
 // in other chunks leaves its sums in `parts`, for embed_join_kernel.
+//
+// The rows are on their way to shared memory kSumStages ahead.
+template <int DT>
+constexpr int sum_stages() { return DT == IRIS_F32 ? 8 : 12; }   // 8 KB or 6 KB a warp
+template <int DT, int GT>
+constexpr int sum_bytes() { return sum_stages<DT>() * Segment<DT, 1>::kBytes + Segment<GT, 1>::kBytes; }   // of a warp
+
 template <int DT, int GT>
 __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_constant__ EmbedGradParams p) {
-  using C = Columns<DT>;
-  constexpr int U = 8 / C::N;   // rows under way
+  using G = Segment<DT, 1>;
+  constexpr int kStages = sum_stages<DT>();
+  extern __shared__ __align__(16) char ring[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   ptx::let_next_begin();
   ptx::begin_after_previous();
@@ -269,59 +275,84 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
     return;
   }
   const int64_t unit = (int64_t)blockIdx.x * kSumWarps + warp;
-  const int c = (int)(unit / p.tiles), first = (int)(unit % p.tiles) * kWarpColumns + lane * kLaneColumns;
+  const int c = (int)(unit / p.tiles), column = (int)(unit % p.tiles) * kWarpColumns, first = column + lane * kLaneColumns;
   if (c >= p.chunks) return;
+  const uint32_t own = ptx::smem_u32(ring) + warp * sum_bytes<DT, GT>(), out = own + kStages * G::kBytes;
   const int begin = c * p.chunk, end = min(p.n, begin + p.chunk);
+  // The places and tokens of 32 entries are held by the threads, and the next 32 places, as copies begin ahead.
+  const auto key_of = [&](int i) { return i < end ? p.keys[i] : p.vocab; };
+  const auto place_of = [&](int i) { return i < end ? p.places[i] : 0u; };
   uint32_t now = p.keys[begin];
   if (now >= p.vocab) return;
   bool goes_on = begin > 0 && p.keys[begin - 1] == now;   // the run came from the chunk before
-  float sum[kLaneColumns] = {};
+  uint32_t key = key_of(begin + lane), place = place_of(begin + lane), next_place = place_of(begin + 32 + lane);
+  uint64_t sum[kLaneColumns / 2] = {};
+  typename G::Lone lone;
+  const auto row_of = [&](uint32_t i) { return p.dy + (int64_t)i * p.dy_stride; };
+  const auto fetch = [&](int i, int base, int stage) {   // base: of `place`
+    lone.settle();
+    if (i < end) {
+      const uint32_t at = __shfl_sync(~0u, i - base < 32 ? place : next_place, (i - base) & 31);
+      G::fetch(own + stage * G::kBytes, row_of(at), column, p.dim, lone);
+    }
+    copy_async_commit();
+  };
   const auto finish = [&](bool more) {   // more: the run goes on in the next chunk
+    float s[kLaneColumns];
+#pragma unroll
+    for (int e = 0; e < kLaneColumns / 2; ++e) {
+      const float2 f = unpair(sum[e]);
+      s[2 * e] = f.x;
+      s[2 * e + 1] = f.y;
+    }
     if (!goes_on && !more) {
-      write_row<GT>(p, now, first, sum);
+      write_row<GT>(p, now, out, column, s);
     } else {
       float* const to = p.parts + ((int64_t)2 * c + !goes_on) * p.dim;
 #pragma unroll
       for (int e = 0; e < kLaneColumns; ++e)
-        if (first + e < p.dim) to[first + e] = sum[e];
+        if (first + e < p.dim) to[first + e] = s[e];
     }
   };
-  for (int at = begin; at < end; at += 32) {
-    const int m = min(32, end - at);
-    const uint32_t key = lane < m ? p.keys[at + lane] : p.vocab, place = lane < m ? p.places[at + lane] : 0;
-    for (int b = 0; b < m; b += U) {
-      uint4 v[U][C::N];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const uint32_t i = __shfl_sync(~0u, place, min(b + u, m - 1));
-        C::template load<1>(p.dy + (int64_t)i * p.dy_stride, first, p.dim, v[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (b + u >= m) break;
-        const uint32_t k = __shfl_sync(~0u, key, b + u);
-        if (k != now) {
-          finish(false);
-          if (k >= p.vocab) return;
-          now = k;
-          goes_on = false;
-#pragma unroll
-          for (int e = 0; e < kLaneColumns; ++e) sum[e] = 0.f;
-        }
-        float x[kLaneColumns];
-        C::unpack(v[u], x);
-#pragma unroll
-        for (int e = 0; e < kLaneColumns; ++e) sum[e] += x[e];
-      }
+#pragma unroll 1
+  for (int k = 0; k < kStages - 1; ++k) fetch(begin + k, begin, k);
+  int base = begin, stage = 0;
+#pragma unroll 1
+  for (int i = begin; i < end; ++i) {
+    if (i - base == 32) {
+      base = i;
+      place = next_place;
+      key = key_of(base + lane);
+      next_place = place_of(base + 32 + lane);
     }
+    const uint32_t k = __shfl_sync(~0u, key, i - base), at = __shfl_sync(~0u, place, i - base);
+    if (k != now) {
+      finish(false);
+      if (k >= p.vocab) break;
+      now = k;
+      goes_on = false;
+#pragma unroll
+      for (int e = 0; e < kLaneColumns / 2; ++e) sum[e] = 0;
+    }
+    lone.settle();
+    copy_async_wait_but<kStages - 2>();
+    __syncwarp();
+    fetch(i + kStages - 1, base, stage == 0 ? kStages - 1 : stage - 1);
+    uint64_t x[kLaneColumns / 2];
+    G::read(own + stage * G::kBytes, row_of(at), column, p.dim, 0, x);
+#pragma unroll
+    for (int e = 0; e < kLaneColumns / 2; ++e) sum[e] = add2f(sum[e], x[e]);
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+    if (i + 1 == end) finish(end < p.n && p.keys[end] == now);
   }
-  finish(end < p.n && p.keys[end] == now);
+  copy_async_wait();   // a block does not end while copies are under way
 }
 
 // Runs that go over several chunks: the sums of their parts, by the block of the chunk where a run begins; its warps take the parts in turn.
 template <int GT>
 __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(const __grid_constant__ EmbedGradParams p) {
   __shared__ float sums[kSumWarps][kWarpColumns];
+  __shared__ __align__(16) char out[Segment<GT, 1>::kBytes];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   ptx::let_next_begin();
   ptx::begin_after_previous();
@@ -350,7 +381,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(const __grid_co
   for (int w = 1; w < min(kSumWarps, last - c); ++w)
 #pragma unroll
     for (int e = 0; e < kLaneColumns; ++e) sum[e] += sums[w][lane * kLaneColumns + e];
-  write_row<GT>(p, key, first, sum);
+  write_row<GT>(p, key, ptx::smem_u32(out), first - lane * kLaneColumns, sum);
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
@@ -375,7 +406,10 @@ static EmbedGradPlan embed_grad_plan(int64_t n, int64_t vocab, int64_t dim) {
 
 template <int DT, int GT>
 static int launch_embed_grad(const EmbedGradParams& p, unsigned fill_blocks, cudaStream_t st) {
-  IRIS_CHECK(launch_rows(embed_sum_kernel<DT, GT>, p, p.sum_blocks + fill_blocks, 1, kSumThreads, 0, st));
+  constexpr auto kernel = embed_sum_kernel<DT, GT>;
+  constexpr int bytes = kSumWarps * sum_bytes<DT, GT>();
+  IRIS_CHECK(allow_shared<kernel>(bytes));
+  IRIS_CHECK(launch_rows(kernel, p, p.sum_blocks + fill_blocks, 1, kSumThreads, bytes, st));
   if (p.chunks < 2) return IRIS_OK;
   return launch_rows(embed_join_kernel<GT>, p, (unsigned)((int64_t)p.chunks * p.tiles), 1, kSumThreads, 0, st);
 }

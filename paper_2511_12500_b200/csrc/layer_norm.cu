@@ -4,15 +4,22 @@
 //   g = dy w:   dx = r (g - mean g - h mean(g h)),   dw = sum over rows dy h,   db = sum over rows dy
 //
 // A row is held in registers by a group of warps, 8 columns a thread and a few such runs, and where that is not enough by a cluster of blocks.
+// Blocks stay and take rows in turn; the next ones are under way to shared memory meanwhile.
 #include "any_rows.cuh"
 
 namespace iris {
 namespace rows {
 
-constexpr int kNormRuns = 4, kNormGradRuns = 2;   // runs of 8 columns that a thread holds
-constexpr int kNormWarps = 16;                  // of a block
+constexpr int kNormRuns = 4, kNormGradRuns = 2;   // runs of 8 columns that a thread holds, of one row or of several short ones
+constexpr int kNormRowWarps = 8, kNormGradRowWarps = 16;   // of a row in a block, at most
 constexpr int kNormSplit = 8;                   // blocks (one cluster) that share a row
-constexpr int64_t kNormMaxDim = (int64_t)kNormGradRuns * kWarpColumns * kNormWarps * kNormSplit;
+constexpr int64_t kNormMaxDim = (int64_t)kNormRuns * kWarpColumns * kNormRowWarps * kNormSplit;
+static_assert(kNormRuns * kNormRowWarps == kNormGradRuns * kNormGradRowWarps, "the same limit for both directions");
+// Of a block, which has an SM to itself: what registers and shared memory allow.
+constexpr int norm_warps(int dtype) { return dtype == IRIS_F32 ? 16 : 24; }
+constexpr int kNormGradWarps = 16;
+constexpr int norm_stages(int dtype) { return dtype == IRIS_F32 ? 2 : 3; }        // rows (or R of them) in shared memory
+constexpr int norm_grad_stages(int dtype) { return dtype == IRIS_F32 ? 2 : 3; }
 
 struct NormParams {
   const char* x;
@@ -38,7 +45,7 @@ struct NormGradParams {
 
 // What a warp knows of a row, and the sum over the warps of a row, which all of its threads get.
 struct NormShared {
-  float2 of[2][kNormWarps * kNormSplit];   // twice: one is read while the next row's is written
+  float2 of[2][norm_warps(IRIS_F16) > kNormGradRowWarps * kNormSplit ? norm_warps(IRIS_F16) : kNormGradRowWarps * kNormSplit];   // twice: one is read while the next row's is written
 };
 struct Group {
   int warps, split, rank, index, warp, lane, id;   // index: of the group in its block; warp: in its row, over all blocks; id: of its barrier
@@ -64,6 +71,22 @@ struct Group {
   }
   __device__ __forceinline__ int all() const { return warps * split; }
   __device__ __forceinline__ const float2* of(const NormShared& s, int turn) const { return s.of[turn] + (split > 1 ? 0 : index * warps); }
+  // Means and squares' sums (about those means) of the warps' shares, `each` columns but for the last ones -> of the whole row.
+  __device__ __forceinline__ void join(NormShared& s, int turn, int dim, int each, float& mean, float& squares) const {
+    exchange(s, turn, make_float2(mean, squares));
+    const float2* const v = of(s, turn);
+    float m = 0.f, q = 0.f;
+#pragma unroll 4
+    for (int w = 0; w < all(); ++w) m = fmaf(v[w].x, (float)max(0, min(dim - w * each, each)), m);
+    mean = m / (float)dim;
+#pragma unroll 4
+    for (int w = 0; w < all(); ++w) {
+      const float2 x = v[w];
+      const float d = x.x - mean;
+      q += fmaf(d * d, (float)max(0, min(dim - w * each, each)), x.y);
+    }
+    squares = q;
+  }
 };
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
@@ -71,200 +94,319 @@ __device__ __forceinline__ float warp_sum(float x) {
   return x;
 }
 
-template <int DT, int PT, int I>
-__global__ void __launch_bounds__(kNormWarps * 32) norm_kernel(const NormParams p) {
-  using C = Columns<DT>;
-  using W = Columns<PT>;
-  __shared__ NormShared shared;
-  const Group group(p.warps, p.split);
-  const int64_t r = (int64_t)(blockIdx.x / p.split) * (blockDim.x / (p.warps * 32)) + group.index;
-  const int begin = group.warp * I * kWarpColumns, first = begin + group.lane * kLaneColumns;
-  ptx::let_next_begin();
-  if (p.split > 1) ptx::cluster_sync();   // the others may write to this block's shared memory
-  ptx::begin_after_previous();
-  if (r >= p.rows) return;   // a whole group, and of one block only
-  uint4 raw[I * C::N];
-  C::template load<I>(p.x + r * p.x_stride, first, p.dim, raw);
-  float x[I][kLaneColumns], sum = 0.f;
-#pragma unroll
+// A vector of parameters in shared memory, in 32 bits, so that a thread's columns of run i are two accesses of 16 bytes side by side with the other
+// threads': [runs of the block, 2, 32 threads, 4].  `none`: what stands for a vector that is not there.
+template <int PT, int I>
+__device__ __forceinline__ void put_params(float* to, const char* from, float none, const Group& group, int begin, int dim) {
+  if (group.index) return;   // the other groups have the same columns
+#pragma unroll 1
   for (int i = 0; i < I; ++i) {
-    C::unpack(raw + i * C::N, x[i]);
+    float x[kLaneColumns];
 #pragma unroll
-    for (int e = 0; e < kLaneColumns; ++e) sum += x[i][e];
+    for (int e = 0; e < kLaneColumns; ++e) x[e] = none;
+    if (from) Columns<PT>::load(from, begin + group.lane * kLaneColumns + i * kWarpColumns, dim, x);
+    float4* const at = reinterpret_cast<float4*>(to) + ((group.warp - group.rank * group.warps) * I + i) * 64 + group.lane;
+    at[0] = make_float4(x[0], x[1], x[2], x[3]);
+    at[32] = make_float4(x[4], x[5], x[6], x[7]);
   }
-  // The warp's mean, and the squares' sum about it: nothing is lost where the mean is large.
-  const int has = max(0, min(p.dim - begin, I * kWarpColumns));
-  const float mine = has ? warp_sum(sum) / (float)has : 0.f;
-  float squares = 0.f;
-#pragma unroll
-  for (int i = 0; i < I; ++i)
-#pragma unroll
-    for (int e = 0; e < kLaneColumns; ++e) {
-      const float d = first + i * kWarpColumns + e < p.dim ? x[i][e] - mine : 0.f;
-      squares = fmaf(d, d, squares);
-    }
-  squares = warp_sum(squares);
-  float mean = mine;
-  if (group.all() > 1) {
-    group.exchange(shared, 0, make_float2(mine, squares));
-    const float2* const of = group.of(shared, 0);
-    float s = 0.f, q = 0.f;
-    for (int w = group.lane; w < group.all(); w += 32) {
-      s = fmaf(of[w].x, (float)max(0, min(p.dim - w * I * kWarpColumns, I * kWarpColumns)), s);
-    }
-    mean = warp_sum(s) / (float)p.dim;
-    for (int w = group.lane; w < group.all(); w += 32) {
-      const float d = of[w].x - mean;
-      q += fmaf(d * d, (float)max(0, min(p.dim - w * I * kWarpColumns, I * kWarpColumns)), of[w].y);
-    }
-    squares = warp_sum(q);
-  }
-  const float rstd = 1.f / sqrtf(squares / (float)p.dim + p.eps);
-  if (p.stats && group.warp == 0 && group.lane == 0) {
-    p.stats[2 * r] = mean;
-    p.stats[2 * r + 1] = rstd;
-  }
-#pragma unroll
-  for (int i = 0; i < I; ++i)
-#pragma unroll
-    for (int e = 0; e < kLaneColumns; ++e) x[i][e] = (x[i][e] - mean) * rstd;
-  if (p.weight) {
-    uint4 v[I * W::N];
-    W::template load<I>(p.weight, first, p.dim, v);
-#pragma unroll
-    for (int i = 0; i < I; ++i) {
-      float w[kLaneColumns];
-      W::unpack(v + i * W::N, w);
-#pragma unroll
-      for (int e = 0; e < kLaneColumns; ++e) x[i][e] *= w[e];
-    }
-  }
-  if (p.bias) {
-    uint4 v[I * W::N];
-    W::template load<I>(p.bias, first, p.dim, v);
-#pragma unroll
-    for (int i = 0; i < I; ++i) {
-      float w[kLaneColumns];
-      W::unpack(v + i * W::N, w);
-#pragma unroll
-      for (int e = 0; e < kLaneColumns; ++e) x[i][e] += w[e];
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < I; ++i) C::pack(x[i], raw + i * C::N);
-  C::template store<I>(p.y + r * p.y_stride, first, p.dim, raw);
+}
+// `at`: of the thread's run 0.
+__device__ __forceinline__ void get_params(uint32_t at, int i, uint64_t (&x)[kLaneColumns / 2]) {
+  const uint4 a = ld_shared_v4(at + i * 1024), b = ld_shared_v4(at + i * 1024 + 512);
+  x[0] = (uint64_t)a.y << 32 | a.x;
+  x[1] = (uint64_t)a.w << 32 | a.z;
+  x[2] = (uint64_t)b.y << 32 | b.x;
+  x[3] = (uint64_t)b.w << 32 | b.z;
+}
+__device__ __forceinline__ float both(uint64_t x) {
+  const float2 f = unpair(x);
+  return f.x + f.y;
 }
 
-// A block's groups take rows in turn and add up dw and db of their columns in registers, in chains of at most kNormChain rows, then of such sums.
-constexpr int kNormChain = 128;
-
-template <int DT, int PT, int I>
-__global__ void __launch_bounds__(kNormWarps * 32) norm_grad_kernel(const NormGradParams p) {
+// R rows at a time.
+template <int DT, int PT, int R, int I>
+__global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormParams p) {
   using C = Columns<DT>;
-  using W = Columns<PT>;
+  using G = Segment<DT, I>;
+  constexpr int kStages = norm_stages(DT), H = kLaneColumns / 2;
   __shared__ NormShared shared;
-  extern __shared__ float sums[];   // [groups, 2, columns of the block]
+  extern __shared__ __align__(16) char ring[];   // [warps, stages, R] segments; weight, bias
   const Group group(p.warps, p.split);
   const int groups = blockDim.x / (p.warps * 32);
-  const int begin = group.warp * I * kWarpColumns, first = begin + group.lane * kLaneColumns;
-  const int64_t step = (int64_t)(gridDim.x / p.split) * groups;
-  const int columns = p.warps * I * kWarpColumns;   // of the block
-  float* const own = sums + group.index * 2 * columns + first - group.rank * columns;
+  const int begin = group.warp * G::kColumns, first = begin + group.lane * kLaneColumns;
+  const int64_t step = (int64_t)(gridDim.x / p.split) * groups * R;
+  const uint32_t own = ptx::smem_u32(ring) + (threadIdx.x >> 5) * (kStages * R * G::kBytes);
+  float* const params = reinterpret_cast<float*>(ring + (blockDim.x >> 5) * (kStages * R * G::kBytes));
+  const int columns = p.warps * G::kColumns;   // of the block
+  const uint32_t weight = ptx::smem_u32(params) + ((group.warp - group.rank * group.warps) * I * 64 + group.lane) * 16, bias = weight + columns * 4;
+  if (p.split > 1) ptx::cluster_sync();   // the others may write to this block's shared memory
+  ptx::let_next_begin();
+  ptx::begin_after_previous();
+  typename G::Lone lone[R];
+  const auto fetch = [&](int64_t r, int stage) {
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      lone[q].settle();
+      if (r + q < p.rows) G::fetch(own + (stage * R + q) * G::kBytes, p.x + (r + q) * p.x_stride, begin, p.dim, lone[q]);
+    }
+    copy_async_commit();
+  };
+  int64_t r = ((int64_t)(blockIdx.x / p.split) * groups + group.index) * R;
+#pragma unroll
+  for (int k = 0; k < kStages - 1; ++k) fetch(r + k * step, k);
+  put_params<PT, I>(params, p.weight, 1.f, group, begin, p.dim);
+  put_params<PT, I>(params + columns, p.bias, 0.f, group, begin, p.dim);
+  __syncthreads();
+  const int has = max(0, min(p.dim - begin, G::kColumns));
+  const float count = (float)max(has, 1), dim = (float)p.dim;   // division, so that the mean of equal small whole numbers is that number
+  const bool full = has == G::kColumns;
+  int stage = 0;
+  for (int turn = 0; r < p.rows; r += step, turn ^= 1) {
+#pragma unroll
+    for (int q = 0; q < R; ++q) lone[q].settle();
+    copy_async_wait_but<kStages - 2>();
+    __syncwarp();
+    const uint32_t here = own + stage * (R * G::kBytes);
+    fetch(r + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);   // where the row before was
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+    uint64_t x[R][I][H];
+    float mean[R], squares[R];
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      uint64_t s = 0;
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        G::read(here + q * G::kBytes, p.x + (r + q) * p.x_stride, begin, p.dim, i, x[q][i]);
+#pragma unroll
+        for (int e = 0; e < H; ++e) s = add2f(s, x[q][i][e]);
+      }
+      mean[q] = both(s);
+    }
+    // The warp's mean, and the squares' sum about it: nothing is lost where the mean is large.
+#pragma unroll
+    for (int q = 0; q < R; ++q) mean[q] = warp_sum(mean[q]) / count;
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      const uint64_t minus = pair(-mean[q], -mean[q]);
+      uint64_t s = 0;
+      if (full) {
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+          for (int e = 0; e < H; ++e) {
+            const uint64_t d = add2f(x[q][i][e], minus);
+            s = fma2f(d, d, s);
+          }
+      } else {
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+          for (int e = 0; e < H; ++e) {
+            const float2 d = unpair(add2f(x[q][i][e], minus));
+            const int c = first + i * kWarpColumns + 2 * e;
+            const uint64_t there = pair(c < p.dim ? d.x : 0.f, c + 1 < p.dim ? d.y : 0.f);
+            s = fma2f(there, there, s);
+          }
+      }
+      squares[q] = both(s);
+    }
+#pragma unroll
+    for (int q = 0; q < R; ++q) squares[q] = warp_sum(squares[q]);
+    if (R == 1 && group.all() > 1) group.join(shared, turn, p.dim, G::kColumns, mean[0], squares[0]);
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      squares[q] = 1.f / sqrtf(squares[q] / dim + p.eps);
+      if (p.stats && group.warp == 0 && group.lane == 0 && r + q < p.rows)
+        *reinterpret_cast<float2*>(p.stats + 2 * (r + q)) = make_float2(mean[q], squares[q]);
+    }
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      uint64_t w[H], b[H];
+      get_params(weight, i, w);
+      get_params(bias, i, b);
+#pragma unroll
+      for (int q = 0; q < R; ++q)
+#pragma unroll
+        for (int e = 0; e < H; ++e) x[q][i][e] = fma2f(mul2f(add2f(x[q][i][e], pair(-mean[q], -mean[q])), pair(squares[q], squares[q])), w[e], b[e]);
+    }
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      if (r + q >= p.rows) break;
+      uint4 out[I * C::N];
+#pragma unroll
+      for (int i = 0; i < I; ++i) C::pack2(x[q][i], out + i * C::N);
+      G::write(here + q * G::kBytes, p.y + (r + q) * p.y_stride, begin, p.dim, out);
+    }
+  }
+}
+
+// A block's groups add up dw and db of their columns in registers, in chains of at most kNormChain rows, then of such sums.  R rows at a time.
+constexpr int kNormChain = 128;
+
+template <int DT, int R, int I>
+constexpr int norm_grad_stage_bytes() { return R * (2 * Segment<DT, I>::kBytes + 16); }   // x, dy, statistics
+
+template <int DT, int PT, int R, int I>
+__global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const NormGradParams p) {
+  using C = Columns<DT>;
+  using G = Segment<DT, I>;
+  constexpr int kStages = norm_grad_stages(DT), kRow = 2 * G::kBytes + 16, kStage = norm_grad_stage_bytes<DT, R, I>(), H = kLaneColumns / 2;
+  __shared__ NormShared shared;
+  extern __shared__ __align__(16) char ring[];   // [warps, stages, R] segments of x, of dy, statistics; weight; with several groups sums [groups, 2, columns of the block]
+  const Group group(p.warps, p.split);
+  const int groups = blockDim.x / (p.warps * 32);
+  const int begin = group.warp * G::kColumns, first = begin + group.lane * kLaneColumns;
+  const int64_t step = (int64_t)(gridDim.x / p.split) * groups * R;
+  const int columns = p.warps * G::kColumns;   // of the block
+  const uint32_t own = ptx::smem_u32(ring) + (threadIdx.x >> 5) * (kStages * kStage);
+  float* const params = reinterpret_cast<float*>(ring + (blockDim.x >> 5) * (kStages * kStage));
+  float* const sums = params + columns;
+  const uint32_t weight = ptx::smem_u32(params) + ((group.warp - group.rank * group.warps) * I * 64 + group.lane) * 16;
+  const float whole = 1.f / (float)p.dim;
   if (p.split > 1) ptx::cluster_sync();   // the others may write to this block's shared memory
   ptx::begin_after_previous();
-  float dw[I][kLaneColumns] = {}, db[I][kLaneColumns] = {};
+  uint64_t dw[I][H] = {}, db[I][H] = {};
+  float* const part = p.parts + (int64_t)(blockIdx.x / p.split) * 2 * p.dim;
+  // The sums so far: to shared memory, or, where a group has the block to itself, to their place in the end.
   const auto put = [&](bool more) {
+    float* const to = groups > 1 ? sums + group.index * 2 * columns + first - group.rank * columns : part + first;
+    const int second = groups > 1 ? columns : p.dim;
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
-      for (int e = 0; e < kLaneColumns; ++e) {
-        float* const s = own + i * kWarpColumns + e;
-        s[0] = more ? s[0] + dw[i][e] : dw[i][e];
-        s[columns] = more ? s[columns] + db[i][e] : db[i][e];
-        dw[i][e] = db[i][e] = 0.f;
+      for (int e = 0; e < H; ++e) {
+        const int c = i * kWarpColumns + 2 * e;
+        const float2 w = unpair(dw[i][e]), b = unpair(db[i][e]);
+        if (groups > 1 || first + c < p.dim) {
+          to[c] = more ? to[c] + w.x : w.x;
+          to[second + c] = more ? to[second + c] + b.x : b.x;
+        }
+        if (groups > 1 || first + c + 1 < p.dim) {
+          to[c + 1] = more ? to[c + 1] + w.y : w.y;
+          to[second + c + 1] = more ? to[second + c + 1] + b.y : b.y;
+        }
+        dw[i][e] = db[i][e] = 0;
       }
   };
-  int turn = 0, chain = 0;
+  typename G::Lone lone[R][2];
+  const auto fetch = [&](int64_t r, int stage) {
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      lone[q][0].settle();
+      lone[q][1].settle();
+      if (r + q < p.rows) {
+        const uint32_t to = own + stage * kStage + q * kRow;
+        G::fetch(to, p.x + (r + q) * p.x_stride, begin, p.dim, lone[q][0]);
+        G::fetch(to + G::kBytes, p.dy + (r + q) * p.dy_stride, begin, p.dim, lone[q][1]);
+        if (group.lane == 0) copy_async_pair(to + 2 * G::kBytes, p.stats + 2 * (r + q));
+      }
+    }
+    copy_async_commit();
+  };
+  int64_t r = ((int64_t)(blockIdx.x / p.split) * groups + group.index) * R;
+#pragma unroll
+  for (int k = 0; k < kStages - 1; ++k) fetch(r + k * step, k);
+  put_params<PT, I>(params, p.weight, 1.f, group, begin, p.dim);
+  __syncthreads();
+  int chain = 0, stage = 0;
   bool more = false;
-  for (int64_t r = (int64_t)(blockIdx.x / p.split) * groups + group.index; r < p.rows; r += step, turn ^= 1) {
-    if (p.parts && chain++ == kNormChain) {
+  for (int turn = 0; r < p.rows; r += step, turn ^= 1) {
+    if (p.parts && chain >= kNormChain) {
       put(more);
       more = true;
-      chain = 1;
+      chain = 0;
     }
-    uint4 xr[I * C::N], gr[I * C::N];
-    C::template load<I>(p.x + r * p.x_stride, first, p.dim, xr);
-    C::template load<I>(p.dy + r * p.dy_stride, first, p.dim, gr);
-    const float mean = p.stats[2 * r], rstd = p.stats[2 * r + 1];
-    float h[I][kLaneColumns], g[I][kLaneColumns];
+    chain += R;
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-      C::unpack(xr + i * C::N, h[i]);
-      C::unpack(gr + i * C::N, g[i]);
+    for (int q = 0; q < R; ++q) {
+      lone[q][0].settle();
+      lone[q][1].settle();
+    }
+    copy_async_wait_but<kStages - 2>();
+    __syncwarp();
+    const uint32_t here = own + stage * kStage;
+    fetch(r + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);   // where the row before was
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+    uint64_t h[R][I][H], g[R][I][H];
+    float rstd[R], a[R], b[R];
 #pragma unroll
-      for (int e = 0; e < kLaneColumns; ++e) {
-        h[i][e] = (h[i][e] - mean) * rstd;
-        dw[i][e] = fmaf(g[i][e], h[i][e], dw[i][e]);
-        db[i][e] += g[i][e];
+    for (int q = 0; q < R; ++q) {
+      const float2 stats = unpair(ld_shared_u64(here + q * kRow + 2 * G::kBytes));
+      const uint64_t minus = pair(-stats.x, -stats.x), by = pair(stats.y, stats.y);
+      rstd[q] = stats.y;
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        G::read(here + q * kRow, p.x + (r + q) * p.x_stride, begin, p.dim, i, h[q][i]);
+        G::read(here + q * kRow + G::kBytes, p.dy + (r + q) * p.dy_stride, begin, p.dim, i, g[q][i]);
+#pragma unroll
+        for (int e = 0; e < H; ++e) h[q][i][e] = mul2f(add2f(h[q][i][e], minus), by);
+        if (q == 0 || r + q < p.rows) {
+#pragma unroll
+          for (int e = 0; e < H; ++e) {
+            dw[i][e] = fma2f(g[q][i][e], h[q][i][e], dw[i][e]);
+            db[i][e] = add2f(g[q][i][e], db[i][e]);
+          }
+        }
       }
     }
     if (!p.dx) continue;
-    if (p.weight) {
-      uint4 v[I * W::N];
-      W::template load<I>(p.weight, first, p.dim, v);
-#pragma unroll
-      for (int i = 0; i < I; ++i) {
-        float w[kLaneColumns];
-        W::unpack(v + i * W::N, w);
-#pragma unroll
-        for (int e = 0; e < kLaneColumns; ++e) g[i][e] *= w[e];
-      }
-    }
-    float a = 0.f, b = 0.f;   // dy is 0 behind the row's end
-#pragma unroll
-    for (int i = 0; i < I; ++i)
-#pragma unroll
-      for (int e = 0; e < kLaneColumns; ++e) {
-        a += g[i][e];
-        b = fmaf(g[i][e], h[i][e], b);
-      }
-    a = warp_sum(a);
-    b = warp_sum(b);
-    if (group.all() > 1) {
-      group.exchange(shared, turn, make_float2(a, b));
-      const float2* const of = group.of(shared, turn);
-      a = b = 0.f;
-      for (int w = group.lane; w < group.all(); w += 32) {
-        a += of[w].x;
-        b += of[w].y;
-      }
-      a = warp_sum(a);
-      b = warp_sum(b);
-    }
-    a /= (float)p.dim;
-    b /= (float)p.dim;
+    uint64_t a2[R] = {}, b2[R] = {};   // dy is 0 behind the row's end
 #pragma unroll
     for (int i = 0; i < I; ++i) {
+      uint64_t w[H];
+      get_params(weight, i, w);
 #pragma unroll
-      for (int e = 0; e < kLaneColumns; ++e) g[i][e] = (g[i][e] - a - h[i][e] * b) * rstd;
-      C::pack(g[i], xr + i * C::N);
+      for (int q = 0; q < R; ++q)
+#pragma unroll
+        for (int e = 0; e < H; ++e) {
+          g[q][i][e] = mul2f(g[q][i][e], w[e]);
+          a2[q] = add2f(g[q][i][e], a2[q]);
+          b2[q] = fma2f(g[q][i][e], h[q][i][e], b2[q]);
+        }
     }
-    C::template store<I>(p.dx + r * p.dx_stride, first, p.dim, xr);
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      a[q] = warp_sum(both(a2[q]));
+      b[q] = warp_sum(both(b2[q]));
+    }
+    if (R == 1 && group.all() > 1) {
+      group.exchange(shared, turn, make_float2(a[0], b[0]));
+      const float2* const of = group.of(shared, turn);
+      a[0] = b[0] = 0.f;
+#pragma unroll 4
+      for (int w = 0; w < group.all(); ++w) {
+        const float2 v = of[w];
+        a[0] += v.x;
+        b[0] += v.y;
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      if (r + q >= p.rows) break;
+      uint4 out[I * C::N];
+      const uint64_t minus_a = pair(-a[q] * whole, -a[q] * whole), minus_b = pair(-b[q] * whole, -b[q] * whole), by = pair(rstd[q], rstd[q]);
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+#pragma unroll
+        for (int e = 0; e < H; ++e) g[q][i][e] = mul2f(fma2f(h[q][i][e], minus_b, add2f(g[q][i][e], minus_a)), by);
+        C::pack2(g[q][i], out + i * C::N);
+      }
+      G::write(here + q * kRow, p.dx + (r + q) * p.dx_stride, begin, p.dim, out);
+    }
   }
+  ptx::let_next_begin();
   if (!p.parts) return;
   put(more);
+  if (groups == 1) return;
   __syncthreads();
-  float* const to = p.parts + (int64_t)(blockIdx.x / p.split) * 2 * p.dim;
-  for (int c = threadIdx.x; c < columns; c += blockDim.x) {
-    const int column = group.rank * columns + c;
-    if (column >= p.dim) continue;
+  for (int c = threadIdx.x; c < columns && c < p.dim; c += blockDim.x) {   // of the only block of the row
     float w = sums[c], b = sums[columns + c];
     for (int q = 1; q < groups; ++q) {
       w += sums[q * 2 * columns + c];
       b += sums[(q * 2 + 1) * columns + c];
     }
-    to[column] = w;
-    to[p.dim + column] = b;
+    part[c] = w;
+    part[p.dim + c] = b;
   }
 }
 
@@ -297,43 +439,59 @@ __global__ void __launch_bounds__(512) norm_join_kernel(const NormJoinParams p) 
 
 // ---- host side -----------------------------------------------------------------------------------------------------
 struct NormPlan {
-  int split, warps, runs, groups;
+  int split, warps, runs, rows, groups;   // rows: at a time (several only of one run, or of two); groups: of a block
 };
-static NormPlan norm_plan(int64_t dim, int most) {   // most: runs that a thread can hold
+// most: runs that a thread holds; row_warps: of a row in a block, at most; all: of a block.
+static NormPlan norm_plan(int64_t rows, int64_t dim, int most, int row_warps, int all) {
   NormPlan n;
   n.split = 1;
-  while ((int64_t)n.split * most * kWarpColumns * kNormWarps < dim) n.split *= 2;
+  while ((int64_t)n.split * most * kWarpColumns * row_warps < dim) n.split *= 2;
   const int runs = (int)((dim + (int64_t)n.split * kWarpColumns - 1) / ((int64_t)n.split * kWarpColumns));   // of 256 columns in a block
   n.warps = (runs + most - 1) / most;
   n.runs = (runs + n.warps - 1) / n.warps;
-  n.groups = n.split > 1 ? 1 : kNormWarps / n.warps;
+  n.rows = n.split == 1 && n.warps == 1 ? most / n.runs : 1;
+  n.groups = n.split > 1 ? 1 : all / n.warps;
+  const int64_t each = (rows + (int64_t)kSms * n.rows - 1) / ((int64_t)kSms * n.rows);   // few rows are spread over the SMs
+  if (n.groups > each) n.groups = each < 1 ? 1 : (int)each;
   return n;
 }
-static int64_t norm_grad_blocks(const NormPlan& n, int64_t rows) {   // times split
-  const int64_t full = (rows + n.groups - 1) / n.groups, room = kSms / n.split;
+static NormPlan norm_plan(int64_t rows, int64_t dim, int dtype) { return norm_plan(rows, dim, kNormRuns, kNormRowWarps, norm_warps(dtype)); }
+static NormPlan norm_grad_plan(int64_t rows, int64_t dim) { return norm_plan(rows, dim, kNormGradRuns, kNormGradRowWarps, kNormGradWarps); }
+static int64_t norm_grid(const NormPlan& n, int64_t rows) {   // times split
+  const int64_t each = (int64_t)n.groups * n.rows, full = (rows + each - 1) / each, room = kSms / n.split;
   return full < room ? full : room;
 }
 
+template <int DT, int PT, int R, int I>
+static int launch_norm(const NormParams& p, const NormPlan& n, cudaStream_t st) {
+  constexpr auto kernel = norm_kernel<DT, PT, R, I>;
+  constexpr int stages = norm_stages(DT) * R * Segment<DT, I>::kBytes, params = 2 * I * kWarpColumns * (int)sizeof(float);   // of a warp, of a warp of a row
+  IRIS_CHECK(allow_shared<kernel>(norm_warps(DT) * stages + kNormRowWarps * params));
+  return launch_rows(kernel, p, (unsigned)(norm_grid(n, p.rows) * n.split), n.split, n.warps * n.groups * 32,
+                     (size_t)n.warps * (n.groups * stages + params), st);
+}
 template <int DT, int PT>
 static int launch_norm(const NormParams& p, const NormPlan& n, cudaStream_t st) {
-  void (*const kernels[kNormRuns])(NormParams) = {norm_kernel<DT, PT, 1>, norm_kernel<DT, PT, 2>, norm_kernel<DT, PT, 3>, norm_kernel<DT, PT, 4>};
-  const int64_t blocks = (p.rows + n.groups - 1) / n.groups * n.split;
-  if (blocks > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "iris_layer_norm: more than 2^31 - 1 blocks");
-  return launch_rows(kernels[n.runs - 1], p, (unsigned)blocks, n.split, n.warps * n.groups * 32, 0, st);
+  return n.runs == 1   ? launch_norm<DT, PT, 4, 1>(p, n, st)
+         : n.runs == 2 ? launch_norm<DT, PT, 2, 2>(p, n, st)
+         : n.runs == 3 ? launch_norm<DT, PT, 1, 3>(p, n, st)
+                       : launch_norm<DT, PT, 1, 4>(p, n, st);
 }
-template <int DT, int PT, int I>
-static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, int64_t blocks, cudaStream_t st) {
-  constexpr auto kernel = norm_grad_kernel<DT, PT, I>;
-  const size_t bytes = p.parts ? (size_t)2 * n.groups * n.warps * I * kWarpColumns * sizeof(float) : 0;
-  if (bytes > 48 * 1024) IRIS_CHECK(allow_shared<kernel>(2 * kNormWarps * I * kWarpColumns * (int)sizeof(float)));
-  return launch_rows(kernel, p, (unsigned)(blocks * n.split), n.split, n.warps * n.groups * 32, bytes, st);
+template <int DT, int PT, int R, int I>
+static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, cudaStream_t st) {
+  constexpr auto kernel = norm_grad_kernel<DT, PT, R, I>;
+  constexpr int stages = norm_grad_stages(DT) * norm_grad_stage_bytes<DT, R, I>(), params = I * kWarpColumns * (int)sizeof(float);
+  const int sums = p.parts && n.groups > 1 ? 2 * params : 0;   // of a warp
+  IRIS_CHECK(allow_shared<kernel>(kNormGradWarps * (stages + 2 * params) + kNormGradRowWarps / 2 * params));   // one group has more parameters, but no sums
+  return launch_rows(kernel, p, (unsigned)(norm_grid(n, p.rows) * n.split), n.split, n.warps * n.groups * 32,
+                     (size_t)n.warps * (n.groups * (stages + sums) + params), st);
 }
 template <int DT, int PT>
 static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, void* dweight, void* dbias, cudaStream_t st) {
-  int64_t blocks = norm_grad_blocks(n, p.rows);
-  IRIS_CHECK(n.runs == 1 ? launch_norm_grad<DT, PT, 1>(p, n, blocks, st) : launch_norm_grad<DT, PT, 2>(p, n, blocks, st));
+  IRIS_CHECK(n.runs == 1 ? launch_norm_grad<DT, PT, 2, 1>(p, n, st) : launch_norm_grad<DT, PT, 1, 2>(p, n, st));
   if (!p.parts) return IRIS_OK;
-  return launch_rows(norm_join_kernel<PT>, NormJoinParams{p.parts, (int)blocks, p.dim, {dweight, dbias}}, (unsigned)((p.dim + 31) / 32 * 2), 1, 512, 0, st);
+  return launch_rows(norm_join_kernel<PT>, NormJoinParams{p.parts, (int)norm_grid(n, p.rows), p.dim, {dweight, dbias}}, (unsigned)((p.dim + 31) / 32 * 2), 1,
+                     512, 0, st);
 }
 
 static int check_norm(const char* fn, int64_t rows, int64_t dim, int dtype, int param_dtype) {
@@ -363,12 +521,12 @@ extern "C" int iris_layer_norm(const iris_layer_norm_args* a, void* stream) {
   IRIS_CHECK(check_matrix(fn, "y", a->y, a->dtype, a->rows, a->dim, &ys));
   IRIS_CHECK(check_params(fn, "weight", a->weight, a->param_dtype, false));
   IRIS_CHECK(check_params(fn, "bias", a->bias, a->param_dtype, false));
-  IRIS_CHECK(check_aligned(fn, "stats", a->stats, 4, false));
+  IRIS_CHECK(check_aligned(fn, "stats", a->stats, 8, false));
   if (!(a->eps >= 0.f) || std::isinf(a->eps)) return fail(IRIS_ERR_ARG, "%s: eps has to be finite and not negative", fn);
   IRIS_CHECK(check_overlap(fn, "y", "x", a->x, xs, a->y, ys, a->rows, a->dim, a->dtype));
   if (a->rows == 0) return IRIS_OK;
   const int64_t es = (int64_t)elem_size(a->dtype);
-  const NormPlan n = norm_plan(a->dim, kNormRuns);
+  const NormPlan n = norm_plan(a->rows, a->dim, a->dtype);
   NormParams p{static_cast<const char*>(a->x), static_cast<char*>(a->y), xs * es, ys * es, static_cast<const char*>(a->weight),
                static_cast<const char*>(a->bias), a->stats, a->rows, (int)a->dim, n.warps, n.split, a->eps};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -379,8 +537,8 @@ extern "C" int iris_layer_norm(const iris_layer_norm_args* a, void* stream) {
 }
 
 extern "C" size_t iris_layer_norm_workspace_bytes(int64_t rows, int64_t dim) {
-  if (rows <= 0 || dim <= 0 || dim > kNormMaxDim) return 0;
-  return (size_t)norm_grad_blocks(norm_plan(dim, kNormGradRuns), rows) * 2 * dim * sizeof(float);
+  if (rows <= 0 || rows > INT32_MAX || dim <= 0 || dim > kNormMaxDim) return 0;
+  return (size_t)norm_grid(norm_grad_plan(rows, dim), rows) * 2 * dim * sizeof(float);
 }
 
 extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void* stream) {
@@ -395,7 +553,7 @@ extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void
     IRIS_CHECK(check_overlap(fn, "dx", "x", a->x, xs, a->dx, ds, a->rows, a->dim, a->dtype));
     IRIS_CHECK(check_overlap(fn, "dx", "dy", a->dy, gs, a->dx, ds, a->rows, a->dim, a->dtype));
   }
-  IRIS_CHECK(check_aligned(fn, "stats", a->stats, 4, a->rows > 0));
+  IRIS_CHECK(check_aligned(fn, "stats", a->stats, 8, a->rows > 0));
   IRIS_CHECK(check_params(fn, "weight", a->weight, a->param_dtype, false));
   IRIS_CHECK(check_params(fn, "dweight", a->dweight, a->param_dtype, false));
   IRIS_CHECK(check_params(fn, "dbias", a->dbias, a->param_dtype, false));
@@ -413,7 +571,7 @@ extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void
     return IRIS_OK;
   }
   const int64_t es = (int64_t)elem_size(a->dtype);
-  const NormPlan n = norm_plan(a->dim, kNormGradRuns);
+  const NormPlan n = norm_grad_plan(a->rows, a->dim);
   NormGradParams p{static_cast<const char*>(a->x), static_cast<const char*>(a->dy), static_cast<char*>(a->dx), xs * es, gs * es, ds * es,
                    static_cast<const char*>(a->weight), a->stats, sums ? static_cast<float*>(a->workspace) : nullptr, a->rows, (int)a->dim, n.warps,
                    n.split};
