@@ -154,8 +154,8 @@ struct Columns {
 };
 
 // I times 256 columns of a row, from column `begin`, in a warp's shared memory at `at` (16-byte aligned, kBytes): bytes from the aligned 16
-// in which they begin.
-template <int DT, int I>
+// in which they begin.  ALIGNED: rows begin at 16 bytes, and their lengths are multiples of that.
+template <int DT, int I, bool ALIGNED = false>
 struct Segment {
   using C = Columns<DT>;
   static constexpr int ES = C::ES, N = C::N, kColumns = I * kWarpColumns, kBytes = kColumns * ES + 32;
@@ -171,6 +171,15 @@ struct Segment {
   };
   static __device__ __forceinline__ void fetch(uint32_t at, const char* row, int begin, int dim, Lone& lone) {
     const int lane = threadIdx.x & 31, bytes = dim * ES, start = begin * ES;
+    if constexpr (ALIGNED) {
+      const char* const p = row + start + lane * 16;
+      const int left = bytes - start - lane * 16;
+#pragma unroll
+      for (int k = 0; k < I * N; ++k)
+        if (begin + kColumns <= dim || k * 512 < left) copy_async(at + (k * 32 + lane) * 16, p + k * 512);
+        else ptx::st_shared_v4(at + (k * 32 + lane) * 16, make_uint4(0, 0, 0, 0));
+      return;
+    }
     const int a = (int)phase(row + start);
     const char* const somewhere = row - phase(row);   // aligned, for copies of 0 bytes
     if (begin + kColumns <= dim) {
@@ -204,7 +213,7 @@ struct Segment {
   }
   // Run i of the thread's columns; zeros behind the row's end.  After a barrier of the warp behind the copies and `settle`.
   static __device__ __forceinline__ void read(uint32_t at, const char* row, int begin, int dim, int i, uint64_t (&x)[kLaneColumns / 2]) {
-    const uint32_t a = phase(row + begin * ES);
+    const uint32_t a = ALIGNED ? 0 : phase(row + begin * ES);
     uint4 v[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -230,8 +239,8 @@ struct Segment {
     const int lane = threadIdx.x & 31, bytes = min(dim - begin, kColumns) * ES;   // of the segment
     if (bytes <= 0) return;
     char* const to = row + begin * ES;
-    const int a = (int)phase(to);
-    if (a == 0 && bytes % 16 == 0) {
+    const int a = ALIGNED ? 0 : (int)phase(to);
+    if (ALIGNED || (a == 0 && bytes % 16 == 0)) {
 #pragma unroll
       for (int k = 0; k < I * N; ++k) {
         const int b = ((k / N * 32 + lane) * N + k % N) * 16;
@@ -278,6 +287,8 @@ inline int allow_shared(int bytes) {
   if (dev < kDevices) done[dev].store(true, std::memory_order_release);
   return IRIS_OK;
 }
+// Whether rows `stride` bytes apart all begin at 16 bytes.
+inline bool aligned_rows(const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0; }
 // A matrix of rows; `stride` comes back as the elements between rows.
 inline int check_matrix(const char* fn, const char* what, const void* p, int dtype, int64_t rows, int64_t columns, int64_t* stride) {
   if (*stride == 0) *stride = columns;

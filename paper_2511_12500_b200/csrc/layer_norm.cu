@@ -20,6 +20,7 @@ constexpr int norm_warps(int dtype) { return dtype == IRIS_F32 ? 16 : 24; }
 constexpr int kNormGradWarps = 16;
 constexpr int norm_stages(int dtype) { return dtype == IRIS_F32 ? 2 : 3; }        // rows (or R of them) in shared memory
 constexpr int norm_grad_stages(int dtype) { return dtype == IRIS_F32 ? 2 : 3; }
+constexpr int kNormChain = 128;                 // rows that a thread adds up before the sum goes to the sum of such sums
 
 struct NormParams {
   const char* x;
@@ -38,14 +39,14 @@ struct NormGradParams {
   int64_t x_stride, dy_stride, dx_stride;
   const char* weight;
   const float* stats;
-  float* parts;                 // [blocks / split, 2, dim]: sums of dy h and of dy over a block's rows; nullptr: not wanted
+  float* parts;                 // [blocks / split (times groups if by_group), 2, dim]: sums of dy h and of dy; nullptr: not wanted
   int64_t rows;
-  int dim, warps, split;
+  int dim, warps, split, by_group;
 };
 
 // What a warp knows of a row, and the sum over the warps of a row, which all of its threads get.
 struct NormShared {
-  float2 of[2][norm_warps(IRIS_F16) > kNormGradRowWarps * kNormSplit ? norm_warps(IRIS_F16) : kNormGradRowWarps * kNormSplit];   // twice: one is read while the next row's is written
+  float2 of[2][kNormGradRowWarps * kNormSplit];   // twice: one is read while the next row's is written
 };
 struct Group {
   int warps, split, rank, index, warp, lane, id;   // index: of the group in its block; warp: in its row, over all blocks; id: of its barrier
@@ -71,22 +72,19 @@ struct Group {
   }
   __device__ __forceinline__ int all() const { return warps * split; }
   __device__ __forceinline__ const float2* of(const NormShared& s, int turn) const { return s.of[turn] + (split > 1 ? 0 : index * warps); }
-  // Means and squares' sums (about those means) of the warps' shares, `each` columns but for the last ones -> of the whole row.
-  __device__ __forceinline__ void join(NormShared& s, int turn, int dim, int each, float& mean, float& squares) const {
-    exchange(s, turn, make_float2(mean, squares));
-    const float2* const v = of(s, turn);
-    float m = 0.f, q = 0.f;
-#pragma unroll 4
-    for (int w = 0; w < all(); ++w) m = fmaf(v[w].x, (float)max(0, min(dim - w * each, each)), m);
-    mean = m / (float)dim;
-#pragma unroll 4
-    for (int w = 0; w < all(); ++w) {
-      const float2 x = v[w];
-      const float d = x.x - mean;
-      q += fmaf(d * d, (float)max(0, min(dim - w * each, each)), x.y);
-    }
-    squares = q;
+};
+
+// How the columns of a row are shared by its warps: `each` a warp, `rest` in the last one that has any.
+struct Shares {
+  int last;
+  float each, rest, dim;
+  __device__ __forceinline__ Shares(int each_, int dim_) {
+    last = (dim_ - 1) / each_;
+    each = (float)each_;
+    rest = (float)(dim_ - last * each_);
+    dim = (float)dim_;
   }
+  __device__ __forceinline__ float of(int warp) const { return warp < last ? each : warp == last ? rest : 0.f; }
 };
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
@@ -124,10 +122,10 @@ __device__ __forceinline__ float both(uint64_t x) {
 }
 
 // R rows at a time.
-template <int DT, int PT, int R, int I>
+template <int DT, int PT, int R, int I, bool ALIGNED>
 __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormParams p) {
   using C = Columns<DT>;
-  using G = Segment<DT, I>;
+  using G = Segment<DT, I, ALIGNED>;
   constexpr int kStages = norm_stages(DT), H = kLaneColumns / 2;
   __shared__ NormShared shared;
   extern __shared__ __align__(16) char ring[];   // [warps, stages, R] segments; weight, bias
@@ -143,31 +141,34 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
   ptx::let_next_begin();
   ptx::begin_after_previous();
   typename G::Lone lone[R];
-  const auto fetch = [&](int64_t r, int stage) {
+  const auto fetch = [&](int64_t r, const char* from, int stage) {
 #pragma unroll
     for (int q = 0; q < R; ++q) {
       lone[q].settle();
-      if (r + q < p.rows) G::fetch(own + (stage * R + q) * G::kBytes, p.x + (r + q) * p.x_stride, begin, p.dim, lone[q]);
+      if (r + q < p.rows) G::fetch(own + (stage * R + q) * G::kBytes, from + q * p.x_stride, begin, p.dim, lone[q]);
     }
     copy_async_commit();
   };
   int64_t r = ((int64_t)(blockIdx.x / p.split) * groups + group.index) * R;
+  const char* x_row = p.x + r * p.x_stride;
+  char* y_row = p.y + r * p.y_stride;
+  const int64_t x_step = step * p.x_stride, y_step = step * p.y_stride;
 #pragma unroll
-  for (int k = 0; k < kStages - 1; ++k) fetch(r + k * step, k);
+  for (int k = 0; k < kStages - 1; ++k) fetch(r + k * step, x_row + k * x_step, k);
   put_params<PT, I>(params, p.weight, 1.f, group, begin, p.dim);
   put_params<PT, I>(params + columns, p.bias, 0.f, group, begin, p.dim);
   __syncthreads();
-  const int has = max(0, min(p.dim - begin, G::kColumns));
-  const float count = (float)max(has, 1), dim = (float)p.dim;   // division, so that the mean of equal small whole numbers is that number
-  const bool full = has == G::kColumns;
+  const Shares shares(G::kColumns, p.dim);
+  const float mine = fmaxf(shares.of(group.warp), 1.f), whole = 1.f / shares.dim;
+  const bool full = begin + G::kColumns <= p.dim;
   int stage = 0;
-  for (int turn = 0; r < p.rows; r += step, turn ^= 1) {
+  for (int turn = 0; r < p.rows; r += step, x_row += x_step, y_row += y_step, turn ^= 1) {
 #pragma unroll
     for (int q = 0; q < R; ++q) lone[q].settle();
     copy_async_wait_but<kStages - 2>();
     __syncwarp();
     const uint32_t here = own + stage * (R * G::kBytes);
-    fetch(r + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);   // where the row before was
+    fetch(r + (kStages - 1) * step, x_row + (kStages - 1) * x_step, stage == 0 ? kStages - 1 : stage - 1);   // where the row before was
     stage = stage + 1 == kStages ? 0 : stage + 1;
     uint64_t x[R][I][H];
     float mean[R], squares[R];
@@ -176,15 +177,16 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
       uint64_t s = 0;
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        G::read(here + q * G::kBytes, p.x + (r + q) * p.x_stride, begin, p.dim, i, x[q][i]);
+        G::read(here + q * G::kBytes, x_row + q * p.x_stride, begin, p.dim, i, x[q][i]);
 #pragma unroll
         for (int e = 0; e < H; ++e) s = add2f(s, x[q][i][e]);
       }
       mean[q] = both(s);
     }
-    // The warp's mean, and the squares' sum about it: nothing is lost where the mean is large.
+    // The warp's mean, and the squares' sum about it: nothing is lost where the mean is large.  A quotient, so that the mean of equal small whole
+    // numbers is that number.
 #pragma unroll
-    for (int q = 0; q < R; ++q) mean[q] = warp_sum(mean[q]) / count;
+    for (int q = 0; q < R; ++q) mean[q] = warp_sum(mean[q]) / mine;
 #pragma unroll
     for (int q = 0; q < R; ++q) {
       const uint64_t minus = pair(-mean[q], -mean[q]);
@@ -212,10 +214,24 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
     }
 #pragma unroll
     for (int q = 0; q < R; ++q) squares[q] = warp_sum(squares[q]);
-    if (R == 1 && group.all() > 1) group.join(shared, turn, p.dim, G::kColumns, mean[0], squares[0]);
+    if (R == 1 && group.all() > 1) {
+      group.exchange(shared, turn, make_float2(mean[0], squares[0]));
+      const float2* const of = group.of(shared, turn);
+      float m = 0.f, s = 0.f;
+#pragma unroll 4
+      for (int w = 0; w < group.all(); ++w) m = fmaf(of[w].x, shares.of(w), m);
+      mean[0] = m / shares.dim;
+#pragma unroll 4
+      for (int w = 0; w < group.all(); ++w) {   // from the warp's mean to the row's
+        const float2 v = of[w];
+        const float d = v.x - mean[0];
+        s += fmaf(d * d, shares.of(w), v.y);
+      }
+      squares[0] = s;
+    }
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      squares[q] = 1.f / sqrtf(squares[q] / dim + p.eps);
+      squares[q] = rsqrtf(fmaf(squares[q], whole, p.eps));
       if (p.stats && group.warp == 0 && group.lane == 0 && r + q < p.rows)
         *reinterpret_cast<float2*>(p.stats + 2 * (r + q)) = make_float2(mean[q], squares[q]);
     }
@@ -235,24 +251,22 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
       uint4 out[I * C::N];
 #pragma unroll
       for (int i = 0; i < I; ++i) C::pack2(x[q][i], out + i * C::N);
-      G::write(here + q * G::kBytes, p.y + (r + q) * p.y_stride, begin, p.dim, out);
+      G::write(here + q * G::kBytes, y_row + q * p.y_stride, begin, p.dim, out);
     }
   }
 }
 
-// A block's groups add up dw and db of their columns in registers, in chains of at most kNormChain rows, then of such sums.  R rows at a time.
-constexpr int kNormChain = 128;
-
+// A block's groups add up dw and db of their columns in registers.  R rows at a time.
 template <int DT, int R, int I>
 constexpr int norm_grad_stage_bytes() { return R * (2 * Segment<DT, I>::kBytes + 16); }   // x, dy, statistics
 
-template <int DT, int PT, int R, int I>
+template <int DT, int PT, int R, int I, bool ALIGNED>
 __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const NormGradParams p) {
   using C = Columns<DT>;
-  using G = Segment<DT, I>;
+  using G = Segment<DT, I, ALIGNED>;
   constexpr int kStages = norm_grad_stages(DT), kRow = 2 * G::kBytes + 16, kStage = norm_grad_stage_bytes<DT, R, I>(), H = kLaneColumns / 2;
   __shared__ NormShared shared;
-  extern __shared__ __align__(16) char ring[];   // [warps, stages, R] segments of x, of dy, statistics; weight; with several groups sums [groups, 2, columns of the block]
+  extern __shared__ __align__(16) char ring[];   // [warps, stages, R] segments of x, of dy, statistics; weight
   const Group group(p.warps, p.split);
   const int groups = blockDim.x / (p.warps * 32);
   const int begin = group.warp * G::kColumns, first = begin + group.lane * kLaneColumns;
@@ -260,58 +274,59 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
   const int columns = p.warps * G::kColumns;   // of the block
   const uint32_t own = ptx::smem_u32(ring) + (threadIdx.x >> 5) * (kStages * kStage);
   float* const params = reinterpret_cast<float*>(ring + (blockDim.x >> 5) * (kStages * kStage));
-  float* const sums = params + columns;
   const uint32_t weight = ptx::smem_u32(params) + ((group.warp - group.rank * group.warps) * I * 64 + group.lane) * 16;
   const float whole = 1.f / (float)p.dim;
   if (p.split > 1) ptx::cluster_sync();   // the others may write to this block's shared memory
   ptx::begin_after_previous();
   uint64_t dw[I][H] = {}, db[I][H] = {};
-  float* const part = p.parts + (int64_t)(blockIdx.x / p.split) * 2 * p.dim;
-  // The sums so far: to shared memory, or, where a group has the block to itself, to their place in the end.
+  // The sums so far, to this group's part.
+  const int64_t block = blockIdx.x / p.split;
   const auto put = [&](bool more) {
-    float* const to = groups > 1 ? sums + group.index * 2 * columns + first - group.rank * columns : part + first;
-    const int second = groups > 1 ? columns : p.dim;
+    float* const to = p.parts + (p.by_group ? block * groups + group.index : block) * 2 * p.dim + first;
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
       for (int e = 0; e < H; ++e) {
         const int c = i * kWarpColumns + 2 * e;
         const float2 w = unpair(dw[i][e]), b = unpair(db[i][e]);
-        if (groups > 1 || first + c < p.dim) {
+        if (first + c < p.dim) {
           to[c] = more ? to[c] + w.x : w.x;
-          to[second + c] = more ? to[second + c] + b.x : b.x;
+          to[p.dim + c] = more ? to[p.dim + c] + b.x : b.x;
         }
-        if (groups > 1 || first + c + 1 < p.dim) {
+        if (first + c + 1 < p.dim) {
           to[c + 1] = more ? to[c + 1] + w.y : w.y;
-          to[second + c + 1] = more ? to[second + c + 1] + b.y : b.y;
+          to[p.dim + c + 1] = more ? to[p.dim + c + 1] + b.y : b.y;
         }
         dw[i][e] = db[i][e] = 0;
       }
   };
   typename G::Lone lone[R][2];
-  const auto fetch = [&](int64_t r, int stage) {
+  const auto fetch = [&](int64_t r, const char* x, const char* dy, int stage) {
 #pragma unroll
     for (int q = 0; q < R; ++q) {
       lone[q][0].settle();
       lone[q][1].settle();
       if (r + q < p.rows) {
         const uint32_t to = own + stage * kStage + q * kRow;
-        G::fetch(to, p.x + (r + q) * p.x_stride, begin, p.dim, lone[q][0]);
-        G::fetch(to + G::kBytes, p.dy + (r + q) * p.dy_stride, begin, p.dim, lone[q][1]);
+        G::fetch(to, x + q * p.x_stride, begin, p.dim, lone[q][0]);
+        G::fetch(to + G::kBytes, dy + q * p.dy_stride, begin, p.dim, lone[q][1]);
         if (group.lane == 0) copy_async_pair(to + 2 * G::kBytes, p.stats + 2 * (r + q));
       }
     }
     copy_async_commit();
   };
   int64_t r = ((int64_t)(blockIdx.x / p.split) * groups + group.index) * R;
+  const char *x_row = p.x + r * p.x_stride, *dy_row = p.dy + r * p.dy_stride;
+  char* dx_row = p.dx + r * p.dx_stride;
+  const int64_t x_step = step * p.x_stride, dy_step = step * p.dy_stride, dx_step = step * p.dx_stride;
 #pragma unroll
-  for (int k = 0; k < kStages - 1; ++k) fetch(r + k * step, k);
+  for (int k = 0; k < kStages - 1; ++k) fetch(r + k * step, x_row + k * x_step, dy_row + k * dy_step, k);
   put_params<PT, I>(params, p.weight, 1.f, group, begin, p.dim);
   __syncthreads();
   int chain = 0, stage = 0;
   bool more = false;
-  for (int turn = 0; r < p.rows; r += step, turn ^= 1) {
-    if (p.parts && chain >= kNormChain) {
+  for (int turn = 0; r < p.rows; r += step, x_row += x_step, dy_row += dy_step, dx_row += dx_step, turn ^= 1) {
+    if (p.by_group && chain >= kNormChain) {
       put(more);
       more = true;
       chain = 0;
@@ -325,21 +340,21 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
     copy_async_wait_but<kStages - 2>();
     __syncwarp();
     const uint32_t here = own + stage * kStage;
-    fetch(r + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);   // where the row before was
+    fetch(r + (kStages - 1) * step, x_row + (kStages - 1) * x_step, dy_row + (kStages - 1) * dy_step,
+          stage == 0 ? kStages - 1 : stage - 1);   // where the row before was
     stage = stage + 1 == kStages ? 0 : stage + 1;
     uint64_t h[R][I][H], g[R][I][H];
     float rstd[R], a[R], b[R];
 #pragma unroll
     for (int q = 0; q < R; ++q) {
       const float2 stats = unpair(ld_shared_u64(here + q * kRow + 2 * G::kBytes));
-      const uint64_t minus = pair(-stats.x, -stats.x), by = pair(stats.y, stats.y);
       rstd[q] = stats.y;
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        G::read(here + q * kRow, p.x + (r + q) * p.x_stride, begin, p.dim, i, h[q][i]);
-        G::read(here + q * kRow + G::kBytes, p.dy + (r + q) * p.dy_stride, begin, p.dim, i, g[q][i]);
+        G::read(here + q * kRow, x_row + q * p.x_stride, begin, p.dim, i, h[q][i]);
+        G::read(here + q * kRow + G::kBytes, dy_row + q * p.dy_stride, begin, p.dim, i, g[q][i]);
 #pragma unroll
-        for (int e = 0; e < H; ++e) h[q][i][e] = mul2f(add2f(h[q][i][e], minus), by);
+        for (int e = 0; e < H; ++e) h[q][i][e] = mul2f(add2f(h[q][i][e], pair(-stats.x, -stats.x)), pair(stats.y, stats.y));
         if (q == 0 || r + q < p.rows) {
 #pragma unroll
           for (int e = 0; e < H; ++e) {
@@ -391,15 +406,29 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
         for (int e = 0; e < H; ++e) g[q][i][e] = mul2f(fma2f(h[q][i][e], minus_b, add2f(g[q][i][e], minus_a)), by);
         C::pack2(g[q][i], out + i * C::N);
       }
-      G::write(here + q * kRow, p.dx + (r + q) * p.dx_stride, begin, p.dim, out);
+      G::write(here + q * kRow, dx_row + q * p.dx_stride, begin, p.dim, out);
     }
   }
   ptx::let_next_begin();
   if (!p.parts) return;
-  put(more);
-  if (groups == 1) return;
+  if (p.by_group || groups == 1) {
+    put(more);
+    return;
+  }
+  // The groups' sums, through the ring: [groups, 2, columns].
   __syncthreads();
-  for (int c = threadIdx.x; c < columns && c < p.dim; c += blockDim.x) {   // of the only block of the row
+  float* const sums = reinterpret_cast<float*>(ring);
+  float2* const to = reinterpret_cast<float2*>(sums + group.index * 2 * columns + first);   // a row lies in one block
+#pragma unroll
+  for (int i = 0; i < I; ++i)
+#pragma unroll
+    for (int e = 0; e < H; ++e) {
+      to[i * (kWarpColumns / 2) + e] = unpair(dw[i][e]);
+      to[columns / 2 + i * (kWarpColumns / 2) + e] = unpair(db[i][e]);
+    }
+  __syncthreads();
+  float* const part = p.parts + block * 2 * p.dim;
+  for (int c = threadIdx.x; c < p.dim; c += blockDim.x) {
     float w = sums[c], b = sums[columns + c];
     for (int q = 1; q < groups; ++q) {
       w += sums[q * 2 * columns + c];
@@ -411,28 +440,35 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
 }
 
 // dw and db: the sums of `n` parts.  32 columns a block, its warps take parts in turn.
+constexpr int kJoinWarps = 16;
 struct NormJoinParams {
   const float* parts;
   int n, dim;
   void* out[2];
 };
 template <int PT>
-__global__ void __launch_bounds__(512) norm_join_kernel(const NormJoinParams p) {
-  __shared__ float s[16][32];
+__global__ void __launch_bounds__(kJoinWarps * 32) norm_join_kernel(const NormJoinParams p) {
+  __shared__ float s[kJoinWarps][32];
   ptx::let_next_begin();
   ptx::begin_after_previous();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, which = blockIdx.x & 1, c = (blockIdx.x >> 1) * 32 + lane;
   void* const out = which ? p.out[1] : p.out[0];
   if (!out) return;
+  const float* const from = p.parts + (int64_t)which * p.dim + min(c, p.dim - 1);
   float sum = 0.f;
-  if (c < p.dim)
-    for (int i = warp; i < p.n; i += 16) sum += p.parts[((int64_t)2 * i + which) * p.dim + c];
+  for (int i = warp; i < p.n; i += kJoinWarps * 8) {
+    float x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = i + u * kJoinWarps < p.n ? __ldcg(from + (int64_t)2 * (i + u * kJoinWarps) * p.dim) : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sum += x[u];
+  }
   s[warp][lane] = sum;
   __syncthreads();
   if (warp == 0 && c < p.dim) {
     float all = 0.f;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) all += s[w][lane];
+    for (int w = 0; w < kJoinWarps; ++w) all += s[w][lane];
     static_cast<typename Elem<PT>::T*>(out)[c] = Elem<PT>::from(all);
   }
 }
@@ -441,8 +477,8 @@ __global__ void __launch_bounds__(512) norm_join_kernel(const NormJoinParams p) 
 struct NormPlan {
   int split, warps, runs, rows, groups;   // rows: at a time (several only of one run, or of two); groups: of a block
 };
-// most: runs that a thread holds; row_warps: of a row in a block, at most; all: of a block.
-static NormPlan norm_plan(int64_t rows, int64_t dim, int most, int row_warps, int all) {
+// most: runs that a thread holds; row_warps: of a row in a block, at most; warps: of a block.
+static NormPlan norm_plan(int64_t rows, int64_t dim, int most, int row_warps, int warps) {
   NormPlan n;
   n.split = 1;
   while ((int64_t)n.split * most * kWarpColumns * row_warps < dim) n.split *= 2;
@@ -450,7 +486,7 @@ static NormPlan norm_plan(int64_t rows, int64_t dim, int most, int row_warps, in
   n.warps = (runs + most - 1) / most;
   n.runs = (runs + n.warps - 1) / n.warps;
   n.rows = n.split == 1 && n.warps == 1 ? most / n.runs : 1;
-  n.groups = n.split > 1 ? 1 : all / n.warps;
+  n.groups = n.split > 1 ? 1 : warps / n.warps;
   const int64_t each = (rows + (int64_t)kSms * n.rows - 1) / ((int64_t)kSms * n.rows);   // few rows are spread over the SMs
   if (n.groups > each) n.groups = each < 1 ? 1 : (int)each;
   return n;
@@ -462,36 +498,49 @@ static int64_t norm_grid(const NormPlan& n, int64_t rows) {   // times split
   return full < room ? full : room;
 }
 
-template <int DT, int PT, int R, int I>
+// Whether a group has more than kNormChain rows, and its sums their own part.
+static bool norm_by_group(const NormPlan& n, int64_t rows) { return rows > norm_grid(n, rows) * n.groups * kNormChain; }
+static int64_t norm_parts(const NormPlan& n, int64_t rows) { return norm_grid(n, rows) * (norm_by_group(n, rows) ? n.groups : 1); }
+
+template <int DT, int PT, int R, int I, bool ALIGNED>
 static int launch_norm(const NormParams& p, const NormPlan& n, cudaStream_t st) {
-  constexpr auto kernel = norm_kernel<DT, PT, R, I>;
+  constexpr auto kernel = norm_kernel<DT, PT, R, I, ALIGNED>;
   constexpr int stages = norm_stages(DT) * R * Segment<DT, I>::kBytes, params = 2 * I * kWarpColumns * (int)sizeof(float);   // of a warp, of a warp of a row
   IRIS_CHECK(allow_shared<kernel>(norm_warps(DT) * stages + kNormRowWarps * params));
   return launch_rows(kernel, p, (unsigned)(norm_grid(n, p.rows) * n.split), n.split, n.warps * n.groups * 32,
                      (size_t)n.warps * (n.groups * stages + params), st);
 }
+template <int DT, int PT, bool ALIGNED>
+static int launch_norm(const NormParams& p, const NormPlan& n, cudaStream_t st) {
+  return n.runs == 1   ? launch_norm<DT, PT, 4, 1, ALIGNED>(p, n, st)
+         : n.runs == 2 ? launch_norm<DT, PT, 2, 2, ALIGNED>(p, n, st)
+         : n.runs == 3 ? launch_norm<DT, PT, 1, 3, ALIGNED>(p, n, st)
+                       : launch_norm<DT, PT, 1, 4, ALIGNED>(p, n, st);
+}
 template <int DT, int PT>
 static int launch_norm(const NormParams& p, const NormPlan& n, cudaStream_t st) {
-  return n.runs == 1   ? launch_norm<DT, PT, 4, 1>(p, n, st)
-         : n.runs == 2 ? launch_norm<DT, PT, 2, 2>(p, n, st)
-         : n.runs == 3 ? launch_norm<DT, PT, 1, 3>(p, n, st)
-                       : launch_norm<DT, PT, 1, 4>(p, n, st);
+  const bool aligned = p.dim * Columns<DT>::ES % 16 == 0 && aligned_rows(p.x, p.x_stride) && aligned_rows(p.y, p.y_stride);
+  return aligned ? launch_norm<DT, PT, true>(p, n, st) : launch_norm<DT, PT, false>(p, n, st);
 }
-template <int DT, int PT, int R, int I>
+template <int DT, int PT, int R, int I, bool ALIGNED>
 static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, cudaStream_t st) {
-  constexpr auto kernel = norm_grad_kernel<DT, PT, R, I>;
-  constexpr int stages = norm_grad_stages(DT) * norm_grad_stage_bytes<DT, R, I>(), params = I * kWarpColumns * (int)sizeof(float);
-  const int sums = p.parts && n.groups > 1 ? 2 * params : 0;   // of a warp
-  IRIS_CHECK(allow_shared<kernel>(kNormGradWarps * (stages + 2 * params) + kNormGradRowWarps / 2 * params));   // one group has more parameters, but no sums
-  return launch_rows(kernel, p, (unsigned)(norm_grid(n, p.rows) * n.split), n.split, n.warps * n.groups * 32,
-                     (size_t)n.warps * (n.groups * (stages + sums) + params), st);
+  constexpr auto kernel = norm_grad_kernel<DT, PT, R, I, ALIGNED>;
+  constexpr int stages = norm_grad_stages(DT) * norm_grad_stage_bytes<DT, R, I>(), params = I * kWarpColumns * (int)sizeof(float);   // of a warp, of a warp of a row
+  static_assert(stages >= 2 * params, "the groups' sums take the place of the rows");
+  IRIS_CHECK(allow_shared<kernel>(kNormGradWarps * stages + kNormGradRowWarps * params));
+  return launch_rows(kernel, p, (unsigned)(norm_grid(n, p.rows) * n.split), n.split, n.warps * n.groups * 32, (size_t)n.warps * (n.groups * stages + params), st);
+}
+template <int DT, int PT, bool ALIGNED>
+static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, cudaStream_t st) {
+  return n.runs == 1 ? launch_norm_grad<DT, PT, 2, 1, ALIGNED>(p, n, st) : launch_norm_grad<DT, PT, 1, 2, ALIGNED>(p, n, st);
 }
 template <int DT, int PT>
 static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, void* dweight, void* dbias, cudaStream_t st) {
-  IRIS_CHECK(n.runs == 1 ? launch_norm_grad<DT, PT, 2, 1>(p, n, st) : launch_norm_grad<DT, PT, 1, 2>(p, n, st));
+  const bool aligned = p.dim * Columns<DT>::ES % 16 == 0 && aligned_rows(p.x, p.x_stride) && aligned_rows(p.dy, p.dy_stride) && aligned_rows(p.dx, p.dx_stride);
+  IRIS_CHECK(aligned ? launch_norm_grad<DT, PT, true>(p, n, st) : launch_norm_grad<DT, PT, false>(p, n, st));
   if (!p.parts) return IRIS_OK;
-  return launch_rows(norm_join_kernel<PT>, NormJoinParams{p.parts, (int)norm_grid(n, p.rows), p.dim, {dweight, dbias}}, (unsigned)((p.dim + 31) / 32 * 2), 1,
-                     512, 0, st);
+  return launch_rows(norm_join_kernel<PT>, NormJoinParams{p.parts, (int)norm_parts(n, p.rows), p.dim, {dweight, dbias}}, (unsigned)((p.dim + 31) / 32 * 2), 1,
+                     kJoinWarps * 32, 0, st);
 }
 
 static int check_norm(const char* fn, int64_t rows, int64_t dim, int dtype, int param_dtype) {
@@ -538,7 +587,7 @@ extern "C" int iris_layer_norm(const iris_layer_norm_args* a, void* stream) {
 
 extern "C" size_t iris_layer_norm_workspace_bytes(int64_t rows, int64_t dim) {
   if (rows <= 0 || rows > INT32_MAX || dim <= 0 || dim > kNormMaxDim) return 0;
-  return (size_t)norm_grid(norm_grad_plan(rows, dim), rows) * 2 * dim * sizeof(float);
+  return (size_t)norm_parts(norm_grad_plan(rows, dim), rows) * 2 * dim * sizeof(float);
 }
 
 extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void* stream) {
@@ -574,7 +623,7 @@ extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void
   const NormPlan n = norm_grad_plan(a->rows, a->dim);
   NormGradParams p{static_cast<const char*>(a->x), static_cast<const char*>(a->dy), static_cast<char*>(a->dx), xs * es, gs * es, ds * es,
                    static_cast<const char*>(a->weight), a->stats, sums ? static_cast<float*>(a->workspace) : nullptr, a->rows, (int)a->dim, n.warps,
-                   n.split};
+                   n.split, sums && norm_by_group(n, a->rows)};
   const bool wide = a->param_dtype == IRIS_F32;
   if (a->dtype == IRIS_BF16)
     return wide ? launch_norm_grad<IRIS_BF16, IRIS_F32>(p, n, a->dweight, a->dbias, st) : launch_norm_grad<IRIS_BF16, IRIS_BF16>(p, n, a->dweight, a->dbias, st);
