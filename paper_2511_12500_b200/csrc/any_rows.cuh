@@ -275,15 +275,16 @@ struct Segment {
 };
 
 // ---- host side -----------------------------------------------------------------------------------------------------
-// Lets a kernel have up to `bytes` of dynamic shared memory on the current device, once.
+// Lets a kernel have up to `bytes` of dynamic shared memory on the current device, and clusters of more than 8 blocks, once.
 template <auto KERNEL>
-inline int allow_shared(int bytes) {
+inline int allow_shared(int bytes, bool large_clusters = false) {
   constexpr int kDevices = 64;
   static std::atomic<bool> done[kDevices] = {};   // calls may come from several threads; the setting may be made twice
   int dev = -1;
   IRIS_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < kDevices && done[dev].load(std::memory_order_acquire)) return IRIS_OK;
   IRIS_CUDA_TRY(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  if (large_clusters) IRIS_CUDA_TRY(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   if (dev < kDevices) done[dev].store(true, std::memory_order_release);
   return IRIS_OK;
 }

@@ -79,30 +79,50 @@ static int launch_embed(const EmbedParams& p, cudaStream_t st) {
 
 // ---- gradient: sorted tokens ---------------------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
-constexpr int kSortBlocks = 8;      // one cluster
+constexpr int kSortBlocks = 16;     // one cluster
 constexpr int kSortMaxBits = 10;    // of a digit
 
 struct SortParams {
   const int64_t* tokens;
   int n;
-  uint32_t vocab, per, present;     // present: a bit for each shard that is there
+  uint32_t vocab, per, present;     // present: a bit for each shard that is there, all set: each is
   uint32_t *keys[2], *places[2];    // of pass 0, 2, .. and 1, 3, ..
   uint32_t* used;                   // a bit for each row of the table that a token names; nullptr: not wanted
-  int passes, bits, split;
+  int passes, split;
 };
 
 __device__ __forceinline__ uint32_t sort_key(const SortParams& p, int64_t t) {   // vocab: no token, behind all others
   if (t < 0 || t >= p.vocab) return p.vocab;
-  return p.present >> ((uint32_t)t / p.per) & 1 ? (uint32_t)t : p.vocab;
+  return p.present == ~0u || p.present >> ((uint32_t)t / p.per) & 1 ? (uint32_t)t : p.vocab;
 }
 
 // Tokens in rising order, equal ones in the order of their places, so that the sums over them have one order: a radix sort by one cluster.
 // Each warp has a run of the places and counts its digits; a digit's places follow from the counts of all warps before; then the warps
 // place their runs, 32 at a time.  Buffers lie in global memory (L2); what one block writes and another reads is ordered by the cluster's barrier.
+// Bound by latencies: kSortItems loads of a thread are under way at a time, and keys stay in registers between counting and placing where a thread has no more
+// than that.  Threads with equal digits find one another by a vote on each bit, as the instruction that finds them at once takes far longer (65536
+// tokens of 16 bits: 40 us with it).
+constexpr int kSortItems = 8;
+
+// The threads of the warp that are there and have the same digit.
+template <int BITS>
+__device__ __forceinline__ uint32_t same_digit(uint32_t digit, bool there) {
+  uint32_t same = __ballot_sync(~0u, there);
+#pragma unroll
+  for (int b = 0; b < BITS; ++b) {
+    const bool one = digit >> b & 1;
+    const uint32_t ones = __ballot_sync(~0u, one);
+    same &= one ? ones : ~ones;
+  }
+  return same;
+}
+
+template <int BITS>
 __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_constant__ SortParams p) {
   extern __shared__ uint32_t count[];   // [kSortWarps, digits]; totals [split, digits]; base [digits]
   __shared__ uint32_t of_warp[kSortWarps];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, digits = 1 << p.bits;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  constexpr int digits = 1 << BITS;
   const int rank = p.split > 1 ? (int)ptx::cluster_ctarank() : 0;
   uint32_t* const mine = count + warp * digits;
   uint32_t* const totals = count + kSortWarps * digits;
@@ -111,34 +131,56 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
   const int64_t b64 = (int64_t)(rank * kSortWarps + warp) * each;
   const int begin = (int)(b64 < p.n ? b64 : p.n), end = (int)(b64 + each < p.n ? b64 + each : p.n);
   ptx::let_next_begin();
-  if (p.split > 1) ptx::cluster_sync();
   ptx::begin_after_previous();
   if (p.used)
     for (uint32_t i = rank * kSortThreads + tid; i < (p.vocab + 31) / 32; i += p.split * kSortThreads) p.used[i] = 0;
+  if (p.split > 1) ptx::cluster_sync();   // behind it all blocks write to one another, and to `used`
+  const bool held = each <= 32 * kSortItems;
+  uint32_t key[kSortItems], same[kSortItems];
   for (int pass = 0; pass < p.passes; ++pass) {
-    const int shift = pass * p.bits;
+    const int shift = pass * BITS;
     const uint32_t *const keys = p.keys[pass & 1 ^ 1], *const places = p.places[pass & 1 ^ 1];
     uint32_t *const to_keys = p.keys[pass & 1], *const to_places = p.places[pass & 1];
-    const auto key_at = [&](int i) { return pass ? __ldcg(keys + i) : sort_key(p, p.tokens[i]); };
+    const auto load = [&](int at) {
+      if (pass) {
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) key[k] = at + k * 32 + lane < end ? __ldcg(keys + at + k * 32 + lane) : 0;
+      } else {
+        int64_t t[kSortItems];
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) t[k] = at + k * 32 + lane < end ? p.tokens[at + k * 32 + lane] : -1;
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) key[k] = sort_key(p, t[k]);
+      }
+    };
     for (int i = tid; i < kSortWarps * digits; i += kSortThreads) count[i] = 0;
     __syncthreads();
-    for (int i = begin + lane; i - lane < end; i += 32) {
-      const uint32_t d = i < end ? key_at(i) >> shift & (digits - 1) : ~0u;
-      const uint32_t same = __match_any_sync(~0u, d);
-      if (i < end && (same & ((1u << lane) - 1)) == 0) mine[d] += __popc(same);
-      __syncwarp();
+    for (int at = begin; at < end; at += 32 * kSortItems) {
+      load(at);
+#pragma unroll
+      for (int k = 0; k < kSortItems; ++k) {
+        if (at + k * 32 >= end) break;
+        const bool there = at + k * 32 + lane < end;
+        const uint32_t d = key[k] >> shift & (digits - 1);
+        same[k] = same_digit<BITS>(d, there);
+        if (there && (same[k] & ((1u << lane) - 1)) == 0) mine[d] += __popc(same[k]);
+        __syncwarp();
+        if (pass == 0 && p.used && there && key[k] < p.vocab) atomicOr(p.used + (key[k] >> 5), 1u << (key[k] & 31));
+      }
     }
     __syncthreads();
     if (tid < digits) {
-      uint32_t sum = 0;
+      uint32_t c[kSortWarps], sum = 0;
+#pragma unroll
+      for (int w = 0; w < kSortWarps; ++w) c[w] = count[w * digits + tid];
+#pragma unroll
       for (int w = 0; w < kSortWarps; ++w) {
-        const uint32_t c = count[w * digits + tid];
         count[w * digits + tid] = sum;
-        sum += c;
+        sum += c[w];
       }
-      for (int s = 0; s < p.split; ++s)
-        if (p.split > 1) ptx::st_shared_cluster_u32(ptx::mapa(ptx::smem_u32(totals + rank * digits + tid), s), sum);
-        else totals[tid] = sum;
+      if (p.split > 1)
+        for (int s = 0; s < p.split; ++s) ptx::st_shared_cluster_u32(ptx::mapa(ptx::smem_u32(totals + rank * digits + tid), s), sum);
+      else totals[tid] = sum;
     }
     if (p.split > 1) ptx::cluster_sync();
     else __syncthreads();
@@ -166,33 +208,39 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
     w = __shfl_sync(~0u, w, max(warp - 1, 0));
     if (tid < digits) base[tid] = up - all + (warp ? w : 0) + before;
     __syncthreads();
-    for (int i = begin + lane; i - lane < end; i += 32) {
-      const uint32_t key = i < end ? key_at(i) : 0, d = i < end ? key >> shift & (digits - 1) : ~0u;
-      const uint32_t same = __match_any_sync(~0u, d), lower = same & ((1u << lane) - 1);
-      uint32_t at = 0;
-      if (i < end) {
-        at = base[d] + mine[d] + __popc(lower);
-        to_keys[at] = key;
-        to_places[at] = pass ? __ldcg(places + i) : (uint32_t)i;
+    for (int at = begin; at < end; at += 32 * kSortItems) {
+      if (!held) load(at);
+      uint32_t place[kSortItems];
+#pragma unroll
+      for (int k = 0; k < kSortItems; ++k) {
+        const int i = at + k * 32 + lane;
+        place[k] = pass && i < end ? __ldcg(places + i) : (uint32_t)i;
       }
-      __syncwarp();
-      if (i < end && lower == 0) mine[d] += __popc(same);
-      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < kSortItems; ++k) {
+        if (at + k * 32 >= end) break;
+        const bool there = at + k * 32 + lane < end;
+        const uint32_t d = key[k] >> shift & (digits - 1);
+        if (!held) same[k] = same_digit<BITS>(d, there);
+        const uint32_t lower = same[k] & ((1u << lane) - 1);
+        if (there) {
+          const uint32_t to = base[d] + mine[d] + __popc(lower);
+          to_keys[to] = key[k];
+          to_places[to] = place[k];
+        }
+        __syncwarp();
+        if (there && lower == 0) mine[d] += __popc(same[k]);
+        __syncwarp();
+      }
     }
     if (p.split > 1) ptx::cluster_sync();
     else __syncthreads();
-  }
-  if (!p.used) return;
-  const uint32_t* const keys = p.keys[p.passes & 1 ^ 1];
-  for (int i = begin + lane; i < end; i += 32) {
-    const uint32_t key = __ldcg(keys + i);
-    if (key < p.vocab && (i == 0 || __ldcg(keys + i - 1) != key)) atomicOr(p.used + (key >> 5), 1u << (key & 31));
   }
 }
 
 // ---- gradient: sums ------------------------------------------------------------------------------------------------
 constexpr int kSumThreads = 256, kSumWarps = kSumThreads / 32;
-constexpr int kFillBytes = 2048;    // of a row that a warp clears at a time
+constexpr int kFillRows = 8, kFillBytes = 2048;   // that a warp clears
 
 struct EmbedGradParams {
   const char* dy;
@@ -205,7 +253,7 @@ struct EmbedGradParams {
   uint32_t vocab, per;
   unsigned sum_blocks;
   float scale;
-  int accumulate, aligned;
+  int accumulate, aligned;          // aligned: grad_out and the shards begin at 16 bytes
 };
 
 template <int GT>
@@ -213,39 +261,40 @@ __device__ __forceinline__ char* table_row(const EmbedGradParams& p, uint32_t v)
   const uint32_t r = v / p.per;
   return p.shard[r] ? p.shard[r] + (int64_t)(v - r * p.per) * p.shard_stride : nullptr;
 }
-// All threads of a warp: their columns of row v, from column `begin` on; `at`: shared memory of the warp's, Segment<GT, 1>::kBytes.
-template <int GT>
-__device__ __forceinline__ void write_row(const EmbedGradParams& p, uint32_t v, uint32_t at, int begin, const float (&sum)[kLaneColumns]) {
+// All threads of a warp: their columns of row v, from column `begin` on; `at`: shared memory of the warp's, Segment<GT, I>::kBytes.
+template <int GT, int I, bool ALIGNED>
+__device__ __forceinline__ void write_row(const EmbedGradParams& p, uint32_t v, uint32_t at, int begin, const uint64_t (&sum)[I][kLaneColumns / 2]) {
   using C = Columns<GT>;
   char* const row = table_row<GT>(p, v);
-  float x[kLaneColumns];
+  uint4 w[I * C::N];
 #pragma unroll
-  for (int e = 0; e < kLaneColumns; ++e) x[e] = sum[e] * p.scale;
-  uint4 w[C::N];
-  if (p.accumulate) {
-    float old[kLaneColumns];
-    C::load(row, begin + (threadIdx.x & 31) * kLaneColumns, p.dim, old);
+  for (int i = 0; i < I; ++i) {
+    uint64_t x[kLaneColumns / 2];
 #pragma unroll
-    for (int e = 0; e < kLaneColumns; ++e) x[e] += old[e];
+    for (int e = 0; e < kLaneColumns / 2; ++e) x[e] = mul2f(sum[i][e], pair(p.scale, p.scale));
+    if (p.accumulate) {
+      float old[kLaneColumns];
+      C::load(row, begin + i * kWarpColumns + (threadIdx.x & 31) * kLaneColumns, p.dim, old);
+#pragma unroll
+      for (int e = 0; e < kLaneColumns / 2; ++e) x[e] = add2f(x[e], pair(old[2 * e], old[2 * e + 1]));
+    }
+    C::pack2(x, w + i * C::N);
   }
-  C::pack(x, w);
   __syncwarp();
-  Segment<GT, 1>::write(at, row, begin, p.dim, w);
+  Segment<GT, I, ALIGNED>::write(at, row, begin, p.dim, w);
 }
 
-// Zeros in the rows that no token names: a warp has 32 rows and kFillBytes of each.
+// Zeros in the rows that no token names: a warp has kFillRows rows and kFillBytes of each.
 template <int GT>
 __device__ __forceinline__ void fill_rows(const EmbedGradParams& p, int64_t unit) {
   constexpr int ES = Columns<GT>::ES;
-  const uint32_t word = (uint32_t)(unit / p.fill_parts);
+  const int64_t group = unit / p.fill_parts;
   const int part = (int)(unit % p.fill_parts), lane = threadIdx.x & 31;
-  if (word >= (p.vocab + 31) / 32) return;
-  const uint32_t used = p.used[word];
-  for (int b = 0; b < 32; ++b) {
-    const uint32_t v = word * 32 + b;
-    if (v >= p.vocab) return;
+  if (group * kFillRows >= p.vocab) return;
+  const uint32_t v0 = (uint32_t)group * kFillRows, used = p.used[v0 >> 5] >> (v0 & 31);
+  for (int b = 0; b < kFillRows && v0 + b < p.vocab; ++b) {
     if (used >> b & 1) continue;
-    char* const row = table_row<GT>(p, v);
+    char* const row = table_row<GT>(p, v0 + b);
     if (!row) continue;
     char* const lo = row + (int64_t)part * kFillBytes;
     char* const hi = row + min((int64_t)p.dim * ES, (int64_t)(part + 1) * kFillBytes);
@@ -257,15 +306,15 @@ __device__ __forceinline__ void fill_rows(const EmbedGradParams& p, int64_t unit
 // in other chunks leaves its sums in `parts`, for embed_join_kernel.
 //
 // The rows are on their way to shared memory kSumStages ahead.
-template <int DT>
-constexpr int sum_stages() { return DT == IRIS_F32 ? 8 : 12; }   // 8 KB or 6 KB a warp
-template <int DT, int GT>
-constexpr int sum_bytes() { return sum_stages<DT>() * Segment<DT, 1>::kBytes + Segment<GT, 1>::kBytes; }   // of a warp
+template <int DT, int I>
+constexpr int sum_stages() { return (DT == IRIS_F32 ? 8 : 12) / I; }   // about 8 KB or 6 KB a warp
+template <int DT, int GT, int I>
+constexpr int sum_bytes() { return sum_stages<DT, I>() * Segment<DT, I>::kBytes + Segment<GT, I>::kBytes; }   // of a warp
 
-template <int DT, int GT>
+template <int DT, int GT, int I, bool ALIGNED>
 __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_constant__ EmbedGradParams p) {
-  using G = Segment<DT, 1>;
-  constexpr int kStages = sum_stages<DT>();
+  using G = Segment<DT, I, ALIGNED>;
+  constexpr int kStages = sum_stages<DT, I>(), H = kLaneColumns / 2;
   extern __shared__ __align__(16) char ring[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   ptx::let_next_begin();
@@ -275,9 +324,9 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
     return;
   }
   const int64_t unit = (int64_t)blockIdx.x * kSumWarps + warp;
-  const int c = (int)(unit / p.tiles), column = (int)(unit % p.tiles) * kWarpColumns, first = column + lane * kLaneColumns;
+  const int c = (int)(unit / p.tiles), column = (int)(unit % p.tiles) * G::kColumns, first = column + lane * kLaneColumns;
   if (c >= p.chunks) return;
-  const uint32_t own = ptx::smem_u32(ring) + warp * sum_bytes<DT, GT>(), out = own + kStages * G::kBytes;
+  const uint32_t own = ptx::smem_u32(ring) + warp * sum_bytes<DT, GT, I>(), out = own + kStages * G::kBytes;
   const int begin = c * p.chunk, end = min(p.n, begin + p.chunk);
   // The places and tokens of 32 entries are held by the threads, and the next 32 places, as copies begin ahead.
   const auto key_of = [&](int i) { return i < end ? p.keys[i] : p.vocab; };
@@ -286,37 +335,37 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
   if (now >= p.vocab) return;
   bool goes_on = begin > 0 && p.keys[begin - 1] == now;   // the run came from the chunk before
   uint32_t key = key_of(begin + lane), place = place_of(begin + lane), next_place = place_of(begin + 32 + lane);
-  uint64_t sum[kLaneColumns / 2] = {};
+  uint64_t sum[I][H] = {};
   typename G::Lone lone;
   const auto row_of = [&](uint32_t i) { return p.dy + (int64_t)i * p.dy_stride; };
-  const auto fetch = [&](int i, int base, int stage) {   // base: of `place`
+  const auto fetch = [&](int i, int base, uint32_t to) {   // base: of `place`
     lone.settle();
     if (i < end) {
       const uint32_t at = __shfl_sync(~0u, i - base < 32 ? place : next_place, (i - base) & 31);
-      G::fetch(own + stage * G::kBytes, row_of(at), column, p.dim, lone);
+      G::fetch(to, row_of(at), column, p.dim, lone);
     }
     copy_async_commit();
   };
   const auto finish = [&](bool more) {   // more: the run goes on in the next chunk
-    float s[kLaneColumns];
-#pragma unroll
-    for (int e = 0; e < kLaneColumns / 2; ++e) {
-      const float2 f = unpair(sum[e]);
-      s[2 * e] = f.x;
-      s[2 * e + 1] = f.y;
-    }
     if (!goes_on && !more) {
-      write_row<GT>(p, now, out, column, s);
+      write_row<GT, I, ALIGNED>(p, now, out, column, sum);
     } else {
-      float* const to = p.parts + ((int64_t)2 * c + !goes_on) * p.dim;
+      float* const to = p.parts + ((int64_t)2 * c + !goes_on) * p.dim + first;
 #pragma unroll
-      for (int e = 0; e < kLaneColumns; ++e)
-        if (first + e < p.dim) to[first + e] = s[e];
+      for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int e = 0; e < H; ++e) {
+          const float2 s = unpair(sum[i][e]);
+          const int at = i * kWarpColumns + 2 * e;
+          if (first + at < p.dim) to[at] = s.x;
+          if (first + at + 1 < p.dim) to[at + 1] = s.y;
+        }
     }
   };
 #pragma unroll 1
-  for (int k = 0; k < kStages - 1; ++k) fetch(begin + k, begin, k);
-  int base = begin, stage = 0;
+  for (int k = 0; k < kStages - 1; ++k) fetch(begin + k, begin, own + k * G::kBytes);
+  int base = begin;
+  uint32_t here = own, before = own + (kStages - 1) * G::kBytes;
 #pragma unroll 1
   for (int i = begin; i < end; ++i) {
     if (i - base == 32) {
@@ -325,73 +374,129 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
       key = key_of(base + lane);
       next_place = place_of(base + 32 + lane);
     }
-    const uint32_t k = __shfl_sync(~0u, key, i - base), at = __shfl_sync(~0u, place, i - base);
+    const uint32_t k = __shfl_sync(~0u, key, i - base);
     if (k != now) {
       finish(false);
       if (k >= p.vocab) break;
       now = k;
       goes_on = false;
 #pragma unroll
-      for (int e = 0; e < kLaneColumns / 2; ++e) sum[e] = 0;
+      for (int r = 0; r < I; ++r)
+#pragma unroll
+        for (int e = 0; e < H; ++e) sum[r][e] = 0;
     }
     lone.settle();
     copy_async_wait_but<kStages - 2>();
     __syncwarp();
-    fetch(i + kStages - 1, base, stage == 0 ? kStages - 1 : stage - 1);
-    uint64_t x[kLaneColumns / 2];
-    G::read(own + stage * G::kBytes, row_of(at), column, p.dim, 0, x);
+    fetch(i + kStages - 1, base, before);
+    const char* const row = ALIGNED ? nullptr : row_of(__shfl_sync(~0u, place, i - base));
 #pragma unroll
-    for (int e = 0; e < kLaneColumns / 2; ++e) sum[e] = add2f(sum[e], x[e]);
-    stage = stage + 1 == kStages ? 0 : stage + 1;
+    for (int r = 0; r < I; ++r) {
+      uint64_t x[H];
+      G::read(here, row, column, p.dim, r, x);
+#pragma unroll
+      for (int e = 0; e < H; ++e) sum[r][e] = add2f(sum[r][e], x[e]);
+    }
+    before = here;
+    here = here == own + (kStages - 1) * G::kBytes ? own : here + G::kBytes;
     if (i + 1 == end) finish(end < p.n && p.keys[end] == now);
   }
   copy_async_wait();   // a block does not end while copies are under way
 }
 
-// Runs that go over several chunks: the sums of their parts, by the block of the chunk where a run begins; its warps take the parts in turn.
+// Runs that go over several chunks: the sums of their parts.  A warp looks after the run that begins in a chunk and goes on beyond it, over 256 columns;
+// the parts of a long one are shared by the warps of the block.
+constexpr int kJoinWarps = 16, kLongRun = 16;
+
 template <int GT>
-__global__ void __launch_bounds__(kSumThreads) embed_join_kernel(const __grid_constant__ EmbedGradParams p) {
-  __shared__ float sums[kSumWarps][kWarpColumns];
-  __shared__ __align__(16) char out[Segment<GT, 1>::kBytes];
+__global__ void __launch_bounds__(kJoinWarps * 32) embed_join_kernel(const __grid_constant__ EmbedGradParams p) {
+  constexpr int kOut = Segment<GT, 1>::kBytes;
+  __shared__ __align__(16) char out[kJoinWarps][kOut > kWarpColumns * 4 ? kOut : kWarpColumns * 4];
+  __shared__ int lasts[kJoinWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   ptx::let_next_begin();
   ptx::begin_after_previous();
-  const int c = (int)(blockIdx.x / p.tiles), first = (int)(blockIdx.x % p.tiles) * kWarpColumns + lane * kLaneColumns;
-  const int begin = c * p.chunk, end = min(p.n, begin + p.chunk);
-  if (end >= p.n) return;
-  const uint32_t key = p.keys[end - 1];
-  if (key >= p.vocab || p.keys[end] != key || (begin > 0 && p.keys[begin - 1] == key)) return;
-  int last = c + 1;   // the chunks c + 1 .. last - 1 begin with the run
-  for (;;) {
-    const int i = last + lane;
-    const uint32_t there = __ballot_sync(~0u, i < p.chunks && p.keys[(int64_t)i * p.chunk < p.n ? i * p.chunk : 0] == key);
-    last += __popc(there);   // of consecutive chunks, as the keys are sorted
-    if (there != ~0u) break;
+  const int tiles = (p.dim + kWarpColumns - 1) / kWarpColumns;
+  const int c0 = (int)(blockIdx.x / tiles) * kJoinWarps, column = (int)(blockIdx.x % tiles) * kWarpColumns, first = column + lane * kLaneColumns;
+  const auto key_at = [&](int64_t i) { return i < p.n ? p.keys[i] : p.vocab; };   // vocab: no token
+  // The chunks c + 1 .. last - 1 begin with the run of chunk c (or there is none: 0).
+  const auto last_of = [&](int c) -> int {
+    const int64_t begin = (int64_t)c * p.chunk, end = begin + p.chunk;
+    const uint32_t key = key_at(end - 1), after = key_at(end), before = begin ? key_at(begin - 1) : p.vocab;
+    if (key >= p.vocab || after != key || before == key) return 0;
+    int last = c + 1;
+    for (;;) {
+      const uint32_t there = __ballot_sync(~0u, last + lane < p.chunks && key_at((int64_t)(last + lane) * p.chunk) == key);
+      last += __popc(there);   // of consecutive chunks, as the keys are sorted
+      if (there != ~0u) return last;
+    }
+  };
+  float sum[kLaneColumns];
+  const auto add = [&](int c, int from, int step, int last) {   // parts from, from + step .. of the run of chunk c
+#pragma unroll
+    for (int e = 0; e < kLaneColumns; ++e) sum[e] = 0.f;
+    for (int i = from; i < last; i += 4 * step) {
+      float x[4][kLaneColumns];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int k = i + u * step;
+        const float* const at = p.parts + ((int64_t)2 * k + (k == c)) * p.dim + first;
+        if (p.dim % 4 == 0) {
+          const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+          const float4 a = k < last && first < p.dim ? *reinterpret_cast<const float4*>(at) : none;
+          const float4 b = k < last && first + 4 < p.dim ? *reinterpret_cast<const float4*>(at + 4) : none;
+          x[u][0] = a.x, x[u][1] = a.y, x[u][2] = a.z, x[u][3] = a.w, x[u][4] = b.x, x[u][5] = b.y, x[u][6] = b.z, x[u][7] = b.w;
+        } else {
+#pragma unroll
+          for (int e = 0; e < kLaneColumns; ++e) x[u][e] = k < last && first + e < p.dim ? at[e] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int e = 0; e < kLaneColumns; ++e) sum[e] += x[u][e];
+    }
+  };
+  const auto write = [&](int c, uint32_t at) {
+    uint64_t x[1][kLaneColumns / 2];
+#pragma unroll
+    for (int e = 0; e < kLaneColumns / 2; ++e) x[0][e] = pair(sum[2 * e], sum[2 * e + 1]);
+    write_row<GT, 1, false>(p, p.keys[(int64_t)c * p.chunk + p.chunk - 1], at, column, x);
+  };
+  const int c = c0 + warp, last = c < p.chunks ? last_of(c) : 0;
+  if (lane == 0) lasts[warp] = last - c > kLongRun ? last : 0;
+  if (last && last - c <= kLongRun) {
+    add(c, c, 1, last);
+    write(c, ptx::smem_u32(out[warp]));
   }
-  float sum[kLaneColumns] = {};
-  for (int i = c + warp; i < last; i += kSumWarps) {
-    const float* const from = p.parts + ((int64_t)2 * i + (i == c)) * p.dim;
+  for (int w = 0; w < kJoinWarps; ++w) {
+    __syncthreads();
+    const int run = c0 + w, until = lasts[w];
+    if (!until) continue;   // all warps
+    add(run, run + warp, kJoinWarps, until);
+    float* const own = reinterpret_cast<float*>(out[warp]);
+    __syncwarp();
 #pragma unroll
-    for (int e = 0; e < kLaneColumns; ++e) sum[e] += first + e < p.dim ? from[first + e] : 0.f;
+    for (int e = 0; e < kLaneColumns; ++e) own[lane * kLaneColumns + e] = sum[e];
+    __syncthreads();
+    if (warp == 0) {
+      for (int v = 1; v < kJoinWarps; ++v)
+#pragma unroll
+        for (int e = 0; e < kLaneColumns; ++e) sum[e] += reinterpret_cast<const float*>(out[v])[lane * kLaneColumns + e];
+      write(run, ptx::smem_u32(out[0]));
+    }
   }
-#pragma unroll
-  for (int e = 0; e < kLaneColumns; ++e) sums[warp][lane * kLaneColumns + e] = sum[e];
-  __syncthreads();
-  if (warp) return;
-  for (int w = 1; w < min(kSumWarps, last - c); ++w)
-#pragma unroll
-    for (int e = 0; e < kLaneColumns; ++e) sum[e] += sums[w][lane * kLaneColumns + e];
-  write_row<GT>(p, key, ptx::smem_u32(out), first - lane * kLaneColumns, sum);
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
 struct EmbedGradPlan {
-  int chunk, chunks, tiles;
+  int chunk, chunks, runs, tiles;   // runs: of 256 columns that a warp adds up
   size_t list, used, parts, bytes;   // list: of one list of n; offsets of the others
 };
 static EmbedGradPlan embed_grad_plan(int64_t n, int64_t vocab, int64_t dim) {
   EmbedGradPlan g;
-  g.tiles = (int)((dim + kWarpColumns - 1) / kWarpColumns);
+  g.runs = dim > kWarpColumns ? 2 : 1;
+  g.tiles = (int)((dim + g.runs * kWarpColumns - 1) / (g.runs * kWarpColumns));
   // About 32 warps an SM, chunks of 16 to 256 (their parts are written and read again: 16 bytes a column for two).
   int64_t chunk = n * g.tiles / (kSms * 32) + 1;
   chunk = chunk < 16 ? 16 : chunk > 256 ? 256 : chunk;
@@ -404,14 +509,28 @@ static EmbedGradPlan embed_grad_plan(int64_t n, int64_t vocab, int64_t dim) {
   return g;
 }
 
-template <int DT, int GT>
-static int launch_embed_grad(const EmbedGradParams& p, unsigned fill_blocks, cudaStream_t st) {
-  constexpr auto kernel = embed_sum_kernel<DT, GT>;
-  constexpr int bytes = kSumWarps * sum_bytes<DT, GT>();
+template <int BITS>
+static int launch_sort(const SortParams& p, cudaStream_t st) {
+  constexpr auto kernel = sort_tokens_kernel<BITS>;
+  constexpr int bytes = (kSortWarps + kSortBlocks + 1) * 4 << BITS;
+  IRIS_CHECK(allow_shared<kernel>(bytes, true));
+  return launch_rows(kernel, p, (unsigned)p.split, p.split, kSortThreads, bytes, st);
+}
+template <int DT, int GT, int I, bool ALIGNED>
+static int launch_sum(const EmbedGradParams& p, unsigned fill_blocks, cudaStream_t st) {
+  constexpr auto kernel = embed_sum_kernel<DT, GT, I, ALIGNED>;
+  constexpr int bytes = kSumWarps * sum_bytes<DT, GT, I>();
   IRIS_CHECK(allow_shared<kernel>(bytes));
-  IRIS_CHECK(launch_rows(kernel, p, p.sum_blocks + fill_blocks, 1, kSumThreads, bytes, st));
+  return launch_rows(kernel, p, p.sum_blocks + fill_blocks, 1, kSumThreads, bytes, st);
+}
+template <int DT, int GT>
+static int launch_embed_grad(const EmbedGradParams& p, const EmbedGradPlan& g, unsigned fill_blocks, cudaStream_t st) {
+  const bool aligned = p.dim * Columns<DT>::ES % 16 == 0 && p.dim * Columns<GT>::ES % 16 == 0 && p.aligned && p.dy_stride % 16 == 0 && p.shard_stride % 16 == 0;
+  if (g.runs == 1) IRIS_CHECK(aligned ? launch_sum<DT, GT, 1, true>(p, fill_blocks, st) : launch_sum<DT, GT, 1, false>(p, fill_blocks, st));
+  else IRIS_CHECK(aligned ? launch_sum<DT, GT, 2, true>(p, fill_blocks, st) : launch_sum<DT, GT, 2, false>(p, fill_blocks, st));
   if (p.chunks < 2) return IRIS_OK;
-  return launch_rows(embed_join_kernel<GT>, p, (unsigned)((int64_t)p.chunks * p.tiles), 1, kSumThreads, 0, st);
+  const int64_t blocks = (int64_t)((p.chunks + kJoinWarps - 1) / kJoinWarps) * ((p.dim + kWarpColumns - 1) / kWarpColumns);
+  return launch_rows(embed_join_kernel<GT>, p, (unsigned)blocks, 1, kJoinWarps * 32, 0, st);
 }
 
 static int check_table(const char* fn, int dtype, int world, int64_t vocab, int64_t dim, int64_t n) {
@@ -495,7 +614,7 @@ extern "C" int iris_embed_tokens_backward(const iris_embed_grad_args* a, void* s
   p.dim = (int)a->dim;
   p.fill_parts = (int)((a->dim * gs + kFillBytes - 1) / kFillBytes);
   const int64_t sum_blocks = ((int64_t)g.chunks * g.tiles + kSumWarps - 1) / kSumWarps;
-  const int64_t fill_blocks = a->accumulate ? 0 : ((a->vocab + 31) / 32 * p.fill_parts + kSumWarps - 1) / kSumWarps;
+  const int64_t fill_blocks = a->accumulate ? 0 : ((a->vocab + kFillRows - 1) / kFillRows * p.fill_parts + kSumWarps - 1) / kSumWarps;
   if (sum_blocks + fill_blocks > INT32_MAX || (int64_t)g.chunks * g.tiles > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 blocks", fn);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
 
@@ -505,7 +624,7 @@ extern "C" int iris_embed_tokens_backward(const iris_embed_grad_args* a, void* s
   s.n = (int)a->n;
   s.vocab = (uint32_t)a->vocab;
   s.per = (uint32_t)per;
-  s.present = present;
+  s.present = present == (1u << a->world) - 1 ? ~0u : present;
   for (int i = 0; i < 2; ++i) {
     s.keys[i] = reinterpret_cast<uint32_t*>(ws + i * g.list);
     s.places[i] = reinterpret_cast<uint32_t*>(ws + (2 + i) * g.list);
@@ -514,15 +633,15 @@ extern "C" int iris_embed_tokens_backward(const iris_embed_grad_args* a, void* s
   int bits = 1;
   while (a->vocab >> bits) ++bits;   // vocab itself is a key
   s.passes = (bits + kSortMaxBits - 1) / kSortMaxBits;
-  s.bits = (bits + s.passes - 1) / s.passes;
-  s.split = a->n > 4 * kSortThreads ? kSortBlocks : 1;
-  const size_t shared = (size_t)(kSortWarps + s.split + 1) * 4 << s.bits;
-  IRIS_CHECK(allow_shared<sort_tokens_kernel>((kSortWarps + kSortBlocks + 1) * 4 << kSortMaxBits));
-  IRIS_CHECK(launch_rows(sort_tokens_kernel, s, (unsigned)s.split, s.split, kSortThreads, shared, st));
+  bits = (bits + s.passes - 1) / s.passes;
+  s.split = a->n > 2 * kSortThreads ? kSortBlocks : 1;
+  IRIS_CHECK(bits <= 6 ? launch_sort<6>(s, st) : bits == 7 ? launch_sort<7>(s, st) : bits == 8 ? launch_sort<8>(s, st) : bits == 9 ? launch_sort<9>(s, st) : launch_sort<10>(s, st));
 
   p.dy = static_cast<const char*>(a->grad_out);
   p.dy_stride = ds * es;
   p.shard_stride = ss * gs;
+  p.aligned = reinterpret_cast<uintptr_t>(a->grad_out) % 16 == 0;
+  for (int r = 0; r < a->world; ++r) p.aligned &= reinterpret_cast<uintptr_t>(a->grad_shards[r]) % 16 == 0;
   p.keys = s.keys[s.passes & 1 ^ 1];
   p.places = s.places[s.passes & 1 ^ 1];
   p.used = s.used;
@@ -538,7 +657,7 @@ extern "C" int iris_embed_tokens_backward(const iris_embed_grad_args* a, void* s
   p.accumulate = a->accumulate;
   const bool wide = a->grad_dtype == IRIS_F32;
   const unsigned f = (unsigned)fill_blocks;
-  if (a->dtype == IRIS_BF16) return wide ? launch_embed_grad<IRIS_BF16, IRIS_F32>(p, f, st) : launch_embed_grad<IRIS_BF16, IRIS_BF16>(p, f, st);
-  if (a->dtype == IRIS_F16) return wide ? launch_embed_grad<IRIS_F16, IRIS_F32>(p, f, st) : launch_embed_grad<IRIS_F16, IRIS_F16>(p, f, st);
-  return launch_embed_grad<IRIS_F32, IRIS_F32>(p, f, st);
+  if (a->dtype == IRIS_BF16) return wide ? launch_embed_grad<IRIS_BF16, IRIS_F32>(p, g, f, st) : launch_embed_grad<IRIS_BF16, IRIS_BF16>(p, g, f, st);
+  if (a->dtype == IRIS_F16) return wide ? launch_embed_grad<IRIS_F16, IRIS_F32>(p, g, f, st) : launch_embed_grad<IRIS_F16, IRIS_F16>(p, g, f, st);
+  return launch_embed_grad<IRIS_F32, IRIS_F32>(p, g, f, st);
 }
