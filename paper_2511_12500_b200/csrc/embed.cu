@@ -15,66 +15,130 @@ struct EmbedParams {
   const int64_t* tokens;
   char* out;
   int64_t n, vocab;
-  uint32_t per, each;                 // rows of a shard; 16-byte granules that a row of the output may touch
+  uint32_t per, each;                 // rows of a shard; warps of a row
   int bytes;                          // of a row
   float scale;
 };
 
-// A thread moves granules of the output, counted over all rows, so that blocks are full whatever a row's length is.
+// A warp moves U times 512 bytes of a row of the output, 16 aligned bytes a thread at a time.  Where the table's row does not lie like the output's,
+// those are cut out of two of the table's, of which the second are the next thread's first and come from L1.
+template <int ES, int U>
+__device__ __forceinline__ void load_like(const char* from, int begin, int bytes, uint4 (&v)[U]) {   // begin: byte of the row, of this thread
+  const int a = (int)phase(from + begin), lane = threadIdx.x & 31;   // a: the same for all threads
+  const bool inside = begin - lane * 16 - a >= 0 && begin - lane * 16 - a + U * 512 + 16 <= bytes;
+  uint4 next[U];
+  if (inside) {
+    const char* const p = from + begin - a;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      v[u] = ld_global_v4(p + u * 512);
+      if (a) next[u] = ld_global_v4(p + u * 512 + 16);
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      v[u] = edge_load<ES>(from, begin + u * 512 - a, bytes);
+      if (a) next[u] = edge_load<ES>(from, begin + u * 512 - a + 16, bytes);
+    }
+  }
+  if (a) cut_all(v, next, a);
+}
+template <int DT>
+__device__ __forceinline__ uint4 scaled(const uint4& v, float scale) {
+  using E = Elem<DT>;
+  float x[E::VE];
+  E::unpack(v, x);
+#pragma unroll
+  for (int e = 0; e < E::VE; ++e) x[e] *= scale;
+  return E::pack(x);
+}
+__device__ __forceinline__ const char* embed_row(const EmbedParams& p, int64_t i) {
+  const int64_t t = p.tokens[i];
+  if (t < 0 || t >= p.vocab) return nullptr;
+  const uint32_t r = (uint32_t)t / p.per;
+  return p.shard[r] ? p.shard[r] + (int64_t)((uint32_t)t - r * p.per) * p.shard_stride : nullptr;
+}
+
 template <int DT, int U>
 __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const __grid_constant__ EmbedParams p) {
-  using E = Elem<DT>;
-  constexpr int ES = sizeof(typename E::T), T = kEmbedThreads;
-  const int64_t f0 = (int64_t)blockIdx.x * (T * U), row0 = f0 / p.each;
-  const uint32_t in_row = (uint32_t)(f0 - row0 * p.each);
+  constexpr int ES = sizeof(typename Elem<DT>::T);
+  const int lane = threadIdx.x & 31;
+  const int64_t unit = (int64_t)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5), i = unit / p.each;
+  const int part = (int)(unit - i * p.each);
   ptx::let_next_begin();
   ptx::begin_after_previous();
-  char* to[U];
+  if (i >= p.n) return;
+  char* const to = p.out + i * p.out_stride;
+  const char* const from = embed_row(p, i);
+  const int begin = part * (U * 512) - (int)phase(to) + lane * 16;   // byte of the row
+  uint4 v[U];
+  if (from) {
+    load_like<ES>(from, begin, p.bytes, v);
+    if (p.scale != 1.f) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = scaled<DT>(v[u], p.scale);
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = make_uint4(0, 0, 0, 0);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int b = begin + u * 512;
+    if (b >= 0 && b + 16 <= p.bytes) st_global_v4(to + b, v[u]);
+    else if (b > -16 && b < p.bytes) store_elements<ES>(to + b, to, to + p.bytes, v[u]);
+  }
+}
+
+// Short rows, of at most 16 * L bytes with what their ends touch: L threads a row, and U rows of theirs under way at a time.
+template <int DT, int L>
+__global__ void __launch_bounds__(kEmbedThreads) embed_short_kernel(const __grid_constant__ EmbedParams p) {
+  constexpr int ES = sizeof(typename Elem<DT>::T), U = 4;
+  const int64_t first = ((int64_t)blockIdx.x * kEmbedThreads + threadIdx.x) / L * U;
+  ptx::let_next_begin();
+  ptx::begin_after_previous();
   const char* from[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const uint32_t at = in_row + u * T + threadIdx.x, down = at / p.each;
-    const int64_t i = row0 + down;
-    to[u] = nullptr;
-    from[u] = nullptr;
-    if (i >= p.n) continue;
-    const int64_t t = p.tokens[i];
-    to[u] = p.out + i * p.out_stride;
-    if (t >= 0 && t < p.vocab) {
-      const uint32_t r = (uint32_t)t / p.per;
-      if (p.shard[r]) from[u] = p.shard[r] + (int64_t)((uint32_t)t - r * p.per) * p.shard_stride;
-    }
-  }
-  uint4 v[U];
+  for (int u = 0; u < U; ++u) from[u] = first + u < p.n ? embed_row(p, first + u) : nullptr;
+  uint4 v[U], next[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const uint32_t at = in_row + u * T + threadIdx.x;
-    const int byte = (int)(at - at / p.each * p.each) * 16 - (int)phase(to[u]);
-    v[u] = from[u] ? load_piece<ES>(from[u] + byte, from[u], from[u] + p.bytes) : make_uint4(0, 0, 0, 0);
+    v[u] = next[u] = make_uint4(0, 0, 0, 0);
+    if (!from[u]) continue;
+    const int begin = (threadIdx.x % L) * 16 - (int)phase(p.out + (first + u) * p.out_stride), a = (int)phase(from[u] + begin);
+    v[u] = edge_load<ES>(from[u], begin - a, p.bytes);
+    if (a) next[u] = edge_load<ES>(from[u], begin - a + 16, p.bytes);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (!to[u]) continue;
-    const uint32_t at = in_row + u * T + threadIdx.x;
-    const int byte = (int)(at - at / p.each * p.each) * 16 - (int)phase(to[u]);
-    if (p.scale != 1.f) {
-      float x[E::VE];
-      E::unpack(v[u], x);
-#pragma unroll
-      for (int e = 0; e < E::VE; ++e) x[e] *= p.scale;
-      v[u] = E::pack(x);
-    }
-    store16<ES>(to[u] + byte, to[u], to[u] + p.bytes, v[u]);
+    if (first + u >= p.n) break;
+    char* const to = p.out + (first + u) * p.out_stride;
+    const int b = (threadIdx.x % L) * 16 - (int)phase(to);
+    uint4 w = cut(v[u], next[u], phase(from[u] + b));
+    if (p.scale != 1.f) w = scaled<DT>(w, p.scale);
+    if (b >= 0 && b + 16 <= p.bytes) st_global_v4(to + b, w);
+    else if (b > -16 && b < p.bytes) store_elements<ES>(to + b, to, to + p.bytes, w);
   }
 }
 
 template <int DT>
-static int launch_embed(const EmbedParams& p, cudaStream_t st) {
-  const int64_t granules = p.n * p.each;
-  const bool few = granules < (int64_t)kSms * 8 * kEmbedThreads * 4;
-  const int64_t blocks = (granules + kEmbedThreads * (few ? 1 : 4) - 1) / (kEmbedThreads * (few ? 1 : 4));
+static int launch_embed(EmbedParams p, bool aligned, cudaStream_t st) {
+  const int bytes = p.bytes + (aligned ? 0 : 16 - (int)elem_size(DT));   // that the aligned 16 bytes touched by a row may have
+  const bool few = p.n * ((bytes + 2047) / 2048) < (int64_t)kSms * 64;   // rather more warps
+  int64_t blocks;
+  void (*kernel)(EmbedParams);
+  if (bytes <= 512 && !few) {
+    const int threads = bytes <= 128 ? 8 : bytes <= 256 ? 16 : 32;   // of a row
+    kernel = threads == 8 ? embed_short_kernel<DT, 8> : threads == 16 ? embed_short_kernel<DT, 16> : embed_short_kernel<DT, 32>;
+    blocks = ((p.n + 3) / 4 * threads + kEmbedThreads - 1) / kEmbedThreads;
+  } else {
+    const int runs = (bytes + 511) / 512, most = few ? 1 : 4, each = (runs + most - 1) / most, u = (runs + each - 1) / each;   // equal parts of a row
+    p.each = (uint32_t)((runs + u - 1) / u);
+    kernel = u == 1 ? embed_kernel<DT, 1> : u == 2 ? embed_kernel<DT, 2> : u == 3 ? embed_kernel<DT, 3> : embed_kernel<DT, 4>;
+    blocks = (p.n * p.each + kEmbedThreads / 32 - 1) / (kEmbedThreads / 32);
+  }
   if (blocks > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "iris_embed_tokens: more than 2^31 - 1 blocks");
-  return launch_rows(few ? embed_kernel<DT, 1> : embed_kernel<DT, 4>, p, (unsigned)blocks, 1, kEmbedThreads, 0, st);
+  return launch_rows(kernel, p, (unsigned)blocks, 1, kEmbedThreads, 0, st);
 }
 
 // ---- gradient: sorted tokens ---------------------------------------------------------------------------------------
@@ -86,12 +150,13 @@ struct SortParams {
   const int64_t* tokens;
   int n;
   uint32_t vocab, per, present;     // present: a bit for each shard that is there, all set: each is
-  uint32_t *keys[2], *places[2];    // of pass 0, 2, .. and 1, 3, ..
+  uint2* lists[2];                  // (token, place): of pass 0, 2, .. and 1, 3, ..
   uint32_t* used;                   // a bit for each row of the table that a token names; nullptr: not wanted
   int passes, split;
 };
 
-__device__ __forceinline__ uint32_t sort_key(const SortParams& p, int64_t t) {   // vocab: no token, behind all others
+template <class P>
+__device__ __forceinline__ uint32_t key_of(const P& p, int64_t t) {   // vocab: no token, behind all others
   if (t < 0 || t >= p.vocab) return p.vocab;
   return p.present == ~0u || p.present >> ((uint32_t)t / p.per) & 1 ? (uint32_t)t : p.vocab;
 }
@@ -130,27 +195,34 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
   const int each = (int)(((int64_t)p.n + p.split * kSortWarps * 32 - 1) / (p.split * kSortWarps * 32)) * 32;
   const int64_t b64 = (int64_t)(rank * kSortWarps + warp) * each;
   const int begin = (int)(b64 < p.n ? b64 : p.n), end = (int)(b64 + each < p.n ? b64 + each : p.n);
+  if (p.split > 1) ptx::cluster_arrive_release();
   ptx::let_next_begin();
   ptx::begin_after_previous();
-  if (p.used)
+  if (p.used)   // set behind the first pass's barrier
     for (uint32_t i = rank * kSortThreads + tid; i < (p.vocab + 31) / 32; i += p.split * kSortThreads) p.used[i] = 0;
-  if (p.split > 1) ptx::cluster_sync();   // behind it all blocks write to one another, and to `used`
   const bool held = each <= 32 * kSortItems;
-  uint32_t key[kSortItems], same[kSortItems];
+  uint32_t key[kSortItems], place[kSortItems], same[kSortItems];
   for (int pass = 0; pass < p.passes; ++pass) {
     const int shift = pass * BITS;
-    const uint32_t *const keys = p.keys[pass & 1 ^ 1], *const places = p.places[pass & 1 ^ 1];
-    uint32_t *const to_keys = p.keys[pass & 1], *const to_places = p.places[pass & 1];
+    const uint2* const from = p.lists[pass & 1 ^ 1];
+    uint2* const list = p.lists[pass & 1];
     const auto load = [&](int at) {
       if (pass) {
 #pragma unroll
-        for (int k = 0; k < kSortItems; ++k) key[k] = at + k * 32 + lane < end ? __ldcg(keys + at + k * 32 + lane) : 0;
+        for (int k = 0; k < kSortItems; ++k) {
+          const uint2 x = at + k * 32 + lane < end ? __ldcg(from + at + k * 32 + lane) : make_uint2(0, 0);
+          key[k] = x.x;
+          place[k] = x.y;
+        }
       } else {
         int64_t t[kSortItems];
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k) t[k] = at + k * 32 + lane < end ? p.tokens[at + k * 32 + lane] : -1;
 #pragma unroll
-        for (int k = 0; k < kSortItems; ++k) key[k] = sort_key(p, t[k]);
+        for (int k = 0; k < kSortItems; ++k) {
+          key[k] = key_of(p, t[k]);
+          place[k] = (uint32_t)(at + k * 32 + lane);
+        }
       }
     };
     for (int i = tid; i < kSortWarps * digits; i += kSortThreads) count[i] = 0;
@@ -165,9 +237,9 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
         same[k] = same_digit<BITS>(d, there);
         if (there && (same[k] & ((1u << lane) - 1)) == 0) mine[d] += __popc(same[k]);
         __syncwarp();
-        if (pass == 0 && p.used && there && key[k] < p.vocab) atomicOr(p.used + (key[k] >> 5), 1u << (key[k] & 31));
       }
     }
+    if (p.split > 1 && pass == 0) ptx::cluster_wait();   // all blocks have started
     __syncthreads();
     if (tid < digits) {
       uint32_t c[kSortWarps], sum = 0;
@@ -210,12 +282,6 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
     __syncthreads();
     for (int at = begin; at < end; at += 32 * kSortItems) {
       if (!held) load(at);
-      uint32_t place[kSortItems];
-#pragma unroll
-      for (int k = 0; k < kSortItems; ++k) {
-        const int i = at + k * 32 + lane;
-        place[k] = pass && i < end ? __ldcg(places + i) : (uint32_t)i;
-      }
 #pragma unroll
       for (int k = 0; k < kSortItems; ++k) {
         if (at + k * 32 >= end) break;
@@ -225,8 +291,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
         const uint32_t lower = same[k] & ((1u << lane) - 1);
         if (there) {
           const uint32_t to = base[d] + mine[d] + __popc(lower);
-          to_keys[to] = key[k];
-          to_places[to] = place[k];
+          list[to] = make_uint2(key[k], place[k]);
+          if (pass == 0 && p.used && key[k] < p.vocab) atomicOr(p.used + (key[k] >> 5), 1u << (key[k] & 31));
         }
         __syncwarp();
         if (there && lower == 0) mine[d] += __popc(same[k]);
@@ -247,25 +313,27 @@ struct EmbedGradParams {
   int64_t dy_stride;                // bytes
   char* shard[IRIS_MAX_WORLD];
   int64_t shard_stride;             // bytes
-  const uint32_t *keys, *places, *used;
-  float* parts;                     // [chunks, 2, dim]: sums of the run at a chunk's start and of the one at its end, where they go on beyond it
-  int n, chunk, chunks, dim, tiles, fill_parts;   // chunk: sorted places of a chunk
-  uint32_t vocab, per;
+  const uint2* list;                // (token, place), sorted
+  const uint32_t* used;
+  const int64_t* tokens;            // of the kernel for few of them
+  float* parts;                     // [chunks, 2, part_stride]: sums of the run at a chunk's start and of the one at its end, where they go on beyond it
+  int n, chunk, chunks, dim, part_stride, tiles, fill_parts;   // chunk: sorted places of a chunk
+  uint32_t vocab, per, present;     // present: see SortParams
   unsigned sum_blocks;
   float scale;
   int accumulate, aligned;          // aligned: grad_out and the shards begin at 16 bytes
 };
 
-template <int GT>
 __device__ __forceinline__ char* table_row(const EmbedGradParams& p, uint32_t v) {
   const uint32_t r = v / p.per;
   return p.shard[r] ? p.shard[r] + (int64_t)(v - r * p.per) * p.shard_stride : nullptr;
 }
+__device__ __forceinline__ uint4 pairs(uint64_t a, uint64_t b) { return make_uint4((uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)); }
 // All threads of a warp: their columns of row v, from column `begin` on; `at`: shared memory of the warp's, Segment<GT, I>::kBytes.
 template <int GT, int I, bool ALIGNED>
 __device__ __forceinline__ void write_row(const EmbedGradParams& p, uint32_t v, uint32_t at, int begin, const uint64_t (&sum)[I][kLaneColumns / 2]) {
   using C = Columns<GT>;
-  char* const row = table_row<GT>(p, v);
+  char* const row = table_row(p, v);
   uint4 w[I * C::N];
 #pragma unroll
   for (int i = 0; i < I; ++i) {
@@ -286,15 +354,12 @@ __device__ __forceinline__ void write_row(const EmbedGradParams& p, uint32_t v, 
 
 // Zeros in the rows that no token names: a warp has kFillRows rows and kFillBytes of each.
 template <int GT>
-__device__ __forceinline__ void fill_rows(const EmbedGradParams& p, int64_t unit) {
+__device__ __forceinline__ void fill_rows(const EmbedGradParams& p, int64_t v0, int part, uint32_t used) {   // used: a bit for each of the rows
   constexpr int ES = Columns<GT>::ES;
-  const int64_t group = unit / p.fill_parts;
-  const int part = (int)(unit % p.fill_parts), lane = threadIdx.x & 31;
-  if (group * kFillRows >= p.vocab) return;
-  const uint32_t v0 = (uint32_t)group * kFillRows, used = p.used[v0 >> 5] >> (v0 & 31);
+  const int lane = threadIdx.x & 31;
   for (int b = 0; b < kFillRows && v0 + b < p.vocab; ++b) {
     if (used >> b & 1) continue;
-    char* const row = table_row<GT>(p, v0 + b);
+    char* const row = table_row(p, (uint32_t)v0 + b);
     if (!row) continue;
     char* const lo = row + (int64_t)part * kFillBytes;
     char* const hi = row + min((int64_t)p.dim * ES, (int64_t)(part + 1) * kFillBytes);
@@ -320,7 +385,8 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
   ptx::let_next_begin();
   ptx::begin_after_previous();
   if (blockIdx.x >= p.sum_blocks) {
-    fill_rows<GT>(p, (int64_t)(blockIdx.x - p.sum_blocks) * kSumWarps + warp);
+    const int64_t unit = (int64_t)(blockIdx.x - p.sum_blocks) * kSumWarps + warp, v0 = unit / p.fill_parts * kFillRows;
+    if (v0 < p.vocab) fill_rows<GT>(p, v0, (int)(unit % p.fill_parts), p.used[v0 >> 5] >> (v0 & 31));
     return;
   }
   const int64_t unit = (int64_t)blockIdx.x * kSumWarps + warp;
@@ -328,20 +394,19 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
   if (c >= p.chunks) return;
   const uint32_t own = ptx::smem_u32(ring) + warp * sum_bytes<DT, GT, I>(), out = own + kStages * G::kBytes;
   const int begin = c * p.chunk, end = min(p.n, begin + p.chunk);
-  // The places and tokens of 32 entries are held by the threads, and the next 32 places, as copies begin ahead.
-  const auto key_of = [&](int i) { return i < end ? p.keys[i] : p.vocab; };
-  const auto place_of = [&](int i) { return i < end ? p.places[i] : 0u; };
-  uint32_t now = p.keys[begin];
+  // 32 entries are held by the threads, and the next 32, as copies begin ahead.
+  const auto entry = [&](int i) { return i < end ? p.list[i] : make_uint2(p.vocab, 0); };
+  uint32_t now = p.list[begin].x;
   if (now >= p.vocab) return;
-  bool goes_on = begin > 0 && p.keys[begin - 1] == now;   // the run came from the chunk before
-  uint32_t key = key_of(begin + lane), place = place_of(begin + lane), next_place = place_of(begin + 32 + lane);
+  bool goes_on = begin > 0 && p.list[begin - 1].x == now;   // the run came from the chunk before
+  uint2 held = entry(begin + lane), next = entry(begin + 32 + lane);
   uint64_t sum[I][H] = {};
   typename G::Lone lone;
   const auto row_of = [&](uint32_t i) { return p.dy + (int64_t)i * p.dy_stride; };
-  const auto fetch = [&](int i, int base, uint32_t to) {   // base: of `place`
+  const auto fetch = [&](int i, int base, uint32_t to) {   // base: of `held`
     lone.settle();
     if (i < end) {
-      const uint32_t at = __shfl_sync(~0u, i - base < 32 ? place : next_place, (i - base) & 31);
+      const uint32_t at = __shfl_sync(~0u, i - base < 32 ? held.y : next.y, (i - base) & 31);
       G::fetch(to, row_of(at), column, p.dim, lone);
     }
     copy_async_commit();
@@ -350,15 +415,12 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
     if (!goes_on && !more) {
       write_row<GT, I, ALIGNED>(p, now, out, column, sum);
     } else {
-      float* const to = p.parts + ((int64_t)2 * c + !goes_on) * p.dim + first;
+      float* const to = p.parts + ((int64_t)2 * c + !goes_on) * p.part_stride + first;
 #pragma unroll
       for (int i = 0; i < I; ++i)
-#pragma unroll
-        for (int e = 0; e < H; ++e) {
-          const float2 s = unpair(sum[i][e]);
-          const int at = i * kWarpColumns + 2 * e;
-          if (first + at < p.dim) to[at] = s.x;
-          if (first + at + 1 < p.dim) to[at + 1] = s.y;
+        if (first + i * kWarpColumns < p.dim) {
+          st_global_v4(to + i * kWarpColumns, pairs(sum[i][0], sum[i][1]));
+          st_global_v4(to + i * kWarpColumns + 4, pairs(sum[i][2], sum[i][3]));
         }
     }
   };
@@ -370,11 +432,10 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
   for (int i = begin; i < end; ++i) {
     if (i - base == 32) {
       base = i;
-      place = next_place;
-      key = key_of(base + lane);
-      next_place = place_of(base + 32 + lane);
+      held = next;
+      next = entry(base + 32 + lane);
     }
-    const uint32_t k = __shfl_sync(~0u, key, i - base);
+    const uint32_t k = __shfl_sync(~0u, held.x, i - base);
     if (k != now) {
       finish(false);
       if (k >= p.vocab) break;
@@ -389,7 +450,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
     copy_async_wait_but<kStages - 2>();
     __syncwarp();
     fetch(i + kStages - 1, base, before);
-    const char* const row = ALIGNED ? nullptr : row_of(__shfl_sync(~0u, place, i - base));
+    const char* const row = ALIGNED ? nullptr : row_of(__shfl_sync(~0u, held.y, i - base));
 #pragma unroll
     for (int r = 0; r < I; ++r) {
       uint64_t x[H];
@@ -399,7 +460,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
     }
     before = here;
     here = here == own + (kStages - 1) * G::kBytes ? own : here + G::kBytes;
-    if (i + 1 == end) finish(end < p.n && p.keys[end] == now);
+    if (i + 1 == end) finish(end < p.n && p.list[end].x == now);
   }
   copy_async_wait();   // a block does not end while copies are under way
 }
@@ -418,7 +479,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) embed_join_kernel(const __gri
   ptx::begin_after_previous();
   const int tiles = (p.dim + kWarpColumns - 1) / kWarpColumns;
   const int c0 = (int)(blockIdx.x / tiles) * kJoinWarps, column = (int)(blockIdx.x % tiles) * kWarpColumns, first = column + lane * kLaneColumns;
-  const auto key_at = [&](int64_t i) { return i < p.n ? p.keys[i] : p.vocab; };   // vocab: no token
+  const auto key_at = [&](int64_t i) { return i < p.n ? p.list[i].x : p.vocab; };   // vocab: no token
   // The chunks c + 1 .. last - 1 begin with the run of chunk c (or there is none: 0).
   const auto last_of = [&](int c) -> int {
     const int64_t begin = (int64_t)c * p.chunk, end = begin + p.chunk;
@@ -440,16 +501,11 @@ __global__ void __launch_bounds__(kJoinWarps * 32) embed_join_kernel(const __gri
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int k = i + u * step;
-        const float* const at = p.parts + ((int64_t)2 * k + (k == c)) * p.dim + first;
-        if (p.dim % 4 == 0) {
-          const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
-          const float4 a = k < last && first < p.dim ? *reinterpret_cast<const float4*>(at) : none;
-          const float4 b = k < last && first + 4 < p.dim ? *reinterpret_cast<const float4*>(at + 4) : none;
-          x[u][0] = a.x, x[u][1] = a.y, x[u][2] = a.z, x[u][3] = a.w, x[u][4] = b.x, x[u][5] = b.y, x[u][6] = b.z, x[u][7] = b.w;
-        } else {
-#pragma unroll
-          for (int e = 0; e < kLaneColumns; ++e) x[u][e] = k < last && first + e < p.dim ? at[e] : 0.f;
-        }
+        const float* const at = p.parts + ((int64_t)2 * k + (k == c)) * p.part_stride + first;
+        const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float4 a = k < last && first < p.dim ? __ldcg(reinterpret_cast<const float4*>(at)) : none;
+        const float4 b = k < last && first < p.dim ? __ldcg(reinterpret_cast<const float4*>(at + 4)) : none;
+        x[u][0] = a.x, x[u][1] = a.y, x[u][2] = a.z, x[u][3] = a.w, x[u][4] = b.x, x[u][5] = b.y, x[u][6] = b.z, x[u][7] = b.w;
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u)
@@ -461,7 +517,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) embed_join_kernel(const __gri
     uint64_t x[1][kLaneColumns / 2];
 #pragma unroll
     for (int e = 0; e < kLaneColumns / 2; ++e) x[0][e] = pair(sum[2 * e], sum[2 * e + 1]);
-    write_row<GT, 1, false>(p, p.keys[(int64_t)c * p.chunk + p.chunk - 1], at, column, x);
+    write_row<GT, 1, false>(p, p.list[(int64_t)c * p.chunk + p.chunk - 1].x, at, column, x);
   };
   const int c = c0 + warp, last = c < p.chunks ? last_of(c) : 0;
   if (lane == 0) lasts[warp] = last - c > kLongRun ? last : 0;
@@ -488,11 +544,75 @@ __global__ void __launch_bounds__(kJoinWarps * 32) embed_join_kernel(const __gri
   }
 }
 
+// Few tokens, without sorting: a warp looks after one place and 256 columns, and adds up the rows of all places with its token, in their order, if it
+// is the first of them; other warps clear the rows that no token names.  A third of the time of sorting and adding up (64 tokens: 8 us, 24).
+constexpr int kFewTokens = 256;
+
+template <int DT, int GT, bool ALIGNED>
+__global__ void __launch_bounds__(kSumThreads) embed_few_kernel(const __grid_constant__ EmbedGradParams p) {
+  using G = Segment<DT, 1, ALIGNED>;
+  constexpr int kAhead = 4, H = kLaneColumns / 2, kOut = Segment<GT, 1>::kBytes;
+  __shared__ uint32_t keys[kFewTokens];
+  __shared__ __align__(16) char rows[kSumWarps][kAhead * G::kBytes + kOut];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  ptx::let_next_begin();
+  ptx::begin_after_previous();
+  const int64_t unit = (int64_t)blockIdx.x * kSumWarps + warp;
+  for (int i = threadIdx.x; i < kFewTokens; i += kSumThreads) keys[i] = i < p.n ? key_of(p, p.tokens[i]) : p.vocab;
+  __syncthreads();
+  if (blockIdx.x >= p.sum_blocks) {
+    const int64_t at = unit - (int64_t)p.sum_blocks * kSumWarps;
+    const int64_t v0 = at / p.fill_parts * kFillRows;
+    uint32_t used = 0;
+    for (int i = lane; i < p.n; i += 32) used |= keys[i] >= v0 && keys[i] < v0 + kFillRows && keys[i] < p.vocab ? 1u << (keys[i] - v0) : 0u;
+    fill_rows<GT>(p, v0, (int)(at % p.fill_parts), __reduce_or_sync(~0u, used));
+    return;
+  }
+  const int place = (int)(unit / p.tiles), column = (int)(unit % p.tiles) * kWarpColumns;
+  if (place >= p.n) return;
+  const uint32_t key = keys[place];
+  if (key >= p.vocab) return;
+  const uint32_t own = ptx::smem_u32(rows[warp]);
+  uint64_t sum[1][H] = {};
+  typename G::Lone lone[kAhead];
+  for (int at = 0; at < p.n; at += 32) {
+    uint32_t same = __ballot_sync(~0u, keys[at + lane] == key);
+    if (same && (at + __ffs(same) - 1 < place)) return;   // it is not the first
+    while (same) {
+      const char* row[kAhead];
+      int m = 0;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (same) {
+          row[u] = p.dy + (int64_t)(at + __ffs(same) - 1) * p.dy_stride;
+          same &= same - 1;
+          G::fetch(own + u * G::kBytes, row[u], column, p.dim, lone[u]);
+          m = u + 1;
+        }
+      copy_async_wait();
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) lone[u].settle();
+      __syncwarp();
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (u < m) {
+          uint64_t x[H];
+          G::read(own + u * G::kBytes, row[u], column, p.dim, 0, x);
+#pragma unroll
+          for (int e = 0; e < H; ++e) sum[0][e] = add2f(sum[0][e], x[e]);
+        }
+      __syncwarp();
+    }
+  }
+  write_row<GT, 1, ALIGNED>(p, key, own + kAhead * G::kBytes, column, sum);
+}
+
 // ---- host side -----------------------------------------------------------------------------------------------------
 struct EmbedGradPlan {
   int chunk, chunks, runs, tiles;   // runs: of 256 columns that a warp adds up
   size_t list, used, parts, bytes;   // list: of one list of n; offsets of the others
 };
+static int part_stride(int64_t dim) { return (int)((dim + kLaneColumns - 1) / kLaneColumns * kLaneColumns); }
 static EmbedGradPlan embed_grad_plan(int64_t n, int64_t vocab, int64_t dim) {
   EmbedGradPlan g;
   g.runs = dim > kWarpColumns ? 2 : 1;
@@ -502,10 +622,10 @@ static EmbedGradPlan embed_grad_plan(int64_t n, int64_t vocab, int64_t dim) {
   chunk = chunk < 16 ? 16 : chunk > 256 ? 256 : chunk;
   g.chunk = (int)chunk;
   g.chunks = (int)((n + chunk - 1) / chunk);
-  g.list = align_up((uint64_t)n * 4, 256);
-  g.used = 4 * g.list;
+  g.list = align_up((uint64_t)n * 8, 256);
+  g.used = 2 * g.list;
   g.parts = g.used + align_up((uint64_t)(vocab + 31) / 32 * 4, 256);
-  g.bytes = g.parts + (uint64_t)g.chunks * 2 * dim * 4;
+  g.bytes = g.parts + (uint64_t)g.chunks * 2 * part_stride(dim) * 4;
   return g;
 }
 
@@ -525,7 +645,8 @@ static int launch_sum(const EmbedGradParams& p, unsigned fill_blocks, cudaStream
 }
 template <int DT, int GT>
 static int launch_embed_grad(const EmbedGradParams& p, const EmbedGradPlan& g, unsigned fill_blocks, cudaStream_t st) {
-  const bool aligned = p.dim * Columns<DT>::ES % 16 == 0 && p.dim * Columns<GT>::ES % 16 == 0 && p.aligned && p.dy_stride % 16 == 0 && p.shard_stride % 16 == 0;
+  const bool few = p.n <= kFewTokens, aligned = p.dim * Columns<DT>::ES % 16 == 0 && p.dim * Columns<GT>::ES % 16 == 0 && p.aligned && p.dy_stride % 16 == 0 && p.shard_stride % 16 == 0;
+  if (few) return launch_rows(aligned ? embed_few_kernel<DT, GT, true> : embed_few_kernel<DT, GT, false>, p, p.sum_blocks + fill_blocks, 1, kSumThreads, 0, st);
   if (g.runs == 1) IRIS_CHECK(aligned ? launch_sum<DT, GT, 1, true>(p, fill_blocks, st) : launch_sum<DT, GT, 1, false>(p, fill_blocks, st));
   else IRIS_CHECK(aligned ? launch_sum<DT, GT, 2, true>(p, fill_blocks, st) : launch_sum<DT, GT, 2, false>(p, fill_blocks, st));
   if (p.chunks < 2) return IRIS_OK;
@@ -575,13 +696,13 @@ extern "C" int iris_embed_tokens(const iris_embed_args* a, void* stream) {
   p.n = a->n;
   p.vocab = a->vocab;
   p.per = (uint32_t)(per ? per : 1);
-  p.each = (uint32_t)part_granules(a->out, os, a->dim, a->dtype, 1);
+  const bool aligned = aligned_rows(a->out, os * es);
   p.bytes = (int)(a->dim * es);
   p.scale = a->scale;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (a->dtype == IRIS_BF16) return launch_embed<IRIS_BF16>(p, st);
-  if (a->dtype == IRIS_F16) return launch_embed<IRIS_F16>(p, st);
-  return launch_embed<IRIS_F32>(p, st);
+  if (a->dtype == IRIS_BF16) return launch_embed<IRIS_BF16>(p, aligned, st);
+  if (a->dtype == IRIS_F16) return launch_embed<IRIS_F16>(p, aligned, st);
+  return launch_embed<IRIS_F32>(p, aligned, st);
 }
 
 extern "C" size_t iris_embed_workspace_bytes(int64_t n, int64_t vocab, int64_t dim) {
@@ -611,50 +732,51 @@ extern "C" int iris_embed_tokens_backward(const iris_embed_grad_args* a, void* s
   IRIS_CHECK(check_aligned(fn, "tokens", a->tokens, 8, a->n > 0));
   IRIS_CHECK(check_aligned(fn, "workspace", a->workspace, 16, true));
   if (a->workspace_bytes < g.bytes) return fail(IRIS_ERR_ARG, "%s: workspace has %zu bytes, the call needs %zu", fn, a->workspace_bytes, g.bytes);
-  p.dim = (int)a->dim;
-  p.fill_parts = (int)((a->dim * gs + kFillBytes - 1) / kFillBytes);
-  const int64_t sum_blocks = ((int64_t)g.chunks * g.tiles + kSumWarps - 1) / kSumWarps;
-  const int64_t fill_blocks = a->accumulate ? 0 : ((a->vocab + kFillRows - 1) / kFillRows * p.fill_parts + kSumWarps - 1) / kSumWarps;
-  if (sum_blocks + fill_blocks > INT32_MAX || (int64_t)g.chunks * g.tiles > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 blocks", fn);
+  const bool few = a->n <= kFewTokens;
+  const int fill_parts = (int)((a->dim * gs + kFillBytes - 1) / kFillBytes), tiles = few ? (int)((a->dim + kWarpColumns - 1) / kWarpColumns) : g.tiles;
+  const int64_t units = few ? a->n * tiles : (int64_t)g.chunks * g.tiles, sum_blocks = (units + kSumWarps - 1) / kSumWarps;
+  const int64_t fill_blocks = a->accumulate ? 0 : ((a->vocab + kFillRows - 1) / kFillRows * fill_parts + kSumWarps - 1) / kSumWarps;
+  if (sum_blocks + fill_blocks > INT32_MAX || units > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 blocks", fn);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-
   char* const ws = static_cast<char*>(a->workspace);
-  SortParams s{};
-  s.tokens = a->tokens;
-  s.n = (int)a->n;
-  s.vocab = (uint32_t)a->vocab;
-  s.per = (uint32_t)per;
-  s.present = present == (1u << a->world) - 1 ? ~0u : present;
-  for (int i = 0; i < 2; ++i) {
-    s.keys[i] = reinterpret_cast<uint32_t*>(ws + i * g.list);
-    s.places[i] = reinterpret_cast<uint32_t*>(ws + (2 + i) * g.list);
-  }
-  s.used = a->accumulate ? nullptr : reinterpret_cast<uint32_t*>(ws + g.used);
-  int bits = 1;
-  while (a->vocab >> bits) ++bits;   // vocab itself is a key
-  s.passes = (bits + kSortMaxBits - 1) / kSortMaxBits;
-  bits = (bits + s.passes - 1) / s.passes;
-  s.split = a->n > 2 * kSortThreads ? kSortBlocks : 1;
-  IRIS_CHECK(bits <= 6 ? launch_sort<6>(s, st) : bits == 7 ? launch_sort<7>(s, st) : bits == 8 ? launch_sort<8>(s, st) : bits == 9 ? launch_sort<9>(s, st) : launch_sort<10>(s, st));
-
+  p.dim = (int)a->dim;
+  p.part_stride = part_stride(a->dim);
+  p.fill_parts = fill_parts;
+  p.tiles = tiles;
+  p.sum_blocks = (unsigned)sum_blocks;
+  p.n = (int)a->n;
+  p.chunk = g.chunk;
+  p.chunks = g.chunks;
+  p.vocab = (uint32_t)a->vocab;
+  p.per = (uint32_t)per;
+  p.present = present == (1u << a->world) - 1 ? ~0u : present;
+  p.tokens = a->tokens;
+  p.scale = a->scale;
+  p.accumulate = a->accumulate;
   p.dy = static_cast<const char*>(a->grad_out);
   p.dy_stride = ds * es;
   p.shard_stride = ss * gs;
   p.aligned = reinterpret_cast<uintptr_t>(a->grad_out) % 16 == 0;
   for (int r = 0; r < a->world; ++r) p.aligned &= reinterpret_cast<uintptr_t>(a->grad_shards[r]) % 16 == 0;
-  p.keys = s.keys[s.passes & 1 ^ 1];
-  p.places = s.places[s.passes & 1 ^ 1];
-  p.used = s.used;
-  p.parts = reinterpret_cast<float*>(ws + g.parts);
-  p.n = (int)a->n;
-  p.chunk = g.chunk;
-  p.chunks = g.chunks;
-  p.tiles = g.tiles;
-  p.vocab = (uint32_t)a->vocab;
-  p.per = (uint32_t)per;
-  p.sum_blocks = (unsigned)sum_blocks;
-  p.scale = a->scale;
-  p.accumulate = a->accumulate;
+  if (!few) {
+    SortParams s{};
+    s.tokens = a->tokens;
+    s.n = p.n;
+    s.vocab = p.vocab;
+    s.per = p.per;
+    s.present = p.present;
+    for (int i = 0; i < 2; ++i) s.lists[i] = reinterpret_cast<uint2*>(ws + i * g.list);
+    s.used = a->accumulate ? nullptr : reinterpret_cast<uint32_t*>(ws + g.used);
+    int bits = 1;
+    while (a->vocab >> bits) ++bits;   // vocab itself is a key
+    s.passes = (bits + kSortMaxBits - 1) / kSortMaxBits;
+    bits = (bits + s.passes - 1) / s.passes;
+    s.split = p.n > kSortItems * kSortThreads ? kSortBlocks : 1;
+    IRIS_CHECK(bits <= 6 ? launch_sort<6>(s, st) : bits == 7 ? launch_sort<7>(s, st) : bits == 8 ? launch_sort<8>(s, st) : bits == 9 ? launch_sort<9>(s, st) : launch_sort<10>(s, st));
+    p.list = s.lists[s.passes & 1 ^ 1];
+    p.used = s.used;
+    p.parts = reinterpret_cast<float*>(ws + g.parts);
+  }
   const bool wide = a->grad_dtype == IRIS_F32;
   const unsigned f = (unsigned)fill_blocks;
   if (a->dtype == IRIS_BF16) return wide ? launch_embed_grad<IRIS_BF16, IRIS_F32>(p, g, f, st) : launch_embed_grad<IRIS_BF16, IRIS_BF16>(p, g, f, st);
