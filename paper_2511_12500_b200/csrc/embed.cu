@@ -22,26 +22,64 @@ struct EmbedParams {
 
 // A warp moves U times 512 bytes of a row of the output, 16 aligned bytes a thread at a time.  Where the table's row does not lie like the output's,
 // those are cut out of two of the table's, of which the second are the next thread's first and come from L1.
+// 16 bytes from byte b of the row on, all of which lie in it, though the aligned ones that they touch do not.
+template <int ES>
+__device__ __forceinline__ uint4 load_apart(const char* from, int b) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = ES == 4 ? *reinterpret_cast<const uint32_t*>(from + b + i * 4)
+                   : *reinterpret_cast<const uint16_t*>(from + b + i * 4) | (uint32_t)*reinterpret_cast<const uint16_t*>(from + b + i * 4 + 2) << 16;
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// For those 16 bytes of each 512 that lie in the row; begin: byte of the row, of this thread.
 template <int ES, int U>
-__device__ __forceinline__ void load_like(const char* from, int begin, int bytes, uint4 (&v)[U]) {   // begin: byte of the row, of this thread
+__device__ __forceinline__ void load_like(const char* from, int begin, int bytes, uint4 (&v)[U]) {
   const int a = (int)phase(from + begin), lane = threadIdx.x & 31;   // a: the same for all threads
   const bool inside = begin - lane * 16 - a >= 0 && begin - lane * 16 - a + U * 512 + 16 <= bytes;
+  const char* const p = from + begin - a;
   uint4 next[U];
   if (inside) {
-    const char* const p = from + begin - a;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       v[u] = ld_global_v4(p + u * 512);
       if (a) next[u] = ld_global_v4(p + u * 512 + 16);
     }
-  } else {
+    if (a) cut_all(v, next, a);
+    return;
+  }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      v[u] = edge_load<ES>(from, begin + u * 512 - a, bytes);
-      if (a) next[u] = edge_load<ES>(from, begin + u * 512 - a + 16, bytes);
+  for (int u = 0; u < U; ++u) {
+    const int b = begin + u * 512;
+    v[u] = next[u] = make_uint4(0, 0, 0, 0);
+    if (b - a >= 0 && b - a + (a ? 32 : 16) <= bytes) {
+      v[u] = ld_global_v4(p + u * 512);
+      if (a) next[u] = ld_global_v4(p + u * 512 + 16);
     }
   }
   if (a) cut_all(v, next, a);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int b = begin + u * 512;
+    if (a && b >= 0 && b + 16 <= bytes && !(b - a >= 0 && b - a + 32 <= bytes)) v[u] = load_apart<ES>(from, b);
+  }
+}
+// What does not fill 16 aligned bytes of the output: its first elements and its last ones, one a thread.  `first`, `last`: whether the warp looks after them.
+template <int DT>
+__device__ __forceinline__ void move_ends(const char* from, char* to, int bytes, float scale, bool first, bool last) {
+  using E = Elem<DT>;
+  using T = typename E::T;
+  constexpr int ES = sizeof(T);
+  const int lane = threadIdx.x & 31, head = (int)(-phase(to) & 15), tail = bytes - (int)phase(to + bytes);
+  int b = -1;
+  if (lane < 8) {
+    if (first && lane * ES < min(head, bytes)) b = lane * ES;
+  } else if (lane < 16) {
+    if (last && tail >= head && tail + (lane - 8) * ES < bytes) b = tail + (lane - 8) * ES;
+  }
+  if (b < 0) return;
+  const T x = from ? *reinterpret_cast<const T*>(from + b) : E::from(0.f);
+  *reinterpret_cast<T*>(to + b) = scale == 1.f ? x : E::from(E::to(x) * scale);
 }
 template <int DT>
 __device__ __forceinline__ uint4 scaled(const uint4& v, float scale) {
@@ -63,8 +101,10 @@ template <int DT, int U>
 __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const __grid_constant__ EmbedParams p) {
   constexpr int ES = sizeof(typename Elem<DT>::T);
   const int lane = threadIdx.x & 31;
-  const int64_t unit = (int64_t)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5), i = unit / p.each;
-  const int part = (int)(unit - i * p.each);
+  constexpr uint32_t kWarps = kEmbedThreads / 32;
+  const uint32_t q = blockIdx.x / p.each, in = (blockIdx.x - q * p.each) * kWarps + (threadIdx.x >> 5), down = in / p.each;
+  const int64_t i = (int64_t)q * kWarps + down;
+  const int part = (int)(in - down * p.each);
   ptx::let_next_begin();
   ptx::begin_after_previous();
   if (i >= p.n) return;
@@ -86,8 +126,8 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const __grid_const
   for (int u = 0; u < U; ++u) {
     const int b = begin + u * 512;
     if (b >= 0 && b + 16 <= p.bytes) st_global_v4(to + b, v[u]);
-    else if (b > -16 && b < p.bytes) store_elements<ES>(to + b, to, to + p.bytes, v[u]);
   }
+  if (part == 0 || part + 1 == (int)p.each) move_ends<DT>(from, to, p.bytes, p.scale, part == 0, part + 1 == (int)p.each);
 }
 
 // Short rows, of at most 16 * L bytes with what their ends touch: L threads a row, and U rows of theirs under way at a time.
@@ -306,7 +346,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
 
 // ---- gradient: sums ------------------------------------------------------------------------------------------------
 constexpr int kSumThreads = 256, kSumWarps = kSumThreads / 32;
-constexpr int kFillRows = 8, kFillBytes = 2048;   // that a warp clears
+constexpr int kFillBytes = 8192;    // that a warp clears
 
 struct EmbedGradParams {
   const char* dy;
@@ -317,13 +357,18 @@ struct EmbedGradParams {
   const uint32_t* used;
   const int64_t* tokens;            // of the kernel for few of them
   float* parts;                     // [chunks, 2, part_stride]: sums of the run at a chunk's start and of the one at its end, where they go on beyond it
-  int n, chunk, chunks, dim, part_stride, tiles, fill_parts;   // chunk: sorted places of a chunk
+  int n, chunk, chunks, dim, part_stride, tiles, fill_parts, fill_shift;   // chunk: sorted places of a chunk
   uint32_t vocab, per, present;     // present: see SortParams
   unsigned sum_blocks;
   float scale;
   int accumulate, aligned;          // aligned: grad_out and the shards begin at 16 bytes
 };
 
+template <int ES>
+__device__ __forceinline__ void store_zero(char* at) {
+  if (ES == 4) *reinterpret_cast<uint32_t*>(at) = 0;
+  else *reinterpret_cast<uint16_t*>(at) = 0;
+}
 __device__ __forceinline__ char* table_row(const EmbedGradParams& p, uint32_t v) {
   const uint32_t r = v / p.per;
   return p.shard[r] ? p.shard[r] + (int64_t)(v - r * p.per) * p.shard_stride : nullptr;
@@ -352,18 +397,45 @@ __device__ __forceinline__ void write_row(const EmbedGradParams& p, uint32_t v, 
   Segment<GT, I, ALIGNED>::write(at, row, begin, p.dim, w);
 }
 
-// Zeros in the rows that no token names: a warp has kFillRows rows and kFillBytes of each.
-template <int GT>
-__device__ __forceinline__ void fill_rows(const EmbedGradParams& p, int64_t v0, int part, uint32_t used) {   // used: a bit for each of the rows
-  constexpr int ES = Columns<GT>::ES;
+// Zeros in bytes lo .. hi - 1, by a warp.
+template <int ES>
+__device__ __forceinline__ void clear(char* lo, char* hi) {
   const int lane = threadIdx.x & 31;
-  for (int b = 0; b < kFillRows && v0 + b < p.vocab; ++b) {
-    if (used >> b & 1) continue;
-    char* const row = table_row(p, (uint32_t)v0 + b);
-    if (!row) continue;
-    char* const lo = row + (int64_t)part * kFillBytes;
-    char* const hi = row + min((int64_t)p.dim * ES, (int64_t)(part + 1) * kFillBytes);
-    for (char* at = lo - phase(lo) + lane * 16; at < hi; at += 32 * 16) store16<ES>(at, lo, hi, make_uint4(0, 0, 0, 0));
+  char* const begin = lo + (-phase(lo) & 15);
+  char* const end = hi - phase(hi);
+  if (begin > end) {   // within 16 aligned bytes
+    if (lo + lane * ES < hi) store_zero<ES>(lo + lane * ES);
+    return;
+  }
+  if (lane < 8) {
+    if (lo + lane * ES < begin) store_zero<ES>(lo + lane * ES);
+  } else if (lane < 16) {
+    if (end + (lane - 8) * ES < hi) store_zero<ES>(end + (lane - 8) * ES);
+  }
+  for (char* at = begin + lane * 16; at < end; at += 512) st_global_v4(at, make_uint4(0, 0, 0, 0));
+}
+// Zeros in the rows that no token names: a warp has 2^fill_shift rows, or kFillBytes of one.  used: a bit for each of the rows.
+template <int GT>
+__device__ __forceinline__ void fill_rows(const EmbedGradParams& p, int64_t v0, int part, uint32_t used) {
+  constexpr int ES = Columns<GT>::ES;
+  const int64_t bytes = (int64_t)p.dim * ES;
+  const int64_t left = p.vocab - v0;
+  const int rows = 1 << p.fill_shift, n = left < rows ? (int)left : rows;
+  if (n <= 0) return;
+  if (p.fill_parts > 1) {
+    char* const row = used & 1 ? nullptr : table_row(p, (uint32_t)v0);
+    if (row) clear<ES>(row + (int64_t)part * kFillBytes, row + min(bytes, (int64_t)(part + 1) * kFillBytes));
+    return;
+  }
+  for (int b = 0; b < n;) {   // rows side by side are cleared at once
+    int m = used >> b & 1 ? 0 : 1;
+    char* const row = m ? table_row(p, (uint32_t)v0 + b) : nullptr;
+    if (row) {
+      if (p.shard_stride == bytes)
+        while (b + m < n && !(used >> (b + m) & 1) && table_row(p, (uint32_t)v0 + b + m) == row + m * bytes) ++m;
+      clear<ES>(row, row + m * bytes);
+    }
+    b += m ? m : 1;
   }
 }
 
@@ -385,7 +457,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
   ptx::let_next_begin();
   ptx::begin_after_previous();
   if (blockIdx.x >= p.sum_blocks) {
-    const int64_t unit = (int64_t)(blockIdx.x - p.sum_blocks) * kSumWarps + warp, v0 = unit / p.fill_parts * kFillRows;
+    const int64_t unit = (int64_t)(blockIdx.x - p.sum_blocks) * kSumWarps + warp, v0 = unit / p.fill_parts << p.fill_shift;
     if (v0 < p.vocab) fill_rows<GT>(p, v0, (int)(unit % p.fill_parts), p.used[v0 >> 5] >> (v0 & 31));
     return;
   }
@@ -562,9 +634,9 @@ __global__ void __launch_bounds__(kSumThreads) embed_few_kernel(const __grid_con
   __syncthreads();
   if (blockIdx.x >= p.sum_blocks) {
     const int64_t at = unit - (int64_t)p.sum_blocks * kSumWarps;
-    const int64_t v0 = at / p.fill_parts * kFillRows;
+    const int64_t v0 = at / p.fill_parts << p.fill_shift;
     uint32_t used = 0;
-    for (int i = lane; i < p.n; i += 32) used |= keys[i] >= v0 && keys[i] < v0 + kFillRows && keys[i] < p.vocab ? 1u << (keys[i] - v0) : 0u;
+    for (int i = lane; i < p.n; i += 32) used |= keys[i] >= v0 && keys[i] < v0 + (1 << p.fill_shift) && keys[i] < p.vocab ? 1u << (keys[i] - v0) : 0u;
     fill_rows<GT>(p, v0, (int)(at % p.fill_parts), __reduce_or_sync(~0u, used));
     return;
   }
@@ -733,15 +805,19 @@ extern "C" int iris_embed_tokens_backward(const iris_embed_grad_args* a, void* s
   IRIS_CHECK(check_aligned(fn, "workspace", a->workspace, 16, true));
   if (a->workspace_bytes < g.bytes) return fail(IRIS_ERR_ARG, "%s: workspace has %zu bytes, the call needs %zu", fn, a->workspace_bytes, g.bytes);
   const bool few = a->n <= kFewTokens;
-  const int fill_parts = (int)((a->dim * gs + kFillBytes - 1) / kFillBytes), tiles = few ? (int)((a->dim + kWarpColumns - 1) / kWarpColumns) : g.tiles;
+  const int fill_parts = (int)((a->dim * gs + kFillBytes - 1) / kFillBytes);
+  int fill_shift = 0;
+  while (fill_shift < 5 && (a->dim * gs << (fill_shift + 1)) <= kFillBytes) ++fill_shift;
+  const int tiles = few ? (int)((a->dim + kWarpColumns - 1) / kWarpColumns) : g.tiles;
   const int64_t units = few ? a->n * tiles : (int64_t)g.chunks * g.tiles, sum_blocks = (units + kSumWarps - 1) / kSumWarps;
-  const int64_t fill_blocks = a->accumulate ? 0 : ((a->vocab + kFillRows - 1) / kFillRows * fill_parts + kSumWarps - 1) / kSumWarps;
+  const int64_t fill_blocks = a->accumulate ? 0 : (((a->vocab + (1 << fill_shift) - 1) >> fill_shift) * fill_parts + kSumWarps - 1) / kSumWarps;
   if (sum_blocks + fill_blocks > INT32_MAX || units > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 blocks", fn);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   char* const ws = static_cast<char*>(a->workspace);
   p.dim = (int)a->dim;
   p.part_stride = part_stride(a->dim);
   p.fill_parts = fill_parts;
+  p.fill_shift = fill_shift;
   p.tiles = tiles;
   p.sum_blocks = (unsigned)sum_blocks;
   p.n = (int)a->n;
