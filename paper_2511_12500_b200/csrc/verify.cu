@@ -9,7 +9,7 @@ namespace iris {
 namespace rows {
 
 constexpr int kVerifyThreads = 256, kVerifyWarps = kVerifyThreads / 32;
-constexpr int kVerifySplit = 8;      // blocks (one cluster) that share a row
+constexpr int kVerifySplit = 16;     // blocks (one cluster) that share a row
 constexpr int kMaxDrafts = 128;
 
 // What is known of a place of a sequence: largest logit and sum exp(scale (z - largest)) of the target's row and the draft's, both logits of the
@@ -38,76 +38,92 @@ __device__ __forceinline__ float scale_of(const VerifyParams& p, int b) {
 }
 __device__ __forceinline__ bool is_greedy(float scale) { return scale > kMaxScale; }
 
-// The block's share of a row: largest logit and sum.
+// The block's share of a row: largest logit and sum; the next batch is under way while one is summed.
 template <int DT>
-__device__ __forceinline__ Acc sum_part(const Row<DT>& row, const Part<DT>& part, float k, float4* upper, Warps<kVerifyWarps>& buf) {
-  constexpr int T = kVerifyThreads, U = 4;
+__device__ __forceinline__ Acc sum_part(const Row<DT>& row, const Part<DT>& part, float k, float4* upper) {
+  constexpr int T = kVerifyThreads, U = 4, B = T * U;
   const int tid = threadIdx.x, n = part.n_all;
   Sums<DT, false, true> sums(k, upper + tid);
-  batches<T, U>(part.n_int, [&](int b, auto all) {
-    if constexpr (decltype(all)::value) {
-      uint4 g[U];
+  const uint4* const from = reinterpret_cast<const uint4*>(row.at(part.w0)) + tid;
+  uint4 g[U], h[U];
+  const auto fetch = [&](int at, uint4(&to)[U]) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) g[u] = ld_once(row.at(part.w0 + b + u * T + tid));
-      sums.template pace<T, U>(b);
-      sums.template add<true>(g, largest<DT, true>(g, 0, T));
-    }
-  });
-  for (int b = part.n_int / (T * U) * (T * U); b < n; b += T * U) {
+    for (int u = 0; u < U; ++u) to[u] = ld_once(from + at + u * T);
+  };
+  int b = 0;
+  if (B <= part.n_int) fetch(0, g);
+  for (; b + 3 * B <= part.n_int; b += 2 * B) {
+    fetch(b + B, h);
+    sums.template add<true>(g, largest<DT, true>(g, 0, T));
+    fetch(b + 2 * B, g);
+    sums.template add<true>(h, largest<DT, true>(h, 0, T));
+    sums.template pace<T, U>(b);
+  }
+  if (b + 2 * B <= part.n_int) {
+    fetch(b + B, h);
+    sums.template add<true>(g, largest<DT, true>(g, 0, T));
+    sums.template add<true>(h, largest<DT, true>(h, 0, T));
+    b += 2 * B;
+  } else if (b + B <= part.n_int) {
+    sums.template add<true>(g, largest<DT, true>(g, 0, T));
+    b += B;
+  }
+  for (; b < n; b += B) {
     const int left = n - b - tid;
-    uint4 g[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (u * T < left) g[u] = part.raw(row, b + u * T + tid);
-    sums.template pace<T, U>(b);
     sums.template add<false>(g, largest<DT, false>(g, left, T), left, T);
   }
-  warp_share<false>(sums.done(), k, buf);
-  __syncthreads();
-  const Acc a = warps_join<false>(k, buf);
-  __syncthreads();
-  return a;
+  return sums.done();
 }
-
 __device__ __forceinline__ uint64_t larger_key(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
-// The block's share of a row: the key of its largest logit, 0 where none is left.
+// The block's share of a row: the key of its largest logit, 0 where none is left.  A thread remembers its largest logit and the first of its batches that
+// has it, and looks at that again in the end.  (What the row covers of granules in part comes last, and has keys of its own.)
 template <int DT>
 __device__ __forceinline__ uint64_t best_part(const Row<DT>& row, const Part<DT>& part, uint64_t (&of_warp)[kVerifyWarps]) {
-  constexpr int T = kVerifyThreads, U = 4;
-  const int tid = threadIdx.x, n = part.n_all;
+  constexpr int T = kVerifyThreads, U = 4, B = T * U, VE = Elem<DT>::VE;
+  const int tid = threadIdx.x, n = part.n_int;
   uint64_t key = 0;
   float best = -INFINITY;
   int at = -1;
-  for (int b = 0; b < n; b += T * U) {
-    const int left = n - b - tid;
-    uint4 g[U];
+  const uint4* const from = reinterpret_cast<const uint4*>(row.at(part.w0)) + tid;
+  const auto keys_of = [&](const uint4& g, int granule) {
+    float y[VE];
+    Elem<DT>::unpack(g, y);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (u * T < left) g[u] = part.raw(row, b + u * T + tid);
+    for (int e = 0; e < VE; ++e)
+      if (y[e] != -INFINITY) key = larger_key(key, order_key<DT>(y[e], granule * VE + e - row.ph));
+  };
+  uint4 g[U], h[U];
+  const auto fetch = [&](int b, uint4(&to)[U]) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (u * T < left) {
-        const float x = largest<DT>(g[u]);
-        if (x > best || x != x) {
-          best = x;
-          at = part.granule(b + u * T + tid);
-          float y[Elem<DT>::VE];   // columns of a thread need not rise (partial granules come last): keys decide
-          Elem<DT>::unpack(g[u], y);
-          uint64_t k = 0;
-#pragma unroll
-          for (int e = 0; e < Elem<DT>::VE; ++e) k = larger_key(k, y[e] == -INFINITY ? 0 : order_key<DT>(y[e], at * Elem<DT>::VE + e - row.ph));
-          key = larger_key(key, k);
-        } else if (x == best && at > part.granule(b + u * T + tid)) {
-          float y[Elem<DT>::VE];
-          at = part.granule(b + u * T + tid);
-          Elem<DT>::unpack(g[u], y);
-#pragma unroll
-          for (int e = 0; e < Elem<DT>::VE; ++e)
-            if (y[e] == best) key = larger_key(key, order_key<DT>(y[e], at * Elem<DT>::VE + e - row.ph));
-        }
-      }
+    for (int u = 0; u < U; ++u) to[u] = ld_once(from + b + u * T);
+  };
+  const auto look = [&](int b, const uint4(&x)[U]) {
+    const float mx = largest<DT, true>(x, 0, T);
+    if (mx > best || mx != mx) {   // NaN comes before all
+      best = mx;
+      at = b;
+    }
+  };
+  int b = 0;
+  if (B <= n) fetch(0, g);
+  for (; b + 2 * B <= n; b += 2 * B) {
+    fetch(b + B, h);
+    look(b, g);
+    if (b + 3 * B <= n) fetch(b + 2 * B, g);
+    look(b + B, h);
   }
+  if (b + B <= n) {
+    look(b, g);
+    b += B;
+  }
+  for (int i = b + tid; i < part.n_all; i += T) keys_of(part.raw(row, i), part.granule(i));
+  if (at >= 0)
+#pragma unroll
+    for (int u = 0; u < U; ++u) keys_of(from[at + u * T], part.w0 + at + u * T + tid);
 #pragma unroll
   for (int o = 16; o; o >>= 1) key = larger_key(key, __shfl_xor_sync(~0u, key, o));
   if ((tid & 31) == 0) of_warp[tid >> 5] = key;
@@ -118,34 +134,39 @@ __device__ __forceinline__ uint64_t best_part(const Row<DT>& row, const Part<DT>
   return key;
 }
 
-// One cluster of `split` blocks a place of a sequence: what the drawing needs of its rows.
+// One cluster of `split` blocks a row, the target's first: what the drawing needs of it.
+//
+// Bound by memory where there are many rows.  Rows behind a draft that is refused need not be read, but to know that in time takes longer than to read them:
+// places one after the other, in clusters that leave out what follows, 64 sequences of 4 drafts over 128000 tokens took 53 us, all at once 34.
 template <int DT>
 __global__ void __launch_bounds__(kVerifyThreads, 4) verify_rows_kernel(const __grid_constant__ VerifyParams p) {
   using E = Elem<DT>;
   __shared__ Warps<kVerifyWarps> buf;
-  __shared__ Warps<kVerifySplit> parts, draft_parts;   // of the cluster's blocks, in the first one
+  __shared__ Warps<kVerifySplit> parts;   // of the cluster's blocks, in the first one
   __shared__ uint64_t keys[kVerifySplit], of_warp[kVerifyWarps];
   __shared__ float4 upper[kVerifyThreads];
   const int split = p.split, rank = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x;
-  const int place = blockIdx.x / split, b = place % p.sequences, i = place / p.sequences;
-  ptx::let_next_begin();
+  const int unit = blockIdx.x / split, targets = p.sequences * (p.drafts + 1);
+  const bool draft = unit >= targets;
+  const int each = p.drafts + !draft, in = draft ? unit - targets : unit, b = in / each, i = in - b * each;   // place i of sequence b
   if (tid < kVerifySplit) {
-    parts.of[tid] = draft_parts.of[tid] = Acc{};
+    parts.of[tid] = Acc{};
     keys[tid] = 0;
   }
-  if (split > 1) ptx::cluster_sync();   // the others may write to the first block
+  if (split > 1) ptx::cluster_arrive_release();   // behind the wait the others may write to the first block
+  ptx::let_next_begin();
   ptx::begin_after_previous();
   const int64_t* const ids = p.ids + (int64_t)b * p.drafts;
-  bool gone = false;   // a draft before this place is absent
-  for (int j = tid; j < i; j += kVerifyThreads) gone |= ids[j] < 0 || ids[j] >= p.vocab;
-  if (__syncthreads_or(gone)) return;   // all blocks of the cluster
-  const int64_t id = i < p.drafts ? ids[i] : -1;
-  const bool drafted = id >= 0 && id < p.vocab;
   const float scale = scale_of(p, b), k = scale * kLog2e;
-  const int64_t r = (int64_t)b * (p.drafts + 1) + i;
-  const Row<DT> row(p.logits, r, p.stride, p.vocab);
-  const Part<DT> part(row, rank, p.each);
-  Seat* const seat = p.seats + r;
+  const int64_t id = i < p.drafts ? ids[i] : -1;
+  const bool there = id >= 0 && id < p.vocab;
+  bool absent = draft && (!there || is_greedy(scale));   // or a draft before this place is: the row is not needed
+  for (int j = tid; j < i; j += kVerifyThreads) absent |= ids[j] < 0 || ids[j] >= p.vocab;
+  if (split > 1) ptx::cluster_wait();
+  if (__syncthreads_or(absent)) return;   // all blocks of the cluster
+  const Row<DT> row(draft ? p.draft_logits : p.logits, in, draft ? p.draft_stride : p.stride, p.vocab);
+  const Part<DT> part(row, rank, draft ? p.draft_each : p.each);
+  Seat* const seat = p.seats + (int64_t)b * (p.drafts + 1) + i;
   if (is_greedy(scale)) {
     uint64_t key = best_part<DT>(row, part, of_warp);
     if (split > 1) {
@@ -154,63 +175,80 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_rows_kernel(const __
       key = 0;
       for (int s = 0; s < split; ++s) key = larger_key(key, keys[s]);
     }
-    if (rank == 0 && tid == 0) {
-      const float x = key_value<DT>(key);
-      seat->best = key && fabsf(x) < INFINITY ? key_column(key) : -1;
-    }
+    if (rank == 0 && tid == 0) seat->best = key && fabsf(key_value<DT>(key)) < INFINITY ? key_column(key) : -1;
     return;
   }
-  const bool draft = drafted && p.draft_logits;
-  const Row<DT> draft_row(p.draft_logits, draft ? (int64_t)b * p.drafts + i : 0, p.draft_stride, p.vocab);
-  Acc a = sum_part<DT>(row, part, k, upper, buf), aq;
-  if (draft) aq = sum_part<DT>(draft_row, Part<DT>(draft_row, rank, p.draft_each), k, upper, buf);
+  const float z = rank == 0 && tid == 0 && there ? E::to(row.column((int)id)) : 0.f;
+  Acc a = sum_part<DT>(row, part, k, upper);
+  warp_share<false>(a, k, buf);
+  __syncthreads();
+  a = warps_join<false>(k, buf);
   if (split > 1) {
     if (tid == 0) {
-      const uint32_t to = ptx::mapa(ptx::smem_u32(&parts.of[rank]), 0), to_q = ptx::mapa(ptx::smem_u32(&draft_parts.of[rank]), 0);
+      const uint32_t to = ptx::mapa(ptx::smem_u32(&parts.of[rank]), 0);
       ptx::st_shared_cluster_u32(to, __float_as_uint(a.m));
       ptx::st_shared_cluster_u32(to + 4, __float_as_uint(a.s));
-      ptx::st_shared_cluster_u32(to_q, __float_as_uint(aq.m));
-      ptx::st_shared_cluster_u32(to_q + 4, __float_as_uint(aq.s));
     }
     ptx::cluster_sync();
     if (rank) return;
     a = warps_join<false>(k, parts);
-    aq = warps_join<false>(k, draft_parts);
   }
   if (tid == 0) {
-    Seat s{a.m, a.s, aq.m, aq.s, 0.f, 0.f, -1, 0};
-    if (drafted) s.z = E::to(row.column((int)id));
-    if (draft) s.zq = E::to(draft_row.column((int)id));
-    *seat = s;
+    (draft ? seat->mq : seat->m) = a.m;
+    (draft ? seat->sq : seat->s) = a.s;
+    (draft ? seat->zq : seat->z) = z;
   }
 }
 
 __device__ __forceinline__ double prob(float z, float m, float s, float scale) {
   return z == -INFINITY ? 0. : exp(((double)z - (double)m) * (double)scale) / (double)s;
 }
+// Whether a draft is accepted: in 32 bits, and in 64 where that is too near to tell (or NaN).
+__device__ __forceinline__ bool accepts(const Seat& s, float u, bool with_q, float scale) {
+  const float k = scale * kLog2e;
+  const float pd = ex2((s.z - s.m) * k) / s.s, qd = with_q ? ex2((s.zq - s.mq) * k) / s.sq : 1.f, t = u * qd;
+  if (fabsf(t - pd) > 1e-4f * fmaxf(t, pd) && fmaxf(t, pd) > 1e-30f) return t < pd;
+  return (double)u * (with_q ? prob(s.zq, s.mq, s.sq, scale) : 1.) < prob(s.z, s.m, s.s, scale);
+}
+__device__ __forceinline__ float log_prob64(float z, const Seat& s, float scale) {   // rounded once but for the logarithm
+  return (float)(((double)z - (double)s.m) * (double)scale - (double)logf(s.s));
+}
 
 struct Runner {   // of the race; column -1: none
-  double score;
+  float score;
   int column;
-  __device__ __forceinline__ void meet(double s, int c) {
-    if (c >= 0 && (column < 0 || s > score || (s == score && c < column))) {
-      score = s;
-      column = c;
-    }
-  }
 };
+// The winner among n runners, which all threads of the warp get: n <= 32, thread i has runner i.  Those whose scores are too near one another for 32
+// bits are compared in 64 (`exactly`: the score of a column); the lowest column among equal ones.
+template <class F>
+__device__ __forceinline__ Runner winner(Runner r, F exactly) {
+  const float best = warp_max(r.column >= 0 ? r.score : -1.f);
+  const uint32_t near = __ballot_sync(~0u, r.column >= 0 && !(r.score < best * (1.f - 1e-4f)));
+  if (!near) return Runner{0.f, -1};
+  double score = r.score;
+  if (near & (near - 1)) score = near >> (threadIdx.x & 31) & 1 ? exactly(r.column) : 0.;
+  int at = __ffs(near) - 1;
+  for (uint32_t rest = near & (near - 1); rest; rest &= rest - 1) {
+    const int i = __ffs(rest) - 1;
+    const double a = __shfl_sync(~0u, score, at), b = __shfl_sync(~0u, score, i);
+    const int ca = __shfl_sync(~0u, r.column, at), cb = __shfl_sync(~0u, r.column, i);
+    if (b > a || (b == a && cb < ca)) at = i;
+  }
+  return Runner{__shfl_sync(~0u, r.score, at), __shfl_sync(~0u, r.column, at)};
+}
 
 // One cluster of `split` blocks a sequence: accepts drafts up to the first that is refused, and draws the token behind them.
 template <int DT>
-__global__ void __launch_bounds__(kVerifyThreads) verify_draw_kernel(const __grid_constant__ VerifyParams p) {
+__global__ void __launch_bounds__(kVerifyThreads, 4) verify_draw_kernel(const __grid_constant__ VerifyParams p) {
   using E = Elem<DT>;
-  constexpr int T = kVerifyThreads, VE = E::VE, ES = sizeof(typename E::T);
+  constexpr int T = kVerifyThreads, VE = E::VE, ES = sizeof(typename E::T), U = 1;
   __shared__ Runner of_warp[kVerifyWarps], parts[2][kVerifySplit];   // parts: of the cluster's blocks, of the first and the second race
+  static_assert(kVerifyWarps <= 32 && kVerifySplit <= 32, "one a thread");
   __shared__ int stop_at;
   const int split = p.split, rank = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x, lane = tid & 31;
   const int b = blockIdx.x / split, n = p.drafts;
   ptx::let_next_begin();
-  if (split > 1) ptx::cluster_sync();   // the others may write to this block
+  if (split > 1) ptx::cluster_arrive_release();   // behind the wait the others may write to this block
   ptx::begin_after_previous();
   const float scale = scale_of(p, b);
   const bool greedy = is_greedy(scale);
@@ -220,16 +258,8 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_draw_kernel(const __gri
     int stop = 0;
     for (;; stop += 32) {
       const int i = stop + lane;
-      bool ok = false;
-      if (i < n && ids[i] >= 0 && ids[i] < p.vocab) {
-        const Seat s = seats[i];
-        if (greedy) {
-          ok = s.best == (int)ids[i];
-        } else {
-          const double pd = prob(s.z, s.m, s.s, scale), qd = p.draft_logits ? prob(s.zq, s.mq, s.sq, scale) : 1.;
-          ok = (double)p.uniform[(int64_t)b * n + i] * qd < pd;
-        }
-      }
+      bool ok = i < n && ids[i] >= 0 && ids[i] < p.vocab;
+      if (ok) ok = greedy ? seats[i].best == (int)ids[i] : accepts(seats[i], p.uniform[(int64_t)b * n + i], p.draft_logits != nullptr, scale);
       const uint32_t no = __ballot_sync(~0u, !ok);
       if (no) {
         stop += __ffs(no) - 1;
@@ -238,6 +268,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_draw_kernel(const __gri
     }
     if (lane == 0) stop_at = stop;
   }
+  if (split > 1) ptx::cluster_wait();
   __syncthreads();
   const int stop = stop_at;
   const Seat seat = seats[stop];
@@ -255,55 +286,103 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_draw_kernel(const __gri
       const Row<DT> draft_row(p.draft_logits, with_q ? (int64_t)b * n + stop : 0, p.draft_stride, p.vocab);
       const char* const draft = reinterpret_cast<const char*>(draft_row.granule0 + draft_row.ph);
       const float rs = 1.f / seat.s, rsq = with_q ? 1.f / seat.sq : 0.f, mq = with_q ? seat.mq : 0.f;
+      // `score`: the warp's best so far, `best`: the thread's, if it was better than that when it came.
       float score = 0.f;
-      Runner best{0., -1};
-      for (int i = tid; i < part.n_all; i += T) {
-        const int v = part.granule(i), column = v * VE - row.ph;
-        float z[VE], y[VE], e[VE];
-        E::unpack(part.raw(row, i), z);
-        if (with_q) E::unpack(load_piece<ES>(draft + (int64_t)column * ES, draft, draft + (int64_t)p.vocab * ES), y);
+      Runner best{0.f, -1};
+      // A granule's columns c .. c + VE - 1, `there` if the thread has one; w > score e instead of w / e > score, as a new best one is rare.
+      const auto run = [&](bool there, int c, const uint4& zr, const uint4& yr, const uint4 (&er)[VE / 4]) {
+        float z[VE], y[VE], e[VE], w[VE];
+        E::unpack(zr, z);
+        if (with_q) E::unpack(yr, y);
 #pragma unroll
         for (int h = 0; h < VE / 4; ++h) {
-          float four[4];
-          Elem<IRIS_F32>::unpack(load_piece<4>(noise + ((int64_t)column + 4 * h) * 4, noise, noise + (int64_t)p.vocab * 4), four);
-#pragma unroll
-          for (int u = 0; u < 4; ++u) e[4 * h + u] = four[u];
+          e[4 * h] = __uint_as_float(er[h].x), e[4 * h + 1] = __uint_as_float(er[h].y);
+          e[4 * h + 2] = __uint_as_float(er[h].z), e[4 * h + 3] = __uint_as_float(er[h].w);
         }
+        bool any = false;
 #pragma unroll
         for (int u = 0; u < VE; ++u) {
-          float w = ex2((z[u] - seat.m) * k) * rs;
-          if (with_q) w -= ex2((y[u] - mq) * k) * rsq;
-          if (column + u == without) w = 0.f;
-          const float x = __fdividef(w, e[u]);
-          if (w > 0.f && (x > score || (x == score && column + u < best.column))) {
-            score = x;
-            best.column = column + u;
+          w[u] = ex2((z[u] - seat.m) * k) * rs;
+          if (with_q) w[u] = fmaf(ex2((y[u] - mq) * k), -rsq, w[u]);
+          any |= w[u] > 0.f && !(w[u] <= score * e[u]);
+        }
+        if (!__any_sync(~0u, there && any)) return;
+        if (there) {
+#pragma unroll
+          for (int u = 0; u < VE; ++u) {
+            const float x = __fdividef(w[u], e[u]);
+            if (w[u] > 0.f && c + u != without && x > 0.f && (x > best.score || (x == best.score && c + u < best.column))) best = Runner{x, c + u};
           }
         }
+        score = warp_max(best.score);
+      };
+      const auto column_of = [&](int i) { return part.granule(i) * VE - row.ph; };
+      const auto alone = [&](bool there, int i) {   // where what the columns' 16 bytes touch may leave the rows
+        const int c = there ? column_of(i) : 0;
+        uint4 z = make_uint4(0, 0, 0, 0), y = z, e[VE / 4];
+        if (there) {
+          z = part.raw(row, i);
+          if (with_q) y = load_piece<ES>(draft + (int64_t)c * ES, draft, draft + (int64_t)p.vocab * ES);
+        }
+#pragma unroll
+        for (int h = 0; h < VE / 4; ++h) e[h] = there ? load_piece<4>(noise + ((int64_t)c + 4 * h) * 4, noise, noise + (int64_t)p.vocab * 4) : z;
+        run(there, c, z, y, e);
+      };
+      // The row's first columns, if they do not fill a granule, then those of the granules, then the last ones; the ends by the first warp.
+      if (tid < 32 && part.v0 < part.w0) alone(lane == 0, part.n_int);
+      const uint32_t aq = phase(draft - (int64_t)row.ph * ES), ae = phase(noise - (int64_t)row.ph * 4);   // of every granule
+      for (int at = 0; at < part.n_int; at += U * T) {
+        uint4 zr[U], yr[U], yn[U], er[U][VE / 4], last[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = at + u * T + tid, c = column_of(i);
+          if (i >= part.n_int || c < VE || c + 2 * VE > p.vocab) continue;
+          zr[u] = ld_once(row.at(part.w0 + i));
+          if (with_q) {
+            const char* const from = draft + (int64_t)c * ES - aq;
+            yr[u] = ld_global_v4(from);
+            if (aq) yn[u] = ld_global_v4(from + 16);
+          }
+          const char* const from = noise + (int64_t)c * 4 - ae;
+#pragma unroll
+          for (int h = 0; h < VE / 4; ++h) er[u][h] = ld_global_v4(from + h * 16);
+          if (ae) last[u] = ld_global_v4(from + VE * 4);
+        }
+        if (with_q && aq) cut_all(yr, yn, aq);
+        if (ae) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            uint4 follow[VE / 4];
+#pragma unroll
+            for (int h = 0; h < VE / 4; ++h) follow[h] = h + 1 < VE / 4 ? er[u][h + 1 < VE / 4 ? h + 1 : 0] : last[u];
+            cut_all(er[u], follow, ae);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = at + u * T + tid, c = column_of(i);
+          const bool there = i < part.n_int, end = there && (c < VE || c + 2 * VE > p.vocab);
+          if (__any_sync(~0u, end)) alone(end, i);
+          run(there && !end, c, zr[u], yr[u], er[u]);
+        }
       }
-      if (best.column >= 0) {   // in 64 bits: the race between threads, blocks
-        const int c = best.column;
+      if (tid < 32 && part.n_all > part.n_int + (part.v0 < part.w0)) alone(lane == 0, part.n_all - 1);
+      const auto exactly = [&](int c) {
         double w = prob(E::to(row.column(c)), seat.m, seat.s, scale);
         if (with_q) w -= prob(E::to(draft_row.column(c)), seat.mq, seat.sq, scale);
-        best.score = w / (double)p.noise[(int64_t)b * p.vocab + c];
-      }
-#pragma unroll
-      for (int o = 16; o; o >>= 1) {
-        const double s = __shfl_xor_sync(~0u, best.score, o);
-        const int c = __shfl_xor_sync(~0u, best.column, o);
-        best.meet(s, c);
-      }
+        return w / (double)p.noise[(int64_t)b * p.vocab + c];
+      };
+      best = winner(best, exactly);
       if (lane == 0) of_warp[tid >> 5] = best;
       __syncthreads();
-      for (int w = 0; w < kVerifyWarps; ++w) best.meet(of_warp[w].score, of_warp[w].column);
+      best = winner(lane < kVerifyWarps ? of_warp[lane] : Runner{0.f, -1}, exactly);
       if (split > 1) {
         if (tid < split) {
           const uint32_t to = ptx::mapa(ptx::smem_u32(&parts[race][rank]), tid);
-          ptx::st_shared_cluster_u64(to, (uint64_t)__double_as_longlong(best.score));
-          ptx::st_shared_cluster_u32(to + 8, (uint32_t)best.column);
+          ptx::st_shared_cluster_u64(to, (uint64_t)(uint32_t)best.column << 32 | __float_as_uint(best.score));
         }
         ptx::cluster_sync();
-        for (int s = 0; s < split; ++s) best.meet(parts[race][s].score, parts[race][s].column);
+        best = winner(lane < split ? parts[race][lane] : Runner{0.f, -1}, exactly);
       }
       next = best.column;
       if (next >= 0) break;   // all blocks of the cluster
@@ -316,9 +395,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_draw_kernel(const __gri
     p.tokens[(int64_t)b * (n + 1) + i] = token;
     if (p.logprob) {
       const Seat s = i < stop ? seats[i] : seat;
-      double lp = 0.;
-      if (token >= 0 && !greedy) lp = ((double)(i < stop ? s.z : E::to(row.column(next))) - (double)s.m) * (double)scale - log((double)s.s);
-      p.logprob[(int64_t)b * (n + 1) + i] = (float)lp;
+      p.logprob[(int64_t)b * (n + 1) + i] = token < 0 || greedy ? 0.f : log_prob64(i < stop ? s.z : E::to(row.column(next)), s, scale);
     }
   }
   if (tid == 0) p.accepted[b] = stop;
@@ -326,18 +403,20 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_draw_kernel(const __gri
 
 template <int DT>
 static int launch_verify(VerifyParams p, const iris_verify_args* a, cudaStream_t st) {
-  const auto split_for = [&](int64_t rows, int least, int full) {   // a row is shared while rows alone leave SMs without work
-    const int64_t granules = part_granules(a->logits, p.stride, p.vocab, a->dtype, 1);
+  IRIS_CHECK(allow_shared<verify_rows_kernel<DT>>(0, true));
+  IRIS_CHECK(allow_shared<verify_draw_kernel<DT>>(0, true));
+  const int64_t granules = part_granules(a->logits, p.stride, p.vocab, a->dtype, 1);
+  const auto share = [&](int64_t rows, int least) {   // a row is shared while rows alone leave SMs without work and a block has at least so many granules
     int split = 1;
-    while (split < kVerifySplit && rows * split < full && granules > (int64_t)split * least) split *= 2;
+    while (split < kVerifySplit && rows * split * 2 <= kSms * 4 && granules > (int64_t)split * least) split *= 2;
     p.split = split;
     p.each = part_granules(a->logits, p.stride, p.vocab, a->dtype, split);
     p.draft_each = a->draft_logits ? part_granules(a->draft_logits, p.draft_stride, p.vocab, a->dtype, split) : 0;
   };
-  const int64_t places = (int64_t)p.sequences * (p.drafts + 1);
-  split_for(places, 1024, kSms * 5 / 2);
-  IRIS_CHECK(launch_rows(verify_rows_kernel<DT>, p, (unsigned)(places * p.split), p.split, kVerifyThreads, 0, st));
-  split_for(p.sequences, 512, kSms * 5 / 2);
+  const int64_t rows = (int64_t)p.sequences * (p.drafts + 1 + (p.draft_logits ? p.drafts : 0));
+  share(rows, 512);
+  IRIS_CHECK(launch_rows(verify_rows_kernel<DT>, p, (unsigned)(rows * p.split), p.split, kVerifyThreads, 0, st));
+  share(p.sequences, 256);
   return launch_rows(verify_draw_kernel<DT>, p, (unsigned)(p.sequences * p.split), p.split, kVerifyThreads, 0, st);
 }
 
@@ -357,7 +436,7 @@ extern "C" int iris_verify_drafts(const iris_verify_args* a, void* stream) {
   if (!a) return fail(IRIS_ERR_ARG, "%s: args is NULL", fn);
   if (a->drafts < 0 || a->drafts > kMaxDrafts) return fail(IRIS_ERR_ARG, "%s: drafts=%d not in [0, %d]", fn, a->drafts, kMaxDrafts);
   if (a->sequences < 0) return fail(IRIS_ERR_ARG, "%s: sequences=%lld", fn, (long long)a->sequences);
-  if (a->sequences > INT32_MAX / (kMaxDrafts + 1) / kVerifySplit) return fail(IRIS_ERR_UNSUPPORTED, "%s: too many sequences", fn);
+  if (a->sequences > INT32_MAX / (2 * kMaxDrafts + 1) / kVerifySplit) return fail(IRIS_ERR_UNSUPPORTED, "%s: too many sequences", fn);
   int64_t stride = a->row_stride, dstride = a->draft_stride;
   const int64_t rows = a->sequences * (a->drafts + 1);
   IRIS_CHECK(check_logits(fn, "logits", a->logits, a->dtype, rows, a->vocab, &stride));
