@@ -214,6 +214,11 @@ __device__ __forceinline__ float log_prob64(float z, const Seat& s, float scale)
   return (float)(((double)z - (double)s.m) * (double)scale - (double)logf(s.s));
 }
 
+__device__ __forceinline__ float reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 struct Runner {   // of the race; column -1: none
   float score;
   int column;
@@ -241,9 +246,12 @@ __device__ __forceinline__ Runner winner(Runner r, F exactly) {
 template <int DT>
 __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draw_kernel(const __grid_constant__ VerifyParams p) {
   using E = Elem<DT>;
-  constexpr int T = kVerifyThreads, VE = E::VE, ES = sizeof(typename E::T), U = 1;
-  __shared__ Runner of_warp[kVerifyWarps], parts[2][kVerifySplit];   // parts: of the cluster's blocks, of the first and the second race
-  static_assert(kVerifyWarps <= 32 && kVerifySplit <= 32, "one a thread");
+  constexpr int T = kVerifyThreads, VE = E::VE, ES = sizeof(typename E::T);
+  __shared__ Runner block_best, parts[2][kVerifySplit];   // parts: of the cluster's blocks, of the first and the second race
+  __shared__ float of_warp[kVerifyWarps];
+  __shared__ unsigned long long exact_best;
+  __shared__ int lowest;
+  static_assert(kVerifySplit <= 32, "one a thread");
   __shared__ int stop_at;
   const int split = p.split, rank = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x, lane = tid & 31;
   const int b = blockIdx.x / split, n = p.drafts;
@@ -286,96 +294,110 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draw_kernel(const __
       const Row<DT> draft_row(p.draft_logits, with_q ? (int64_t)b * n + stop : 0, p.draft_stride, p.vocab);
       const char* const draft = reinterpret_cast<const char*>(draft_row.granule0 + draft_row.ph);
       const float rs = 1.f / seat.s, rsq = with_q ? 1.f / seat.sq : 0.f, mq = with_q ? seat.mq : 0.f;
-      // `score`: the warp's best so far, `best`: the thread's, if it was better than that when it came.
-      float score = 0.f;
-      Runner best{0.f, -1};
-      // A granule's columns c .. c + VE - 1, `there` if the thread has one; w > score e instead of w / e > score, as a new best one is rare.
-      const auto run = [&](bool there, int c, const uint4& zr, const uint4& yr, const uint4 (&er)[VE / 4]) {
-        float z[VE], y[VE], e[VE], w[VE];
-        E::unpack(zr, z);
-        if (with_q) E::unpack(yr, y);
-#pragma unroll
-        for (int h = 0; h < VE / 4; ++h) {
-          e[4 * h] = __uint_as_float(er[h].x), e[4 * h + 1] = __uint_as_float(er[h].y);
-          e[4 * h + 2] = __uint_as_float(er[h].z), e[4 * h + 3] = __uint_as_float(er[h].w);
-        }
-        bool any = false;
-#pragma unroll
-        for (int u = 0; u < VE; ++u) {
-          w[u] = ex2((z[u] - seat.m) * k) * rs;
-          if (with_q) w[u] = fmaf(ex2((y[u] - mq) * k), -rsq, w[u]);
-          any |= w[u] > 0.f && !(w[u] <= score * e[u]);
-        }
-        if (!__any_sync(~0u, there && any)) return;
-        if (there) {
-#pragma unroll
-          for (int u = 0; u < VE; ++u) {
-            const float x = __fdividef(w[u], e[u]);
-            if (w[u] > 0.f && c + u != without && x > 0.f && (x > best.score || (x == best.score && c + u < best.column))) best = Runner{x, c + u};
-          }
-        }
-        score = warp_max(best.score);
-      };
-      const auto column_of = [&](int i) { return part.granule(i) * VE - row.ph; };
-      const auto alone = [&](bool there, int i) {   // where what the columns' 16 bytes touch may leave the rows
-        const int c = there ? column_of(i) : 0;
-        uint4 z = make_uint4(0, 0, 0, 0), y = z, e[VE / 4];
-        if (there) {
-          z = part.raw(row, i);
-          if (with_q) y = load_piece<ES>(draft + (int64_t)c * ES, draft, draft + (int64_t)p.vocab * ES);
-        }
-#pragma unroll
-        for (int h = 0; h < VE / 4; ++h) e[h] = there ? load_piece<4>(noise + ((int64_t)c + 4 * h) * 4, noise, noise + (int64_t)p.vocab * 4) : z;
-        run(there, c, z, y, e);
-      };
-      // The row's first columns, if they do not fill a granule, then those of the granules, then the last ones; the ends by the first warp.
-      if (tid < 32 && part.v0 < part.w0) alone(lane == 0, part.n_int);
       const uint32_t aq = phase(draft - (int64_t)row.ph * ES), ae = phase(noise - (int64_t)row.ph * 4);   // of every granule
-      for (int at = 0; at < part.n_int; at += U * T) {
-        uint4 zr[U], yr[U], yn[U], er[U][VE / 4], last[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int i = at + u * T + tid, c = column_of(i);
-          if (i >= part.n_int || c < VE || c + 2 * VE > p.vocab) continue;
-          zr[u] = ld_once(row.at(part.w0 + i));
+      // The scores of granule v: max(0, weight) / noise.
+      const auto scores = [&](int v, float (&x)[VE]) {
+        const int c = v * VE - row.ph;
+        uint4 zr[1], yr[1], e[VE / 4];
+        if (c >= VE && c + 2 * VE <= p.vocab) {
+          uint4 yn[1], en[VE / 4];
+          zr[0] = ld_once(row.at(v));
           if (with_q) {
             const char* const from = draft + (int64_t)c * ES - aq;
-            yr[u] = ld_global_v4(from);
-            if (aq) yn[u] = ld_global_v4(from + 16);
+            yr[0] = ld_global_v4(from);
+            if (aq) yn[0] = ld_global_v4(from + 16);
           }
           const char* const from = noise + (int64_t)c * 4 - ae;
 #pragma unroll
-          for (int h = 0; h < VE / 4; ++h) er[u][h] = ld_global_v4(from + h * 16);
-          if (ae) last[u] = ld_global_v4(from + VE * 4);
-        }
-        if (with_q && aq) cut_all(yr, yn, aq);
-        if (ae) {
+          for (int h = 0; h < VE / 4; ++h) e[h] = ld_global_v4(from + h * 16);
+          if (ae) {
+            en[VE / 4 - 1] = ld_global_v4(from + VE * 4);
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            uint4 follow[VE / 4];
-#pragma unroll
-            for (int h = 0; h < VE / 4; ++h) follow[h] = h + 1 < VE / 4 ? er[u][h + 1 < VE / 4 ? h + 1 : 0] : last[u];
-            cut_all(er[u], follow, ae);
+            for (int h = 0; h + 1 < VE / 4; ++h) en[h] = e[h + 1];
+            cut_all(e, en, ae);
           }
+          if (with_q && aq) cut_all(yr, yn, aq);
+        } else {   // what the columns' 16 bytes touch may leave the rows
+          zr[0] = row.raw(v);
+          if (with_q) yr[0] = load_piece<ES>(draft + (int64_t)c * ES, draft, draft + (int64_t)p.vocab * ES);
+#pragma unroll
+          for (int h = 0; h < VE / 4; ++h) e[h] = load_piece<4>(noise + ((int64_t)c + 4 * h) * 4, noise, noise + (int64_t)p.vocab * 4);
+        }
+        float z[VE], y[VE], f[VE];
+        E::unpack(zr[0], z);
+#pragma unroll
+        for (int h = 0; h < VE / 4; ++h) {
+          f[4 * h] = __uint_as_float(e[h].x), f[4 * h + 1] = __uint_as_float(e[h].y), f[4 * h + 2] = __uint_as_float(e[h].z), f[4 * h + 3] = __uint_as_float(e[h].w);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int i = at + u * T + tid, c = column_of(i);
-          const bool there = i < part.n_int, end = there && (c < VE || c + 2 * VE > p.vocab);
-          if (__any_sync(~0u, end)) alone(end, i);
-          run(there && !end, c, zr[u], yr[u], er[u]);
+        for (int u = 0; u < VE; ++u) x[u] = ex2((z[u] - seat.m) * k) * rs;
+        if (with_q) {
+          E::unpack(yr[0], y);
+#pragma unroll
+          for (int u = 0; u < VE; ++u) x[u] = fmaf(ex2((y[u] - mq) * k), -rsq, x[u]);
+        }
+        if ((uint32_t)(without - c) < (uint32_t)VE) {
+#pragma unroll
+          for (int u = 0; u < VE; ++u) x[u] = c + u == without ? 0.f : x[u];
+        }
+#pragma unroll
+        for (int u = 0; u < VE; ++u) x[u] = fmaxf(x[u], 0.f) * reciprocal(f[u]);
+      };
+      // The thread's best score and the first of its granules that has it (NaN is no score).
+      float score = 0.f;
+      int at = -1;
+      for (int v = part.v0 + tid; v < part.v1; v += T) {
+        float x[VE], m = 0.f;
+        scores(v, x);
+#pragma unroll
+        for (int u = 0; u < VE; ++u) m = fmaxf(m, x[u]);
+        if (m > score) {
+          score = m;
+          at = v;
         }
       }
-      if (tid < 32 && part.n_all > part.n_int + (part.v0 < part.w0)) alone(lane == 0, part.n_all - 1);
       const auto exactly = [&](int c) {
         double w = prob(E::to(row.column(c)), seat.m, seat.s, scale);
         if (with_q) w -= prob(E::to(draft_row.column(c)), seat.mq, seat.sq, scale);
         return w / (double)p.noise[(int64_t)b * p.vocab + c];
       };
-      best = winner(best, exactly);
-      if (lane == 0) of_warp[tid >> 5] = best;
+      // The block's: its threads whose scores are near the best; if there are several, their exact scores decide, and the lowest column of equal ones.
+      const float of_this = warp_max(score);
+      if (lane == 0) of_warp[tid >> 5] = of_this;
+      if (tid == 0) {
+        block_best = Runner{0.f, -1};
+        exact_best = 0;
+        lowest = INT32_MAX;
+      }
       __syncthreads();
-      best = winner(lane < kVerifyWarps ? of_warp[lane] : Runner{0.f, -1}, exactly);
+      const float top = warp_max(of_warp[lane & (kVerifyWarps - 1)]);
+      const bool near = at >= 0 && !(score < top * (1.f - 1e-4f));
+      int column = 0;
+      if (near) {
+        float x[VE];
+        scores(at, x);
+        float m = 0.f;
+#pragma unroll
+        for (int u = VE - 1; u >= 0; --u)
+          if (x[u] >= m && x[u] > 0.f) {
+            m = x[u];
+            column = at * VE - row.ph + u;
+          }
+      }
+      const bool several = __syncthreads_count(near) > 1;
+      unsigned long long exact = 0;
+      if (several) {
+        if (near) {
+          exact = (unsigned long long)__double_as_longlong(exactly(column));   // of numbers that are not negative the larger has the larger bits
+          atomicMax(&exact_best, exact);
+        }
+        __syncthreads();
+        if (near && exact == exact_best) atomicMin(&lowest, column);
+        __syncthreads();
+      }
+      if (near && (!several || (exact == exact_best && column == lowest))) block_best = Runner{score, column};
+      __syncthreads();
+      Runner best = block_best;
       if (split > 1) {
         if (tid < split) {
           const uint32_t to = ptx::mapa(ptx::smem_u32(&parts[race][rank]), tid);
