@@ -39,19 +39,26 @@ __device__ __forceinline__ float scale_of(const VerifyParams& p, int b) {
 __device__ __forceinline__ bool is_greedy(float scale) { return scale > kMaxScale; }
 
 // The block's share of a row: largest logit and sum; the next batch is under way while one is summed.
+constexpr int kBatch = 4;   // granules of a thread
 template <int DT>
-__device__ __forceinline__ Acc sum_part(const Row<DT>& row, const Part<DT>& part, float k, float4* upper) {
-  constexpr int T = kVerifyThreads, U = 4, B = T * U;
+__device__ __forceinline__ void fetch_first(const Row<DT>& row, const Part<DT>& part, uint4 (&g)[kBatch]) {
+  if (kBatch * kVerifyThreads <= part.n_int)
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) g[u] = ld_once(row.at(part.w0 + u * kVerifyThreads + threadIdx.x));
+}
+// g: of fetch_first.
+template <int DT>
+__device__ __forceinline__ Acc sum_part(const Row<DT>& row, const Part<DT>& part, float k, float4* upper, uint4 (&g)[kBatch]) {
+  constexpr int T = kVerifyThreads, U = kBatch, B = T * U;
   const int tid = threadIdx.x, n = part.n_all;
   Sums<DT, false, true> sums(k, upper + tid);
   const uint4* const from = reinterpret_cast<const uint4*>(row.at(part.w0)) + tid;
-  uint4 g[U], h[U];
+  uint4 h[U];
   const auto fetch = [&](int at, uint4(&to)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u) to[u] = ld_once(from + at + u * T);
   };
   int b = 0;
-  if (B <= part.n_int) fetch(0, g);
   for (; b + 3 * B <= part.n_int; b += 2 * B) {
     fetch(b + B, h);
     sums.template add<true>(g, largest<DT, true>(g, 0, T));
@@ -82,8 +89,8 @@ __device__ __forceinline__ uint64_t larger_key(uint64_t a, uint64_t b) { return 
 // The block's share of a row: the key of its largest logit, 0 where none is left.  A thread remembers its largest logit and the first of its batches that
 // has it, and looks at that again in the end.  (What the row covers of granules in part comes last, and has keys of its own.)
 template <int DT>
-__device__ __forceinline__ uint64_t best_part(const Row<DT>& row, const Part<DT>& part, uint64_t (&of_warp)[kVerifyWarps]) {
-  constexpr int T = kVerifyThreads, U = 4, B = T * U, VE = Elem<DT>::VE;
+__device__ __forceinline__ uint64_t best_part(const Row<DT>& row, const Part<DT>& part, uint64_t (&of_warp)[kVerifyWarps], uint4 (&g)[kBatch]) {
+  constexpr int T = kVerifyThreads, U = kBatch, B = T * U, VE = Elem<DT>::VE;
   const int tid = threadIdx.x, n = part.n_int;
   uint64_t key = 0;
   float best = -INFINITY;
@@ -96,7 +103,7 @@ __device__ __forceinline__ uint64_t best_part(const Row<DT>& row, const Part<DT>
     for (int e = 0; e < VE; ++e)
       if (y[e] != -INFINITY) key = larger_key(key, order_key<DT>(y[e], granule * VE + e - row.ph));
   };
-  uint4 g[U], h[U];
+  uint4 h[U];
   const auto fetch = [&](int b, uint4(&to)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u) to[u] = ld_once(from + b + u * T);
@@ -109,7 +116,6 @@ __device__ __forceinline__ uint64_t best_part(const Row<DT>& row, const Part<DT>
     }
   };
   int b = 0;
-  if (B <= n) fetch(0, g);
   for (; b + 2 * B <= n; b += 2 * B) {
     fetch(b + B, h);
     look(b, g);
@@ -156,6 +162,10 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_rows_kernel(const __
   if (split > 1) ptx::cluster_arrive_release();   // behind the wait the others may write to the first block
   ptx::let_next_begin();
   ptx::begin_after_previous();
+  const Row<DT> row(draft ? p.draft_logits : p.logits, in, draft ? p.draft_stride : p.stride, p.vocab);
+  const Part<DT> part(row, rank, draft ? p.draft_each : p.each);
+  uint4 g[kBatch];
+  fetch_first(row, part, g);   // under way while it turns out whether the row is needed
   const int64_t* const ids = p.ids + (int64_t)b * p.drafts;
   const float scale = scale_of(p, b), k = scale * kLog2e;
   const int64_t id = i < p.drafts ? ids[i] : -1;
@@ -164,11 +174,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_rows_kernel(const __
   for (int j = tid; j < i; j += kVerifyThreads) absent |= ids[j] < 0 || ids[j] >= p.vocab;
   if (split > 1) ptx::cluster_wait();
   if (__syncthreads_or(absent)) return;   // all blocks of the cluster
-  const Row<DT> row(draft ? p.draft_logits : p.logits, in, draft ? p.draft_stride : p.stride, p.vocab);
-  const Part<DT> part(row, rank, draft ? p.draft_each : p.each);
   Seat* const seat = p.seats + (int64_t)b * (p.drafts + 1) + i;
   if (is_greedy(scale)) {
-    uint64_t key = best_part<DT>(row, part, of_warp);
+    uint64_t key = best_part<DT>(row, part, of_warp, g);
     if (split > 1) {
       if (tid == 0) ptx::st_shared_cluster_u64(ptx::mapa(ptx::smem_u32(&keys[rank]), 0), key);
       ptx::cluster_sync();
@@ -179,7 +187,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_rows_kernel(const __
     return;
   }
   const float z = rank == 0 && tid == 0 && there ? E::to(row.column((int)id)) : 0.f;
-  Acc a = sum_part<DT>(row, part, k, upper);
+  Acc a = sum_part<DT>(row, part, k, upper, g);
   warp_share<false>(a, k, buf);
   __syncthreads();
   a = warps_join<false>(k, buf);
@@ -359,7 +367,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draw_kernel(const __
       const auto exactly = [&](int c) {
         double w = prob(E::to(row.column(c)), seat.m, seat.s, scale);
         if (with_q) w -= prob(E::to(draft_row.column(c)), seat.mq, seat.sq, scale);
-        return w / (double)p.noise[(int64_t)b * p.vocab + c];
+        return (w > 0. ? w : 0.) / (double)p.noise[(int64_t)b * p.vocab + c];
       };
       // The block's: its threads whose scores are near the best; if there are several, their exact scores decide, and the lowest column of equal ones.
       const float of_this = warp_max(score);
