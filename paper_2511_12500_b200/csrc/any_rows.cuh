@@ -327,6 +327,95 @@ struct Segment {
   }
 };
 
+// The same for rows that all begin at the same place of 16 bytes (`ph`, in bytes): columns are counted from the aligned 16 bytes in which a row begins, so
+// that no piece has to be cut.  row: that place; dim: columns counted so, up to the row's end; the first ph / ES of them are not the row's.
+template <int DT, int I>
+struct Aligned {
+  using C = Columns<DT>;
+  using Lone = typename Segment<DT, I>::Lone;
+  static constexpr int ES = C::ES, N = C::N, VE = C::E::VE, kColumns = I * kWarpColumns, kBytes = kColumns * ES;
+  static __device__ __forceinline__ bool whole(int begin, int dim, int ph) { return (begin > 0 || ph == 0) && begin + kColumns <= dim; }   // all are the row's
+  static __device__ __forceinline__ void fetch(uint32_t at, const char* row, int begin, int dim, int ph, Lone& lone) {
+    const int lane = threadIdx.x & 31;
+    const char* const p = row + begin * ES + lane * 16;
+    if (whole(begin, dim, ph)) {
+#pragma unroll
+      for (int k = 0; k < I * N; ++k) copy_async(at + (k * 32 + lane) * 16, p + k * 512);
+      return;
+    }
+    const int left = dim * ES - begin * ES - lane * 16;
+#pragma unroll
+    for (int k = 0; k < I * N; ++k) {
+      if (k == 0 && ph && begin + lane == 0) continue;
+      if (k * 512 < left) copy_async_part(at + (k * 32 + lane) * 16, p + k * 512, min(16, left - k * 512));
+      else ptx::st_shared_v4(at + (k * 32 + lane) * 16, make_uint4(0, 0, 0, 0));
+    }
+    if (ph && begin == 0) {   // the row's first elements
+      const int from = lane * 4, bytes = dim * ES;
+      if (lane < 4 && from + 4 > ph && from < bytes) {
+        if (from >= ph && from + 4 <= bytes) {
+          copy_async_word(at + from, row + from);
+        } else if (ES == 2) {   // half a word
+          const int half = from >= ph ? from : from + 2;
+          if (half < bytes) {
+            lone.at = at + half;
+            lone.value = *reinterpret_cast<const uint16_t*>(row + half);
+          }
+        }
+      }
+    }
+  }
+  static __device__ __forceinline__ void read(uint32_t at, int begin, int dim, int ph, int i, uint64_t (&x)[kLaneColumns / 2]) {
+    const int lane = threadIdx.x & 31;
+    uint4 v[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = ld_shared_v4(at + ((i * 32 + lane) * N + n) * 16);
+    if (i == 0 && ph && begin + lane == 0) {   // the aligned 16 bytes in which the row begins (and may end)
+      uint32_t w[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+      for (int e = 0; e < VE; ++e)
+        if (e < ph / ES || e >= dim) w[e * ES / 4] &= ES == 4 ? 0u : e % 2 ? 0xffffu : 0xffff0000u;
+      v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    C::unpack2(v, x);
+  }
+  // at: 32 bytes of the warp's shared memory that nobody reads any more.
+  static __device__ __forceinline__ void write(uint32_t at, char* row, int begin, int dim, int ph, const uint4 (&v)[I * N]) {
+    const int lane = threadIdx.x & 31;
+    char* const p = row + (begin + lane * kLaneColumns) * ES;
+    if (whole(begin, dim, ph)) {
+#pragma unroll
+      for (int k = 0; k < I * N; ++k) st_global_v4(p + k / N * kWarpColumns * ES + k % N * 16, v[k]);
+      return;
+    }
+    // The 16 bytes in which the row begins, and those in which it ends, by elements, a thread each.
+    const int from = begin * ES, bytes = dim * ES, end = bytes & ~15;   // end: of the whole 16 bytes
+    const bool head = ph && begin == 0, tail = end != bytes && end >= from && end < from + kColumns * ES && !(head && end == 0);
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < I * N; ++k) {
+      const int b = from + ((k / N * 32 + lane) * N + k % N) * 16;
+      if (b + 16 <= bytes && b >= ph) st_global_v4(row + b, v[k]);
+      else if (b < ph) ptx::st_shared_v4(at, v[k]);
+      else if (b == end) ptx::st_shared_v4(at + 16, v[k]);
+    }
+    __syncwarp();
+    const int b = lane < 16 / ES ? lane * ES : end + (lane - 16) * ES;
+    if (lane < 16 / ES ? head && b >= ph && b < bytes : tail && lane >= 16 && b < bytes) {
+      const uint32_t one = at + (lane < 16 / ES ? 0 : 16) + b % 16;
+      if (ES == 4) {
+        uint32_t x;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(one) : "memory");
+        *reinterpret_cast<uint32_t*>(row + b) = x;
+      } else {
+        uint16_t x;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(one) : "memory");
+        *reinterpret_cast<uint16_t*>(row + b) = x;
+      }
+    }
+  }
+};
+
 // ---- host side -----------------------------------------------------------------------------------------------------
 // Lets a kernel have up to `bytes` of dynamic shared memory on the current device, and clusters of more than 8 blocks, once.
 template <auto KERNEL>

@@ -22,6 +22,9 @@ constexpr int norm_stages(int dtype) { return dtype == IRIS_F32 ? 2 : 3; }      
 constexpr int norm_grad_stages(int dtype) { return dtype == IRIS_F32 ? 2 : 3; }
 constexpr int kNormChain = 128;                 // rows that a thread adds up before the sum goes to the sum of such sums
 
+// How rows lie: all at 16 bytes, and their lengths multiples of that; those of all matrices alike, at any places of 16 bytes; anyhow.
+enum { kAny, kAligned, kSame };
+
 struct NormParams {
   const char* x;
   char* y;
@@ -30,6 +33,7 @@ struct NormParams {
   float* stats;
   int64_t rows;
   int dim, warps, split;        // warps: of a row in one block
+  int period;                   // kSame: rows that far apart begin at the same place of 16 bytes
   float eps;
 };
 
@@ -41,7 +45,7 @@ struct NormGradParams {
   const float* stats;
   float* parts;                 // [blocks / split (times groups if by_group), 2, dim]: sums of dy h and of dy; nullptr: not wanted
   int64_t rows;
-  int dim, warps, split, by_group;
+  int dim, warps, split, period, by_group;
 };
 
 // What a warp knows of a row, and the sum over the warps of a row, which all of its threads get.
@@ -74,17 +78,35 @@ struct Group {
   __device__ __forceinline__ const float2* of(const NormShared& s, int turn) const { return s.of[turn] + (split > 1 ? 0 : index * warps); }
 };
 
-// How the columns of a row are shared by its warps: `each` a warp, `rest` in the last one that has any.
+// How the columns of a row are shared by its warps: `each` a warp, `rest` in the last one that has any, of which the first has `none` that are not the row's.
 struct Shares {
   int last;
-  float each, rest, dim;
-  __device__ __forceinline__ Shares(int each_, int dim_) {
+  float each, rest, none, dim;
+  __device__ __forceinline__ Shares(int each_, int dim_, int none_) {
     last = (dim_ - 1) / each_;
     each = (float)each_;
     rest = (float)(dim_ - last * each_);
-    dim = (float)dim_;
+    none = (float)none_;
+    dim = (float)(dim_ - none_);
   }
-  __device__ __forceinline__ float of(int warp) const { return warp < last ? each : warp == last ? rest : 0.f; }
+  __device__ __forceinline__ float of(int warp) const { return (warp < last ? each : warp == last ? rest : 0.f) - (warp == 0 ? none : 0.f); }
+};
+// The rows of a group.  SAME (mode kSame): those of a block begin at the same place of 16 bytes (`ph`, in bytes): every `period`-th row, one set of them a block.
+// Columns are then counted from there, `none` are not the row's, and rows are addressed so.
+struct Rows {
+  int64_t first, each, step;   // the group's first row, between rows taken at once, between those and the next ones
+  int ph, none;
+  template <bool SAME, int R>
+  static __device__ __forceinline__ Rows of(const Group& group, int groups, int period_, const char* base, int64_t stride, int es) {
+    const int64_t block = blockIdx.x / group.split, blocks = gridDim.x / group.split, period = SAME ? period_ : 1, set = SAME ? block % period : 0;
+    Rows r;
+    r.first = set + period * ((SAME ? block / period : block) * groups + group.index) * R;
+    r.each = period;
+    r.step = period * (SAME ? (blocks - set + period - 1) / period : blocks) * groups * R;
+    r.ph = SAME ? (int)phase(base + set * stride) : 0;
+    r.none = r.ph / es;
+    return r;
+  }
 };
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
@@ -122,21 +144,24 @@ __device__ __forceinline__ float both(uint64_t x) {
 }
 
 // R rows at a time.
-template <int DT, int PT, int R, int I, bool ALIGNED>
+template <int DT, int PT, int R, int I, int MODE>
 __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormParams p) {
   using C = Columns<DT>;
-  using G = Segment<DT, I, ALIGNED>;
+  using G = Segment<DT, I, MODE == kAligned>;
+  using A = Aligned<DT, I>;
+  constexpr bool SAME = MODE == kSame;
   constexpr int kStages = norm_stages(DT), H = kLaneColumns / 2;
   __shared__ NormShared shared;
   extern __shared__ __align__(16) char ring[];   // [warps, stages, R] segments; weight, bias
   const Group group(p.warps, p.split);
   const int groups = blockDim.x / (p.warps * 32);
-  const int begin = group.warp * G::kColumns, first = begin + group.lane * kLaneColumns;
-  const int64_t step = (int64_t)(gridDim.x / p.split) * groups * R;
+  const int begin = group.warp * G::kColumns;
   const uint32_t own = ptx::smem_u32(ring) + (threadIdx.x >> 5) * (kStages * R * G::kBytes);
   float* const params = reinterpret_cast<float*>(ring + (blockDim.x >> 5) * (kStages * R * G::kBytes));
   const int columns = p.warps * G::kColumns;   // of the block
   const uint32_t weight = ptx::smem_u32(params) + ((group.warp - group.rank * group.warps) * I * 64 + group.lane) * 16, bias = weight + columns * 4;
+  const Rows rows = Rows::of<SAME, R>(group, groups, p.period, p.x, p.x_stride, C::ES);
+  const int dim = p.dim + rows.none, first = begin + group.lane * kLaneColumns;   // counted as rows are
   if (p.split > 1) ptx::cluster_sync();   // the others may write to this block's shared memory
   ptx::let_next_begin();
   ptx::begin_after_previous();
@@ -145,30 +170,34 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
 #pragma unroll
     for (int q = 0; q < R; ++q) {
       lone[q].settle();
-      if (r + q < p.rows) G::fetch(own + (stage * R + q) * G::kBytes, from + q * p.x_stride, begin, p.dim, lone[q]);
+      if (r + q * rows.each < p.rows) {
+        const uint32_t to = own + (stage * R + q) * G::kBytes;
+        if constexpr (SAME) A::fetch(to, from + q * rows.each * p.x_stride, begin, dim, rows.ph, lone[q]);
+        else G::fetch(to, from + q * rows.each * p.x_stride, begin, dim, lone[q]);
+      }
     }
     copy_async_commit();
   };
-  int64_t r = ((int64_t)(blockIdx.x / p.split) * groups + group.index) * R;
-  const char* x_row = p.x + r * p.x_stride;
-  char* y_row = p.y + r * p.y_stride;
-  const int64_t x_step = step * p.x_stride, y_step = step * p.y_stride;
+  int64_t r = rows.first;
+  const char* x_row = p.x + r * p.x_stride - rows.ph;
+  char* y_row = p.y + r * p.y_stride - rows.ph;
+  const int64_t x_step = rows.step * p.x_stride, y_step = rows.step * p.y_stride;
 #pragma unroll
-  for (int k = 0; k < kStages - 1; ++k) fetch(r + k * step, x_row + k * x_step, k);
-  put_params<PT, I>(params, p.weight, 1.f, group, begin, p.dim);
-  put_params<PT, I>(params + columns, p.bias, 0.f, group, begin, p.dim);
+  for (int k = 0; k < kStages - 1; ++k) fetch(r + k * rows.step, x_row + k * x_step, k);
+  put_params<PT, I>(params, p.weight, 1.f, group, begin - rows.none, p.dim);
+  put_params<PT, I>(params + columns, p.bias, 0.f, group, begin - rows.none, p.dim);
   __syncthreads();
-  const Shares shares(G::kColumns, p.dim);
+  const Shares shares(G::kColumns, dim, rows.none);
   const float mine = fmaxf(shares.of(group.warp), 1.f), whole = 1.f / shares.dim;
-  const bool full = begin + G::kColumns <= p.dim;
+  const bool full = begin >= rows.none && begin + G::kColumns <= dim;
   int stage = 0;
-  for (int turn = 0; r < p.rows; r += step, x_row += x_step, y_row += y_step, turn ^= 1) {
+  for (int turn = 0; r < p.rows; r += rows.step, x_row += x_step, y_row += y_step, turn ^= 1) {
 #pragma unroll
     for (int q = 0; q < R; ++q) lone[q].settle();
     copy_async_wait_but<kStages - 2>();
     __syncwarp();
     const uint32_t here = own + stage * (R * G::kBytes);
-    fetch(r + (kStages - 1) * step, x_row + (kStages - 1) * x_step, stage == 0 ? kStages - 1 : stage - 1);   // where the row before was
+    fetch(r + (kStages - 1) * rows.step, x_row + (kStages - 1) * x_step, stage == 0 ? kStages - 1 : stage - 1);   // where the row before was
     stage = stage + 1 == kStages ? 0 : stage + 1;
     uint64_t x[R][I][H];
     float mean[R], squares[R];
@@ -177,7 +206,8 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
       uint64_t s = 0;
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        G::read(here + q * G::kBytes, x_row + q * p.x_stride, begin, p.dim, i, x[q][i]);
+        if constexpr (SAME) A::read(here + q * G::kBytes, begin, dim, rows.ph, i, x[q][i]);
+        else G::read(here + q * G::kBytes, x_row + q * rows.each * p.x_stride, begin, dim, i, x[q][i]);
 #pragma unroll
         for (int e = 0; e < H; ++e) s = add2f(s, x[q][i][e]);
       }
@@ -206,7 +236,7 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
           for (int e = 0; e < H; ++e) {
             const float2 d = unpair(add2f(x[q][i][e], minus));
             const int c = first + i * kWarpColumns + 2 * e;
-            const uint64_t there = pair(c < p.dim ? d.x : 0.f, c + 1 < p.dim ? d.y : 0.f);
+            const uint64_t there = pair(c >= rows.none && c < dim ? d.x : 0.f, c + 1 >= rows.none && c + 1 < dim ? d.y : 0.f);
             s = fma2f(there, there, s);
           }
       }
@@ -232,8 +262,8 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
 #pragma unroll
     for (int q = 0; q < R; ++q) {
       squares[q] = rsqrtf(fmaf(squares[q], whole, p.eps));
-      if (p.stats && group.warp == 0 && group.lane == 0 && r + q < p.rows)
-        *reinterpret_cast<float2*>(p.stats + 2 * (r + q)) = make_float2(mean[q], squares[q]);
+      if (p.stats && group.warp == 0 && group.lane == 0 && r + q * rows.each < p.rows)
+        *reinterpret_cast<float2*>(p.stats + 2 * (r + q * rows.each)) = make_float2(mean[q], squares[q]);
     }
 #pragma unroll
     for (int i = 0; i < I; ++i) {
@@ -247,11 +277,12 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
     }
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      if (r + q >= p.rows) break;
+      if (r + q * rows.each >= p.rows) break;
       uint4 out[I * C::N];
 #pragma unroll
       for (int i = 0; i < I; ++i) C::pack2(x[q][i], out + i * C::N);
-      G::write(here + q * G::kBytes, y_row + q * p.y_stride, begin, p.dim, out);
+      if constexpr (SAME) A::write(here + q * G::kBytes, y_row + q * rows.each * p.y_stride, begin, dim, rows.ph, out);
+      else G::write(here + q * G::kBytes, y_row + q * rows.each * p.y_stride, begin, dim, out);
     }
   }
 }
@@ -260,18 +291,21 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
 template <int DT, int R, int I>
 constexpr int norm_grad_stage_bytes() { return R * (2 * Segment<DT, I>::kBytes + 16); }   // x, dy, statistics
 
-template <int DT, int PT, int R, int I, bool ALIGNED>
+template <int DT, int PT, int R, int I, int MODE>
 __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const NormGradParams p) {
   using C = Columns<DT>;
-  using G = Segment<DT, I, ALIGNED>;
+  using G = Segment<DT, I, MODE == kAligned>;
+  using A = Aligned<DT, I>;
+  constexpr bool SAME = MODE == kSame;
   constexpr int kStages = norm_grad_stages(DT), kRow = 2 * G::kBytes + 16, kStage = norm_grad_stage_bytes<DT, R, I>(), H = kLaneColumns / 2;
   __shared__ NormShared shared;
   extern __shared__ __align__(16) char ring[];   // [warps, stages, R] segments of x, of dy, statistics; weight
   const Group group(p.warps, p.split);
   const int groups = blockDim.x / (p.warps * 32);
   const int begin = group.warp * G::kColumns, first = begin + group.lane * kLaneColumns;
-  const int64_t step = (int64_t)(gridDim.x / p.split) * groups * R;
   const int columns = p.warps * G::kColumns;   // of the block
+  const Rows rows = Rows::of<SAME, R>(group, groups, p.period, p.x, p.x_stride, C::ES);
+  const int dim = p.dim + rows.none;   // counted as rows are, like `first`
   const uint32_t own = ptx::smem_u32(ring) + (threadIdx.x >> 5) * (kStages * kStage);
   float* const params = reinterpret_cast<float*>(ring + (blockDim.x >> 5) * (kStages * kStage));
   const uint32_t weight = ptx::smem_u32(params) + ((group.warp - group.rank * group.warps) * I * 64 + group.lane) * 16;
@@ -282,18 +316,18 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
   // The sums so far, to this group's part.
   const int64_t block = blockIdx.x / p.split;
   const auto put = [&](bool more) {
-    float* const to = p.parts + (p.by_group ? block * groups + group.index : block) * 2 * p.dim + first;
+    float* const to = p.parts + (p.by_group ? block * groups + group.index : block) * 2 * p.dim;
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
       for (int e = 0; e < H; ++e) {
-        const int c = i * kWarpColumns + 2 * e;
+        const int c = first - rows.none + i * kWarpColumns + 2 * e;
         const float2 w = unpair(dw[i][e]), b = unpair(db[i][e]);
-        if (first + c < p.dim) {
+        if (c >= 0 && c < p.dim) {
           to[c] = more ? to[c] + w.x : w.x;
           to[p.dim + c] = more ? to[p.dim + c] + b.x : b.x;
         }
-        if (first + c + 1 < p.dim) {
+        if (c + 1 >= 0 && c + 1 < p.dim) {
           to[c + 1] = more ? to[c + 1] + w.y : w.y;
           to[p.dim + c + 1] = more ? to[p.dim + c + 1] + b.y : b.y;
         }
@@ -306,26 +340,32 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
     for (int q = 0; q < R; ++q) {
       lone[q][0].settle();
       lone[q][1].settle();
-      if (r + q < p.rows) {
+      if (r + q * rows.each < p.rows) {
         const uint32_t to = own + stage * kStage + q * kRow;
-        G::fetch(to, x + q * p.x_stride, begin, p.dim, lone[q][0]);
-        G::fetch(to + G::kBytes, dy + q * p.dy_stride, begin, p.dim, lone[q][1]);
-        if (group.lane == 0) copy_async_pair(to + 2 * G::kBytes, p.stats + 2 * (r + q));
+        const int64_t at = q * rows.each;
+        if constexpr (SAME) {
+          A::fetch(to, x + at * p.x_stride, begin, dim, rows.ph, lone[q][0]);
+          A::fetch(to + G::kBytes, dy + at * p.dy_stride, begin, dim, rows.ph, lone[q][1]);
+        } else {
+          G::fetch(to, x + at * p.x_stride, begin, dim, lone[q][0]);
+          G::fetch(to + G::kBytes, dy + at * p.dy_stride, begin, dim, lone[q][1]);
+        }
+        if (group.lane == 0) copy_async_pair(to + 2 * G::kBytes, p.stats + 2 * (r + at));
       }
     }
     copy_async_commit();
   };
-  int64_t r = ((int64_t)(blockIdx.x / p.split) * groups + group.index) * R;
-  const char *x_row = p.x + r * p.x_stride, *dy_row = p.dy + r * p.dy_stride;
-  char* dx_row = p.dx + r * p.dx_stride;
-  const int64_t x_step = step * p.x_stride, dy_step = step * p.dy_stride, dx_step = step * p.dx_stride;
+  int64_t r = rows.first;
+  const char *x_row = p.x + r * p.x_stride - rows.ph, *dy_row = p.dy + r * p.dy_stride - rows.ph;
+  char* dx_row = p.dx + r * p.dx_stride - rows.ph;
+  const int64_t x_step = rows.step * p.x_stride, dy_step = rows.step * p.dy_stride, dx_step = rows.step * p.dx_stride;
 #pragma unroll
-  for (int k = 0; k < kStages - 1; ++k) fetch(r + k * step, x_row + k * x_step, dy_row + k * dy_step, k);
-  put_params<PT, I>(params, p.weight, 1.f, group, begin, p.dim);
+  for (int k = 0; k < kStages - 1; ++k) fetch(r + k * rows.step, x_row + k * x_step, dy_row + k * dy_step, k);
+  put_params<PT, I>(params, p.weight, 1.f, group, begin - rows.none, p.dim);
   __syncthreads();
   int chain = 0, stage = 0;
   bool more = false;
-  for (int turn = 0; r < p.rows; r += step, x_row += x_step, dy_row += dy_step, dx_row += dx_step, turn ^= 1) {
+  for (int turn = 0; r < p.rows; r += rows.step, x_row += x_step, dy_row += dy_step, dx_row += dx_step, turn ^= 1) {
     if (p.by_group && chain >= kNormChain) {
       put(more);
       more = true;
@@ -340,7 +380,7 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
     copy_async_wait_but<kStages - 2>();
     __syncwarp();
     const uint32_t here = own + stage * kStage;
-    fetch(r + (kStages - 1) * step, x_row + (kStages - 1) * x_step, dy_row + (kStages - 1) * dy_step,
+    fetch(r + (kStages - 1) * rows.step, x_row + (kStages - 1) * x_step, dy_row + (kStages - 1) * dy_step,
           stage == 0 ? kStages - 1 : stage - 1);   // where the row before was
     stage = stage + 1 == kStages ? 0 : stage + 1;
     uint64_t h[R][I][H], g[R][I][H];
@@ -351,11 +391,16 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
       rstd[q] = stats.y;
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        G::read(here + q * kRow, x_row + q * p.x_stride, begin, p.dim, i, h[q][i]);
-        G::read(here + q * kRow + G::kBytes, dy_row + q * p.dy_stride, begin, p.dim, i, g[q][i]);
+        if constexpr (SAME) {
+          A::read(here + q * kRow, begin, dim, rows.ph, i, h[q][i]);
+          A::read(here + q * kRow + G::kBytes, begin, dim, rows.ph, i, g[q][i]);
+        } else {
+          G::read(here + q * kRow, x_row + q * rows.each * p.x_stride, begin, dim, i, h[q][i]);
+          G::read(here + q * kRow + G::kBytes, dy_row + q * rows.each * p.dy_stride, begin, dim, i, g[q][i]);
+        }
 #pragma unroll
         for (int e = 0; e < H; ++e) h[q][i][e] = mul2f(add2f(h[q][i][e], pair(-stats.x, -stats.x)), pair(stats.y, stats.y));
-        if (q == 0 || r + q < p.rows) {
+        if (q == 0 || r + q * rows.each < p.rows) {
 #pragma unroll
           for (int e = 0; e < H; ++e) {
             dw[i][e] = fma2f(g[q][i][e], h[q][i][e], dw[i][e]);
@@ -397,7 +442,7 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
     }
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      if (r + q >= p.rows) break;
+      if (r + q * rows.each >= p.rows) break;
       uint4 out[I * C::N];
       const uint64_t minus_a = pair(-a[q] * whole, -a[q] * whole), minus_b = pair(-b[q] * whole, -b[q] * whole), by = pair(rstd[q], rstd[q]);
 #pragma unroll
@@ -406,7 +451,8 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
         for (int e = 0; e < H; ++e) g[q][i][e] = mul2f(fma2f(h[q][i][e], minus_b, add2f(g[q][i][e], minus_a)), by);
         C::pack2(g[q][i], out + i * C::N);
       }
-      G::write(here + q * kRow, dx_row + q * p.dx_stride, begin, p.dim, out);
+      if constexpr (SAME) A::write(here + q * kRow, dx_row + q * rows.each * p.dx_stride, begin, dim, rows.ph, out);
+      else G::write(here + q * kRow, dx_row + q * rows.each * p.dx_stride, begin, dim, out);
     }
   }
   ptx::let_next_begin();
@@ -429,10 +475,10 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
   __syncthreads();
   float* const part = p.parts + block * 2 * p.dim;
   for (int c = threadIdx.x; c < p.dim; c += blockDim.x) {
-    float w = sums[c], b = sums[columns + c];
-    for (int q = 1; q < groups; ++q) {
-      w += sums[q * 2 * columns + c];
-      b += sums[(q * 2 + 1) * columns + c];
+    float w = 0.f, b = 0.f;
+    for (int q = 0; q < groups; ++q) {
+      w += sums[q * 2 * columns + rows.none + c];
+      b += sums[(q * 2 + 1) * columns + rows.none + c];
     }
     part[c] = w;
     part[p.dim + c] = b;
@@ -491,53 +537,69 @@ static NormPlan norm_plan(int64_t rows, int64_t dim, int most, int row_warps, in
   if (n.groups > each) n.groups = each < 1 ? 1 : (int)each;
   return n;
 }
-static NormPlan norm_plan(int64_t rows, int64_t dim, int dtype) { return norm_plan(rows, dim, kNormRuns, kNormRowWarps, norm_warps(dtype)); }
-static NormPlan norm_grad_plan(int64_t rows, int64_t dim) { return norm_plan(rows, dim, kNormGradRuns, kNormGradRowWarps, kNormGradWarps); }
-static int64_t norm_grid(const NormPlan& n, int64_t rows) {   // times split
-  const int64_t each = (int64_t)n.groups * n.rows, full = (rows + each - 1) / each, room = kSms / n.split;
-  return full < room ? full : room;
+constexpr int kNormPeriod = 8;   // places of 16 bytes where a row may begin
+static int64_t norm_grid(const NormPlan& n, int64_t rows) {   // times split; at least a block for each place where a row begins
+  const int64_t each = (int64_t)n.groups * n.rows, full = (rows + each - 1) / each, room = kSms / n.split, most = rows < kNormPeriod ? rows : kNormPeriod;
+  return full < most ? most : full < room ? full : room;
 }
+// Whether the rows of two matrices lie alike in 16 bytes.
+static bool lie_alike(const void* a, int64_t a_stride, const void* b, int64_t b_stride) {
+  return (reinterpret_cast<uintptr_t>(a) - reinterpret_cast<uintptr_t>(b)) % 16 == 0 && (a_stride - b_stride) % 16 == 0;
+}
+static int period_of(int64_t stride) {   // bytes
+  int n = 1;
+  while (stride * n % 16) n *= 2;
+  return n;
+}
+// How the rows lie that a call reads and writes (`alike`: the others as x's).  Comes back with the columns counted as the kernel does.
+static int norm_mode(const void* x, int64_t stride, bool alike, int64_t row_bytes, int64_t* columns) {
+  if (!alike) return kAny;
+  if (reinterpret_cast<uintptr_t>(x) % 16 == 0 && stride % 16 == 0) return row_bytes % 16 == 0 ? kAligned : kSame;
+  if (*columns + kNormPeriod - 1 > kNormMaxDim) return kAny;
+  *columns += kNormPeriod - 1;
+  return kSame;
+}
+static NormPlan norm_plan(int64_t rows, int64_t columns, int dtype) { return norm_plan(rows, columns, kNormRuns, kNormRowWarps, norm_warps(dtype)); }
+static NormPlan norm_grad_plan(int64_t rows, int64_t columns) { return norm_plan(rows, columns, kNormGradRuns, kNormGradRowWarps, kNormGradWarps); }
 
 // Whether a group has more than kNormChain rows, and its sums their own part.
 static bool norm_by_group(const NormPlan& n, int64_t rows) { return rows > norm_grid(n, rows) * n.groups * kNormChain; }
 static int64_t norm_parts(const NormPlan& n, int64_t rows) { return norm_grid(n, rows) * (norm_by_group(n, rows) ? n.groups : 1); }
 
-template <int DT, int PT, int R, int I, bool ALIGNED>
+template <int DT, int PT, int R, int I, int MODE>
 static int launch_norm(const NormParams& p, const NormPlan& n, cudaStream_t st) {
-  constexpr auto kernel = norm_kernel<DT, PT, R, I, ALIGNED>;
+  constexpr auto kernel = norm_kernel<DT, PT, R, I, MODE>;
   constexpr int stages = norm_stages(DT) * R * Segment<DT, I>::kBytes, params = 2 * I * kWarpColumns * (int)sizeof(float);   // of a warp, of a warp of a row
   IRIS_CHECK(allow_shared<kernel>(norm_warps(DT) * stages + kNormRowWarps * params));
   return launch_rows(kernel, p, (unsigned)(norm_grid(n, p.rows) * n.split), n.split, n.warps * n.groups * 32,
                      (size_t)n.warps * (n.groups * stages + params), st);
 }
-template <int DT, int PT, bool ALIGNED>
+template <int DT, int PT, int MODE>
 static int launch_norm(const NormParams& p, const NormPlan& n, cudaStream_t st) {
-  return n.runs == 1   ? launch_norm<DT, PT, 4, 1, ALIGNED>(p, n, st)
-         : n.runs == 2 ? launch_norm<DT, PT, 2, 2, ALIGNED>(p, n, st)
-         : n.runs == 3 ? launch_norm<DT, PT, 1, 3, ALIGNED>(p, n, st)
-                       : launch_norm<DT, PT, 1, 4, ALIGNED>(p, n, st);
+  return n.runs == 1   ? launch_norm<DT, PT, 4, 1, MODE>(p, n, st)
+         : n.runs == 2 ? launch_norm<DT, PT, 2, 2, MODE>(p, n, st)
+         : n.runs == 3 ? launch_norm<DT, PT, 1, 3, MODE>(p, n, st)
+                       : launch_norm<DT, PT, 1, 4, MODE>(p, n, st);
 }
 template <int DT, int PT>
-static int launch_norm(const NormParams& p, const NormPlan& n, cudaStream_t st) {
-  const bool aligned = p.dim * Columns<DT>::ES % 16 == 0 && aligned_rows(p.x, p.x_stride) && aligned_rows(p.y, p.y_stride);
-  return aligned ? launch_norm<DT, PT, true>(p, n, st) : launch_norm<DT, PT, false>(p, n, st);
+static int launch_norm(const NormParams& p, const NormPlan& n, int mode, cudaStream_t st) {
+  return mode == kAligned ? launch_norm<DT, PT, kAligned>(p, n, st) : mode == kSame ? launch_norm<DT, PT, kSame>(p, n, st) : launch_norm<DT, PT, kAny>(p, n, st);
 }
-template <int DT, int PT, int R, int I, bool ALIGNED>
+template <int DT, int PT, int R, int I, int MODE>
 static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, cudaStream_t st) {
-  constexpr auto kernel = norm_grad_kernel<DT, PT, R, I, ALIGNED>;
+  constexpr auto kernel = norm_grad_kernel<DT, PT, R, I, MODE>;
   constexpr int stages = norm_grad_stages(DT) * norm_grad_stage_bytes<DT, R, I>(), params = I * kWarpColumns * (int)sizeof(float);   // of a warp, of a warp of a row
   static_assert(stages >= 2 * params, "the groups' sums take the place of the rows");
   IRIS_CHECK(allow_shared<kernel>(kNormGradWarps * stages + kNormGradRowWarps * params));
   return launch_rows(kernel, p, (unsigned)(norm_grid(n, p.rows) * n.split), n.split, n.warps * n.groups * 32, (size_t)n.warps * (n.groups * stages + params), st);
 }
-template <int DT, int PT, bool ALIGNED>
+template <int DT, int PT, int MODE>
 static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, cudaStream_t st) {
-  return n.runs == 1 ? launch_norm_grad<DT, PT, 2, 1, ALIGNED>(p, n, st) : launch_norm_grad<DT, PT, 1, 2, ALIGNED>(p, n, st);
+  return n.runs == 1 ? launch_norm_grad<DT, PT, 2, 1, MODE>(p, n, st) : launch_norm_grad<DT, PT, 1, 2, MODE>(p, n, st);
 }
 template <int DT, int PT>
-static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, void* dweight, void* dbias, cudaStream_t st) {
-  const bool aligned = p.dim * Columns<DT>::ES % 16 == 0 && aligned_rows(p.x, p.x_stride) && aligned_rows(p.dy, p.dy_stride) && aligned_rows(p.dx, p.dx_stride);
-  IRIS_CHECK(aligned ? launch_norm_grad<DT, PT, true>(p, n, st) : launch_norm_grad<DT, PT, false>(p, n, st));
+static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, int mode, void* dweight, void* dbias, cudaStream_t st) {
+  IRIS_CHECK(mode == kAligned ? launch_norm_grad<DT, PT, kAligned>(p, n, st) : mode == kSame ? launch_norm_grad<DT, PT, kSame>(p, n, st) : launch_norm_grad<DT, PT, kAny>(p, n, st));
   if (!p.parts) return IRIS_OK;
   return launch_rows(norm_join_kernel<PT>, NormJoinParams{p.parts, (int)norm_parts(n, p.rows), p.dim, {dweight, dbias}}, (unsigned)((p.dim + 31) / 32 * 2), 1,
                      kJoinWarps * 32, 0, st);
@@ -575,19 +637,23 @@ extern "C" int iris_layer_norm(const iris_layer_norm_args* a, void* stream) {
   IRIS_CHECK(check_overlap(fn, "y", "x", a->x, xs, a->y, ys, a->rows, a->dim, a->dtype));
   if (a->rows == 0) return IRIS_OK;
   const int64_t es = (int64_t)elem_size(a->dtype);
-  const NormPlan n = norm_plan(a->rows, a->dim, a->dtype);
+  int64_t columns = a->dim;
+  const int mode = norm_mode(a->x, xs * es, lie_alike(a->x, xs * es, a->y, ys * es), a->dim * es, &columns);
+  const NormPlan n = norm_plan(a->rows, columns, a->dtype);
   NormParams p{static_cast<const char*>(a->x), static_cast<char*>(a->y), xs * es, ys * es, static_cast<const char*>(a->weight),
-               static_cast<const char*>(a->bias), a->stats, a->rows, (int)a->dim, n.warps, n.split, a->eps};
+               static_cast<const char*>(a->bias), a->stats, a->rows, (int)a->dim, n.warps, n.split, period_of(xs * es), a->eps};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool wide = a->param_dtype == IRIS_F32;
-  if (a->dtype == IRIS_BF16) return wide ? launch_norm<IRIS_BF16, IRIS_F32>(p, n, st) : launch_norm<IRIS_BF16, IRIS_BF16>(p, n, st);
-  if (a->dtype == IRIS_F16) return wide ? launch_norm<IRIS_F16, IRIS_F32>(p, n, st) : launch_norm<IRIS_F16, IRIS_F16>(p, n, st);
-  return launch_norm<IRIS_F32, IRIS_F32>(p, n, st);
+  if (a->dtype == IRIS_BF16) return wide ? launch_norm<IRIS_BF16, IRIS_F32>(p, n, mode, st) : launch_norm<IRIS_BF16, IRIS_BF16>(p, n, mode, st);
+  if (a->dtype == IRIS_F16) return wide ? launch_norm<IRIS_F16, IRIS_F32>(p, n, mode, st) : launch_norm<IRIS_F16, IRIS_F16>(p, n, mode, st);
+  return launch_norm<IRIS_F32, IRIS_F32>(p, n, mode, st);
 }
 
 extern "C" size_t iris_layer_norm_workspace_bytes(int64_t rows, int64_t dim) {
   if (rows <= 0 || rows > INT32_MAX || dim <= 0 || dim > kNormMaxDim) return 0;
-  return (size_t)norm_parts(norm_grad_plan(rows, dim), rows) * 2 * dim * sizeof(float);
+  const int64_t more = dim + kNormPeriod - 1 < kNormMaxDim ? dim + kNormPeriod - 1 : kNormMaxDim;   // rows may begin anywhere
+  const int64_t a = norm_parts(norm_grad_plan(rows, dim), rows), b = norm_parts(norm_grad_plan(rows, more), rows);
+  return (size_t)(a > b ? a : b) * 2 * dim * sizeof(float);
 }
 
 extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void* stream) {
@@ -620,14 +686,17 @@ extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void
     return IRIS_OK;
   }
   const int64_t es = (int64_t)elem_size(a->dtype);
-  const NormPlan n = norm_grad_plan(a->rows, a->dim);
+  int64_t columns = a->dim;
+  const bool alike = lie_alike(a->x, xs * es, a->dy, gs * es) && (!a->dx || lie_alike(a->x, xs * es, a->dx, ds * es));
+  const int mode = norm_mode(a->x, xs * es, alike, a->dim * es, &columns);
+  const NormPlan n = norm_grad_plan(a->rows, columns);
   NormGradParams p{static_cast<const char*>(a->x), static_cast<const char*>(a->dy), static_cast<char*>(a->dx), xs * es, gs * es, ds * es,
                    static_cast<const char*>(a->weight), a->stats, sums ? static_cast<float*>(a->workspace) : nullptr, a->rows, (int)a->dim, n.warps,
-                   n.split, sums && norm_by_group(n, a->rows)};
+                   n.split, period_of(xs * es), sums && norm_by_group(n, a->rows)};
   const bool wide = a->param_dtype == IRIS_F32;
   if (a->dtype == IRIS_BF16)
-    return wide ? launch_norm_grad<IRIS_BF16, IRIS_F32>(p, n, a->dweight, a->dbias, st) : launch_norm_grad<IRIS_BF16, IRIS_BF16>(p, n, a->dweight, a->dbias, st);
+    return wide ? launch_norm_grad<IRIS_BF16, IRIS_F32>(p, n, mode, a->dweight, a->dbias, st) : launch_norm_grad<IRIS_BF16, IRIS_BF16>(p, n, mode, a->dweight, a->dbias, st);
   if (a->dtype == IRIS_F16)
-    return wide ? launch_norm_grad<IRIS_F16, IRIS_F32>(p, n, a->dweight, a->dbias, st) : launch_norm_grad<IRIS_F16, IRIS_F16>(p, n, a->dweight, a->dbias, st);
-  return launch_norm_grad<IRIS_F32, IRIS_F32>(p, n, a->dweight, a->dbias, st);
+    return wide ? launch_norm_grad<IRIS_F16, IRIS_F32>(p, n, mode, a->dweight, a->dbias, st) : launch_norm_grad<IRIS_F16, IRIS_F16>(p, n, mode, a->dweight, a->dbias, st);
+  return launch_norm_grad<IRIS_F32, IRIS_F32>(p, n, mode, a->dweight, a->dbias, st);
 }
