@@ -608,7 +608,8 @@ size_t iris_verify_workspace_bytes(int64_t sequences, int drafts);
  * Workspaces: device memory of the caller's whose contents neither have to be prepared nor are of use afterwards.  Calls that may
  * run at the same time (on different streams, in graphs that are replayed at the same time) need one each.
  * Rows: row r starts at its matrix + r * stride elements of type `dtype` (IRIS_F16, IRIS_BF16, IRIS_F32); strides are in elements, 0 = rows one after the
- * other.  Rows may start at any element; nothing outside a row is read or written. */
+ * other.  Rows may start at any element.  Nothing outside a row is written; what lies between two rows of a matrix may be read (no use is made of it), nothing
+ * in front of its first row or behind its last one. */
 
 /* Embedding lookup: out row i = scale * table row tokens[i], rounded once.  The table is cut by rows into `world` shards of vocab / world rows: the
  * B shards of gemm_all_scatter are such a table (tied embeddings), in this process's memory or mapped from another's.

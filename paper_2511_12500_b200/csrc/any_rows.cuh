@@ -327,30 +327,45 @@ struct Segment {
   }
 };
 
+// Bytes lo .. hi - 1 of 16, zeros elsewhere (both multiples of 2).
+__device__ __forceinline__ uint4 between(const uint4& v, int lo, int hi) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int a = min(32, max(0, lo * 8 - i * 32)), b = min(32, max(0, hi * 8 - i * 32));   // bits
+    w[i] &= (uint32_t)((1ull << b) - 1) & ~(uint32_t)((1ull << a) - 1);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
 // The same for rows that all begin at the same place of 16 bytes (`ph`, in bytes): columns are counted from the aligned 16 bytes in which a row begins, so
 // that no piece has to be cut.  row: that place; dim: columns counted so, up to the row's end; the first ph / ES of them are not the row's.
+// Of the aligned 16 bytes in which a row begins or ends, all are read, as they lie between the matrix's rows; but not in front of the first row and behind
+// the last one (`first`, `last`).
 template <int DT, int I>
 struct Aligned {
   using C = Columns<DT>;
   using Lone = typename Segment<DT, I>::Lone;
   static constexpr int ES = C::ES, N = C::N, VE = C::E::VE, kColumns = I * kWarpColumns, kBytes = kColumns * ES;
   static __device__ __forceinline__ bool whole(int begin, int dim, int ph) { return (begin > 0 || ph == 0) && begin + kColumns <= dim; }   // all are the row's
-  static __device__ __forceinline__ void fetch(uint32_t at, const char* row, int begin, int dim, int ph, Lone& lone) {
+  static __device__ __forceinline__ void fetch(uint32_t at, const char* row, int begin, int dim, int ph, bool first, bool last, Lone& lone) {
     const int lane = threadIdx.x & 31;
     const char* const p = row + begin * ES + lane * 16;
-    if (whole(begin, dim, ph)) {
+    const int left = dim * ES - begin * ES - lane * 16;
+    const bool careful = (first && ph) || (last && dim * ES % 16);
+    if (!careful) {
 #pragma unroll
-      for (int k = 0; k < I * N; ++k) copy_async(at + (k * 32 + lane) * 16, p + k * 512);
+      for (int k = 0; k < I * N; ++k)
+        if (k * 512 < left) copy_async(at + (k * 32 + lane) * 16, p + k * 512);
+        else ptx::st_shared_v4(at + (k * 32 + lane) * 16, make_uint4(0, 0, 0, 0));
       return;
     }
-    const int left = dim * ES - begin * ES - lane * 16;
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < I * N; ++k) {
-      if (k == 0 && ph && begin + lane == 0) continue;
-      if (k * 512 < left) copy_async_part(at + (k * 32 + lane) * 16, p + k * 512, min(16, left - k * 512));
+      if (k == 0 && first && ph && begin + lane == 0) continue;
+      if (k * 512 < left) copy_async_part(at + (k * 32 + lane) * 16, p + k * 512, last ? min(16, left - k * 512) : 16);
       else ptx::st_shared_v4(at + (k * 32 + lane) * 16, make_uint4(0, 0, 0, 0));
     }
-    if (ph && begin == 0) {   // the row's first elements
+    if (first && ph && begin == 0) {   // the row's first elements
       const int from = lane * 4, bytes = dim * ES;
       if (lane < 4 && from + 4 > ph && from < bytes) {
         if (from >= ph && from + 4 <= bytes) {
@@ -370,12 +385,14 @@ struct Aligned {
     uint4 v[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) v[n] = ld_shared_v4(at + ((i * 32 + lane) * N + n) * 16);
-    if (i == 0 && ph && begin + lane == 0) {   // the aligned 16 bytes in which the row begins (and may end)
-      uint32_t w[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+    // Zeros where a column is not the row's; 16 bytes that lie behind it altogether are 0 already.
+    const int from = (begin + i * kWarpColumns) * ES, bytes = dim * ES;
+    if ((i == 0 && begin == 0 && ph) || (from < bytes && bytes < from + kWarpColumns * ES && bytes % 16)) {
 #pragma unroll
-      for (int e = 0; e < VE; ++e)
-        if (e < ph / ES || e >= dim) w[e * ES / 4] &= ES == 4 ? 0u : e % 2 ? 0xffffu : 0xffff0000u;
-      v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int n = 0; n < N; ++n) {
+        const int b = from + (lane * N + n) * 16;
+        if (b < ph || (b < bytes && bytes < b + 16)) v[n] = between(v[n], max(0, ph - b), min(16, bytes - b));
+      }
     }
     C::unpack2(v, x);
   }

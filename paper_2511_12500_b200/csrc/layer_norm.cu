@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
       lone[q].settle();
       if (r + q * rows.each < p.rows) {
         const uint32_t to = own + (stage * R + q) * G::kBytes;
-        if constexpr (SAME) A::fetch(to, from + q * rows.each * p.x_stride, begin, dim, rows.ph, lone[q]);
+        if constexpr (SAME) A::fetch(to, from + q * rows.each * p.x_stride, begin, dim, rows.ph, r + q * rows.each == 0, r + q * rows.each == p.rows - 1, lone[q]);
         else G::fetch(to, from + q * rows.each * p.x_stride, begin, dim, lone[q]);
       }
     }
@@ -344,8 +344,8 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
         const uint32_t to = own + stage * kStage + q * kRow;
         const int64_t at = q * rows.each;
         if constexpr (SAME) {
-          A::fetch(to, x + at * p.x_stride, begin, dim, rows.ph, lone[q][0]);
-          A::fetch(to + G::kBytes, dy + at * p.dy_stride, begin, dim, rows.ph, lone[q][1]);
+          A::fetch(to, x + at * p.x_stride, begin, dim, rows.ph, r + at == 0, r + at == p.rows - 1, lone[q][0]);
+          A::fetch(to + G::kBytes, dy + at * p.dy_stride, begin, dim, rows.ph, r + at == 0, r + at == p.rows - 1, lone[q][1]);
         } else {
           G::fetch(to, x + at * p.x_stride, begin, dim, lone[q][0]);
           G::fetch(to + G::kBytes, dy + at * p.dy_stride, begin, dim, lone[q][1]);
