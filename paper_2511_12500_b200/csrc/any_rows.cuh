@@ -327,15 +327,28 @@ struct Segment {
   }
 };
 
-// Bytes lo .. hi - 1 of 16, zeros elsewhere (both multiples of 2).
+__device__ __forceinline__ uint32_t ones_below(int bit) {   // of a word; none below 0, all from 32 on
+  uint32_t m;
+  asm("bmsk.clamp.b32 %0, 0, %1;" : "=r"(m) : "r"(max(0, bit)));
+  return m;
+}
+// Bytes lo .. hi - 1 of 16, zeros elsewhere.
 __device__ __forceinline__ uint4 between(const uint4& v, int lo, int hi) {
-  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  lo *= 8;
+  hi *= 8;
+  return make_uint4(v.x & ones_below(hi) & ~ones_below(lo), v.y & ones_below(hi - 32) & ~ones_below(lo - 32),
+                    v.z & ones_below(hi - 64) & ~ones_below(lo - 64), v.w & ones_below(hi - 96) & ~ones_below(lo - 96));
+}
+// Elements of v from byte lo on and before byte hi, to `at` + their place.
+template <int ES>
+__device__ __forceinline__ void store_between(char* at, const uint4& v, int lo, int hi) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int a = min(32, max(0, lo * 8 - i * 32)), b = min(32, max(0, hi * 8 - i * 32));   // bits
-    w[i] &= (uint32_t)((1ull << b) - 1) & ~(uint32_t)((1ull << a) - 1);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  for (int e = 0; e < 16 / ES; ++e)
+    if (e * ES >= lo && e * ES < hi) {
+      if (ES == 4) *reinterpret_cast<uint32_t*>(at + e * ES) = w[e * ES / 4];
+      else *reinterpret_cast<uint16_t*>(at + e * ES) = (uint16_t)(w[e * ES / 4] >> (e % 2 * 16));
+    }
 }
 // The same for rows that all begin at the same place of 16 bytes (`ph`, in bytes): columns are counted from the aligned 16 bytes in which a row begins, so
 // that no piece has to be cut.  row: that place; dim: columns counted so, up to the row's end; the first ph / ES of them are not the row's.
@@ -391,13 +404,12 @@ struct Aligned {
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         const int b = from + (lane * N + n) * 16;
-        if (b < ph || (b < bytes && bytes < b + 16)) v[n] = between(v[n], max(0, ph - b), min(16, bytes - b));
+        if (b < ph || (b < bytes && bytes < b + 16)) v[n] = between(v[n], ph - b, bytes - b);
       }
     }
     C::unpack2(v, x);
   }
-  // at: 32 bytes of the warp's shared memory that nobody reads any more.
-  static __device__ __forceinline__ void write(uint32_t at, char* row, int begin, int dim, int ph, const uint4 (&v)[I * N]) {
+  static __device__ __forceinline__ void write(char* row, int begin, int dim, int ph, const uint4 (&v)[I * N]) {
     const int lane = threadIdx.x & 31;
     char* const p = row + (begin + lane * kLaneColumns) * ES;
     if (whole(begin, dim, ph)) {
@@ -405,31 +417,23 @@ struct Aligned {
       for (int k = 0; k < I * N; ++k) st_global_v4(p + k / N * kWarpColumns * ES + k % N * 16, v[k]);
       return;
     }
-    // The 16 bytes in which the row begins, and those in which it ends, by elements, a thread each.
-    const int from = begin * ES, bytes = dim * ES, end = bytes & ~15;   // end: of the whole 16 bytes
-    const bool head = ph && begin == 0, tail = end != bytes && end >= from && end < from + kColumns * ES && !(head && end == 0);
-    __syncwarp();
+    // The 16 bytes in which the row begins, and those in which it ends, by elements.
+    const int from = begin * ES + lane * (N * 16), bytes = dim * ES;
+    uint4 end = v[0];
+    int end_at = -1;
 #pragma unroll
     for (int k = 0; k < I * N; ++k) {
-      const int b = from + ((k / N * 32 + lane) * N + k % N) * 16;
-      if (b + 16 <= bytes && b >= ph) st_global_v4(row + b, v[k]);
-      else if (b < ph) ptx::st_shared_v4(at, v[k]);
-      else if (b == end) ptx::st_shared_v4(at + 16, v[k]);
-    }
-    __syncwarp();
-    const int b = lane < 16 / ES ? lane * ES : end + (lane - 16) * ES;
-    if (lane < 16 / ES ? head && b >= ph && b < bytes : tail && lane >= 16 && b < bytes) {
-      const uint32_t one = at + (lane < 16 / ES ? 0 : 16) + b % 16;
-      if (ES == 4) {
-        uint32_t x;
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(one) : "memory");
-        *reinterpret_cast<uint32_t*>(row + b) = x;
-      } else {
-        uint16_t x;
-        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(one) : "memory");
-        *reinterpret_cast<uint16_t*>(row + b) = x;
+      const int b = from + k / N * (kWarpColumns * ES) + k % N * 16;
+      if (k == 0 && b < ph) continue;
+      if (b + 16 <= bytes) {
+        st_global_v4(row + b, v[k]);
+      } else if (b < bytes) {
+        end = v[k];
+        end_at = b;
       }
     }
+    if (end_at >= 0) store_between<ES>(row + end_at, end, 0, bytes - end_at);
+    if (from < ph) store_between<ES>(row, v[0], ph, bytes);
   }
 };
 

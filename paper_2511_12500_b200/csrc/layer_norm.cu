@@ -15,10 +15,11 @@ constexpr int kNormRowWarps = 8, kNormGradRowWarps = 16;   // of a row in a bloc
 constexpr int kNormSplit = 8;                   // blocks (one cluster) that share a row
 constexpr int64_t kNormMaxDim = (int64_t)kNormRuns * kWarpColumns * kNormRowWarps * kNormSplit;
 static_assert(kNormRuns * kNormRowWarps == kNormGradRuns * kNormGradRowWarps, "the same limit for both directions");
-// Of a block, which has an SM to itself: what registers and shared memory allow.
-constexpr int norm_warps(int dtype) { return dtype == IRIS_F32 ? 16 : 24; }
-constexpr int kNormGradWarps = 16;
-constexpr int norm_stages(int dtype) { return dtype == IRIS_F32 ? 2 : 3; }        // rows (or R of them) in shared memory
+constexpr int kNormRows = 2;                    // that several warps have at a time, at most
+// Warps of a block, which has an SM to itself, and rows (or R of them) in shared memory: what registers and shared memory allow.
+constexpr int norm_warps(int dtype, int rows_runs) { return dtype == IRIS_F32 || rows_runs > 4 ? 16 : 24; }
+constexpr int norm_stages(int dtype, int rows_runs) { return dtype == IRIS_F32 || rows_runs > 4 ? 2 : 3; }
+constexpr int norm_grad_warps(int rows_runs) { return rows_runs > 2 ? 12 : 16; }
 constexpr int norm_grad_stages(int dtype) { return dtype == IRIS_F32 ? 2 : 3; }
 constexpr int kNormChain = 128;                 // rows that a thread adds up before the sum goes to the sum of such sums
 
@@ -50,7 +51,7 @@ struct NormGradParams {
 
 // What a warp knows of a row, and the sum over the warps of a row, which all of its threads get.
 struct NormShared {
-  float2 of[2][kNormGradRowWarps * kNormSplit];   // twice: one is read while the next row's is written
+  float2 of[2][kNormRows][kNormGradRowWarps * kNormSplit];   // twice: one is read while the next rows' is written
 };
 struct Group {
   int warps, split, rank, index, warp, lane, id;   // index: of the group in its block; warp: in its row, over all blocks; id: of its barrier
@@ -61,21 +62,26 @@ struct Group {
     warp = (int)(threadIdx.x >> 5) % warps + rank * warps;
     id = 1 + index;
   }
-  // Every warp of the row puts its value into `turn`'s half and waits for the others'.
-  __device__ __forceinline__ void exchange(NormShared& s, int turn, float2 v) const {
+  // Every warp of the rows puts its values into `turn`'s half and waits for the others'.
+  template <int R>
+  __device__ __forceinline__ void exchange(NormShared& s, int turn, const float (&a)[R], const float (&b)[R]) const {
+    static_assert(R <= kNormRows, "room for them");
     if (split > 1) {
       if (lane < split) {
-        const uint32_t to = ptx::mapa(ptx::smem_u32(&s.of[turn][warp]), lane);
-        ptx::st_shared_cluster_u64(to, pair(v.x, v.y));
+#pragma unroll
+        for (int q = 0; q < R; ++q) ptx::st_shared_cluster_u64(ptx::mapa(ptx::smem_u32(&s.of[turn][q][warp]), lane), pair(a[q], b[q]));
       }
       ptx::cluster_sync();
     } else {
-      if (lane == 0) s.of[turn][index * warps + warp] = v;
+      if (lane == 0) {
+#pragma unroll
+        for (int q = 0; q < R; ++q) s.of[turn][q][index * warps + warp] = make_float2(a[q], b[q]);
+      }
       asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(warps * 32) : "memory");
     }
   }
   __device__ __forceinline__ int all() const { return warps * split; }
-  __device__ __forceinline__ const float2* of(const NormShared& s, int turn) const { return s.of[turn] + (split > 1 ? 0 : index * warps); }
+  __device__ __forceinline__ const float2* of(const NormShared& s, int turn, int q) const { return s.of[turn][q] + (split > 1 ? 0 : index * warps); }
 };
 
 // How the columns of a row are shared by its warps: `each` a warp, `rest` in the last one that has any, of which the first has `none` that are not the row's.
@@ -145,12 +151,12 @@ __device__ __forceinline__ float both(uint64_t x) {
 
 // R rows at a time.
 template <int DT, int PT, int R, int I, int MODE>
-__global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormParams p) {
+__global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const NormParams p) {
   using C = Columns<DT>;
   using G = Segment<DT, I, MODE == kAligned>;
   using A = Aligned<DT, I>;
   constexpr bool SAME = MODE == kSame;
-  constexpr int kStages = norm_stages(DT), H = kLaneColumns / 2;
+  constexpr int kStages = norm_stages(DT, R * I), H = kLaneColumns / 2;
   __shared__ NormShared shared;
   extern __shared__ __align__(16) char ring[];   // [warps, stages, R] segments; weight, bias
   const Group group(p.warps, p.split);
@@ -244,21 +250,25 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
     }
 #pragma unroll
     for (int q = 0; q < R; ++q) squares[q] = warp_sum(squares[q]);
-    if (R == 1 && group.all() > 1) {
-      group.exchange(shared, turn, make_float2(mean[0], squares[0]));
-      const float2* const of = group.of(shared, turn);
-      float m = 0.f, s = 0.f;
+    if constexpr (R <= kNormRows)
+      if (group.all() > 1) {
+        group.exchange(shared, turn, mean, squares);
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+          const float2* const of = group.of(shared, turn, q);
+          float m = 0.f, s = 0.f;
 #pragma unroll 4
-      for (int w = 0; w < group.all(); ++w) m = fmaf(of[w].x, shares.of(w), m);
-      mean[0] = m / shares.dim;
+          for (int w = 0; w < group.all(); ++w) m = fmaf(of[w].x, shares.of(w), m);
+          mean[q] = m / shares.dim;
 #pragma unroll 4
-      for (int w = 0; w < group.all(); ++w) {   // from the warp's mean to the row's
-        const float2 v = of[w];
-        const float d = v.x - mean[0];
-        s += fmaf(d * d, shares.of(w), v.y);
+          for (int w = 0; w < group.all(); ++w) {   // from the warp's mean to the row's
+            const float2 v = of[w];
+            const float d = v.x - mean[q];
+            s += fmaf(d * d, shares.of(w), v.y);
+          }
+          squares[q] = s;
+        }
       }
-      squares[0] = s;
-    }
 #pragma unroll
     for (int q = 0; q < R; ++q) {
       squares[q] = rsqrtf(fmaf(squares[q], whole, p.eps));
@@ -281,7 +291,7 @@ __global__ void __launch_bounds__(norm_warps(DT) * 32) norm_kernel(const NormPar
       uint4 out[I * C::N];
 #pragma unroll
       for (int i = 0; i < I; ++i) C::pack2(x[q][i], out + i * C::N);
-      if constexpr (SAME) A::write(here + q * G::kBytes, y_row + q * rows.each * p.y_stride, begin, dim, rows.ph, out);
+      if constexpr (SAME) A::write(y_row + q * rows.each * p.y_stride, begin, dim, rows.ph, out);
       else G::write(here + q * G::kBytes, y_row + q * rows.each * p.y_stride, begin, dim, out);
     }
   }
@@ -292,7 +302,7 @@ template <int DT, int R, int I>
 constexpr int norm_grad_stage_bytes() { return R * (2 * Segment<DT, I>::kBytes + 16); }   // x, dy, statistics
 
 template <int DT, int PT, int R, int I, int MODE>
-__global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const NormGradParams p) {
+__global__ void __launch_bounds__(norm_grad_warps(R * I) * 32) norm_grad_kernel(const NormGradParams p) {
   using C = Columns<DT>;
   using G = Segment<DT, I, MODE == kAligned>;
   using A = Aligned<DT, I>;
@@ -429,15 +439,18 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
       a[q] = warp_sum(both(a2[q]));
       b[q] = warp_sum(both(b2[q]));
     }
-    if (R == 1 && group.all() > 1) {
-      group.exchange(shared, turn, make_float2(a[0], b[0]));
-      const float2* const of = group.of(shared, turn);
-      a[0] = b[0] = 0.f;
+    if (group.all() > 1) {
+      group.exchange(shared, turn, a, b);
+#pragma unroll
+      for (int q = 0; q < R; ++q) {
+        const float2* const of = group.of(shared, turn, q);
+        a[q] = b[q] = 0.f;
 #pragma unroll 4
-      for (int w = 0; w < group.all(); ++w) {
-        const float2 v = of[w];
-        a[0] += v.x;
-        b[0] += v.y;
+        for (int w = 0; w < group.all(); ++w) {
+          const float2 v = of[w];
+          a[q] += v.x;
+          b[q] += v.y;
+        }
       }
     }
 #pragma unroll
@@ -451,7 +464,7 @@ __global__ void __launch_bounds__(kNormGradWarps * 32) norm_grad_kernel(const No
         for (int e = 0; e < H; ++e) g[q][i][e] = mul2f(fma2f(h[q][i][e], minus_b, add2f(g[q][i][e], minus_a)), by);
         C::pack2(g[q][i], out + i * C::N);
       }
-      if constexpr (SAME) A::write(here + q * kRow, dx_row + q * rows.each * p.dx_stride, begin, dim, rows.ph, out);
+      if constexpr (SAME) A::write(dx_row + q * rows.each * p.dx_stride, begin, dim, rows.ph, out);
       else G::write(here + q * kRow, dx_row + q * rows.each * p.dx_stride, begin, dim, out);
     }
   }
@@ -523,19 +536,17 @@ __global__ void __launch_bounds__(kJoinWarps * 32) norm_join_kernel(const NormJo
 struct NormPlan {
   int split, warps, runs, rows, groups;   // rows: at a time (several only of one run, or of two); groups: of a block
 };
-// most: runs that a thread holds; row_warps: of a row in a block, at most; warps: of a block.
-static NormPlan norm_plan(int64_t rows, int64_t dim, int most, int row_warps, int warps) {
-  NormPlan n;
+static void plan_runs(NormPlan& n, int64_t columns, int most, int row_warps) {   // most: runs that a thread holds of a row
   n.split = 1;
-  while ((int64_t)n.split * most * kWarpColumns * row_warps < dim) n.split *= 2;
-  const int runs = (int)((dim + (int64_t)n.split * kWarpColumns - 1) / ((int64_t)n.split * kWarpColumns));   // of 256 columns in a block
+  while ((int64_t)n.split * most * kWarpColumns * row_warps < columns) n.split *= 2;
+  const int runs = (int)((columns + (int64_t)n.split * kWarpColumns - 1) / ((int64_t)n.split * kWarpColumns));   // of 256 columns in a block
   n.warps = (runs + most - 1) / most;
   n.runs = (runs + n.warps - 1) / n.warps;
-  n.rows = n.split == 1 && n.warps == 1 ? most / n.runs : 1;
+}
+static void plan_groups(NormPlan& n, int64_t rows, int warps) {   // warps: of a block
   n.groups = n.split > 1 ? 1 : warps / n.warps;
   const int64_t each = (rows + (int64_t)kSms * n.rows - 1) / ((int64_t)kSms * n.rows);   // few rows are spread over the SMs
   if (n.groups > each) n.groups = each < 1 ? 1 : (int)each;
-  return n;
 }
 constexpr int kNormPeriod = 8;   // places of 16 bytes where a row may begin
 static int64_t norm_grid(const NormPlan& n, int64_t rows) {   // times split; at least a block for each place where a row begins
@@ -559,9 +570,24 @@ static int norm_mode(const void* x, int64_t stride, bool alike, int64_t row_byte
   *columns += kNormPeriod - 1;
   return kSame;
 }
-static NormPlan norm_plan(int64_t rows, int64_t columns, int dtype) { return norm_plan(rows, columns, kNormRuns, kNormRowWarps, norm_warps(dtype)); }
-static NormPlan norm_grad_plan(int64_t rows, int64_t columns) { return norm_plan(rows, columns, kNormGradRuns, kNormGradRowWarps, kNormGradWarps); }
-
+static NormPlan norm_plan(int64_t rows, int64_t columns, int dtype) {
+  NormPlan n;
+  plan_runs(n, columns, kNormRuns, kNormRowWarps);
+  // Two rows at a time share a barrier and the parameters; short ones are four, or two; few rows are spread over the SMs first.
+  n.rows = n.warps == 1 && n.split == 1 && n.runs < 3 ? kNormRuns / n.runs : dtype != IRIS_F32 && rows > 2 * kSms ? 2 : 1;
+  plan_groups(n, rows, norm_warps(dtype, n.rows * n.runs));
+  return n;
+}
+static NormPlan norm_grad_plan(int64_t rows, int64_t columns, int dtype) {
+  NormPlan n;
+  plan_runs(n, columns, kNormGradRuns, kNormGradRowWarps);
+  // Two rows at a time leave room for fewer warps: where rows have so many that it makes no difference.
+  const bool two = n.runs == 1 ? n.warps == 1 && n.split == 1
+                               : dtype != IRIS_F32 && rows > 2 * kSms && norm_grad_warps(4) / n.warps * n.warps >= norm_grad_warps(2) / n.warps * n.warps;
+  n.rows = two ? 2 : 1;
+  plan_groups(n, rows, norm_grad_warps(n.rows * n.runs));
+  return n;
+}
 // Whether a group has more than kNormChain rows, and its sums their own part.
 static bool norm_by_group(const NormPlan& n, int64_t rows) { return rows > norm_grid(n, rows) * n.groups * kNormChain; }
 static int64_t norm_parts(const NormPlan& n, int64_t rows) { return norm_grid(n, rows) * (norm_by_group(n, rows) ? n.groups : 1); }
@@ -569,17 +595,18 @@ static int64_t norm_parts(const NormPlan& n, int64_t rows) { return norm_grid(n,
 template <int DT, int PT, int R, int I, int MODE>
 static int launch_norm(const NormParams& p, const NormPlan& n, cudaStream_t st) {
   constexpr auto kernel = norm_kernel<DT, PT, R, I, MODE>;
-  constexpr int stages = norm_stages(DT) * R * Segment<DT, I>::kBytes, params = 2 * I * kWarpColumns * (int)sizeof(float);   // of a warp, of a warp of a row
-  IRIS_CHECK(allow_shared<kernel>(norm_warps(DT) * stages + kNormRowWarps * params));
+  constexpr int stages = norm_stages(DT, R * I) * R * Segment<DT, I>::kBytes, params = 2 * I * kWarpColumns * (int)sizeof(float);   // of a warp, of a warp of a row
+  IRIS_CHECK(allow_shared<kernel>(norm_warps(DT, R * I) * stages + kNormRowWarps * params));
   return launch_rows(kernel, p, (unsigned)(norm_grid(n, p.rows) * n.split), n.split, n.warps * n.groups * 32,
                      (size_t)n.warps * (n.groups * stages + params), st);
 }
 template <int DT, int PT, int MODE>
 static int launch_norm(const NormParams& p, const NormPlan& n, cudaStream_t st) {
-  return n.runs == 1   ? launch_norm<DT, PT, 4, 1, MODE>(p, n, st)
-         : n.runs == 2 ? launch_norm<DT, PT, 2, 2, MODE>(p, n, st)
-         : n.runs == 3 ? launch_norm<DT, PT, 1, 3, MODE>(p, n, st)
-                       : launch_norm<DT, PT, 1, 4, MODE>(p, n, st);
+  if (n.runs == 1) return launch_norm<DT, PT, 4, 1, MODE>(p, n, st);
+  if (n.runs == 2) return launch_norm<DT, PT, 2, 2, MODE>(p, n, st);
+  if constexpr (DT != IRIS_F32)
+    if (n.rows == 2) return n.runs == 3 ? launch_norm<DT, PT, 2, 3, MODE>(p, n, st) : launch_norm<DT, PT, 2, 4, MODE>(p, n, st);
+  return n.runs == 3 ? launch_norm<DT, PT, 1, 3, MODE>(p, n, st) : launch_norm<DT, PT, 1, 4, MODE>(p, n, st);
 }
 template <int DT, int PT>
 static int launch_norm(const NormParams& p, const NormPlan& n, int mode, cudaStream_t st) {
@@ -590,12 +617,15 @@ static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, cudaStre
   constexpr auto kernel = norm_grad_kernel<DT, PT, R, I, MODE>;
   constexpr int stages = norm_grad_stages(DT) * norm_grad_stage_bytes<DT, R, I>(), params = I * kWarpColumns * (int)sizeof(float);   // of a warp, of a warp of a row
   static_assert(stages >= 2 * params, "the groups' sums take the place of the rows");
-  IRIS_CHECK(allow_shared<kernel>(kNormGradWarps * stages + kNormGradRowWarps * params));
+  IRIS_CHECK(allow_shared<kernel>(norm_grad_warps(R * I) * (stages + params)));
   return launch_rows(kernel, p, (unsigned)(norm_grid(n, p.rows) * n.split), n.split, n.warps * n.groups * 32, (size_t)n.warps * (n.groups * stages + params), st);
 }
 template <int DT, int PT, int MODE>
 static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, cudaStream_t st) {
-  return n.runs == 1 ? launch_norm_grad<DT, PT, 2, 1, MODE>(p, n, st) : launch_norm_grad<DT, PT, 1, 2, MODE>(p, n, st);
+  if (n.runs == 1) return launch_norm_grad<DT, PT, 2, 1, MODE>(p, n, st);
+  if constexpr (DT != IRIS_F32)
+    if (n.rows == 2) return launch_norm_grad<DT, PT, 2, 2, MODE>(p, n, st);
+  return launch_norm_grad<DT, PT, 1, 2, MODE>(p, n, st);
 }
 template <int DT, int PT>
 static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, int mode, void* dweight, void* dbias, cudaStream_t st) {
@@ -651,9 +681,14 @@ extern "C" int iris_layer_norm(const iris_layer_norm_args* a, void* stream) {
 
 extern "C" size_t iris_layer_norm_workspace_bytes(int64_t rows, int64_t dim) {
   if (rows <= 0 || rows > INT32_MAX || dim <= 0 || dim > kNormMaxDim) return 0;
-  const int64_t more = dim + kNormPeriod - 1 < kNormMaxDim ? dim + kNormPeriod - 1 : kNormMaxDim;   // rows may begin anywhere
-  const int64_t a = norm_parts(norm_grad_plan(rows, dim), rows), b = norm_parts(norm_grad_plan(rows, more), rows);
-  return (size_t)(a > b ? a : b) * 2 * dim * sizeof(float);
+  int64_t parts = 0;
+  for (int dtype : {(int)IRIS_F16, (int)IRIS_F32})
+    for (int64_t columns : {dim, dim + kNormPeriod - 1})   // rows may begin anywhere
+      if (columns <= kNormMaxDim || columns == dim) {
+        const int64_t n = norm_parts(norm_grad_plan(rows, columns, dtype), rows);
+        parts = n > parts ? n : parts;
+      }
+  return (size_t)parts * 2 * dim * sizeof(float);
 }
 
 extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void* stream) {
@@ -689,7 +724,7 @@ extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void
   int64_t columns = a->dim;
   const bool alike = lie_alike(a->x, xs * es, a->dy, gs * es) && (!a->dx || lie_alike(a->x, xs * es, a->dx, ds * es));
   const int mode = norm_mode(a->x, xs * es, alike, a->dim * es, &columns);
-  const NormPlan n = norm_grad_plan(a->rows, columns);
+  const NormPlan n = norm_grad_plan(a->rows, columns, a->dtype);
   NormGradParams p{static_cast<const char*>(a->x), static_cast<const char*>(a->dy), static_cast<char*>(a->dx), xs * es, gs * es, ds * es,
                    static_cast<const char*>(a->weight), a->stats, sums ? static_cast<float*>(a->workspace) : nullptr, a->rows, (int)a->dim, n.warps,
                    n.split, period_of(xs * es), sums && norm_by_group(n, a->rows)};
