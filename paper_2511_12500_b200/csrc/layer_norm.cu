@@ -235,16 +235,28 @@ __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const 
             const uint64_t d = add2f(x[q][i][e], minus);
             s = fma2f(d, d, s);
           }
-      } else {
+      } else {   // columns that are not the row's do not count
 #pragma unroll
-        for (int i = 0; i < I; ++i)
+        for (int i = 0; i < I; ++i) {
+          uint64_t t = 0;
 #pragma unroll
           for (int e = 0; e < H; ++e) {
-            const float2 d = unpair(add2f(x[q][i][e], minus));
-            const int c = first + i * kWarpColumns + 2 * e;
-            const uint64_t there = pair(c >= rows.none && c < dim ? d.x : 0.f, c + 1 >= rows.none && c + 1 < dim ? d.y : 0.f);
-            s = fma2f(there, there, s);
+            const uint64_t d = add2f(x[q][i][e], minus);
+            t = fma2f(d, d, t);
           }
+          const int c = first + i * kWarpColumns;
+          if (c < rows.none || c + kLaneColumns > dim) {   // few threads
+            t = 0;
+            if (c < dim)
+#pragma unroll
+              for (int e = 0; e < H; ++e) {
+                const float2 d = unpair(add2f(x[q][i][e], minus));
+                const uint64_t there = pair(c + 2 * e >= rows.none && c + 2 * e < dim ? d.x : 0.f, c + 2 * e + 1 >= rows.none && c + 2 * e + 1 < dim ? d.y : 0.f);
+                t = fma2f(there, there, t);
+              }
+          }
+          s = add2f(s, t);
+        }
       }
       squares[q] = both(s);
     }
