@@ -576,7 +576,7 @@ int iris_distill_topk_backward(const iris_distill_args* args, void* stream);
  * Tokens drawn this way are distributed as if the target alone had drawn them.  Drawn by a race: the token with the largest weight / noise, the
  * lowest column among equals, so that with exponential noise (-ln of a uniform number) a token has its weight's probability.
  * A scale of +inf, or above 2e38, is greedy: p is 1 at the largest logit (the lowest column among equals), drafts are compared with it, and
- * uniform, noise and draft_logits are not read.  A row of target logits with nothing left, or with NaN or +inf, accepts nothing and its next token is
+ * uniform, noise and draft_logits are not read (with such a scale and no scales they may be NULL).  A row of target logits with nothing left, or with NaN or +inf, accepts nothing and its next token is
  * -1; a row of draft logits with NaN or +inf rejects its draft, and the next token is drawn from p. */
 typedef struct iris_verify_args {
   const void* logits;        /* [sequences * (drafts + 1)] rows: see "Common arguments"                              */
@@ -614,7 +614,7 @@ size_t iris_verify_workspace_bytes(int64_t sequences, int drafts);
 /* Embedding lookup: out row i = scale * table row tokens[i], rounded once.  The table is cut by rows into `world` shards of vocab / world rows: the
  * B shards of gemm_all_scatter are such a table (tied embeddings), in this process's memory or mapped from another's.
  * A token outside [0, vocab) gives a row of 0, and so does one whose shard is NULL (a process that has its own shard only: the sum of
- * all processes' rows is then the lookup). */
+ * all processes' rows is then the lookup).  out must not overlap the shards. */
 typedef struct iris_embed_args {
   const void* shards[IRIS_MAX_WORLD]; /* device pointers; [vocab / world, dim] each                       */
   int world, dtype;                   /* vocab % world == 0                                               */
