@@ -1,8 +1,9 @@
-"""A vocabulary-parallel LM head on the symmetric heap, and what follows it: scores of the next tokens and one distillation step.
+"""A vocabulary-parallel LM head on the symmetric heap, what leads to it and what follows it: scores of the next tokens and one distillation step.
 
-Every rank holds a column shard of the output embedding.  gemm_all_scatter leaves all logits in every rank's slot; the rows are then shared out,
-and each rank scores and distils its own rows from its own slot:
+Every rank holds a column shard of the output embedding, which is the input embedding too.  gemm_all_scatter leaves all logits in every rank's slot; the
+rows are then shared out, and each rank scores and distils its own rows from its own slot:
 
+    tokens           --> their rows of the shards, normed                                iris_embed_tokens, iris_layer_norm
     teacher's logits --> the 64 largest of each row with their log probabilities          iris_token_logprobs
     student's logits --> log probability of the next token, entropy                       iris_token_logprobs
                      --> loss against the teacher's list and, in place, its gradient      iris_distill_topk
@@ -32,6 +33,15 @@ class Head:
     def logits(self, hidden: torch.Tensor, shards: list[torch.Tensor]):
         """hidden [tokens, d] bf16, shards [vocab / world, d] bf16."""
         iris.gemm_all_scatter(hidden, shards, self.handle, self.tokens, self.vocab, hidden.shape[1], self.world, iris.IRIS_MODE_FUSED_SEQUENTIAL)
+
+    def inputs(self, tokens: torch.Tensor, shards: list[torch.Tensor], layers: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor) -> torch.Tensor:
+        """The head's input (bf16 [tokens, d]): the tokens' embeddings plus what a model's layers add to them (here as given), normed."""
+        n, d = self.tokens, shards[0].shape[1]
+        hidden = torch.empty(n, d, dtype=torch.bfloat16, device="cuda")
+        iris.iris_embed_tokens(shards, self.vocab, d, iris.IRIS_BF16, tokens, n, hidden)
+        hidden += layers
+        iris.iris_layer_norm(hidden, n, d, iris.IRIS_BF16, hidden, weight=weight, bias=bias)
+        return hidden
 
     def rows_of(self, rank: int) -> tuple[int, int, int]:
         """(device address, first row, number of rows) of rank's share in rank's own slot."""
@@ -70,7 +80,9 @@ def main(argv=None):
     p.add_argument("--list", type=int, default=64)
     a = p.parse_args(argv)
     gen = torch.Generator(device="cuda").manual_seed(0)
-    hidden = torch.randn(a.tokens, a.hidden, device="cuda", generator=gen).bfloat16()
+    tokens = torch.randint(0, a.vocab, (a.tokens,), device="cuda", generator=gen)
+    layers = torch.randn(a.tokens, a.hidden, device="cuda", generator=gen).bfloat16()
+    rest = layers, torch.ones(a.hidden, device="cuda"), torch.zeros(a.hidden, device="cuda")   # the norm's weight and bias
     embed = [torch.randn(a.vocab // a.world, a.hidden, device="cuda", generator=gen).mul_(2 / a.hidden ** 0.5).bfloat16() for _ in range(a.world)]
     better = [(e + 0.2 * torch.randn(e.shape, device="cuda", generator=gen) / a.hidden ** 0.5).bfloat16() for e in embed]
     next_token = torch.randint(0, a.vocab, (a.tokens, 1), device="cuda", generator=gen)
@@ -79,8 +91,8 @@ def main(argv=None):
     begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     try:
         for _ in range(3):
-            teacher.logits(hidden, better)
-            student.logits(hidden, embed)
+            teacher.logits(teacher.inputs(tokens, better, *rest), better)
+            student.logits(student.inputs(tokens, embed, *rest), embed)
             begin.record()
             out = step(teacher, student, next_token, weight, a.list)
             end.record()
