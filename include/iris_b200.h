@@ -620,7 +620,7 @@ typedef struct iris_embed_args {
   int world, dtype;                   /* vocab % world == 0                                               */
   int64_t vocab, dim, shard_stride;   /* vocab <= 2^30, dim <= 2^24 (IRIS_ERR_UNSUPPORTED beyond that)    */
   const int64_t* tokens;              /* [n]                                                              */
-  int64_t n;                          /* < 2^31                                                           */
+  int64_t n;                          /* <= 2^30 (IRIS_ERR_UNSUPPORTED beyond that), in both calls        */
   void* out;                          /* [n, dim]                                                         */
   int64_t out_stride;
   float scale;

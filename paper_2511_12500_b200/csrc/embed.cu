@@ -7,6 +7,7 @@ namespace iris {
 namespace rows {
 
 // ---- lookup --------------------------------------------------------------------------------------------------------
+constexpr int64_t kMaxTokens = 1 << 30;   // places, and those a little behind the last, are counted in 32 bits
 constexpr int kEmbedThreads = 256;
 
 struct EmbedParams {
@@ -736,7 +737,7 @@ static int check_table(const char* fn, int dtype, int world, int64_t vocab, int6
   if (dtype != IRIS_F16 && dtype != IRIS_BF16 && dtype != IRIS_F32) return fail(IRIS_ERR_ARG, "%s: unknown dtype %d", fn, dtype);
   if (world < 1 || world > IRIS_MAX_WORLD) return fail(IRIS_ERR_ARG, "%s: world=%d not in [1, %d]", fn, world, IRIS_MAX_WORLD);
   if (vocab < 0 || dim < 0 || n < 0) return fail(IRIS_ERR_ARG, "%s: vocab=%lld, dim=%lld, n=%lld", fn, (long long)vocab, (long long)dim, (long long)n);
-  if (vocab > kMaxVocab || dim > kMaxDim || n > INT32_MAX) return fail(IRIS_ERR_UNSUPPORTED, "%s: at most 2^31 - 1 tokens, 2^30 rows of 2^24 columns", fn);
+  if (vocab > kMaxVocab || dim > kMaxDim || n > kMaxTokens) return fail(IRIS_ERR_UNSUPPORTED, "%s: at most 2^30 tokens, 2^30 rows of 2^24 columns", fn);
   if (vocab % world) return fail(IRIS_ERR_ARG, "%s: vocab=%lld is not a multiple of world=%d", fn, (long long)vocab, world);
   return IRIS_OK;
 }
@@ -784,7 +785,7 @@ extern "C" int iris_embed_tokens(const iris_embed_args* a, void* stream) {
 }
 
 extern "C" size_t iris_embed_workspace_bytes(int64_t n, int64_t vocab, int64_t dim) {
-  if (n < 0 || vocab < 0 || dim < 0 || n > INT32_MAX || vocab > kMaxVocab || dim > kMaxDim) return 0;
+  if (n < 0 || vocab < 0 || dim < 0 || n > kMaxTokens || vocab > kMaxVocab || dim > kMaxDim) return 0;
   return embed_grad_plan(n, vocab, dim).bytes;
 }
 

@@ -588,7 +588,7 @@ static int period_of(int64_t stride) {   // bytes
 }
 // How the rows lie that a call reads and writes (`alike`: the others as x's).  Comes back with the columns counted as the kernel does.
 static int norm_mode(const void* x, int64_t stride, bool alike, int64_t row_bytes, int64_t* columns) {
-  if (!alike) return kAny;
+  if (!alike || stride < 16) return kAny;   // kSame reads whole 16 bytes where rows begin and end, which are to lie between the rows before and behind
   if (reinterpret_cast<uintptr_t>(x) % 16 == 0 && stride % 16 == 0) return row_bytes % 16 == 0 ? kAligned : kSame;
   if (*columns + kNormPeriod - 1 > kNormMaxDim) return kAny;
   *columns += kNormPeriod - 1;
@@ -747,7 +747,7 @@ extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void
   const int64_t es = (int64_t)elem_size(a->dtype);
   int64_t columns = a->dim;
   const bool alike = lie_alike(a->x, xs * es, a->dy, gs * es) && (!a->dx || lie_alike(a->x, xs * es, a->dx, ds * es));
-  const int mode = norm_mode(a->x, xs * es, alike, a->dim * es, &columns);
+  const int mode = norm_mode(a->x, xs * es, alike && gs * es >= 16, a->dim * es, &columns);
   const NormPlan n = norm_grad_plan(a->rows, columns, a->dtype);
   NormGradParams p{static_cast<const char*>(a->x), static_cast<const char*>(a->dy), static_cast<char*>(a->dx), xs * es, gs * es, ds * es,
                    static_cast<const char*>(a->weight), a->stats, sums ? static_cast<float*>(a->workspace) : nullptr, a->rows, (int)a->dim, n.warps,

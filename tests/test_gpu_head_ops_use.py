@@ -225,6 +225,28 @@ def test_norm_of_a_column_range_next_to_another(dtype):
     assert bool((y[:, :a] == GUARD).all())
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("n,dim,stride,shift", [(300, 1, 1, 0), (300, 1, 1, 3), (40, 3, 4, 1), (40, 5, 7, 2), (40, 7, 7, 1), (40, 8, 9, 5)])
+def test_norm_of_rows_shorter_than_16_bytes(dtype, n, dim, stride, shift):
+    """Several rows in the same 16 bytes; around the matrix nothing counts, whatever lies there."""
+    def matrix(seed):
+        store = torch.full((n * stride + 64,), math.nan, dtype=dtype, device="cuda")
+        view = store[shift:].as_strided((n, dim), (stride, 1), shift)
+        view.copy_(randn(n, dim, seed=seed))
+        return view
+
+    x, dy, w = matrix(1), matrix(2), randn(dim, seed=3)
+    y, dx, stats, dw = matrix(4), matrix(5), torch.empty(n, 2, device="cuda"), torch.empty(dim, device="cuda")
+    work = torch.empty(iris.iris_layer_norm_workspace_bytes(n, dim), dtype=torch.uint8, device="cuda")
+    iris.iris_layer_norm(x, n, dim, KIND[dtype], y, weight=w, stats=stats, eps=0.5, row_stride=stride, out_stride=stride)
+    iris.iris_layer_norm_backward(x, n, dim, KIND[dtype], dy, stats, work, weight=w, dx=dx, dweight=dw, row_stride=stride, dy_stride=stride, dx_stride=stride)
+    want, _, off, _ = ref.norm(x, w, None, 0.5)
+    near(y, want, off, dtype)
+    want_x, want_w, _, off_x, off_w, _ = ref.norm_grad(x, dy, w, stats)
+    near(dx, want_x, off_x, dtype)
+    near(dw, want_w, off_w, FP32)
+
+
 def test_verify_drafts_end_at_the_first_that_is_absent():
     b, n, vocab = 8, 4, 500
     z, t, u, e, q = drafted(b, n, vocab, BF16, 11, agree=0.1)

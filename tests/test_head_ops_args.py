@@ -74,8 +74,8 @@ def test_refusals(call, change, says):
 
 
 @pytest.mark.parametrize("call,change", [
-    ("iris_verify_drafts", dict(vocab=(1 << 30) + 1)), ("iris_verify_drafts", dict(sequences=1 << 28)), ("iris_embed_tokens", dict(n=1 << 31)),
-    ("iris_embed_tokens", dict(vocab=1 << 31)), ("iris_embed_tokens", dict(dim=(1 << 24) + 1)), ("iris_embed_tokens_backward", dict(n=1 << 31)),
+    ("iris_verify_drafts", dict(vocab=(1 << 30) + 1)), ("iris_verify_drafts", dict(sequences=1 << 28)), ("iris_embed_tokens", dict(n=(1 << 30) + 1)),
+    ("iris_embed_tokens", dict(vocab=1 << 31)), ("iris_embed_tokens", dict(dim=(1 << 24) + 1)), ("iris_embed_tokens_backward", dict(n=(1 << 30) + 1)),
     ("iris_embed_tokens_backward", dict(dim=(1 << 24) + 1)), ("iris_layer_norm", dict(dim=65537)), ("iris_layer_norm", dict(rows=1 << 31)),
     ("iris_layer_norm_backward", dict(dim=65537))])
 def test_sizes_beyond_the_limits(call, change):
