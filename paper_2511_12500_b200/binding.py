@@ -611,9 +611,12 @@ def _rows(names, *specs):
         _first_call()
     at = _accept_rows(_device(), *specs)
     if at is None:
+        at = []
         for i, what in enumerate(names):
-            _look_at_rows_of(*specs[5 * i: 5 * i + 5], what)
-        at = [_ptr(x) or 0 for x in specs[::5]]
+            x, *spec = specs[5 * i: 5 * i + 5]
+            for one in x if isinstance(x, list) else [x]:
+                _look_at_rows_of(one, *spec, what)
+                at.append(_ptr(one) or 0)
     return at
 
 
@@ -654,10 +657,7 @@ def _world(shards):
 def iris_embed_tokens(shards, vocab, dim, dtype, tokens, n, out, scale=1.0, shard_stride=0, out_stride=0, stream=None):
     """out[i] = scale * the table's row tokens[i]; shards: the table's rows in equal parts, one after the other (None: not here)."""
     world = _world(shards)
-    specs = []
-    for x in shards:
-        specs += (x, dtype, vocab // world, dim, shard_stride)
-    t, o, *at = _rows(("tokens", "out") + ("shard",) * world, tokens, _INT64, n, 1, _BUFFER, out, dtype, n, dim, out_stride, *specs)
+    t, o, *at = _rows(("tokens", "out", "shard"), tokens, _INT64, n, 1, _BUFFER, out, dtype, n, dim, out_stride, list(shards), dtype, vocab // world, dim, shard_stride)
     rc = lib().iris_embed_tokens(_EMBED_ARGS.pack(*at, *_NO_SHARDS[IRIS_MAX_WORLD - world], world, dtype, vocab, dim, shard_stride, t, n, o, out_stride, scale),
                                  _stream(stream))
     if rc:
@@ -672,11 +672,8 @@ def iris_embed_tokens_backward(grad_out, n, dim, dtype, tokens, grad_shards, voc
                                shard_stride=0, stream=None):
     """The table's gradient, into shards of its own layout."""
     world, size = _world(grad_shards), _size_of(workspace)
-    specs = []
-    for x in grad_shards:
-        specs += (x, grad_dtype, vocab // world, dim, shard_stride)
-    t, g, w, *at = _rows(("tokens", "grad_out", "workspace") + ("grad_shard",) * world, tokens, _INT64, n, 1, _BUFFER,
-                         grad_out, dtype, n, dim, grad_out_stride, workspace, _BYTES, 1, size, _BUFFER, *specs)
+    t, g, w, *at = _rows(("tokens", "grad_out", "workspace", "grad_shard"), tokens, _INT64, n, 1, _BUFFER, grad_out, dtype, n, dim, grad_out_stride,
+                         workspace, _BYTES, 1, size, _BUFFER, list(grad_shards), grad_dtype, vocab // world, dim, shard_stride)
     rc = lib().iris_embed_tokens_backward(_EMBED_GRAD_ARGS.pack(g, n, dim, grad_out_stride, dtype, grad_dtype, t, *at, *_NO_SHARDS[IRIS_MAX_WORLD - world], world,
                                                                 bool(accumulate), vocab, shard_stride, scale, w, size), _stream(stream))
     if rc:

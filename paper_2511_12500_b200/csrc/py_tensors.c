@@ -161,46 +161,48 @@ static int of_kind(const Description* t, long long kind) {
   return kind >= 0 && kind <= 4 && t->type_code == kinds[kind].code && t->type_bits == kinds[kind].bits && t->type_lanes == 1;
 }
 
+/* Whether x is a matrix of rows, as rows() below describes them. */
+static int rows_of(PyObject* x, long long device, long long kind, long long rows, long long columns, long long stride, unsigned long long* at) {
+  Description t;
+  int is_tensor;
+  int64_t count;
+  if (!address(x, at, &t, &is_tensor)) return 0;
+  if (!is_tensor || rows <= 0 || columns <= 0) return 1;
+  if (!of_kind(&t, kind) || rows > INT32_MAX || columns > INT64_MAX / 4 / rows || (t.device_type == ON_GPU && t.device_id != device)) return 0;
+  const int whole = contiguous(&t, &count);
+  if (stride < 0) return whole && count >= rows * columns;
+  if (whole) {
+    if (stride == 0 && rows > 1 && (t.ndim == 0 || (t.ndim > 1 && t.shape[t.ndim - 1] != columns))) return 0;
+  } else {
+    if ((stride == 0 && rows > 1) || t.ndim < 1 || (columns > 1 && t.strides[t.ndim - 1] != 1)) return 0;
+    count = 1;
+    for (int j = 0; j < t.ndim; ++j) {
+      if (t.shape[j] == 0) return 0;
+      count += (t.shape[j] - 1) * t.strides[j];
+    }
+  }
+  if (stride == 0) stride = columns;
+  return stride <= INT64_MAX / 4 / rows && (rows - 1) * stride + columns <= count;
+}
+
 /* rows(device, {tensor, kind, rows, columns, stride} ...) -> the addresses (0 for None), or None: look again.  Each is a matrix of rows `stride`
- * elements apart (0: the tensor's own rows, one after the other; -1: a contiguous buffer of rows * columns elements).  Tensors are on GPU `device`
- * or in pinned or managed memory. */
+ * elements apart (0: the tensor's own rows, one after the other; -1: a contiguous buffer of rows * columns elements), or a list of such.  Tensors
+ * are on GPU `device` or in pinned or managed memory. */
 static PyObject* rows(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-  unsigned long long at[40];
+  enum { MOST = 64 };
+  unsigned long long at[MOST];
   Py_ssize_t k = 0;
-  if (!exchange || n < 1 || (n - 1) % 5 || (n - 1) / 5 > 40) Py_RETURN_NONE;
+  if (!exchange || n < 1 || (n - 1) % 5) Py_RETURN_NONE;
   const long long device = PyLong_AsLongLong(args[0]);
-  for (Py_ssize_t i = 1; i < n; i += 5, ++k) {
-    Description t;
-    int is_tensor;
-    int64_t count;
+  for (Py_ssize_t i = 1; i < n; i += 5) {
     long long v[4];
-    if (!address(args[i], &at[k], &t, &is_tensor)) Py_RETURN_NONE;
-    if (!is_tensor) continue;
     for (int j = 0; j < 4; ++j) v[j] = PyLong_AsLongLong(args[i + 1 + j]);
     if (PyErr_Occurred()) goto again;
-    const long long rows = v[1], columns = v[2];
-    long long stride = v[3];
-    if (rows <= 0 || columns <= 0) continue;
-    if (!of_kind(&t, v[0]) || rows > INT32_MAX || columns > INT64_MAX / 4 / rows || (t.device_type == ON_GPU && t.device_id != device)) Py_RETURN_NONE;
-    const int whole = contiguous(&t, &count);
-    if (stride < 0) {
-      if (!whole || count < rows * columns) Py_RETURN_NONE;
-      continue;
-    }
-    if (whole) {
-      if (stride == 0 && rows > 1 && (t.ndim == 0 || (t.ndim > 1 && t.shape[t.ndim - 1] != columns))) Py_RETURN_NONE;
-    } else {
-      if ((stride == 0 && rows > 1) || t.ndim < 1 || (columns > 1 && t.strides[t.ndim - 1] != 1)) Py_RETURN_NONE;
-      count = 1;
-      for (int j = 0; j < t.ndim; ++j) {
-        if (t.shape[j] == 0) Py_RETURN_NONE;
-        count += (t.shape[j] - 1) * t.strides[j];
-      }
-    }
-    if (stride == 0) stride = columns;
-    if (stride > INT64_MAX / 4 / rows || (rows - 1) * stride + columns > count) Py_RETURN_NONE;
+    const int list = PyList_CheckExact(args[i]);
+    const Py_ssize_t m = list ? PyList_GET_SIZE(args[i]) : 1;
+    for (Py_ssize_t j = 0; j < m; ++j)
+      if (k == MOST || !rows_of(list ? PyList_GET_ITEM(args[i], j) : args[i], device, v[0], v[1], v[2], v[3], &at[k++])) Py_RETURN_NONE;
   }
-  if (PyErr_Occurred()) goto again;
   PyObject* out = PyTuple_New(k);
   if (!out) return NULL;
   for (Py_ssize_t i = 0; i < k; ++i) {
