@@ -26,7 +26,7 @@ struct EmbedParams {
 //
 // 32768 x 4096 bf16 70 us, 74 % of the copy rate; 32771 x 4099 fp16, where no two rows lie alike, 84 us (62 %): token, row and store come one after the other
 // in a warp, 32 warps an SM.  With the ends of a row moved by single threads one element after the other 116 us; shifts by selections instead of cases 118; parts
-// of all rows counted through, with a division a thread, 147.  64 rows of 8192: 7.3 us, of which the launch and three latencies are nearly all.
+// of all rows counted through, with a division a thread, 147.  64 rows of 8192: 6.2 us, of which the launch and three latencies are nearly all.
 // 16 bytes from byte b of the row on, all of which lie in it, though the aligned ones that they touch do not.
 template <int ES>
 __device__ __forceinline__ uint4 load_apart(const char* from, int b) {
@@ -624,15 +624,23 @@ __global__ void __launch_bounds__(kJoinWarps * 32) embed_join_kernel(const __gri
 }
 
 // Few tokens, without sorting: a warp looks after one place and 256 columns, and adds up the rows of all places with its token, in their order, if it
-// is the first of them; other warps clear the rows that no token names.  64 tokens, 8192 rows of 1024: 9.5 us instead of 24.
-constexpr int kFewTokens = 256;
+// is the first of them; other warps clear the rows that no token names.  64 tokens, 8192 rows of 1024: 8 us instead of 24; 400: 10.5 instead of 25.
+// Where nearly all tokens are one, its warps take 0.11 us a row, the latency of the seven rows under way: 150 of 500 make it 22 us, all 500 55, sorting 20.
+constexpr int kFewTokens = 512;
 
 template <int DT, int GT, bool ALIGNED>
-__global__ void __launch_bounds__(kSumThreads) embed_few_kernel(const __grid_constant__ EmbedGradParams p) {
+struct Few {
   using G = Segment<DT, 1, ALIGNED>;
-  constexpr int kAhead = 4, H = kLaneColumns / 2, kOut = Segment<GT, 1>::kBytes;
-  __shared__ uint32_t keys[kFewTokens];
-  __shared__ __align__(16) char rows[kSumWarps][kAhead * G::kBytes + kOut];
+  static constexpr int kStages = 8, kWarp = kStages * G::kBytes + Segment<GT, 1>::kBytes + kFewTokens * 2;   // rows, a row of the result, places
+  static constexpr int kBytes = kFewTokens * 4 + kSumWarps * kWarp;                                          // tokens
+};
+template <int DT, int GT, bool ALIGNED>
+__global__ void __launch_bounds__(kSumThreads) embed_few_kernel(const __grid_constant__ EmbedGradParams p) {
+  using F = Few<DT, GT, ALIGNED>;
+  using G = typename F::G;
+  constexpr int H = kLaneColumns / 2, kStages = F::kStages;
+  extern __shared__ __align__(16) char few[];
+  uint32_t* const keys = reinterpret_cast<uint32_t*>(few);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   ptx::let_next_begin();
   ptx::begin_after_previous();
@@ -651,39 +659,43 @@ __global__ void __launch_bounds__(kSumThreads) embed_few_kernel(const __grid_con
   if (place >= p.n) return;
   const uint32_t key = keys[place];
   if (key >= p.vocab) return;
-  const uint32_t own = ptx::smem_u32(rows[warp]);
-  uint64_t sum[1][H] = {};
-  typename G::Lone lone[kAhead];
+  char* const mine = few + kFewTokens * 4 + warp * F::kWarp;
+  const uint32_t own = ptx::smem_u32(mine);
+  uint16_t* const list = reinterpret_cast<uint16_t*>(mine + kStages * G::kBytes + Segment<GT, 1>::kBytes);
+  int m = 0;   // places with this token
   for (int at = 0; at < p.n; at += 32) {
-    uint32_t same = __ballot_sync(~0u, keys[at + lane] == key);
-    if (same && (at + __ffs(same) - 1 < place)) return;   // it is not the first
-    while (same) {
-      const char* row[kAhead];
-      int m = 0;
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (same) {
-          row[u] = p.dy + (int64_t)(at + __ffs(same) - 1) * p.dy_stride;
-          same &= same - 1;
-          G::fetch(own + u * G::kBytes, row[u], column, p.dim, lone[u]);
-          m = u + 1;
-        }
-      copy_async_wait();
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) lone[u].settle();
-      __syncwarp();
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (u < m) {
-          uint64_t x[H];
-          G::read(own + u * G::kBytes, row[u], column, p.dim, 0, x);
-#pragma unroll
-          for (int e = 0; e < H; ++e) sum[0][e] = add2f(sum[0][e], x[e]);
-        }
-      __syncwarp();
-    }
+    const bool one = keys[at + lane] == key;
+    const uint32_t same = __ballot_sync(~0u, one);
+    if (m == 0 && same && at + __ffs(same) - 1 < place) return;   // it is not the first
+    if (one) list[m + __popc(same & ((1u << lane) - 1))] = (uint16_t)(at + lane);
+    m += __popc(same);
   }
-  write_row<GT, 1, ALIGNED>(p, key, own + kAhead * G::kBytes, column, sum);
+  __syncwarp();
+  uint64_t sum[1][H] = {};
+  typename G::Lone lone;
+  const auto row_of = [&](int i) { return p.dy + (int64_t)list[i] * p.dy_stride; };
+  const auto fetch = [&](int i, uint32_t to) {
+    lone.settle();
+    if (i < m) G::fetch(to, row_of(i), column, p.dim, lone);
+    copy_async_commit();
+  };
+#pragma unroll 1
+  for (int k = 0; k < kStages - 1; ++k) fetch(k, own + k * G::kBytes);
+  uint32_t here = own, before = own + (kStages - 1) * G::kBytes;
+#pragma unroll 1
+  for (int i = 0; i < m; ++i) {
+    lone.settle();
+    copy_async_wait_but<kStages - 2>();
+    __syncwarp();
+    fetch(i + kStages - 1, before);
+    uint64_t x[H];
+    G::read(here, row_of(i), column, p.dim, 0, x);
+#pragma unroll
+    for (int e = 0; e < H; ++e) sum[0][e] = add2f(sum[0][e], x[e]);
+    before = here;
+    here = here == own + (kStages - 1) * G::kBytes ? own : here + G::kBytes;
+  }
+  write_row<GT, 1, ALIGNED>(p, key, own + kStages * G::kBytes, column, sum);
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
@@ -722,10 +734,16 @@ static int launch_sum(const EmbedGradParams& p, unsigned fill_blocks, cudaStream
   IRIS_CHECK(allow_shared<kernel>(bytes));
   return launch_rows(kernel, p, p.sum_blocks + fill_blocks, 1, kSumThreads, bytes, st);
 }
+template <int DT, int GT, bool ALIGNED>
+static int launch_few(const EmbedGradParams& p, unsigned fill_blocks, cudaStream_t st) {
+  constexpr auto kernel = embed_few_kernel<DT, GT, ALIGNED>;
+  IRIS_CHECK(allow_shared<kernel>(Few<DT, GT, ALIGNED>::kBytes));
+  return launch_rows(kernel, p, p.sum_blocks + fill_blocks, 1, kSumThreads, Few<DT, GT, ALIGNED>::kBytes, st);
+}
 template <int DT, int GT>
 static int launch_embed_grad(const EmbedGradParams& p, const EmbedGradPlan& g, unsigned fill_blocks, cudaStream_t st) {
   const bool few = p.n <= kFewTokens, aligned = p.dim * Columns<DT>::ES % 16 == 0 && p.dim * Columns<GT>::ES % 16 == 0 && p.aligned && p.dy_stride % 16 == 0 && p.shard_stride % 16 == 0;
-  if (few) return launch_rows(aligned ? embed_few_kernel<DT, GT, true> : embed_few_kernel<DT, GT, false>, p, p.sum_blocks + fill_blocks, 1, kSumThreads, 0, st);
+  if (few) return aligned ? launch_few<DT, GT, true>(p, fill_blocks, st) : launch_few<DT, GT, false>(p, fill_blocks, st);
   if (g.runs == 1) IRIS_CHECK(aligned ? launch_sum<DT, GT, 1, true>(p, fill_blocks, st) : launch_sum<DT, GT, 1, false>(p, fill_blocks, st));
   else IRIS_CHECK(aligned ? launch_sum<DT, GT, 2, true>(p, fill_blocks, st) : launch_sum<DT, GT, 2, false>(p, fill_blocks, st));
   if (p.chunks < 2) return IRIS_OK;
