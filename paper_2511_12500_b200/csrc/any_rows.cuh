@@ -451,6 +451,38 @@ inline int allow_shared(int bytes, bool large_clusters = false) {
   if (dev < kDevices) done[dev].store(true, std::memory_order_release);
   return IRIS_OK;
 }
+// How many clusters of `split` blocks (a power of two, at most 8) of a kernel whose blocks have an SM to themselves are there at once: an SM that is left over in its
+// part of the chip has none, so that clusters of 4 and 8 do not get all of them.  threads, bytes: the kernel's most.
+template <auto KERNEL>
+inline int clusters_at_once(int split, int threads, int bytes, int* clusters) {
+  constexpr int kDevices = 64, kSplits = 4;
+  static std::atomic<int> known[kDevices][kSplits] = {};
+  int dev = -1, which = 0;
+  if (split == 1) {
+    *clusters = kSms;
+    return IRIS_OK;
+  }
+  while (1 << which < split) ++which;
+  IRIS_CUDA_TRY(cudaGetDevice(&dev));
+  int n = dev < kDevices ? known[dev][which].load(std::memory_order_acquire) : 0;
+  if (!n) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)split);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)bytes;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)split;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    IRIS_CUDA_TRY(cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg));
+    n = n < 1 ? 1 : n > kSms / split ? kSms / split : n;
+    if (dev < kDevices) known[dev][which].store(n, std::memory_order_release);
+  }
+  *clusters = n;
+  return IRIS_OK;
+}
 // Whether rows `stride` bytes apart all begin at 16 bytes.
 inline bool aligned_rows(const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0; }
 // A matrix of rows; `stride` comes back as the elements between rows.

@@ -12,6 +12,7 @@ namespace rows {
 
 constexpr int kNormRuns = 4, kNormGradRuns = 2;   // runs of 8 columns that a thread holds, of one row or of several short ones
 constexpr int kNormRowWarps = 8, kNormGradRowWarps = 16;   // of a row in a block, at most
+constexpr int kNormSplitGroups = 4;             // of a block in a cluster, at most
 constexpr int kNormSplit = 8;                   // blocks (one cluster) that share a row
 constexpr int64_t kNormMaxDim = (int64_t)kNormRuns * kWarpColumns * kNormRowWarps * kNormSplit;
 static_assert(kNormRuns * kNormRowWarps == kNormGradRuns * kNormGradRowWarps, "the same limit for both directions");
@@ -21,6 +22,7 @@ constexpr int norm_warps(int dtype, int rows_runs) { return dtype == IRIS_F32 ||
 constexpr int norm_stages(int dtype, int rows_runs) { return dtype == IRIS_F32 || rows_runs > 4 ? 2 : 3; }
 constexpr int norm_grad_warps(int rows_runs) { return rows_runs > 2 ? 12 : 16; }
 constexpr int norm_grad_stages(int dtype) { return dtype == IRIS_F32 ? 2 : 3; }
+constexpr uint64_t kNormWait = 1000000000;      // ns for another block's values, after which they are taken for lost
 constexpr int kNormChain = 128;                 // rows that a thread adds up before the sum goes to the sum of such sums
 
 // How rows lie: all at 16 bytes, and their lengths multiples of that; those of all matrices alike, at any places of 16 bytes; anyhow.
@@ -46,11 +48,12 @@ struct NormGradParams {
   const float* stats;
   float* parts;                 // [blocks / split (times groups if by_group), 2, dim]: sums of dy h and of dy; nullptr: not wanted
   int64_t rows;
-  int dim, warps, split, period, by_group;
+  int dim, warps, split, period, by_group;   // by_group: of norm_by_group
 };
 
 // What a warp knows of a row, and the sum over the warps of a row, which all of its threads get.
 struct NormShared {
+  uint64_t arrived[kNormSplitGroups][2];   // of a group's values in a cluster, one for each half
   float2 of[2][kNormRows][kNormGradRowWarps * kNormSplit];   // twice: one is read while the next rows' is written
 };
 struct Group {
@@ -62,16 +65,47 @@ struct Group {
     warp = (int)(threadIdx.x >> 5) % warps + rank * warps;
     id = 1 + index;
   }
-  // Every warp of the rows puts its values into `turn`'s half and waits for the others'.
+  // Before the first exchange; all blocks of the cluster.
   template <int R>
-  __device__ __forceinline__ void exchange(NormShared& s, int turn, const float (&a)[R], const float (&b)[R]) const {
+  __device__ __forceinline__ void prepare(NormShared& s) const {
+    if (split == 1) return;
+    if (warp == rank * warps && lane == 0) {
+      for (int h = 0; h < 2; ++h) {
+        ptx::mbar_init(ptx::smem_u32(&s.arrived[index][h]), 1);
+        ptx::mbar_arrive_expect_tx(ptx::smem_u32(&s.arrived[index][h]), all() * R * 8);
+      }
+      ptx::fence_mbar_init();
+    }
+    ptx::cluster_sync();
+  }
+  // The last thing a block does: the others may still write to its shared memory.
+  __device__ __forceinline__ void finish() const {
+    __syncwarp();
+    if (split > 1) ptx::cluster_sync();
+  }
+  // Every warp of the rows puts its values into a half of the shared memory (the halves in turn) and waits for the others'.  `lost`
+  // becomes NaN, and stays it, where they have not come within a second (the rows are NaN from then on).
+  //
+  // In a cluster the values count themselves on the mbarrier of the block that they go to.  A barrier of the cluster would wait for
+  // the stores of the row before as well.  A warp writes to a half again when all values of the exchange after have come, which each warp
+  // sends when it has read that half; for the same reason one thread may prepare the mbarrier for its next use as soon as it has seen the values come.
+  template <int R>
+  __device__ __forceinline__ void exchange(NormShared& s, uint32_t count, const float (&a)[R], const float (&b)[R], float& lost) const {
     static_assert(R <= kNormRows, "room for them");
+    const uint32_t turn = count & 1;
     if (split > 1) {
+      const uint32_t bar = ptx::smem_u32(&s.arrived[index][turn]), parity = count >> 1 & 1;
       if (lane < split) {
 #pragma unroll
-        for (int q = 0; q < R; ++q) ptx::st_shared_cluster_u64(ptx::mapa(ptx::smem_u32(&s.of[turn][q][warp]), lane), pair(a[q], b[q]));
+        for (int q = 0; q < R; ++q) ptx::st_async_u64(ptx::mapa(ptx::smem_u32(&s.of[turn][q][index * all() + warp]), lane), pair(a[q], b[q]), ptx::mapa(bar, lane));
       }
-      ptx::cluster_sync();
+      if (!ptx::mbar_try_wait_cluster(bar, parity)) {
+        const uint64_t start = globaltimer_ns();
+        while (lost == 0.f && !ptx::mbar_try_wait_cluster(bar, parity))
+          if (globaltimer_ns() - start > kNormWait) lost = NAN;
+      }
+      __syncwarp();
+      if (warp == rank * warps && lane == 0) ptx::mbar_arrive_expect_tx(bar, all() * R * 8);
     } else {
       if (lane == 0) {
 #pragma unroll
@@ -81,7 +115,7 @@ struct Group {
     }
   }
   __device__ __forceinline__ int all() const { return warps * split; }
-  __device__ __forceinline__ const float2* of(const NormShared& s, int turn, int q) const { return s.of[turn][q] + (split > 1 ? 0 : index * warps); }
+  __device__ __forceinline__ const float2* of(const NormShared& s, int turn, int q) const { return s.of[turn][q] + index * all(); }
 };
 
 // How the columns of a row are shared by its warps: `each` a warp, `rest` in the last one that has any, of which the first has `none` that are not the row's.
@@ -156,7 +190,7 @@ __device__ __forceinline__ float both(uint64_t x) {
 // shared memory nothing waits for memory long (1.0 warps an issue); what is left is chains of dependent instructions, shuffles and barriers at 16 warps an SM, so
 // the rows in work count: 4104 columns, whose fifth warp has 8 of them, take 71 us for 16001 rows, 4096 columns 57; rows of 4096 that begin at
 // any element 96.  Held in registers one row ahead instead of copied ahead: 244; parameters read from L1 instead of shared memory: 212; one row at a time 110.
-template <int DT, int PT, int R, int I, int MODE>
+template <int DT, int PT, int R, int I, int MODE, bool SPLIT>
 __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const NormParams p) {
   using C = Columns<DT>;
   using G = Segment<DT, I, MODE == kAligned>;
@@ -165,7 +199,7 @@ __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const 
   constexpr int kStages = norm_stages(DT, R * I), H = kLaneColumns / 2;
   __shared__ NormShared shared;
   extern __shared__ __align__(16) char ring[];   // [warps, stages, R] segments; weight, bias
-  const Group group(p.warps, p.split);
+  const Group group(p.warps, SPLIT ? p.split : 1);
   const int groups = blockDim.x / (p.warps * 32);
   const int begin = group.warp * G::kColumns;
   const uint32_t own = ptx::smem_u32(ring) + (threadIdx.x >> 5) * (kStages * R * G::kBytes);
@@ -174,7 +208,7 @@ __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const 
   const uint32_t weight = ptx::smem_u32(params) + ((group.warp - group.rank * group.warps) * I * 64 + group.lane) * 16, bias = weight + columns * 4;
   const Rows rows = Rows::of<SAME, R>(group, groups, p.period, p.x, p.x_stride, C::ES);
   const int dim = p.dim + rows.none, first = begin + group.lane * kLaneColumns;   // counted as rows are
-  if (p.split > 1) ptx::cluster_sync();   // the others may write to this block's shared memory
+  group.prepare<R <= kNormRows ? R : 1>(shared);
   ptx::let_next_begin();
   ptx::begin_after_previous();
   typename G::Lone lone[R];
@@ -203,7 +237,8 @@ __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const 
   const float mine = fmaxf(shares.of(group.warp), 1.f), whole = 1.f / shares.dim;
   const bool full = begin >= rows.none && begin + G::kColumns <= dim;
   int stage = 0;
-  for (int turn = 0; r < p.rows; r += rows.step, x_row += x_step, y_row += y_step, turn ^= 1) {
+  float lost = 0.f;
+  for (uint32_t count = 0; r < p.rows; r += rows.step, x_row += x_step, y_row += y_step, ++count) {
 #pragma unroll
     for (int q = 0; q < R; ++q) lone[q].settle();
     copy_async_wait_but<kStages - 2>();
@@ -270,11 +305,22 @@ __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const 
     for (int q = 0; q < R; ++q) squares[q] = warp_sum(squares[q]);
     if constexpr (R <= kNormRows)
       if (group.all() > 1) {
-        group.exchange(shared, turn, mean, squares);
+        group.exchange(shared, count, mean, squares, lost);
 #pragma unroll
         for (int q = 0; q < R; ++q) {
-          const float2* const of = group.of(shared, turn, q);
-          float m = 0.f, s = 0.f;
+          const float2* const of = group.of(shared, count & 1, q);
+          float m = lost, s = 0.f;
+          if (SPLIT && group.all() > 16) {   // a lane takes a warp, or a few
+            for (int w = group.lane; w < group.all(); w += 32) m = fmaf(of[w].x, shares.of(w), m);
+            mean[q] = warp_sum(m) / shares.dim;
+            for (int w = group.lane; w < group.all(); w += 32) {
+              const float2 v = of[w];
+              const float d = v.x - mean[q];
+              s += fmaf(d * d, shares.of(w), v.y);
+            }
+            squares[q] = warp_sum(s);
+            continue;
+          }
 #pragma unroll 4
           for (int w = 0; w < group.all(); ++w) m = fmaf(of[w].x, shares.of(w), m);
           mean[q] = m / shares.dim;
@@ -313,6 +359,7 @@ __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const 
       else G::write(here + q * G::kBytes, y_row + q * rows.each * p.y_stride, begin, dim, out);
     }
   }
+  group.finish();
 }
 
 // A block's groups add up dw and db of their columns in registers, so blocks stay and a thread has the same columns of every row.  R rows at a time.
@@ -324,7 +371,7 @@ __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const 
 template <int DT, int R, int I>
 constexpr int norm_grad_stage_bytes() { return R * (2 * Segment<DT, I>::kBytes + 16); }   // x, dy, statistics
 
-template <int DT, int PT, int R, int I, int MODE>
+template <int DT, int PT, int R, int I, int MODE, bool SPLIT>
 __global__ void __launch_bounds__(norm_grad_warps(R * I) * 32) norm_grad_kernel(const NormGradParams p) {
   using C = Columns<DT>;
   using G = Segment<DT, I, MODE == kAligned>;
@@ -333,7 +380,7 @@ __global__ void __launch_bounds__(norm_grad_warps(R * I) * 32) norm_grad_kernel(
   constexpr int kStages = norm_grad_stages(DT), kRow = 2 * G::kBytes + 16, kStage = norm_grad_stage_bytes<DT, R, I>(), H = kLaneColumns / 2;
   __shared__ NormShared shared;
   extern __shared__ __align__(16) char ring[];   // [warps, stages, R] segments of x, of dy, statistics; weight
-  const Group group(p.warps, p.split);
+  const Group group(p.warps, SPLIT ? p.split : 1);
   const int groups = blockDim.x / (p.warps * 32);
   const int begin = group.warp * G::kColumns, first = begin + group.lane * kLaneColumns;
   const int columns = p.warps * G::kColumns;   // of the block
@@ -343,11 +390,11 @@ __global__ void __launch_bounds__(norm_grad_warps(R * I) * 32) norm_grad_kernel(
   float* const params = reinterpret_cast<float*>(ring + (blockDim.x >> 5) * (kStages * kStage));
   const uint32_t weight = ptx::smem_u32(params) + ((group.warp - group.rank * group.warps) * I * 64 + group.lane) * 16;
   const float whole = 1.f / (float)p.dim;
-  if (p.split > 1) ptx::cluster_sync();   // the others may write to this block's shared memory
+  group.prepare<R <= kNormRows ? R : 1>(shared);
   ptx::begin_after_previous();
   uint64_t dw[I][H] = {}, db[I][H] = {};
   // The sums so far, to this group's part.
-  const int64_t block = blockIdx.x / p.split;
+  const int64_t block = blockIdx.x / group.split;
   const auto put = [&](bool more) {
     float* const to = p.parts + (p.by_group ? block * groups + group.index : block) * 2 * p.dim;
 #pragma unroll
@@ -398,7 +445,8 @@ __global__ void __launch_bounds__(norm_grad_warps(R * I) * 32) norm_grad_kernel(
   __syncthreads();
   int chain = 0, stage = 0;
   bool more = false;
-  for (int turn = 0; r < p.rows; r += rows.step, x_row += x_step, dy_row += dy_step, dx_row += dx_step, turn ^= 1) {
+  float lost = 0.f;
+  for (uint32_t count = 0; r < p.rows; r += rows.step, x_row += x_step, dy_row += dy_step, dx_row += dx_step, ++count) {
     if (p.by_group && chain >= kNormChain) {
       put(more);
       more = true;
@@ -463,11 +511,21 @@ __global__ void __launch_bounds__(norm_grad_warps(R * I) * 32) norm_grad_kernel(
       b[q] = warp_sum(both(b2[q]));
     }
     if (group.all() > 1) {
-      group.exchange(shared, turn, a, b);
+      group.exchange(shared, count, a, b, lost);
 #pragma unroll
       for (int q = 0; q < R; ++q) {
-        const float2* const of = group.of(shared, turn, q);
-        a[q] = b[q] = 0.f;
+        const float2* const of = group.of(shared, count & 1, q);
+        a[q] = b[q] = lost;
+        if (SPLIT && group.all() > 16) {   // a lane takes a warp, or a few
+          for (int w = group.lane; w < group.all(); w += 32) {
+            const float2 v = of[w];
+            a[q] += v.x;
+            b[q] += v.y;
+          }
+          a[q] = warp_sum(a[q]);
+          b[q] = warp_sum(b[q]);
+          continue;
+        }
 #pragma unroll 4
         for (int w = 0; w < group.all(); ++w) {
           const float2 v = of[w];
@@ -492,6 +550,7 @@ __global__ void __launch_bounds__(norm_grad_warps(R * I) * 32) norm_grad_kernel(
     }
   }
   ptx::let_next_begin();
+  group.finish();
   if (!p.parts) return;
   if (p.by_group || groups == 1) {
     put(more);
@@ -500,7 +559,7 @@ __global__ void __launch_bounds__(norm_grad_warps(R * I) * 32) norm_grad_kernel(
   // The groups' sums, through the ring: [groups, 2, columns].
   __syncthreads();
   float* const sums = reinterpret_cast<float*>(ring);
-  float2* const to = reinterpret_cast<float2*>(sums + group.index * 2 * columns + first);   // a row lies in one block
+  float2* const to = reinterpret_cast<float2*>(sums + group.index * 2 * columns + first - group.rank * columns);
 #pragma unroll
   for (int i = 0; i < I; ++i)
 #pragma unroll
@@ -510,14 +569,16 @@ __global__ void __launch_bounds__(norm_grad_warps(R * I) * 32) norm_grad_kernel(
     }
   __syncthreads();
   float* const part = p.parts + block * 2 * p.dim;
-  for (int c = threadIdx.x; c < p.dim; c += blockDim.x) {
+  const int from = group.rank * columns - rows.none;   // the block's first column
+  for (int c = threadIdx.x; c < columns; c += blockDim.x) {
+    if (from + c < 0 || from + c >= p.dim) continue;
     float w = 0.f, b = 0.f;
     for (int q = 0; q < groups; ++q) {
-      w += sums[q * 2 * columns + rows.none + c];
-      b += sums[(q * 2 + 1) * columns + rows.none + c];
+      w += sums[q * 2 * columns + c];
+      b += sums[(q * 2 + 1) * columns + c];
     }
-    part[c] = w;
-    part[p.dim + c] = b;
+    part[from + c] = w;
+    part[p.dim + from + c] = b;
   }
 }
 
@@ -568,13 +629,15 @@ static void plan_runs(NormPlan& n, int64_t columns, int most, int row_warps) {  
   n.runs = (runs + n.warps - 1) / n.warps;
 }
 static void plan_groups(NormPlan& n, int64_t rows, int warps) {   // warps: of a block
-  n.groups = n.split > 1 ? 1 : warps / n.warps;
-  const int64_t each = (rows + (int64_t)kSms * n.rows - 1) / ((int64_t)kSms * n.rows);   // few rows are spread over the SMs
+  if (n.split > 1 && warps > kNormGradRowWarps) warps = kNormGradRowWarps;   // that there is room for in NormShared
+  n.groups = warps / n.warps;
+  if (n.split > 1 && n.groups > kNormSplitGroups) n.groups = kNormSplitGroups;
+  const int64_t each = (rows * n.split + (int64_t)kSms * n.rows - 1) / ((int64_t)kSms * n.rows);   // few rows are spread over the SMs
   if (n.groups > each) n.groups = each < 1 ? 1 : (int)each;
 }
 constexpr int kNormPeriod = 8;   // places of 16 bytes where a row may begin
-static int64_t norm_grid(const NormPlan& n, int64_t rows) {   // times split; at least a block for each place where a row begins
-  const int64_t each = (int64_t)n.groups * n.rows, full = (rows + each - 1) / each, room = kSms / n.split, most = rows < kNormPeriod ? rows : kNormPeriod;
+static int64_t norm_grid(const NormPlan& n, int64_t rows, int64_t room) {   // clusters, of which there are `room` at once; at least a block for each place where a row begins
+  const int64_t each = (int64_t)n.groups * n.rows, full = (rows + each - 1) / each, most = rows < kNormPeriod ? rows : kNormPeriod;
   return full < most ? most : full < room ? full : room;
 }
 // Whether the rows of two matrices lie alike in 16 bytes.
@@ -604,7 +667,10 @@ static NormPlan norm_plan(int64_t rows, int64_t columns, int dtype) {
 }
 static NormPlan norm_grad_plan(int64_t rows, int64_t columns, int dtype) {
   NormPlan n;
-  plan_runs(n, columns, kNormGradRuns, kNormGradRowWarps);
+  // Rows of more than 8 warps are shared by two blocks of two groups rather than held by one group (8192 x 8192 bf16 93 us instead of 101, fp32 91 instead of 103);
+  // four blocks instead of two leave 16 of 148 SMs without a cluster (5500 x 12000: 113 us instead of 110).
+  const bool pairs = columns > kNormGradRuns * kWarpColumns * kNormGradRowWarps / 2 && columns <= kNormGradRuns * kWarpColumns * kNormGradRowWarps;
+  plan_runs(n, columns, kNormGradRuns, pairs ? kNormGradRowWarps / 2 : kNormGradRowWarps);
   // Two rows at a time leave room for fewer warps: where rows have so many that it makes no difference.
   const bool two = n.runs == 1 ? n.warps == 1 && n.split == 1
                                : dtype != IRIS_F32 && rows > 2 * kSms && norm_grad_warps(4) / n.warps * n.warps >= norm_grad_warps(2) / n.warps * n.warps;
@@ -613,15 +679,23 @@ static NormPlan norm_grad_plan(int64_t rows, int64_t columns, int dtype) {
   return n;
 }
 // Whether a group has more than kNormChain rows, and its sums their own part.
-static bool norm_by_group(const NormPlan& n, int64_t rows) { return rows > norm_grid(n, rows) * n.groups * kNormChain; }
-static int64_t norm_parts(const NormPlan& n, int64_t rows) { return norm_grid(n, rows) * (norm_by_group(n, rows) ? n.groups : 1); }
+static bool norm_by_group(const NormPlan& n, int64_t rows, int64_t grid) { return rows > grid * n.groups * kNormChain; }
+static int64_t norm_parts(const NormPlan& n, int64_t rows) {   // at most: a device may have fewer clusters at once, and more rows for each
+  const int64_t grid = norm_grid(n, rows, kSms / n.split);
+  return grid * (n.split > 1 || norm_by_group(n, rows, grid) ? n.groups : 1);
+}
 
-template <int DT, int PT, int R, int I, int MODE>
+template <int DT, int PT, int R, int I, int MODE, bool SPLIT = false>
 static int launch_norm(const NormParams& p, const NormPlan& n, cudaStream_t st) {
-  constexpr auto kernel = norm_kernel<DT, PT, R, I, MODE>;
+  if constexpr (!SPLIT && I == kNormRuns)   // as rows of several blocks have
+    if (n.split > 1) return launch_norm<DT, PT, R, I, MODE, true>(p, n, st);
+  constexpr auto kernel = norm_kernel<DT, PT, R, I, MODE, SPLIT>;
   constexpr int stages = norm_stages(DT, R * I) * R * Segment<DT, I>::kBytes, params = 2 * I * kWarpColumns * (int)sizeof(float);   // of a warp, of a warp of a row
-  IRIS_CHECK(allow_shared<kernel>(norm_warps(DT, R * I) * stages + kNormRowWarps * params));
-  return launch_rows(kernel, p, (unsigned)(norm_grid(n, p.rows) * n.split), n.split, n.warps * n.groups * 32,
+  constexpr int most = norm_warps(DT, R * I) * stages + kNormRowWarps * params;
+  int room;
+  IRIS_CHECK(allow_shared<kernel>(most));
+  IRIS_CHECK(clusters_at_once<kernel>(n.split, norm_warps(DT, R * I) * 32, most, &room));
+  return launch_rows(kernel, p, (unsigned)(norm_grid(n, p.rows, room) * n.split), n.split, n.warps * n.groups * 32,
                      (size_t)n.warps * (n.groups * stages + params), st);
 }
 template <int DT, int PT, int MODE>
@@ -636,26 +710,36 @@ template <int DT, int PT>
 static int launch_norm(const NormParams& p, const NormPlan& n, int mode, cudaStream_t st) {
   return mode == kAligned ? launch_norm<DT, PT, kAligned>(p, n, st) : mode == kSame ? launch_norm<DT, PT, kSame>(p, n, st) : launch_norm<DT, PT, kAny>(p, n, st);
 }
-template <int DT, int PT, int R, int I, int MODE>
-static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, cudaStream_t st) {
-  constexpr auto kernel = norm_grad_kernel<DT, PT, R, I, MODE>;
+template <int DT, int PT, int R, int I, int MODE, bool SPLIT = false>
+static int launch_norm_grad(NormGradParams p, const NormPlan& n, cudaStream_t st, int* parts) {
+  if constexpr (!SPLIT && I == kNormGradRuns)
+    if (n.split > 1) return launch_norm_grad<DT, PT, R, I, MODE, true>(p, n, st, parts);
+  constexpr auto kernel = norm_grad_kernel<DT, PT, R, I, MODE, SPLIT>;
   constexpr int stages = norm_grad_stages(DT) * norm_grad_stage_bytes<DT, R, I>(), params = I * kWarpColumns * (int)sizeof(float);   // of a warp, of a warp of a row
   static_assert(stages >= 2 * params, "the groups' sums take the place of the rows");
-  IRIS_CHECK(allow_shared<kernel>(norm_grad_warps(R * I) * (stages + params)));
-  return launch_rows(kernel, p, (unsigned)(norm_grid(n, p.rows) * n.split), n.split, n.warps * n.groups * 32, (size_t)n.warps * (n.groups * stages + params), st);
+  constexpr int most = norm_grad_warps(R * I) * (stages + params);
+  int room;
+  IRIS_CHECK(allow_shared<kernel>(most));
+  IRIS_CHECK(clusters_at_once<kernel>(n.split, norm_grad_warps(R * I) * 32, most, &room));
+  const int64_t grid = norm_grid(n, p.rows, room);
+  p.by_group = p.parts && norm_by_group(n, p.rows, grid);
+  *parts = (int)(grid * (p.by_group ? n.groups : 1));
+  return launch_rows(kernel, p, (unsigned)(grid * n.split), n.split, n.warps * n.groups * 32, (size_t)n.warps * (n.groups * stages + params), st);
 }
 template <int DT, int PT, int MODE>
-static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, cudaStream_t st) {
-  if (n.runs == 1) return launch_norm_grad<DT, PT, 2, 1, MODE>(p, n, st);
+static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, cudaStream_t st, int* parts) {
+  if (n.runs == 1) return launch_norm_grad<DT, PT, 2, 1, MODE>(p, n, st, parts);
   if constexpr (DT != IRIS_F32)
-    if (n.rows == 2) return launch_norm_grad<DT, PT, 2, 2, MODE>(p, n, st);
-  return launch_norm_grad<DT, PT, 1, 2, MODE>(p, n, st);
+    if (n.rows == 2) return launch_norm_grad<DT, PT, 2, 2, MODE>(p, n, st, parts);
+  return launch_norm_grad<DT, PT, 1, 2, MODE>(p, n, st, parts);
 }
 template <int DT, int PT>
 static int launch_norm_grad(const NormGradParams& p, const NormPlan& n, int mode, void* dweight, void* dbias, cudaStream_t st) {
-  IRIS_CHECK(mode == kAligned ? launch_norm_grad<DT, PT, kAligned>(p, n, st) : mode == kSame ? launch_norm_grad<DT, PT, kSame>(p, n, st) : launch_norm_grad<DT, PT, kAny>(p, n, st));
+  int parts = 0;
+  IRIS_CHECK(mode == kAligned ? launch_norm_grad<DT, PT, kAligned>(p, n, st, &parts) : mode == kSame ? launch_norm_grad<DT, PT, kSame>(p, n, st, &parts)
+                                                                                              : launch_norm_grad<DT, PT, kAny>(p, n, st, &parts));
   if (!p.parts) return IRIS_OK;
-  return launch_rows(norm_join_kernel<PT>, NormJoinParams{p.parts, (int)norm_parts(n, p.rows), p.dim, {dweight, dbias}}, (unsigned)((p.dim + 31) / 32 * 2), 1,
+  return launch_rows(norm_join_kernel<PT>, NormJoinParams{p.parts, parts, p.dim, {dweight, dbias}}, (unsigned)((p.dim + 31) / 32 * 2), 1,
                      kJoinWarps * 32, 0, st);
 }
 
@@ -751,7 +835,7 @@ extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void
   const NormPlan n = norm_grad_plan(a->rows, columns, a->dtype);
   NormGradParams p{static_cast<const char*>(a->x), static_cast<const char*>(a->dy), static_cast<char*>(a->dx), xs * es, gs * es, ds * es,
                    static_cast<const char*>(a->weight), a->stats, sums ? static_cast<float*>(a->workspace) : nullptr, a->rows, (int)a->dim, n.warps,
-                   n.split, period_of(xs * es), sums && norm_by_group(n, a->rows)};
+                   n.split, period_of(xs * es), 0};
   const bool wide = a->param_dtype == IRIS_F32;
   if (a->dtype == IRIS_BF16)
     return wide ? launch_norm_grad<IRIS_BF16, IRIS_F32>(p, n, mode, a->dweight, a->dbias, st) : launch_norm_grad<IRIS_BF16, IRIS_BF16>(p, n, mode, a->dweight, a->dbias, st);

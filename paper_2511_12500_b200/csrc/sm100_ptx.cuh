@@ -202,6 +202,10 @@ __device__ __forceinline__ void st_shared_cluster_u32(uint32_t cluster_addr, uin
 __device__ __forceinline__ void st_shared_cluster_u64(uint32_t cluster_addr, uint64_t v) {
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_addr), "l"(v) : "memory");
 }
+// 8 bytes to another CTA's shared memory, counted on an mbarrier there (both addresses from mapa).  Unlike a cluster barrier it waits for no other store.
+__device__ __forceinline__ void st_async_u64(uint32_t cluster_addr, uint64_t v, uint32_t bar_cluster_addr) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u64 [%0], %1, [%2];" ::"r"(cluster_addr), "l"(v), "r"(bar_cluster_addr) : "memory");
+}
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t dst_smem, uint32_t ncols) {
   asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(ncols) : "memory");
 }

@@ -246,6 +246,34 @@ def test_norm_of_many_rows():
     near(db, want_b, off_b, FP32)
 
 
+@pytest.mark.parametrize("n,dim,dtype,pad", [(700, 4200, BF16, 0), (600, 6001, FP16, 3), (500, 8192, FP32, 0), (700, 12008, BF16, 0), (400, 20001, BF16, 1), (310, 33000, FP16, 0),
+                                             (200, 65536, FP32, 0), (20000, 4104, BF16, 0), (9700, 8200, BF16, 0)])
+def test_norm_of_many_rows_of_several_blocks(n, dim, dtype, pad):
+    """Clusters whose groups take several rows each, the last two cases more than a chain of 128; twice the same bits."""
+    x, w, b = norm_inputs(n, dim, dtype, dtype, pad, 0, offset=1.0)
+    dy, _ = rows(n, dim, dtype, pad, 0, torch.rand(n, dim, device="cuda", generator=gen(2)) - 0.3)
+    stats = torch.empty(n, 2, device="cuda")
+    y, store = rows(n, dim, dtype, pad, 0)
+    got = []
+    for _ in range(2):
+        iris.iris_layer_norm(x, n, dim, KIND[dtype], y, weight=w, bias=b, param_dtype=KIND[dtype], stats=stats, row_stride=dim + pad, out_stride=dim + pad)
+        dx, dx_store = rows(n, dim, dtype, pad, 0)
+        dw, db = torch.empty(2, dim, device="cuda", dtype=dtype)
+        work = torch.empty(iris.iris_layer_norm_workspace_bytes(n, dim), dtype=torch.uint8, device="cuda").fill_(0xA5)
+        iris.iris_layer_norm_backward(x, n, dim, KIND[dtype], dy, stats, work, weight=w, param_dtype=KIND[dtype], dx=dx, dweight=dw, dbias=db,
+                                      row_stride=dim + pad, dy_stride=dim + pad, dx_stride=dim + pad)
+        got.append([t.clone() for t in (y, stats, dx, dw, db)])
+    assert all(bool((p == q).all()) for p, q in zip(*got)) and outside_kept(y, store, 0) and outside_kept(dx, dx_store, 0)
+    want, want_stats, off, off_stats = ref.norm(x, w, b, 1e-5)
+    near(y, want, off, dtype)
+    near(stats, want_stats, off_stats, FP32)
+    del want, off
+    want_x, want_w, want_b, off_x, off_w, off_b = ref.norm_grad(x, dy, w, stats)
+    near(dx, want_x, off_x, dtype)
+    near(dw, want_w, off_w, dtype)
+    near(db, want_b, off_b, dtype)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n,dim,pad", [(50, 1000, 0), (9, 4097, 3), (4, 20000, 8)])
 def test_norm_in_place(dtype, n, dim, pad):
