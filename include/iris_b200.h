@@ -576,8 +576,8 @@ int iris_distill_topk_backward(const iris_distill_args* args, void* stream);
  * Tokens drawn this way are distributed as if the target alone had drawn them.  Drawn by a race: the token with the largest weight / noise, the
  * lowest column among equals, so that with exponential noise (-ln of a uniform number) a token has its weight's probability.
  * A scale of +inf, or above 2e38, is greedy: p is 1 at the largest logit (the lowest column among equals), drafts are compared with it, and
- * uniform, noise and draft_logits are not read (with such a scale and no scales they may be NULL).  A row of target logits with nothing left, or with NaN or +inf, accepts nothing and its next token is
- * -1; a row of draft logits with NaN or +inf rejects its draft, and the next token is drawn from p. */
+ * uniform, noise and draft_logits do not matter (with such a scale and no scales they are not read and may be NULL).  A row of target
+ * logits with nothing left, or with NaN or +inf, accepts nothing and its next token is -1; a row of draft logits with NaN or +inf rejects its draft, and the next token is drawn from p. */
 typedef struct iris_verify_args {
   const void* logits;        /* [sequences * (drafts + 1)] rows: see "Common arguments"                              */
   int64_t sequences, vocab, row_stride;

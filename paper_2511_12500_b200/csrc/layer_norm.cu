@@ -12,7 +12,7 @@ namespace rows {
 
 constexpr int kNormRuns = 4, kNormGradRuns = 2;   // runs of 8 columns that a thread holds, of one row or of several short ones
 constexpr int kNormRowWarps = 8, kNormGradRowWarps = 16;   // of a row in a block, at most
-constexpr int kNormSplitGroups = 4;             // of a block in a cluster, at most
+constexpr int kNormSplitGroups = 4;             // of a block in a cluster, at most (a row has 5 of the block's 16 warps or more)
 constexpr int kNormSplit = 8;                   // blocks (one cluster) that share a row
 constexpr int64_t kNormMaxDim = (int64_t)kNormRuns * kWarpColumns * kNormRowWarps * kNormSplit;
 static_assert(kNormRuns * kNormRowWarps == kNormGradRuns * kNormGradRowWarps, "the same limit for both directions");
@@ -186,10 +186,11 @@ __device__ __forceinline__ float both(uint64_t x) {
 // R rows at a time.
 //
 // Statistics in one exchange among a row's warps: each sums the squares about its own mean, and means and squares' sums are joined (squares of the differences
-// of means, weighted by columns, come on top).  Long rows are read once and written once: 32768 x 4096 bf16 106 us, 5.1 TB/s.  With rows fetched ahead to
+// of means, weighted by columns, come on top).  Long rows are read once and written once: 32768 x 4096 bf16 102 us, 5.2 TB/s.  With rows fetched ahead to
 // shared memory nothing waits for memory long (1.0 warps an issue); what is left is chains of dependent instructions, shuffles and barriers at 16 warps an SM, so
-// the rows in work count: 4104 columns, whose fifth warp has 8 of them, take 71 us for 16001 rows, 4096 columns 57; rows of 4096 that begin at
-// any element 96.  Held in registers one row ahead instead of copied ahead: 244; parameters read from L1 instead of shared memory: 212; one row at a time 110.
+// the rows in work count: 4104 columns, whose fifth warp has 8 of them, take 69 us for 16001 rows, 4096 columns 52; rows of 4096 that begin at
+// any element 90.  Held in registers one row ahead instead of copied ahead: 244; parameters read from L1 instead of shared memory: 212; one row at a time 110.
+// Rows of more than 8192 columns are shared by a cluster (SPLIT): 4096 x 16384 77 us; 111 with a cluster's barrier in every turn and one group of 8 warps a block.
 template <int DT, int PT, int R, int I, int MODE, bool SPLIT>
 __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const NormParams p) {
   using C = Columns<DT>;
@@ -310,7 +311,7 @@ __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const 
         for (int q = 0; q < R; ++q) {
           const float2* const of = group.of(shared, count & 1, q);
           float m = lost, s = 0.f;
-          if (SPLIT && group.all() > 16) {   // a lane takes a warp, or a few
+          if (SPLIT && group.all() > 16) {   // a lane takes a warp, or a few (1024 x 65536: 200 us instead of 367; at 16 warps the same within 5 %)
             for (int w = group.lane; w < group.all(); w += 32) m = fmaf(of[w].x, shares.of(w), m);
             mean[q] = warp_sum(m) / shares.dim;
             for (int w = group.lane; w < group.all(); w += 32) {

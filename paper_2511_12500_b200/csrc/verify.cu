@@ -446,7 +446,7 @@ static int launch_verify(VerifyParams p, const iris_verify_args* a, cudaStream_t
     while (split < kVerifySplit && rows * split * 2 <= kSms * 4 && granules > (int64_t)split * least) split *= 2;
     p.split = split;
     p.each = part_granules(a->logits, p.stride, p.vocab, a->dtype, split);
-    p.draft_each = a->draft_logits ? part_granules(a->draft_logits, p.draft_stride, p.vocab, a->dtype, split) : 0;
+    p.draft_each = p.draft_logits ? part_granules(a->draft_logits, p.draft_stride, p.vocab, a->dtype, split) : 0;
   };
   const int64_t rows = (int64_t)p.sequences * (p.drafts + 1 + (p.draft_logits ? p.drafts : 0));
   share(rows, 512);
@@ -493,7 +493,7 @@ extern "C" int iris_verify_drafts(const iris_verify_args* a, void* stream) {
   if (a->workspace_bytes < need) return fail(IRIS_ERR_ARG, "%s: workspace has %zu bytes, the call needs %zu", fn, a->workspace_bytes, need);
   VerifyParams p{};
   p.logits = a->logits;
-  p.draft_logits = draft ? a->draft_logits : nullptr;
+  p.draft_logits = draft && !greedy ? a->draft_logits : nullptr;   // greedy drafts are compared with the target's largest logit only
   p.stride = stride;
   p.draft_stride = dstride;
   p.sequences = (int)a->sequences;
