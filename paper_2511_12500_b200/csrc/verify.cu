@@ -209,8 +209,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_rows_kernel(const __
   }
 }
 
-__device__ __forceinline__ double prob(float z, float m, float s, float scale) {
-  return z == -INFINITY ? 0. : exp(((double)z - (double)m) * (double)scale) / (double)s;
+__device__ __forceinline__ double prob(float z, float m, float s, float scale) {   // NaN in a row without a distribution, for masked tokens too
+  return s != s ? (double)s : z == -INFINITY ? 0. : exp(((double)z - (double)m) * (double)scale) / (double)s;
 }
 // Whether a draft is accepted: in 32 bits, and in 64 where that is too near to tell (or NaN).
 __device__ __forceinline__ bool accepts(const Seat& s, float u, bool with_q, float scale) {
