@@ -228,6 +228,11 @@ __device__ __forceinline__ float reciprocal(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// p - q counts as nothing up to so much of p.  The rows' sums are of 32 bits.  A term's exponent is rounded twice and up to 24 + 17 large on average (the slack
+// of the reference that it is counted from, and what a row of 128000 columns has): 41 ln 2 2^-23; counting it from another reference 24 ln 2 2^-23; the
+// exponential 2^-22; chains of at most 128 equal terms that round to one side 2^-20: together below 2^-17.  So two rows that are the same but lie unlike
+// in 16 bytes, and are summed in other orders, leave less than 2^-16 of p.
+constexpr float kNothing = 1.f / (1 << 16);
 struct Runner {   // of the race; column -1: none
   float score;
   int column;
@@ -347,7 +352,10 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draw_kernel(const __
         if (with_q) {
           E::unpack(yr[0], y);
 #pragma unroll
-          for (int u = 0; u < VE; ++u) x[u] = fmaf(ex2((y[u] - mq) * k), -rsq, x[u]);
+          for (int u = 0; u < VE; ++u) {   // rounded like p, so that equal rows leave nothing
+            const float left = __fsub_rn(x[u], __fmul_rn(ex2((y[u] - mq) * k), rsq));
+            x[u] = left > x[u] * kNothing ? left : 0.f;
+          }
         }
         if ((uint32_t)(without - c) < (uint32_t)VE) {
 #pragma unroll
@@ -371,8 +379,11 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draw_kernel(const __
       }
       const auto exactly = [&](int c) {
         double w = prob(E::to(row.column(c)), seat.m, seat.s, scale);
-        if (with_q) w -= prob(E::to(draft_row.column(c)), seat.mq, seat.sq, scale);
-        return (w > 0. ? w : 0.) / (double)p.noise[(int64_t)b * p.vocab + c];
+        if (with_q) {
+          const double left = w - prob(E::to(draft_row.column(c)), seat.mq, seat.sq, scale);
+          w = left > w * kNothing ? left : 0.;
+        }
+        return w > 0. ? w / (double)p.noise[(int64_t)b * p.vocab + c] : 0.;
       };
       // The block's: its threads whose scores are near the best; if there are several, their exact scores decide, and the lowest column of equal ones.
       const float of_this = warp_max(score);
