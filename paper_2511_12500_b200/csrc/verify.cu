@@ -233,18 +233,21 @@ __device__ __forceinline__ float reciprocal(float x) {
 // exponential 2^-22; chains of at most 128 equal terms that round to one side 2^-20: together below 2^-17.  So two rows that are the same but lie unlike
 // in 16 bytes, and are summed in other orders, leave less than 2^-16 of p.
 constexpr float kNothing = 1.f / (1 << 16);
-struct Runner {   // of the race; column -1: none
-  float score;
+// How far, relative to p, a weight may be off in 32 bits: an exponent is at most 126 (below that the exponential is 0) and rounded four times (difference,
+// scale's logarithm twice, product), 126 ln 2 2^-22 < 2^-15 of p with the exponential's and the sum's own 2^-22, and the same again for q <= p.
+constexpr float kOff = 1.f / (1 << 14);
+struct Runner {   // of the race: a column (-1: none) and between which bounds its score lies
+  float low, high;
   int column;
 };
-// The winner among n runners, which all threads of the warp get: n <= 32, thread i has runner i.  Those whose scores are too near one another for 32
-// bits are compared in 64 (`exactly`: the score of a column); the lowest column among equal ones.
+// The winner's column among n runners, which all threads of the warp get: n <= 32, thread i has runner i.  Those that may be the best by their bounds are
+// compared in 64 bits (`exactly`: the score of a column); the lowest column among equal ones; -1: none.
 template <class F>
-__device__ __forceinline__ Runner winner(Runner r, F exactly) {
-  const float best = warp_max(r.column >= 0 ? r.score : -1.f);
-  const uint32_t near = __ballot_sync(~0u, r.column >= 0 && !(r.score < best * (1.f - 1e-4f)));
-  if (!near) return Runner{0.f, -1};
-  double score = r.score;
+__device__ __forceinline__ int winner(Runner r, F exactly) {
+  const float least = warp_max(r.column >= 0 ? r.low : 0.f);
+  const uint32_t near = __ballot_sync(~0u, r.column >= 0 && r.high >= least);
+  if (!near) return -1;
+  double score = 0.;
   if (near & (near - 1)) score = near >> (threadIdx.x & 31) & 1 ? exactly(r.column) : 0.;
   int at = __ffs(near) - 1;
   for (uint32_t rest = near & (near - 1); rest; rest &= rest - 1) {
@@ -253,7 +256,7 @@ __device__ __forceinline__ Runner winner(Runner r, F exactly) {
     const int ca = __shfl_sync(~0u, r.column, at), cb = __shfl_sync(~0u, r.column, i);
     if (b > a || (b == a && cb < ca)) at = i;
   }
-  return Runner{__shfl_sync(~0u, r.score, at), __shfl_sync(~0u, r.column, at)};
+  return __shfl_sync(~0u, r.column, at);
 }
 
 // One cluster of `split` blocks a sequence: accepts drafts up to the first that is refused, and draws the token behind them.
@@ -268,7 +271,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draw_kernel(const __
   __shared__ Runner block_best, parts[2][kVerifySplit];   // parts: of the cluster's blocks, of the first and the second race
   __shared__ float of_warp[kVerifyWarps];
   __shared__ unsigned long long exact_best;
-  __shared__ int lowest;
+  __shared__ int lowest, bound, runners;
   static_assert(kVerifySplit <= 32, "one a thread");
   __shared__ int stop_at;
   const int split = p.split, rank = split > 1 ? (int)ptx::cluster_ctarank() : 0, tid = threadIdx.x, lane = tid & 31;
@@ -311,10 +314,10 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draw_kernel(const __
       const int without = rest && !p.draft_logits ? (int)ids[stop] : -1;
       const Row<DT> draft_row(p.draft_logits, with_q ? (int64_t)b * n + stop : 0, p.draft_stride, p.vocab);
       const char* const draft = reinterpret_cast<const char*>(draft_row.granule0 + draft_row.ph);
-      const float rs = 1.f / seat.s, rsq = with_q ? 1.f / seat.sq : 0.f, mq = with_q ? seat.mq : 0.f;
+      const float rs = (1.f + kOff) / seat.s, rsq = with_q ? 1.f / seat.sq : 0.f, mq = with_q ? seat.mq : 0.f;
       const uint32_t aq = phase(draft - (int64_t)row.ph * ES), ae = phase(noise - (int64_t)row.ph * 4);   // of every granule
-      // The scores of granule v: max(0, weight) / noise.
-      const auto scores = [&](int v, float (&x)[VE]) {
+      // The most that the scores of granule v may be, max(0, weight) / noise with p taken kOff too large, and the least: 0 where the weight may be nothing.
+      const auto scores = [&](int v, float (&x)[VE], float (&low)[VE]) {
         const int c = v * VE - row.ph;
         uint4 zr[1], yr[1], e[VE / 4];
         if (c >= VE && c + 2 * VE <= p.vocab) {
@@ -348,30 +351,35 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draw_kernel(const __
           f[4 * h] = __uint_as_float(e[h].x), f[4 * h + 1] = __uint_as_float(e[h].y), f[4 * h + 2] = __uint_as_float(e[h].z), f[4 * h + 3] = __uint_as_float(e[h].w);
         }
 #pragma unroll
-        for (int u = 0; u < VE; ++u) x[u] = ex2((z[u] - seat.m) * k) * rs;
+        for (int u = 0; u < VE; ++u) {
+          x[u] = ex2((z[u] - seat.m) * k) * rs;
+          low[u] = x[u] * -(2.f * kOff + kNothing);
+        }
         if (with_q) {
           E::unpack(yr[0], y);
 #pragma unroll
-          for (int u = 0; u < VE; ++u) {   // rounded like p, so that equal rows leave nothing
-            const float left = __fsub_rn(x[u], __fmul_rn(ex2((y[u] - mq) * k), rsq));
-            x[u] = left > x[u] * kNothing ? left : 0.f;
-          }
+          for (int u = 0; u < VE; ++u) x[u] = fmaf(ex2((y[u] - mq) * k), -rsq, x[u]);
         }
         if ((uint32_t)(without - c) < (uint32_t)VE) {
 #pragma unroll
           for (int u = 0; u < VE; ++u) x[u] = c + u == without ? 0.f : x[u];
         }
 #pragma unroll
-        for (int u = 0; u < VE; ++u) x[u] = fmaxf(x[u], 0.f) * reciprocal(f[u]);
+        for (int u = 0; u < VE; ++u) {
+          const float by = reciprocal(f[u]);
+          low[u] = fmaxf(x[u] + low[u], 0.f) * by;
+          x[u] = fmaxf(x[u], 0.f) * by;
+        }
       };
-      // The thread's best score and the first of its granules that has it (NaN is no score).
-      float score = 0.f;
+      // The thread's best score, the first of its granules that has it, and the best of the others (NaN is no score).
+      float score = 0.f, second = 0.f;
       int at = -1;
       for (int v = part.v0 + tid; v < part.v1; v += T) {
-        float x[VE], m = 0.f;
-        scores(v, x);
+        float x[VE], low[VE], m = 0.f;
+        scores(v, x, low);
 #pragma unroll
         for (int u = 0; u < VE; ++u) m = fmaxf(m, x[u]);
+        second = fmaxf(second, fminf(m, score));
         if (m > score) {
           score = m;
           at = v;
@@ -385,52 +393,91 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draw_kernel(const __
         }
         return w > 0. ? w / (double)p.noise[(int64_t)b * p.vocab + c] : 0.;
       };
-      // The block's: its threads whose scores are near the best; if there are several, their exact scores decide, and the lowest column of equal ones.
+      // The block's: all columns that may be the best are at least as good, at most, as the best thread's is at least.  If there are several (or that is 0,
+      // and it may be nothing), their 64-bit scores decide, and the lowest column of equal ones.
       const float of_this = warp_max(score);
       if (lane == 0) of_warp[tid >> 5] = of_this;
       if (tid == 0) {
-        block_best = Runner{0.f, -1};
+        block_best = Runner{0.f, 0.f, -1};
         exact_best = 0;
         lowest = INT32_MAX;
+        bound = runners = 0;
       }
       __syncthreads();
       const float top = warp_max(of_warp[lane & (kVerifyWarps - 1)]);
-      const bool near = at >= 0 && !(score < top * (1.f - 1e-4f));
-      int column = 0;
-      if (near) {
-        float x[VE];
-        scores(at, x);
-        float m = 0.f;
+      // Threads that are not far behind look at their granule again for the bound, all together, and count their columns that reach their own.  Then, if
+      // several threads or columns are near (or one that was far), each compares its own in 64 bits, in all of its granules if others may be near too.
+      Runner mine{0.f, 0.f, -1};
+      double exact = 0.;
+      float least = 0.f;
+      bool looks = at >= 0 && score >= top * 0.5f, all = false, several = false;
+#pragma unroll 1
+      for (int look = 0; look < 2; ++look) {
+        int n_mine = looks ? 0 : 2;
+        if (looks)
+#pragma unroll 1
+          for (int v = all ? part.v0 + tid : at; v < part.v1; v += T) {
+            float x[VE], low[VE], m = 0.f;
+            scores(v, x, low);
 #pragma unroll
-        for (int u = VE - 1; u >= 0; --u)
-          if (x[u] >= m && x[u] > 0.f) {
-            m = x[u];
-            column = at * VE - row.ph + u;
+            for (int u = 0; u < VE; ++u) m = fmaxf(m, low[u]);
+            if (look == 0) {
+              least = m;
+              atomicMax(&bound, __float_as_int(m));
+            }
+            uint32_t rest = 0;
+#pragma unroll
+            for (int u = VE - 1; u >= 0; --u)
+              if (x[u] >= least && x[u] > 0.f) {
+                rest |= 1u << u;
+                if (look == 0) mine = Runner{low[u], x[u], v * VE - row.ph + u};
+              }
+            n_mine += __popc(rest);
+            if (look)
+#pragma unroll 1
+              for (; rest; rest &= rest - 1) {
+                const int c = v * VE - row.ph + __ffs(rest) - 1;
+                const double e = exactly(c);
+                if (e > exact) {
+                  exact = e;
+                  mine = Runner{__double2float_rd(e), __double2float_ru(e), c};
+                }
+              }
+            if (!all) break;
           }
+        if (look) break;
+        __syncthreads();
+        least = __int_as_float(bound);
+        looks = at >= 0 && score >= least;   // from here on: is near
+        all = second >= least;
+        if (looks) atomicAdd(&runners, all ? 2 : n_mine);
+        __syncthreads();
+        several = runners > 1;
+        if (!looks || several) mine.column = -1;
+        if (!several) break;
       }
-      const bool several = __syncthreads_count(near) > 1;
-      unsigned long long exact = 0;
       if (several) {
-        if (near) {
-          exact = (unsigned long long)__double_as_longlong(exactly(column));   // of numbers that are not negative the larger has the larger bits
-          atomicMax(&exact_best, exact);
-        }
+        if (mine.column >= 0) atomicMax(&exact_best, (unsigned long long)__double_as_longlong(exact));   // of positive numbers the larger has the larger bits
         __syncthreads();
-        if (near && exact == exact_best) atomicMin(&lowest, column);
+        if (mine.column >= 0 && (unsigned long long)__double_as_longlong(exact) == exact_best) atomicMin(&lowest, mine.column);
         __syncthreads();
+        if (mine.column == lowest) block_best = mine;
+      } else if (mine.column >= 0) {
+        block_best = mine;
       }
-      if (near && (!several || (exact == exact_best && column == lowest))) block_best = Runner{score, column};
       __syncthreads();
-      Runner best = block_best;
+      const Runner best = block_best;
+      next = best.column;
       if (split > 1) {
         if (tid < split) {
           const uint32_t to = ptx::mapa(ptx::smem_u32(&parts[race][rank]), tid);
-          ptx::st_shared_cluster_u64(to, (uint64_t)(uint32_t)best.column << 32 | __float_as_uint(best.score));
+          ptx::st_shared_cluster_u32(to, __float_as_uint(best.low));
+          ptx::st_shared_cluster_u32(to + 4, __float_as_uint(best.high));
+          ptx::st_shared_cluster_u32(to + 8, (uint32_t)best.column);
         }
         ptx::cluster_sync();
-        best = winner(lane < split ? parts[race][lane] : Runner{0.f, -1}, exactly);
+        next = winner(lane < split ? parts[race][lane] : Runner{0.f, 0.f, -1}, exactly);
       }
-      next = best.column;
       if (next >= 0) break;   // all blocks of the cluster
       __syncthreads();
     }
