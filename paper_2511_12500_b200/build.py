@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "lib", "libiris_b200.so")
 SOURCES = ["heap.cu", "tile_ops.cu", "gemm_all_scatter.cu", "consumer.cu", "token_logprobs.cu", "distill.cu", "verify.cu", "embed.cu", "layer_norm.cu"]
-HEADERS = ["iris_internal.h", "iris_device.cuh", "sm100_ptx.cuh", "logit_rows.cuh", "logit_grad.cuh", "top_list.cuh", "any_rows.cuh"]
+HEADERS = ["iris_internal.h", "iris_device.cuh", "sm100_ptx.cuh", "logit_rows.cuh", "logit_grad.cuh", "top_list.cuh", "any_rows.cuh", "norm_rows.h"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-O3", "-lineinfo", "-Xcompiler", "-fPIC",
               "-Xptxas", "-v", "--expt-relaxed-constexpr"]
 

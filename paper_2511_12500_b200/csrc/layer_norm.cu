@@ -6,6 +6,7 @@
 // A row is held in registers by a group of warps, 8 columns a thread and a few such runs, and where that is not enough by a cluster of blocks.
 // Blocks stay and take rows in turn; the next ones are under way to shared memory meanwhile.
 #include "any_rows.cuh"
+#include "norm_rows.h"
 
 namespace iris {
 namespace rows {
@@ -131,18 +132,15 @@ struct Shares {
   }
   __device__ __forceinline__ float of(int warp) const { return (warp < last ? each : warp == last ? rest : 0.f) - (warp == 0 ? none : 0.f); }
 };
-// The rows of a group.  SAME (mode kSame): those of a block begin at the same place of 16 bytes (`ph`, in bytes): every `period`-th row, one set of them a block.
-// Columns are then counted from there, `none` are not the row's, and rows are addressed so.
-struct Rows {
-  int64_t first, each, step;   // the group's first row, between rows taken at once, between those and the next ones
+// The rows of a group.  SAME (mode kSame): those of a block begin at the same place of 16 bytes (`ph`, in bytes).  Columns are then counted from there, `none`
+// are not the row's, and rows are addressed so.
+struct Rows : NormWalk {
   int ph, none;
   template <bool SAME, int R>
   static __device__ __forceinline__ Rows of(const Group& group, int groups, int period_, const char* base, int64_t stride, int es) {
-    const int64_t block = blockIdx.x / group.split, blocks = gridDim.x / group.split, period = SAME ? period_ : 1, set = SAME ? block % period : 0;
+    const int64_t block = blockIdx.x / group.split, blocks = gridDim.x / group.split, period = SAME ? period_ : 1, set = norm_set(block, period);
     Rows r;
-    r.first = set + period * ((SAME ? block / period : block) * groups + group.index) * R;
-    r.each = period;
-    r.step = period * (SAME ? (blocks - set + period - 1) / period : blocks) * groups * R;
+    static_cast<NormWalk&>(r) = norm_walk(block, blocks, group.index, groups, period, set, R);
     r.ph = SAME ? (int)phase(base + set * stride) : 0;
     r.none = r.ph / es;
     return r;
@@ -636,11 +634,7 @@ static void plan_groups(NormPlan& n, int64_t rows, int warps) {   // warps: of a
   const int64_t each = (rows * n.split + (int64_t)kSms * n.rows - 1) / ((int64_t)kSms * n.rows);   // few rows are spread over the SMs
   if (n.groups > each) n.groups = each < 1 ? 1 : (int)each;
 }
-constexpr int kNormPeriod = 8;   // places of 16 bytes where a row may begin
-static int64_t norm_grid(const NormPlan& n, int64_t rows, int64_t room) {   // clusters, of which there are `room` at once; at least a block for each place where a row begins
-  const int64_t each = (int64_t)n.groups * n.rows, full = (rows + each - 1) / each, most = rows < kNormPeriod ? rows : kNormPeriod;
-  return full < most ? most : full < room ? full : room;
-}
+static int64_t norm_grid(const NormPlan& n, int64_t rows, int64_t room) { return norm_grid(n.groups, n.rows, rows, room); }
 // Whether the rows of two matrices lie alike in 16 bytes.
 static bool lie_alike(const void* a, int64_t a_stride, const void* b, int64_t b_stride) {
   return (reinterpret_cast<uintptr_t>(a) - reinterpret_cast<uintptr_t>(b)) % 16 == 0 && (a_stride - b_stride) % 16 == 0;
