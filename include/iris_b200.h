@@ -679,6 +679,15 @@ typedef struct iris_layer_norm_grad_args {
 int iris_layer_norm_backward(const iris_layer_norm_grad_args* args, void* stream);
 size_t iris_layer_norm_workspace_bytes(int64_t rows, int64_t dim);
 
+/* Rows of more than 8192 columns (4096 in the gradient) are shared by blocks that run at the same time and wait for one another's sums.  A wait is limited, to
+ * 2^18 looks (about a second).  If one runs out, y (dx) is NaN from that row on in the columns of the threads that gave up, and the wait is recorded on its
+ * device; dweight and dbias do not hang on it.  iris_layer_norm_status waits for `stream`, reads the current device's record and clears it: IRIS_OK, or
+ * IRIS_ERR_TIMEOUT with detail[0..7], if not NULL, as iris_status_check gives it.  Not while a stream is captured. */
+int iris_layer_norm_status(void* stream, int32_t* detail);
+/* on != 0: in later calls of this process such blocks keep their sums to themselves, and every wait runs out, after 16 looks (to test what a caller does
+ * then).  0: as above. */
+void iris_layer_norm_withhold(int on);
+
 #ifdef __cplusplus
 }
 #endif

@@ -44,6 +44,7 @@ EXPORTS = [
     "iris_token_logprobs", "iris_token_logprobs_backward", "iris_distill_topk", "iris_distill_topk_backward",
     "iris_verify_drafts", "iris_verify_workspace_bytes", "iris_embed_tokens", "iris_embed_tokens_backward", "iris_embed_workspace_bytes",
     "iris_layer_norm", "iris_layer_norm_backward", "iris_layer_norm_workspace_bytes",
+    "iris_layer_norm_status", "iris_layer_norm_withhold",
 ]
 
 
@@ -150,6 +151,8 @@ def lib() -> C.CDLL:
     L.iris_verify_workspace_bytes.argtypes, L.iris_verify_workspace_bytes.restype = [i64, ci], sz
     L.iris_embed_workspace_bytes.argtypes, L.iris_embed_workspace_bytes.restype = [i64, i64, i64], sz
     L.iris_layer_norm_workspace_bytes.argtypes, L.iris_layer_norm_workspace_bytes.restype = [i64, i64], sz
+    L.iris_layer_norm_status.argtypes = [vp, C.POINTER(i32)]
+    L.iris_layer_norm_withhold.argtypes, L.iris_layer_norm_withhold.restype = [ci], None
     _lib = L
     return L
 
@@ -283,7 +286,10 @@ def iris_translate(heap: int, ptr: int, from_rank: int, to_rank: int) -> int:
 def iris_status_check(heap: int, stream=None):
     """Synchronise and raise IrisError(IRIS_ERR_TIMEOUT) if a device-side wait expired."""
     detail = (C.c_int32 * 8)()
-    rc = lib().iris_status_check(heap, _stream(stream), detail)
+    _ck_detail(lib().iris_status_check(heap, _stream(stream), detail), detail)
+
+
+def _ck_detail(rc, detail):
     if rc != IRIS_OK:
         e = IrisError(rc, iris_last_error())
         e.detail = list(detail)
@@ -703,3 +709,13 @@ def iris_layer_norm_backward(x, rows, dim, dtype, dy, stats, workspace=None, wei
                                         _stream(stream))
     if rc:
         _ck(rc)
+
+
+def iris_layer_norm_status(stream=None):
+    """Synchronise and raise IrisError(IRIS_ERR_TIMEOUT) if blocks that share a row waited for one another in vain."""
+    detail = (C.c_int32 * 8)()
+    _ck_detail(lib().iris_layer_norm_status(_stream(stream), detail), detail)
+
+
+def iris_layer_norm_withhold(on):
+    lib().iris_layer_norm_withhold(bool(on))

@@ -16,7 +16,7 @@ constexpr int kStatusWords = 8;               // {code, kernel, block, tile, slo
 constexpr uint64_t kDefaultTimeoutNs = 2000000000ull;
 
 // Kernel ids recorded in the status block.
-enum { KID_GEMM = 1, KID_SCATTER = 2, KID_CONSUMER = 3, KID_ALLSTORE = 4 };
+enum { KID_GEMM = 1, KID_SCATTER = 2, KID_CONSUMER = 3, KID_ALLSTORE = 4, KID_NORM = 5 };
 
 // The table every kernel receives by value: the B200 form of the paper's `heap_bases` tensor
 // (Section 3.3: 64 bytes at W = 8; here it sits in constant-bank kernel parameters).

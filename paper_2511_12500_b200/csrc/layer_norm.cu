@@ -23,7 +23,13 @@ constexpr int norm_warps(int dtype, int rows_runs) { return dtype == IRIS_F32 ||
 constexpr int norm_stages(int dtype, int rows_runs) { return dtype == IRIS_F32 || rows_runs > 4 ? 2 : 3; }
 constexpr int norm_grad_warps(int rows_runs) { return rows_runs > 2 ? 12 : 16; }
 constexpr int norm_grad_stages(int dtype) { return dtype == IRIS_F32 ? 2 : 3; }
-constexpr uint64_t kNormWait = 1000000000;      // ns for another block's values, after which they are taken for lost
+// Another block's values are taken for lost after so many looks, of 4 us at most each (a second in all; looks are counted, as a clock runs on while the kernel is
+// off the GPU).  sends: to how many blocks a warp sends its values.
+struct NormPatience {
+  uint32_t looks, sends;
+};
+constexpr uint32_t kNormLooks = 1 << 18;
+__device__ int32_t norm_status[kStatusWords];   // the first wait that ran out on the device, as the status block of a heap has it
 constexpr int kNormChain = 128;                 // rows that a thread adds up before the sum goes to the sum of such sums
 
 // How rows lie: all at 16 bytes, and their lengths multiples of that; those of all matrices alike, at any places of 16 bytes; anyhow.
@@ -39,6 +45,7 @@ struct NormParams {
   int dim, warps, split;        // warps: of a row in one block
   int period;                   // kSame: rows that far apart begin at the same place of 16 bytes
   float eps;
+  NormPatience patience;
 };
 
 struct NormGradParams {
@@ -50,11 +57,13 @@ struct NormGradParams {
   float* parts;                 // [blocks / split (times groups if by_group), 2, dim]: sums of dy h and of dy; nullptr: not wanted
   int64_t rows;
   int dim, warps, split, period, by_group;   // by_group: of norm_by_group
+  NormPatience patience;
 };
 
 // What a warp knows of a row, and the sum over the warps of a row, which all of its threads get.
 struct NormShared {
   uint64_t arrived[kNormSplitGroups][2];   // of a group's values in a cluster, one for each half
+  int lost[kNormGradRowWarps];             // of a warp: its wait has run out
   float2 of[2][kNormRows][kNormGradRowWarps * kNormSplit];   // twice: one is read while the next rows' is written
 };
 struct Group {
@@ -70,6 +79,7 @@ struct Group {
   template <int R>
   __device__ __forceinline__ void prepare(NormShared& s) const {
     if (split == 1) return;
+    if (lane == 0) s.lost[threadIdx.x >> 5] = 0;
     if (warp == rank * warps && lane == 0) {
       for (int h = 0; h < 2; ++h) {
         ptx::mbar_init(ptx::smem_u32(&s.arrived[index][h]), 1);
@@ -84,29 +94,41 @@ struct Group {
     __syncwarp();
     if (split > 1) ptx::cluster_sync();
   }
-  // Every warp of the rows puts its values into a half of the shared memory (the halves in turn) and waits for the others'.  `lost`
-  // becomes NaN, and stays it, where they have not come within a second (the rows are NaN from then on).
+  // In the end: a wait that ran out is recorded.  Values may still be on their way to this block, which is to outlive them: about a second.
+  __device__ __forceinline__ void report_lost(const NormShared& s) const {
+    __syncwarp();
+    if (!*reinterpret_cast<const volatile int*>(&s.lost[threadIdx.x >> 5])) return;
+    if (lane == 0) report_timeout(norm_status, KID_NORM, index, warp, 0, 0);
+#pragma unroll 1
+    for (int i = 0; i < 1000000; ++i) __nanosleep(1000);
+  }
+  // Every warp of the rows puts its values into a half of the shared memory (the halves in turn) and waits for the others'.  `lost` becomes NaN, and stays it,
+  // for a thread that has not seen them come: its columns are NaN from then on.  It sends nothing more and prepares nothing, so that the others give up in turn
+  // and no mbarrier is used out of step.
   //
   // In a cluster the values count themselves on the mbarrier of the block that they go to.  A barrier of the cluster would wait for
   // the stores of the row before as well.  A warp writes to a half again when all values of the exchange after have come, which each warp
   // sends when it has read that half; for the same reason one thread may prepare the mbarrier for its next use as soon as it has seen the values come.
   template <int R>
-  __device__ __forceinline__ void exchange(NormShared& s, uint32_t count, const float (&a)[R], const float (&b)[R], float& lost) const {
+  __device__ __forceinline__ void exchange(NormShared& s, uint32_t count, const float (&a)[R], const float (&b)[R], float& lost, const NormPatience& patience) const {
     static_assert(R <= kNormRows, "room for them");
     const uint32_t turn = count & 1;
     if (split > 1) {
       const uint32_t bar = ptx::smem_u32(&s.arrived[index][turn]), parity = count >> 1 & 1;
-      if (lane < split) {
+      if (lane < patience.sends && lost == 0.f) {
 #pragma unroll
         for (int q = 0; q < R; ++q) ptx::st_async_u64(ptx::mapa(ptx::smem_u32(&s.of[turn][q][index * all() + warp]), lane), pair(a[q], b[q]), ptx::mapa(bar, lane));
       }
       if (!ptx::mbar_try_wait_cluster(bar, parity)) {
-        const uint64_t start = globaltimer_ns();
+        uint32_t looks = 1;
         while (lost == 0.f && !ptx::mbar_try_wait_cluster(bar, parity))
-          if (globaltimer_ns() - start > kNormWait) lost = NAN;
+          if (++looks >= patience.looks) {
+            lost = NAN;
+            *reinterpret_cast<volatile int*>(&s.lost[threadIdx.x >> 5]) = 1;
+          }
       }
       __syncwarp();
-      if (warp == rank * warps && lane == 0) ptx::mbar_arrive_expect_tx(bar, all() * R * 8);
+      if (warp == rank * warps && lane == 0 && lost == 0.f) ptx::mbar_arrive_expect_tx(bar, all() * R * 8);
     } else {
       if (lane == 0) {
 #pragma unroll
@@ -304,7 +326,7 @@ __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const 
     for (int q = 0; q < R; ++q) squares[q] = warp_sum(squares[q]);
     if constexpr (R <= kNormRows)
       if (group.all() > 1) {
-        group.exchange(shared, count, mean, squares, lost);
+        group.exchange(shared, count, mean, squares, lost, p.patience);
 #pragma unroll
         for (int q = 0; q < R; ++q) {
           const float2* const of = group.of(shared, count & 1, q);
@@ -358,6 +380,7 @@ __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const 
       else G::write(here + q * G::kBytes, y_row + q * rows.each * p.y_stride, begin, dim, out);
     }
   }
+  if (SPLIT) group.report_lost(shared);
   group.finish();
 }
 
@@ -510,7 +533,7 @@ __global__ void __launch_bounds__(norm_grad_warps(R * I) * 32) norm_grad_kernel(
       b[q] = warp_sum(both(b2[q]));
     }
     if (group.all() > 1) {
-      group.exchange(shared, count, a, b, lost);
+      group.exchange(shared, count, a, b, lost, p.patience);
 #pragma unroll
       for (int q = 0; q < R; ++q) {
         const float2* const of = group.of(shared, count & 1, q);
@@ -549,11 +572,14 @@ __global__ void __launch_bounds__(norm_grad_warps(R * I) * 32) norm_grad_kernel(
     }
   }
   ptx::let_next_begin();
-  group.finish();
-  if (!p.parts) return;
+  const auto end = [&] {   // behind the parts: between the rows and them it costs registers (8192 x 8192: 101 us instead of 97)
+    if (SPLIT) group.report_lost(shared);
+    group.finish();
+  };
+  if (!p.parts) return end();
   if (p.by_group || groups == 1) {
     put(more);
-    return;
+    return end();
   }
   // The groups' sums, through the ring: [groups, 2, columns].
   __syncthreads();
@@ -579,6 +605,7 @@ __global__ void __launch_bounds__(norm_grad_warps(R * I) * 32) norm_grad_kernel(
     part[from + c] = w;
     part[p.dim + from + c] = b;
   }
+  end();
 }
 
 // dw and db: the sums of `n` parts.  32 columns a block, its warps take parts in turn, eight loads of a thread under way (148 parts of 4096 columns: 6 us,
@@ -617,6 +644,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) norm_join_kernel(const NormJo
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
+static std::atomic<bool> norm_withhold{false};
+static NormPatience norm_patience(int split) { return norm_withhold.load() ? NormPatience{16, 0} : NormPatience{kNormLooks, (uint32_t)split}; }
 struct NormPlan {
   int split, warps, runs, rows, groups;   // rows: at a time (several only of one run, or of two); groups: of a block
 };
@@ -774,7 +803,7 @@ extern "C" int iris_layer_norm(const iris_layer_norm_args* a, void* stream) {
   const int mode = norm_mode(a->x, xs * es, lie_alike(a->x, xs * es, a->y, ys * es), a->dim * es, &columns);
   const NormPlan n = norm_plan(a->rows, columns, a->dtype);
   NormParams p{static_cast<const char*>(a->x), static_cast<char*>(a->y), xs * es, ys * es, static_cast<const char*>(a->weight),
-               static_cast<const char*>(a->bias), a->stats, a->rows, (int)a->dim, n.warps, n.split, period_of(xs * es), a->eps};
+               static_cast<const char*>(a->bias), a->stats, a->rows, (int)a->dim, n.warps, n.split, period_of(xs * es), a->eps, norm_patience(n.split)};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool wide = a->param_dtype == IRIS_F32;
   if (a->dtype == IRIS_BF16) return wide ? launch_norm<IRIS_BF16, IRIS_F32>(p, n, mode, st) : launch_norm<IRIS_BF16, IRIS_BF16>(p, n, mode, st);
@@ -830,7 +859,7 @@ extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void
   const NormPlan n = norm_grad_plan(a->rows, columns, a->dtype);
   NormGradParams p{static_cast<const char*>(a->x), static_cast<const char*>(a->dy), static_cast<char*>(a->dx), xs * es, gs * es, ds * es,
                    static_cast<const char*>(a->weight), a->stats, sums ? static_cast<float*>(a->workspace) : nullptr, a->rows, (int)a->dim, n.warps,
-                   n.split, period_of(xs * es), 0};
+                   n.split, period_of(xs * es), 0, norm_patience(n.split)};
   const bool wide = a->param_dtype == IRIS_F32;
   if (a->dtype == IRIS_BF16)
     return wide ? launch_norm_grad<IRIS_BF16, IRIS_F32>(p, n, mode, a->dweight, a->dbias, st) : launch_norm_grad<IRIS_BF16, IRIS_BF16>(p, n, mode, a->dweight, a->dbias, st);
@@ -838,3 +867,19 @@ extern "C" int iris_layer_norm_backward(const iris_layer_norm_grad_args* a, void
     return wide ? launch_norm_grad<IRIS_F16, IRIS_F32>(p, n, mode, a->dweight, a->dbias, st) : launch_norm_grad<IRIS_F16, IRIS_F16>(p, n, mode, a->dweight, a->dbias, st);
   return launch_norm_grad<IRIS_F32, IRIS_F32>(p, n, mode, a->dweight, a->dbias, st);
 }
+
+extern "C" int iris_layer_norm_status(void* stream, int32_t* detail) {
+  int32_t host[kStatusWords];
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  IRIS_CUDA_TRY(cudaMemcpyFromSymbolAsync(host, norm_status, sizeof(host), 0, cudaMemcpyDeviceToHost, st));
+  IRIS_CUDA_TRY(cudaStreamSynchronize(st));
+  if (detail)
+    for (int i = 0; i < kStatusWords; ++i) detail[i] = host[i];
+  if (!host[0]) return IRIS_OK;
+  const int32_t none[kStatusWords] = {};
+  IRIS_CUDA_TRY(cudaMemcpyToSymbolAsync(norm_status, none, sizeof(none), 0, cudaMemcpyHostToDevice, st));
+  IRIS_CUDA_TRY(cudaStreamSynchronize(st));
+  return fail(host[0], "iris_layer_norm: a wait of a block for the others of its rows ran out: kernel=%d block=%d group=%d warp=%d", host[1], host[2], host[3], host[4]);
+}
+
+extern "C" void iris_layer_norm_withhold(int on) { norm_withhold.store(on != 0); }
