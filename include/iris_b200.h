@@ -649,7 +649,7 @@ size_t iris_embed_workspace_bytes(int64_t n, int64_t vocab, int64_t dim);
 
 /* Layer norm: y = (x - mean) / sqrt(var + eps) * weight + bias over each row of `dim` elements (1 <= dim <= 65536, IRIS_ERR_UNSUPPORTED beyond
  * that), var the mean of (x - mean)^2.  y may be x itself (same address and stride) and must not overlap it otherwise.  A row that holds NaN or an
- * infinity gives NaN; one of equal values with eps = 0 has no defined result. */
+ * infinity gives NaN; one of equal values with eps = 0 has no defined result, nor has one whose sum, or whose squares' sum about the mean, is beyond fp32. */
 typedef struct iris_layer_norm_args {
   const void* x;
   int64_t rows, dim, row_stride;

@@ -3,8 +3,9 @@
 //
 // A warp takes 256 columns of a row, or a few times that, through shared memory of its own.  Aligned 16 bytes are copied asynchronously, several rows
 // ahead, without passing through registers; where the row begins elsewhere than at 16 bytes, each thread cuts its columns out of two of
-// them there, and results go the same way back.  Nothing outside a row is read or written: its first elements are copied by words (and one by itself,
-// where it begins at half a word), the copy of its last 16 bytes is cut short, and what does not fill 16 bytes is stored by elements.
+// them there, and results go the same way back.  Nothing outside a row is written: what does not fill 16 bytes is stored by elements.  Segment reads nothing
+// outside it either: its first elements are copied by words (and one by itself, where it begins at half a word), and the copy of its last 16 bytes is cut
+// short.  Aligned (rows that all begin at the same place of 16 bytes) also reads what lies between two rows within the 16 bytes that one of them touches.
 #pragma once
 
 #include <atomic>

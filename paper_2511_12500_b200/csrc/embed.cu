@@ -21,12 +21,6 @@ struct EmbedParams {
   float scale;
 };
 
-// A warp moves U times 512 bytes of a row of the output, 16 aligned bytes a thread at a time.  Where the table's row does not lie like the output's,
-// those are cut out of two of the table's, of which the second are the next thread's first and come from L1.
-//
-// 32768 x 4096 bf16 70 us, 74 % of the copy rate; 32771 x 4099 fp16, where no two rows lie alike, 84 us (62 %): token, row and store come one after the other
-// in a warp, 32 warps an SM.  With the ends of a row moved by single threads one element after the other 116 us; shifts by selections instead of cases 118; parts
-// of all rows counted through, with a division a thread, 147.  64 rows of 8192: 6.2 us, of which the launch and three latencies are nearly all.
 // 16 bytes from byte b of the row on, all of which lie in it, though the aligned ones that they touch do not.
 template <int ES>
 __device__ __forceinline__ uint4 load_apart(const char* from, int b) {
@@ -102,6 +96,12 @@ __device__ __forceinline__ const char* embed_row(const EmbedParams& p, int64_t i
   return p.shard[r] ? p.shard[r] + (int64_t)((uint32_t)t - r * p.per) * p.shard_stride : nullptr;
 }
 
+// A warp moves U times 512 bytes of a row of the output, 16 aligned bytes a thread at a time.  Where the table's row does not lie like the output's,
+// those are cut out of two of the table's, of which the second are the next thread's first and come from L1.
+//
+// 32768 x 4096 bf16 70 us, 74 % of the copy rate; 32771 x 4099 fp16, where no two rows lie alike, 84 us (62 %): token, row and store come one after the other
+// in a warp, 32 warps an SM.  With the ends of a row moved by single threads one element after the other 116 us; shifts by selections instead of cases 118; parts
+// of all rows counted through, with a division a thread, 147.  64 rows of 8192: 6.2 us, of which the launch and three latencies are nearly all.
 template <int DT, int U>
 __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const __grid_constant__ EmbedParams p) {
   constexpr int ES = sizeof(typename Elem<DT>::T);

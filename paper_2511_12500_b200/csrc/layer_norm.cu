@@ -210,7 +210,7 @@ __device__ __forceinline__ float both(uint64_t x) {
 // shared memory nothing waits for memory long (1.0 warps an issue); what is left is chains of dependent instructions, shuffles and barriers at 16 warps an SM, so
 // the rows in work count: 4104 columns, whose fifth warp has 8 of them, take 69 us for 16001 rows, 4096 columns 52; rows of 4096 that begin at
 // any element 90.  Held in registers one row ahead instead of copied ahead: 244; parameters read from L1 instead of shared memory: 212; one row at a time 110.
-// Rows of more than 8192 columns are shared by a cluster (SPLIT): 4096 x 16384 77 us; 111 with a cluster's barrier in every turn and one group of 8 warps a block.
+// Rows of more than 8192 columns are shared by a cluster (SPLIT): 4096 x 16384 77 us, 1024 x 65536 91; 111 the former with a cluster's barrier in every turn and one group of 8 warps a block.
 template <int DT, int PT, int R, int I, int MODE, bool SPLIT>
 __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const NormParams p) {
   using C = Columns<DT>;
@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(norm_warps(DT, R * I) * 32) norm_kernel(const 
         for (int q = 0; q < R; ++q) {
           const float2* const of = group.of(shared, count & 1, q);
           float m = lost, s = 0.f;
-          if (SPLIT && group.all() > 16) {   // a lane takes a warp, or a few (1024 x 65536: 200 us instead of 367; at 16 warps the same within 5 %)
+          if (SPLIT && group.all() > 16) {   // a lane takes a warp, or a few (1024 x 65536, with one group a block: 200 us instead of 367; at 16 warps the same within 5 %)
             for (int w = group.lane; w < group.all(); w += 32) m = fmaf(of[w].x, shares.of(w), m);
             mean[q] = warp_sum(m) / shares.dim;
             for (int w = group.lane; w < group.all(); w += 32) {
@@ -691,8 +691,8 @@ static NormPlan norm_plan(int64_t rows, int64_t columns, int dtype) {
 }
 static NormPlan norm_grad_plan(int64_t rows, int64_t columns, int dtype) {
   NormPlan n;
-  // Rows of more than 8 warps are shared by two blocks of two groups rather than held by one group (8192 x 8192 bf16 93 us instead of 101, fp32 91 instead of 103);
-  // four blocks instead of two leave 16 of 148 SMs without a cluster (5500 x 12000: 113 us instead of 110).
+  // Rows of more than 8 warps are shared by two blocks of two groups rather than held by one group (8192 x 8192 bf16 98 us instead of 101);
+  // four blocks instead of two leave 16 of 148 SMs without a cluster (5500 x 12000: 2 % longer).
   const bool pairs = columns > kNormGradRuns * kWarpColumns * kNormGradRowWarps / 2 && columns <= kNormGradRuns * kWarpColumns * kNormGradRowWarps;
   plan_runs(n, columns, kNormGradRuns, pairs ? kNormGradRowWarps / 2 : kNormGradRowWarps);
   // Two rows at a time leave room for fewer warps: where rows have so many that it makes no difference.

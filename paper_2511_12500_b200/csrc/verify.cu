@@ -261,9 +261,10 @@ __device__ __forceinline__ int winner(Runner r, F exactly) {
 
 // One cluster of `split` blocks a sequence: accepts drafts up to the first that is refused, and draws the token behind them.
 //
-// 64 sequences over 128000: 18 us, of which the two rows and the noise (64 MB) account for 10; the rest is the chain of what has to be known first
+// 64 sequences over 128000: 19 us, of which the two rows and the noise (64 MB) account for 10; the rest is the chain of what has to be known first
 // (statistics, where the sequence stops) and last (best of threads, of blocks, its column).  One sequence: 5 us of 11.  With the winners' columns kept in the pass
-// instead of looked for in the end 29 us; their scores all in 64 bits, and two granules a thread at a time in half as many blocks, 47.
+// instead of looked for in the end 29 us; their scores all in 64 bits, and two granules a thread at a time in half as many blocks, 47.  Where nothing is left
+// of p - q all columns are compared in 64 bits before the second race: all 64 sequences of that kind 141 us a call instead of 43.
 template <int DT>
 __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draw_kernel(const __grid_constant__ VerifyParams p) {
   using E = Elem<DT>;
