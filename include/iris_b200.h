@@ -575,7 +575,8 @@ int iris_distill_topk_backward(const iris_distill_args* args, void* stream);
  *   (from p_i where that leaves nothing), behind the last draft from p.  A sequence's drafts end at the first id outside [0, vocab).
  * Tokens drawn this way are distributed as if the target alone had drawn them.  Drawn by a race: the token with the largest weight / noise, the
  * lowest column among equals, so that with exponential noise (-ln of a uniform number) a token has its weight's probability.  Scores that are too near one
- * another for 32 bits are compared in 64, given the rows' sums; a weight below 2^-126 is 0, noise above 2^126 is infinite.
+ * another for 32 bits are compared in 64, given the rows' sums; a weight below 2^-126 is 0; noise above 2^126 is infinite, and such
+ * below 2^-126 comes before all other.
  * A scale of +inf, or above 2e38, is greedy: p is 1 at the largest logit (the lowest column among equals), drafts are compared with it, and
  * uniform, noise and draft_logits do not matter (with such a scale and no scales they are not read and may be NULL).  A row of target
  * logits with nothing left, or with NaN or +inf, accepts nothing and its next token is -1; a row of draft logits with NaN or +inf rejects its draft, and the next token is drawn from p. */
