@@ -573,6 +573,7 @@ int iris_distill_topk_backward(const iris_distill_args* args, void* stream);
  * b * drafts + i, with the same scale; without draft_logits a drafted token was certain (q_i = 1 there).
  *   Draft i is accepted while u_i q_i(d_i) < p_i(d_i).  At the first place where it is not, the next token is drawn from max(0, p_i - q_i)
  *   (from p_i where that leaves nothing), behind the last draft from p.  A sequence's drafts end at the first id outside [0, vocab).
+ *   Sums over a row are fp32, so p_i - q_i counts as nothing up to 2^-16 of p_i: rows that are the same leave nothing wherever they lie.
  * Tokens drawn this way are distributed as if the target alone had drawn them.  Drawn by a race: the token with the largest weight / noise, the
  * lowest column among equals, so that with exponential noise (-ln of a uniform number) a token has its weight's probability.  Scores that are too near one
  * another for 32 bits are compared in 64, given the rows' sums; a weight below 2^-126 is 0; noise above 2^126 is infinite, and such
